@@ -250,6 +250,83 @@ beagle_status beagle_block_grad(beagle_ctx* ctx, int32_t batch, int32_t S, const
                                 int32_t logits_dtype, const int32_t* target_ids_dev, float vloss_coef, const beagle_grads* grads,
                                 float* loss_out_dev, void* ws_dev, size_t ws_bytes, void* stream);
 
+/* ---- Key/value states in pages, and the attention that reads them ----------------------------------------------------
+ * A cache whose sequences take fixed-size pages from one pool instead of a reserved run each, so that ragged sequences,
+ * forks that share a prefix and sequences longer than any reserved length fit one buffer.  These calls need no context: all
+ * state lies in the caller's device memory and is read and changed on the device only, in stream order, so every call can be
+ * captured and replayed and lengths that only the device knows (an accept_len_dev) need no copy to the host.  Calls on one
+ * cache must be ordered by the caller (one stream, or events).  Slot lists are HOST arrays, at most BEAGLE_MAX_CALL_BATCH
+ * entries, passed by value.
+ *   k, v      [n_pages, n_kv_heads, page_size, head_dim] in the storage type, 16-byte aligned
+ *   table     int32 [max_slots, max_pages]: page of positions [i * page_size, ..) of a slot, -1 = none
+ *   length    int32 [max_slots]: positions the slot holds
+ *   refs      int32 [n_pages]: table entries that name the page (0 = free), 16-byte aligned
+ *   ws        scratch of beagle_pages_workspace_bytes, 16-byte aligned, contents irrelevant between calls
+ * page_size: a power of two, 8..256.  head_dim: bf16 32|64|128|256, fp32 16|32|64|128.  Limits: n_pages * n_kv_heads *
+ * page_size and max_slots * max_pages below 2^31 (CAPACITY).  Entries, lengths and counts outside their range (a damaged
+ * table) never lead to an access outside these buffers.  Positions at and past a slot's length keep what they held. */
+typedef struct beagle_pages {
+    void* k;
+    void* v;
+    int32_t* table;
+    int32_t* length;
+    int32_t* refs;
+    void* ws;
+    size_t ws_bytes;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t dtype;
+    int32_t max_slots;
+    int32_t max_pages;
+} beagle_pages;
+
+beagle_status beagle_pages_workspace_bytes(const beagle_pages* pages, size_t* bytes);    /* reads n_pages only */
+
+/* Every slot empty, every page free (the table, lengths and counts of a new cache). */
+beagle_status beagle_pages_reset(const beagle_pages* pages, void* stream);
+
+/* Appends new rows to `batch` distinct slots: row b takes the first n_new_dev[b] (int32, clamped to [0, T]; NULL = T each)
+ * of its T rows of k_new / v_new ([batch, T, n_kv_heads, head_dim]; the heads of a row are dense, rows k_stride / v_stride
+ * elements apart, e.g. a view of a fused projection; 16-byte aligned rows).  Pages are taken lowest free id first, in the
+ * order of the rows, from the pages free at entry.  A partly filled last page that other slots hold too (at entry) is
+ * copied into a new page first, its filled positions only.  ok_dev int32 [batch] (nullable): 1, or 0 for a row that found
+ * too few free pages or passes max_pages * page_size; such a row is left as it was, and so is every later row that needs a
+ * page when the free pages ran out before it. */
+beagle_status beagle_pages_append(const beagle_pages* pages, int32_t batch, const int32_t* slot_host, int32_t T, const int32_t* n_new_dev,
+                                  const void* k_new_dev, int64_t k_stride, const void* v_new_dev, int64_t v_stride, int32_t* ok_dev, void* stream);
+
+/* Cuts n distinct slots to their first keep_dev[i] positions (int32, clamped to [0, length]; NULL = 0: the slot is freed)
+ * and gives back the pages behind. */
+beagle_status beagle_pages_truncate(const beagle_pages* pages, int32_t n, const int32_t* slot_host, const int32_t* keep_dev, void* stream);
+
+/* Slot dst[i] becomes a fork of slot src[i]: it shares every page (no rows move; the first append to either copies the
+ * partly filled last page).  What dst held is given back.  dst distinct; src may repeat; no slot in both lists. */
+beagle_status beagle_pages_fork(const beagle_pages* pages, int32_t n, const int32_t* src_host, const int32_t* dst_host, void* stream);
+
+/* Slot dst[i] becomes a copy of slot src[i] in pages of its own (lowest free ids, in call order, after what the dst slots
+ * held has been given back).  Whole pages are copied.  ok_dev int32 [n] (nullable): 0 where too few pages were free; such a dst is empty. */
+beagle_status beagle_pages_copy(const beagle_pages* pages, int32_t n, const int32_t* src_host, const int32_t* dst_host, int32_t* ok_dev, void* stream);
+
+/* Moves the live pages to the ids 0 .. live-1: those at or above `live` go to the holes below, both in ascending order; the
+ * table follows.  refs must count the table's entries. */
+beagle_status beagle_pages_compact(const beagle_pages* pages, void* stream);
+
+/* Cross-attention (Eq. 2, lines 2-3) of one query token per row over the pages of its slot; a slot may serve several rows.
+ *   o_h = sum_j softmax_j(<q_h, K_j> / sqrt(head_dim)) V_j   over the visible positions j < n = length[slot]:
+ *   all of them (window 0), or j >= n - window (the newest `window`) and j < sinks (the first few, which stay visible).
+ * q_dev [batch, n_q_heads, head_dim] in the storage type, rows q_stride elements apart; out_dev the same, dense; lse_dev
+ * fp32 [batch, n_q_heads] (nullable): ln sum_j exp(score).  An empty slot gives o = 0 and lse = -inf.  What lies in
+ * positions that are not visible (NaN included) has no effect.  Scores, softmax and sums are fp32; the bf16 kernel rounds
+ * the softmax weights to bf16 for the product with V.  n_q_heads / n_kv_heads: 1..8 (bf16 head_dim 256: 1..4).  ws_dev:
+ * beagle_paged_attn_workspace_bytes, 16-byte aligned, contents irrelevant; two calls that may run at the same time need
+ * two.  Results do not depend on timing.  A kernel that gives up on a bounded wait leaves NaN in the rows concerned. */
+beagle_status beagle_paged_attn_workspace_bytes(const beagle_pages* pages, int32_t n_q_heads, size_t* bytes);
+beagle_status beagle_paged_attn(const beagle_pages* pages, int32_t batch, const int32_t* slot_host, int32_t n_q_heads, const void* q_dev,
+                                int64_t q_stride, int32_t window, int32_t sinks, void* out_dev, float* lse_dev, void* ws_dev,
+                                size_t ws_bytes, void* stream);
+
 /* Greedy acceptance (Section 3: in greedy decoding the draft's and the target's top-1 tokens are
  * matched and only a contiguous prefix is accepted, plus one extra target token).  Exactly one of
  * target_logits_dev ([batch, gamma+1, V], logits_dtype BEAGLE_FP32 or BEAGLE_BF16) and

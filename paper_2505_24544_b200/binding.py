@@ -31,6 +31,8 @@ EXPORTED_SYMBOLS = (
     "beagle_workspace_buffer", "beagle_block_workspace_buffer", "beagle_verify_sample", "beagle_block_loss", "beagle_draft_tree", "beagle_verify_tree_greedy",
     "beagle_block_grad_workspace_bytes", "beagle_block_grad", "beagle_quantize_rows_e4m3",
     "beagle_packed_weights_bytes", "beagle_pack_weights",
+    "beagle_pages_workspace_bytes", "beagle_pages_reset", "beagle_pages_append", "beagle_pages_truncate", "beagle_pages_fork",
+    "beagle_pages_copy", "beagle_pages_compact", "beagle_paged_attn_workspace_bytes", "beagle_paged_attn",
 )
 
 BUFFER_IDS = {"x": 0, "xn": 1, "q": 2, "o": 3, "y": 4, "yn": 5, "act": 6, "h": 7, "kt": 8, "vt": 9, "kp": 10, "vp": 11}
@@ -51,6 +53,11 @@ class BeagleWeights(C.Structure):
 
 class BeagleGrads(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in WEIGHT_NAMES]
+
+
+class BeaglePages(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "table", "length", "refs", "ws")] + [("ws_bytes", C.c_size_t)] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype", "max_slots", "max_pages")]
 
 
 class BeagleError(RuntimeError):
@@ -121,6 +128,20 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.beagle_packed_weights_bytes.restype = C.c_int
     lib.beagle_pack_weights.argtypes = [vp, vp, C.c_size_t, vp]
     lib.beagle_pack_weights.restype = C.c_int
+    pg, i64 = C.POINTER(BeaglePages), C.c_int64
+    lib.beagle_pages_workspace_bytes.argtypes = [pg, szp]
+    lib.beagle_pages_reset.argtypes = [pg, vp]
+    lib.beagle_pages_append.argtypes = [pg, i32, i32p, i32, vp, vp, i64, vp, i64, vp, vp]
+    lib.beagle_pages_truncate.argtypes = [pg, i32, i32p, vp, vp]
+    lib.beagle_pages_fork.argtypes = [pg, i32, i32p, i32p, vp]
+    lib.beagle_pages_copy.argtypes = [pg, i32, i32p, i32p, vp, vp]
+    lib.beagle_pages_compact.argtypes = [pg, vp]
+    lib.beagle_paged_attn_workspace_bytes.argtypes = [pg, i32, szp]
+    lib.beagle_paged_attn.argtypes = [pg, i32, i32p, i32, vp, i64, i32, i32, vp, vp, vp, C.c_size_t, vp]
+    for name in ("workspace_bytes", "reset", "append", "truncate", "fork", "copy", "compact"):
+        getattr(lib, "beagle_pages_" + name).restype = C.c_int
+    lib.beagle_paged_attn_workspace_bytes.restype = C.c_int
+    lib.beagle_paged_attn.restype = C.c_int
     lib.beagle_check_device.argtypes = [vp, vp]
     lib.beagle_check_device.restype = C.c_int
     lib.beagle_selftest_wait_timeout.argtypes = [vp, vp]
@@ -482,6 +503,159 @@ def beagle_profile_read(ctx: Context) -> Dict[str, Tuple[float, int]]:
     ms, cnt = (C.c_float * n)(), (C.c_int32 * n)()
     ctx.check(ctx.lib.beagle_profile_read(ctx.handle, ms, cnt))
     return {ctx.lib.beagle_profile_stage_name(i).decode(): (float(ms[i]), int(cnt[i])) for i in range(n) if cnt[i]}
+
+
+# ---- key/value states in pages -----------------------------------------------------------------
+
+def _check(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], dense: bool = True) -> int:
+    """The tensor's address, after checking its type, shape, layout and that it lies on the current device."""
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: must be on the current CUDA device")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name}: tensor must be contiguous")
+    return t.data_ptr()
+
+
+def _row_stride(name: str, t: torch.Tensor, lead: int) -> int:
+    """Elements between consecutive rows of a tensor whose last two dimensions ([heads, head_dim]) are dense and whose first
+    `lead` dimensions count rows at one distance (a dense tensor, or a slice of a fused projection)."""
+    heads, dh = t.shape[lead:]
+    st = t.stride()
+    if (dh > 1 and st[-1] != 1) or (heads > 1 and st[-2] != dh):
+        raise ValueError(f"{name}: the heads of a row must be dense")
+    if lead == 2 and t.shape[1] > 1:
+        if t.shape[0] > 1 and st[0] != st[1] * t.shape[1]:
+            raise ValueError(f"{name}: rows must lie at one distance")
+        return st[1] if st[1] != 0 else -1
+    return st[0] if t.shape[0] > 1 else max(st[0], heads * dh)
+
+
+class PagedCache:
+    """A key/value cache in pages (``beagle_pages``): the device tensors, owned here, and the structure that names them.
+
+    k, v: [n_pages, n_kv_heads, page_size, head_dim]; table: int32 [max_slots, max_pages] (-1 = none); length: int32
+    [max_slots]; refs: int32 [n_pages].  Use one cache from one stream at a time."""
+
+    def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, max_slots: int, max_pages: int,
+                 dtype: str = "bf16", device="cuda"):
+        dt = torch_dtype({"fp32": BEAGLE_FP32, "bf16": BEAGLE_BF16}[dtype])
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        i32 = dict(dtype=torch.int32, device=device)
+        self._bind(torch.empty(shape, dtype=dt, device=device), torch.empty(shape, dtype=dt, device=device),
+                   torch.empty(max_slots, max_pages, **i32), torch.empty(max_slots, **i32), torch.empty(n_pages, **i32))
+        beagle_pages_reset(self)
+
+    @classmethod
+    def from_tensors(cls, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, length: torch.Tensor, refs: torch.Tensor) -> "PagedCache":
+        """Adopts existing tensors as they are (a cache that was saved, or filled by other code)."""
+        cache = cls.__new__(cls)
+        cache._bind(k, v, table, length, refs)
+        return cache
+
+    def _bind(self, k, v, table, length, refs):
+        if k.dim() != 4 or table.dim() != 2 or k.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("k: [n_pages, n_kv_heads, page_size, head_dim] float32 / bfloat16; table: [max_slots, max_pages]")
+        self.lib = load_library()
+        self.k, self.v, self.table, self.length, self.refs = k, v, table, length, refs
+        p = BeaglePages()
+        p.n_pages, p.n_kv_heads, p.page_size, p.head_dim = k.shape
+        p.max_slots, p.max_pages = table.shape
+        p.dtype = BEAGLE_BF16 if k.dtype == torch.bfloat16 else BEAGLE_FP32
+        for name, t, dt, shape in (("k", k, k.dtype, tuple(k.shape)), ("v", v, k.dtype, tuple(k.shape)), ("table", table, torch.int32, tuple(table.shape)),
+                                   ("length", length, torch.int32, (p.max_slots,)), ("refs", refs, torch.int32, (p.n_pages,))):
+            setattr(p, name, _check(name, t, dt, shape))
+        n = C.c_size_t()
+        _pages_ok(self.lib.beagle_pages_workspace_bytes(C.byref(p), C.byref(n)), "beagle_pages_workspace_bytes")
+        self.ws = torch.empty(n.value, dtype=torch.uint8, device=k.device)
+        p.ws, p.ws_bytes = self.ws.data_ptr(), n.value
+        self.struct, self.ref = p, C.byref(p)
+        self.attn_ws_bytes: Dict[int, int] = {}      # query heads -> workspace of beagle_paged_attn
+
+    def on_current_device(self) -> int:
+        """The current stream, after checking that the cache lies on the current device."""
+        if self.k.device.index != torch.cuda.current_device():
+            raise ValueError("the cache must be on the current CUDA device")
+        return _stream()
+
+
+def _pages_ok(st: int, what: str) -> None:
+    if st != 0:
+        raise BeagleError(st, what)
+
+
+def beagle_pages_reset(cache: PagedCache) -> None:
+    _pages_ok(cache.lib.beagle_pages_reset(cache.ref, cache.on_current_device()), "beagle_pages_reset")
+
+
+def beagle_pages_append(cache: PagedCache, slots: Sequence[int], k_new: torch.Tensor, v_new: torch.Tensor,
+                        n_new: Optional[torch.Tensor] = None, ok: Optional[torch.Tensor] = None) -> None:
+    """k_new, v_new: [len(slots), T, n_kv_heads, head_dim] (views with one row distance are fine); n_new: int32 [len(slots)] rows
+    to take (None: T); ok: int32 [len(slots)], 1 or 0 (too few free pages, or the slot is full: left as it was)."""
+    c, B = cache.struct, len(slots)
+    shape = (B, k_new.shape[1] if k_new.dim() == 4 else -1, c.n_kv_heads, c.head_dim)
+    kp, vp = _check("k_new", k_new, cache.k.dtype, shape, False), _check("v_new", v_new, cache.k.dtype, shape, False)
+    n_ptr = None if n_new is None else _check("n_new", n_new, torch.int32, (B,))
+    ok_ptr = None if ok is None else _check("ok", ok, torch.int32, (B,))
+    _pages_ok(cache.lib.beagle_pages_append(cache.ref, B, _i32_array(slots), shape[1], n_ptr, kp, _row_stride("k_new", k_new, 2), vp,
+                                            _row_stride("v_new", v_new, 2), ok_ptr, cache.on_current_device()), "beagle_pages_append")
+
+
+def beagle_pages_truncate(cache: PagedCache, slots: Sequence[int], keep: Optional[torch.Tensor] = None) -> None:
+    """Cuts the slots to ``keep`` positions (int32 on the device; None: frees them)."""
+    keep_ptr = None if keep is None else _check("keep", keep, torch.int32, (len(slots),))
+    _pages_ok(cache.lib.beagle_pages_truncate(cache.ref, len(slots), _i32_array(slots), keep_ptr, cache.on_current_device()), "beagle_pages_truncate")
+
+
+def _pairs(src: Sequence[int], dst: Sequence[int]):
+    if len(src) != len(dst):
+        raise ValueError("src and dst must have the same length")
+    return len(src), _i32_array(src), _i32_array(dst)
+
+
+def beagle_pages_fork(cache: PagedCache, src: Sequence[int], dst: Sequence[int]) -> None:
+    n, s, d = _pairs(src, dst)
+    _pages_ok(cache.lib.beagle_pages_fork(cache.ref, n, s, d, cache.on_current_device()), "beagle_pages_fork")
+
+
+def beagle_pages_copy(cache: PagedCache, src: Sequence[int], dst: Sequence[int], ok: Optional[torch.Tensor] = None) -> None:
+    n, s, d = _pairs(src, dst)
+    ok_ptr = None if ok is None else _check("ok", ok, torch.int32, (n,))
+    _pages_ok(cache.lib.beagle_pages_copy(cache.ref, n, s, d, ok_ptr, cache.on_current_device()), "beagle_pages_copy")
+
+
+def beagle_pages_compact(cache: PagedCache) -> None:
+    _pages_ok(cache.lib.beagle_pages_compact(cache.ref, cache.on_current_device()), "beagle_pages_compact")
+
+
+def beagle_paged_attn_workspace_bytes(cache: PagedCache, n_q_heads: int) -> int:
+    n = cache.attn_ws_bytes.get(n_q_heads)
+    if n is None:
+        v = C.c_size_t()
+        _pages_ok(cache.lib.beagle_paged_attn_workspace_bytes(cache.ref, n_q_heads, C.byref(v)), "beagle_paged_attn_workspace_bytes")
+        n = cache.attn_ws_bytes[n_q_heads] = v.value
+    return n
+
+
+def beagle_paged_attn(cache: PagedCache, slots: Sequence[int], q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                      window: int = 0, sinks: int = 0, ws: Optional[torch.Tensor] = None) -> None:
+    """One query token per row over its slot's pages.  q: [len(slots), n_q_heads, head_dim] (rows may be strided); out: the same,
+    dense; lse: fp32 [len(slots), n_q_heads].  window 0: every position; else the newest ``window`` and the first ``sinks``.
+    ws: scratch of ``beagle_paged_attn_workspace_bytes`` (None: taken from torch's allocator for this call)."""
+    c, B = cache.struct, len(slots)
+    if q.dim() != 3:
+        raise ValueError("q: [batch, n_q_heads, head_dim]")
+    hq = q.shape[1]
+    qp = _check("q", q, cache.k.dtype, (B, hq, c.head_dim), False)
+    op = _check("out", out, cache.k.dtype, (B, hq, c.head_dim))
+    lp = None if lse is None else _check("lse", lse, torch.float32, (B, hq))
+    stream = cache.on_current_device()
+    need = beagle_paged_attn_workspace_bytes(cache, hq)
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _pages_ok(cache.lib.beagle_paged_attn(cache.ref, B, _i32_array(slots), hq, qp, _row_stride("q", q, 1), window, sinks, op, lp,
+                                          ws.data_ptr(), ws.numel() * ws.element_size(), stream), "beagle_paged_attn")
 
 
 # ---- convenience wrapper -----------------------------------------------------------------------

@@ -1,0 +1,136 @@
+"""Refusals of the paged-cache entry points: all are found on the host before anything is launched (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+OK, INVALID, SHAPE, CAPACITY = 0, 1, 2, 3
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2505_24544_b200 import build
+    from paper_2505_24544_b200.binding import load_library
+    build.build()
+    return load_library()
+
+
+def pages(lib, **kw):
+    from paper_2505_24544_b200.binding import BeaglePages
+    p = BeaglePages()
+    base = dict(k=1 << 20, v=2 << 20, table=3 << 20, length=4 << 20, refs=5 << 20, ws=6 << 20, n_pages=40, page_size=16, n_kv_heads=2, head_dim=64,
+                dtype=1, max_slots=4, max_pages=8)
+    base.update(kw)
+    for n, x in base.items():
+        setattr(p, n, x)
+    n = C.c_size_t()
+    if "ws_bytes" not in kw:
+        lib.beagle_pages_workspace_bytes(C.byref(p), C.byref(n))
+        p.ws_bytes = n.value
+    return p
+
+
+def arr(*v):
+    return (C.c_int32 * max(1, len(v)))(*v)
+
+
+def test_structure_matches_header():
+    from paper_2505_24544_b200.binding import BeaglePages
+    assert C.sizeof(BeaglePages) == 7 * 8 + 7 * 4 + 4            # six pointers, one size, seven int32, tail padding
+
+
+def test_workspace_bytes(lib):
+    p = pages(lib)
+    n = C.c_size_t()
+    assert lib.beagle_pages_workspace_bytes(C.byref(p), C.byref(n)) == OK and n.value % 256 == 0 and n.value >= 40 * 12
+    assert lib.beagle_pages_workspace_bytes(None, C.byref(n)) == INVALID
+    assert lib.beagle_pages_workspace_bytes(C.byref(p), None) == INVALID
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 8, C.byref(n)) == OK and n.value > 0
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 0, C.byref(n)) == INVALID
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 3, C.byref(n)) == SHAPE             # not a multiple of the K/V heads
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 18, C.byref(n)) == SHAPE            # nine grouped heads
+
+
+@pytest.mark.parametrize("kw, want", [
+    (dict(k=0), INVALID), (dict(v=0), INVALID), (dict(table=0), INVALID), (dict(length=0), INVALID), (dict(refs=0), INVALID), (dict(ws=0), INVALID),
+    (dict(k=8 + (1 << 20)), INVALID), (dict(refs=4 + (1 << 20)), INVALID), (dict(table=2 + (1 << 20)), INVALID),
+    (dict(n_pages=0), INVALID), (dict(n_kv_heads=0), INVALID), (dict(max_slots=0), INVALID), (dict(max_pages=-1), INVALID), (dict(dtype=2), INVALID),
+    (dict(page_size=4), SHAPE), (dict(page_size=24), SHAPE), (dict(page_size=512), SHAPE), (dict(head_dim=48), SHAPE),
+    (dict(head_dim=256, dtype=0), SHAPE), (dict(head_dim=16, dtype=1), SHAPE),
+    (dict(ws_bytes=16), CAPACITY), (dict(n_pages=1 << 27), CAPACITY), (dict(max_slots=1 << 29), CAPACITY), (dict(max_pages=1 << 27), CAPACITY),
+])
+def test_bad_cache(lib, kw, want):
+    p = C.byref(pages(lib, **kw))
+    one, q = arr(0), 1 << 21
+    assert lib.beagle_pages_reset(p, None) == want
+    assert lib.beagle_pages_append(p, 1, one, 1, None, q, 128, q, 128, None, None) == want
+    assert lib.beagle_pages_truncate(p, 1, one, None, None) == want
+    assert lib.beagle_pages_fork(p, 1, one, arr(1), None) == want
+    assert lib.beagle_pages_copy(p, 1, one, arr(1), None, None) == want
+    assert lib.beagle_pages_compact(p, None) == want
+    assert lib.beagle_paged_attn(p, 1, one, 4, q, 256, 0, 0, q, None, q, 1 << 30, None) == want
+
+
+def test_bad_slots(lib):
+    p = C.byref(pages(lib))
+    q = 1 << 21
+    many = arr(*range(65))
+    for bad, want in ((arr(4), INVALID), (arr(-1), INVALID), (None, INVALID)):
+        assert lib.beagle_pages_append(p, 1, bad, 1, None, q, 128, q, 128, None, None) == want
+        assert lib.beagle_pages_truncate(p, 1, bad, None, None) == want
+        assert lib.beagle_pages_fork(p, 1, bad, arr(1), None) == want
+        assert lib.beagle_pages_fork(p, 1, arr(1), bad, None) == want
+        assert lib.beagle_pages_copy(p, 1, bad, arr(1), None, None) == want
+        assert lib.beagle_paged_attn(p, 1, bad, 4, q, 256, 0, 0, q, None, q, 1 << 30, None) == want
+    twice = arr(1, 1)
+    assert lib.beagle_pages_append(p, 2, twice, 1, None, q, 128, q, 128, None, None) == INVALID
+    assert lib.beagle_pages_truncate(p, 2, twice, None, None) == INVALID
+    assert lib.beagle_pages_fork(p, 2, arr(0, 0), twice, None) == INVALID
+    assert lib.beagle_pages_fork(p, 2, arr(0, 1), arr(1, 2), None) == INVALID           # a slot in both lists
+    assert lib.beagle_pages_copy(p, 1, arr(2), arr(2), None, None) == INVALID
+    assert lib.beagle_pages_append(p, 65, many, 1, None, q, 128, q, 128, None, None) == CAPACITY
+    assert lib.beagle_paged_attn(p, 65, many, 4, q, 256, 0, 0, q, None, q, 1 << 30, None) == CAPACITY
+    assert lib.beagle_pages_truncate(p, -1, arr(0), None, None) == INVALID
+    # nothing to do
+    assert lib.beagle_pages_append(p, 0, None, 1, None, None, 0, None, 0, None, None) == OK
+    assert lib.beagle_pages_truncate(p, 0, None, None, None) == OK
+    assert lib.beagle_pages_fork(p, 0, None, None, None) == OK
+    assert lib.beagle_paged_attn(p, 0, None, 4, None, 0, 0, 0, None, None, None, 0, None) == OK
+
+
+def test_bad_rows(lib):
+    p = C.byref(pages(lib))
+    q, one = 1 << 21, arr(0)
+    for a in ((None, 128, q, 128), (q, 128, None, 128), (q + 8, 128, q, 128), (q, 127, q, 128), (q, 132, q, 128), (q, 128, q, 64)):
+        assert lib.beagle_pages_append(p, 1, one, 1, None, *a, None, None) == INVALID
+    assert lib.beagle_pages_append(p, 1, one, -1, None, q, 128, q, 128, None, None) == INVALID
+    assert lib.beagle_pages_append(p, 1, one, 0x7fffffff, None, q, 128, q, 128, None, None) == CAPACITY
+    big = 1 << 30
+    for hq, qp, st, w, k, o, ws, n, want in (
+            (4, None, 256, 0, 0, q, q, big, INVALID), (4, q, 255, 0, 0, q, q, big, INVALID), (4, q, 260, 0, 0, q, q, big, INVALID),
+            (4, q, 256, -1, 0, q, q, big, INVALID), (4, q, 256, 0, -1, q, q, big, INVALID), (4, q, 256, 0, 0, None, q, big, INVALID),
+            (4, q, 256, 0, 0, q, None, big, INVALID), (4, q + 2, 256, 0, 0, q, q, big, INVALID), (4, q, 256, 0, 0, q, q, 64, CAPACITY),
+            (5, q, 512, 0, 0, q, q, big, SHAPE), (18, q, 2048, 0, 0, q, q, big, SHAPE)):
+        assert lib.beagle_paged_attn(p, 1, one, hq, qp, st, w, k, o, None, ws, n, None) == want
+    wide = C.byref(pages(lib, head_dim=256))
+    assert lib.beagle_paged_attn(wide, 1, one, 16, q, 4096, 0, 0, q, None, q, big, None) == SHAPE
+
+
+def test_binding_checks_tensors():
+    """The binding refuses tensors on another device, of another type or shape before the library sees their addresses."""
+    torch = pytest.importorskip("torch")
+    from paper_2505_24544_b200 import binding as b
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    i32 = dict(dtype=torch.int32)
+    with pytest.raises(ValueError):
+        b.PagedCache.from_tensors(k, k.clone(), torch.zeros(2, 3, **i32), torch.zeros(2, **i32), torch.zeros(4, **i32))       # host tensors
+    with pytest.raises(ValueError):
+        b.PagedCache.from_tensors(k.half(), k.half(), torch.zeros(2, 3, **i32), torch.zeros(2, **i32), torch.zeros(4, **i32))
+    x = torch.zeros(3, 5, 4, 8)
+    assert b._row_stride("x", x, 2) == 32
+    fused = torch.zeros(3, 5, 96)
+    assert b._row_stride("x", fused[:, :, 32:64].unflatten(2, (4, 8)), 2) == 96
+    assert b._row_stride("x", fused[:, :1, 32:64].unflatten(2, (4, 8)), 2) == 480
+    with pytest.raises(ValueError):
+        b._row_stride("x", fused[:, :4, 32:64].unflatten(2, (4, 8)), 2)
+    with pytest.raises(ValueError):
+        b._row_stride("x", x.transpose(2, 3), 2)
