@@ -327,6 +327,50 @@ beagle_status beagle_paged_attn(const beagle_pages* pages, int32_t batch, const 
                                 int64_t q_stride, int32_t window, int32_t sinks, void* out_dev, float* lse_dev, void* ws_dev,
                                 size_t ws_bytes, void* stream);
 
+/* ---- Attention over whole sequences with a sliding window and sinks, forward and backward ---------------------------
+ * The training and prompt form of beagle_paged_attn's window.  `batch` sequences (at most BEAGLE_MAX_CALL_BATCH) lie one
+ * after the other: sequence b has q_len_host[b] query rows and kv_len_host[b] key / value rows (HOST arrays, any length from
+ * 0; the packed matrices have the sums).  The ends are aligned: query i of a sequence sees the keys
+ *     j <= last = i + kv_len - q_len - strict,   with   j > last - window   or   j < sinks
+ * (window 0: no lower bound).  strict 0: its own position is the newest key; strict 1: strictly earlier ones (Section 4.2's
+ * Mask_{i,j} = 0 for j >= i).  A query that sees nothing has o = 0, lse = -inf and no gradient; a key that nobody sees has
+ * gradient 0.  q_dev [.., n_q_heads, head_dim], k_dev and v_dev [.., n_kv_heads, head_dim] in the storage type, the heads of a
+ * row dense, rows *_stride elements apart (slices of a fused projection are fine; rows 16-byte aligned).
+ * n_q_heads a multiple of n_kv_heads; head_dim 64 | 128, fp32 also 16 | 32; with a window sinks <= 1024; at most 2^27 rows.
+ * Scores, softmax, statistics and sums are fp32; the bf16 kernels round the softmax weights and dS to bf16 for their products.
+ * Keys and values of a sequence must be finite; rows of other sequences and rows behind the last one are never mixed in and
+ * outputs behind the last row are left as they were.  Results do not depend on timing. */
+typedef struct beagle_window_attn {
+    const void* q_dev;
+    const void* k_dev;
+    const void* v_dev;
+    int64_t q_stride;
+    int64_t k_stride;
+    int64_t v_stride;
+    const int32_t* q_len_host;
+    const int32_t* kv_len_host;
+    int32_t batch;
+    int32_t dtype;
+    int32_t n_q_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t window;
+    int32_t sinks;
+    int32_t strict;
+} beagle_window_attn;
+
+/* out_dev: like q, dense; lse_dev fp32 [rows, n_q_heads] (nullable): ln sum_j exp(score), needed by the backward pass. */
+beagle_status beagle_window_attn_forward(const beagle_window_attn* attn, void* out_dev, float* lse_dev, void* stream);
+
+/* Gradients of sum(out * dout): dq like q, dk like k, dv like v, every row overwritten, with row strides of their own; the
+ * query heads that share a K/V head are summed (in fp32, in a fixed order).  out_dev and lse_dev are the forward's.  ws_dev:
+ * beagle_window_attn_workspace_bytes (the pointers of `attn` are not read), 256-byte aligned, contents irrelevant; two calls
+ * that may run at the same time need two. */
+beagle_status beagle_window_attn_workspace_bytes(const beagle_window_attn* attn, size_t* bytes);
+beagle_status beagle_window_attn_backward(const beagle_window_attn* attn, const void* out_dev, const float* lse_dev, const void* dout_dev,
+                                          int64_t dout_stride, void* dq_dev, int64_t dq_stride, void* dk_dev, int64_t dk_stride,
+                                          void* dv_dev, int64_t dv_stride, void* ws_dev, size_t ws_bytes, void* stream);
+
 /* Greedy acceptance (Section 3: in greedy decoding the draft's and the target's top-1 tokens are
  * matched and only a contiguous prefix is accepted, plus one extra target token).  Exactly one of
  * target_logits_dev ([batch, gamma+1, V], logits_dtype BEAGLE_FP32 or BEAGLE_BF16) and

@@ -33,6 +33,7 @@ EXPORTED_SYMBOLS = (
     "beagle_packed_weights_bytes", "beagle_pack_weights",
     "beagle_pages_workspace_bytes", "beagle_pages_reset", "beagle_pages_append", "beagle_pages_truncate", "beagle_pages_fork",
     "beagle_pages_copy", "beagle_pages_compact", "beagle_paged_attn_workspace_bytes", "beagle_paged_attn",
+    "beagle_window_attn_forward", "beagle_window_attn_workspace_bytes", "beagle_window_attn_backward",
 )
 
 BUFFER_IDS = {"x": 0, "xn": 1, "q": 2, "o": 3, "y": 4, "yn": 5, "act": 6, "h": 7, "kt": 8, "vt": 9, "kp": 10, "vp": 11}
@@ -58,6 +59,12 @@ class BeagleGrads(C.Structure):
 class BeaglePages(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "table", "length", "refs", "ws")] + [("ws_bytes", C.c_size_t)] + \
                [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype", "max_slots", "max_pages")]
+
+
+class BeagleWindowAttn(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_dev", "k_dev", "v_dev")] + [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + \
+               [(n, C.POINTER(C.c_int32)) for n in ("q_len_host", "kv_len_host")] + \
+               [(n, C.c_int32) for n in ("batch", "dtype", "n_q_heads", "n_kv_heads", "head_dim", "window", "sinks", "strict")]
 
 
 class BeagleError(RuntimeError):
@@ -141,6 +148,12 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     for name in ("workspace_bytes", "reset", "append", "truncate", "fork", "copy", "compact"):
         getattr(lib, "beagle_pages_" + name).restype = C.c_int
     lib.beagle_paged_attn_workspace_bytes.restype = C.c_int
+    wa = C.POINTER(BeagleWindowAttn)
+    lib.beagle_window_attn_forward.argtypes = [wa, vp, vp, vp]
+    lib.beagle_window_attn_workspace_bytes.argtypes = [wa, szp]
+    lib.beagle_window_attn_backward.argtypes = [wa, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, C.c_size_t, vp]
+    for name in ("forward", "workspace_bytes", "backward"):
+        getattr(lib, "beagle_window_attn_" + name).restype = C.c_int
     lib.beagle_paged_attn.restype = C.c_int
     lib.beagle_check_device.argtypes = [vp, vp]
     lib.beagle_check_device.restype = C.c_int
@@ -656,6 +669,59 @@ def beagle_paged_attn(cache: PagedCache, slots: Sequence[int], q: torch.Tensor, 
         ws = torch.empty(need, dtype=torch.uint8, device=q.device)
     _pages_ok(cache.lib.beagle_paged_attn(cache.ref, B, _i32_array(slots), hq, qp, _row_stride("q", q, 1), window, sinks, op, lp,
                                           ws.data_ptr(), ws.numel() * ws.element_size(), stream), "beagle_paged_attn")
+
+
+# ---- attention over whole sequences with a window and sinks -------------------------------------
+
+def _window_attn(q, k, v, q_len, kv_len, window, sinks, strict) -> Tuple[BeagleWindowAttn, int]:
+    """The call's structure (its length arrays kept alive by it) and the current stream, after checking the tensors."""
+    if q.dim() != 3 or k.dim() != 3 or q.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("q: [rows, n_q_heads, head_dim], k and v: [rows, n_kv_heads, head_dim], float32 / bfloat16")
+    if len(q_len) != len(kv_len):
+        raise ValueError("q_len and kv_len must have the same length")
+    nq, hq, dh = q.shape
+    nk, hkv = k.shape[:2]
+    if nq != sum(q_len) or nk != sum(kv_len):
+        raise ValueError("q, k and v must have as many rows as the sequences")
+    w = BeagleWindowAttn()
+    w.q_dev = _check("q", q, q.dtype, (nq, hq, dh), False)
+    w.k_dev = _check("k", k, q.dtype, (nk, hkv, dh), False)
+    w.v_dev = _check("v", v, q.dtype, (nk, hkv, dh), False)
+    w.q_stride, w.k_stride, w.v_stride = _row_stride("q", q, 1), _row_stride("k", k, 1), _row_stride("v", v, 1)
+    w.q_len_host, w.kv_len_host = _i32_array(q_len), _i32_array(kv_len)
+    w.batch, w.dtype = len(q_len), BEAGLE_BF16 if q.dtype == torch.bfloat16 else BEAGLE_FP32
+    w.n_q_heads, w.n_kv_heads, w.head_dim = hq, hkv, dh
+    w.window, w.sinks, w.strict = window, sinks, int(strict)
+    return w, _stream()
+
+
+def beagle_window_attn_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_len: Sequence[int], kv_len: Sequence[int], out: torch.Tensor,
+                               lse: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0, strict: bool = False) -> None:
+    """Causal attention of packed sequences (q: [sum(q_len), n_q_heads, head_dim]; k, v: [sum(kv_len), n_kv_heads, head_dim]; rows may be
+    strided), ends aligned; window 0: every earlier key, else the newest ``window`` and the first ``sinks``; strict: without the
+    query's own position.  out: like q, dense; lse: fp32 [rows, n_q_heads], which the backward pass needs."""
+    w, stream = _window_attn(q, k, v, q_len, kv_len, window, sinks, strict)
+    op = _check("out", out, q.dtype, tuple(q.shape))
+    lp = None if lse is None else _check("lse", lse, torch.float32, tuple(q.shape[:2]))
+    _pages_ok(load_library().beagle_window_attn_forward(C.byref(w), op, lp, stream), "beagle_window_attn_forward")
+
+
+def beagle_window_attn_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                                q_len: Sequence[int], kv_len: Sequence[int], dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, window: int = 0,
+                                sinks: int = 0, strict: bool = False, ws: Optional[torch.Tensor] = None) -> None:
+    """Gradients of sum(out * dout) for the forward's out and lse; dq, dk, dv like q, k, v (rows may be strided), overwritten.
+    ws: scratch of ``beagle_window_attn_workspace_bytes`` (None: taken from torch's allocator for this call)."""
+    w, stream = _window_attn(q, k, v, q_len, kv_len, window, sinks, strict)
+    qs, ks = tuple(q.shape), tuple(k.shape)
+    op, lp = _check("out", out, q.dtype, qs), _check("lse", lse, torch.float32, qs[:2])
+    ptr = {n: (_check(n, t, q.dtype, s, False), _row_stride(n, t, 1)) for n, t, s in (("dout", dout, qs), ("dq", dq, qs), ("dk", dk, ks), ("dv", dv, ks))}
+    lib = load_library()
+    if ws is None:
+        n = C.c_size_t()
+        _pages_ok(lib.beagle_window_attn_workspace_bytes(C.byref(w), C.byref(n)), "beagle_window_attn_workspace_bytes")
+        ws = torch.empty(n.value, dtype=torch.uint8, device=q.device)
+    _pages_ok(lib.beagle_window_attn_backward(C.byref(w), op, lp, *ptr["dout"], *ptr["dq"], *ptr["dk"], *ptr["dv"], ws.data_ptr(),
+                                              ws.numel() * ws.element_size(), stream), "beagle_window_attn_backward")
 
 
 # ---- convenience wrapper -----------------------------------------------------------------------

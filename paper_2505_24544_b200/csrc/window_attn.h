@@ -1,0 +1,58 @@
+// Shared pieces of the windowed attention kernels (beagle_window_attn_*).  Internal to the library.
+#pragma once
+#include "../../include/beagle.h"
+#include "common.cuh"
+
+namespace beagle {
+
+// The sequences of one call, by value in the kernel parameters.  Query i of sequence b sees the keys
+//     j <= last(i) = i + shift[b]   with   j > last(i) - window   or   j < sinks,     shift = kv_len - q_len - strict.
+struct WinSeqs {
+    int32_t q_start[kMaxCallBatch], k_start[kMaxCallBatch];      // first packed row
+    int32_t q_len[kMaxCallBatch], kv_len[kMaxCallBatch];
+    int32_t item[kMaxCallBatch + 1];                             // prefix sum of the launch's tiles per sequence
+};
+
+struct WinArgs {
+    int32_t batch, Hq, Hkv, G, window, sinks, strict;            // window: "none" is kNoWindow
+    float scale, scale_log2;
+    const void *q, *k, *v, *out, *dout;
+    const float* lse;
+    long long q_stride, k_stride, v_stride, dout_stride, dq_stride, dk_stride, dv_stride;
+    void *o, *dq, *dk, *dv;
+    float* lse_out;
+    float2* stats;                                               // [Hq][stat_rows]: log-sum-exp (log2 units) and delta of every query
+    float* sink_part;                                            // fp32 partials of the sinks' dK, dV
+    int32_t stat_rows;                                           // sum over the sequences of q_len padded to kStatPad
+    int32_t sink_rows, sink_tiles, sink_segs;                    // layout of sink_part, see window_attn_bwd.cu
+};
+constexpr int kNoWindow = 0x3fffffff;
+constexpr int kStatPad = 128;
+constexpr int kQTile = 128;              // queries of one tile
+constexpr int kKTile = 128;              // keys of one tile of the key side
+
+struct WinPlan;                          // tensor maps etc. of the bf16 kernels
+
+// Which sequence a linear item belongs to (the item's index inside it in `in`).
+__device__ __forceinline__ int win_find(const int32_t* item, int batch, int at, int& in) {
+    int b = 0;
+    while (b + 1 < batch && at >= item[b + 1]) ++b;
+    in = at - item[b];
+    return b;
+}
+
+// 32-bit visibility of columns [0, 32) of a chunk: bits [lo, hi).
+__device__ __forceinline__ uint32_t bit_range(int lo, int hi) {
+    lo = max(lo, 0);
+    hi = min(hi, 32);
+    if (hi <= lo) return 0u;
+    return (0xffffffffu >> (32 - (hi - lo))) << lo;
+}
+
+// host side
+int window_fwd_bf16(const WinArgs& a, const WinSeqs& s, int dh, long long q_rows, long long k_rows, cudaStream_t stream);
+int window_bwd_bf16(const WinArgs& a, const WinSeqs& s, int dh, long long q_rows, long long k_rows, cudaStream_t stream);
+int window_fwd_fp32(const WinArgs& a, const WinSeqs& s, int dh, cudaStream_t stream);
+int window_bwd_fp32(const WinArgs& a, const WinSeqs& s, int dh, cudaStream_t stream);
+
+}  // namespace beagle

@@ -1,0 +1,379 @@
+// The windowed attention in fp32 (forward and backward), head_dim 16 | 32 | 64 | 128, on the CUDA cores: the tiny head's type,
+// for which exactness counts more than rate (no tensor-core product keeps 24 bits).
+//
+// Tiles of 64 queries x 64 keys; 256 threads as 16 x 16, each with a 4 x 4 piece of S (operands read as 16-byte vectors from
+// padded shared-memory rows, 64 fused multiply-adds per 8 loads) and with its 4 rows x head_dim / 16 columns of the accumulators.
+// The 16 threads of a row are half a warp, so row maxima, sums and the hand-over of P through shared memory need no CTA barrier.
+// Backward as in the bf16 kernels: a query side (dQ, and delta) and a key side (dK, dV); the key side gives every query head its
+// own CTA and, where heads share keys, leaves fp32 partials that a last launch adds in the order of the heads.
+#include "window_attn.h"
+
+namespace beagle {
+namespace {
+
+constexpr int kT = 64;                   // queries, and keys, of a tile
+constexpr int kPad = 4;
+constexpr int kThreads = 256;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+template <int DH> __host__ __device__ constexpr int row_len() { return DH + kPad; }
+constexpr int kPRow = kT + kPad;
+
+__device__ __forceinline__ bool visible(int key, int last, const WinArgs& a) { return key <= last && (key > last - a.window || key < a.sinks); }
+
+// Rows [r0, r0 + 64) of a packed matrix (column offset `col`) into shared memory; rows at and past `rows` as zero.
+template <int DH>
+__device__ __forceinline__ void load_tile(float* dst, const float* src, long long stride, int r0, int rows, size_t col) {
+    for (int i = threadIdx.x; i < kT * (DH / 4); i += kThreads) {
+        const int r = i / (DH / 4), c = i % (DH / 4);
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r0 + r < rows) x = *reinterpret_cast<const float4*>(src + (size_t)(r0 + r) * stride + col + 4 * c);
+        *reinterpret_cast<float4*>(dst + r * row_len<DH>() + 4 * c) = x;
+    }
+}
+// acc[r][c] = <A row (4 ty + r), B row (tx + 16 c)>
+template <int DH>
+__device__ __forceinline__ void dots(const float* A, const float* B, int ty, int tx, float acc[4][4]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[r][c] = 0.f;
+#pragma unroll 4
+    for (int d = 0; d < DH; d += 4) {
+        float4 x[4], y[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = *reinterpret_cast<const float4*>(A + (4 * ty + r) * row_len<DH>() + d);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = *reinterpret_cast<const float4*>(B + (tx + 16 * c) * row_len<DH>() + d);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                acc[r][c] = fmaf(x[r].x, y[c].x, fmaf(x[r].y, y[c].y, fmaf(x[r].z, y[c].z, fmaf(x[r].w, y[c].w, acc[r][c]))));
+    }
+}
+// acc[r][e] += sum_k P[4 ty + r][k] X[k][tx + 16 e]
+template <int DH>
+__device__ __forceinline__ void weigh(const float* P, const float* X, int ty, int tx, float acc[4][DH / 16]) {
+#pragma unroll 2
+    for (int k = 0; k < kT; k += 4) {
+        float p[4][4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float4 t = *reinterpret_cast<const float4*>(P + (4 * ty + r) * kPRow + k);
+            p[r][0] = t.x; p[r][1] = t.y; p[r][2] = t.z; p[r][3] = t.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < DH / 16; ++e) {
+                const float x = X[(k + i) * row_len<DH>() + tx + 16 * e];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[r][e] = fmaf(p[r][i], x, acc[r][e]);
+            }
+    }
+}
+__device__ __forceinline__ void put(float* P, int ty, int tx, const float v[4][4]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) P[(4 * ty + r) * kPRow + tx + 16 * c] = v[r][c];
+}
+
+// The key tiles of the queries [q0, q0 + 64): sinks in front of the window, then the band.
+struct Keys {
+    int lo, hi, sink_end, n_sink, n;
+    __device__ __forceinline__ void init(int q0, int q_len, int shift, const WinArgs& a) {
+        hi = min(q0 + kT, q_len) + shift;
+        lo = max(0, q0 + shift - a.window + 1);
+        sink_end = min(a.sinks, lo);
+        n_sink = (sink_end + kT - 1) / kT;
+        n = hi > 0 ? n_sink + (hi - lo + kT - 1) / kT : 0;
+    }
+    __device__ __forceinline__ void tile(int j, int& start, int& end) const {
+        if (j < n_sink) { start = j * kT; end = min(start + kT, sink_end); }
+        else { start = lo + (j - n_sink) * kT; end = min(start + kT, hi); }
+    }
+};
+
+template <int DH>
+__global__ void __launch_bounds__(kThreads) window_fwd_fp32_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
+    extern __shared__ __align__(16) float sm[];
+    float *Q = sm, *K = Q + kT * row_len<DH>(), *V = K + kT * row_len<DH>(), *P = V + kT * row_len<DH>();
+    int tile;
+    const int b = win_find(seqs.item, a.batch, blockIdx.x, tile);
+    const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
+    const int q0 = ((q_len + kT - 1) / kT - 1 - tile) * kT, h = blockIdx.y, kvh = h / a.G;
+    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    load_tile<DH>(Q, static_cast<const float*>(a.q) + (size_t)seqs.q_start[b] * a.q_stride, a.q_stride, q0, q_len, (size_t)h * DH);
+    Keys w;
+    w.init(q0, q_len, shift, a);
+    float o[4][DH / 16], m[4], l[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        m[r] = -INFINITY; l[r] = 0.f;
+#pragma unroll
+        for (int e = 0; e < DH / 16; ++e) o[r][e] = 0.f;
+    }
+    for (int j = 0; j < w.n; ++j) {
+        int start, end;
+        w.tile(j, start, end);
+        __syncthreads();                                 // the previous tile has been read
+        load_tile<DH>(K, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, start, end, (size_t)kvh * DH);
+        load_tile<DH>(V, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, start, end, (size_t)kvh * DH);
+        __syncthreads();
+        float s[4][4];
+        dots<DH>(Q, K, ty, tx, s);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int last = q0 + 4 * ty + r + shift;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int key = start + tx + 16 * c;
+                s[r][c] = (key < end && visible(key, last, a)) ? s[r][c] * a.scale_log2 : -INFINITY;
+                mx = fmaxf(mx, s[r][c]);
+            }
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+            mx = fmaxf(mx, m[r]);
+            const float f = m[r] == -INFINITY ? 1.f : exp2f(m[r] - mx);
+            const float neg = mx == -INFINITY ? 0.f : -mx;
+            m[r] = mx;
+            l[r] *= f;
+#pragma unroll
+            for (int e = 0; e < DH / 16; ++e) o[r][e] *= f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                s[r][c] = exp2f(s[r][c] + neg);
+                l[r] += s[r][c];
+            }
+        }
+        put(P, ty, tx, s);
+        __syncwarp();                                    // a row's 16 threads are half of one warp
+        weigh<DH>(P, V, ty, tx, o);
+        __syncwarp();
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+        const int i = q0 + 4 * ty + r;
+        if (i >= q_len) continue;
+        const size_t row = ((size_t)(seqs.q_start[b] + i) * a.Hq + h);
+        const float inv = l[r] > 0.f ? __fdiv_rn(1.f, l[r]) : 0.f;
+#pragma unroll
+        for (int e = 0; e < DH / 16; ++e) static_cast<float*>(a.o)[row * DH + tx + 16 * e] = o[r][e] * inv;
+        if (tx == 0 && a.lse_out != nullptr) a.lse_out[row] = l[r] > 0.f ? (m[r] + log2f(l[r])) * kLn2 : -INFINITY;
+    }
+}
+
+__device__ __forceinline__ int stat_row0(const WinSeqs& s, int b) {
+    int at = 0;
+    for (int i = 0; i < b; ++i) at += (s.q_len[i] + kStatPad - 1) / kStatPad * kStatPad;
+    return at;
+}
+
+template <int DH>
+__global__ void __launch_bounds__(kThreads) window_bwd_q_fp32_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
+    extern __shared__ __align__(16) float sm[];
+    float *Q = sm, *dO = Q + kT * row_len<DH>(), *K = dO + kT * row_len<DH>(), *V = K + kT * row_len<DH>(), *P = V + kT * row_len<DH>();
+    int tile;
+    const int b = win_find(seqs.item, a.batch, blockIdx.x, tile);
+    const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
+    const int q0 = ((q_len + kT - 1) / kT - 1 - tile) * kT, h = blockIdx.y, kvh = h / a.G;
+    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    load_tile<DH>(Q, static_cast<const float*>(a.q) + (size_t)seqs.q_start[b] * a.q_stride, a.q_stride, q0, q_len, (size_t)h * DH);
+    load_tile<DH>(dO, static_cast<const float*>(a.dout) + (size_t)seqs.q_start[b] * a.dout_stride, a.dout_stride, q0, q_len, (size_t)h * DH);
+    __syncthreads();
+    float lse2[4], delta[4], dq[4][DH / 16];
+    const int stat0 = stat_row0(seqs, b);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = q0 + 4 * ty + r;
+        const size_t row = (size_t)(seqs.q_start[b] + min(i, q_len - 1)) * a.Hq + h;
+        float t = 0.f;
+#pragma unroll
+        for (int e = 0; e < DH / 16; ++e) {
+            t = fmaf(dO[(4 * ty + r) * row_len<DH>() + tx + 16 * e], static_cast<const float*>(a.out)[row * DH + tx + 16 * e], t);
+            dq[r][e] = 0.f;
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+        const bool sees = i + shift >= 0;
+        delta[r] = sees ? t : 0.f;
+        lse2[r] = sees ? a.lse[row] * kLog2e : 0.f;
+        if (tx == 0 && i < q_len) a.stats[(size_t)h * a.stat_rows + stat0 + i] = make_float2(lse2[r], delta[r]);
+    }
+    Keys w;
+    w.init(q0, q_len, shift, a);
+    for (int j = 0; j < w.n; ++j) {
+        int start, end;
+        w.tile(j, start, end);
+        __syncthreads();
+        load_tile<DH>(K, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, start, end, (size_t)kvh * DH);
+        load_tile<DH>(V, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, start, end, (size_t)kvh * DH);
+        __syncthreads();
+        float s[4][4], dp[4][4];
+        dots<DH>(Q, K, ty, tx, s);
+        dots<DH>(dO, V, ty, tx, dp);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int last = q0 + 4 * ty + r + shift;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int key = start + tx + 16 * c;
+                s[r][c] = (key < end && visible(key, last, a)) ? exp2f(fmaf(s[r][c], a.scale_log2, -lse2[r])) * (dp[r][c] - delta[r]) : 0.f;
+            }
+        }
+        put(P, ty, tx, s);
+        __syncwarp();
+        weigh<DH>(P, K, ty, tx, dq);
+        __syncwarp();
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = q0 + 4 * ty + r;
+        if (i >= q_len) continue;
+#pragma unroll
+        for (int e = 0; e < DH / 16; ++e)
+            static_cast<float*>(a.dq)[(size_t)(seqs.q_start[b] + i) * a.dq_stride + (size_t)h * DH + tx + 16 * e] = dq[r][e] * a.scale;
+    }
+}
+
+// One CTA = 64 keys of one (sequence, query head).  a.sink_part (when heads share keys): fp32 [kv rows][Hq][2][DH], dV then dK.
+template <int DH>
+__global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
+    extern __shared__ __align__(16) float sm[];
+    float *K = sm, *V = K + kT * row_len<DH>(), *Q = V + kT * row_len<DH>(), *dO = Q + kT * row_len<DH>(), *P = dO + kT * row_len<DH>(), *dS = P + kT * kPRow;
+    int tile;
+    const int b = win_find(seqs.item, a.batch, blockIdx.x, tile);
+    const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
+    const int k0 = tile * kT, h = blockIdx.y, kvh = h / a.G;
+    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+    load_tile<DH>(K, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, k0, kv_len, (size_t)kvh * DH);
+    load_tile<DH>(V, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, k0, kv_len, (size_t)kvh * DH);
+    const int from = max(0, k0 - shift);
+    const int to = k0 < a.sinks ? q_len : max(0, min(q_len, min(k0 + kT, kv_len) - 1 - shift + a.window));
+    const float2* stats = a.stats + (size_t)h * a.stat_rows + stat_row0(seqs, b);
+    float dk[4][DH / 16], dv[4][DH / 16];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int e = 0; e < DH / 16; ++e) dk[r][e] = dv[r][e] = 0.f;
+    for (int q0 = from; q0 < to; q0 += kT) {
+        __syncthreads();
+        load_tile<DH>(Q, static_cast<const float*>(a.q) + (size_t)seqs.q_start[b] * a.q_stride, a.q_stride, q0, q_len, (size_t)h * DH);
+        load_tile<DH>(dO, static_cast<const float*>(a.dout) + (size_t)seqs.q_start[b] * a.dout_stride, a.dout_stride, q0, q_len, (size_t)h * DH);
+        __syncthreads();
+        float s[4][4], dp[4][4];
+        dots<DH>(K, Q, ty, tx, s);
+        dots<DH>(V, dO, ty, tx, dp);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int i = q0 + tx + 16 * c;
+            const float2 t = i < q_len ? __ldg(stats + i) : make_float2(0.f, 0.f);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool vis = i < q_len && visible(k0 + 4 * ty + r, i + shift, a);
+                const float p = vis ? exp2f(fmaf(s[r][c], a.scale_log2, -t.x)) : 0.f;
+                s[r][c] = p;
+                dp[r][c] = vis ? p * (dp[r][c] - t.y) : 0.f;
+            }
+        }
+        put(P, ty, tx, s);
+        put(dS, ty, tx, dp);
+        __syncwarp();
+        weigh<DH>(P, dO, ty, tx, dv);
+        weigh<DH>(dS, Q, ty, tx, dk);
+        __syncwarp();
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int key = k0 + 4 * ty + r;
+        if (key >= kv_len) continue;
+        const size_t row = (size_t)(seqs.k_start[b] + key);
+#pragma unroll
+        for (int e = 0; e < DH / 16; ++e) {
+            const int c = tx + 16 * e;
+            if (a.G > 1) {
+                float* part = a.sink_part + (row * a.Hq + h) * 2 * DH;
+                part[c] = dv[r][e];
+                part[DH + c] = dk[r][e] * a.scale;
+            } else {
+                static_cast<float*>(a.dv)[row * a.dv_stride + (size_t)kvh * DH + c] = dv[r][e];
+                static_cast<float*>(a.dk)[row * a.dk_stride + (size_t)kvh * DH + c] = dk[r][e] * a.scale;
+            }
+        }
+    }
+}
+
+// dK, dV of one key row: the query heads of every group added in order.
+__global__ void __launch_bounds__(256) window_group_join_fp32_kernel(const __grid_constant__ WinArgs a, int DH, long long rows) {
+    const long long n = rows * a.Hkv * 2 * DH;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const int c = (int)(i % (2 * DH));
+        const long long rest = i / (2 * DH);
+        const int kvh = (int)(rest % a.Hkv);
+        const long long row = rest / a.Hkv;
+        const float* p = a.sink_part + ((size_t)row * a.Hq + (size_t)kvh * a.G) * 2 * DH + c;
+        float x = 0.f;
+        for (int g = 0; g < a.G; ++g) x += p[(size_t)g * 2 * DH];
+        if (c < DH) static_cast<float*>(a.dv)[(size_t)row * a.dv_stride + (size_t)kvh * DH + c] = x;
+        else static_cast<float*>(a.dk)[(size_t)row * a.dk_stride + (size_t)kvh * DH + c - DH] = x;
+    }
+}
+
+void retile(WinSeqs& s, int batch, const int32_t* len) {
+    s.item[0] = 0;
+    for (int b = 0; b < batch; ++b) s.item[b + 1] = s.item[b] + (len[b] + kT - 1) / kT;
+}
+
+template <int DH>
+int fwd(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
+    constexpr int bytes = (3 * kT * row_len<DH>() + kT * kPRow) * 4;
+    static PerDeviceOnce attr;
+    if (!attr.ensure([] { return cudaFuncSetAttribute(window_fwd_fp32_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess; })) return -1;
+    retile(s, a.batch, s.q_len);
+    window_fwd_fp32_kernel<DH><<<dim3(s.item[a.batch], a.Hq), kThreads, bytes, stream>>>(a, s);
+    return 1;
+}
+
+template <int DH>
+int bwd(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
+    constexpr int bytes_q = (4 * kT * row_len<DH>() + kT * kPRow) * 4, bytes_k = (4 * kT * row_len<DH>() + 2 * kT * kPRow) * 4;
+    static PerDeviceOnce attr;
+    if (!attr.ensure([] {
+            return cudaFuncSetAttribute(window_bwd_q_fp32_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes_q) == cudaSuccess &&
+                   cudaFuncSetAttribute(window_bwd_kv_fp32_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes_k) == cudaSuccess;
+        }))
+        return -1;
+    int launched = 0;
+    retile(s, a.batch, s.q_len);
+    if (s.item[a.batch] > 0) {
+        window_bwd_q_fp32_kernel<DH><<<dim3(s.item[a.batch], a.Hq), kThreads, bytes_q, stream>>>(a, s);
+        ++launched;
+    }
+    retile(s, a.batch, s.kv_len);
+    if (s.item[a.batch] > 0) {
+        window_bwd_kv_fp32_kernel<DH><<<dim3(s.item[a.batch], a.Hq), kThreads, bytes_k, stream>>>(a, s);
+        ++launched;
+        if (a.G > 1) {
+            const long long rows = (long long)s.k_start[a.batch - 1] + s.kv_len[a.batch - 1], n = rows * a.Hkv * 2 * DH;
+            window_group_join_fp32_kernel<<<dim3((unsigned)((n + 255) / 256 < 148 * 8 ? (n + 255) / 256 : 148 * 8)), 256, 0, stream>>>(a, DH, rows);
+            ++launched;
+        }
+    }
+    return launched;
+}
+
+}  // namespace
+
+int window_fwd_fp32(const WinArgs& a, const WinSeqs& s, int dh, cudaStream_t stream) {
+    return dh == 128 ? fwd<128>(a, s, stream) : dh == 64 ? fwd<64>(a, s, stream) : dh == 32 ? fwd<32>(a, s, stream) : fwd<16>(a, s, stream);
+}
+int window_bwd_fp32(const WinArgs& a, const WinSeqs& s, int dh, cudaStream_t stream) {
+    return dh == 128 ? bwd<128>(a, s, stream) : dh == 64 ? bwd<64>(a, s, stream) : dh == 32 ? bwd<32>(a, s, stream) : bwd<16>(a, s, stream);
+}
+
+}  // namespace beagle
