@@ -9,13 +9,48 @@ namespace tc {
 
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// The product with its A operand in tensor memory: rows are lanes, a column holds two consecutive bf16 of the contraction.
-__device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+// One lane of a converged warp, the same one every time.  The roles that issue asynchronous work run with all 32 lanes and let
+// this one issue: addresses and descriptors then stay in uniform registers, where a branch of a single lane has to move
+// every operand of every instruction there (measured: the issue of eight products 550-750 -> 100-200 cycles).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) { return mbar_wait(bar, parity, abort_flag); }
+// A warp's bounded wait: true for every lane, or false for every lane.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    bool ok = mbar_try_wait(bar, parity);
+    if (!__all_sync(0xffffffffu, ok)) ok = __all_sync(0xffffffffu, ok || mbar_wait_slow(bar, parity, abort_flag));
+    else ok = true;
+    return ok;
+}
+
+// Products and commits of a converged warp, issued by its elected lane (a predicate, not a branch).
+__device__ __forceinline__ void umma_ss(bool leader, uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(tmem_d), "r"(tmem_a), "l"(db), "r"(idesc), "r"(accumulate)
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate), "r"((uint32_t)leader)
+        : "memory");
+}
+// A operand in tensor memory: rows are lanes, a column holds two consecutive bf16 of the contraction.
+__device__ __forceinline__ void umma_ts(bool leader, uint32_t tmem_d, uint32_t tmem_a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "l"(db), "r"(idesc), "r"(accumulate), "r"((uint32_t)leader)
+        : "memory");
+}
+__device__ __forceinline__ void commit_el(bool leader, uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"((uint32_t)leader)
         : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
@@ -35,6 +70,58 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&t);
 }
+// Two fp32 values in one 64-bit register and the packed arithmetic on them (one issue slot for two operations).
+__device__ __forceinline__ uint64_t pk2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void un2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.ftz.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// 2^x of two values on the multiply-add pipe, for x in [-125, 127] (clamped from below), beside the special-function unit that
+// serves four lanes a cycle: x = n + f with n the nearest integer (the addition of 1.5 * 2^23 leaves it in the low mantissa
+// bits), 2^f on [-1/2, 1/2] by the degree-5 polynomial of least largest relative error (Remez exchange, 7.5e-8; 2.4e-7 in
+// fp32 arithmetic), n added to the exponent.
+__device__ __forceinline__ void exp2_poly2(uint64_t x, float& e0, float& e1) {
+    float a, b;
+    un2(x, a, b);
+    x = pk2(fmaxf(a, -125.f), fmaxf(b, -125.f));
+    const uint64_t t = add2(x, pk2(12582912.f, 12582912.f));
+    const uint64_t f = fma2(add2(t, pk2(-12582912.f, -12582912.f)), pk2(-1.f, -1.f), x);
+    uint64_t p = pk2(0x1.5c08e6p-10f, 0x1.5c08e6p-10f);
+    p = fma2(p, f, pk2(0x1.3d0c52p-7f, 0x1.3d0c52p-7f));
+    p = fma2(p, f, pk2(0x1.c6b6e4p-5f, 0x1.c6b6e4p-5f));
+    p = fma2(p, f, pk2(0x1.ebf918p-3f, 0x1.ebf918p-3f));
+    p = fma2(p, f, pk2(0x1.62e428p-1f, 0x1.62e428p-1f));
+    p = fma2(p, f, pk2(0x1.000002p+0f, 0x1.000002p+0f));
+    float t0, t1, p0, p1;
+    un2(t, t0, t1);
+    un2(p, p0, p1);
+    e0 = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
+    e1 = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
+}
+// The pairs of columns (x, x + 1) of a 32-column chunk that take the polynomial: POLY of every eight pairs.
+template <int POLY>
+__device__ __forceinline__ constexpr bool poly_pair(int x) { return (x >> 1) % 8 * POLY / 8 != ((x >> 1) % 8 + 1) * POLY / 8; }
 // Zeroes rows [from, to) of an operand tile of `rows` rows x DH bf16 (64-column blocks of rows * 128 bytes; whole rows, so the
 // swizzle inside a row does not matter).  One warp.
 template <int DH>

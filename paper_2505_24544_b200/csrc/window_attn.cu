@@ -61,7 +61,7 @@ Layout layout(const beagle_window_attn* w, const WinArgs& a, const WinSeqs& s, l
         most_kv = s.kv_len[b] > most_kv ? s.kv_len[b] : most_kv;
     }
     L.stat_rows = (int)rows;
-    size_t off = ((size_t)a.Hq * rows * sizeof(float2) + 255) / 256 * 256;
+    size_t off = ((size_t)a.Hq * rows * 2 * sizeof(float) + 255) / 256 * 256;
     L.part = off;
     const size_t d = w->head_dim;
     if (w->dtype == BEAGLE_FP32) {
@@ -155,7 +155,7 @@ beagle_status beagle_window_attn_backward(const beagle_window_attn* w, const voi
     a.q_stride = w->q_stride; a.k_stride = w->k_stride; a.v_stride = w->v_stride;
     a.dout_stride = dout_stride; a.dq_stride = dq_stride; a.dk_stride = dk_stride; a.dv_stride = dv_stride;
     a.dq = dq_dev; a.dk = dk_dev; a.dv = dv_dev;
-    a.stats = reinterpret_cast<float2*>(static_cast<char*>(ws_dev) + L.stats);
+    a.stats = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.stats);
     a.sink_part = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.part);
     a.stat_rows = L.stat_rows; a.sink_rows = L.sink_rows; a.sink_tiles = L.sink_tiles; a.sink_segs = L.sink_segs;
     const cudaStream_t cs = static_cast<cudaStream_t>(stream);

@@ -21,7 +21,7 @@ struct WinArgs {
     long long q_stride, k_stride, v_stride, dout_stride, dq_stride, dk_stride, dv_stride;
     void *o, *dq, *dk, *dv;
     float* lse_out;
-    float2* stats;                                               // [Hq][stat_rows]: log-sum-exp (log2 units) and delta of every query
+    float* stats;                                                // [Hq][2][stat_rows]: -log-sum-exp (log2 units), and -delta, of every query
     float* sink_part;                                            // fp32 partials of the sinks' dK, dV
     int32_t stat_rows;                                           // sum over the sequences of q_len padded to kStatPad
     int32_t sink_rows, sink_tiles, sink_segs;                    // layout of sink_part, see window_attn_bwd.cu

@@ -203,7 +203,11 @@ __global__ void __launch_bounds__(kThreads) window_bwd_q_fp32_kernel(const __gri
         const bool sees = i + shift >= 0;
         delta[r] = sees ? t : 0.f;
         lse2[r] = sees ? a.lse[row] * kLog2e : 0.f;
-        if (tx == 0 && i < q_len) a.stats[(size_t)h * a.stat_rows + stat0 + i] = make_float2(lse2[r], delta[r]);
+        if (tx == 0 && i < q_len) {
+            float* stat = a.stats + (size_t)h * 2 * a.stat_rows + stat0 + i;
+            stat[0] = -lse2[r];
+            stat[a.stat_rows] = -delta[r];
+        }
     }
     Keys w;
     w.init(q0, q_len, shift, a);
@@ -255,7 +259,7 @@ __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __gr
     load_tile<DH>(V, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, k0, kv_len, (size_t)kvh * DH);
     const int from = max(0, k0 - shift);
     const int to = k0 < a.sinks ? q_len : max(0, min(q_len, min(k0 + kT, kv_len) - 1 - shift + a.window));
-    const float2* stats = a.stats + (size_t)h * a.stat_rows + stat_row0(seqs, b);
+    const float* stats = a.stats + (size_t)h * 2 * a.stat_rows + stat_row0(seqs, b);
     float dk[4][DH / 16], dv[4][DH / 16];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -272,13 +276,13 @@ __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __gr
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const int i = q0 + tx + 16 * c;
-            const float2 t = i < q_len ? __ldg(stats + i) : make_float2(0.f, 0.f);
+            const float nl = i < q_len ? __ldg(stats + i) : 0.f, nd = i < q_len ? __ldg(stats + a.stat_rows + i) : 0.f;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const bool vis = i < q_len && visible(k0 + 4 * ty + r, i + shift, a);
-                const float p = vis ? exp2f(fmaf(s[r][c], a.scale_log2, -t.x)) : 0.f;
+                const float p = vis ? exp2f(fmaf(s[r][c], a.scale_log2, nl)) : 0.f;
                 s[r][c] = p;
-                dp[r][c] = vis ? p * (dp[r][c] - t.y) : 0.f;
+                dp[r][c] = vis ? p * (dp[r][c] + nd) : 0.f;
             }
         }
         put(P, ty, tx, s);
