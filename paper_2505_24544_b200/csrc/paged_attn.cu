@@ -614,18 +614,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
     }
 }
 
-int sm_count() {
-    static std::atomic<int> counts[PerDeviceOnce::kMaxDevices];
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= PerDeviceOnce::kMaxDevices) return 148;
-    n = counts[dev].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
-        counts[dev].store(n, std::memory_order_relaxed);
-    }
-    return n;
-}
-
 constexpr int kMaxRuns = 2048;           // bound of the workspace; the grid is min(this, CTAs that fit the GPU)
 constexpr int kSimtCtasPerSm = 4;
 
@@ -672,6 +660,18 @@ beagle_status check_heads(const beagle_pages* p, int Hq) {
 
 }  // namespace
 
+int device_sm_count() {
+    static std::atomic<int> counts[PerDeviceOnce::kMaxDevices];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= PerDeviceOnce::kMaxDevices) return 148;
+    n = counts[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
+        counts[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
 EncodeTiled tensor_map_encoder() {
     static std::atomic<void*> cached{nullptr};
     void* fn = cached.load(std::memory_order_acquire);
@@ -695,7 +695,7 @@ beagle_status beagle_paged_attn_workspace_bytes(const beagle_pages* p, int32_t n
     if (!pages_valid_shape(p)) return BEAGLE_ERR_SHAPE;
     const beagle_status st = check_heads(p, n_q_heads);
     if (st != BEAGLE_OK) return st;
-    const int sms = sm_count(), per = (p->dtype == BEAGLE_BF16 && (p->head_dim == 64 || p->head_dim == 128)) ? kCtasPerSm : kSimtCtasPerSm;
+    const int sms = device_sm_count(), per = (p->dtype == BEAGLE_BF16 && (p->head_dim == 64 || p->head_dim == 128)) ? kCtasPerSm : kSimtCtasPerSm;
     const int runs = sms * per < kMaxRuns ? sms * per : kMaxRuns;
     *bytes = ((size_t)2 * runs * 8 * (p->head_dim + 2) * sizeof(float) + 255) / 256 * 256;
     return BEAGLE_OK;
@@ -738,7 +738,7 @@ beagle_status beagle_paged_attn(const beagle_pages* p, int32_t batch, const int3
     // no more runs than the cache's capacity has tiles
     const long long most = (long long)batch * p->n_kv_heads * (((long long)p->max_pages * p->page_size + kTile - 1) / kTile);
     const bool mma = p->dtype == BEAGLE_BF16 && (p->head_dim == 64 || p->head_dim == 128);
-    long long runs = (long long)sm_count() * (mma ? kCtasPerSm : kSimtCtasPerSm);
+    long long runs = (long long)device_sm_count() * (mma ? kCtasPerSm : kSimtCtasPerSm);
     if (runs > kMaxRuns) runs = kMaxRuns;
     if (runs > most) runs = most;
     if (mma) st = p->head_dim == 128 ? launch_mma<128>(p, a, (int)runs, stream) : launch_mma<64>(p, a, (int)runs, stream);

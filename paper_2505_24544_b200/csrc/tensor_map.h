@@ -1,4 +1,4 @@
-// The driver's tensor-map encoder for entry points that need no context.  Internal to the library.
+// What entry points without a context ask of the device: the driver's tensor-map encoder, the SM count.  Internal to the library.
 #pragma once
 #include <cuda.h>
 
@@ -8,5 +8,6 @@ typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, v
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 EncodeTiled tensor_map_encoder();       // NULL when the driver has none
+int device_sm_count();                  // of the current device (148 when there is none to ask)
 
 }  // namespace beagle

@@ -26,6 +26,13 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     return ok;
 }
 
+// Both waits, their first tests in flight together (a test that succeeds takes some hundred cycles).
+__device__ __forceinline__ bool warp_wait2(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1, volatile int* abort_flag) {
+    const uint32_t a = mbar_try_wait(bar0, parity0), b = mbar_try_wait(bar1, parity1);
+    if (__all_sync(0xffffffffu, a & b)) return true;
+    return warp_wait(bar0, parity0, abort_flag) && warp_wait(bar1, parity1, abort_flag);
+}
+
 // Products and commits of a converged warp, issued by its elected lane (a predicate, not a branch).
 __device__ __forceinline__ void umma_ss(bool leader, uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -97,31 +104,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.ftz.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// 2^x of two values on the multiply-add pipe, for x in [-125, 127] (clamped from below), beside the special-function unit that
-// serves four lanes a cycle: x = n + f with n the nearest integer (the addition of 1.5 * 2^23 leaves it in the low mantissa
-// bits), 2^f on [-1/2, 1/2] by the degree-5 polynomial of least largest relative error (Remez exchange, 7.5e-8; 2.4e-7 in
-// fp32 arithmetic), n added to the exponent.
-__device__ __forceinline__ void exp2_poly2(uint64_t x, float& e0, float& e1) {
-    float a, b;
-    un2(x, a, b);
-    x = pk2(fmaxf(a, -125.f), fmaxf(b, -125.f));
-    const uint64_t t = add2(x, pk2(12582912.f, 12582912.f));
-    const uint64_t f = fma2(add2(t, pk2(-12582912.f, -12582912.f)), pk2(-1.f, -1.f), x);
-    uint64_t p = pk2(0x1.5c08e6p-10f, 0x1.5c08e6p-10f);
-    p = fma2(p, f, pk2(0x1.3d0c52p-7f, 0x1.3d0c52p-7f));
-    p = fma2(p, f, pk2(0x1.c6b6e4p-5f, 0x1.c6b6e4p-5f));
-    p = fma2(p, f, pk2(0x1.ebf918p-3f, 0x1.ebf918p-3f));
-    p = fma2(p, f, pk2(0x1.62e428p-1f, 0x1.62e428p-1f));
-    p = fma2(p, f, pk2(0x1.000002p+0f, 0x1.000002p+0f));
-    float t0, t1, p0, p1;
-    un2(t, t0, t1);
-    un2(p, p0, p1);
-    e0 = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
-    e1 = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
-}
-// The pairs of columns (x, x + 1) of a 32-column chunk that take the polynomial: POLY of every eight pairs.
-template <int POLY>
-__device__ __forceinline__ constexpr bool poly_pair(int x) { return (x >> 1) % 8 * POLY / 8 != ((x >> 1) % 8 + 1) * POLY / 8; }
 // Zeroes rows [from, to) of an operand tile of `rows` rows x DH bf16 (64-column blocks of rows * 128 bytes; whole rows, so the
 // swizzle inside a row does not matter).  One warp.
 template <int DH>

@@ -13,7 +13,10 @@
 //               S^T = K Q^T -> P^T over S^T -> dV += P^T dO, and dP^T = V dO^T -> dS^T over dP^T -> dK += dS^T Q.  The two
 //               halves take turns: while the threads form P of the next tile, dK and the next dP^T run, while they form dS,
 //               dV and the next S^T run.
-// Both use all 512 columns of tensor memory and about 200 KB of shared memory (one CTA per SM, two threads per tile row).
+// Both use all 512 columns of tensor memory and about 200 KB of shared memory: one CTA per SM, two threads per tile row.  The
+// grid is one CTA per SM and walks the items, the pipeline running on across them: the copies and the first products of an item
+// start under the last products and the epilogue of the one before it (as CTAs of their own, items of five tiles spent 7 us of 16
+// on starting up and draining).
 // P and dS are the tensor-memory operands of their products (rows = lanes), so the accumulating products read one operand
 // from shared memory, and Q, dO, K tiles serve both as K-major and as MN-major operands: nothing is copied or transposed.
 //
@@ -36,7 +39,6 @@ namespace {
 using namespace tc;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kPoly = 3;                 // of every eight pairs of exponentials, those on the multiply-add pipe
 
 
 __device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
@@ -62,52 +64,43 @@ __device__ __forceinline__ void store_row32(uint32_t taddr, float scale, bf16* d
     }
 }
 
-// 32 columns of a tile: P = exp2(S * scale - lse), kept as fp32 in r (masked: 0 where `vis` has no bit).  nl(x) gives the negated
-// log-sum-exp of columns x, x + 1.
-template <bool MASK, typename NegLse>
-__device__ __forceinline__ void chunk_p(uint32_t* r, uint32_t vis, uint64_t scale2, NegLse nl) {
+// The element-wise parts are written once, for whole tiles: masked scores become -inf beforehand, so their P is exactly 0, and
+// the rows behind a sequence are zeroed in shared memory, so that dP is finite wherever P is 0 and dS = 0 follows.  (A second,
+// masked copy of the unrolled code cost more in instruction fetches than its absence does in selects.)
+__device__ __forceinline__ void mask32(uint32_t* r, uint32_t vis) {
+#pragma unroll
+    for (int x = 0; x < 32; ++x) r[x] = (vis >> x & 1u) ? r[x] : 0xff800000u;
+}
+// 32 columns of a tile: P = exp2(S * scale - lse), kept as fp32 in r.  nl(x) gives the negated log-sum-exp of columns x, x + 1.
+template <typename NegLse>
+__device__ __forceinline__ void chunk_p(uint32_t* r, uint64_t scale2, NegLse nl) {
 #pragma unroll
     for (int x = 0; x < 32; x += 2) {
         float e0, e1;
-        const uint64_t z = fma2(pk2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), scale2, nl(x));
-        if (!MASK && poly_pair<kPoly>(x)) {
-            exp2_poly2(z, e0, e1);
-        } else {
-            un2(z, e0, e1);
-            e0 = exp2f(e0);
-            e1 = exp2f(e1);
-        }
-        if (MASK) {
-            e0 = (vis >> x & 1u) ? e0 : 0.f;
-            e1 = (vis >> (x + 1) & 1u) ? e1 : 0.f;
-        }
-        r[x] = __float_as_uint(e0);
-        r[x + 1] = __float_as_uint(e1);
+        un2(fma2(pk2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), scale2, nl(x)), e0, e1);
+        r[x] = __float_as_uint(exp2f(e0));
+        r[x + 1] = __float_as_uint(exp2f(e1));
     }
 }
-// dS = P * (dP - delta) of 32 columns as bf16 pairs; a masked pair's dP and delta may hold anything: its dS is 0.
-template <bool MASK, typename NegDelta>
+// dS = P * (dP - delta) of 32 columns as bf16 pairs.
+template <typename NegDelta>
 __device__ __forceinline__ void chunk_ds(const uint32_t* p, const uint32_t* d, NegDelta nd, uint32_t* y) {
 #pragma unroll
     for (int x = 0; x < 32; x += 2) {
-        const float p0 = __uint_as_float(p[x]), p1 = __uint_as_float(p[x + 1]);
         float d0, d1;
-        un2(mul2(pk2(p0, p1), add2(pk2(__uint_as_float(d[x]), __uint_as_float(d[x + 1])), nd(x))), d0, d1);
-        if (MASK) {
-            d0 = p0 == 0.f ? 0.f : d0;
-            d1 = p1 == 0.f ? 0.f : d1;
-        }
+        un2(mul2(pk2(__uint_as_float(p[x]), __uint_as_float(p[x + 1])), add2(pk2(__uint_as_float(d[x]), __uint_as_float(d[x + 1])), nd(x))), d0, d1);
         y[x >> 1] = pack_bf16(d0, d1);
     }
 }
 
 // ---------------------------------------------------------------------------------------------------------------- query side
-constexpr int kThreads = 320;            // warp 0: TMA producer, warp 1: MMA issuer, warps 2-9: two threads per tile row, 64 columns each
+// warp 0: TMA producer, warp 1: MMA issuer, warps 2-9: two threads per tile row, 64 columns each; query side: warps 10, 11 form delta
+constexpr int kThreads = 320, kQThreads = 384;
 
 template <int DH>
 struct BwdQSmem {
-    static constexpr int kT = kQTile * DH * 2;           // Q, dO, and a K or V tile (two stages of each)
-    static constexpr int kBytes = 6 * kT + 2 * kQTile * 4 + 256;
+    static constexpr int kT = kQTile * DH * 2;           // Q, dO, and a K or V tile (three stages of K, one of V)
+    static constexpr int kBytes = 6 * kT + 4 * kQTile * 4 + 256;
 };
 
 // The key tiles of one query tile: sinks [0, sink_end) first, then the band [lo, hi).
@@ -126,40 +119,56 @@ struct KeyWalk {
     }
 };
 
+// The items of a persistent grid: round after round, every other one backwards, so that neighbours in cost spread over the CTAs.
+__device__ __forceinline__ int item_at(int round) {
+    const int c = (round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    return round * gridDim.x + c;
+}
+
+struct QItem {                           // 128 queries of one (sequence, query head)
+    int b, h, q0, q_len, kv_len, shift, q_row, k_row;
+    KeyWalk w;
+    __device__ __forceinline__ void load(int at, const WinArgs& a, const WinSeqs& s) {
+        const int tiles = s.item[a.batch];
+        int tile;
+        h = at / tiles;
+        b = win_find(s.item, a.batch, at - h * tiles, tile);
+        q_len = s.q_len[b];
+        kv_len = s.kv_len[b];
+        shift = kv_len - q_len - a.strict;
+        q0 = ((q_len + kQTile - 1) / kQTile - 1 - tile) * kQTile;            // the latest (longest) tiles first
+        q_row = s.q_start[b] + q0;
+        k_row = s.k_start[b];
+        w.init(q0, q_len, shift, a.window, a.sinks);
+    }
+};
+
 template <int DH>
-__global__ void __launch_bounds__(kThreads, 1) window_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmdO,
+__global__ void __launch_bounds__(kQThreads, 1) window_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmdO,
                                                                  const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                                                                  const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
     using SM = BwdQSmem<DH>;
     constexpr int kHalves = DH / 64;
     constexpr uint32_t kTmem = 512, kDP = 256, kDQ = 384;    // S / dS at columns 0 and 128, dP at 256, dQ at 384
     extern __shared__ __align__(1024) uint8_t smem[];
-    const uint32_t sQ = smem_u32(smem), sdO = sQ + SM::kT, sKV = sdO + SM::kT;       // stage s: K at sKV + 2 s kT, V behind it
-    float* s_delta = reinterpret_cast<float*>(smem + 6 * SM::kT);                    // [2][128]: the two halves of dO . O
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 6 * SM::kT + 2 * kQTile * 4);
+    const uint32_t sQ = smem_u32(smem), sdO = sQ + SM::kT, sV = sdO + SM::kT, sK = sV + SM::kT;     // stage s of K at sK + s kT
+    float* s_stat = reinterpret_cast<float*>(smem + 6 * SM::kT);                     // [2][2][128]: -lse (log2 units) and -delta, two items
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 6 * SM::kT + 4 * kQTile * 4);
     const uint32_t bar0 = smem_u32(bars);
-    const uint32_t q_full = bar0, dp_full = bar0 + 8, ds_full = bar0 + 16, dq_done = bar0 + 24, k_full = bar0 + 32, k_empty = bar0 + 48, k_fixed = bar0 + 64,
-                   s_full = bar0 + 80, v_full = bar0 + 96, v_empty = bar0 + 112;         // the last six: one per stage
-    uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(bars + 20);
-    volatile int* s_abort = reinterpret_cast<int*>(bars + 21);
+    const uint32_t q_full = bar0, dp_full = bar0 + 8, ds_full = bar0 + 16, q_empty = bar0 + 24, v_full = bar0 + 32, v_empty = bar0 + 40, v_fixed = bar0 + 48;
+    const uint32_t s_full = bar0 + 56, stat_full = bar0 + 72, stat_empty = bar0 + 88;          // two each
+    const uint32_t k_full = bar0 + 104, k_empty = bar0 + 128, k_fixed = bar0 + 152;            // one per stage of K
+    uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(bars + 24);
+    volatile int* s_abort = reinterpret_cast<int*>(bars + 25);
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    int tile;
-    const int b = win_find(seqs.item, a.batch, blockIdx.x, tile);
-    const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
-    const int q0 = ((q_len + kQTile - 1) / kQTile - 1 - tile) * kQTile;
-    const int h = blockIdx.y, kvh = h / a.G;
-    const int q_row = seqs.q_start[b] + q0, k_row = seqs.k_start[b];
-    KeyWalk w;
-    w.init(q0, q_len, shift, a.window, a.sinks);
-    const int J = w.n;
+    const int items = seqs.item[a.batch] * a.Hq;
 
     if (threadIdx.x == 0) {
-        mbar_init(q_full, 1); mbar_init(dp_full, 1); mbar_init(ds_full, 8); mbar_init(dq_done, 1);
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(k_full + 8 * i, 1); mbar_init(k_empty + 8 * i, 1); mbar_init(k_fixed + 8 * i, 1);
-            mbar_init(v_full + 8 * i, 1); mbar_init(v_empty + 8 * i, 1); mbar_init(s_full + 8 * i, 1);
-        }
+        mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(dp_full, 1); mbar_init(ds_full, 8);
+        mbar_init(v_full, 1); mbar_init(v_empty, 1); mbar_init(v_fixed, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(stat_full + 8 * i, 2); mbar_init(stat_empty + 8 * i, 8); }
+        for (int i = 0; i < 3; ++i) { mbar_init(k_full + 8 * i, 1); mbar_init(k_empty + 8 * i, 1); mbar_init(k_fixed + 8 * i, 1); }
         *s_abort = 0;
         fence_barrier_init();
     }
@@ -170,211 +179,277 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_q_kernel(const __grid_
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
 
     if (warp == 0) {
-        if (J > 0) {
+        bool ok = true;
+        int n = 0, st = 0, ph = 0, k_issued = 0, v_issued = 0, loaded = 0;       // tiles walked, K's stage and round, copies, items with tiles
+        for (int r = 0, at; ok && (at = item_at(r)) < items; ++r) {
+            QItem x;
+            x.load(at, a, seqs);
+            if (x.w.n == 0) continue;
+            ok = warp_wait(q_empty, (loaded & 1) ^ 1, s_abort);
+            if (!ok) break;
             if (lane == 0) {
                 mbar_expect_tx(q_full, 2 * SM::kT);
 #pragma unroll
                 for (int hf = 0; hf < kHalves; ++hf) {
-                    tma_load_2d(sQ + hf * (kQTile * 128), &tmQ, q_full, h * DH + hf * 64, q_row);
-                    tma_load_2d(sdO + hf * (kQTile * 128), &tmdO, q_full, h * DH + hf * 64, q_row);
+                    tma_load_2d(sQ + hf * (kQTile * 128), &tmQ, q_full, x.h * DH + hf * 64, x.q_row);
+                    tma_load_2d(sdO + hf * (kQTile * 128), &tmdO, q_full, x.h * DH + hf * 64, x.q_row);
                 }
             }
-            bool ok = true;
-            int issued = 0;
-            for (int j = 0; j < J && ok; ++j) {
-                const int st = j & 1, ph = (j >> 1) & 1;
+            __syncwarp();
+            ++loaded;
+            const int col = x.h / a.G * DH;
+#pragma unroll 1
+            for (int j = 0; j < x.w.n; ++j, ++n) {
                 int start, end;
-                w.tile(j, start, end);
+                x.w.tile(j, start, end);
                 const int boxes = (end - start + 63) / 64;       // of 64 keys
-                auto load = [&](const CUtensorMap* tm, uint32_t at, uint32_t bar) {
+                auto load = [&](const CUtensorMap* tm, uint32_t dst, uint32_t bar) {
                     if (lane == 0) {
                         mbar_expect_tx(bar, boxes * kHalves * 64 * 128);
-                        for (int x = 0; x < boxes; ++x)
+                        for (int y = 0; y < boxes; ++y)
 #pragma unroll
                             for (int hf = 0; hf < kHalves; ++hf)
-                                tma_load_2d(at + hf * (kKTile * 128) + x * (64 * 128), tm, bar, kvh * DH + hf * 64, k_row + start + 64 * x);
+                                tma_load_2d(dst + hf * (kKTile * 128) + y * (64 * 128), tm, bar, col + hf * 64, x.k_row + start + 64 * y);
                     }
                     __syncwarp();
                 };
-                ok = warp_wait(v_empty + 8 * st, ph ^ 1, s_abort);      // (free before the K tile of the same stage)
-                if (!ok) break;
-                load(&tmV, sKV + (2 * st + 1) * SM::kT, v_full + 8 * st);
-                ++issued;
                 ok = warp_wait(k_empty + 8 * st, ph ^ 1, s_abort);
                 if (!ok) break;
-                load(&tmK, sKV + 2 * st * SM::kT, k_full + 8 * st);
-                ++issued;
+                load(&tmK, sK + st * SM::kT, k_full + 8 * st);
+                ++k_issued;
+                ok = warp_wait(v_empty, (n & 1) ^ 1, s_abort);
+                if (!ok) break;
+                load(&tmV, sV, v_full);
+                ++v_issued;
                 const int cols = (end - start + 31) & ~31;
-                if (start + cols > kv_len) {                     // rows of K behind the sequence: zero
-                    ok = warp_wait(k_full + 8 * st, ph, s_abort);
+                if (start + cols > x.kv_len) {                   // rows behind the sequence: zero
+                    ok = warp_wait2(k_full + 8 * st, ph, v_full, n & 1, s_abort);
                     if (!ok) break;
-                    zero_rows<DH>(smem + (2 + 2 * st) * SM::kT, kKTile, kv_len - start, cols, lane);
+                    zero_rows<DH>(smem + 3 * SM::kT + st * SM::kT, kKTile, x.kv_len - start, cols, lane);
+                    zero_rows<DH>(smem + 2 * SM::kT, kKTile, x.kv_len - start, cols, lane);
                     fence_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(k_fixed + 8 * st);
+                    if (lane == 0) { mbar_arrive(k_fixed + 8 * st); mbar_arrive(v_fixed); }
                 }
-            }
-            if (!ok) {                                           // copies already requested still land (bounded)
-                for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(q_full, 0); ++i) {}
-                for (int n = max(0, issued - 4); n < issued; ++n)        // copy n: V of tile n / 2 if even, K if odd
-                    for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait((n & 1 ? k_full : v_full) + 8 * ((n >> 1) & 1), (n >> 2) & 1); ++i) {}
+                if (++st == 3) { st = 0; ph ^= 1; }
             }
         }
+        if (!ok) {                                               // copies already requested still land (bounded)
+            for (uint32_t i = 0; loaded > 0 && i < kSpinLimit && !mbar_try_wait(q_full, (loaded - 1) & 1); ++i) {}
+            for (uint32_t i = 0; v_issued > 0 && i < kSpinLimit && !mbar_try_wait(v_full, (v_issued - 1) & 1); ++i) {}
+            for (int c = max(0, k_issued - 3); c < k_issued; ++c)
+                for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(k_full + 8 * (c % 3), (c / 3) & 1); ++i) {}
+        }
     } else if (warp == 1) {
-        if (J > 0) {
-            const bool leader = elect_one();
-            constexpr uint32_t idesc_q = make_idesc_major(kQTile, DH, false, true);
-            bool ok = warp_wait(q_full, 0, s_abort);
-            uint32_t fixed = 0;                                  // phase of every stage's repair barrier
-            auto cols_of = [&](int j, int& start) {
-                int end;
-                w.tile(j, start, end);
-                return (end - start + 31) & ~31;
-            };
-            auto product = [&](uint32_t dst, uint32_t A, uint32_t B, int cols) {      // [128 x DH] x [cols x DH]^T, both K-major
-                const uint32_t idesc = make_idesc(kQTile, cols);
-#pragma unroll
-                for (int hf = 0; hf < kHalves; ++hf) {
-                    const uint64_t da = umma_desc(A + hf * (kQTile * 128)), db = umma_desc(B + hf * (kKTile * 128));
-#pragma unroll
-                    for (int k = 0; k < BK / UMMA_K; ++k) {
-                        const uint64_t off = static_cast<uint64_t>((k * UMMA_K * 2) >> 4);
-                        umma_ss(leader, dst, da + off, db + off, idesc, (hf > 0 || k > 0) ? 1u : 0u);
-                    }
+        const bool leader = elect_one();
+        constexpr uint32_t idesc_q = make_idesc_major(kQTile, DH, false, true);
+        bool ok = true;
+        uint32_t fixed = 0;                                      // phases of the repair barriers (V's in bit 3)
+        // The walk of S and dP runs one tile ahead of the walk of dQ, across items.
+        QItem x;
+        int r = -1, j = 0, n = -1, loaded = -1;                  // x's round, its tile, tiles before this one, items with tiles before x
+        int st = 2, ph = 1;                                      // K's stage and round of tile n
+        bool more = true;
+        int cols = 0, start = 0;
+        auto advance = [&]() {
+            ++n;
+            if (++st == 3) { st = 0; ph ^= 1; }
+            if (r >= 0 && ++j < x.w.n) {
+            } else {
+                j = 0;
+                for (;;) {
+                    const int at = item_at(++r);
+                    more = at < items;
+                    if (!more) return;
+                    x.load(at, a, seqs);
+                    if (x.w.n > 0) break;
                 }
-            };
-            auto issue_s = [&](int j) {
-                const int st = j & 1;
-                int start;
-                const int cols = cols_of(j, start);
-                if (ok) ok = warp_wait(k_full + 8 * st, (j >> 1) & 1, s_abort);
-                if (ok && start + cols > kv_len) { ok = warp_wait(k_fixed + 8 * st, fixed >> st & 1u, s_abort); fixed ^= 1u << st; }
-                if (!ok) return;                                 // (dS of tile j - 2 has been read: k_full follows k_empty)
-                fence_after();
-                product(tmem + 128 * st, sQ, sKV + st * 2 * SM::kT, cols);
-                commit_el(leader, s_full + 8 * st);
-            };
-            auto issue_dp = [&](int j) {
-                int start;
-                const int cols = cols_of(j, start);
-                if (ok) ok = warp_wait(v_full + 8 * (j & 1), (j >> 1) & 1, s_abort);
-                if (!ok) return;
-                fence_after();
-                product(tmem + kDP, sdO, sKV + (j & 1) * 2 * SM::kT + SM::kT, cols);
-                commit_el(leader, v_empty + 8 * (j & 1));
-                commit_el(leader, dp_full);
-            };
-            issue_s(0);
-            issue_dp(0);
-            for (int j = 0; j < J && ok; ++j) {
-                const int st = j & 1;
-                if (j + 1 < J) issue_s(j + 1);
-                if (ok) ok = warp_wait(ds_full, j & 1, s_abort);         // dS is written, dP has been read
+                ++loaded;
+            }
+            int end;
+            x.w.tile(j, start, end);
+            cols = (end - start + 31) & ~31;
+        };
+        auto product = [&](uint32_t dst, uint32_t A, uint32_t B) {       // [128 x DH] x [cols x DH]^T, both K-major
+            const uint32_t idesc = make_idesc(kQTile, cols);
+#pragma unroll
+            for (int hf = 0; hf < kHalves; ++hf) {
+                const uint64_t da = umma_desc(A + hf * (kQTile * 128)), db = umma_desc(B + hf * (kKTile * 128));
+#pragma unroll
+                for (int k = 0; k < BK / UMMA_K; ++k) {
+                    const uint64_t off = static_cast<uint64_t>((k * UMMA_K * 2) >> 4);
+                    umma_ss(leader, dst, da + off, db + off, idesc, (hf > 0 || k > 0) ? 1u : 0u);
+                }
+            }
+        };
+        auto issue_s = [&]() {
+            if (j == 0) ok = warp_wait(q_full, loaded & 1, s_abort);
+            if (ok) ok = warp_wait(k_full + 8 * st, ph, s_abort);
+            if (ok && start + cols > x.kv_len) { ok = warp_wait(k_fixed + 8 * st, fixed >> st & 1u, s_abort); fixed ^= 1u << st; }
+            if (!ok) return;                                     // (dQ has read dS of tile n - 2: the walk of dQ waits for it before tile n)
+            fence_after();
+            product(tmem + 128 * (n & 1), sQ, sK + st * SM::kT);
+            commit_el(leader, s_full + 8 * (n & 1));
+        };
+        auto issue_dp = [&]() {
+            if (ok) ok = warp_wait(v_full, n & 1, s_abort);
+            if (ok && start + cols > x.kv_len) { ok = warp_wait(v_fixed, fixed >> 3 & 1u, s_abort); fixed ^= 8u; }
+            if (!ok) return;
+            fence_after();
+            product(tmem + kDP, sdO, sV);
+            commit_el(leader, v_empty);
+            commit_el(leader, dp_full);
+            if (j + 1 == x.w.n) commit_el(leader, q_empty);      // the item's last products with Q and dO
+        };
+        advance();
+#pragma unroll 1
+        for (int t = -1; ok; ++t) {                              // tile t's dQ, tile t + 1's S and dP; x is at tile max(t, 0) here
+            const int t_st = st, t_ph = ph, t_cols = cols;
+            const bool first = j == 0;
+            if (t >= 0) {
+                if (!more) break;
+                // dS of tile t - 1 lies where S of tile t + 1 goes
+                if (t > 0) ok = warp_wait(k_empty + 8 * (t_st == 0 ? 2 : t_st - 1), t_st == 0 ? t_ph ^ 1 : t_ph, s_abort);
+                advance();
+            }
+            if (more) issue_s();
+            if (t >= 0) {
+                if (ok) ok = warp_wait(ds_full, t & 1, s_abort); // dS is written, dP has been read (and the last item's dQ, if this is a first tile)
                 if (!ok) break;
                 fence_after();
-                int start;
-                const int cols = cols_of(j, start);
-                const uint64_t dk = umma_desc_mn(sKV + st * 2 * SM::kT, kKTile * 128);
-                for (int k = 0; k < cols / UMMA_K; ++k)
-                    umma_ts(leader, tmem + kDQ, tmem + 128 * st + (k >> 2) * 64 + (k & 3) * 8, dk + static_cast<uint64_t>((k * UMMA_K * 128) >> 4), idesc_q,
-                                 (j > 0 || k > 0) ? 1u : 0u);
-                commit_el(leader, k_empty + 8 * st);
-                if (j + 1 == J) commit_el(leader, dq_done);
-                else issue_dp(j + 1);
+                const uint64_t dk = umma_desc_mn(sK + t_st * SM::kT, kKTile * 128);
+#pragma unroll 1
+                for (int k = 0; k < t_cols / UMMA_K; ++k)
+                    umma_ts(leader, tmem + kDQ, tmem + 128 * (t & 1) + (k >> 2) * 64 + (k & 3) * 8, dk + static_cast<uint64_t>((k * UMMA_K * 128) >> 4), idesc_q,
+                            (!first || k > 0) ? 1u : 0u);
+                commit_el(leader, k_empty + 8 * t_st);
             }
+            if (more) issue_dp();
+        }
+    } else if (warp >= 10) {
+        // ---- delta = dO . O of every query, an item ahead of the others; 16 bytes a lane, so DH / 8 lanes to a row
+        // (a small rolled loop, eight rows of both operands in flight: what it has to hide is memory latency and instruction fetches)
+        constexpr int kLanes = DH / 8, kRows = 32 / kLanes, kUnroll = 8;
+        const int sub = lane % kLanes, in = lane / kLanes;
+        bool ok = true;
+        for (int r = 0, at; ok && (at = item_at(r)) < items; ++r) {
+            QItem x;
+            x.load(at, a, seqs);
+            ok = warp_wait(stat_empty + 8 * (r & 1), ((r >> 1) & 1) ^ 1, s_abort);
+            if (!ok) break;
+            float* part = s_stat + (r & 1) * 2 * kQTile;
+            float* stat = a.stats + (size_t)x.h * 2 * a.stat_rows + stat_row0(seqs, x.b) + x.q0;
+            const uint4* dout = reinterpret_cast<const uint4*>(static_cast<const bf16*>(a.dout) + (size_t)x.q_row * a.dout_stride + (size_t)x.h * DH) + sub;
+            const uint4* out = reinterpret_cast<const uint4*>(static_cast<const bf16*>(a.out) + ((size_t)x.q_row * a.Hq + x.h) * DH) + sub;
+            const float* lse = a.lse + (size_t)x.q_row * a.Hq + x.h;
+            const int rows = min(kQTile, x.q_len - x.q0), blind = -x.shift - x.q0;       // rows of the tile; those below `blind` see nothing
+#pragma unroll 1
+            for (int r0 = (warp - 10) * 64 + in; r0 < (warp - 9) * 64; r0 += kRows * kUnroll) {
+                uint4 g[kUnroll], o[kUnroll];
+                float l[kUnroll];
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    const int row = min(r0 + u * kRows, rows - 1);
+                    g[u] = __ldg(dout + row * (a.dout_stride / 8));
+                    o[u] = __ldg(out + row * (a.Hq * DH / 8));
+                    l[u] = __ldg(lse + row * a.Hq);
+                }
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    float e[8], f[8], delta = 0.f;
+                    unpack16<bf16>(g[u], e);
+                    unpack16<bf16>(o[u], f);
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) delta = fmaf(e[z], f[z], delta);
+#pragma unroll
+                    for (int d = 1; d < kLanes; d <<= 1) delta += __shfl_xor_sync(0xffffffffu, delta, d);
+                    const int row = r0 + u * kRows;
+                    const bool sees = row >= blind;
+                    const float nls = sees ? -l[u] * kLog2e : 0.f, nds = sees ? -delta : 0.f;
+                    if (sub == 0) {
+                        part[row] = nls;
+                        part[kQTile + row] = nds;
+                        if (row < rows) {                        // for the key side, each in a row of its own
+                            stat[row] = nls;
+                            stat[a.stat_rows + row] = nds;
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(stat_full + 8 * (r & 1));
         }
     } else {
         const int q = warp & 3, half = (warp - 2) >> 2;          // tensor-memory lane quarter; which 64 columns of a tile
-        const int row = q * 32 + lane, i = q0 + row;
+        const int row = q * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>(q * 32) << 16;
-        const bool valid = i < q_len;
-        const int last = i + shift, oldest = last - a.window + 1;
-        const int full_lo = min(q0 + kQTile, q_len) - 1 + shift - a.window + 1, full_hi = q0 + shift + 1;
-        // delta = dO . O of this query (each thread of the row half of it), and its log-sum-exp in log2 units
-        float delta = 0.f, lse2 = 0.f;
-        if (valid) {
-            const size_t at = (size_t)(q_row + row);
-            const uint4* x = reinterpret_cast<const uint4*>(static_cast<const bf16*>(a.dout) + at * a.dout_stride + (size_t)h * DH + half * (DH / 2));
-            const uint4* y = reinterpret_cast<const uint4*>(static_cast<const bf16*>(a.out) + (at * a.Hq + h) * DH + half * (DH / 2));
-#pragma unroll
-            for (int c = 0; c < DH / 16; ++c) {
-                float f[8], g[8];
-                unpack16<bf16>(__ldg(x + c), f);
-                unpack16<bf16>(__ldg(y + c), g);
-#pragma unroll
-                for (int z = 0; z < 8; ++z) delta = fmaf(f[z], g[z], delta);
-            }
-            lse2 = __ldg(a.lse + at * a.Hq + h) * kLog2e;
-        }
-        s_delta[half * kQTile + row] = delta;
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        delta = s_delta[row] + s_delta[kQTile + row];
-        if (last < 0) { delta = 0.f; lse2 = 0.f; }               // a query that sees nothing
-        if (valid) {                                             // for the key side: -lse and -delta, each in a row of its own
-            float* stat = a.stats + (size_t)h * 2 * a.stat_rows + stat_row0(seqs, b) + i;
-            if (half == 0) stat[0] = -lse2;
-            else stat[a.stat_rows] = -delta;
-        }
-        const uint64_t scale2 = pk2(a.scale_log2, a.scale_log2), nl2 = pk2(-lse2, -lse2), nd2 = pk2(-delta, -delta);
-        auto nl = [&](int) { return nl2; };
-        auto nd = [&](int) { return nd2; };
+        const uint64_t scale2 = pk2(a.scale_log2, a.scale_log2);
         bool ok = true;
-        for (int j = 0; j < J; ++j) {
-            const int st = j & 1;
-            int start, end;
-            w.tile(j, start, end);
-            start += 64 * half;                                  // this thread's columns
-            const bool one = start < end, two = start + 32 < end;
-            const bool full = start + 64 <= min(end, full_hi) && (start >= full_lo || start + 64 <= a.sinks);
-            if (ok) ok = warp_wait(s_full + 8 * st, (j >> 1) & 1, s_abort);
-            if (!ok) break;
-            fence_after();
-            const uint32_t ts = tmem + 128 * st + 64 * half + lanes;
-            uint32_t s[2][32], d[2][32], y[2][16];
-            if (one) {
-                tmem_ld32(ts, s[0]);
-                if (two) tmem_ld32(ts + 32, s[1]);
-                tmem_ld_wait();
-                if (full) {
-                    chunk_p<false>(s[0], 0u, scale2, nl);
-                    chunk_p<false>(s[1], 0u, scale2, nl);
-                } else {
-                    const int top = valid ? min(last + 1, end) - start : 0;
-                    chunk_p<true>(s[0], bit_range(oldest - start, top) | bit_range(0, min(a.sinks - start, top)), scale2, nl);
-                    if (two) chunk_p<true>(s[1], bit_range(oldest - start - 32, top - 32) | bit_range(0, min(a.sinks - start, top) - 32), scale2, nl);
-                }
-            }
-            ok = warp_wait(dp_full, j & 1, s_abort);
-            if (!ok) break;
-            fence_after();
-            if (one) {
-                tmem_ld32(tmem + kDP + 64 * half + lanes, d[0]);
-                if (two) tmem_ld32(tmem + kDP + 64 * half + 32 + lanes, d[1]);
-                tmem_ld_wait();
-                if (full) {
-                    chunk_ds<false>(s[0], d[0], nd, y[0]);
-                    chunk_ds<false>(s[1], d[1], nd, y[1]);
-                } else {
-                    chunk_ds<true>(s[0], d[0], nd, y[0]);
-                    if (two) chunk_ds<true>(s[1], d[1], nd, y[1]);
-                }
-                tmem_st16(ts, y[0]);                             // dS of this half over its own S columns
-                if (two) tmem_st16(ts + 16, y[1]);
-                tmem_st_wait();
-            }
-            fence_before();
+        int n = 0;
+        for (int r = 0, at; (at = item_at(r)) < items; ++r) {
+            QItem x;
+            x.load(at, a, seqs);
+            const int i = x.q0 + row;
+            const bool valid = i < x.q_len;
+            const int last = i + x.shift, oldest = last - a.window + 1;
+            const int full_lo = min(x.q0 + kQTile, x.q_len) - 1 + x.shift - a.window + 1, full_hi = x.q0 + x.shift + 1;
+            if (ok) ok = warp_wait(stat_full + 8 * (r & 1), (r >> 1) & 1, s_abort);
+            const float nls = s_stat[(r & 1) * 2 * kQTile + row], nds = s_stat[((r & 1) * 2 + 1) * kQTile + row];
             __syncwarp();
-            if (lane == 0) mbar_arrive(ds_full);
-        }
-        if (J > 0) {
-            if (ok) ok = warp_wait(dq_done, 0, s_abort);
-        }
-        fence_after();
-        bf16* dst = static_cast<bf16*>(a.dq) + (size_t)(q_row + row) * a.dq_stride + (size_t)h * DH;
+            if (lane == 0) mbar_arrive(stat_empty + 8 * (r & 1));
+            const uint64_t nl2 = pk2(nls, nls), nd2 = pk2(nds, nds);
+            auto nl = [&](int) { return nl2; };
+            auto nd = [&](int) { return nd2; };
+            for (int j = 0; j < x.w.n; ++j, ++n) {
+                const int st = n & 1;
+                int start, end;
+                x.w.tile(j, start, end);
+                start += 64 * half;                              // this thread's columns
+                const bool one = start < end, two = start + 32 < end;
+                const bool full = start + 64 <= min(end, full_hi) && (start >= full_lo || start + 64 <= a.sinks);
+                if (ok) ok = warp_wait(s_full + 8 * st, (n >> 1) & 1, s_abort);
+                const uint32_t ts = tmem + 128 * st + 64 * half + lanes;
+                uint32_t s[2][32], d[2][32], y[2][16];
+                if (ok && one) {
+                    fence_after();
+                    tmem_ld32(ts, s[0]);
+                    if (two) tmem_ld32(ts + 32, s[1]);
+                    tmem_ld_wait();
+                    if (!full) {
+                        const int top = valid ? min(last + 1, end) - start : 0, sink_top = min(a.sinks - start, top);
+                        mask32(s[0], bit_range(oldest - start, top) | bit_range(0, sink_top));
+                        mask32(s[1], bit_range(oldest - start - 32, top - 32) | bit_range(0, sink_top - 32));
+                    }
+                    chunk_p(s[0], scale2, nl);
+                    if (two) chunk_p(s[1], scale2, nl);
+                }
+                if (ok) ok = warp_wait(dp_full, n & 1, s_abort);
+                if (!ok) continue;
+                fence_after();
+                if (one) {
+                    tmem_ld32(tmem + kDP + 64 * half + lanes, d[0]);
+                    if (two) tmem_ld32(tmem + kDP + 64 * half + 32 + lanes, d[1]);
+                    tmem_ld_wait();
+                    chunk_ds(s[0], d[0], nd, y[0]);
+                    tmem_st16(ts, y[0]);                         // dS of this half over its own S columns
+                    if (two) {
+                        chunk_ds(s[1], d[1], nd, y[1]);
+                        tmem_st16(ts + 16, y[1]);
+                    }
+                    tmem_st_wait();
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(ds_full);
+            }
+            if (x.w.n > 0 && ok) ok = warp_wait(k_empty + 8 * ((n - 1) % 3), ((n - 1) / 3) & 1, s_abort);       // the item's last dQ
+            fence_after();
+            bf16* dst = static_cast<bf16*>(a.dq) + (size_t)(x.q_row + row) * a.dq_stride + (size_t)x.h * DH;
 #pragma unroll
-        for (int c = 0; c < DH / 2; c += 32) {
-            const int col = half * (DH / 2) + c;
-            store_row32(tmem + kDQ + col + lanes, ok ? a.scale : nan_f(), dst + col, valid, J == 0);
+            for (int c = 0; c < DH / 2; c += 32) {
+                const int col = half * (DH / 2) + c;
+                store_row32(tmem + kDQ + col + lanes, ok ? a.scale : nan_f(), dst + col, valid, x.w.n == 0);
+            }
         }
     }
     fence_before();
@@ -408,11 +483,58 @@ __device__ __forceinline__ int band_end(int k0, int kv_len, int q_len, int shift
     return max(0, min(q_len, last_key - shift + window));
 }
 
-// Items of the grid, per sequence: first its key tiles (band), then, for each of the sink_tiles, sink_segs segments.
+// One item: 128 keys of one (sequence, K/V head) and the queries of its band, or a segment of the queries past the band.
+// Per sequence the grid's list has first its key tiles (bands), then, for each of the sink_tiles, sink_segs segments.
+struct KItem {
+    int b, kvh, k0, q_len, kv_len, shift, k_row, seg, band, n;      // seg: -1 = band; band: first query past it; n: jobs
+    int j0;
+    QueryWalk w;
+    __device__ __forceinline__ void load(int at, const WinArgs& a, const WinSeqs& s) {
+        const int per_head = s.item[a.batch];
+        int item;
+        kvh = at / per_head;
+        b = win_find(s.item, a.batch, at - kvh * per_head, item);
+        q_len = s.q_len[b];
+        kv_len = s.kv_len[b];
+        shift = kv_len - q_len - a.strict;
+        const int tiles = (kv_len + kKTile - 1) / kKTile;
+        const bool sink_part = item >= tiles;
+        seg = sink_part ? (item - tiles) % a.sink_segs : -1;
+        k0 = (sink_part ? (item - tiles) / a.sink_segs : item) * kKTile;
+        k_row = s.k_start[b] + k0;
+        band = band_end(k0, kv_len, q_len, shift, a.window);
+        j0 = 0;
+        n = 0;
+        if (!sink_part) {
+            w.init(k0 - shift, band);
+            n = w.n * a.G;
+        } else if (k0 < min(a.sinks, kv_len)) {
+            w.init(band, q_len);
+            const int total = w.n * a.G;
+            j0 = (int)((long long)total * seg / a.sink_segs);
+            n = (int)((long long)total * (seg + 1) / a.sink_segs) - j0;
+        }
+    }
+};
+// Jobs of an item in order: the tiles of one head after the other.
+struct Job {
+    int h, qb, left;                     // query head, first query, tiles left of this head
+    __device__ __forceinline__ void first(const KItem& x, int G) {
+        const int skip = x.j0 > 0 ? x.j0 / x.w.n : 0, in = x.j0 - skip * x.w.n;
+        h = x.kvh * G + skip;
+        qb = x.w.from + in * kQTile;
+        left = x.w.n - in;
+    }
+    __device__ __forceinline__ void next(const KItem& x) {
+        qb += kQTile;
+        if (--left == 0) { ++h; qb = x.w.from; left = x.w.n; }
+    }
+};
+
 template <int DH>
 __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmdO,
-                                                                   const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                                                                   const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
+                                                                  const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                                                                  const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
     using SM = BwdKSmem<DH>;
     constexpr int kHalves = DH / 64;
     constexpr uint32_t kTmem = 512, kY = 128, kDV = 256, kDK = 256 + DH;     // S^T / P^T at column 0, dP^T / dS^T at 128
@@ -421,53 +543,19 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
     const uint32_t sStat = sQ + 4 * SM::kT;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 6 * SM::kT + 4 * SM::kStat);
     const uint32_t bar0 = smem_u32(bars);
-    const uint32_t kv_full = bar0, s_full = bar0 + 8, dp_full = bar0 + 16, ds_full = bar0 + 24;
+    const uint32_t kv_full = bar0, s_full = bar0 + 8, dp_full = bar0 + 16, ds_full = bar0 + 24, kv_empty = bar0 + 32;
     // one per stage; Q is free when dK has read it (so is dS^T's place), dO when dV has (so is P^T's place)
-    const uint32_t p_full = bar0 + 152;                  // P^T in two parts: the first 32 queries of each half of the tile, then the others
     const uint32_t q_full = bar0 + 40, do_full = bar0 + 56, y_free = bar0 + 72, x_free = bar0 + 88, stat_empty = bar0 + 104, q_fixed = bar0 + 120,
                    do_fixed = bar0 + 136;
+    const uint32_t p_full = bar0 + 152;                  // P^T in two parts: the first 32 queries of each half of the tile, then the others
     uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(bars + 24);
     volatile int* s_abort = reinterpret_cast<int*>(bars + 25);
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    int item;
-    const int b = win_find(seqs.item, a.batch, blockIdx.x, item);
-    const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
-    const int kvh = blockIdx.y;
-    const int tiles = (kv_len + kKTile - 1) / kKTile;
-    const bool sink_part = item >= tiles;
-    const int sink_tile = sink_part ? (item - tiles) / a.sink_segs : item;
-    const int seg = sink_part ? (item - tiles) % a.sink_segs : -1;
-    const int k0 = sink_tile * kKTile;
-    QueryWalk w;
-    int j0 = 0, J;
-    {
-        const int end = band_end(k0, kv_len, q_len, shift, a.window);
-        if (!sink_part) {
-            w.init(k0 - shift, end);
-            J = w.n * a.G;
-        } else {                                             // segment `seg` of the queries past the band, of all heads
-            if (k0 >= min(a.sinks, kv_len)) return;          // (uniform over the CTA; nothing allocated yet)
-            w.init(end, q_len);
-            const int total = w.n * a.G;
-            j0 = (int)((long long)total * seg / a.sink_segs);
-            J = (int)((long long)total * (seg + 1) / a.sink_segs) - j0;
-            if (J <= 0) return;                              // the join knows
-        }
-    }
-    const int k_row = seqs.k_start[b] + k0;
-    const int from_query = sink_part ? band_end(k0, kv_len, q_len, shift, a.window) : 0;
-    // Jobs in order: the tiles of one head after the other.
-    struct Job {
-        int h, qb, left;                 // query head, first query, tiles left of this head
-    } const job0 = {kvh * a.G + (w.n > 0 ? j0 / w.n : 0), w.from + (w.n > 0 ? j0 % w.n : 0) * kQTile, w.n - (w.n > 0 ? j0 % w.n : 0)};
-    auto next_job = [&](Job& x) {
-        x.qb += kQTile;
-        if (--x.left == 0) { ++x.h; x.qb = w.from; x.left = w.n; }
-    };
+    const int items = seqs.item[a.batch] * a.Hkv;
 
     if (threadIdx.x == 0) {
-        mbar_init(kv_full, 1); mbar_init(s_full, 1); mbar_init(p_full, 8); mbar_init(p_full + 8, 8); mbar_init(dp_full, 1); mbar_init(ds_full, 8);
+        mbar_init(kv_full, 1); mbar_init(kv_empty, 1); mbar_init(s_full, 1); mbar_init(p_full, 8); mbar_init(p_full + 8, 8); mbar_init(dp_full, 1); mbar_init(ds_full, 8);
         for (int i = 0; i < 2; ++i) {
             mbar_init(q_full + 8 * i, 1); mbar_init(do_full + 8 * i, 1); mbar_init(y_free + 8 * i, 1); mbar_init(x_free + 8 * i, 1);
             mbar_init(stat_empty + 8 * i, 8); mbar_init(q_fixed + 8 * i, 1); mbar_init(do_fixed + 8 * i, 1);
@@ -482,249 +570,279 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
 
     if (warp == 0) {
-        if (J > 0) {
+        bool ok = true;
+        int n = 0, issued = 0, loaded = 0;                       // jobs walked, copies of Q and dO, items with jobs
+        for (int r = 0, at; ok && (at = item_at(r)) < items; ++r) {
+            KItem x;
+            x.load(at, a, seqs);
+            if (x.n == 0) continue;
+            ok = warp_wait(kv_empty, (loaded & 1) ^ 1, s_abort);
+            if (!ok) break;
             if (lane == 0) {
                 mbar_expect_tx(kv_full, 2 * SM::kT);
 #pragma unroll
                 for (int hf = 0; hf < kHalves; ++hf) {
-                    tma_load_2d(sK + hf * (kKTile * 128), &tmK, kv_full, kvh * DH + hf * 64, k_row);
-                    tma_load_2d(sV + hf * (kKTile * 128), &tmV, kv_full, kvh * DH + hf * 64, k_row);
+                    tma_load_2d(sK + hf * (kKTile * 128), &tmK, kv_full, x.kvh * DH + hf * 64, x.k_row);
+                    tma_load_2d(sV + hf * (kKTile * 128), &tmV, kv_full, x.kvh * DH + hf * 64, x.k_row);
                 }
             }
-            const int stat0 = stat_row0(seqs, b);
-            bool ok = true;
-            int issued = 0;
-            Job job = job0;
-            for (int j = 0; j < J && ok; ++j, next_job(job)) {
-                const int st = j & 1, ph = (j >> 1) & 1, h = job.h, qb = job.qb;
-                const uint32_t at = sQ + st * 2 * SM::kT;
+            __syncwarp();
+            ++loaded;
+            const int stat0 = stat_row0(seqs, x.b), q_start = seqs.q_start[x.b];
+            Job job;
+            job.first(x, a.G);
+            for (int j = 0; j < x.n; ++j, ++n, job.next(x)) {
+                const int st = n & 1, ph = (n >> 1) & 1, h = job.h, qb = job.qb;
+                const uint32_t dst = sQ + st * 2 * SM::kT;
                 uint8_t* tile = smem + (2 + 2 * st) * SM::kT;
-                const bool edge = qb + kQTile > q_len;           // rows behind the sequence: zero
-                auto repair = [&](uint32_t full, uint32_t fixed, uint8_t* t) {
-                    ok = warp_wait(full, ph, s_abort);
-                    if (!ok) return;
-                    zero_rows<DH>(t, kQTile, q_len - qb, kQTile, lane);
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(fixed);
-                };
-                ok = warp_wait(x_free + 8 * st, ph ^ 1, s_abort);        // dO is needed last and free first
+                ok = warp_wait(x_free + 8 * st, ph ^ 1, s_abort);        // dO is free first
                 if (!ok) break;
                 if (lane == 0) {
                     mbar_expect_tx(do_full + 8 * st, SM::kT);
 #pragma unroll
                     for (int hf = 0; hf < kHalves; ++hf)
-                        tma_load_2d(at + SM::kT + hf * (kQTile * 128), &tmdO, do_full + 8 * st, h * DH + hf * 64, seqs.q_start[b] + qb);
+                        tma_load_2d(dst + SM::kT + hf * (kQTile * 128), &tmdO, do_full + 8 * st, h * DH + hf * 64, q_start + qb);
                 }
                 __syncwarp();
                 ++issued;
-                ok = warp_wait(y_free + 8 * st, ph ^ 1, s_abort);
-                if (ok) ok = warp_wait(stat_empty + 8 * st, ph ^ 1, s_abort);
+                ok = warp_wait2(y_free + 8 * st, ph ^ 1, stat_empty + 8 * st, ph ^ 1, s_abort);
                 if (!ok) break;
                 if (lane == 0) {
                     mbar_expect_tx(q_full + 8 * st, SM::kT + 2 * SM::kStat);
 #pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf) tma_load_2d(at + hf * (kQTile * 128), &tmQ, q_full + 8 * st, h * DH + hf * 64, seqs.q_start[b] + qb);
+                    for (int hf = 0; hf < kHalves; ++hf) tma_load_2d(dst + hf * (kQTile * 128), &tmQ, q_full + 8 * st, h * DH + hf * 64, q_start + qb);
                     const float* stat = a.stats + (size_t)h * 2 * a.stat_rows + stat0 + qb;
                     bulk_load(sStat + st * 2 * SM::kStat, stat, SM::kStat, q_full + 8 * st);
                     bulk_load(sStat + st * 2 * SM::kStat + SM::kStat, stat + a.stat_rows, SM::kStat, q_full + 8 * st);
                 }
                 __syncwarp();
                 ++issued;
-                if (edge) {
-                    repair(q_full + 8 * st, q_fixed + 8 * st, tile);
-                    if (ok) repair(do_full + 8 * st, do_fixed + 8 * st, tile + SM::kT);
+                if (qb + kQTile > x.q_len) {
+                    // rows behind the sequence: zero, and their statistics
+                    ok = warp_wait2(q_full + 8 * st, ph, do_full + 8 * st, ph, s_abort);
+                    if (!ok) break;
+                    zero_rows<DH>(tile, kQTile, x.q_len - qb, kQTile, lane);
+                    zero_rows<DH>(tile + SM::kT, kQTile, x.q_len - qb, kQTile, lane);
+                    float* stat = reinterpret_cast<float*>(smem + 6 * SM::kT + st * 2 * SM::kStat);
+                    for (int i = x.q_len - qb + lane; i < kQTile; i += 32) stat[i] = stat[kQTile + i] = 0.f;
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) { mbar_arrive(q_fixed + 8 * st); mbar_arrive(do_fixed + 8 * st); }
                 }
-            }
-            if (!ok) {                                           // copies already requested still land (bounded)
-                for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(kv_full, 0); ++i) {}
-                for (int n = max(0, issued - 4); n < issued; ++n)        // copy n: dO of tile n / 2 if even, Q if odd
-                    for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait((n & 1 ? q_full : do_full) + 8 * ((n >> 1) & 1), (n >> 2) & 1); ++i) {}
             }
         }
+        if (!ok) {                                               // copies already requested still land (bounded)
+            for (uint32_t i = 0; loaded > 0 && i < kSpinLimit && !mbar_try_wait(kv_full, (loaded - 1) & 1); ++i) {}
+            for (int c = max(0, issued - 4); c < issued; ++c)    // copy c: dO of tile c / 2 if even, Q if odd
+                for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait((c & 1 ? q_full : do_full) + 8 * ((c >> 1) & 1), (c >> 2) & 1); ++i) {}
+        }
     } else if (warp == 1) {
-        if (J > 0) {
-            const bool leader = elect_one();
-            constexpr uint32_t idesc_s = make_idesc(kKTile, kQTile), idesc_o = make_idesc_major(kKTile, DH, false, true);
-            bool ok = warp_wait(kv_full, 0, s_abort);
-            uint32_t fixed = 0;                                  // phase of every stage's repair barrier
-            auto product = [&](uint32_t dst, uint32_t A, uint32_t B) {       // [128 x DH] x [128 x DH]^T, both K-major
+        const bool leader = elect_one();
+        constexpr uint32_t idesc_s = make_idesc(kKTile, kQTile), idesc_o = make_idesc_major(kKTile, DH, false, true);
+        bool ok = true;
+        uint32_t fixed = 0;                                      // phases of the repair barriers
+        // The walk of S^T and dP^T runs one job ahead of the walk of dV and dK, across items.
+        KItem x;
+        Job job;
+        int r = -1, j = 0, n = -1, loaded = -1;
+        bool more = true;
+        auto advance = [&]() {
+            ++n;
+            if (r >= 0 && ++j < x.n) { job.next(x); return; }
+            j = 0;
+            for (;;) {
+                const int at = item_at(++r);
+                more = at < items;
+                if (!more) return;
+                x.load(at, a, seqs);
+                if (x.n > 0) break;
+            }
+            job.first(x, a.G);
+            ++loaded;
+        };
+        auto product = [&](uint32_t dst, uint32_t A, uint32_t B) {       // [128 x DH] x [128 x DH]^T, both K-major
 #pragma unroll
-                for (int hf = 0; hf < kHalves; ++hf) {
-                    const uint64_t da = umma_desc(A + hf * (kKTile * 128)), db = umma_desc(B + hf * (kQTile * 128));
+            for (int hf = 0; hf < kHalves; ++hf) {
+                const uint64_t da = umma_desc(A + hf * (kKTile * 128)), db = umma_desc(B + hf * (kQTile * 128));
 #pragma unroll
-                    for (int k = 0; k < BK / UMMA_K; ++k) {
-                        const uint64_t off = static_cast<uint64_t>((k * UMMA_K * 2) >> 4);
-                        umma_ss(leader, dst, da + off, db + off, idesc_s, (hf > 0 || k > 0) ? 1u : 0u);
-                    }
+                for (int k = 0; k < BK / UMMA_K; ++k) {
+                    const uint64_t off = static_cast<uint64_t>((k * UMMA_K * 2) >> 4);
+                    umma_ss(leader, dst, da + off, db + off, idesc_s, (hf > 0 || k > 0) ? 1u : 0u);
                 }
-            };
-            // acc += (operand of tile rows x 128 queries, at `src` in two halves of 64 queries) x (B tile [query][DH]), the products of
-            // 16 queries from `k0` to `k1` of each half
-            auto accumulate = [&](uint32_t acc, uint32_t src, uint32_t B, int k0, int k1, bool first) {
-                const uint64_t db = umma_desc_mn(B, kQTile * 128);
+            }
+        };
+        // acc += (operand of tile rows x 128 queries, at `src` in two halves of 64 queries) x (B tile [query][DH]), the products of
+        // 16 queries from `k0` to `k1` of each half
+        auto accumulate = [&](uint32_t acc, uint32_t src, uint32_t B, int k0, int k1, bool first) {
+            const uint64_t db = umma_desc_mn(B, kQTile * 128);
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int k = k0; k < k1; ++k)
-                        umma_ts(leader, tmem + acc, tmem + src + h * 64 + k * 8, db + static_cast<uint64_t>(((4 * h + k) * UMMA_K * 128) >> 4), idesc_o,
-                                (!first || h > 0 || k > k0) ? 1u : 0u);
-            };
-            Job job = job0;                                      // of the next S^T (and, right after it, the next dP^T)
-            auto wait_tile = [&](int j, uint32_t full, uint32_t repaired, int qb) {      // Q or dO of job j is there (and repaired)
-                const int st = j & 1;
-                if (ok) ok = warp_wait(full + 8 * st, (j >> 1) & 1, s_abort);
-                if (ok && qb + kQTile > q_len) {
-                    const uint32_t bit = repaired == q_fixed ? st : 2 + st;
-                    ok = warp_wait(repaired + 8 * st, fixed >> bit & 1u, s_abort);
-                    fixed ^= 1u << bit;
-                }
-            };
-            auto issue_s = [&](int j) {                          // S^T = K Q^T
-                wait_tile(j, q_full, q_fixed, job.qb);
-                if (ok && j > 0) ok = warp_wait(x_free + 8 * ((j - 1) & 1), ((j - 1) >> 1) & 1, s_abort);    // P^T of the last job lies there
-                if (!ok) return;
-                fence_after();
-                product(tmem, sK, sQ + (j & 1) * 2 * SM::kT);
-                commit_el(leader, s_full);
-            };
-            auto issue_dp = [&](int j) {                         // dP^T = V dO^T
-                wait_tile(j, do_full, do_fixed, job.qb);
-                next_job(job);
-                if (ok && j > 0) ok = warp_wait(y_free + 8 * ((j - 1) & 1), ((j - 1) >> 1) & 1, s_abort);    // dS^T of the last job lies there
-                if (!ok) return;
-                fence_after();
-                product(tmem + kY, sV, sQ + (j & 1) * 2 * SM::kT + SM::kT);
-                commit_el(leader, dp_full);
-            };
-            issue_s(0);
-            issue_dp(0);
-            for (int j = 0; j < J && ok; ++j) {
-                const int st = j & 1;
-                const uint32_t Q = sQ + st * 2 * SM::kT;
-                ok = warp_wait(p_full, j & 1, s_abort);
+                for (int k = k0; k < k1; ++k)
+                    umma_ts(leader, tmem + acc, tmem + src + h * 64 + k * 8, db + static_cast<uint64_t>(((4 * h + k) * UMMA_K * 128) >> 4), idesc_o,
+                            (!first || h > 0 || k > k0) ? 1u : 0u);
+        };
+        // Q or dO of job n is there (and repaired) and, from the second job on, the place of its product is free again.
+        auto wait_tile = [&](uint32_t full, uint32_t repaired, uint32_t place) {
+            const int st = n & 1;
+            if (!ok) return;
+            if (n > 0) ok = warp_wait2(full + 8 * st, (n >> 1) & 1, place + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, s_abort);
+            else ok = warp_wait(full + 8 * st, 0, s_abort);
+            if (ok && job.qb + kQTile > x.q_len) {
+                const uint32_t bit = repaired == q_fixed ? st : 2 + st;
+                ok = warp_wait(repaired + 8 * st, fixed >> bit & 1u, s_abort);
+                fixed ^= 1u << bit;
+            }
+        };
+        auto issue_s = [&]() {                                   // S^T = K Q^T
+            if (j == 0) ok = warp_wait(kv_full, loaded & 1, s_abort);
+            wait_tile(q_full, q_fixed, x_free);
+            if (!ok) return;
+            fence_after();
+            product(tmem, sK, sQ + (n & 1) * 2 * SM::kT);
+            commit_el(leader, s_full);
+        };
+        auto issue_dp = [&]() {                                  // dP^T = V dO^T
+            wait_tile(do_full, do_fixed, y_free);
+            if (!ok) return;
+            fence_after();
+            product(tmem + kY, sV, sQ + (n & 1) * 2 * SM::kT + SM::kT);
+            commit_el(leader, dp_full);
+            if (j + 1 == x.n) commit_el(leader, kv_empty);       // the item's last products with K and V
+        };
+        advance();
+#pragma unroll 1
+        for (int t = -1; ok; ++t) {                              // job t's dV and dK, job t + 1's S^T and dP^T; x is at job max(t, 0) here
+            const int st = t & 1;
+            const uint32_t Q = sQ + st * 2 * SM::kT;
+            const bool first = j == 0;
+            if (t >= 0) {
+                if (!more) break;
+                ok = warp_wait(p_full, t & 1, s_abort);          // (and, if this is a first job, the last item's dV and dK have been read)
                 if (!ok) break;
                 fence_after();
-                accumulate(kDV, 0, Q + SM::kT, 0, 2, j == 0);    // dV += P^T dO
-                ok = warp_wait(p_full + 8, j & 1, s_abort);
+                accumulate(kDV, 0, Q + SM::kT, 0, 2, first);     // dV += P^T dO
+                ok = warp_wait(p_full + 8, t & 1, s_abort);
                 if (!ok) break;
                 fence_after();
                 accumulate(kDV, 0, Q + SM::kT, 2, 4, false);
                 commit_el(leader, x_free + 8 * st);
-                if (j + 1 < J) issue_s(j + 1);
-                if (ok) ok = warp_wait(ds_full, j & 1, s_abort);
+                advance();
+            }
+            if (more) issue_s();
+            if (t >= 0) {
+                if (ok) ok = warp_wait(ds_full, t & 1, s_abort);
                 if (!ok) break;
                 fence_after();
-                accumulate(kDK, kY, Q, 0, 4, j == 0);            // dK += dS^T Q
+                accumulate(kDK, kY, Q, 0, 4, first);             // dK += dS^T Q
                 commit_el(leader, y_free + 8 * st);
-                if (j + 1 < J) issue_dp(j + 1);
             }
+            if (more) issue_dp();
         }
     } else {
         const int q = warp & 3, half = (warp - 2) >> 2;          // tensor-memory lane quarter; which 64 of the tile's queries
-        const int key = k0 + q * 32 + lane;
-        const uint32_t at = (static_cast<uint32_t>(q * 32) << 16) + 64 * half;
-        const bool valid = key < kv_len;
-        const bool is_sink = key < a.sinks;
-        // queries that see this key: [first, stop)
-        const int first = max(key - shift, from_query);
-        const int stop = !valid ? 0 : is_sink ? q_len : sink_part ? 0 : min(q_len, key - shift + a.window);
-        const int stop_band = sink_part ? q_len : band_end(k0, kv_len, q_len, shift, a.window);      // a band CTA leaves the rest to the segments
-        const int stop_all = min(stop, stop_band);
-        // every key of the tile is seen by queries [full_lo, full_hi)
-        const int full_lo = max(min(k0 + kKTile, kv_len) - 1 - shift, from_query);
-        const int full_hi = k0 + kKTile > kv_len ? 0 : k0 + kKTile <= a.sinks ? stop_band : sink_part ? 0 : min(q_len, k0 - shift + a.window);
+        const uint32_t lanes = static_cast<uint32_t>(q * 32) << 16, at64 = lanes + 64 * half;
         const uint64_t scale2 = pk2(a.scale_log2, a.scale_log2);
         bool ok = true;
-        Job job = job0;
-        for (int j = 0; j < J; ++j, next_job(job)) {
-            const int st = j & 1, c0 = job.qb + 64 * half;           // first query of this thread's columns
-            const float* stat = reinterpret_cast<const float*>(smem + 6 * SM::kT + st * 2 * SM::kStat) + 64 * half;      // -lse; -delta one kStat on
-            if (ok) ok = warp_wait(q_full + 8 * st, (j >> 1) & 1, s_abort);      // the statistics
-            if (ok) ok = warp_wait(s_full, j & 1, s_abort);
-            if (!ok) break;
-            fence_after();
-            const bool full = c0 >= full_lo && c0 + 64 <= full_hi;
-            uint32_t s[2][32], d[2][32], y[2][16];
-            tmem_ld32(tmem + at, s[0]);
-            tmem_ld32(tmem + at + 32, s[1]);
-            tmem_ld_wait();
+        int n = 0;
+        for (int r = 0, at; (at = item_at(r)) < items; ++r) {
+            KItem x;
+            x.load(at, a, seqs);
+            const bool sink_part = x.seg >= 0;
+            if (sink_part && x.n == 0) continue;                 // the join knows
+            const int key = x.k0 + q * 32 + lane;
+            const bool valid = key < x.kv_len, is_sink = key < a.sinks;
+            // queries that see this key and belong to this item: [first, stop)
+            const int first = sink_part ? x.band : key - x.shift;
+            const int stop = !valid ? 0 : sink_part ? (is_sink ? x.q_len : 0) : is_sink ? x.band : min(x.q_len, key - x.shift + a.window);
+            // every key of the tile is seen by queries [full_lo, full_hi)
+            const int full_lo = sink_part ? x.band : min(x.k0 + kKTile, x.kv_len) - 1 - x.shift;
+            const int full_hi = x.k0 + kKTile > x.kv_len ? 0 : x.k0 + kKTile <= a.sinks ? (sink_part ? x.q_len : x.band)
+                                                           : sink_part ? 0 : min(x.q_len, x.k0 - x.shift + a.window);
+            Job job;
+            if (x.n > 0) job.first(x, a.G);
+            for (int j = 0; j < x.n; ++j, ++n, job.next(x)) {
+                const int st = n & 1, c0 = job.qb + 64 * half;   // first query of this thread's columns
+                const float* stat = reinterpret_cast<const float*>(smem + 6 * SM::kT + st * 2 * SM::kStat) + 64 * half;      // -lse; -delta one kStat on
+                if (ok) ok = warp_wait2(q_full + 8 * st, (n >> 1) & 1, s_full, n & 1, s_abort);      // (q_full: the statistics; their repair precedes S^T)
+                if (!ok) continue;
+                fence_after();
+                const bool full = c0 >= full_lo && c0 + 64 <= full_hi;
+                uint32_t s[2][32], d[2][32], y[2][16];
+                tmem_ld32(tmem + at64, s[0]);
+                tmem_ld32(tmem + at64 + 32, s[1]);
+                tmem_ld_wait();
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                // two columns' words as one 64-bit load, the same for every lane
-                auto nl = [&](int x) { return *reinterpret_cast<const uint64_t*>(stat + 32 * c + x); };
-                if (full) chunk_p<false>(s[c], 0u, scale2, nl);
-                else chunk_p<true>(s[c], bit_range(first - c0 - 32 * c, stop_all - c0 - 32 * c), scale2, nl);
+                for (int c = 0; c < 2; ++c) {
+                    // two columns' words as one 64-bit load, the same for every lane
+                    auto nl = [&](int e) { return *reinterpret_cast<const uint64_t*>(stat + 32 * c + e); };
+                    if (!full) mask32(s[c], bit_range(first - c0 - 32 * c, stop - c0 - 32 * c));
+                    chunk_p(s[c], scale2, nl);
 #pragma unroll
-                for (int x = 0; x < 16; ++x) y[c][x] = pack_bf16(__uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1]));
-                tmem_st16(tmem + at + 16 * c, y[c]);             // P^T of this half over its own S^T columns
+                    for (int e = 0; e < 16; ++e) y[c][e] = pack_bf16(__uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1]));
+                    tmem_st16(tmem + at64 + 16 * c, y[c]);       // P^T of this half over its own S^T columns
+                    tmem_st_wait();
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full + 8 * c);
+                }
+                ok = warp_wait(dp_full, n & 1, s_abort);
+                if (!ok) continue;
+                fence_after();
+                tmem_ld32(tmem + kY + at64, d[0]);
+                tmem_ld32(tmem + kY + at64 + 32, d[1]);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    auto nd = [&](int e) { return *reinterpret_cast<const uint64_t*>(stat + kQTile + 32 * c + e); };
+                    chunk_ds(s[c], d[c], nd, y[c]);
+                    tmem_st16(tmem + kY + at64 + 16 * c, y[c]);  // dS^T over this half's own dP^T columns, which are in registers
+                }
                 tmem_st_wait();
                 fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + 8 * c);
+                if (lane == 0) { mbar_arrive(ds_full); mbar_arrive(stat_empty + 8 * st); }
             }
-
-            ok = warp_wait(dp_full, j & 1, s_abort);
-            if (!ok) break;
+            if (x.n > 0 && ok) ok = warp_wait2(y_free + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, x_free + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, s_abort);
             fence_after();
-            tmem_ld32(tmem + kY + at, d[0]);
-            tmem_ld32(tmem + kY + at + 32, d[1]);
-            tmem_ld_wait();
+            const float sv = ok ? 1.f : nan_f(), sk = ok ? a.scale : nan_f();
+            const bool to_part = a.sink_segs > 0 && is_sink && valid;        // rows that several items share go to the join, in fp32
+            // every thread reads its half of the columns; a warp may hold rows of both kinds
+            const size_t row = (size_t)(x.k_row + q * 32 + lane);
+            bf16* dk = static_cast<bf16*>(a.dk) + row * a.dk_stride + (size_t)x.kvh * DH;
+            bf16* dv = static_cast<bf16*>(a.dv) + row * a.dv_stride + (size_t)x.kvh * DH;
+            float* part = nullptr;
+            if (to_part) part = a.sink_part + ((((size_t)x.b * a.Hkv + x.kvh) * (1 + a.sink_segs) + (1 + x.seg)) * a.sink_rows + key) * 2 * DH;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                auto nd = [&](int x) { return *reinterpret_cast<const uint64_t*>(stat + kQTile + 32 * c + x); };
-                if (full) chunk_ds<false>(s[c], d[c], nd, y[c]);
-                else chunk_ds<true>(s[c], d[c], nd, y[c]);
-                tmem_st16(tmem + kY + at + 16 * c, y[c]);        // dS^T over this half's own dP^T columns, which are in registers
-            }
-            tmem_st_wait();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) { mbar_arrive(ds_full); mbar_arrive(stat_empty + 8 * st); }
-        }
-        if (J > 0) {
-            if (ok) ok = warp_wait(y_free + 8 * ((J - 1) & 1), ((J - 1) >> 1) & 1, s_abort);
-            if (ok) ok = warp_wait(x_free + 8 * ((J - 1) & 1), ((J - 1) >> 1) & 1, s_abort);
-        }
-        fence_after();
-        const float sv = ok ? 1.f : nan_f(), sk = ok ? a.scale : nan_f();
-        const uint32_t lanes = static_cast<uint32_t>(q * 32) << 16;
-        const bool to_part = a.sink_segs > 0 && is_sink && valid;        // rows that several CTAs share go to the join, in fp32
-        // every thread reads its half of the columns; a warp may hold rows of both kinds
-        const size_t row = (size_t)(k_row + q * 32 + lane);
-        bf16* dk = static_cast<bf16*>(a.dk) + row * a.dk_stride + (size_t)kvh * DH;
-        bf16* dv = static_cast<bf16*>(a.dv) + row * a.dv_stride + (size_t)kvh * DH;
-        float* part = nullptr;
-        if (to_part)
-            part = a.sink_part + ((((size_t)b * a.Hkv + kvh) * (1 + a.sink_segs) + (sink_part ? 1 + seg : 0)) * a.sink_rows + key) * 2 * DH;
+            for (int c = 0; c < DH / 2; c += 32) {
+                const int col = half * (DH / 2) + c;
+                uint32_t u[32], v[32];
+                if (x.n > 0) { tmem_ld32(tmem + kDV + col + lanes, u); tmem_ld32(tmem + kDK + col + lanes, v); tmem_ld_wait(); }
+                else {
 #pragma unroll
-        for (int c = 0; c < DH / 2; c += 32) {
-            const int col = half * (DH / 2) + c;
-            uint32_t x[32], y[32];
-            if (J > 0) { tmem_ld32(tmem + kDV + col + lanes, x); tmem_ld32(tmem + kDK + col + lanes, y); tmem_ld_wait(); }
-            else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = y[i] = 0u;
-            }
-            if (to_part) {
-#pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    *reinterpret_cast<float4*>(part + col + i) = make_float4(__uint_as_float(x[i]) * sv, __uint_as_float(x[i + 1]) * sv, __uint_as_float(x[i + 2]) * sv, __uint_as_float(x[i + 3]) * sv);
-                    *reinterpret_cast<float4*>(part + DH + col + i) = make_float4(__uint_as_float(y[i]) * sk, __uint_as_float(y[i + 1]) * sk, __uint_as_float(y[i + 2]) * sk, __uint_as_float(y[i + 3]) * sk);
+                    for (int i = 0; i < 32; ++i) u[i] = v[i] = 0u;
                 }
-            } else if (valid && !sink_part) {
+                if (to_part) {
 #pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    uint32_t u[4], v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        u[e] = pack_bf16(__uint_as_float(x[i + 2 * e]) * sv, __uint_as_float(x[i + 2 * e + 1]) * sv);
-                        v[e] = pack_bf16(__uint_as_float(y[i + 2 * e]) * sk, __uint_as_float(y[i + 2 * e + 1]) * sk);
+                    for (int i = 0; i < 32; i += 4) {
+                        *reinterpret_cast<float4*>(part + col + i) = make_float4(__uint_as_float(u[i]) * sv, __uint_as_float(u[i + 1]) * sv, __uint_as_float(u[i + 2]) * sv, __uint_as_float(u[i + 3]) * sv);
+                        *reinterpret_cast<float4*>(part + DH + col + i) = make_float4(__uint_as_float(v[i]) * sk, __uint_as_float(v[i + 1]) * sk, __uint_as_float(v[i + 2]) * sk, __uint_as_float(v[i + 3]) * sk);
                     }
-                    *reinterpret_cast<uint4*>(dv + col + i) = make_uint4(u[0], u[1], u[2], u[3]);
-                    *reinterpret_cast<uint4*>(dk + col + i) = make_uint4(v[0], v[1], v[2], v[3]);
+                } else if (valid && !sink_part) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        uint32_t e[4], f[4];
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            e[z] = pack_bf16(__uint_as_float(u[i + 2 * z]) * sv, __uint_as_float(u[i + 2 * z + 1]) * sv);
+                            f[z] = pack_bf16(__uint_as_float(v[i + 2 * z]) * sk, __uint_as_float(v[i + 2 * z + 1]) * sk);
+                        }
+                        *reinterpret_cast<uint4*>(dv + col + i) = make_uint4(e[0], e[1], e[2], e[3]);
+                        *reinterpret_cast<uint4*>(dk + col + i) = make_uint4(f[0], f[1], f[2], f[3]);
+                    }
                 }
             }
+            fence_before();                                      // the accumulators have been read before the next item's P^T is announced
         }
     }
     fence_before();
@@ -778,9 +896,12 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
                    cudaFuncSetAttribute(window_bwd_kv_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, SK::kBytes) == cudaSuccess;
         }))
         return -1;
+    const int sms = device_sm_count();
     int launched = 0;
     if (hq) {
-        window_bwd_q_kernel<DH><<<dim3(s.item[a.batch], a.Hq), kThreads, SQ::kBytes, stream>>>(mq, mdo, mk64, mv64, a, s);
+        const long long items = (long long)s.item[a.batch] * a.Hq;
+        if (items > 0x3fffffff) return -1;
+        window_bwd_q_kernel<DH><<<(unsigned)(items < sms ? items : sms), kQThreads, SQ::kBytes, stream>>>(mq, mdo, mk64, mv64, a, s);
         ++launched;
     }
     if (hk) {
@@ -788,7 +909,13 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
         t.item[0] = 0;
         for (int b = 0; b < a.batch; ++b) t.item[b + 1] = t.item[b] + (s.kv_len[b] + kKTile - 1) / kKTile + a.sink_tiles * a.sink_segs;
         if (t.item[a.batch] > 0) {
-            window_bwd_kv_kernel<DH><<<dim3(t.item[a.batch], a.Hkv), kThreads, SK::kBytes, stream>>>(mq, mdo, mk, mv, a, t);
+            const long long items = (long long)t.item[a.batch] * a.Hkv;
+            if (items > 0x3fffffff) return -1;
+            // Items of many jobs run as CTAs of their own (their start-up is small beside them and the hardware balances them:
+            // 17 tiles x 4 heads 747 us against 844 as a fixed share per SM), short ones share a pipeline (5 tiles: 424 against 477).
+            const long long jobs = ((long long)(a.window < 1 << 24 ? a.window : 1 << 24) + 2 * kKTile) / kQTile * a.G;
+            const bool share = jobs < 24 && items > sms;
+            window_bwd_kv_kernel<DH><<<(unsigned)(share ? sms : items), kThreads, SK::kBytes, stream>>>(mq, mdo, mk, mv, a, t);
             ++launched;
             if (a.sink_segs > 0) {
                 window_sink_join_kernel<DH><<<dim3(a.sink_rows, a.Hkv, a.batch), 2 * DH, 0, stream>>>(a, t);

@@ -29,7 +29,6 @@ using namespace tc;
 constexpr int kThreads = 192;            // warp 0: TMA producer, warp 1: MMA issuer, warps 2-5: softmax
 constexpr int kCols = 64;                // keys of a tile
 constexpr float kSlack = 8.f;
-constexpr int kPoly = 3;                 // of every eight pairs of exponentials, those on the multiply-add pipe
 
 template <int DH>
 struct FwdSmem {
@@ -69,22 +68,14 @@ __device__ __forceinline__ float chunk_max(uint32_t* r, uint32_t vis, float mx) 
     return fmaxf(mx, y);
 }
 // exp2(S * scale + neg) of 32 columns as bf16 pairs; their sum (of the unrounded weights) is added to `sum`.
-template <bool MASK>
 __device__ __forceinline__ void chunk_exp(const uint32_t* r, uint64_t scale2, uint64_t neg2, uint32_t* p, uint64_t& sum0, uint64_t& sum1) {
 #pragma unroll
     for (int x = 0; x < 32; x += 4) {
         float e[4];
+        un2(fma2(pk2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), scale2, neg2), e[0], e[1]);
+        un2(fma2(pk2(__uint_as_float(r[x + 2]), __uint_as_float(r[x + 3])), scale2, neg2), e[2], e[3]);
 #pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-            const uint64_t z = fma2(pk2(__uint_as_float(r[x + i]), __uint_as_float(r[x + i + 1])), scale2, neg2);
-            if (!MASK && poly_pair<kPoly>(x + i)) {              // (a masked score, -inf, needs an exact 0)
-                exp2_poly2(z, e[i], e[i + 1]);
-            } else {
-                un2(z, e[i], e[i + 1]);
-                e[i] = exp2f(e[i]);
-                e[i + 1] = exp2f(e[i + 1]);
-            }
-        }
+        for (int i = 0; i < 4; ++i) e[i] = exp2f(e[i]);
         sum0 = add2(sum0, pk2(e[0], e[1]));
         sum1 = add2(sum1, pk2(e[2], e[3]));
         p[x >> 1] = pack_bf16(e[0], e[1]);
@@ -287,12 +278,10 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_kernel(const __grid_co
             const uint64_t neg2 = pk2(neg, neg);
             uint64_t sum0 = 0, sum1 = 0;                         // row sum in fp32 over the unrounded weights
             uint32_t p[16];
-            if (full) chunk_exp<false>(r[0], scale2, neg2, p, sum0, sum1);
-            else chunk_exp<true>(r[0], scale2, neg2, p, sum0, sum1);
+            chunk_exp(r[0], scale2, neg2, p, sum0, sum1);
             tmem_st16(ts, p);                                    // over S: this thread has its row in registers
             if (two) {
-                if (full) chunk_exp<false>(r[1], scale2, neg2, p, sum0, sum1);
-                else chunk_exp<true>(r[1], scale2, neg2, p, sum0, sum1);
+                chunk_exp(r[1], scale2, neg2, p, sum0, sum1);
                 tmem_st16(ts + 16, p);
             }
             float x0, x1;
