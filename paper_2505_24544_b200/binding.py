@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import weakref
+from array import array
 from typing import Dict, Optional, Sequence, Tuple
 
 import torch
@@ -63,7 +64,7 @@ class BeaglePages(C.Structure):
 
 class BeagleWindowAttn(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q_dev", "k_dev", "v_dev")] + [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + \
-               [(n, C.POINTER(C.c_int32)) for n in ("q_len_host", "kv_len_host")] + \
+               [(n, C.c_void_p) for n in ("q_len_host", "kv_len_host")] + \
                [(n, C.c_int32) for n in ("batch", "dtype", "n_q_heads", "n_kv_heads", "head_dim", "window", "sinks", "strict")]
 
 
@@ -138,13 +139,13 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     pg, i64 = C.POINTER(BeaglePages), C.c_int64
     lib.beagle_pages_workspace_bytes.argtypes = [pg, szp]
     lib.beagle_pages_reset.argtypes = [pg, vp]
-    lib.beagle_pages_append.argtypes = [pg, i32, i32p, i32, vp, vp, i64, vp, i64, vp, vp]
-    lib.beagle_pages_truncate.argtypes = [pg, i32, i32p, vp, vp]
-    lib.beagle_pages_fork.argtypes = [pg, i32, i32p, i32p, vp]
-    lib.beagle_pages_copy.argtypes = [pg, i32, i32p, i32p, vp, vp]
+    lib.beagle_pages_append.argtypes = [pg, i32, vp, i32, vp, vp, i64, vp, i64, vp, vp]
+    lib.beagle_pages_truncate.argtypes = [pg, i32, vp, vp, vp]
+    lib.beagle_pages_fork.argtypes = [pg, i32, vp, vp, vp]
+    lib.beagle_pages_copy.argtypes = [pg, i32, vp, vp, vp, vp]
     lib.beagle_pages_compact.argtypes = [pg, vp]
     lib.beagle_paged_attn_workspace_bytes.argtypes = [pg, i32, szp]
-    lib.beagle_paged_attn.argtypes = [pg, i32, i32p, i32, vp, i64, i32, i32, vp, vp, vp, C.c_size_t, vp]
+    lib.beagle_paged_attn.argtypes = [pg, i32, vp, i32, vp, i64, i32, i32, vp, vp, vp, C.c_size_t, vp]
     for name in ("workspace_bytes", "reset", "append", "truncate", "fork", "copy", "compact"):
         getattr(lib, "beagle_pages_" + name).restype = C.c_int
     lib.beagle_paged_attn_workspace_bytes.restype = C.c_int
@@ -184,7 +185,8 @@ def _i32_array(values: Sequence[int]):
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # the raw handle of torch.cuda.current_stream(), without the Stream object around it (3 us a call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def torch_dtype(dtype_code: int) -> torch.dtype:
@@ -520,11 +522,16 @@ def beagle_profile_read(ctx: Context) -> Dict[str, Tuple[float, int]]:
 
 # ---- key/value states in pages -----------------------------------------------------------------
 
+def _host_i32(values: Sequence[int]) -> bytes:
+    """A host list as int32 words, read by the library before the call returns."""
+    return array("i", values).tobytes()
+
+
 def _check(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], dense: bool = True) -> int:
     """The tensor's address, after checking its type, shape, layout and that it lies on the current device."""
-    if t.dtype != dtype or tuple(t.shape) != shape:
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{name}: must be on the current CUDA device")
     if dense and not t.is_contiguous():
         raise ValueError(f"{name}: tensor must be contiguous")
@@ -536,6 +543,8 @@ def _row_stride(name: str, t: torch.Tensor, lead: int) -> int:
     `lead` dimensions count rows at one distance (a dense tensor, or a slice of a fused projection)."""
     heads, dh = t.shape[lead:]
     st = t.stride()
+    if t.is_contiguous():
+        return heads * dh
     if (dh > 1 and st[-1] != 1) or (heads > 1 and st[-2] != dh):
         raise ValueError(f"{name}: the heads of a row must be dense")
     if lead == 2 and t.shape[1] > 1:
@@ -588,7 +597,7 @@ class PagedCache:
 
     def on_current_device(self) -> int:
         """The current stream, after checking that the cache lies on the current device."""
-        if self.k.device.index != torch.cuda.current_device():
+        if self.k.get_device() != torch.cuda.current_device():
             raise ValueError("the cache must be on the current CUDA device")
         return _stream()
 
@@ -611,20 +620,20 @@ def beagle_pages_append(cache: PagedCache, slots: Sequence[int], k_new: torch.Te
     kp, vp = _check("k_new", k_new, cache.k.dtype, shape, False), _check("v_new", v_new, cache.k.dtype, shape, False)
     n_ptr = None if n_new is None else _check("n_new", n_new, torch.int32, (B,))
     ok_ptr = None if ok is None else _check("ok", ok, torch.int32, (B,))
-    _pages_ok(cache.lib.beagle_pages_append(cache.ref, B, _i32_array(slots), shape[1], n_ptr, kp, _row_stride("k_new", k_new, 2), vp,
+    _pages_ok(cache.lib.beagle_pages_append(cache.ref, B, _host_i32(slots), shape[1], n_ptr, kp, _row_stride("k_new", k_new, 2), vp,
                                             _row_stride("v_new", v_new, 2), ok_ptr, cache.on_current_device()), "beagle_pages_append")
 
 
 def beagle_pages_truncate(cache: PagedCache, slots: Sequence[int], keep: Optional[torch.Tensor] = None) -> None:
     """Cuts the slots to ``keep`` positions (int32 on the device; None: frees them)."""
     keep_ptr = None if keep is None else _check("keep", keep, torch.int32, (len(slots),))
-    _pages_ok(cache.lib.beagle_pages_truncate(cache.ref, len(slots), _i32_array(slots), keep_ptr, cache.on_current_device()), "beagle_pages_truncate")
+    _pages_ok(cache.lib.beagle_pages_truncate(cache.ref, len(slots), _host_i32(slots), keep_ptr, cache.on_current_device()), "beagle_pages_truncate")
 
 
 def _pairs(src: Sequence[int], dst: Sequence[int]):
     if len(src) != len(dst):
         raise ValueError("src and dst must have the same length")
-    return len(src), _i32_array(src), _i32_array(dst)
+    return len(src), _host_i32(src), _host_i32(dst)
 
 
 def beagle_pages_fork(cache: PagedCache, src: Sequence[int], dst: Sequence[int]) -> None:
@@ -667,7 +676,7 @@ def beagle_paged_attn(cache: PagedCache, slots: Sequence[int], q: torch.Tensor, 
     need = beagle_paged_attn_workspace_bytes(cache, hq)
     if ws is None:
         ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _pages_ok(cache.lib.beagle_paged_attn(cache.ref, B, _i32_array(slots), hq, qp, _row_stride("q", q, 1), window, sinks, op, lp,
+    _pages_ok(cache.lib.beagle_paged_attn(cache.ref, B, _host_i32(slots), hq, qp, _row_stride("q", q, 1), window, sinks, op, lp,
                                           ws.data_ptr(), ws.numel() * ws.element_size(), stream), "beagle_paged_attn")
 
 
@@ -688,7 +697,8 @@ def _window_attn(q, k, v, q_len, kv_len, window, sinks, strict) -> Tuple[BeagleW
     w.k_dev = _check("k", k, q.dtype, (nk, hkv, dh), False)
     w.v_dev = _check("v", v, q.dtype, (nk, hkv, dh), False)
     w.q_stride, w.k_stride, w.v_stride = _row_stride("q", q, 1), _row_stride("k", k, 1), _row_stride("v", v, 1)
-    w.q_len_host, w.kv_len_host = _i32_array(q_len), _i32_array(kv_len)
+    w.hosts = array("i", q_len), array("i", kv_len)             # kept alive by the structure
+    w.q_len_host, w.kv_len_host = (x.buffer_info()[0] for x in w.hosts)
     w.batch, w.dtype = len(q_len), BEAGLE_BF16 if q.dtype == torch.bfloat16 else BEAGLE_FP32
     w.n_q_heads, w.n_kv_heads, w.head_dim = hq, hkv, dh
     w.window, w.sinks, w.strict = window, sinks, int(strict)

@@ -391,7 +391,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 // ------------------------------------------------------------------------------------------------
 template <typename T, int DH, int GM>
 __global__ void __launch_bounds__(kConsumers * 32) paged_attn_simt_kernel(const __grid_constant__ PagedArgs a) {
-    constexpr int VN = VecOf<T>::N, LPK = DH / VN, KPW = 32 / LPK, U = 2;      // U positions in flight per group
+    constexpr int VN = VecOf<T>::N, LPK = DH / VN, KPW = 32 / LPK, kSteps = (kPerWarp + KPW - 1) / KPW;
+    constexpr int kMost = GM <= 2 ? 8 : GM == 4 ? 4 : 2, U = kSteps < kMost ? kSteps : kMost;      // positions in flight per group
     __shared__ Schedule s;
     __shared__ float s_o[kConsumers][GM][DH], s_m[kConsumers][GM], s_l[kConsumers][GM];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LPK, sub = lane % LPK;

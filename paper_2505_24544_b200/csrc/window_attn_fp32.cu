@@ -1,9 +1,11 @@
 // The windowed attention in fp32 (forward and backward), head_dim 16 | 32 | 64 | 128, on the CUDA cores: the tiny head's type,
 // for which exactness counts more than rate (no tensor-core product keeps 24 bits).
 //
-// Tiles of 64 queries x 64 keys; 256 threads as 16 x 16, each with a 4 x 4 piece of S (operands read as 16-byte vectors from
-// padded shared-memory rows, 64 fused multiply-adds per 8 loads) and with its 4 rows x head_dim / 16 columns of the accumulators.
-// The 16 threads of a row are half a warp, so row maxima, sums and the hand-over of P through shared memory need no CTA barrier.
+// Tiles of R x 64 (R = 64 or 32 rows: queries, or keys on the key side; R = 32 while 64 would leave SMs without a CTA); 256
+// threads as 16 x 16, each with an R/16 x 4 piece of S (operands read as 16-byte vectors from padded shared-memory rows) and
+// with its R/16 rows x head_dim / 16 columns of the accumulators.  The 16 threads of a row are half a warp, so row maxima, sums
+// and the hand-over of P through shared memory need no CTA barrier.  The streamed tiles come by cp.async, the next one under
+// this one's work where shared memory holds two.
 // Backward as in the bf16 kernels: a query side (dQ, and delta) and a key side (dK, dV); the key side gives every query head its
 // own CTA and, where heads share keys, leaves fp32 partials that a last launch adds in the order of the heads.
 #include "window_attn.h"
@@ -21,46 +23,52 @@ constexpr int kPRow = kT + kPad;
 
 __device__ __forceinline__ bool visible(int key, int last, const WinArgs& a) { return key <= last && (key > last - a.window || key < a.sinks); }
 
-// Rows [r0, r0 + 64) of a packed matrix (column offset `col`) into shared memory; rows at and past `rows` as zero.
-template <int DH>
+__device__ __forceinline__ void cp_async16(float* dst, const float* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Rows [r0, r0 + R) of a packed matrix (column offset `col`) on their way into shared memory; rows at and past `rows` as zero.
+template <int DH, int R>
 __device__ __forceinline__ void load_tile(float* dst, const float* src, long long stride, int r0, int rows, size_t col) {
-    for (int i = threadIdx.x; i < kT * (DH / 4); i += kThreads) {
+#pragma unroll
+    for (int i = threadIdx.x; i < R * (DH / 4); i += kThreads) {
         const int r = i / (DH / 4), c = i % (DH / 4);
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r0 + r < rows) x = *reinterpret_cast<const float4*>(src + (size_t)(r0 + r) * stride + col + 4 * c);
-        *reinterpret_cast<float4*>(dst + r * row_len<DH>() + 4 * c) = x;
+        const bool there = r0 + r < rows;
+        cp_async16(dst + r * row_len<DH>() + 4 * c, src + (size_t)(there ? r0 + r : 0) * stride + col + 4 * c, there);
     }
 }
-// acc[r][c] = <A row (4 ty + r), B row (tx + 16 c)>
-template <int DH>
-__device__ __forceinline__ void dots(const float* A, const float* B, int ty, int tx, float acc[4][4]) {
+// acc[r][c] = <A row (RT ty + r), B row (tx + 16 c)>
+template <int DH, int RT>
+__device__ __forceinline__ void dots(const float* A, const float* B, int ty, int tx, float acc[RT][4]) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int c = 0; c < 4; ++c) acc[r][c] = 0.f;
 #pragma unroll 4
     for (int d = 0; d < DH; d += 4) {
-        float4 x[4], y[4];
+        float4 x[RT], y[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = *reinterpret_cast<const float4*>(A + (4 * ty + r) * row_len<DH>() + d);
+        for (int r = 0; r < RT; ++r) x[r] = *reinterpret_cast<const float4*>(A + (RT * ty + r) * row_len<DH>() + d);
 #pragma unroll
         for (int c = 0; c < 4; ++c) y[c] = *reinterpret_cast<const float4*>(B + (tx + 16 * c) * row_len<DH>() + d);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int c = 0; c < 4; ++c)
                 acc[r][c] = fmaf(x[r].x, y[c].x, fmaf(x[r].y, y[c].y, fmaf(x[r].z, y[c].z, fmaf(x[r].w, y[c].w, acc[r][c]))));
     }
 }
-// acc[r][e] += sum_k P[4 ty + r][k] X[k][tx + 16 e]
-template <int DH>
-__device__ __forceinline__ void weigh(const float* P, const float* X, int ty, int tx, float acc[4][DH / 16]) {
+// acc[r][e] += sum_k P[RT ty + r][k] X[k][tx + 16 e]
+template <int DH, int RT>
+__device__ __forceinline__ void weigh(const float* P, const float* X, int ty, int tx, float acc[RT][DH / 16]) {
 #pragma unroll 2
     for (int k = 0; k < kT; k += 4) {
-        float p[4][4];
+        float p[RT][4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float4 t = *reinterpret_cast<const float4*>(P + (4 * ty + r) * kPRow + k);
+        for (int r = 0; r < RT; ++r) {
+            const float4 t = *reinterpret_cast<const float4*>(P + (RT * ty + r) * kPRow + k);
             p[r][0] = t.x; p[r][1] = t.y; p[r][2] = t.z; p[r][3] = t.w;
         }
 #pragma unroll
@@ -69,22 +77,30 @@ __device__ __forceinline__ void weigh(const float* P, const float* X, int ty, in
             for (int e = 0; e < DH / 16; ++e) {
                 const float x = X[(k + i) * row_len<DH>() + tx + 16 * e];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[r][e] = fmaf(p[r][i], x, acc[r][e]);
+                for (int r = 0; r < RT; ++r) acc[r][e] = fmaf(p[r][i], x, acc[r][e]);
             }
     }
 }
-__device__ __forceinline__ void put(float* P, int ty, int tx, const float v[4][4]) {
+template <int RT>
+__device__ __forceinline__ void put(float* P, int ty, int tx, const float v[RT][4]) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) P[(4 * ty + r) * kPRow + tx + 16 * c] = v[r][c];
+        for (int c = 0; c < 4; ++c) P[(RT * ty + r) * kPRow + tx + 16 * c] = v[r][c];
 }
+// Shared memory: NR resident and 2 * stages streamed tiles, NP tiles of P; two stages where they fit.
+template <int DH, int R, int NR, int NP>
+struct Fp32Smem {
+    static constexpr int kRes = R * (DH + kPad), kStr = kT * (DH + kPad), kP = R * kPRow;
+    static constexpr int kStages = (NR * kRes + 4 * kStr + NP * kP) * 4 <= 227 * 1024 ? 2 : 1;
+    static constexpr int kBytes = (NR * kRes + 2 * kStages * kStr + NP * kP) * 4;
+};
 
-// The key tiles of the queries [q0, q0 + 64): sinks in front of the window, then the band.
+// The key tiles of the queries [q0, q0 + R): sinks in front of the window, then the band.
 struct Keys {
     int lo, hi, sink_end, n_sink, n;
-    __device__ __forceinline__ void init(int q0, int q_len, int shift, const WinArgs& a) {
-        hi = min(q0 + kT, q_len) + shift;
+    __device__ __forceinline__ void init(int q0, int rows, int q_len, int shift, const WinArgs& a) {
+        hi = min(q0 + rows, q_len) + shift;
         lo = max(0, q0 + shift - a.window + 1);
         sink_end = min(a.sinks, lo);
         n_sink = (sink_end + kT - 1) / kT;
@@ -96,37 +112,52 @@ struct Keys {
     }
 };
 
-template <int DH>
+template <int DH, int R>
 __global__ void __launch_bounds__(kThreads) window_fwd_fp32_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
     extern __shared__ __align__(16) float sm[];
-    float *Q = sm, *K = Q + kT * row_len<DH>(), *V = K + kT * row_len<DH>(), *P = V + kT * row_len<DH>();
+    using SM = Fp32Smem<DH, R, 1, 1>;
+    constexpr int RT = R / 16;
+    float *Q = sm, *KV = Q + SM::kRes, *P = KV + 2 * SM::kStages * SM::kStr;       // stage s: K at KV + 2 s kStr, V behind it
     int tile;
     const int b = win_find(seqs.item, a.batch, blockIdx.x, tile);
     const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
-    const int q0 = ((q_len + kT - 1) / kT - 1 - tile) * kT, h = blockIdx.y, kvh = h / a.G;
+    const int q0 = ((q_len + R - 1) / R - 1 - tile) * R, h = blockIdx.y, kvh = h / a.G;
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-    load_tile<DH>(Q, static_cast<const float*>(a.q) + (size_t)seqs.q_start[b] * a.q_stride, a.q_stride, q0, q_len, (size_t)h * DH);
+    load_tile<DH, R>(Q, static_cast<const float*>(a.q) + (size_t)seqs.q_start[b] * a.q_stride, a.q_stride, q0, q_len, (size_t)h * DH);
+    cp_commit();
     Keys w;
-    w.init(q0, q_len, shift, a);
-    float o[4][DH / 16], m[4], l[4];
+    w.init(q0, R, q_len, shift, a);
+    float o[RT][DH / 16], m[RT], l[RT];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RT; ++r) {
         m[r] = -INFINITY; l[r] = 0.f;
 #pragma unroll
         for (int e = 0; e < DH / 16; ++e) o[r][e] = 0.f;
     }
+    auto load_kv = [&](int j) {
+        int start, end;
+        w.tile(j, start, end);
+        float* dst = KV + (j % SM::kStages) * 2 * SM::kStr;
+        load_tile<DH, kT>(dst, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, start, end, (size_t)kvh * DH);
+        load_tile<DH, kT>(dst + SM::kStr, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, start, end, (size_t)kvh * DH);
+        cp_commit();
+    };
+    if (SM::kStages == 2 && w.n > 0) load_kv(0);
     for (int j = 0; j < w.n; ++j) {
         int start, end;
         w.tile(j, start, end);
-        __syncthreads();                                 // the previous tile has been read
-        load_tile<DH>(K, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, start, end, (size_t)kvh * DH);
-        load_tile<DH>(V, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, start, end, (size_t)kvh * DH);
+        __syncthreads();                                 // the tile that the next copy overwrites has been read
+        if (SM::kStages == 1) load_kv(j);
+        else if (j + 1 < w.n) load_kv(j + 1);
+        if (SM::kStages == 2 && j + 1 < w.n) cp_wait<1>();
+        else cp_wait<0>();
         __syncthreads();
-        float s[4][4];
-        dots<DH>(Q, K, ty, tx, s);
+        const float *K = KV + (j % SM::kStages) * 2 * SM::kStr, *V = K + SM::kStr;
+        float s[RT][4];
+        dots<DH, RT>(Q, K, ty, tx, s);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int last = q0 + 4 * ty + r + shift;
+        for (int r = 0; r < RT; ++r) {
+            const int last = q0 + RT * ty + r + shift;
             float mx = -INFINITY;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -149,16 +180,16 @@ __global__ void __launch_bounds__(kThreads) window_fwd_fp32_kernel(const __grid_
                 l[r] += s[r][c];
             }
         }
-        put(P, ty, tx, s);
+        put<RT>(P, ty, tx, s);
         __syncwarp();                                    // a row's 16 threads are half of one warp
-        weigh<DH>(P, V, ty, tx, o);
+        weigh<DH, RT>(P, V, ty, tx, o);
         __syncwarp();
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RT; ++r) {
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
-        const int i = q0 + 4 * ty + r;
+        const int i = q0 + RT * ty + r;
         if (i >= q_len) continue;
         const size_t row = ((size_t)(seqs.q_start[b] + i) * a.Hq + h);
         const float inv = l[r] > 0.f ? __fdiv_rn(1.f, l[r]) : 0.f;
@@ -174,28 +205,32 @@ __device__ __forceinline__ int stat_row0(const WinSeqs& s, int b) {
     return at;
 }
 
-template <int DH>
+template <int DH, int R>
 __global__ void __launch_bounds__(kThreads) window_bwd_q_fp32_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
     extern __shared__ __align__(16) float sm[];
-    float *Q = sm, *dO = Q + kT * row_len<DH>(), *K = dO + kT * row_len<DH>(), *V = K + kT * row_len<DH>(), *P = V + kT * row_len<DH>();
+    using SM = Fp32Smem<DH, R, 2, 1>;
+    constexpr int RT = R / 16;
+    float *Q = sm, *dO = Q + SM::kRes, *KV = dO + SM::kRes, *P = KV + 2 * SM::kStages * SM::kStr;
     int tile;
     const int b = win_find(seqs.item, a.batch, blockIdx.x, tile);
     const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
-    const int q0 = ((q_len + kT - 1) / kT - 1 - tile) * kT, h = blockIdx.y, kvh = h / a.G;
+    const int q0 = ((q_len + R - 1) / R - 1 - tile) * R, h = blockIdx.y, kvh = h / a.G;
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-    load_tile<DH>(Q, static_cast<const float*>(a.q) + (size_t)seqs.q_start[b] * a.q_stride, a.q_stride, q0, q_len, (size_t)h * DH);
-    load_tile<DH>(dO, static_cast<const float*>(a.dout) + (size_t)seqs.q_start[b] * a.dout_stride, a.dout_stride, q0, q_len, (size_t)h * DH);
+    load_tile<DH, R>(Q, static_cast<const float*>(a.q) + (size_t)seqs.q_start[b] * a.q_stride, a.q_stride, q0, q_len, (size_t)h * DH);
+    load_tile<DH, R>(dO, static_cast<const float*>(a.dout) + (size_t)seqs.q_start[b] * a.dout_stride, a.dout_stride, q0, q_len, (size_t)h * DH);
+    cp_commit();
+    cp_wait<0>();
     __syncthreads();
-    float lse2[4], delta[4], dq[4][DH / 16];
+    float lse2[RT], delta[RT], dq[RT][DH / 16];
     const int stat0 = stat_row0(seqs, b);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int i = q0 + 4 * ty + r;
+    for (int r = 0; r < RT; ++r) {
+        const int i = q0 + RT * ty + r;
         const size_t row = (size_t)(seqs.q_start[b] + min(i, q_len - 1)) * a.Hq + h;
         float t = 0.f;
 #pragma unroll
         for (int e = 0; e < DH / 16; ++e) {
-            t = fmaf(dO[(4 * ty + r) * row_len<DH>() + tx + 16 * e], static_cast<const float*>(a.out)[row * DH + tx + 16 * e], t);
+            t = fmaf(dO[(RT * ty + r) * row_len<DH>() + tx + 16 * e], static_cast<const float*>(a.out)[row * DH + tx + 16 * e], t);
             dq[r][e] = 0.f;
         }
 #pragma unroll
@@ -210,34 +245,46 @@ __global__ void __launch_bounds__(kThreads) window_bwd_q_fp32_kernel(const __gri
         }
     }
     Keys w;
-    w.init(q0, q_len, shift, a);
+    w.init(q0, R, q_len, shift, a);
+    auto load_kv = [&](int j) {
+        int start, end;
+        w.tile(j, start, end);
+        float* dst = KV + (j % SM::kStages) * 2 * SM::kStr;
+        load_tile<DH, kT>(dst, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, start, end, (size_t)kvh * DH);
+        load_tile<DH, kT>(dst + SM::kStr, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, start, end, (size_t)kvh * DH);
+        cp_commit();
+    };
+    if (SM::kStages == 2 && w.n > 0) load_kv(0);
     for (int j = 0; j < w.n; ++j) {
         int start, end;
         w.tile(j, start, end);
+        __syncthreads();                                 // the tile that the next copy overwrites has been read
+        if (SM::kStages == 1) load_kv(j);
+        else if (j + 1 < w.n) load_kv(j + 1);
+        if (SM::kStages == 2 && j + 1 < w.n) cp_wait<1>();
+        else cp_wait<0>();
         __syncthreads();
-        load_tile<DH>(K, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, start, end, (size_t)kvh * DH);
-        load_tile<DH>(V, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, start, end, (size_t)kvh * DH);
-        __syncthreads();
-        float s[4][4], dp[4][4];
-        dots<DH>(Q, K, ty, tx, s);
-        dots<DH>(dO, V, ty, tx, dp);
+        const float *K = KV + (j % SM::kStages) * 2 * SM::kStr, *V = K + SM::kStr;
+        float s[RT][4], dp[RT][4];
+        dots<DH, RT>(Q, K, ty, tx, s);
+        dots<DH, RT>(dO, V, ty, tx, dp);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int last = q0 + 4 * ty + r + shift;
+        for (int r = 0; r < RT; ++r) {
+            const int last = q0 + RT * ty + r + shift;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const int key = start + tx + 16 * c;
                 s[r][c] = (key < end && visible(key, last, a)) ? exp2f(fmaf(s[r][c], a.scale_log2, -lse2[r])) * (dp[r][c] - delta[r]) : 0.f;
             }
         }
-        put(P, ty, tx, s);
+        put<RT>(P, ty, tx, s);
         __syncwarp();
-        weigh<DH>(P, K, ty, tx, dq);
+        weigh<DH, RT>(P, K, ty, tx, dq);
         __syncwarp();
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int i = q0 + 4 * ty + r;
+    for (int r = 0; r < RT; ++r) {
+        const int i = q0 + RT * ty + r;
         if (i >= q_len) continue;
 #pragma unroll
         for (int e = 0; e < DH / 16; ++e)
@@ -246,55 +293,70 @@ __global__ void __launch_bounds__(kThreads) window_bwd_q_fp32_kernel(const __gri
 }
 
 // One CTA = 64 keys of one (sequence, query head).  a.sink_part (when heads share keys): fp32 [kv rows][Hq][2][DH], dV then dK.
-template <int DH>
+template <int DH, int R>
 __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
     extern __shared__ __align__(16) float sm[];
-    float *K = sm, *V = K + kT * row_len<DH>(), *Q = V + kT * row_len<DH>(), *dO = Q + kT * row_len<DH>(), *P = dO + kT * row_len<DH>(), *dS = P + kT * kPRow;
+    using SM = Fp32Smem<DH, R, 2, 2>;
+    constexpr int RT = R / 16;
+    float *K = sm, *V = K + SM::kRes, *QD = V + SM::kRes, *P = QD + 2 * SM::kStages * SM::kStr, *dS = P + SM::kP;
     int tile;
     const int b = win_find(seqs.item, a.batch, blockIdx.x, tile);
     const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
-    const int k0 = tile * kT, h = blockIdx.y, kvh = h / a.G;
+    const int k0 = tile * R, h = blockIdx.y, kvh = h / a.G;
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-    load_tile<DH>(K, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, k0, kv_len, (size_t)kvh * DH);
-    load_tile<DH>(V, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, k0, kv_len, (size_t)kvh * DH);
+    load_tile<DH, R>(K, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, k0, kv_len, (size_t)kvh * DH);
+    load_tile<DH, R>(V, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, k0, kv_len, (size_t)kvh * DH);
     const int from = max(0, k0 - shift);
-    const int to = k0 < a.sinks ? q_len : max(0, min(q_len, min(k0 + kT, kv_len) - 1 - shift + a.window));
+    const int to = k0 < a.sinks ? q_len : max(0, min(q_len, min(k0 + R, kv_len) - 1 - shift + a.window));
     const float* stats = a.stats + (size_t)h * 2 * a.stat_rows + stat_row0(seqs, b);
-    float dk[4][DH / 16], dv[4][DH / 16];
+    float dk[RT][DH / 16], dv[RT][DH / 16];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int e = 0; e < DH / 16; ++e) dk[r][e] = dv[r][e] = 0.f;
-    for (int q0 = from; q0 < to; q0 += kT) {
+    const int n = to > from ? (to - from + kT - 1) / kT : 0;
+    cp_commit();
+    auto load_qd = [&](int j) {
+        float* dst = QD + (j % SM::kStages) * 2 * SM::kStr;
+        load_tile<DH, kT>(dst, static_cast<const float*>(a.q) + (size_t)seqs.q_start[b] * a.q_stride, a.q_stride, from + j * kT, q_len, (size_t)h * DH);
+        load_tile<DH, kT>(dst + SM::kStr, static_cast<const float*>(a.dout) + (size_t)seqs.q_start[b] * a.dout_stride, a.dout_stride, from + j * kT, q_len, (size_t)h * DH);
+        cp_commit();
+    };
+    if (SM::kStages == 2 && n > 0) load_qd(0);
+    for (int j = 0; j < n; ++j) {
+        const int q0 = from + j * kT;
         __syncthreads();
-        load_tile<DH>(Q, static_cast<const float*>(a.q) + (size_t)seqs.q_start[b] * a.q_stride, a.q_stride, q0, q_len, (size_t)h * DH);
-        load_tile<DH>(dO, static_cast<const float*>(a.dout) + (size_t)seqs.q_start[b] * a.dout_stride, a.dout_stride, q0, q_len, (size_t)h * DH);
+        if (SM::kStages == 1) load_qd(j);
+        else if (j + 1 < n) load_qd(j + 1);
+        if (SM::kStages == 2 && j + 1 < n) cp_wait<1>();
+        else cp_wait<0>();
         __syncthreads();
-        float s[4][4], dp[4][4];
-        dots<DH>(K, Q, ty, tx, s);
-        dots<DH>(V, dO, ty, tx, dp);
+        const float *Q = QD + (j % SM::kStages) * 2 * SM::kStr, *dO = Q + SM::kStr;
+        float s[RT][4], dp[RT][4];
+        dots<DH, RT>(K, Q, ty, tx, s);
+        dots<DH, RT>(V, dO, ty, tx, dp);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const int i = q0 + tx + 16 * c;
             const float nl = i < q_len ? __ldg(stats + i) : 0.f, nd = i < q_len ? __ldg(stats + a.stat_rows + i) : 0.f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const bool vis = i < q_len && visible(k0 + 4 * ty + r, i + shift, a);
+            for (int r = 0; r < RT; ++r) {
+                const bool vis = i < q_len && visible(k0 + RT * ty + r, i + shift, a);
                 const float p = vis ? exp2f(fmaf(s[r][c], a.scale_log2, nl)) : 0.f;
                 s[r][c] = p;
                 dp[r][c] = vis ? p * (dp[r][c] + nd) : 0.f;
             }
         }
-        put(P, ty, tx, s);
-        put(dS, ty, tx, dp);
+        put<RT>(P, ty, tx, s);
+        put<RT>(dS, ty, tx, dp);
         __syncwarp();
-        weigh<DH>(P, dO, ty, tx, dv);
-        weigh<DH>(dS, Q, ty, tx, dk);
+        weigh<DH, RT>(P, dO, ty, tx, dv);
+        weigh<DH, RT>(dS, Q, ty, tx, dk);
         __syncwarp();
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int key = k0 + 4 * ty + r;
+    for (int r = 0; r < RT; ++r) {
+        const int key = k0 + RT * ty + r;
         if (key >= kv_len) continue;
         const size_t row = (size_t)(seqs.k_start[b] + key);
 #pragma unroll
@@ -328,40 +390,61 @@ __global__ void __launch_bounds__(256) window_group_join_fp32_kernel(const __gri
     }
 }
 
-void retile(WinSeqs& s, int batch, const int32_t* len) {
+int retile(WinSeqs& s, int batch, const int32_t* len, int rows) {
     s.item[0] = 0;
-    for (int b = 0; b < batch; ++b) s.item[b + 1] = s.item[b] + (len[b] + kT - 1) / kT;
+    for (int b = 0; b < batch; ++b) s.item[b + 1] = s.item[b] + (len[b] + rows - 1) / rows;
+    return s.item[batch];
+}
+// 64 rows a CTA unless that leaves SMs idle (three sequences of 333, 4 heads of 64: 48 CTAs of 64 rows, 88 of 32).
+bool small_rows(WinSeqs& s, int batch, const int32_t* len, int heads) { return (long long)retile(s, batch, len, 64) * heads < 148; }
+
+template <typename K, typename SM>
+bool raise_limit(K kernel, PerDeviceOnce& once, SM) {
+    return once.ensure([=] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes) == cudaSuccess; });
 }
 
-template <int DH>
-int fwd(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
-    constexpr int bytes = (3 * kT * row_len<DH>() + kT * kPRow) * 4;
-    static PerDeviceOnce attr;
-    if (!attr.ensure([] { return cudaFuncSetAttribute(window_fwd_fp32_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess; })) return -1;
-    retile(s, a.batch, s.q_len);
-    window_fwd_fp32_kernel<DH><<<dim3(s.item[a.batch], a.Hq), kThreads, bytes, stream>>>(a, s);
+template <int DH, int R>
+int fwd_rows(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
+    using SM = Fp32Smem<DH, R, 1, 1>;
+    static PerDeviceOnce once;
+    if (!raise_limit(window_fwd_fp32_kernel<DH, R>, once, SM())) return -1;
+    window_fwd_fp32_kernel<DH, R><<<dim3(retile(s, a.batch, s.q_len, R), a.Hq), kThreads, SM::kBytes, stream>>>(a, s);
+    return 1;
+}
+template <int DH, int R>
+int bwd_q_rows(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
+    using SM = Fp32Smem<DH, R, 2, 1>;
+    static PerDeviceOnce once;
+    if (!raise_limit(window_bwd_q_fp32_kernel<DH, R>, once, SM())) return -1;
+    window_bwd_q_fp32_kernel<DH, R><<<dim3(retile(s, a.batch, s.q_len, R), a.Hq), kThreads, SM::kBytes, stream>>>(a, s);
+    return 1;
+}
+template <int DH, int R>
+int bwd_kv_rows(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
+    using SM = Fp32Smem<DH, R, 2, 2>;
+    static PerDeviceOnce once;
+    if (!raise_limit(window_bwd_kv_fp32_kernel<DH, R>, once, SM())) return -1;
+    window_bwd_kv_fp32_kernel<DH, R><<<dim3(retile(s, a.batch, s.kv_len, R), a.Hq), kThreads, SM::kBytes, stream>>>(a, s);
     return 1;
 }
 
 template <int DH>
+int fwd(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
+    return small_rows(s, a.batch, s.q_len, a.Hq) ? fwd_rows<DH, 32>(a, s, stream) : fwd_rows<DH, 64>(a, s, stream);
+}
+
+template <int DH>
 int bwd(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
-    constexpr int bytes_q = (4 * kT * row_len<DH>() + kT * kPRow) * 4, bytes_k = (4 * kT * row_len<DH>() + 2 * kT * kPRow) * 4;
-    static PerDeviceOnce attr;
-    if (!attr.ensure([] {
-            return cudaFuncSetAttribute(window_bwd_q_fp32_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes_q) == cudaSuccess &&
-                   cudaFuncSetAttribute(window_bwd_kv_fp32_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes_k) == cudaSuccess;
-        }))
-        return -1;
-    int launched = 0;
-    retile(s, a.batch, s.q_len);
-    if (s.item[a.batch] > 0) {
-        window_bwd_q_fp32_kernel<DH><<<dim3(s.item[a.batch], a.Hq), kThreads, bytes_q, stream>>>(a, s);
-        ++launched;
+    int launched = 0, rc = 0;
+    if (retile(s, a.batch, s.q_len, 64) > 0) {
+        rc = small_rows(s, a.batch, s.q_len, a.Hq) ? bwd_q_rows<DH, 32>(a, s, stream) : bwd_q_rows<DH, 64>(a, s, stream);
+        if (rc < 0) return rc;
+        launched += rc;
     }
-    retile(s, a.batch, s.kv_len);
-    if (s.item[a.batch] > 0) {
-        window_bwd_kv_fp32_kernel<DH><<<dim3(s.item[a.batch], a.Hq), kThreads, bytes_k, stream>>>(a, s);
-        ++launched;
+    if (retile(s, a.batch, s.kv_len, 64) > 0) {
+        rc = small_rows(s, a.batch, s.kv_len, a.Hq) ? bwd_kv_rows<DH, 32>(a, s, stream) : bwd_kv_rows<DH, 64>(a, s, stream);
+        if (rc < 0) return rc;
+        launched += rc;
         if (a.G > 1) {
             const long long rows = (long long)s.k_start[a.batch - 1] + s.kv_len[a.batch - 1], n = rows * a.Hkv * 2 * DH;
             window_group_join_fp32_kernel<<<dim3((unsigned)((n + 255) / 256 < 148 * 8 ? (n + 255) / 256 : 148 * 8)), 256, 0, stream>>>(a, DH, rows);

@@ -21,8 +21,10 @@ def attn(**kw):
                 n_q_heads=4, n_kv_heads=2, head_dim=128, window=4, sinks=1, strict=0)
     base.update(kw)
     base.setdefault("batch", len(base["q_len_host"] or ()))
+    w.arrays = [(C.c_int32 * max(1, len(x)))(*x) for x in base.values() if isinstance(x, tuple)]         # kept alive by the structure
+    arrays = iter(w.arrays)
     for n, x in base.items():
-        setattr(w, n, (C.c_int32 * max(1, len(x)))(*x) if isinstance(x, tuple) else x)
+        setattr(w, n, C.addressof(next(arrays)) if isinstance(x, tuple) else x)
     return w
 
 
