@@ -320,9 +320,9 @@ beagle_status beagle_pages_compact(const beagle_pages* pages, void* stream);
  * fp32 [batch, n_q_heads] (nullable): ln sum_j exp(score).  An empty slot gives o = 0 and lse = -inf.  What lies in
  * positions that are not visible (NaN included) has no effect.  Scores, softmax and sums are fp32; the bf16 kernel rounds
  * the softmax weights to bf16 for the product with V.  n_q_heads / n_kv_heads: 1..8 (bf16 head_dim 256: 1..4).  ws_dev:
- * beagle_paged_attn_workspace_bytes, 16-byte aligned, contents irrelevant; two calls that may run at the same time need
- * two.  Results do not depend on timing.  A kernel that gives up on a bounded wait leaves NaN in the rows concerned. */
-beagle_status beagle_paged_attn_workspace_bytes(const beagle_pages* pages, int32_t n_q_heads, size_t* bytes);
+ * beagle_paged_attn_workspace_bytes (0, then ws_dev may be NULL, where max_pages or the window keep every row short), 16-byte
+ * aligned, contents irrelevant; two calls that may run at the same time need two.  Results do not depend on timing.  A kernel that gives up on a bounded wait leaves NaN in the rows concerned. */
+beagle_status beagle_paged_attn_workspace_bytes(const beagle_pages* pages, int32_t n_q_heads, int32_t window, int32_t sinks, size_t* bytes);
 beagle_status beagle_paged_attn(const beagle_pages* pages, int32_t batch, const int32_t* slot_host, int32_t n_q_heads, const void* q_dev,
                                 int64_t q_stride, int32_t window, int32_t sinks, void* out_dev, float* lse_dev, void* ws_dev,
                                 size_t ws_bytes, void* stream);

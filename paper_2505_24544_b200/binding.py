@@ -144,7 +144,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.beagle_pages_fork.argtypes = [pg, i32, vp, vp, vp]
     lib.beagle_pages_copy.argtypes = [pg, i32, vp, vp, vp, vp]
     lib.beagle_pages_compact.argtypes = [pg, vp]
-    lib.beagle_paged_attn_workspace_bytes.argtypes = [pg, i32, szp]
+    lib.beagle_paged_attn_workspace_bytes.argtypes = [pg, i32, i32, i32, szp]
     lib.beagle_paged_attn.argtypes = [pg, i32, vp, i32, vp, i64, i32, i32, vp, vp, vp, C.c_size_t, vp]
     for name in ("workspace_bytes", "reset", "append", "truncate", "fork", "copy", "compact"):
         getattr(lib, "beagle_pages_" + name).restype = C.c_int
@@ -593,7 +593,7 @@ class PagedCache:
         self.ws = torch.empty(n.value, dtype=torch.uint8, device=k.device)
         p.ws, p.ws_bytes = self.ws.data_ptr(), n.value
         self.struct, self.ref = p, C.byref(p)
-        self.attn_ws_bytes: Dict[int, int] = {}      # query heads -> workspace of beagle_paged_attn
+        self.attn_ws_bytes: Dict[Tuple[int, int, int], int] = {}      # (query heads, window, sinks) -> workspace of beagle_paged_attn
 
     def on_current_device(self) -> int:
         """The current stream, after checking that the cache lies on the current device."""
@@ -651,12 +651,12 @@ def beagle_pages_compact(cache: PagedCache) -> None:
     _pages_ok(cache.lib.beagle_pages_compact(cache.ref, cache.on_current_device()), "beagle_pages_compact")
 
 
-def beagle_paged_attn_workspace_bytes(cache: PagedCache, n_q_heads: int) -> int:
-    n = cache.attn_ws_bytes.get(n_q_heads)
+def beagle_paged_attn_workspace_bytes(cache: PagedCache, n_q_heads: int, window: int = 0, sinks: int = 0) -> int:
+    n = cache.attn_ws_bytes.get((n_q_heads, window, sinks))
     if n is None:
         v = C.c_size_t()
-        _pages_ok(cache.lib.beagle_paged_attn_workspace_bytes(cache.ref, n_q_heads, C.byref(v)), "beagle_paged_attn_workspace_bytes")
-        n = cache.attn_ws_bytes[n_q_heads] = v.value
+        _pages_ok(cache.lib.beagle_paged_attn_workspace_bytes(cache.ref, n_q_heads, window, sinks, C.byref(v)), "beagle_paged_attn_workspace_bytes")
+        n = cache.attn_ws_bytes[n_q_heads, window, sinks] = v.value
     return n
 
 
@@ -673,11 +673,12 @@ def beagle_paged_attn(cache: PagedCache, slots: Sequence[int], q: torch.Tensor, 
     op = _check("out", out, cache.k.dtype, (B, hq, c.head_dim))
     lp = None if lse is None else _check("lse", lse, torch.float32, (B, hq))
     stream = cache.on_current_device()
-    need = beagle_paged_attn_workspace_bytes(cache, hq)
-    if ws is None:
+    need = beagle_paged_attn_workspace_bytes(cache, hq, window, sinks)
+    if ws is None and need > 0:
         ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _pages_ok(cache.lib.beagle_paged_attn(cache.ref, B, _host_i32(slots), hq, qp, _row_stride("q", q, 1), window, sinks, op, lp,
-                                          ws.data_ptr(), ws.numel() * ws.element_size(), stream), "beagle_paged_attn")
+    wp, wn = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+    _pages_ok(cache.lib.beagle_paged_attn(cache.ref, B, _host_i32(slots), hq, qp, _row_stride("q", q, 1), window, sinks, op, lp, wp, wn, stream),
+              "beagle_paged_attn")
 
 
 # ---- attention over whole sequences with a window and sinks -------------------------------------

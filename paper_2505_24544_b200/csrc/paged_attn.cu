@@ -9,6 +9,8 @@
 // single long sequence and a batch of short ones are then balanced by the same rule.  A pair that lies inside one run is
 // finished there; the others leave unnormalised partials (fp32, with their maximum and sum) that a second, dependent launch
 // joins in the order of the runs, so results do not depend on timing.  No counter and no initialised workspace is needed.
+// Where the cache's capacity or the window leave a pair only a few tiles (kWholeTiles), every pair is a run of its own and
+// the second launch, most of such a call's latency, is left out.
 //
 // bf16, head_dim 64 / 128: a producer warp copies the tiles' pages by TMA (128-byte swizzle) into a ring of three stages (two
 // CTAs per SM, about 190 KB in flight per SM); four consumer warps own 16 positions of each tile and keep their own running
@@ -52,6 +54,7 @@ struct PagedArgs {
     float* part;                        // [2 * runs][8][dh + 2]: unnormalised O, then maximum (log2 units) and sum
     long long q_stride;
     int batch, n_pages, page_shift, max_pages, Hq, Hkv, G, window, sinks;
+    int whole;                          // every (sequence, K/V head) pair is one run
     float scale_log2;
     PageSlots slots;
 };
@@ -125,6 +128,26 @@ struct Walk {
     __device__ __forceinline__ int tile(const Schedule& s) const { return i < s.sink_tiles[b] ? i : s.first[b] + i - s.sink_tiles[b]; }
 };
 
+// The units of this CTA's run; in whole mode, of its pair.
+__device__ __forceinline__ void run_units(const PagedArgs& a, const Schedule& s, int& u0, int& u1) {
+    if (a.whole) {
+        const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv, n = tiles_of(s, b, a.Hkv);
+        u0 = s.start[b] + kvh * n;
+        u1 = u0 + n;
+    } else {
+        const int total = s.start[kMaxCallBatch];
+        u0 = total > 0 ? run_begin(total, gridDim.x, blockIdx.x) : 0;
+        u1 = total > 0 ? run_begin(total, gridDim.x, blockIdx.x + 1) : 0;
+    }
+}
+// The G heads of a pair without a visible position: o = 0, lse = -inf.  Whole CTA.
+template <typename T>
+__device__ __forceinline__ void empty_pair(const PagedArgs& a, int b, int kvh, int dh) {
+    T* out = static_cast<T*>(a.o) + ((size_t)b * a.Hq + (size_t)kvh * a.G) * dh;
+    for (int i = threadIdx.x; i < a.G * dh; i += blockDim.x) out[i] = from_float<T>(0.f);
+    if (a.lse != nullptr && threadIdx.x < a.G) a.lse[(size_t)b * a.Hq + kvh * a.G + threadIdx.x] = -INFINITY;
+}
+
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
 }
@@ -177,9 +200,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     __syncthreads();
     finish_schedule(s);
     __syncthreads();
-    const int total = s.start[kMaxCallBatch], runs = gridDim.x;
-    const int u0 = total > 0 ? run_begin(total, runs, blockIdx.x) : 0, u1 = total > 0 ? run_begin(total, runs, blockIdx.x + 1) : 0;
-    if (u0 >= u1) return;
+    int u0, u1;
+    run_units(a, s, u0, u1);
+    if (u0 >= u1) {
+        if (a.whole) empty_pair<bf16>(a, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, DH);
+        return;
+    }
     Walk w;
     w.seek(s, u0, a.Hkv);
 
@@ -195,7 +221,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         auto page_of = [&](const Walk& x) {                      // this lane's page of the walk's tile, -1 if it holds no position
             const int pos = x.tile(s) * kTile + lane * rows;
             int id = -1;
-            if (lane < parts && pos < s.len[x.b]) id = __ldcg(a.table + (size_t)a.slots.slot[x.b] * a.max_pages + (pos >> a.page_shift));
+            // (a part without a visible position stays what it was: its weights and its V rows count as 0)
+            if (lane < parts && pos < s.len[x.b] && (pos + rows > s.lo[x.b] || pos < a.sinks)) id = __ldcg(a.table + (size_t)a.slots.slot[x.b] * a.max_pages + (pos >> a.page_shift));
             return (id >= 0 && id < a.n_pages) ? id : -1;
         };
         next_page = page_of(w);
@@ -267,7 +294,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) l = __int_as_float(0x7fffffff);
         const uint32_t sK = base + st * 2 * SM::kTileBytes, sV = sK + SM::kTileBytes;
-        if (ok && pos0 < len) {
+        if (ok && pos0 < len && (pos0 + kPerWarp > lo || pos0 < a.sinks)) {
             float sc[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
             for (int dg = 0; dg < DH / 32; ++dg)
@@ -402,9 +429,12 @@ __global__ void __launch_bounds__(kConsumers * 32) paged_attn_simt_kernel(const 
     __syncthreads();
     finish_schedule(s);
     __syncthreads();
-    const int total = s.start[kMaxCallBatch], runs = gridDim.x;
-    const int u0 = total > 0 ? run_begin(total, runs, blockIdx.x) : 0, u1 = total > 0 ? run_begin(total, runs, blockIdx.x + 1) : 0;
-    if (u0 >= u1) return;
+    int u0, u1;
+    run_units(a, s, u0, u1);
+    if (u0 >= u1) {
+        if (a.whole) empty_pair<T>(a, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, DH);
+        return;
+    }
     Walk w;
     w.seek(s, u0, a.Hkv);
     const T* K = static_cast<const T*>(a.k);
@@ -550,7 +580,8 @@ __global__ void __launch_bounds__(kConsumers * 32) paged_attn_simt_kernel(const 
 
 // ------------------------------------------------------------------------------------------------
 // Joins the partials of every (sequence, query head) that more than one run worked on; zeroes the heads of empty sequences.
-// One CTA of eight warps per head: the warps share the partials, then meet in shared memory, always in the same order.
+// blockIdx.x = run: the CTA joins head blockIdx.y of the pair that begins in this run and ends in a later one (there is at most
+// one); eight warps share the partials, then meet in shared memory, always in the same order.
 // ------------------------------------------------------------------------------------------------
 constexpr int kJoinWarps = 8;
 template <typename T, int DH>
@@ -565,21 +596,22 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
     __syncthreads();
     finish_schedule(s);
     __syncthreads();
-    const int head = blockIdx.x, b = blockIdx.y, kvh = head / a.G, g = head % a.G;
-    const int total = s.start[kMaxCallBatch], n = tiles_of(s, b, a.Hkv);
+    const int total = s.start[kMaxCallBatch], r0 = blockIdx.x, g = blockIdx.y;
+    // empty sequences, one (row, K/V head) after the other over the CTAs
+    if (g == 0)
+        for (int i = r0; i < a.batch * a.Hkv; i += runs)
+            if (s.len[i / a.Hkv] == 0) empty_pair<T>(a, i / a.Hkv, i % a.Hkv, DH);
+    const int u1 = total > 0 ? run_begin(total, runs, r0 + 1) : 0, u0 = total > 0 ? run_begin(total, runs, r0) : 0;
+    if (u0 >= u1) return;
+    Walk w;
+    w.seek(s, u1 - 1, a.Hkv);                                    // the run's last pair
+    const int e0 = u1 - 1 - w.i, e1 = e0 + w.n;                  // its units
+    if (e0 < u0 || e1 <= u1) return;                             // begins in an earlier run, or ends here
+    const int b = w.b, kvh = w.kvh, r1 = run_of(total, runs, e1 - 1), head = kvh * a.G + g;
     T* out = static_cast<T*>(a.o) + ((size_t)b * a.Hq + head) * DH;
-    if (n == 0) {
-        for (int i = threadIdx.x; i < DH; i += kJoinWarps * 32) out[i] = from_float<T>(0.f);
-        if (threadIdx.x == 0 && a.lse != nullptr) a.lse[(size_t)b * a.Hq + head] = -INFINITY;
-        return;
-    }
-    const int e0 = s.start[b] + kvh * n, e1 = e0 + n;
-    const int r0 = run_of(total, runs, e0), r1 = run_of(total, runs, e1 - 1);
-    if (r0 == r1) return;                                        // finished by its run
-    // the first run holds this pair as its second part unless the run begins with it
-    const int seg0 = run_begin(total, runs, r0) == e0 ? 0 : 1;
     const bool gaps = total < runs;                              // fewer tiles than runs: some runs are empty and left no partial
-    auto part = [&](int r) { return a.part + ((size_t)(2 * r + (r == r0 ? seg0 : 0)) * 8 + g) * (DH + 2); };
+    // this run holds the pair as its second part unless it begins with it
+    auto part = [&](int r) { return a.part + ((size_t)(2 * r + (r == r0 && e0 != u0 ? 1 : 0)) * 8 + g) * (DH + 2); };
     float M = -INFINITY, L = 0.f, acc[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
@@ -617,6 +649,20 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
 
 constexpr int kMaxRuns = 2048;           // bound of the workspace; the grid is min(this, CTAs that fit the GPU)
 constexpr int kSimtCtasPerSm = 4;
+// Pairs of at most this many tiles are not cut.  One tile takes a CTA some 0.4 us of a stream (SIMT: 1.5 us), the join launch 4.
+constexpr int kWholeTiles = 8, kWholeTilesSimt = 2;
+
+bool uses_mma(const beagle_pages* p) { return p->dtype == BEAGLE_BF16 && (p->head_dim == 64 || p->head_dim == 128); }
+// The most tiles of one pair, as far as the host can know.
+long long most_tiles(const beagle_pages* p, int window, int sinks) {
+    const long long cap = ((long long)p->max_pages * p->page_size + kTile - 1) / kTile;
+    if (window <= 0) return cap;
+    const long long seen = ((long long)window + kTile - 2) / kTile + 1 + ((long long)sinks + kTile - 1) / kTile;
+    return seen < cap ? seen : cap;
+}
+bool whole_pairs(const beagle_pages* p, int window, int sinks) {
+    return most_tiles(p, window, sinks) <= (uses_mma(p) ? kWholeTiles : kWholeTilesSimt);
+}
 
 template <int DH>
 beagle_status launch_mma(const beagle_pages* p, const PagedArgs& a, int runs, cudaStream_t stream) {
@@ -636,7 +682,7 @@ beagle_status launch_mma(const beagle_pages* p, const PagedArgs& a, int runs, cu
     if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes) == cudaSuccess; }))
         return BEAGLE_ERR_CUDA;
     launch_pdl(paged_attn_kernel<DH>, dim3(runs), dim3((kConsumers + 1) * 32), (size_t)SM::kBytes, stream, mk, mv, a);
-    launch_pdl(paged_attn_join_kernel<bf16, DH>, dim3(a.Hq, a.batch), dim3(kJoinWarps * 32), 0, stream, a, runs);
+    if (!a.whole) launch_pdl(paged_attn_join_kernel<bf16, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a, runs);
     return BEAGLE_OK;
 }
 
@@ -647,7 +693,7 @@ beagle_status launch_simt(const PagedArgs& a, int runs, cudaStream_t stream) {
     else if (a.G <= 4) launch_pdl(paged_attn_simt_kernel<T, DH, 4>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
     else if constexpr (DH * 8 * (int)sizeof(float) * kConsumers <= 16 * 1024 + 0) launch_pdl(paged_attn_simt_kernel<T, DH, 8>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
     else return BEAGLE_ERR_SHAPE;
-    launch_pdl(paged_attn_join_kernel<T, DH>, dim3(a.Hq, a.batch), dim3(kJoinWarps * 32), 0, stream, a, runs);
+    if (!a.whole) launch_pdl(paged_attn_join_kernel<T, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a, runs);
     return BEAGLE_OK;
 }
 
@@ -691,12 +737,16 @@ EncodeTiled tensor_map_encoder() {
 
 extern "C" {
 
-beagle_status beagle_paged_attn_workspace_bytes(const beagle_pages* p, int32_t n_q_heads, size_t* bytes) {
-    if (p == nullptr || bytes == nullptr || p->n_kv_heads <= 0) return BEAGLE_ERR_INVALID_ARG;
+beagle_status beagle_paged_attn_workspace_bytes(const beagle_pages* p, int32_t n_q_heads, int32_t window, int32_t sinks, size_t* bytes) {
+    if (p == nullptr || bytes == nullptr || p->n_kv_heads <= 0 || p->max_pages <= 0 || window < 0 || sinks < 0) return BEAGLE_ERR_INVALID_ARG;
     if (!pages_valid_shape(p)) return BEAGLE_ERR_SHAPE;
     const beagle_status st = check_heads(p, n_q_heads);
     if (st != BEAGLE_OK) return st;
-    const int sms = device_sm_count(), per = (p->dtype == BEAGLE_BF16 && (p->head_dim == 64 || p->head_dim == 128)) ? kCtasPerSm : kSimtCtasPerSm;
+    if (whole_pairs(p, window, sinks)) {
+        *bytes = 0;
+        return BEAGLE_OK;
+    }
+    const int sms = device_sm_count(), per = uses_mma(p) ? kCtasPerSm : kSimtCtasPerSm;
     const int runs = sms * per < kMaxRuns ? sms * per : kMaxRuns;
     *bytes = ((size_t)2 * runs * 8 * (p->head_dim + 2) * sizeof(float) + 255) / 256 * 256;
     return BEAGLE_OK;
@@ -719,10 +769,10 @@ beagle_status beagle_paged_attn(const beagle_pages* p, int32_t batch, const int3
     if (window < 0 || sinks < 0) return BEAGLE_ERR_INVALID_ARG;
     if (batch == 0) return BEAGLE_OK;
     const int e = p->dtype == BEAGLE_BF16 ? 2 : 4;
-    if (q_dev == nullptr || out_dev == nullptr || ws_dev == nullptr || q_stride < (int64_t)n_q_heads * p->head_dim) return BEAGLE_ERR_INVALID_ARG;
-    if ((((uintptr_t)q_dev | (uintptr_t)out_dev | (uintptr_t)ws_dev) & 15) || (q_stride * e) % 16 || ((uintptr_t)lse_dev & 3)) return BEAGLE_ERR_INVALID_ARG;
     size_t need = 0;
-    beagle_paged_attn_workspace_bytes(p, n_q_heads, &need);
+    beagle_paged_attn_workspace_bytes(p, n_q_heads, window, sinks, &need);
+    if (q_dev == nullptr || out_dev == nullptr || (need > 0 && ws_dev == nullptr) || q_stride < (int64_t)n_q_heads * p->head_dim) return BEAGLE_ERR_INVALID_ARG;
+    if ((((uintptr_t)q_dev | (uintptr_t)out_dev | (uintptr_t)ws_dev) & 15) || (q_stride * e) % 16 || ((uintptr_t)lse_dev & 3)) return BEAGLE_ERR_INVALID_ARG;
     if (ws_bytes < need) return BEAGLE_ERR_CAPACITY;
     // tiles are counted in 32 bits
     if ((long long)batch * p->n_kv_heads * ((long long)p->max_pages * p->page_size / kTile + 2) > 0x7fffffffll) return BEAGLE_ERR_CAPACITY;
@@ -737,11 +787,13 @@ beagle_status beagle_paged_attn(const beagle_pages* p, int32_t batch, const int3
     a.window = window; a.sinks = sinks;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)p->head_dim);
     // no more runs than the cache's capacity has tiles
-    const long long most = (long long)batch * p->n_kv_heads * (((long long)p->max_pages * p->page_size + kTile - 1) / kTile);
-    const bool mma = p->dtype == BEAGLE_BF16 && (p->head_dim == 64 || p->head_dim == 128);
+    const long long most = (long long)batch * p->n_kv_heads * most_tiles(p, window, sinks);
+    const bool mma = uses_mma(p);
+    a.whole = whole_pairs(p, window, sinks) ? 1 : 0;
     long long runs = (long long)device_sm_count() * (mma ? kCtasPerSm : kSimtCtasPerSm);
     if (runs > kMaxRuns) runs = kMaxRuns;
     if (runs > most) runs = most;
+    if (a.whole) runs = (long long)batch * p->n_kv_heads;
     if (mma) st = p->head_dim == 128 ? launch_mma<128>(p, a, (int)runs, stream) : launch_mma<64>(p, a, (int)runs, stream);
     else if (p->dtype == BEAGLE_BF16) st = p->head_dim == 256 ? launch_simt<bf16, 256>(a, (int)runs, stream) : launch_simt<bf16, 32>(a, (int)runs, stream);
     else if (p->head_dim == 128) st = launch_simt<float, 128>(a, (int)runs, stream);

@@ -44,10 +44,15 @@ def test_workspace_bytes(lib):
     assert lib.beagle_pages_workspace_bytes(C.byref(p), C.byref(n)) == OK and n.value % 256 == 0 and n.value >= 40 * 12
     assert lib.beagle_pages_workspace_bytes(None, C.byref(n)) == INVALID
     assert lib.beagle_pages_workspace_bytes(C.byref(p), None) == INVALID
-    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 8, C.byref(n)) == OK and n.value > 0
-    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 0, C.byref(n)) == INVALID
-    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 3, C.byref(n)) == SHAPE             # not a multiple of the K/V heads
-    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 18, C.byref(n)) == SHAPE            # nine grouped heads
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 8, 0, 0, C.byref(n)) == OK and n.value == 0              # 128 positions at most: nothing to join
+    wide = pages(lib, max_pages=100)
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(wide), 8, 0, 0, C.byref(n)) == OK and n.value > 0
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(wide), 8, 300, 4, C.byref(n)) == OK and n.value == 0            # 6 tiles of 64 and one
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(wide), 8, 600, 4, C.byref(n)) == OK and n.value > 0
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(wide), 8, -1, 4, C.byref(n)) == INVALID
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 0, 0, 0, C.byref(n)) == INVALID
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 3, 0, 0, C.byref(n)) == SHAPE             # not a multiple of the K/V heads
+    assert lib.beagle_paged_attn_workspace_bytes(C.byref(p), 18, 0, 0, C.byref(n)) == SHAPE            # nine grouped heads
 
 
 @pytest.mark.parametrize("kw, want", [
@@ -108,9 +113,12 @@ def test_bad_rows(lib):
     for hq, qp, st, w, k, o, ws, n, want in (
             (4, None, 256, 0, 0, q, q, big, INVALID), (4, q, 255, 0, 0, q, q, big, INVALID), (4, q, 260, 0, 0, q, q, big, INVALID),
             (4, q, 256, -1, 0, q, q, big, INVALID), (4, q, 256, 0, -1, q, q, big, INVALID), (4, q, 256, 0, 0, None, q, big, INVALID),
-            (4, q, 256, 0, 0, q, None, big, INVALID), (4, q + 2, 256, 0, 0, q, q, big, INVALID), (4, q, 256, 0, 0, q, q, 64, CAPACITY),
+            (4, q + 2, 256, 0, 0, q, q, big, INVALID),
             (5, q, 512, 0, 0, q, q, big, SHAPE), (18, q, 2048, 0, 0, q, q, big, SHAPE)):
         assert lib.beagle_paged_attn(p, 1, one, hq, qp, st, w, k, o, None, ws, n, None) == want
+    long = C.byref(pages(lib, max_pages=100))
+    assert lib.beagle_paged_attn(long, 1, one, 4, q, 256, 0, 0, q, None, None, big, None) == INVALID
+    assert lib.beagle_paged_attn(long, 1, one, 4, q, 256, 0, 0, q, None, q, 64, None) == CAPACITY
     wide = C.byref(pages(lib, head_dim=256))
     assert lib.beagle_paged_attn(wide, 1, one, 16, q, 4096, 0, 0, q, None, q, big, None) == SHAPE
 

@@ -279,9 +279,10 @@ LENS = [0, 1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 300, 0, 1000, 7]
                                             ("bf16", 4, 2, 32), ("bf16", 4, 1, 256), ("fp32", 4, 4, 64), ("fp32", 8, 1, 128), ("fp32", 6, 2, 16),
                                             ("fp32", 4, 2, 32), ("fp32", 5, 1, 64)])
 @pytest.mark.parametrize("ps", [8, 16, 64, 256])
-@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (64, 4), (100, 70), (17, 1000)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (64, 4), (100, 70), (17, 1000), (600, 5)])
 def test_attention(dtype, hq, hkv, dh, ps, window, sinks):
-    """Lengths around every tile and page border, empty slots among them; whatever is not visible is NaN or Inf."""
+    """Lengths around every tile and page border, empty slots among them; whatever is not visible is NaN or Inf.  (The small
+    windows are divided by pairs, the others into runs that are joined.)"""
     cache = filled(LENS, ps, hkv, dh, dtype, 11)
     r = random.Random(3)
     slots = list(range(len(LENS))) + [14, 12]            # a slot may serve several rows
@@ -330,6 +331,7 @@ def test_attention_strided_queries_and_another_stream():
         b.beagle_paged_attn(cache, [2, 0, 9], q, out)
     with pytest.raises(ValueError):
         b.beagle_paged_attn(cache, [2, 0, 1], q, out.cpu())
+    cache = filled([77, 300, 5], 16, 2, 128, "bf16", 9, width=200)
     with pytest.raises(b.BeagleError):
         b.beagle_paged_attn(cache, [2, 0, 1], q, out, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
 
