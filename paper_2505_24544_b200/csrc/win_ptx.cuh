@@ -77,6 +77,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&t);
 }
+// Tile of shared memory to global memory (generic writes before it: fence_async_smem); store_done: the shared memory may be
+// written again.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* tm, uint32_t src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(src), "r"(c0), "r"(c1) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void store_done() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 // Two fp32 values in one 64-bit register and the packed arithmetic on them (one issue slot for two operations).
 __device__ __forceinline__ uint64_t pk2(float lo, float hi) {
     uint64_t r;
@@ -117,15 +124,15 @@ __device__ __forceinline__ void zero_rows(uint8_t* tile, int rows, int from, int
 
 }  // namespace tc
 
-// Tensor map of a bf16 matrix [rows, cols] with rows `ld` elements apart: boxes of 64 columns x box_rows, 128-byte swizzle,
-// out-of-range rows read as zero.
-inline bool win_map(CUtensorMap* out, const void* base, long long rows, long long cols, long long ld, int box_rows) {
+// Tensor map of a bf16 matrix [rows, cols] with rows `ld` elements apart: boxes of 64 columns (128-byte swizzle) or 32 (64-byte
+// swizzle) x box_rows, out-of-range rows read as zero.
+inline bool win_map(CUtensorMap* out, const void* base, long long rows, long long cols, long long ld, int box_rows, int box_cols = 64) {
     const EncodeTiled encode = tensor_map_encoder();
     if (encode == nullptr) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
-    const cuuint32_t box[2] = {64u, (cuuint32_t)box_rows}, one[2] = {1, 1};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, one[2] = {1, 1};
     return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                  box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace beagle

@@ -49,18 +49,35 @@ __device__ __forceinline__ int stat_row0(const WinSeqs& s, int b) {      // firs
     return at;
 }
 
-// One thread's row of an accumulator (n columns from taddr), scaled, as bf16.
-__device__ __forceinline__ void store_row32(uint32_t taddr, float scale, bf16* dst, bool write, bool zero) {
-    uint32_t o[32];
-    if (!zero) { tmem_ld32(taddr, o); tmem_ld_wait(); }
-    if (!write) return;
+// A warp's 32 rows x DH / 2 columns of an accumulator (columns from taddr; not read when `zero`), scaled, as bf16 to global
+// memory: through a slab of shared memory and one TMA store when all 32 rows are this CTA's to write (rows of 64 to 128 bytes at
+// once instead of 16 a lane), else row by row.  (c0, c1): the store's coordinates; dst: this lane's row.
+template <int DH>
+__device__ __forceinline__ void store_rows(uint32_t taddr, float scale, bool zero, const CUtensorMap* tm, uint8_t* slab, int c0, int c1, bf16* dst, bool write,
+                                           int lane) {
+    const bool whole = __all_sync(0xffffffffu, write);
+    if (whole) {
+        if (lane == 0) store_done();                             // the slab's last store has read it
+        __syncwarp();
+    }
+#pragma unroll 1
+    for (int c = 0; c < DH / 2; c += 16) {
+        uint32_t o[16], y[8];
+        if (!zero) { tmem_ld16(taddr + c, o); tmem_ld_wait(); }
 #pragma unroll
-    for (int x = 0; x < 32; x += 8) {
-        uint32_t y[4];
+        for (int z = 0; z < 8; ++z) y[z] = zero ? 0u : pack_bf16(__uint_as_float(o[2 * z]) * scale, __uint_as_float(o[2 * z + 1]) * scale);
 #pragma unroll
-        for (int z = 0; z < 4; ++z)
-            y[z] = zero ? 0u : pack_bf16(__uint_as_float(o[x + 2 * z]) * scale, __uint_as_float(o[x + 2 * z + 1]) * scale);
-        *reinterpret_cast<uint4*>(dst + x) = make_uint4(y[0], y[1], y[2], y[3]);
+        for (int i = 0; i < 2; ++i) {
+            const int chunk = c / 8 + i, place = DH == 128 ? chunk ^ (lane & 7) : chunk ^ ((lane >> 1) & 3);
+            const uint4 v = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+            if (whole) *reinterpret_cast<uint4*>(slab + lane * DH + place * 16) = v;
+            else if (write) *reinterpret_cast<uint4*>(dst + 8 * chunk) = v;
+        }
+    }
+    if (whole) {
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) tma_store_2d(tm, smem_u32(slab), c0, c1);
     }
 }
 
@@ -100,7 +117,8 @@ constexpr int kThreads = 320, kQThreads = 384;
 template <int DH>
 struct BwdQSmem {
     static constexpr int kT = kQTile * DH * 2;           // Q, dO, and a K or V tile (three stages of K, one of V)
-    static constexpr int kBytes = 6 * kT + 4 * kQTile * 4 + 256;
+    static constexpr int kSlab = 32 * DH;                // a warp's rows on their way out
+    static constexpr int kBytes = 6 * kT + 8 * kSlab + 4 * kQTile * 4 + 256;
 };
 
 // The key tiles of one query tile: sinks [0, sink_end) first, then the band [lo, hi).
@@ -146,14 +164,14 @@ struct QItem {                           // 128 queries of one (sequence, query 
 template <int DH>
 __global__ void __launch_bounds__(kQThreads, 1) window_bwd_q_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmdO,
                                                                  const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                                                                 const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
+                                                                 const __grid_constant__ CUtensorMap tmdQ, const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
     using SM = BwdQSmem<DH>;
     constexpr int kHalves = DH / 64;
     constexpr uint32_t kTmem = 512, kDP = 256, kDQ = 384;    // S / dS at columns 0 and 128, dP at 256, dQ at 384
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sQ = smem_u32(smem), sdO = sQ + SM::kT, sV = sdO + SM::kT, sK = sV + SM::kT;     // stage s of K at sK + s kT
-    float* s_stat = reinterpret_cast<float*>(smem + 6 * SM::kT);                     // [2][2][128]: -lse (log2 units) and -delta, two items
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 6 * SM::kT + 4 * kQTile * 4);
+    float* s_stat = reinterpret_cast<float*>(smem + 6 * SM::kT + 8 * SM::kSlab);                     // [2][2][128]: -lse (log2 units) and -delta, two items
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 6 * SM::kT + 8 * SM::kSlab + 4 * kQTile * 4);
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t q_full = bar0, dp_full = bar0 + 8, ds_full = bar0 + 16, q_empty = bar0 + 24, v_full = bar0 + 32, v_empty = bar0 + 40, v_fixed = bar0 + 48;
     const uint32_t s_full = bar0 + 56, stat_full = bar0 + 72, stat_empty = bar0 + 88;          // two each
@@ -444,14 +462,12 @@ __global__ void __launch_bounds__(kQThreads, 1) window_bwd_q_kernel(const __grid
             }
             if (x.w.n > 0 && ok) ok = warp_wait(k_empty + 8 * ((n - 1) % 3), ((n - 1) / 3) & 1, s_abort);       // the item's last dQ
             fence_after();
-            bf16* dst = static_cast<bf16*>(a.dq) + (size_t)(x.q_row + row) * a.dq_stride + (size_t)x.h * DH;
-#pragma unroll
-            for (int c = 0; c < DH / 2; c += 32) {
-                const int col = half * (DH / 2) + c;
-                store_row32(tmem + kDQ + col + lanes, ok ? a.scale : nan_f(), dst + col, valid, x.w.n == 0);
-            }
+            bf16* dst = static_cast<bf16*>(a.dq) + (size_t)(x.q_row + row) * a.dq_stride + (size_t)x.h * DH + half * (DH / 2);
+            store_rows<DH>(tmem + kDQ + half * (DH / 2) + lanes, ok ? a.scale : nan_f(), x.w.n == 0, &tmdQ, smem + 6 * SM::kT + (warp - 2) * SM::kSlab,
+                           x.h * DH + half * (DH / 2), x.q_row + q * 32, dst, valid, lane);
         }
     }
+    if (lane == 0) store_done();                                 // this warp's last stores have read their slab
     fence_before();
     __syncthreads();
     if (warp == 1) {
@@ -465,7 +481,8 @@ template <int DH>
 struct BwdKSmem {
     static constexpr int kT = kKTile * DH * 2;           // K, V, and a tile of Q or dO (two stages)
     static constexpr int kStat = kQTile * 4;             // -lse, and -delta, of a query tile (two stages of each)
-    static constexpr int kBytes = 6 * kT + 4 * kStat + 256;
+    static constexpr int kSlab = 32 * DH;                // a warp's rows on their way out
+    static constexpr int kBytes = 6 * kT + 8 * kSlab + 4 * kStat + 256;
 };
 
 // The query tiles that a CTA of the key side reads: of every head of the group, from `from` in steps of 128 up to `to`.
@@ -534,14 +551,16 @@ struct Job {
 template <int DH>
 __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmdO,
                                                                   const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                                                                  const __grid_constant__ CUtensorMap tmdK, const __grid_constant__ CUtensorMap tmdV,
                                                                   const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
     using SM = BwdKSmem<DH>;
     constexpr int kHalves = DH / 64;
     constexpr uint32_t kTmem = 512, kY = 128, kDV = 256, kDK = 256 + DH;     // S^T / P^T at column 0, dP^T / dS^T at 128
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sK = smem_u32(smem), sV = sK + SM::kT, sQ = sV + SM::kT;      // stage s: Q at sQ + 2 s kT, dO behind it
-    const uint32_t sStat = sQ + 4 * SM::kT;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 6 * SM::kT + 4 * SM::kStat);
+    constexpr int kStatAt = 6 * SM::kT + 8 * SM::kSlab;
+    const uint32_t sStat = sK + kStatAt;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStatAt + 4 * SM::kStat);
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t kv_full = bar0, s_full = bar0 + 8, dp_full = bar0 + 16, ds_full = bar0 + 24, kv_empty = bar0 + 32;
     // one per stage; Q is free when dK has read it (so is dS^T's place), dO when dV has (so is P^T's place)
@@ -623,7 +642,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
                     if (!ok) break;
                     zero_rows<DH>(tile, kQTile, x.q_len - qb, kQTile, lane);
                     zero_rows<DH>(tile + SM::kT, kQTile, x.q_len - qb, kQTile, lane);
-                    float* stat = reinterpret_cast<float*>(smem + 6 * SM::kT + st * 2 * SM::kStat);
+                    float* stat = reinterpret_cast<float*>(smem + kStatAt + st * 2 * SM::kStat);
                     for (int i = x.q_len - qb + lane; i < kQTile; i += 32) stat[i] = stat[kQTile + i] = 0.f;
                     fence_async_smem();
                     __syncwarp();
@@ -763,12 +782,12 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
             if (x.n > 0) job.first(x, a.G);
             for (int j = 0; j < x.n; ++j, ++n, job.next(x)) {
                 const int st = n & 1, c0 = job.qb + 64 * half;   // first query of this thread's columns
-                const float* stat = reinterpret_cast<const float*>(smem + 6 * SM::kT + st * 2 * SM::kStat) + 64 * half;      // -lse; -delta one kStat on
+                const float* stat = reinterpret_cast<const float*>(smem + kStatAt + st * 2 * SM::kStat) + 64 * half;      // -lse; -delta one kStat on
                 if (ok) ok = warp_wait2(q_full + 8 * st, (n >> 1) & 1, s_full, n & 1, s_abort);      // (q_full: the statistics; their repair precedes S^T)
                 if (!ok) continue;
                 fence_after();
                 const bool full = c0 >= full_lo && c0 + 64 <= full_hi;
-                uint32_t s[2][32], d[2][32], y[2][16];
+                uint32_t s[2][32], d[32], y[16];
                 tmem_ld32(tmem + at64, s[0]);
                 tmem_ld32(tmem + at64 + 32, s[1]);
                 tmem_ld_wait();
@@ -779,8 +798,8 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
                     if (!full) mask32(s[c], bit_range(first - c0 - 32 * c, stop - c0 - 32 * c));
                     chunk_p(s[c], scale2, nl);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) y[c][e] = pack_bf16(__uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1]));
-                    tmem_st16(tmem + at64 + 16 * c, y[c]);       // P^T of this half over its own S^T columns
+                    for (int e = 0; e < 16; ++e) y[e] = pack_bf16(__uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1]));
+                    tmem_st16(tmem + at64 + 16 * c, y);          // P^T of this half over its own S^T columns
                     tmem_st_wait();
                     fence_before();
                     __syncwarp();
@@ -789,14 +808,13 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
                 ok = warp_wait(dp_full, n & 1, s_abort);
                 if (!ok) continue;
                 fence_after();
-                tmem_ld32(tmem + kY + at64, d[0]);
-                tmem_ld32(tmem + kY + at64 + 32, d[1]);
-                tmem_ld_wait();
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                for (int c = 0; c < 2; ++c) {                    // (a part at a time: registers are short)
                     auto nd = [&](int e) { return *reinterpret_cast<const uint64_t*>(stat + kQTile + 32 * c + e); };
-                    chunk_ds(s[c], d[c], nd, y[c]);
-                    tmem_st16(tmem + kY + at64 + 16 * c, y[c]);  // dS^T over this half's own dP^T columns, which are in registers
+                    tmem_ld32(tmem + kY + at64 + 32 * c, d);
+                    tmem_ld_wait();
+                    chunk_ds(s[c], d, nd, y);
+                    tmem_st16(tmem + kY + at64 + 16 * c, y);     // dS^T over this half's dP^T columns that have been read
                 }
                 tmem_st_wait();
                 fence_before();
@@ -804,47 +822,43 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
                 if (lane == 0) { mbar_arrive(ds_full); mbar_arrive(stat_empty + 8 * st); }
             }
             if (x.n > 0 && ok) ok = warp_wait2(y_free + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, x_free + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, s_abort);
+            // The item is read again rather than held over the loop above, whose registers are short.
+            asm volatile("" : "+r"(at));
+            x.load(at, a, seqs);
             fence_after();
             const float sv = ok ? 1.f : nan_f(), sk = ok ? a.scale : nan_f();
-            const bool to_part = a.sink_segs > 0 && is_sink && valid;        // rows that several items share go to the join, in fp32
-            // every thread reads its half of the columns; a warp may hold rows of both kinds
+            const int my_key = x.k0 + q * 32 + lane;
+            const bool sink_item = x.seg >= 0, to_part = a.sink_segs > 0 && my_key < min(a.sinks, x.kv_len);        // rows that several items share go to the join, in fp32
             const size_t row = (size_t)(x.k_row + q * 32 + lane);
-            bf16* dk = static_cast<bf16*>(a.dk) + row * a.dk_stride + (size_t)x.kvh * DH;
-            bf16* dv = static_cast<bf16*>(a.dv) + row * a.dv_stride + (size_t)x.kvh * DH;
-            float* part = nullptr;
-            if (to_part) part = a.sink_part + ((((size_t)x.b * a.Hkv + x.kvh) * (1 + a.sink_segs) + (1 + x.seg)) * a.sink_rows + key) * 2 * DH;
+            const int col = half * (DH / 2);                     // this thread's half of the columns
+            const bool write = my_key < x.kv_len && !sink_item && !to_part;
+#pragma unroll 1
+            for (int m = 0; m < 2; ++m) {                        // dV, dK
+                const uint32_t acc = tmem + (m == 0 ? kDV : kDK) + col + lanes;
+                const float f = m == 0 ? sv : sk;
+                if (__any_sync(0xffffffffu, to_part)) {
+                    float* part = a.sink_part + ((((size_t)x.b * a.Hkv + x.kvh) * (1 + a.sink_segs) + (1 + x.seg)) * a.sink_rows + my_key) * 2 * DH + m * DH + col;
+#pragma unroll 1
+                    for (int c = 0; c < DH / 2; c += 16) {
+                        uint32_t u[16];
+                        if (x.n > 0) { tmem_ld16(acc + c, u); tmem_ld_wait(); }
+                        if (to_part)
 #pragma unroll
-            for (int c = 0; c < DH / 2; c += 32) {
-                const int col = half * (DH / 2) + c;
-                uint32_t u[32], v[32];
-                if (x.n > 0) { tmem_ld32(tmem + kDV + col + lanes, u); tmem_ld32(tmem + kDK + col + lanes, v); tmem_ld_wait(); }
-                else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) u[i] = v[i] = 0u;
+                            for (int i = 0; i < 16; i += 4)
+                                *reinterpret_cast<float4*>(part + c + i) = x.n > 0 ? make_float4(__uint_as_float(u[i]) * f, __uint_as_float(u[i + 1]) * f, __uint_as_float(u[i + 2]) * f, __uint_as_float(u[i + 3]) * f)
+                                                                                   : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
                 }
-                if (to_part) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        *reinterpret_cast<float4*>(part + col + i) = make_float4(__uint_as_float(u[i]) * sv, __uint_as_float(u[i + 1]) * sv, __uint_as_float(u[i + 2]) * sv, __uint_as_float(u[i + 3]) * sv);
-                        *reinterpret_cast<float4*>(part + DH + col + i) = make_float4(__uint_as_float(v[i]) * sk, __uint_as_float(v[i + 1]) * sk, __uint_as_float(v[i + 2]) * sk, __uint_as_float(v[i + 3]) * sk);
-                    }
-                } else if (valid && !sink_part) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        uint32_t e[4], f[4];
-#pragma unroll
-                        for (int z = 0; z < 4; ++z) {
-                            e[z] = pack_bf16(__uint_as_float(u[i + 2 * z]) * sv, __uint_as_float(u[i + 2 * z + 1]) * sv);
-                            f[z] = pack_bf16(__uint_as_float(v[i + 2 * z]) * sk, __uint_as_float(v[i + 2 * z + 1]) * sk);
-                        }
-                        *reinterpret_cast<uint4*>(dv + col + i) = make_uint4(e[0], e[1], e[2], e[3]);
-                        *reinterpret_cast<uint4*>(dk + col + i) = make_uint4(f[0], f[1], f[2], f[3]);
-                    }
+                if (__any_sync(0xffffffffu, write)) {
+                    bf16* dst = m == 0 ? static_cast<bf16*>(a.dv) + row * a.dv_stride : static_cast<bf16*>(a.dk) + row * a.dk_stride;
+                    store_rows<DH>(acc, f, x.n == 0, m == 0 ? &tmdV : &tmdK, smem + 6 * SM::kT + (warp - 2) * SM::kSlab, x.kvh * DH + col, x.k_row + q * 32,
+                                   dst + x.kvh * DH + col, write, lane);
                 }
             }
             fence_before();                                      // the accumulators have been read before the next item's P^T is announced
         }
     }
+    if (lane == 0) store_done();                                 // this warp's last stores have read their slab
     fence_before();
     __syncthreads();
     if (warp == 1) {
@@ -881,7 +895,7 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
     const long long qc = (long long)a.Hq * DH, kc = (long long)a.Hkv * DH;
     // where one side has no rows its maps are never used, any valid one does
     const bool hq = q_rows > 0, hk = k_rows > 0;
-    CUtensorMap mq, mdo, mk64, mv64, mk, mv;
+    CUtensorMap mq, mdo, mk64, mv64, mk, mv, mdq, mdk, mdv;
     const void* any = hq ? a.q : a.k;
     const long long any_rows = hq ? q_rows : k_rows, any_cols = hq ? qc : kc, any_ld = hq ? a.q_stride : a.k_stride;
     if (!win_map(&mq, hq ? a.q : any, hq ? q_rows : any_rows, hq ? qc : any_cols, hq ? a.q_stride : any_ld, kQTile)) return -1;
@@ -890,6 +904,8 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
     if (!win_map(&mv64, hk ? a.v : any, hk ? k_rows : any_rows, hk ? kc : any_cols, hk ? a.v_stride : any_ld, 64)) return -1;
     if (!win_map(&mk, hk ? a.k : any, hk ? k_rows : any_rows, hk ? kc : any_cols, hk ? a.k_stride : any_ld, kKTile)) return -1;
     if (!win_map(&mv, hk ? a.v : any, hk ? k_rows : any_rows, hk ? kc : any_cols, hk ? a.v_stride : any_ld, kKTile)) return -1;
+    if (hq && !win_map(&mdq, a.dq, q_rows, qc, a.dq_stride, 32, DH / 2)) return -1;
+    if (hk && (!win_map(&mdk, a.dk, k_rows, kc, a.dk_stride, 32, DH / 2) || !win_map(&mdv, a.dv, k_rows, kc, a.dv_stride, 32, DH / 2))) return -1;
     static PerDeviceOnce attr;
     if (!attr.ensure([] {
             return cudaFuncSetAttribute(window_bwd_q_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, SQ::kBytes) == cudaSuccess &&
@@ -901,7 +917,7 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
     if (hq) {
         const long long items = (long long)s.item[a.batch] * a.Hq;
         if (items > 0x3fffffff) return -1;
-        window_bwd_q_kernel<DH><<<(unsigned)(items < sms ? items : sms), kQThreads, SQ::kBytes, stream>>>(mq, mdo, mk64, mv64, a, s);
+        window_bwd_q_kernel<DH><<<(unsigned)(items < sms ? items : sms), kQThreads, SQ::kBytes, stream>>>(mq, mdo, mk64, mv64, mdq, a, s);
         ++launched;
     }
     if (hk) {
@@ -915,7 +931,7 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
             // 17 tiles x 4 heads 747 us against 844 as a fixed share per SM), short ones share a pipeline (5 tiles: 424 against 477).
             const long long jobs = ((long long)(a.window < 1 << 24 ? a.window : 1 << 24) + 2 * kKTile) / kQTile * a.G;
             const bool share = jobs < 24 && items > sms;
-            window_bwd_kv_kernel<DH><<<(unsigned)(share ? sms : items), kThreads, SK::kBytes, stream>>>(mq, mdo, mk, mv, a, t);
+            window_bwd_kv_kernel<DH><<<(unsigned)(share ? sms : items), kThreads, SK::kBytes, stream>>>(mq, mdo, mk, mv, mdk, mdv, a, t);
             ++launched;
             if (a.sink_segs > 0) {
                 window_sink_join_kernel<DH><<<dim3(a.sink_rows, a.Hkv, a.batch), 2 * DH, 0, stream>>>(a, t);
