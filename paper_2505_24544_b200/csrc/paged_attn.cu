@@ -45,12 +45,14 @@ constexpr int kCtasPerSm = 2;
 constexpr float kSlack = 8.f;           // how far (log2) a score may exceed the row's reference point before it moves
 constexpr float kLn2 = 0.6931471805599453f;
 
+struct JoinItem;
 struct PagedArgs {
     const int32_t *table, *length;
     const void *k, *v;                  // pools (the SIMT kernel; the other one has tensor maps)
     const void* q;
     void* o;
     float* lse;                         // [batch, Hq] or NULL
+    JoinItem* join;                     // [runs]
     float* part;                        // [2 * runs][8][dh + 2]: unnormalised O, then maximum (log2 units) and sum
     long long q_stride;
     int batch, n_pages, page_shift, max_pages, Hq, Hkv, G, window, sinks;
@@ -69,13 +71,18 @@ struct Schedule {
 };
 
 __device__ __forceinline__ int tiles_of(const Schedule& s, int b, int Hkv) { return (s.start[b + 1] - s.start[b]) / Hkv; }
-__device__ __forceinline__ int run_begin(int total, int runs, int r) { return (int)((long long)total * r / runs); }
-__device__ __forceinline__ int run_of(int total, int runs, int unit) {          // the run that holds `unit`
-    int r = (int)(((long long)unit * runs) / total);
-    while (r + 1 < runs && run_begin(total, runs, r + 1) <= unit) ++r;
-    while (r > 0 && run_begin(total, runs, r) > unit) --r;
-    return r;
-}
+// First unit of run r: floor(total * r / runs), in 32 bits (runs <= 2048).
+struct Runs {
+    int total, runs, each, rest;
+    __device__ __forceinline__ Runs(int t, int n) : total(t), runs(n), each(t / n), rest(t - t / n * n) {}
+    __device__ __forceinline__ int begin(int r) const { return each * r + rest * r / runs; }
+    __device__ __forceinline__ int of(int unit) const {                         // the run that holds `unit`
+        int r = min(runs - 1, (int)((float)unit * (float)runs / (float)total));
+        while (r + 1 < runs && begin(r + 1) <= unit) ++r;
+        while (r > 0 && begin(r) > unit) --r;
+        return r;
+    }
+};
 
 // Threads 0..63 of the CTA fill `s`; the caller synchronises afterwards.
 __device__ __forceinline__ void make_schedule(const PagedArgs& a, Schedule& s) {
@@ -109,9 +116,9 @@ __device__ __forceinline__ void finish_schedule(Schedule& s) {          // secon
 // Walks the units [u, end) of one run: for every tile the pair (b, kvh), the tile's first position and whether the pair ends.
 struct Walk {
     int b, kvh, i, n;                   // sequence, K/V head, tile index inside the pair, tiles of the pair
-    __device__ __forceinline__ void seek(const Schedule& s, int unit, int Hkv) {
-        b = 0;
-        while (s.start[b + 1] <= unit) ++b;
+    __device__ __forceinline__ void seek(const Schedule& s, int unit, int Hkv) {          // whole warps
+        const int lane = threadIdx.x & 31;
+        b = __popc(__ballot_sync(0xffffffffu, s.start[lane + 1] <= unit)) + __popc(__ballot_sync(0xffffffffu, s.start[lane + 33] <= unit));
         n = tiles_of(s, b, Hkv);
         const int in = unit - s.start[b];
         kvh = in / n;
@@ -128,24 +135,43 @@ struct Walk {
     __device__ __forceinline__ int tile(const Schedule& s) const { return i < s.sink_tiles[b] ? i : s.first[b] + i - s.sink_tiles[b]; }
 };
 
-// The units of this CTA's run; in whole mode, of its pair.
-__device__ __forceinline__ void run_units(const PagedArgs& a, const Schedule& s, int& u0, int& u1) {
-    if (a.whole) {
-        const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv, n = tiles_of(s, b, a.Hkv);
-        u0 = s.start[b] + kvh * n;
-        u1 = u0 + n;
-    } else {
-        const int total = s.start[kMaxCallBatch];
-        u0 = total > 0 ? run_begin(total, gridDim.x, blockIdx.x) : 0;
-        u1 = total > 0 ? run_begin(total, gridDim.x, blockIdx.x + 1) : 0;
-    }
-}
 // The G heads of a pair without a visible position: o = 0, lse = -inf.  Whole CTA.
 template <typename T>
 __device__ __forceinline__ void empty_pair(const PagedArgs& a, int b, int kvh, int dh) {
     T* out = static_cast<T*>(a.o) + ((size_t)b * a.Hq + (size_t)kvh * a.G) * dh;
     for (int i = threadIdx.x; i < a.G * dh; i += blockDim.x) out[i] = from_float<T>(0.f);
     if (a.lse != nullptr && threadIdx.x < a.G) a.lse[(size_t)b * a.Hq + kvh * a.G + threadIdx.x] = -INFINITY;
+}
+
+// What the join does for a run: the pair that begins in it and ends in a later one, if there is one.
+struct JoinItem { int pair, last_run, second, total; };          // pair: b * Hkv + kvh or -1; second: it is the run's second partial; all tiles
+
+// The units of this CTA's run; in whole mode, of its pair.  Also zeroes the pairs without a visible position (shared out over the
+// CTAs) and leaves the run's join item.  Whole CTA.
+template <typename T>
+__device__ __forceinline__ void begin_run(const PagedArgs& a, const Schedule& s, int dh, int& u0, int& u1) {
+    if (a.whole) {
+        const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv, n = tiles_of(s, b, a.Hkv);
+        u0 = s.start[b] + kvh * n;
+        u1 = u0 + n;
+        if (n == 0) empty_pair<T>(a, b, kvh, dh);
+        return;
+    }
+    const Runs runs(s.start[kMaxCallBatch], gridDim.x);
+    u0 = runs.begin(blockIdx.x);
+    u1 = runs.begin(blockIdx.x + 1);
+    for (int i = blockIdx.x; i < a.batch * a.Hkv; i += gridDim.x)
+        if (s.len[i / a.Hkv] == 0) empty_pair<T>(a, i / a.Hkv, i % a.Hkv, dh);
+    if (threadIdx.x < 32) {
+        JoinItem it = {-1, 0, 0, 0};
+        if (u0 < u1) {
+            Walk w;
+            w.seek(s, u1 - 1, a.Hkv);
+            const int e0 = u1 - 1 - w.i, e1 = e0 + w.n;          // the units of the run's last pair
+            if (e0 >= u0 && e1 > u1) it = {w.b * a.Hkv + w.kvh, runs.of(e1 - 1), e0 != u0 ? 1 : 0, runs.total};
+        }
+        if (threadIdx.x == 0) *reinterpret_cast<int4*>(a.join + blockIdx.x) = make_int4(it.pair, it.last_run, it.second, it.total);
+    }
 }
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
@@ -201,11 +227,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     finish_schedule(s);
     __syncthreads();
     int u0, u1;
-    run_units(a, s, u0, u1);
-    if (u0 >= u1) {
-        if (a.whole) empty_pair<bf16>(a, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, DH);
-        return;
-    }
+    begin_run<bf16>(a, s, DH, u0, u1);
+    if (u0 >= u1) return;
     Walk w;
     w.seek(s, u0, a.Hkv);
 
@@ -430,11 +453,8 @@ __global__ void __launch_bounds__(kConsumers * 32) paged_attn_simt_kernel(const 
     finish_schedule(s);
     __syncthreads();
     int u0, u1;
-    run_units(a, s, u0, u1);
-    if (u0 >= u1) {
-        if (a.whole) empty_pair<T>(a, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, DH);
-        return;
-    }
+    begin_run<T>(a, s, DH, u0, u1);
+    if (u0 >= u1) return;
     Walk w;
     w.seek(s, u0, a.Hkv);
     const T* K = static_cast<const T*>(a.k);
@@ -579,44 +599,31 @@ __global__ void __launch_bounds__(kConsumers * 32) paged_attn_simt_kernel(const 
 }
 
 // ------------------------------------------------------------------------------------------------
-// Joins the partials of every (sequence, query head) that more than one run worked on; zeroes the heads of empty sequences.
+// Joins the partials of every (sequence, query head) that more than one run worked on.
 // blockIdx.x = run: the CTA joins head blockIdx.y of the pair that begins in this run and ends in a later one (there is at most
-// one); eight warps share the partials, then meet in shared memory, always in the same order.
+// one, and the run left word of it); eight warps share the partials, then meet in shared memory, always in the same order.
 // ------------------------------------------------------------------------------------------------
 constexpr int kJoinWarps = 8;
 template <typename T, int DH>
-__global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const __grid_constant__ PagedArgs a, int runs) {
+__global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const __grid_constant__ PagedArgs a) {
     constexpr int kPer = (DH + 31) / 32;
-    __shared__ Schedule s;
     __shared__ float s_o[kJoinWarps][DH], s_m[kJoinWarps], s_l[kJoinWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     pdl_wait();
-    make_schedule(a, s);
-    __syncthreads();
-    finish_schedule(s);
-    __syncthreads();
-    const int total = s.start[kMaxCallBatch], r0 = blockIdx.x, g = blockIdx.y;
-    // empty sequences, one (row, K/V head) after the other over the CTAs
-    if (g == 0)
-        for (int i = r0; i < a.batch * a.Hkv; i += runs)
-            if (s.len[i / a.Hkv] == 0) empty_pair<T>(a, i / a.Hkv, i % a.Hkv, DH);
-    const int u1 = total > 0 ? run_begin(total, runs, r0 + 1) : 0, u0 = total > 0 ? run_begin(total, runs, r0) : 0;
-    if (u0 >= u1) return;
-    Walk w;
-    w.seek(s, u1 - 1, a.Hkv);                                    // the run's last pair
-    const int e0 = u1 - 1 - w.i, e1 = e0 + w.n;                  // its units
-    if (e0 < u0 || e1 <= u1) return;                             // begins in an earlier run, or ends here
-    const int b = w.b, kvh = w.kvh, r1 = run_of(total, runs, e1 - 1), head = kvh * a.G + g;
+    const int r0 = blockIdx.x, g = blockIdx.y;
+    const int4 it = __ldcg(reinterpret_cast<const int4*>(a.join + r0));
+    if (it.x < 0) return;
+    const int b = it.x / a.Hkv, kvh = it.x - b * a.Hkv, r1 = it.y, head = kvh * a.G + g;
     T* out = static_cast<T*>(a.o) + ((size_t)b * a.Hq + head) * DH;
-    const bool gaps = total < runs;                              // fewer tiles than runs: some runs are empty and left no partial
-    // this run holds the pair as its second part unless it begins with it
-    auto part = [&](int r) { return a.part + ((size_t)(2 * r + (r == r0 && e0 != u0 ? 1 : 0)) * 8 + g) * (DH + 2); };
+    const Runs runs(it.w, gridDim.x);
+    const bool gaps = runs.total < runs.runs;                    // fewer tiles than runs: some runs between are empty and left no partial
+    auto part = [&](int r) { return a.part + ((size_t)(2 * r + (r == r0 ? it.z : 0)) * 8 + g) * (DH + 2); };
     float M = -INFINITY, L = 0.f, acc[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
     for (int r = r0 + warp * 32 + lane; r <= r1; r += kJoinWarps * 32)
-        if (!gaps || run_begin(total, runs, r) < run_begin(total, runs, r + 1)) M = fmaxf(M, __ldcg(part(r) + DH));
+        if (!gaps || runs.begin(r) < runs.begin(r + 1)) M = fmaxf(M, __ldcg(part(r) + DH));
     M = warp_max(M);
     if (lane == 0) s_m[warp] = M;
     __syncthreads();
@@ -624,7 +631,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
     for (int i = 0; i < kJoinWarps; ++i) M = fmaxf(M, s_m[i]);
 #pragma unroll 4
     for (int r = r0 + warp; r <= r1; r += kJoinWarps) {
-        if (gaps && run_begin(total, runs, r) >= run_begin(total, runs, r + 1)) continue;
+        if (gaps && runs.begin(r) >= runs.begin(r + 1)) continue;
         const float* p = part(r);
         const float m = __ldcg(p + DH);
         const float f = m == -INFINITY ? 0.f : exp2f(m - M);
@@ -682,7 +689,7 @@ beagle_status launch_mma(const beagle_pages* p, const PagedArgs& a, int runs, cu
     if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes) == cudaSuccess; }))
         return BEAGLE_ERR_CUDA;
     launch_pdl(paged_attn_kernel<DH>, dim3(runs), dim3((kConsumers + 1) * 32), (size_t)SM::kBytes, stream, mk, mv, a);
-    if (!a.whole) launch_pdl(paged_attn_join_kernel<bf16, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a, runs);
+    if (!a.whole) launch_pdl(paged_attn_join_kernel<bf16, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a);
     return BEAGLE_OK;
 }
 
@@ -693,7 +700,7 @@ beagle_status launch_simt(const PagedArgs& a, int runs, cudaStream_t stream) {
     else if (a.G <= 4) launch_pdl(paged_attn_simt_kernel<T, DH, 4>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
     else if constexpr (DH * 8 * (int)sizeof(float) * kConsumers <= 16 * 1024 + 0) launch_pdl(paged_attn_simt_kernel<T, DH, 8>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
     else return BEAGLE_ERR_SHAPE;
-    if (!a.whole) launch_pdl(paged_attn_join_kernel<T, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a, runs);
+    if (!a.whole) launch_pdl(paged_attn_join_kernel<T, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a);
     return BEAGLE_OK;
 }
 
@@ -748,7 +755,7 @@ beagle_status beagle_paged_attn_workspace_bytes(const beagle_pages* p, int32_t n
     }
     const int sms = device_sm_count(), per = uses_mma(p) ? kCtasPerSm : kSimtCtasPerSm;
     const int runs = sms * per < kMaxRuns ? sms * per : kMaxRuns;
-    *bytes = ((size_t)2 * runs * 8 * (p->head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+    *bytes = ((size_t)runs * sizeof(JoinItem) + (size_t)2 * runs * 8 * (p->head_dim + 2) * sizeof(float) + 255) / 256 * 256;
     return BEAGLE_OK;
 }
 
@@ -778,7 +785,6 @@ beagle_status beagle_paged_attn(const beagle_pages* p, int32_t batch, const int3
     if ((long long)batch * p->n_kv_heads * ((long long)p->max_pages * p->page_size / kTile + 2) > 0x7fffffffll) return BEAGLE_ERR_CAPACITY;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     a.table = p->table; a.length = p->length; a.k = p->k; a.v = p->v; a.q = q_dev; a.o = out_dev; a.lse = lse_dev;
-    a.part = static_cast<float*>(ws_dev);
     a.q_stride = q_stride;
     a.batch = batch; a.n_pages = p->n_pages; a.max_pages = p->max_pages;
     a.page_shift = 0;
@@ -794,6 +800,8 @@ beagle_status beagle_paged_attn(const beagle_pages* p, int32_t batch, const int3
     if (runs > kMaxRuns) runs = kMaxRuns;
     if (runs > most) runs = most;
     if (a.whole) runs = (long long)batch * p->n_kv_heads;
+    a.join = static_cast<JoinItem*>(ws_dev);
+    a.part = a.whole ? nullptr : reinterpret_cast<float*>(a.join + runs);
     if (mma) st = p->head_dim == 128 ? launch_mma<128>(p, a, (int)runs, stream) : launch_mma<64>(p, a, (int)runs, stream);
     else if (p->dtype == BEAGLE_BF16) st = p->head_dim == 256 ? launch_simt<bf16, 256>(a, (int)runs, stream) : launch_simt<bf16, 32>(a, (int)runs, stream);
     else if (p->head_dim == 128) st = launch_simt<float, 128>(a, (int)runs, stream);

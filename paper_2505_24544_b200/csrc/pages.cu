@@ -138,13 +138,16 @@ __device__ __forceinline__ void load_refs(const int32_t* refs, int id0, int n_pa
     }
 }
 
-// The first `want` free pages, lowest id first, into list[]; returns how many there are (at most want).  Whole CTA.
-__device__ int find_free(const Book& b, int want, int32_t* list, int* s_warp) {
+constexpr int kNear = 4096;                      // entries of the page list that fit shared memory
+
+// The first `want` free pages, lowest id first, into list[]; returns how many there are (at most want).  `r`: this thread's counts
+// of the first step, loaded beforehand.  Whole CTA.
+__device__ __forceinline__ int find_free(const Book& b, int want, int32_t* list, int* s_warp, int* r) {
     int found = 0;
     for (int base = 0; base < b.n_pages && found < want; base += kBookThreads * kScanPer) {
         const int id0 = base + threadIdx.x * kScanPer;
-        int r[kScanPer], mine = 0, total;
-        load_refs(b.refs, id0, b.n_pages, r);
+        int mine = 0, total;
+        if (base > 0) load_refs(b.refs, id0, b.n_pages, r);
 #pragma unroll
         for (int i = 0; i < kScanPer; ++i) mine += r[i] == 0;
         int at = found + block_scan(mine, s_warp, total);
@@ -173,11 +176,14 @@ __device__ __forceinline__ void release_row(const Book& b, int32_t* row, int fro
 __global__ void __launch_bounds__(kBookThreads) pages_append_book_kernel(const Book b, const PageSlots slots, int batch, int T,
                                                                         const int32_t* n_new, int32_t* ok_out) {
     __shared__ int s_warp[33];
-    __shared__ int s_need[kMaxCallBatch], s_start[kMaxCallBatch], s_have[kMaxCallBatch], s_cow[kMaxCallBatch], s_ok[kMaxCallBatch];
+    __shared__ int s_need[kMaxCallBatch], s_start[kMaxCallBatch], s_have[kMaxCallBatch], s_cow[kMaxCallBatch];
+    __shared__ int32_t s_list[kNear];
     const int t = threadIdx.x;
     pdl_launch_dependents();
     pdl_wait();
     const BookWs ws = book_ws(b.ws, b.n_pages);
+    int refs[kScanPer];
+    load_refs(b.refs, t * kScanPer, b.n_pages, refs);    // on their way while the rows are looked up
     AppendRow r = {0, 0, -1, -1};
     int need = 0, want = 0;
     bool fits = true;
@@ -196,18 +202,19 @@ __global__ void __launch_bounds__(kBookThreads) pages_append_book_kernel(const B
         s_have[t] = have;
     }
     const int start = block_scan(need, s_warp, want);
-    const int got = find_free(b, want, ws.src, s_warp);
+    int32_t* list = want <= kNear ? s_list : ws.src;
+    const int got = find_free(b, want, list, s_warp, refs);
     __syncthreads();                                     // the list is complete (and, for the atomics below, read in full)
     if (t < batch) {
         const bool ok = fits && (need == 0 || start + need <= got);
         if (!ok) { need = 0; r.n = 0; r.cow_src = -1; }
         if (r.cow_src >= 0) {
-            r.cow_dst = ws.src[start];
+            r.cow_dst = list[start];
             b.row(slots.slot[t])[r.len / b.page_size] = r.cow_dst;
             b.refs[r.cow_dst] = 1;
             atomicSub(b.refs + r.cow_src, 1);
         }
-        s_need[t] = need; s_start[t] = start; s_cow[t] = r.cow_src >= 0 ? 1 : 0; s_ok[t] = ok ? 1 : 0;
+        s_need[t] = need; s_start[t] = start; s_cow[t] = r.cow_src >= 0 ? 1 : 0;
         ws.rows[t] = r;
         if (ok && r.n > 0) b.length[slots.slot[t]] = r.len + r.n;
         if (ok_out != nullptr) ok_out[t] = ok ? 1 : 0;
@@ -217,7 +224,7 @@ __global__ void __launch_bounds__(kBookThreads) pages_append_book_kernel(const B
     for (int row = t >> 5; row < batch; row += kBookThreads / 32) {
         int32_t* dst = b.row(slots.slot[row]);
         for (int i = s_cow[row] + lane; i < s_need[row]; i += 32) {
-            const int id = ws.src[s_start[row] + i];
+            const int id = list[s_start[row] + i];
             dst[s_have[row] + i - s_cow[row]] = id;
             b.refs[id] = 1;
         }
@@ -318,13 +325,15 @@ __global__ void __launch_bounds__(kBookThreads) pages_copy_book_kernel(const Boo
     for (int i = t >> 5; i < n; i += kBookThreads / 32) release_row(b, b.row(dst.slot[i]), 0, lane);
     __threadfence();
     __syncthreads();                                     // what the destinations held is free now
+    int refs[kScanPer];
+    load_refs(b.refs, t * kScanPer, b.n_pages, refs);
     int need = 0, len = 0, want = 0;
     if (t < n) {
         len = b.clamp_len(__ldcg(b.length + src.slot[t]));
         need = (len + b.page_size - 1) / b.page_size;
     }
     const int start = block_scan(need, s_warp, want);
-    const int got = find_free(b, want, ws.dst, s_warp);
+    const int got = find_free(b, want, ws.dst, s_warp, refs);
     __syncthreads();
     if (t < n) {
         const bool ok = need == 0 || start + need <= got;
