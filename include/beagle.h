@@ -327,6 +327,28 @@ beagle_status beagle_paged_attn(const beagle_pages* pages, int32_t batch, const 
                                 int64_t q_stride, int32_t window, int32_t sinks, void* out_dev, float* lse_dev, void* ws_dev,
                                 size_t ws_bytes, void* stream);
 
+/* The draft head over a paged cache.  The slots of these calls are both the context's (previous token and state of a chain)
+ * and the cache's (keys and values); the cache has the context's storage type, n_kv_heads and head_dim (SHAPE otherwise); the
+ * context's own cache is not touched.  A slot has one chain: drop it (beagle_rollback) before going over from pages to the
+ * context's cache or back.  No rotary option (UNSUPPORTED): its positions live on the host, these lengths do not.  max_ctx and
+ * max_draft do not bound a paged slot; max_pages and the free pages do.
+ *
+ * beagle_prefill_pages: beagle_prefill_kv into pages.  The new_len[b] rows of hidden_dev (packed) are projected with W_k, W_v
+ *   and appended to slot seq_slot[b] as beagle_pages_append does (ok_dev as there); the chain of the slot starts anew.  The
+ *   draft states of a chain stay in the slot until the caller cuts them off (beagle_pages_truncate to the true length).
+ *   ws_dev: beagle_prefill_pages_workspace_bytes, 256-byte aligned.  Works like beagle_prefill_kv under stream capture.
+ * beagle_draft_step_pages: beagle_draft_step whose attention reads the slot's pages, whole (window 0) or through the window
+ *   and sinks of beagle_paged_attn.  With concat the slot's previous state is projected and appended to its pages first;
+ *   ok_dev int32 [batch] (nullable): 0 where no page was free for it (the step then reads the slot without it), else 1. */
+beagle_status beagle_prefill_pages_workspace_bytes(const beagle_config* cfg, int64_t rows, size_t* bytes);
+beagle_status beagle_prefill_pages(beagle_ctx* ctx, const beagle_pages* pages, int32_t batch, const int32_t* seq_slot_host,
+                                   const int32_t* new_len_host, const void* hidden_dev, int32_t* ok_dev, void* ws_dev,
+                                   size_t ws_bytes, void* stream);
+beagle_status beagle_draft_step_pages(beagle_ctx* ctx, const beagle_pages* pages, int32_t batch, const int32_t* seq_slot_host,
+                                      const int32_t* tokens_in_dev, int32_t concat, int32_t window, int32_t sinks,
+                                      int32_t* tokens_out_dev, int32_t tokens_out_stride, float* logits_out_dev,
+                                      void* hidden_out_dev, int32_t* ok_dev, void* stream);
+
 /* ---- Attention over whole sequences with a sliding window and sinks, forward and backward ---------------------------
  * The training and prompt form of beagle_paged_attn's window.  `batch` sequences (at most BEAGLE_MAX_CALL_BATCH) lie one
  * after the other: sequence b has q_len_host[b] query rows and kv_len_host[b] key / value rows (HOST arrays, any length from

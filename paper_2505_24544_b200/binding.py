@@ -34,6 +34,7 @@ EXPORTED_SYMBOLS = (
     "beagle_packed_weights_bytes", "beagle_pack_weights",
     "beagle_pages_workspace_bytes", "beagle_pages_reset", "beagle_pages_append", "beagle_pages_truncate", "beagle_pages_fork",
     "beagle_pages_copy", "beagle_pages_compact", "beagle_paged_attn_workspace_bytes", "beagle_paged_attn",
+    "beagle_prefill_pages_workspace_bytes", "beagle_prefill_pages", "beagle_draft_step_pages",
     "beagle_window_attn_forward", "beagle_window_attn_workspace_bytes", "beagle_window_attn_backward",
 )
 
@@ -149,6 +150,11 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     for name in ("workspace_bytes", "reset", "append", "truncate", "fork", "copy", "compact"):
         getattr(lib, "beagle_pages_" + name).restype = C.c_int
     lib.beagle_paged_attn_workspace_bytes.restype = C.c_int
+    lib.beagle_prefill_pages_workspace_bytes.argtypes = [C.POINTER(BeagleConfig), i64, szp]
+    lib.beagle_prefill_pages.argtypes = [vp, pg, i32, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.beagle_draft_step_pages.argtypes = [vp, pg, i32, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp, vp]
+    for name in ("beagle_prefill_pages_workspace_bytes", "beagle_prefill_pages", "beagle_draft_step_pages"):
+        getattr(lib, name).restype = C.c_int
     wa = C.POINTER(BeagleWindowAttn)
     lib.beagle_window_attn_forward.argtypes = [wa, vp, vp, vp]
     lib.beagle_window_attn_workspace_bytes.argtypes = [wa, szp]
@@ -681,6 +687,35 @@ def beagle_paged_attn(cache: PagedCache, slots: Sequence[int], q: torch.Tensor, 
               "beagle_paged_attn")
 
 
+def beagle_prefill_pages(ctx: Context, cache: PagedCache, seq_slot: Sequence[int], new_len: Sequence[int], hidden: Optional[torch.Tensor],
+                         ok: Optional[torch.Tensor] = None) -> None:
+    """Keys and values of the target's states (packed rows, as ``beagle_prefill_kv``) into the slots' pages."""
+    rows = sum(new_len)
+    hp = None if hidden is None else _check("hidden", hidden, torch_dtype(ctx.cfg.dtype), (rows, ctx.cfg.hidden))
+    ok_ptr = None if ok is None else _check("ok", ok, torch.int32, (len(seq_slot),))
+    n = C.c_size_t()
+    st = ctx.lib.beagle_prefill_pages_workspace_bytes(C.byref(ctx.cfg), rows, C.byref(n))
+    if st != 0:
+        raise BeagleError(st, "beagle_prefill_pages_workspace_bytes")
+    ws = torch.empty(max(n.value, 1), dtype=torch.uint8, device=cache.k.device)
+    ctx.check(ctx.lib.beagle_prefill_pages(ctx.handle, cache.ref, len(seq_slot), _host_i32(seq_slot), _host_i32(new_len), hp, ok_ptr, ws.data_ptr(),
+                                           ws.numel(), cache.on_current_device()))
+
+
+def beagle_draft_step_pages(ctx: Context, cache: PagedCache, seq_slot: Sequence[int], tokens_in: Optional[torch.Tensor], concat: bool,
+                            tokens_out: Optional[torch.Tensor], logits_out: Optional[torch.Tensor] = None, hidden_out: Optional[torch.Tensor] = None,
+                            window: int = 0, sinks: int = 0, ok: Optional[torch.Tensor] = None) -> None:
+    """``beagle_draft_step`` over the slots' pages, whole or through a window with sinks."""
+    stride, out_ptr = 1, None
+    if tokens_out is not None:
+        if tokens_out.dim() != 1 or tokens_out.dtype != torch.int32:
+            raise ValueError("tokens_out must be a 1-D int32 tensor (a column view is fine)")
+        stride, out_ptr = int(tokens_out.stride(0)), tokens_out.data_ptr()
+    ok_ptr = None if ok is None else _check("ok", ok, torch.int32, (len(seq_slot),))
+    ctx.check(ctx.lib.beagle_draft_step_pages(ctx.handle, cache.ref, len(seq_slot), _host_i32(seq_slot), _ptr(tokens_in), int(bool(concat)), window, sinks,
+                                              out_ptr, stride, _ptr(logits_out), _ptr(hidden_out), ok_ptr, cache.on_current_device()))
+
+
 # ---- attention over whole sequences with a window and sinks -------------------------------------
 
 def _window_attn(q, k, v, q_len, kv_len, window, sinks, strict) -> Tuple[BeagleWindowAttn, int]:
@@ -783,6 +818,22 @@ class BeagleHead:
         logits = torch.empty(B, self.cfg.vocab, dtype=torch.float32, device=self.device) if want_logits else None
         hidden = torch.empty(B, self.cfg.hidden, dtype=self.dtype, device=self.device) if want_hidden else None
         beagle_draft_step(self.ctx, seq_slot, tokens_in, concat, tokens_out, logits, hidden)
+        return tokens_out, logits, hidden
+
+    def paged_cache(self, n_pages, page_size, max_slots, max_pages) -> PagedCache:
+        """A paged cache of this head's type and shape (for ``prefill_pages`` and ``draft_step_pages``)."""
+        return PagedCache(n_pages, page_size, self.cfg.n_kv_heads, self.cfg.head_dim, max_slots, max_pages,
+                          "bf16" if self.cfg.dtype == BEAGLE_BF16 else "fp32", self.device)
+
+    def prefill_pages(self, cache, seq_slot, new_len, hidden, ok=None):
+        beagle_prefill_pages(self.ctx, cache, seq_slot, new_len, hidden, ok)
+
+    def draft_step_pages(self, cache, seq_slot, tokens_in=None, concat=True, want_logits=False, want_hidden=False, window=0, sinks=0, ok=None):
+        B = len(seq_slot)
+        tokens_out = torch.empty(B, dtype=torch.int32, device=self.device)
+        logits = torch.empty(B, self.cfg.vocab, dtype=torch.float32, device=self.device) if want_logits else None
+        hidden = torch.empty(B, self.cfg.hidden, dtype=self.dtype, device=self.device) if want_hidden else None
+        beagle_draft_step_pages(self.ctx, cache, seq_slot, tokens_in, concat, tokens_out, logits, hidden, window, sinks, ok)
         return tokens_out, logits, hidden
 
     def block_forward(self, tokens, hidden, block, offset=0, sim_steps=1, want_logits=True, want_hidden=True):

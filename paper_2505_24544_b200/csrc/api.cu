@@ -9,6 +9,7 @@
 #include "../../include/beagle.h"
 #include "kernels.h"
 #include "gemm_tc.h"
+#include "pages.h"
 
 using namespace beagle;
 
@@ -46,6 +47,7 @@ struct beagle_ctx {
     void* vs_scratch = nullptr;     // log-sum-exp partials and chunk masses of beagle_verify_sample
     void* tree_mem = nullptr;       // node / frontier arrays of beagle_draft_tree
     float* tree_logits = nullptr;   // [kTreeMaxTopk, V] logits of the frontier rows
+    void *kv_rows = nullptr, *paged_ws = nullptr;   // paged steps: the keys and values of the appended states, attention partials
     void* hq = nullptr;             // FP8 LM head: quantised states of the step and their row scales
     float* hscale = nullptr;
     float* rope_table = nullptr;    // (cos, sin) per (position, i < dh/2); rotary option only
@@ -144,7 +146,7 @@ beagle_status check_config(const beagle_config* c) {
 }
 
 struct ServeLayout {
-    size_t x, xn, q, o, y, yn, act, h, h_slot, hs, attn, sk_partial, last_token, ids, lm_partials, verify_keys, vs_scratch, tree_mem, tree_logits, rope, hq, hscale, dev_error, total;
+    size_t x, xn, q, o, y, yn, act, h, h_slot, hs, attn, sk_partial, last_token, ids, lm_partials, verify_keys, vs_scratch, tree_mem, tree_logits, rope, hq, hscale, kv_rows, paged, dev_error, total;
     int lm_blocks;
 };
 // Device words that must read zero before the first kernel uses them: the error word (first 256 bytes), one completion
@@ -169,7 +171,7 @@ ServeLayout serve_layout(const beagle_config& c) {
         const int kd = c.n_kv_heads * c.head_dim;
         size_t need = 0;
         if (c.dtype == BEAGLE_BF16) {
-            const size_t cand[5] = {tc_skinny_partial_bytes((int)qd, (int)d, 1), tc_skinny_partial_bytes(kd, (int)d, 2),
+            const size_t cand[6] = {tc_skinny_partial_bytes((int)qd, (int)d, 1), tc_skinny_partial_bytes(kd, (int)d, 2), tc_skinny_partial_bytes(kd, (int)d, 1),
                                     tc_skinny_partial_bytes((int)d, (int)qd, 1), tc_skinny_partial_bytes((int)m, (int)d, 2),
                                     tc_skinny_partial_bytes((int)d, (int)m, 1)};
             for (size_t v : cand) need = v > need ? v : need;
@@ -187,6 +189,8 @@ ServeLayout serve_layout(const beagle_config& c) {
     L.tree_logits = take(c.dtype == BEAGLE_BF16 ? (size_t)kTreeMaxTopk * c.vocab * sizeof(float) : 0);
     L.rope = take(c.rope_theta > 0.f ? ((size_t)c.max_ctx + c.max_draft + 1) * (c.head_dim / 2) * 2 * sizeof(float) : 0);
     L.hq = take(B * d); L.hscale = take(B * sizeof(float));                    // FP8 LM head: the step's states as E4M3 bytes + row scales
+    L.kv_rows = take(2 * B * c.n_kv_heads * c.head_dim * elt);
+    L.paged = take(paged_attn_workspace_most(c.dtype, c.head_dim));
     L.dev_error = take(dev_words_bytes(c));    // error word, the attention completion counters, the verification tickets
     L.total = off;
     return L;
@@ -424,6 +428,8 @@ beagle_status beagle_create(const beagle_config* cfg, const beagle_weights* w, v
     c->vs_scratch = c->ws + L.vs_scratch;
     c->tree_mem = c->ws + L.tree_mem;
     c->tree_logits = reinterpret_cast<float*>(c->ws + L.tree_logits);
+    c->kv_rows = c->ws + L.kv_rows;
+    c->paged_ws = c->ws + L.paged;
     c->hq = c->ws + L.hq;
     c->hscale = reinterpret_cast<float*>(c->ws + L.hscale);
     c->rope_table = reinterpret_cast<float*>(c->ws + L.rope);
@@ -729,12 +735,39 @@ beagle_status beagle_prefill_kv(beagle_ctx* ctx, int32_t batch, const int32_t* s
     return BEAGLE_OK;
 }
 
-beagle_status beagle_draft_step(beagle_ctx* ctx, int32_t batch, const int32_t* seq_slot, const int32_t* tokens_in_dev,
+// The cache of a paged step: the slots' keys and values lie in pages, of which every query sees a window and the sinks.
+struct PagedStep {
+    const beagle_pages* pages;
+    int window, sinks;
+    int32_t* ok;            // device [batch] or NULL: the append of each row
+};
+
+// A cache that fits the context: same storage type and K/V heads, every listed slot in its table.  Rotary keys need their
+// positions on the host, which a paged cache does not have.
+static beagle_status check_pages(beagle_ctx* ctx, const beagle_pages* pages, int32_t batch, const int32_t* seq_slot) {
+    const beagle_status st = pages_check(pages);
+    if (st != BEAGLE_OK) return fail(ctx, st, "pages: the cache structure is not valid");
+    const beagle_config& c = ctx->cfg;
+    if (pages->dtype != c.dtype || pages->n_kv_heads != c.n_kv_heads || pages->head_dim != c.head_dim)
+        return fail(ctx, BEAGLE_ERR_SHAPE, "pages: storage type, K/V heads and head_dim must be the context's");
+    if (c.rope_theta > 0.f) return fail(ctx, BEAGLE_ERR_UNSUPPORTED, "pages: no rotary embedding");
+    for (int b = 0; b < batch; ++b)
+        if (seq_slot[b] >= pages->max_slots) return fail(ctx, BEAGLE_ERR_INVALID_ARG, "pages: slot %d out of range", seq_slot[b]);
+    if (!paged_attn_fits(pages, batch)) return fail(ctx, BEAGLE_ERR_CAPACITY, "pages: more tiles than one call counts");
+    return BEAGLE_OK;
+}
+
+static beagle_status draft_step(beagle_ctx* ctx, int32_t batch, const int32_t* seq_slot, const int32_t* tokens_in_dev,
                                 int32_t concat, int32_t* tokens_out_dev, int32_t tokens_out_stride, float* logits_out_dev,
-                                void* hidden_out_dev, void* stream_) {
+                                void* hidden_out_dev, const PagedStep* paged, void* stream_) {
     if (ctx == nullptr) return BEAGLE_ERR_INVALID_ARG;
     beagle_status st = check_slots(ctx, batch, seq_slot);
     if (st != BEAGLE_OK) return st;
+    if (paged != nullptr) {
+        st = check_pages(ctx, paged->pages, batch, seq_slot);
+        if (st != BEAGLE_OK) return st;
+        if (paged->window < 0 || paged->sinks < 0) return fail(ctx, BEAGLE_ERR_INVALID_ARG, "window and sinks must not be negative");
+    }
     if (batch == 0) return BEAGLE_OK;
     if (tokens_out_dev != nullptr && tokens_out_stride < 1) return fail(ctx, BEAGLE_ERR_INVALID_ARG, "tokens_out_stride must be >= 1");
     const beagle_config& c = ctx->cfg;
@@ -744,7 +777,7 @@ beagle_status beagle_draft_step(beagle_ctx* ctx, int32_t batch, const int32_t* s
         if (tokens_in_dev == nullptr && !ctx->has_token[s])
             return fail(ctx, BEAGLE_ERR_STATE, "slot %d has no previous draft token; pass tokens_in", s);
         if (concat && ctx->pending[s]) {
-            if (ctx->n_draft[s] >= c.max_draft)
+            if (paged == nullptr && ctx->n_draft[s] >= c.max_draft)
                 return fail(ctx, BEAGLE_ERR_CAPACITY, "slot %d: draft tail already holds max_draft = %d states", s, c.max_draft);
             any_append = true;
         }
@@ -773,6 +806,24 @@ beagle_status beagle_draft_step(beagle_ctx* ctx, int32_t batch, const int32_t* s
         meta.kv_len[b] = ctx->n_true[s] + ctx->n_draft[s] + (app ? 1 : 0);
         slots.idx[b] = s;
         if (meta.kv_len[b] > max_kv) max_kv = meta.kv_len[b];
+    }
+    // Where the projections of the appended states go: the cache tail, or (paged) dense rows that the pages' append then takes.
+    void *k_to = ctx->kcache, *v_to = ctx->vcache;
+    int to_cap = ctx->cap;
+    RowMap to_slot = slots;
+    AppendRows app_rows;
+    if (paged != nullptr) {
+        k_to = ctx->kv_rows;
+        v_to = static_cast<char*>(ctx->kv_rows) + (size_t)kMaxCallBatch * ctx->kd * ctx->elt;
+        to_cap = 1;
+        to_slot = ident;
+        memset(&app_rows, 0, sizeof(app_rows));
+        for (int b = 0; b < batch; ++b) {
+            const bool app = app_pos.idx[b] >= 0;
+            app_pos.idx[b] = app ? 0 : -1;
+            app_rows.start[b] = b;
+            app_rows.count[b] = app ? 1 : 0;
+        }
     }
 
     // Batches above 8 rows run their projections on the tensor cores (weights streamed once);
@@ -805,8 +856,8 @@ beagle_status beagle_draft_step(beagle_ctx* ctx, int32_t batch, const int32_t* s
         q.W = ctx->w.w_q; q.N = ctx->qd; q.K = c.hidden; q.X = ctx->xn; q.ldx = c.hidden; q.B = batch;
         q.out = ctx->q; q.ldo = ctx->qd; q.error_word = ctx->dev_error;
         kv.W = ctx->w.w_k; kv.W2 = ctx->w.w_v; kv.N = ctx->kd; kv.K = c.hidden; kv.X = ctx->hs; kv.ldx = c.hidden; kv.B = batch;
-        kv.kcache = ctx->kcache; kv.vcache = ctx->vcache; kv.Hkv = c.n_kv_heads; kv.dh = c.head_dim; kv.cap = ctx->cap;
-        kv.slot = slots; kv.pos = app_pos;
+        kv.kcache = k_to; kv.vcache = v_to; kv.Hkv = c.n_kv_heads; kv.dh = c.head_dim; kv.cap = to_cap;
+        kv.slot = to_slot; kv.pos = app_pos;
         rc = tc_skinny_qkv(ctx->tc, q, kv, stream);
         if (rc > 0) { ctx->launches += rc; merged_qkv = true; }
     }
@@ -817,16 +868,16 @@ beagle_status beagle_draft_step(beagle_ctx* ctx, int32_t batch, const int32_t* s
             SkinnyArgs a;
             memset(&a, 0, sizeof(a));
             a.W = ctx->w.w_k; a.W2 = ctx->w.w_v; a.N = ctx->kd; a.K = c.hidden; a.X = ctx->hs; a.ldx = c.hidden; a.B = batch;
-            a.kcache = ctx->kcache; a.vcache = ctx->vcache; a.Hkv = c.n_kv_heads; a.dh = c.head_dim; a.cap = ctx->cap;
-            a.slot = slots; a.pos = app_pos;
+            a.kcache = k_to; a.vcache = v_to; a.Hkv = c.n_kv_heads; a.dh = c.head_dim; a.cap = to_cap;
+            a.slot = to_slot; a.pos = app_pos;
             BEAGLE_SKINNY(SK_KV, a, "K/V append");
         } else {
             GemvArgs a;
             memset(&a, 0, sizeof(a));
             a.W = ctx->w.w_k; a.W2 = ctx->w.w_v; a.N = ctx->kd; a.K = c.hidden;
             a.X = ctx->h_slot; a.ldx = c.hidden; a.B = batch; a.xrow = slots;
-            a.kcache = ctx->kcache; a.vcache = ctx->vcache; a.Hkv = c.n_kv_heads; a.dh = c.head_dim; a.cap = ctx->cap;
-            a.orow2 = slots; a.pos = app_pos;
+            a.kcache = k_to; a.vcache = v_to; a.Hkv = c.n_kv_heads; a.dh = c.head_dim; a.cap = to_cap;
+            a.orow2 = to_slot; a.pos = app_pos;
             ctx->launches += launch_gemv(dt, GEMV_KV, a, stream);
         }
     }
@@ -860,7 +911,21 @@ beagle_status beagle_draft_step(beagle_ctx* ctx, int32_t batch, const int32_t* s
                                            slots, app_pos, qpos, kpos, ctx->rope_table, stream);
     }
     // (4) o = softmax(Q K^T / sqrt(dh)) V over the cache
-    {
+    if (paged != nullptr) {
+        if (any_append || paged->ok != nullptr) {
+            StageTimer timer_(ctx, ST_KV_APPEND, stream);
+            st = pages_append_rows(paged->pages, batch, seq_slot, app_rows, nullptr, k_to, ctx->kd, v_to, ctx->kd, paged->ok, stream);
+            if (st != BEAGLE_OK) return fail(ctx, st, "draft_step: the append to the pages failed");
+            ctx->launches += any_append ? 2 : 1;
+        }
+        StageTimer timer_(ctx, ST_ATTN_DECODE, stream);
+        st = beagle_paged_attn(paged->pages, batch, seq_slot, c.n_q_heads, ctx->q, ctx->qd, paged->window, paged->sinks, ctx->o, nullptr, ctx->paged_ws,
+                               paged_attn_workspace_most(c.dtype, c.head_dim), stream);
+        if (st != BEAGLE_OK) return fail(ctx, st, "draft_step: the attention over the pages failed");
+        size_t joined = 0;              // an attention that splits its sequences takes a second launch
+        beagle_paged_attn_workspace_bytes(paged->pages, c.n_q_heads, paged->window, paged->sinks, &joined);
+        ctx->launches += joined > 0 ? 2 : 1;
+    } else {
         StageTimer timer_(ctx, ST_ATTN_DECODE, stream);
         rc = -1;
         if (ctx->tc != nullptr) {       // bf16, head_dim 64 / 128: TMA-staged tiles
@@ -975,10 +1040,114 @@ beagle_status beagle_draft_step(beagle_ctx* ctx, int32_t batch, const int32_t* s
     if (st != BEAGLE_OK) return st;
     for (int b = 0; b < batch; ++b) {
         const int s = seq_slot[b];
-        if (concat && ctx->pending[s]) ctx->n_draft[s] += 1;
+        if (paged == nullptr && concat && ctx->pending[s]) ctx->n_draft[s] += 1;
         ctx->pending[s] = 1;
         ctx->has_token[s] = 1;
         ctx->steps[s] += 1;
+    }
+    return BEAGLE_OK;
+}
+
+beagle_status beagle_draft_step(beagle_ctx* ctx, int32_t batch, const int32_t* seq_slot, const int32_t* tokens_in_dev,
+                                int32_t concat, int32_t* tokens_out_dev, int32_t tokens_out_stride, float* logits_out_dev,
+                                void* hidden_out_dev, void* stream) {
+    return draft_step(ctx, batch, seq_slot, tokens_in_dev, concat, tokens_out_dev, tokens_out_stride, logits_out_dev, hidden_out_dev, nullptr, stream);
+}
+
+beagle_status beagle_draft_step_pages(beagle_ctx* ctx, const beagle_pages* pages, int32_t batch, const int32_t* seq_slot, const int32_t* tokens_in_dev,
+                                      int32_t concat, int32_t window, int32_t sinks, int32_t* tokens_out_dev, int32_t tokens_out_stride,
+                                      float* logits_out_dev, void* hidden_out_dev, int32_t* ok_dev, void* stream) {
+    if (ctx == nullptr || pages == nullptr) return BEAGLE_ERR_INVALID_ARG;
+    const PagedStep paged = {pages, window, sinks, ok_dev};
+    return draft_step(ctx, batch, seq_slot, tokens_in_dev, concat, tokens_out_dev, tokens_out_stride, logits_out_dev, hidden_out_dev, &paged, stream);
+}
+
+beagle_status beagle_prefill_pages_workspace_bytes(const beagle_config* cfg, int64_t rows, size_t* bytes) {
+    const beagle_status st = check_config(cfg);
+    if (st != BEAGLE_OK) return st;
+    if (bytes == nullptr || rows < 0) return BEAGLE_ERR_INVALID_ARG;
+    if (rows > (1ll << 24)) return BEAGLE_ERR_CAPACITY;
+    *bytes = 2 * align_up((size_t)rows * cfg->n_kv_heads * cfg->head_dim * (cfg->dtype == BEAGLE_BF16 ? 2 : 4));
+    return BEAGLE_OK;
+}
+
+beagle_status beagle_prefill_pages(beagle_ctx* ctx, const beagle_pages* pages, int32_t batch, const int32_t* seq_slot, const int32_t* new_len,
+                                   const void* hidden_dev, int32_t* ok_dev, void* ws_dev, size_t ws_bytes, void* stream_) {
+    if (ctx == nullptr || pages == nullptr) return BEAGLE_ERR_INVALID_ARG;
+    beagle_status st = check_slots(ctx, batch, seq_slot);
+    if (st != BEAGLE_OK) return st;
+    st = check_pages(ctx, pages, batch, seq_slot);
+    if (st != BEAGLE_OK) return st;
+    if (batch > 0 && new_len == nullptr) return fail(ctx, BEAGLE_ERR_INVALID_ARG, "new_len is NULL");
+    const beagle_config& c = ctx->cfg;
+    AppendRows rows;
+    memset(&rows, 0, sizeof(rows));
+    long long total = 0;
+    for (int b = 0; b < batch; ++b) {
+        if (new_len[b] < 0) return fail(ctx, BEAGLE_ERR_INVALID_ARG, "new_len[%d] is negative", b);
+        rows.start[b] = total;
+        rows.count[b] = new_len[b];
+        total += new_len[b];
+    }
+    size_t need = 0;
+    if (beagle_prefill_pages_workspace_bytes(&c, total, &need) != BEAGLE_OK) return fail(ctx, BEAGLE_ERR_CAPACITY, "%lld rows in one call", total);
+    if (total > 0) {
+        if (hidden_dev == nullptr || (reinterpret_cast<uintptr_t>(hidden_dev) & 15)) return fail(ctx, BEAGLE_ERR_INVALID_ARG, "hidden is NULL or not 16-byte aligned");
+        if (ws_dev == nullptr || (reinterpret_cast<uintptr_t>(ws_dev) & (kAlign - 1))) return fail(ctx, BEAGLE_ERR_INVALID_ARG, "workspace is NULL or not 256-byte aligned");
+        if (ws_bytes < need) return fail(ctx, BEAGLE_ERR_CAPACITY, "workspace: %zu bytes, %zu needed", ws_bytes, need);
+    }
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    char *K = static_cast<char*>(ws_dev), *V = K + need / 2;
+    if (total > 0) {
+        st = device_setup_once(ctx, stream);
+        if (st != BEAGLE_OK) return st;
+        StageTimer timer_(ctx, ST_PREFILL, stream);
+        const bool small = total <= (ctx->tc != nullptr ? kServeTcMinBatch : 16);
+        for (int m = 0; m < 2; ++m) {                       // K = H W_k^T, V = H W_v^T as dense rows; kernels by row count as in prefill_kv
+            const void* W = m == 0 ? ctx->w.w_k : ctx->w.w_v;
+            char* out = m == 0 ? K : V;
+            if (total <= (ctx->tc != nullptr ? kServeTcMinBatch : 16)) {
+                GemvArgs a;
+                memset(&a, 0, sizeof(a));
+                a.W = W; a.N = ctx->kd; a.K = c.hidden; a.X = hidden_dev; a.ldx = c.hidden; a.B = (int)total; a.out = out; a.ldo = ctx->kd;
+                for (int i = 0; i < a.B; ++i) a.xrow.idx[i] = i;
+                ctx->launches += launch_gemv(c.dtype, GEMV_STORE, a, stream);
+            } else if (ctx->tc != nullptr && total <= kPrefillSkinnyMaxRows) {
+                for (long long r0 = 0; r0 < total; r0 += kMaxCallBatch) {
+                    SkinnyArgs a;
+                    memset(&a, 0, sizeof(a));
+                    a.W = W; a.N = ctx->kd; a.K = c.hidden;
+                    a.X = static_cast<const char*>(hidden_dev) + (size_t)r0 * c.hidden * ctx->elt; a.ldx = c.hidden;
+                    a.B = (int)(total - r0 < kMaxCallBatch ? total - r0 : kMaxCallBatch);
+                    a.out = out + (size_t)r0 * ctx->kd * ctx->elt; a.ldo = ctx->kd;
+                    a.partial = ctx->sk_partial; a.error_word = ctx->dev_error;
+                    const int rc = tc_skinny(ctx->tc, SK_STORE, a, stream);
+                    if (rc < 0) return fail(ctx, BEAGLE_ERR_SHAPE, "K/V projection: unsupported shape");
+                    ctx->launches += rc;
+                }
+            } else {
+                GemmArgs g;
+                memset(&g, 0, sizeof(g));
+                g.A = hidden_dev; g.lda = c.hidden; g.M = (int)total; g.N = ctx->kd; g.K = c.hidden; g.W = W; g.C = out; g.ldc = ctx->kd;
+                const int rc = dense_gemm(ctx, GEMM_STORE, g, stream);
+                if (rc < 0) return fail(ctx, BEAGLE_ERR_SHAPE, "K/V projection: unsupported shape");
+                ctx->launches += rc;
+            }
+        }
+    }
+    if (total > 0 || (ok_dev != nullptr && batch > 0)) {
+        StageTimer timer_(ctx, ST_PREFILL, stream);
+        st = pages_append_rows(pages, batch, seq_slot, rows, nullptr, total > 0 ? K : nullptr, ctx->kd, total > 0 ? V : nullptr, ctx->kd, ok_dev, stream);
+        if (st != BEAGLE_OK) return fail(ctx, st, "prefill_pages: the append to the pages failed");
+        ctx->launches += total > 0 ? 2 : 1;
+        st = cuda_ok(ctx, "prefill_pages");
+        if (st != BEAGLE_OK) return st;
+    }
+    for (int b = 0; b < batch; ++b) {
+        const int s = seq_slot[b];
+        ctx->pending[s] = 0;
+        ctx->has_token[s] = 0;
+        ctx->steps[s] = 0;
     }
     return BEAGLE_OK;
 }

@@ -714,6 +714,16 @@ beagle_status check_heads(const beagle_pages* p, int Hq) {
 
 }  // namespace
 
+bool paged_attn_fits(const beagle_pages* p, int batch) {
+    return (long long)batch * p->n_kv_heads * ((long long)p->max_pages * p->page_size / kTile + 2) <= 0x7fffffffll;
+}
+
+size_t paged_attn_workspace_most(int dtype, int head_dim) {
+    const int per = dtype == BEAGLE_BF16 && (head_dim == 64 || head_dim == 128) ? kCtasPerSm : kSimtCtasPerSm;
+    const int sms = device_sm_count(), runs = sms * per < kMaxRuns ? sms * per : kMaxRuns;
+    return ((size_t)runs * sizeof(JoinItem) + (size_t)2 * runs * 8 * (head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+}
+
 int device_sm_count() {
     static std::atomic<int> counts[PerDeviceOnce::kMaxDevices];
     int dev = 0, n = 0;
@@ -753,9 +763,7 @@ beagle_status beagle_paged_attn_workspace_bytes(const beagle_pages* p, int32_t n
         *bytes = 0;
         return BEAGLE_OK;
     }
-    const int sms = device_sm_count(), per = uses_mma(p) ? kCtasPerSm : kSimtCtasPerSm;
-    const int runs = sms * per < kMaxRuns ? sms * per : kMaxRuns;
-    *bytes = ((size_t)runs * sizeof(JoinItem) + (size_t)2 * runs * 8 * (p->head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+    *bytes = paged_attn_workspace_most(p->dtype, p->head_dim);
     return BEAGLE_OK;
 }
 
@@ -781,8 +789,7 @@ beagle_status beagle_paged_attn(const beagle_pages* p, int32_t batch, const int3
     if (q_dev == nullptr || out_dev == nullptr || (need > 0 && ws_dev == nullptr) || q_stride < (int64_t)n_q_heads * p->head_dim) return BEAGLE_ERR_INVALID_ARG;
     if ((((uintptr_t)q_dev | (uintptr_t)out_dev | (uintptr_t)ws_dev) & 15) || (q_stride * e) % 16 || ((uintptr_t)lse_dev & 3)) return BEAGLE_ERR_INVALID_ARG;
     if (ws_bytes < need) return BEAGLE_ERR_CAPACITY;
-    // tiles are counted in 32 bits
-    if ((long long)batch * p->n_kv_heads * ((long long)p->max_pages * p->page_size / kTile + 2) > 0x7fffffffll) return BEAGLE_ERR_CAPACITY;
+    if (!paged_attn_fits(p, batch)) return BEAGLE_ERR_CAPACITY;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     a.table = p->table; a.length = p->length; a.k = p->k; a.v = p->v; a.q = q_dev; a.o = out_dev; a.lse = lse_dev;
     a.q_stride = q_stride;

@@ -173,8 +173,9 @@ __device__ __forceinline__ void release_row(const Book& b, int32_t* row, int fro
     }
 }
 
-__global__ void __launch_bounds__(kBookThreads) pages_append_book_kernel(const Book b, const PageSlots slots, int batch, int T,
-                                                                        const int32_t* n_new, int32_t* ok_out) {
+__global__ void __launch_bounds__(kBookThreads) pages_append_book_kernel(const Book b, const __grid_constant__ PageSlots slots,
+                                                                        const __grid_constant__ AppendRows rows, int batch, const int32_t* n_new,
+                                                                        int32_t* ok_out) {
     __shared__ int s_warp[33];
     __shared__ int s_need[kMaxCallBatch], s_start[kMaxCallBatch], s_have[kMaxCallBatch], s_cow[kMaxCallBatch];
     __shared__ int32_t s_list[kNear];
@@ -189,7 +190,7 @@ __global__ void __launch_bounds__(kBookThreads) pages_append_book_kernel(const B
     bool fits = true;
     if (t < batch) {
         r.len = b.clamp_len(__ldcg(b.length + slots.slot[t]));
-        r.n = n_new != nullptr ? min(max(__ldcg(n_new + t), 0), T) : T;
+        r.n = n_new != nullptr ? min(max(__ldcg(n_new + t), 0), rows.count[t]) : rows.count[t];
         const int have = (r.len + b.page_size - 1) / b.page_size;
         fits = r.len + r.n <= b.max_pages * b.page_size;
         if (fits && r.n > 0) {
@@ -233,8 +234,9 @@ __global__ void __launch_bounds__(kBookThreads) pages_append_book_kernel(const B
 
 // Rows of the append, and the valid part of every page that is copied before it is written.  blockIdx.y = row of the call;
 // blockIdx.x < chunks: that many 16-byte pieces of its new rows (keys, then values); past them: one CTA per K/V head for the copy.
-__global__ void __launch_bounds__(kMoveThreads) pages_append_write_kernel(const Book b, const PageSlots slots, uint4* K, uint4* V, const uint4* k_new,
-                                                                         const uint4* v_new, long long k_stride, long long v_stride, int T,
+__global__ void __launch_bounds__(kMoveThreads) pages_append_write_kernel(const Book b, const __grid_constant__ PageSlots slots,
+                                                                         const __grid_constant__ AppendRows rows, uint4* K, uint4* V, const uint4* k_new,
+                                                                         const uint4* v_new, long long k_stride, long long v_stride,
                                                                          int heads, int piece_shift, int chunks) {
     pdl_launch_dependents();
     pdl_wait();
@@ -268,7 +270,7 @@ __global__ void __launch_bounds__(kMoveThreads) pages_append_write_kernel(const 
         if (i < pieces) {
             const int tok = (int)(i / per_pos), off = (int)(i - (long long)tok * per_pos);
             const int h = off >> piece_shift, c = off & (dv - 1);
-            const long long srow = (long long)row * T + tok;
+            const long long srow = rows.start[row] + tok;
             x[u] = __ldcs(k_new + srow * k_stride + off);
             y[u] = __ldcs(v_new + srow * v_stride + off);
             const int pos = r.len + tok;
@@ -471,6 +473,34 @@ void launch_move(const beagle_pages* p, int most_pages, int remap, cudaStream_t 
 }
 
 }  // namespace
+
+beagle_status pages_append_rows(const beagle_pages* p, int batch, const int32_t* slot_host, const AppendRows& rows, const int32_t* n_new_dev,
+                                const void* k_new_dev, long long k_stride, const void* v_new_dev, long long v_stride, int32_t* ok_dev, cudaStream_t stream) {
+    beagle_status st = pages_check(p);
+    if (st != BEAGLE_OK) return st;
+    PageSlots slots;
+    st = pages_check_slots(p, batch, slot_host, &slots);
+    if (st != BEAGLE_OK) return st;
+    if (batch == 0) return BEAGLE_OK;
+    int most = 0;
+    for (int b = 0; b < batch; ++b) most = rows.count[b] > most ? rows.count[b] : most;
+    const int e = elt_bytes(p), width = p->n_kv_heads * p->head_dim;
+    if (most > 0 && (k_new_dev == nullptr || v_new_dev == nullptr || k_stride < width || v_stride < width)) return BEAGLE_ERR_INVALID_ARG;
+    if ((((uintptr_t)k_new_dev | (uintptr_t)v_new_dev) & 15) || (k_stride * e) % 16 || (v_stride * e) % 16) return BEAGLE_ERR_INVALID_ARG;
+    const int dv = p->head_dim * e / 16;
+    int shift = 0;
+    while ((1 << shift) < dv) ++shift;
+    const long long pieces = (long long)most * p->n_kv_heads * dv;
+    const long long chunks = (pieces + kMoveThreads * kMoveVecs - 1) / (kMoveThreads * kMoveVecs);
+    if (chunks > 0x3fffffff) return BEAGLE_ERR_CAPACITY;
+    launch_pdl(pages_append_book_kernel, dim3(1), dim3(kBookThreads), 0, stream, book_of(p), slots, rows, batch, n_new_dev, ok_dev);
+    if (most > 0)
+        launch_pdl(pages_append_write_kernel, dim3((unsigned)(chunks + p->n_kv_heads), batch), dim3(kMoveThreads), 0, stream, book_of(p), slots, rows,
+                   static_cast<uint4*>(p->k), static_cast<uint4*>(p->v), static_cast<const uint4*>(k_new_dev), static_cast<const uint4*>(v_new_dev),
+                   k_stride * e / 16, v_stride * e / 16, p->n_kv_heads, shift, (int)chunks);
+    return launched();
+}
+
 }  // namespace beagle
 
 extern "C" {
@@ -489,31 +519,17 @@ beagle_status beagle_pages_reset(const beagle_pages* p, void* stream) {
 }
 
 beagle_status beagle_pages_append(const beagle_pages* p, int32_t batch, const int32_t* slot_host, int32_t T, const int32_t* n_new_dev,
-                                  const void* k_new_dev, int64_t k_stride, const void* v_new_dev, int64_t v_stride, int32_t* ok_dev, void* stream_) {
-    beagle_status st = pages_check(p);
-    if (st != BEAGLE_OK) return st;
-    PageSlots slots;
-    st = pages_check_slots(p, batch, slot_host, &slots);
+                                  const void* k_new_dev, int64_t k_stride, const void* v_new_dev, int64_t v_stride, int32_t* ok_dev, void* stream) {
+    const beagle_status st = pages_check(p);
     if (st != BEAGLE_OK) return st;
     if (T < 0) return BEAGLE_ERR_INVALID_ARG;
     if (T > 0x40000000) return BEAGLE_ERR_CAPACITY;
-    if (batch == 0) return BEAGLE_OK;
-    const int e = elt_bytes(p), width = p->n_kv_heads * p->head_dim;
-    if (T > 0 && (k_new_dev == nullptr || v_new_dev == nullptr || k_stride < width || v_stride < width)) return BEAGLE_ERR_INVALID_ARG;
-    if ((((uintptr_t)k_new_dev | (uintptr_t)v_new_dev) & 15) || (k_stride * e) % 16 || (v_stride * e) % 16) return BEAGLE_ERR_INVALID_ARG;
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if ((long long)T * p->n_kv_heads * p->head_dim > (1ll << 40)) return BEAGLE_ERR_CAPACITY;
-    launch_pdl(pages_append_book_kernel, dim3(1), dim3(kBookThreads), 0, stream, book_of(p), slots, batch, T, n_new_dev, ok_dev);
-    if (T == 0) return launched();
-    const int dv = p->head_dim * e / 16;
-    int shift = 0;
-    while ((1 << shift) < dv) ++shift;
-    const long long pieces = (long long)T * p->n_kv_heads * dv;
-    const long long chunks = (pieces + kMoveThreads * kMoveVecs - 1) / (kMoveThreads * kMoveVecs);
-    launch_pdl(pages_append_write_kernel, dim3((unsigned)(chunks + p->n_kv_heads), batch), dim3(kMoveThreads), 0, stream, book_of(p), slots,
-               static_cast<uint4*>(p->k), static_cast<uint4*>(p->v), static_cast<const uint4*>(k_new_dev), static_cast<const uint4*>(v_new_dev),
-               (long long)(k_stride * e / 16), (long long)(v_stride * e / 16), T, p->n_kv_heads, shift, (int)chunks);
-    return launched();
+    AppendRows rows;
+    for (int b = 0; b < kMaxCallBatch; ++b) {
+        rows.start[b] = (long long)b * T;
+        rows.count[b] = T;
+    }
+    return pages_append_rows(p, batch, slot_host, rows, n_new_dev, k_new_dev, k_stride, v_new_dev, v_stride, ok_dev, static_cast<cudaStream_t>(stream));
 }
 
 beagle_status beagle_pages_truncate(const beagle_pages* p, int32_t n, const int32_t* slot_host, const int32_t* keep_dev, void* stream) {

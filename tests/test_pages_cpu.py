@@ -142,3 +142,58 @@ def test_binding_checks_tensors():
         b._row_stride("x", fused[:, :4, 32:64].unflatten(2, (4, 8)), 2)
     with pytest.raises(ValueError):
         b._row_stride("x", x.transpose(2, 3), 2)
+
+
+def test_head_over_pages_refusals(lib):
+    """What the paged prefill and step refuse before any launch, and the state they leave: a context over addresses nobody reads."""
+    from paper_2505_24544_b200.binding import BeagleConfig, BeagleWeights
+    assert lib.beagle_draft_step_pages(None, None, 0, None, None, 1, 0, 0, None, 1, None, None, None, None) == INVALID
+    assert lib.beagle_prefill_pages(None, None, 0, None, None, None, None, None, 0, None) == INVALID
+
+    def context(theta=0.0):
+        cfg = BeagleConfig(512, 8, 2, 64, 1024, 4096, 1, 1e-5, 1, 1, 6, 64, 8, theta)
+        w = BeagleWeights()
+        for name, _ in BeagleWeights._fields_:
+            setattr(w, name, 4096)
+        w.w_lm_fp8 = w.w_lm_scale = None
+        h = C.c_void_p()
+        assert lib.beagle_create(C.byref(cfg), C.byref(w), 256, 1 << 40, 256, 1 << 40, C.byref(h)) == OK
+        return h
+
+    n = C.c_size_t()
+    cfg = BeagleConfig(512, 8, 2, 64, 1024, 4096, 1, 1e-5, 1, 1, 6, 64, 8, 0.0)
+    assert lib.beagle_prefill_pages_workspace_bytes(C.byref(cfg), 3, C.byref(n)) == OK and n.value == 2 * 768
+    assert lib.beagle_prefill_pages_workspace_bytes(C.byref(cfg), 0, C.byref(n)) == OK and n.value == 0
+    assert lib.beagle_prefill_pages_workspace_bytes(C.byref(cfg), -1, C.byref(n)) == INVALID
+    assert lib.beagle_prefill_pages_workspace_bytes(C.byref(cfg), (1 << 24) + 1, C.byref(n)) == CAPACITY
+    assert lib.beagle_prefill_pages_workspace_bytes(C.byref(cfg), 3, None) == INVALID
+    h = context()
+
+    def step(p, slots=(0,), tokens=4096, window=0, sinks=0, ctx=h):
+        return lib.beagle_draft_step_pages(ctx, C.byref(p), len(slots), arr(*slots), tokens, 1, window, sinks, 1 << 30, 1, None, None, None, None)
+
+    def prefill(p, slots=(0,), lens=(3,), hidden=1 << 30, ws=1 << 29, size=1 << 20, ctx=h):
+        return lib.beagle_prefill_pages(ctx, C.byref(p), len(slots), arr(*slots), arr(*lens), hidden, None, ws, size, None)
+
+    for call in (step, prefill):
+        assert call(pages(lib, head_dim=128)) == SHAPE
+        assert call(pages(lib, n_kv_heads=4)) == SHAPE
+        assert call(pages(lib, dtype=0)) == SHAPE
+        assert call(pages(lib, k=0)) == INVALID
+        assert call(pages(lib, ws_bytes=16)) == CAPACITY
+        assert call(pages(lib), slots=(4,)) == INVALID                       # the context has six slots, the cache four
+        assert call(pages(lib, max_slots=8), slots=(6,)) == INVALID          # and the other way round
+        assert call(pages(lib), slots=(1, 1)) == INVALID
+        turned = context(10000.0)
+        assert call(pages(lib), ctx=turned) == 5                             # UNSUPPORTED
+        lib.beagle_destroy(turned)
+    assert step(pages(lib), window=-1) == INVALID and step(pages(lib), sinks=-1) == INVALID
+    assert step(pages(lib), tokens=None) == 4                                # no previous token: STATE
+    assert step(pages(lib), slots=()) == OK
+    assert prefill(pages(lib), lens=(-1,)) == INVALID
+    assert prefill(pages(lib), lens=(1 << 25,)) == CAPACITY
+    assert prefill(pages(lib), hidden=None) == INVALID and prefill(pages(lib), hidden=(1 << 30) + 2) == INVALID
+    assert prefill(pages(lib), ws=None) == INVALID and prefill(pages(lib), ws=(1 << 29) + 16) == INVALID
+    assert prefill(pages(lib), size=2 * 768 - 1) == CAPACITY
+    assert prefill(pages(lib), lens=(0,), hidden=None, ws=None, size=0) == OK and prefill(pages(lib), slots=()) == OK
+    lib.beagle_destroy(h)
