@@ -289,7 +289,7 @@ beagle_status beagle_pages_reset(const beagle_pages* pages, void* stream);
 
 /* Appends new rows to `batch` distinct slots: row b takes the first n_new_dev[b] (int32, clamped to [0, T]; NULL = T each)
  * of its T rows of k_new / v_new ([batch, T, n_kv_heads, head_dim]; the heads of a row are dense, rows k_stride / v_stride
- * elements apart, e.g. a view of a fused projection; 16-byte aligned rows).  Pages are taken lowest free id first, in the
+ * elements apart, e.g. a view of a fused projection; 16-byte aligned rows, not part of the pools).  Pages are taken lowest free id first, in the
  * order of the rows, from the pages free at entry.  A partly filled last page that other slots hold too (at entry) is
  * copied into a new page first, its filled positions only.  ok_dev int32 [batch] (nullable): 1, or 0 for a row that found
  * too few free pages or passes max_pages * page_size; such a row is left as it was, and so is every later row that needs a
@@ -361,7 +361,8 @@ beagle_status beagle_draft_step_pages(beagle_ctx* ctx, const beagle_pages* pages
  * n_q_heads a multiple of n_kv_heads; head_dim 64 | 128, fp32 also 16 | 32; with a window sinks <= 1024; at most 2^27 rows.
  * Scores, softmax, statistics and sums are fp32; the bf16 kernels round the softmax weights and dS to bf16 for their products.
  * Keys and values of a sequence must be finite; rows of other sequences and rows behind the last one are never mixed in and
- * outputs behind the last row are left as they were.  Results do not depend on timing. */
+ * outputs behind the last row are left as they were.  A query row with a NaN has a NaN lse and NaN outputs.  Outputs must not
+ * overlap inputs.  Results do not depend on timing. */
 typedef struct beagle_window_attn {
     const void* q_dev;
     const void* k_dev;

@@ -557,7 +557,7 @@ def _row_stride(name: str, t: torch.Tensor, lead: int) -> int:
         if t.shape[0] > 1 and st[0] != st[1] * t.shape[1]:
             raise ValueError(f"{name}: rows must lie at one distance")
         return st[1] if st[1] != 0 else -1
-    return st[0] if t.shape[0] > 1 else max(st[0], heads * dh)
+    return st[0] if t.shape[0] > 1 else heads * dh           # one row: any distance
 
 
 class PagedCache:

@@ -698,7 +698,7 @@ beagle_status launch_simt(const PagedArgs& a, int runs, cudaStream_t stream) {
     if (a.G == 1) launch_pdl(paged_attn_simt_kernel<T, DH, 1>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
     else if (a.G <= 2) launch_pdl(paged_attn_simt_kernel<T, DH, 2>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
     else if (a.G <= 4) launch_pdl(paged_attn_simt_kernel<T, DH, 4>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
-    else if constexpr (DH * 8 * (int)sizeof(float) * kConsumers <= 16 * 1024 + 0) launch_pdl(paged_attn_simt_kernel<T, DH, 8>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
+    else if constexpr (DH * 8 * (int)sizeof(float) * kConsumers <= 16 * 1024) launch_pdl(paged_attn_simt_kernel<T, DH, 8>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
     else return BEAGLE_ERR_SHAPE;
     if (!a.whole) launch_pdl(paged_attn_join_kernel<T, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a);
     return BEAGLE_OK;

@@ -31,8 +31,6 @@ constexpr int kStatPad = 128;
 constexpr int kQTile = 128;              // queries of one tile
 constexpr int kKTile = 128;              // keys of one tile of the key side
 
-struct WinPlan;                          // tensor maps etc. of the bf16 kernels
-
 // Which sequence a linear item belongs to (the item's index inside it in `in`).
 __device__ __forceinline__ int win_find(const int32_t* item, int batch, int at, int& in) {
     int b = 0;

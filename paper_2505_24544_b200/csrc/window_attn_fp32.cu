@@ -192,10 +192,10 @@ __global__ void __launch_bounds__(kThreads) window_fwd_fp32_kernel(const __grid_
         const int i = q0 + RT * ty + r;
         if (i >= q_len) continue;
         const size_t row = ((size_t)(seqs.q_start[b] + i) * a.Hq + h);
-        const float inv = l[r] > 0.f ? __fdiv_rn(1.f, l[r]) : 0.f;
+        const float inv = l[r] != 0.f ? __fdiv_rn(1.f, l[r]) : 0.f;
 #pragma unroll
         for (int e = 0; e < DH / 16; ++e) static_cast<float*>(a.o)[row * DH + tx + 16 * e] = o[r][e] * inv;
-        if (tx == 0 && a.lse_out != nullptr) a.lse_out[row] = l[r] > 0.f ? (m[r] + log2f(l[r])) * kLn2 : -INFINITY;
+        if (tx == 0 && a.lse_out != nullptr) a.lse_out[row] = l[r] != 0.f ? (m[r] + log2f(l[r])) * kLn2 : -INFINITY;
     }
 }
 

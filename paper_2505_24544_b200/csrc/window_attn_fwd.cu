@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_kernel(const __grid_co
         if (J > 0) {
             if (ok) ok = warp_wait(pv_done + 8 * ((J - 1) & 1), ((J - 1) >> 1) & 1, s_abort);
         }
-        const float inv = !ok ? __int_as_float(0x7fffffff) : l > 0.f ? 1.f / l : 0.f;
+        const float inv = !ok ? __int_as_float(0x7fffffff) : l != 0.f ? 1.f / l : 0.f;
         bf16* dst = static_cast<bf16*>(a.o) + ((size_t)(q_row + q * 32 + lane) * a.Hq + h) * DH;
         fence_after();
 #pragma unroll
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_kernel(const __grid_co
             }
         }
         if (valid && a.lse_out != nullptr)
-            a.lse_out[(size_t)(q_row + q * 32 + lane) * a.Hq + h] = !ok ? inv : l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            a.lse_out[(size_t)(q_row + q * 32 + lane) * a.Hq + h] = !ok ? inv : l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
     }
     fence_before();
     __syncthreads();

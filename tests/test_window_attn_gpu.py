@@ -258,3 +258,31 @@ def test_refusals():
     with pytest.raises(b.BeagleError):
         b.beagle_window_attn_backward(q, k, v, out, lse, do, [5], [5], torch.empty_like(q), torch.empty_like(k), torch.empty_like(v),
                                       ws=torch.empty(64, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("fp32", 16), ("fp32", 64)])
+def test_a_nan_query_stays_in_its_row(dtype, dh):
+    """A NaN in one query makes that row's outputs and lse NaN, in that head, and nothing else."""
+    q_len, kv_len = [150, 40], [200, 40]
+    q, k, v, do = inputs(q_len, kv_len, 4, 2, dh, dtype, 5)
+    out, lse = torch.empty_like(q), torch.empty(190, 4, device="cuda")
+    b.beagle_window_attn_forward(q, k, v, q_len, kv_len, out, lse, 70, 3)
+    bad = q.clone()
+    bad[131, 1, 3] = float("nan")
+    out2, lse2 = torch.empty_like(q), torch.empty_like(lse)
+    b.beagle_window_attn_forward(bad, k, v, q_len, kv_len, out2, lse2, 70, 3)
+    assert bool(out2[131, 1].isnan().all()) and bool(lse2[131, 1].isnan())
+    out2[131, 1], lse2[131, 1] = out[131, 1], lse[131, 1]
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_one_row_at_any_distance(dtype):
+    """A single query and key taken out of a larger matrix whose rows are an odd number of elements apart."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    wide = [torch.randn(2 * (4 * 64 + 1), generator=g, device="cuda").to(DT[dtype]) for _ in range(4)]
+    q, k, v, do = (torch.as_strided(x, (1, 4, 64), (257, 64, 1)) for x in wide)
+    dense = [x.contiguous().clone() for x in (q, k, v, do)]
+    got, want = run(q, k, v, do, [1], [1], 0, 0, False), run(*dense, [1], [1], 0, 0, False)
+    for name in want:
+        assert torch.equal(got[name], want[name]), name
