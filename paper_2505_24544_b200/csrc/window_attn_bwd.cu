@@ -26,6 +26,11 @@
 //
 // Rows behind a sequence (the next one's) are zeroed in shared memory where they would be multiplied by a weight of 0.
 // Every wait is bounded; a CTA that gives up leaves NaN in its rows.
+//
+// Measured (head_dim 128, 32 heads): 8 x 2048, window 512: query side 319 us, key side 408 (tensor pipe 0.39 and 0.44 of its cycles,
+// nothing else above 0.3 but issue slots); two sequences up to 8191, window 2048, 4 heads a group: 650 and 700.  A key-side job takes
+// 3050 cycles there, of which its four products are 2048: the threads form P for 1450 (special-function unit 1024), then dS for 730, and
+// wait some 500 for the next scores, whose place P holds until dV has read it.
 #include <cstring>
 
 #include "tc_ptx.cuh"
@@ -147,10 +152,10 @@ struct QItem {                           // 128 queries of one (sequence, query 
     int b, h, q0, q_len, kv_len, shift, q_row, k_row;
     KeyWalk w;
     __device__ __forceinline__ void load(int at, const WinArgs& a, const WinSeqs& s) {
-        const int tiles = s.item[a.batch];
         int tile;
-        h = at / tiles;
-        b = win_find(s.item, a.batch, at - h * tiles, tile);
+        const int unit = at / a.Hq;
+        h = at - unit * a.Hq;
+        b = win_find(s.item, a.batch, unit, tile);
         q_len = s.q_len[b];
         kv_len = s.kv_len[b];
         shift = kv_len - q_len - a.strict;
@@ -507,17 +512,17 @@ struct KItem {
     int j0;
     QueryWalk w;
     __device__ __forceinline__ void load(int at, const WinArgs& a, const WinSeqs& s) {
-        const int per_head = s.item[a.batch];
         int item;
-        kvh = at / per_head;
-        b = win_find(s.item, a.batch, at - kvh * per_head, item);
+        const int unit = at / a.Hkv;                             // the heads of a tile side by side: the cheap tiles, the last ones, stay for the end
+        kvh = at - unit * a.Hkv;
+        b = win_find(s.item, a.batch, unit, item);
         q_len = s.q_len[b];
         kv_len = s.kv_len[b];
         shift = kv_len - q_len - a.strict;
-        const int tiles = (kv_len + kKTile - 1) / kKTile;
-        const bool sink_part = item >= tiles;
-        seg = sink_part ? (item - tiles) % a.sink_segs : -1;
-        k0 = (sink_part ? (item - tiles) / a.sink_segs : item) * kKTile;
+        const int parts = a.sink_tiles * a.sink_segs;            // the sinks' segments first, then the bands of the tiles
+        const bool sink_part = item < parts;
+        seg = sink_part ? item % a.sink_segs : -1;
+        k0 = (sink_part ? item / a.sink_segs : item - parts) * kKTile;
         k_row = s.k_start[b] + k0;
         band = band_end(k0, kv_len, q_len, shift, a.window);
         j0 = 0;
@@ -927,8 +932,9 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
         if (t.item[a.batch] > 0) {
             const long long items = (long long)t.item[a.batch] * a.Hkv;
             if (items > 0x3fffffff) return -1;
-            // Items of many jobs run as CTAs of their own (their start-up is small beside them and the hardware balances them:
-            // 17 tiles x 4 heads 747 us against 844 as a fixed share per SM), short ones share a pipeline (5 tiles: 424 against 477).
+            // Items of many jobs run as CTAs of their own (their start-up is small beside them and the hardware balances them: 17 tiles x
+            // 4 heads, backward of sequences up to 8191 1406 us against 1432 as a fixed share per SM), short ones share a pipeline
+            // (5 tiles, 8 x 2048: 731 against 783).
             const long long jobs = ((long long)(a.window < 1 << 24 ? a.window : 1 << 24) + 2 * kKTile) / kQTile * a.G;
             const bool share = jobs < 24 && items > sms;
             window_bwd_kv_kernel<DH><<<(unsigned)(share ? sms : items), kThreads, SK::kBytes, stream>>>(mq, mdo, mk, mv, mdk, mdv, a, t);

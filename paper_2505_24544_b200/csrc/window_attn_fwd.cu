@@ -12,6 +12,11 @@
 // Two S buffers of 64 columns and O take 256 tensor-memory columns, Q and two stages of K and V 96 KB, so two CTAs share
 // an SM and fill each other's waits.
 //
+// Measured (head_dim 128, 32 heads): 8 x 2048, window 512: 210 us; two sequences up to 8191, window 2048: 408; chunks of 300 to 1024
+// over 7000 cached keys, window 4096: 188.  No pipe is saturated (8 x 2048: tensor 0.39, special functions 0.39, issue 0.36): a tile
+// takes a thread about 1500 cycles, 700 of them exponentials and the rest the hand-over with the tensor cores, and two tiles per
+// SM are in flight.  One CTA per SM with two query tiles that share K and V, 128 keys at a time, took 298 and 560 us.
+//
 // Rows of V past the sequence's keys (the next sequence's rows) are zeroed in shared memory before use, since their weight 0
 // would not silence a NaN.  Every wait is bounded; a CTA that gives up leaves NaN in its rows.
 #include <cstring>
@@ -102,10 +107,10 @@ __global__ void __launch_bounds__(kThreads, 2) window_fwd_kernel(const __grid_co
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     int tile;
-    const int b = win_find(seqs.item, a.batch, blockIdx.x, tile);
+    const int unit = blockIdx.x / a.Hq, h = blockIdx.x - unit * a.Hq, kvh = h / a.G;      // the heads of a tile side by side
+    const int b = win_find(seqs.item, a.batch, unit, tile);
     const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
     const int q0 = ((q_len + kQTile - 1) / kQTile - 1 - tile) * kQTile;      // the latest (longest) tiles first
-    const int h = blockIdx.y, kvh = h / a.G;
     const int q_row = seqs.q_start[b] + q0, k_row = seqs.k_start[b];
     KeyWalk w;
     w.init(q0, q_len, shift, a.window, a.sinks);
@@ -334,7 +339,9 @@ int launch_fwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
     if (!win_map(&mv, k_rows > 0 ? a.v : a.q, k_rows > 0 ? k_rows : q_rows, (long long)a.Hkv * DH, k_rows > 0 ? a.v_stride : a.q_stride, 64)) return -1;
     static PerDeviceOnce attr;
     if (!attr.ensure([] { return cudaFuncSetAttribute(window_fwd_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes) == cudaSuccess; })) return -1;
-    window_fwd_kernel<DH><<<dim3(s.item[a.batch], a.Hq), kThreads, SM::kBytes, stream>>>(mq, mk, mv, a, s);
+    const long long items = (long long)s.item[a.batch] * a.Hq;
+    if (items > 0x7fffffff) return -1;
+    window_fwd_kernel<DH><<<(unsigned)items, kThreads, SM::kBytes, stream>>>(mq, mk, mv, a, s);
     return 1;
 }
 
