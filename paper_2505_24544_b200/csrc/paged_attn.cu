@@ -17,10 +17,12 @@
 // reference point, sum and O accumulator in registers over the whole run, so they meet only where a pair ends.  Products on
 // mma.sync m16n8k16 with the G <= 8 query heads as rows: tcgen05 tiles have 64 rows at least, and the CUDA cores cannot do
 // G * 4 flop per 4 bytes next to unpacking at memory speed.
-// Other types and widths: paged_attn_simt_kernel, 16-byte loads straight into registers, one group of lanes per position.
+// Other types and widths: paged_attn_simt_kernel, the same ring in front of the CUDA cores.
 //
 // Measured: 32 sequences of 512 to 8192, 32 heads over 8 of 128: 103 us of stream (5.8 to 6.0 TB/s of cache) and 5 us of join; 16
-// sequences of 65000 to 131072: 1012 us, the rate of a plain copy; the smallest fp32 call: 6 us on the GPU.
+// sequences of 65000 to 131072: 1012 us, the rate of a plain copy; the smallest fp32 call: 4 us on the GPU.  fp32, 32 sequences of 2000,
+// 8 K/V heads of 128 (524 MB): 111 us with one query head each, 118 with four, 142 with eight (loading straight into registers, without the
+// ring, took 165, 212 and 490).
 //
 // Masked positions (past the length, outside the window) have their weight and their V row replaced by zero before use, so
 // whatever the pool holds there (NaN included) has no effect.
@@ -189,6 +191,10 @@ __device__ __forceinline__ void mma_rows8(float* d, uint32_t a0, uint32_t a2, ui
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%5}, {%7,%8}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(z0), "+f"(z1)
                  : "r"(a0), "r"(0u), "r"(a2), "r"(b0), "r"(b1));
+}
+// Untiled copy: both addresses 16-byte aligned, `bytes` a multiple of 16.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
@@ -439,16 +445,43 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 }
 
 // ------------------------------------------------------------------------------------------------
-// fp32, and bf16 at head_dim 32 and 256: LPK lanes share a position (16 bytes of its row each), the warp's 32 / LPK groups walk
-// positions side by side, each with its own running maximum, sum and O; they meet where a pair ends.
+// fp32, and bf16 at head_dim 32 and 256, on the CUDA cores.  The same ring, filled by untiled bulk copies (a page's rows of one
+// head are contiguous) of 64 positions, or 32 where a row has 512 bytes.  LPK lanes share a position (16 bytes of its row each),
+// a warp's 32 / LPK groups walk its positions side by side with their own reference point, sum and O; they meet where a pair ends.
+// The LPK partial sums of the heads' scores are added by halving: a lane hands half of its heads on and keeps the other half, so
+// GM heads take about GM exchanges instead of GM log2(LPK), and each weight is formed in one place and handed to the other lanes.
 // ------------------------------------------------------------------------------------------------
 template <typename T, int DH, int GM>
-__global__ void __launch_bounds__(kConsumers * 32) paged_attn_simt_kernel(const __grid_constant__ PagedArgs a) {
-    constexpr int VN = VecOf<T>::N, LPK = DH / VN, KPW = 32 / LPK, kSteps = (kPerWarp + KPW - 1) / KPW;
-    constexpr int kMost = GM <= 2 ? 8 : GM == 4 ? 4 : 2, U = kSteps < kMost ? kSteps : kMost;      // positions in flight per group
+struct SimtCfg {
+    static constexpr int VN = 16 / (int)sizeof(T), LPK = DH / VN, KPW = 32 / LPK;
+    static constexpr int kWarps = GM * VN >= 32 ? 4 : 8;                                // consumer warps: a thread keeps 2 GM VN of q and O
+    static constexpr int kRow = DH * (int)sizeof(T), kSub = kRow >= 512 ? 32 : 64;       // bytes of a row; positions of a stage
+    static constexpr int kPer = kSub / kWarps, kSteps = kPer / KPW;                      // positions of a warp; of each of its groups
+    static constexpr int HV = GM > LPK ? GM / LPK : 1, kSpan = GM > LPK ? 1 : LPK / GM;  // heads a lane keeps; lanes that keep the same ones
+    static constexpr int kStage = 2 * kSub * kRow, kJoin = (kWarps / 2) * GM * DH * 4;
+    static constexpr int kFit = (104 * 1024 - kJoin) / kStage, kRing = kFit < 6 ? kFit : 6;
+    static constexpr int kBytes = kRing * kStage + kJoin + 128;                          // + alignment slack
+    static_assert(kPer % KPW == 0 && kRing >= 2, "shape");
+    static __device__ __forceinline__ int owner(int h) { return GM > LPK ? h / HV : h * kSpan; }      // the lane of a group that keeps head h
+};
+template <typename T, int DH, int GM>
+__global__ void __launch_bounds__((SimtCfg<T, DH, GM>::kWarps + 1) * 32, 2) paged_attn_simt_kernel(const __grid_constant__ PagedArgs a) {
+    using S = SimtCfg<T, DH, GM>;
+    constexpr int VN = S::VN, LPK = S::LPK, KPW = S::KPW, HV = S::HV, kSteps = S::kSteps;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* ring = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
+    float* s_o = reinterpret_cast<float*>(ring + S::kRing * S::kStage);                  // [kWarps / 2][GM][DH]
     __shared__ Schedule s;
-    __shared__ float s_o[kConsumers][GM][DH], s_m[kConsumers][GM], s_l[kConsumers][GM];
+    __shared__ __align__(8) uint64_t bars[2 * S::kRing];
+    __shared__ float s_m[S::kWarps][GM], s_l[S::kWarps][GM];
+    __shared__ int s_abort;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * S::kRing;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LPK, sub = lane % LPK;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kRing; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, S::kWarps); }
+        s_abort = 0;
+        fence_barrier_init();
+    }
     pdl_launch_dependents();
     pdl_wait();
     make_schedule(a, s);
@@ -460,17 +493,70 @@ __global__ void __launch_bounds__(kConsumers * 32) paged_attn_simt_kernel(const 
     if (u0 >= u1) return;
     Walk w;
     w.seek(s, u0, a.Hkv);
-    const T* K = static_cast<const T*>(a.k);
-    const T* V = static_cast<const T*>(a.v);
-    float q[GM][VN], o[GM][VN], m[GM], l[GM];
-#pragma unroll
-    for (int h = 0; h < GM; ++h) {
-        m[h] = -INFINITY; l[h] = 0.f;
-#pragma unroll
-        for (int i = 0; i < VN; ++i) { q[h][i] = 0.f; o[h][i] = 0.f; }
+
+    if (warp == S::kWarps) {
+        // ---------------- producer: lane p copies page p of the stage
+        const int rows = min(1 << a.page_shift, S::kSub), parts = S::kSub / rows;
+        const uint32_t bytes = (uint32_t)rows * S::kRow;
+        bool ok = true;
+        int st = 0, ph = 0, issued = 0;
+        for (int u = u0; u < u1 && ok; ++u) {
+#pragma unroll 1
+            for (int x = 0; x < kTile / S::kSub; ++x) {
+                const int pos = w.tile(s) * kTile + x * S::kSub + lane * rows;
+                int page = -1;
+                // (a part without a visible position stays what it was: its weights and its V rows count as 0)
+                if (lane < parts && pos < s.len[w.b] && (pos + rows > s.lo[w.b] || pos < a.sinks))
+                    page = __ldcg(a.table + (size_t)a.slots.slot[w.b] * a.max_pages + (pos >> a.page_shift));
+                if (page >= a.n_pages) page = -1;
+                const int copies = __popc(__ballot_sync(0xffffffffu, page >= 0));
+                ok = mbar_wait(empty + 8 * st, ph ^ 1, &s_abort);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (lane == 0) {
+                    if (copies > 0) mbar_expect_tx(full + 8 * st, 2 * copies * bytes);
+                    else mbar_arrive(full + 8 * st);
+                }
+                __syncwarp();
+                if (page >= 0) {
+                    const size_t at = (((((size_t)page * a.Hkv + w.kvh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)))) * S::kRow;
+                    const uint32_t dst = smem_u32(ring) + st * S::kStage + lane * bytes;
+                    bulk_load(dst, static_cast<const uint8_t*>(a.k) + at, bytes, full + 8 * st);
+                    bulk_load(dst + S::kSub * S::kRow, static_cast<const uint8_t*>(a.v) + at, bytes, full + 8 * st);
+                }
+                ++issued;
+                if (++st == S::kRing) { st = 0; ph ^= 1; }
+            }
+            w.next(s, a.batch, a.Hkv);
+        }
+        if (!ok)                         // copies already requested still land: wait (bounded) for the last of each stage
+            for (int n = max(0, issued - S::kRing); n < issued; ++n)
+                for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(full + 8 * (n % S::kRing), (n / S::kRing) & 1); ++i) {}
+        return;
     }
-    int have_q = -1, seg = 0;
-    bool first_pair_open = w.i > 0;
+
+    // ---------------- consumers
+    auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(S::kWarps * 32) : "memory"); };
+    const int base_lane = lane - sub;
+    float q[GM][VN], o[GM][VN], m[HV], l[HV];                    // m, l: of this lane's own heads
+    auto clear = [&]() {
+#pragma unroll
+        for (int i = 0; i < HV; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+#pragma unroll
+        for (int h = 0; h < GM; ++h)
+#pragma unroll
+            for (int i = 0; i < VN; ++i) o[h][i] = 0.f;
+    };
+    auto of_head = [&](const float* v, int h) {                  // the owner's value of head h
+        return GM == 1 ? v[0] : __shfl_sync(0xffffffffu, v[GM > LPK ? h % HV : 0], base_lane + S::owner(h));
+    };
+    clear();
+#pragma unroll
+    for (int h = 0; h < GM; ++h)
+#pragma unroll
+        for (int i = 0; i < VN; ++i) q[h][i] = 0.f;
+    int have_q = -1, seg = 0, st = 0, ph = 0;
+    bool ok = true, first_pair_open = w.i > 0;
     for (int u = u0; u < u1; ++u) {
         const int pair = w.b * a.Hkv + w.kvh;
         if (pair != have_q) {
@@ -482,109 +568,163 @@ __global__ void __launch_bounds__(kConsumers * 32) paged_attn_simt_kernel(const 
                     unpack16<T>(x, q[h]);
                 }
         }
-        const int len = s.len[w.b], lo = s.lo[w.b], pos_base = w.tile(s) * kTile + warp * kPerWarp;
-        const int32_t* row = a.table + (size_t)a.slots.slot[w.b] * a.max_pages;
+        const int len = s.len[w.b], lo = s.lo[w.b];
 #pragma unroll 1
-        for (int k0 = 0; k0 < kPerWarp; k0 += KPW * U) {
-            uint4 kx[U], vx[U];
-            bool vis[U];
+        for (int x0 = 0; x0 < kTile / S::kSub; ++x0) {
+            const int pos0 = w.tile(s) * kTile + x0 * S::kSub + warp * S::kPer;
+            // A wait that runs out leaves NaN in what depends on it; the warp still meets the others where pairs end.
+            if (ok) ok = mbar_wait(full + 8 * st, ph, &s_abort);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok)
 #pragma unroll
-            for (int x = 0; x < U; ++x) {
-                const int k = k0 + x * KPW + grp, pos = pos_base + k;
-                vis[x] = k < kPerWarp && pos < len && (pos >= lo || pos < a.sinks);
-                kx[x] = vx[x] = make_uint4(0u, 0u, 0u, 0u);
-                if (vis[x]) {
-                    const int page = __ldcg(row + (pos >> a.page_shift));
-                    if (page >= 0 && page < a.n_pages) {
-                        const size_t at = (((((size_t)page * a.Hkv + w.kvh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)))) * DH + sub * VN;
-                        kx[x] = __ldcs(reinterpret_cast<const uint4*>(K + at));
-                        vx[x] = __ldcs(reinterpret_cast<const uint4*>(V + at));
+                for (int i = 0; i < HV; ++i) l[i] = __int_as_float(0x7fffffff);
+            if (ok && pos0 < len && (pos0 + S::kPer > lo || pos0 < a.sinks)) {
+                const bool plain = pos0 + S::kPer <= len && (pos0 >= lo || pos0 + S::kPer <= a.sinks);
+                const uint8_t* K = ring + st * S::kStage + (warp * S::kPer + grp) * S::kRow + sub * 16;
+                const uint8_t* V = K + S::kSub * S::kRow;
+                float sc[kSteps][HV], mx[HV];
+#pragma unroll
+                for (int i = 0; i < HV; ++i) mx[i] = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < kSteps; ++x) {
+                    float f[VN], v[GM];
+                    unpack16<T>(*reinterpret_cast<const uint4*>(K + x * KPW * S::kRow), f);
+#pragma unroll
+                    for (int h = 0; h < GM; ++h) {
+                        v[h] = 0.f;
+#pragma unroll
+                        for (int i = 0; i < VN; ++i) v[h] = fmaf(q[h][i], f[i], v[h]);
+                    }
+                    int n = GM;
+#pragma unroll
+                    for (int d = LPK / 2; d > 0; d >>= 1) {
+                        if (n > 1) {
+                            n /= 2;
+                            const bool upper = (lane & d) != 0;
+#pragma unroll
+                            for (int h = 0; h < GM / 2; ++h)
+                                if (h < n) {
+                                    const float give = upper ? v[h] : v[h + n], keep = upper ? v[h + n] : v[h];
+                                    v[h] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+                                }
+                        } else {
+                            v[0] += __shfl_xor_sync(0xffffffffu, v[0], d);
+                        }
+                    }
+                    const int pos = pos0 + x * KPW + grp;
+                    const bool vis = plain || (pos < len && (pos >= lo || pos < a.sinks));
+#pragma unroll
+                    for (int i = 0; i < HV; ++i) {
+                        sc[x][i] = vis ? v[i] * a.scale_log2 : -INFINITY;
+                        mx[i] = fmaxf(mx[i], sc[x][i]);
+                    }
+                }
+                // the reference point moves only when a score exceeds it by more than kSlack: weights stay below 2^8
+                bool grow = false;
+#pragma unroll
+                for (int i = 0; i < HV; ++i) grow |= mx[i] > m[i] + kSlack;
+                if (__any_sync(0xffffffffu, grow)) {
+                    float r[HV];
+#pragma unroll
+                    for (int i = 0; i < HV; ++i) {
+                        const bool g = mx[i] > m[i] + kSlack;
+                        r[i] = g && m[i] != -INFINITY ? exp2f(m[i] - mx[i]) : 1.f;
+                        if (g) m[i] = mx[i];
+                        l[i] *= r[i];
+                    }
+#pragma unroll
+                    for (int h = 0; h < GM; ++h) {
+                        const float f = of_head(r, h);
+#pragma unroll
+                        for (int i = 0; i < VN; ++i) o[h][i] *= f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < HV; ++i) {
+                    const float neg = m[i] == -INFINITY ? 0.f : -m[i];       // no visible position so far: every weight is 0
+#pragma unroll
+                    for (int x = 0; x < kSteps; ++x) {
+                        sc[x][i] = exp2f(sc[x][i] + neg);
+                        l[i] += sc[x][i];
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < kSteps; ++x) {
+                    uint4 raw = *reinterpret_cast<const uint4*>(V + x * KPW * S::kRow);
+                    if (!plain) {
+                        const int pos = pos0 + x * KPW + grp;
+                        if (!(pos < len && (pos >= lo || pos < a.sinks))) raw = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    float f[VN];
+                    unpack16<T>(raw, f);
+#pragma unroll
+                    for (int h = 0; h < GM; ++h) {
+                        const float p = of_head(sc[x], h);
+#pragma unroll
+                        for (int i = 0; i < VN; ++i) o[h][i] = fmaf(p, f[i], o[h][i]);
                     }
                 }
             }
-            float sc[U][GM];
-#pragma unroll
-            for (int x = 0; x < U; ++x) {
-                float f[VN];
-                unpack16<T>(kx[x], f);
-#pragma unroll
-                for (int h = 0; h < GM; ++h) {
-                    float t = 0.f;
-#pragma unroll
-                    for (int i = 0; i < VN; ++i) t = fmaf(q[h][i], f[i], t);
-                    sc[x][h] = t;
-                }
-            }
-#pragma unroll
-            for (int d = 1; d < LPK; d <<= 1)
-#pragma unroll
-                for (int x = 0; x < U; ++x)
-#pragma unroll
-                    for (int h = 0; h < GM; ++h) sc[x][h] += __shfl_xor_sync(0xffffffffu, sc[x][h], d);
-#pragma unroll
-            for (int x = 0; x < U; ++x) {
-                float f[VN];
-                unpack16<T>(vx[x], f);
-#pragma unroll
-                for (int h = 0; h < GM; ++h) {
-                    const float z = vis[x] ? sc[x][h] * a.scale_log2 : -INFINITY;
-                    if (z > m[h] + kSlack) {
-                        const float r = m[h] == -INFINITY ? 1.f : exp2f(m[h] - z);
-                        m[h] = z;
-                        l[h] *= r;
-#pragma unroll
-                        for (int i = 0; i < VN; ++i) o[h][i] *= r;
-                    }
-                    const float p = vis[x] ? exp2f(z - m[h]) : 0.f;
-                    l[h] += p;
-#pragma unroll
-                    for (int i = 0; i < VN; ++i) o[h][i] = fmaf(p, f[i], o[h][i]);
-                }
-            }
+            __syncwarp();
+            if (ok && lane == 0) mbar_arrive(empty + 8 * st);
+            if (++st == S::kRing) { st = 0; ph ^= 1; }
         }
         const int b = w.b, kvh = w.kvh;
         const bool last = w.i + 1 == w.n;
         w.next(s, a.batch, a.Hkv);
         if (!last && u + 1 < u1) continue;
 
-        // ---- join the warp's groups, then the four warps
+        // ---- join the warp's groups, then the warps
 #pragma unroll
         for (int h = 0; h < GM; ++h) {
-            float M = m[h];
+            const float mh = of_head(m, h);
+            float lh = of_head(l, h), M = mh;
 #pragma unroll
             for (int d = LPK; d < 32; d <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-            const float f = m[h] == -INFINITY ? 0.f : exp2f(m[h] - M);
-            l[h] *= f;
+            const float f = mh == -INFINITY ? 0.f : exp2f(mh - M);
+            lh = mh == -INFINITY ? lh : lh * f;                  // (no position seen: the sum is 0, or NaN after a wait that ran out)
 #pragma unroll
             for (int i = 0; i < VN; ++i) o[h][i] *= f;
 #pragma unroll
             for (int d = LPK; d < 32; d <<= 1) {
-                l[h] += __shfl_xor_sync(0xffffffffu, l[h], d);
+                lh += __shfl_xor_sync(0xffffffffu, lh, d);
 #pragma unroll
                 for (int i = 0; i < VN; ++i) o[h][i] += __shfl_xor_sync(0xffffffffu, o[h][i], d);
             }
-            if (grp == 0) {
-#pragma unroll
-                for (int i = 0; i < VN; ++i) s_o[warp][h][sub * VN + i] = o[h][i];
-                if (sub == 0) { s_m[warp][h] = M; s_l[warp][h] = l[h]; }
-            }
-            m[h] = -INFINITY; l[h] = 0.f;
-#pragma unroll
-            for (int i = 0; i < VN; ++i) o[h][i] = 0.f;
+            if (lane == 0) { s_m[warp][h] = M; s_l[warp][h] = lh; }
         }
-        __syncthreads();
+        meet();
+        // the upper half of the warps hand theirs to the lower half, which add and leave the sums for all
+        constexpr int kHalf = S::kWarps / 2;
+#pragma unroll
+        for (int h = 0; h < GM; ++h) {
+            float M = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < S::kWarps; ++x) M = fmaxf(M, s_m[x][h]);
+            const float f = s_m[warp][h] == -INFINITY ? 0.f : exp2f(s_m[warp][h] - M);
+#pragma unroll
+            for (int i = 0; i < VN; ++i) {
+                o[h][i] *= f;
+                if (warp >= kHalf && grp == 0) s_o[((warp - kHalf) * GM + h) * DH + sub * VN + i] = o[h][i];
+            }
+        }
+        meet();
+        if (warp < kHalf && grp == 0)
+#pragma unroll
+            for (int h = 0; h < GM; ++h)
+#pragma unroll
+                for (int i = 0; i < VN; ++i) s_o[(warp * GM + h) * DH + sub * VN + i] += o[h][i];
+        meet();
         const bool whole = last && !first_pair_open;
-        for (int i = threadIdx.x; i < a.G * DH; i += kConsumers * 32) {
+        for (int i = threadIdx.x; i < a.G * DH; i += S::kWarps * 32) {
             const int h = i / DH, d = i % DH;
             float M = -INFINITY, L = 0.f, acc = 0.f;
 #pragma unroll
-            for (int x = 0; x < kConsumers; ++x) M = fmaxf(M, s_m[x][h]);
+            for (int x = 0; x < S::kWarps; ++x) M = fmaxf(M, s_m[x][h]);
 #pragma unroll
-            for (int x = 0; x < kConsumers; ++x) {
-                const float f = s_m[x][h] == -INFINITY ? 0.f : exp2f(s_m[x][h] - M);
-                L = fmaf(f, s_l[x][h], L);
-                acc = fmaf(f, s_o[x][h][d], acc);
-            }
+            for (int x = 0; x < S::kWarps; ++x) L += s_m[x][h] == -INFINITY ? s_l[x][h] : s_l[x][h] * exp2f(s_m[x][h] - M);
+#pragma unroll
+            for (int x = 0; x < kHalf; ++x) acc += s_o[(x * GM + h) * DH + d];
             const int head = kvh * a.G + h;
             if (whole) {
                 static_cast<T*>(a.o)[((size_t)b * a.Hq + head) * DH + d] = from_float<T>(L != 0.f ? acc / L : 0.f);
@@ -595,7 +735,8 @@ __global__ void __launch_bounds__(kConsumers * 32) paged_attn_simt_kernel(const 
                 if (d == 0) { dst[DH] = M; dst[DH + 1] = L; }
             }
         }
-        __syncthreads();
+        meet();
+        clear();
         first_pair_open = false;
         seg = 1;
     }
@@ -658,9 +799,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
 }
 
 constexpr int kMaxRuns = 2048;           // bound of the workspace; the grid is min(this, CTAs that fit the GPU)
-constexpr int kSimtCtasPerSm = 4;
-// Pairs of at most this many tiles are not cut.  One tile takes a CTA some 0.4 us of a stream (SIMT: 1.5 us), the join launch 4.
-constexpr int kWholeTiles = 8, kWholeTilesSimt = 2;
+constexpr int kSimtCtasPerSm = 2;
+// Pairs of at most this many tiles are not cut: the join launch takes some 3 us, a tile on its own 0.4 (tensor cores), 0.9 (up to four
+// heads a pair on the CUDA cores) or 3.5 (more).  Measured whole against cut, us: 4 heads of 64, fp32, 4 tiles, 32 sequences 7.6 against 9.2,
+// one sequence 6.4 against 6.3, 6 tiles 8.2 against 6.4; 8 heads a pair of 128, fp32, 2 tiles 12.2 against 12.7, 3 tiles 15.7 against 13.0.
+constexpr int kWholeTiles = 8, kWholeTilesSimt = 4, kWholeTilesMany = 2;
 
 bool uses_mma(const beagle_pages* p) { return p->dtype == BEAGLE_BF16 && (p->head_dim == 64 || p->head_dim == 128); }
 // The most tiles of one pair, as far as the host can know.
@@ -670,8 +813,8 @@ long long most_tiles(const beagle_pages* p, int window, int sinks) {
     const long long seen = ((long long)window + kTile - 2) / kTile + 1 + ((long long)sinks + kTile - 1) / kTile;
     return seen < cap ? seen : cap;
 }
-bool whole_pairs(const beagle_pages* p, int window, int sinks) {
-    return most_tiles(p, window, sinks) <= (uses_mma(p) ? kWholeTiles : kWholeTilesSimt);
+bool whole_pairs(const beagle_pages* p, int Hq, int window, int sinks) {
+    return most_tiles(p, window, sinks) <= (uses_mma(p) ? kWholeTiles : Hq / p->n_kv_heads <= 4 ? kWholeTilesSimt : kWholeTilesMany);
 }
 
 template <int DH>
@@ -696,13 +839,25 @@ beagle_status launch_mma(const beagle_pages* p, const PagedArgs& a, int runs, cu
     return BEAGLE_OK;
 }
 
+template <typename T, int DH, int GM>
+beagle_status launch_simt_heads(const PagedArgs& a, int runs, cudaStream_t stream) {
+    using S = SimtCfg<T, DH, GM>;
+    static PerDeviceOnce smem_attr;
+    if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_simt_kernel<T, DH, GM>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) == cudaSuccess; }))
+        return BEAGLE_ERR_CUDA;
+    launch_pdl(paged_attn_simt_kernel<T, DH, GM>, dim3(runs), dim3((S::kWarps + 1) * 32), (size_t)S::kBytes, stream, a);
+    return BEAGLE_OK;
+}
+
 template <typename T, int DH>
 beagle_status launch_simt(const PagedArgs& a, int runs, cudaStream_t stream) {
-    if (a.G == 1) launch_pdl(paged_attn_simt_kernel<T, DH, 1>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
-    else if (a.G <= 2) launch_pdl(paged_attn_simt_kernel<T, DH, 2>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
-    else if (a.G <= 4) launch_pdl(paged_attn_simt_kernel<T, DH, 4>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
-    else if constexpr (DH * 8 * (int)sizeof(float) * kConsumers <= 16 * 1024) launch_pdl(paged_attn_simt_kernel<T, DH, 8>, dim3(runs), dim3(kConsumers * 32), 0, stream, a);
+    beagle_status st;
+    if (a.G == 1) st = launch_simt_heads<T, DH, 1>(a, runs, stream);
+    else if (a.G <= 2) st = launch_simt_heads<T, DH, 2>(a, runs, stream);
+    else if (a.G <= 4) st = launch_simt_heads<T, DH, 4>(a, runs, stream);
+    else if constexpr (DH < 256) st = launch_simt_heads<T, DH, 8>(a, runs, stream);
     else return BEAGLE_ERR_SHAPE;
+    if (st != BEAGLE_OK) return st;
     if (!a.whole) launch_pdl(paged_attn_join_kernel<T, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a);
     return BEAGLE_OK;
 }
@@ -762,7 +917,7 @@ beagle_status beagle_paged_attn_workspace_bytes(const beagle_pages* p, int32_t n
     if (!pages_valid_shape(p)) return BEAGLE_ERR_SHAPE;
     const beagle_status st = check_heads(p, n_q_heads);
     if (st != BEAGLE_OK) return st;
-    if (whole_pairs(p, window, sinks)) {
+    if (whole_pairs(p, n_q_heads, window, sinks)) {
         *bytes = 0;
         return BEAGLE_OK;
     }
@@ -805,7 +960,7 @@ beagle_status beagle_paged_attn(const beagle_pages* p, int32_t batch, const int3
     // no more runs than the cache's capacity has tiles
     const long long most = (long long)batch * p->n_kv_heads * most_tiles(p, window, sinks);
     const bool mma = uses_mma(p);
-    a.whole = whole_pairs(p, window, sinks) ? 1 : 0;
+    a.whole = whole_pairs(p, n_q_heads, window, sinks) ? 1 : 0;
     long long runs = (long long)device_sm_count() * (mma ? kCtasPerSm : kSimtCtasPerSm);
     if (runs > kMaxRuns) runs = kMaxRuns;
     if (runs > most) runs = most;
