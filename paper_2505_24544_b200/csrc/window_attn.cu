@@ -8,7 +8,7 @@ using namespace beagle;
 namespace {
 
 struct Layout {
-    size_t stats, part, total;
+    size_t stats, part, group, total;
     int stat_rows, sink_rows, sink_tiles, sink_segs;
 };
 
@@ -62,23 +62,28 @@ Layout layout(const beagle_window_attn* w, const WinArgs& a, const WinSeqs& s, l
     }
     L.stat_rows = (int)rows;
     size_t off = ((size_t)a.Hq * rows * 2 * sizeof(float) + 255) / 256 * 256;
-    L.part = off;
     const size_t d = w->head_dim;
-    if (w->dtype == BEAGLE_FP32) {
-        if (a.G > 1) off += (size_t)k_rows * a.Hq * 2 * d * sizeof(float);
-    } else if (a.sinks > 0) {
+    const bool fp32 = w->dtype == BEAGLE_FP32;
+    if (fp32 && a.G > 1) {
+        L.group = off;
+        off += ((size_t)k_rows * a.Hq * 2 * d * sizeof(float) + 255) / 256 * 256;
+    }
+    L.part = off;
+    if (a.sinks > 0) {
         // Segments of the queries past the band of the sinks' key tiles, about as long as a band CTA's work (at least eight
-        // tiles), as many as the longest sequence needs.
+        // tiles, fp32 two), as many as the longest sequence needs.
         const int rows_s = a.sinks < most_kv ? a.sinks : most_kv;
         int segs = 0;
         for (int b = 0; b < a.batch; ++b) {
             const long long shift = s.kv_len[b] - s.q_len[b] - a.strict;
             long long end = (s.kv_len[b] < kKTile ? s.kv_len[b] : kKTile) - 1 - shift + a.window;
             end = end < 0 ? 0 : end > s.q_len[b] ? s.q_len[b] : end;
-            const long long jobs = (s.q_len[b] - end + 1 + kQTile - 1) / kQTile * a.G;
+            const int heads = fp32 ? 1 : a.G;            // that one CTA serves; the fp32 kernels' tiles are half as long
+            const long long jobs = (s.q_len[b] - end + 1 + kQTile - 1) / kQTile * heads;
             if (s.q_len[b] == end || s.kv_len[b] == 0) continue;
-            long long band = ((long long)a.window + 2 * kKTile) / kQTile * a.G;
-            if (band < 8) band = 8;
+            long long band = ((long long)a.window + 2 * kKTile) / kQTile * heads;
+            const int least = fp32 ? 2 : 8;
+            if (band < least) band = least;
             const int need = (int)((jobs + band - 1) / band);
             segs = need > segs ? need : segs;
         }
@@ -86,7 +91,7 @@ Layout layout(const beagle_window_attn* w, const WinArgs& a, const WinSeqs& s, l
         if (L.sink_segs > 0) {
             L.sink_rows = rows_s;
             L.sink_tiles = (rows_s + kKTile - 1) / kKTile;
-            off += (size_t)a.batch * a.Hkv * (1 + L.sink_segs) * rows_s * 2 * d * sizeof(float);
+            off += (size_t)a.batch * (fp32 ? a.Hq : a.Hkv) * (1 + L.sink_segs) * rows_s * 2 * d * sizeof(float);
         }
     }
     L.total = (off + 255) / 256 * 256;
@@ -157,6 +162,7 @@ beagle_status beagle_window_attn_backward(const beagle_window_attn* w, const voi
     a.dq = dq_dev; a.dk = dk_dev; a.dv = dv_dev;
     a.stats = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.stats);
     a.sink_part = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.part);
+    a.group_part = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.group);
     a.stat_rows = L.stat_rows; a.sink_rows = L.sink_rows; a.sink_tiles = L.sink_tiles; a.sink_segs = L.sink_segs;
     const cudaStream_t cs = static_cast<cudaStream_t>(stream);
     const int rc = w->dtype == BEAGLE_BF16 ? window_bwd_bf16(a, s, w->head_dim, q_rows, k_rows, cs) : window_bwd_fp32(a, s, w->head_dim, cs);

@@ -6,8 +6,9 @@
 // with its R/16 rows x head_dim / 16 columns of the accumulators.  The 16 threads of a row are half a warp, so row maxima, sums
 // and the hand-over of P through shared memory need no CTA barrier.  The streamed tiles come by cp.async, the next one under
 // this one's work where shared memory holds two.
-// Backward as in the bf16 kernels: a query side (dQ, and delta) and a key side (dK, dV); the key side gives every query head its
-// own CTA and, where heads share keys, leaves fp32 partials that a last launch adds in the order of the heads.
+// Backward as in the bf16 kernels: a query side (dQ, and delta) and a key side (dK, dV), what lies past the band of the sinks in segments;
+// the key side gives every query head its own CTA and, where heads share keys, leaves fp32 partials that a last launch adds in the
+// order of the heads.
 //
 // Measured: three sequences up to 333, 4 heads of 64, window 64: forward 14 us, query side 20, key side 36, all latency (88 CTAs).
 #include "window_attn.h"
@@ -62,7 +63,34 @@ __device__ __forceinline__ void dots(const float* A, const float* B, int ty, int
                 acc[r][c] = fmaf(x[r].x, y[c].x, fmaf(x[r].y, y[c].y, fmaf(x[r].z, y[c].z, fmaf(x[r].w, y[c].w, acc[r][c]))));
     }
 }
-// acc[r][e] += sum_k P[RT ty + r][k] X[k][tx + 16 e]
+// The accumulator columns of a thread: runs of up to four, so that they load and store as vectors.
+template <int DH>
+__device__ __forceinline__ int col(int tx, int e) { return DH >= 64 ? 64 * (e / 4) + 4 * tx + e % 4 : DH / 16 * tx + e; }
+// DH / 16 values at the thread's columns of a row.
+template <int DH>
+__device__ __forceinline__ void get_cols(const float* row, int tx, float* x) {
+    if constexpr (DH >= 64) {
+#pragma unroll
+        for (int e = 0; e < DH / 16; e += 4) {
+            const float4 t = *reinterpret_cast<const float4*>(row + col<DH>(tx, e));
+            x[e] = t.x; x[e + 1] = t.y; x[e + 2] = t.z; x[e + 3] = t.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < DH / 16; ++e) x[e] = row[col<DH>(tx, e)];
+    }
+}
+template <int DH>
+__device__ __forceinline__ void set_cols(float* row, int tx, const float* x, float f) {
+    if constexpr (DH >= 64) {
+#pragma unroll
+        for (int e = 0; e < DH / 16; e += 4) *reinterpret_cast<float4*>(row + col<DH>(tx, e)) = make_float4(x[e] * f, x[e + 1] * f, x[e + 2] * f, x[e + 3] * f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < DH / 16; ++e) row[col<DH>(tx, e)] = x[e] * f;
+    }
+}
+// acc[r][e] += sum_k P[RT ty + r][k] X[k][col(e)]
 template <int DH, int RT>
 __device__ __forceinline__ void weigh(const float* P, const float* X, int ty, int tx, float acc[RT][DH / 16]) {
 #pragma unroll 2
@@ -74,13 +102,14 @@ __device__ __forceinline__ void weigh(const float* P, const float* X, int ty, in
             p[r][0] = t.x; p[r][1] = t.y; p[r][2] = t.z; p[r][3] = t.w;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+            float x[DH / 16];
+            get_cols<DH>(X + (k + i) * row_len<DH>(), tx, x);
 #pragma unroll
-            for (int e = 0; e < DH / 16; ++e) {
-                const float x = X[(k + i) * row_len<DH>() + tx + 16 * e];
+            for (int e = 0; e < DH / 16; ++e)
 #pragma unroll
-                for (int r = 0; r < RT; ++r) acc[r][e] = fmaf(p[r][i], x, acc[r][e]);
-            }
+                for (int r = 0; r < RT; ++r) acc[r][e] = fmaf(p[r][i], x[e], acc[r][e]);
+        }
     }
 }
 template <int RT>
@@ -195,8 +224,7 @@ __global__ void __launch_bounds__(kThreads) window_fwd_fp32_kernel(const __grid_
         if (i >= q_len) continue;
         const size_t row = ((size_t)(seqs.q_start[b] + i) * a.Hq + h);
         const float inv = l[r] != 0.f ? __fdiv_rn(1.f, l[r]) : 0.f;
-#pragma unroll
-        for (int e = 0; e < DH / 16; ++e) static_cast<float*>(a.o)[row * DH + tx + 16 * e] = o[r][e] * inv;
+        set_cols<DH>(static_cast<float*>(a.o) + row * DH, tx, o[r], inv);
         if (tx == 0 && a.lse_out != nullptr) a.lse_out[row] = l[r] != 0.f ? (m[r] + log2f(l[r])) * kLn2 : -INFINITY;
     }
 }
@@ -232,7 +260,7 @@ __global__ void __launch_bounds__(kThreads) window_bwd_q_fp32_kernel(const __gri
         float t = 0.f;
 #pragma unroll
         for (int e = 0; e < DH / 16; ++e) {
-            t = fmaf(dO[(RT * ty + r) * row_len<DH>() + tx + 16 * e], static_cast<const float*>(a.out)[row * DH + tx + 16 * e], t);
+            t = fmaf(dO[(RT * ty + r) * row_len<DH>() + tx + 16 * e], static_cast<const float*>(a.out)[row * DH + tx + 16 * e], t);      // (any order of the columns)
             dq[r][e] = 0.f;
         }
 #pragma unroll
@@ -288,13 +316,13 @@ __global__ void __launch_bounds__(kThreads) window_bwd_q_fp32_kernel(const __gri
     for (int r = 0; r < RT; ++r) {
         const int i = q0 + RT * ty + r;
         if (i >= q_len) continue;
-#pragma unroll
-        for (int e = 0; e < DH / 16; ++e)
-            static_cast<float*>(a.dq)[(size_t)(seqs.q_start[b] + i) * a.dq_stride + (size_t)h * DH + tx + 16 * e] = dq[r][e] * a.scale;
+        set_cols<DH>(static_cast<float*>(a.dq) + (size_t)(seqs.q_start[b] + i) * a.dq_stride + (size_t)h * DH, tx, dq[r], a.scale);
     }
 }
 
-// One CTA = 64 keys of one (sequence, query head).  a.sink_part (when heads share keys): fp32 [kv rows][Hq][2][DH], dV then dK.
+// One CTA = R keys of one (sequence, query head).  What lies past the band of a sink tile is cut into segments, CTAs of their own that
+// come first; the rows of sinks then go to a.sink_part, fp32 [sequence][Hq][1 + segments][sink_rows][2][DH] (the band's part, then the
+// segments'), dV then dK.  a.group_part (where heads share keys): [kv rows][Hq][2][DH].  The last launches add both up in order.
 template <int DH, int R>
 __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
     extern __shared__ __align__(16) float sm[];
@@ -304,12 +332,21 @@ __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __gr
     int tile;
     const int b = win_find(seqs.item, a.batch, blockIdx.x, tile);
     const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
-    const int k0 = tile * R, h = blockIdx.y, kvh = h / a.G;
+    const int parts = (a.sink_rows + R - 1) / R * a.sink_segs;
+    const int seg = tile < parts ? tile % a.sink_segs : -1;
+    const int k0 = (seg >= 0 ? tile / a.sink_segs : tile - parts) * R, h = blockIdx.y, kvh = h / a.G;
+    if (seg >= 0 && k0 >= kv_len) return;
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     load_tile<DH, R>(K, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, k0, kv_len, (size_t)kvh * DH);
     load_tile<DH, R>(V, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, k0, kv_len, (size_t)kvh * DH);
-    const int from = max(0, k0 - shift);
-    const int to = k0 < a.sinks ? q_len : max(0, min(q_len, min(k0 + R, kv_len) - 1 - shift + a.window));
+    const int band = max(0, min(q_len, min(k0 + R, kv_len) - 1 - shift + a.window));      // the first query past the band
+    int from = max(0, k0 - shift), to = k0 < a.sinks && a.sink_segs == 0 ? q_len : band;
+    if (seg >= 0) {
+        from = max(from, band);
+        const int all = from < q_len ? (q_len - from + kT - 1) / kT : 0;
+        to = min(q_len, from + (int)((long long)all * (seg + 1) / a.sink_segs) * kT);
+        from += (int)((long long)all * seg / a.sink_segs) * kT;
+    }
     const float* stats = a.stats + (size_t)h * 2 * a.stat_rows + stat_row0(seqs, b);
     float dk[RT][DH / 16], dv[RT][DH / 16];
 #pragma unroll
@@ -343,7 +380,7 @@ __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __gr
             const float nl = i < q_len ? __ldg(stats + i) : 0.f, nd = i < q_len ? __ldg(stats + a.stat_rows + i) : 0.f;
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const bool vis = i < q_len && visible(k0 + RT * ty + r, i + shift, a);
+                const bool vis = i < to && visible(k0 + RT * ty + r, i + shift, a);
                 const float p = vis ? exp2f(fmaf(s[r][c], a.scale_log2, nl)) : 0.f;
                 s[r][c] = p;
                 dp[r][c] = vis ? p * (dp[r][c] + nd) : 0.f;
@@ -361,18 +398,13 @@ __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __gr
         const int key = k0 + RT * ty + r;
         if (key >= kv_len) continue;
         const size_t row = (size_t)(seqs.k_start[b] + key);
-#pragma unroll
-        for (int e = 0; e < DH / 16; ++e) {
-            const int c = tx + 16 * e;
-            if (a.G > 1) {
-                float* part = a.sink_part + (row * a.Hq + h) * 2 * DH;
-                part[c] = dv[r][e];
-                part[DH + c] = dk[r][e] * a.scale;
-            } else {
-                static_cast<float*>(a.dv)[row * a.dv_stride + (size_t)kvh * DH + c] = dv[r][e];
-                static_cast<float*>(a.dk)[row * a.dk_stride + (size_t)kvh * DH + c] = dk[r][e] * a.scale;
-            }
-        }
+        const bool part = a.sink_segs > 0 && key < a.sinks;
+        if (seg >= 0 && !part) continue;
+        float* to_v = part ? a.sink_part + ((((size_t)b * a.Hq + h) * (1 + a.sink_segs) + (1 + seg)) * a.sink_rows + key) * 2 * DH
+                    : a.G > 1 ? a.group_part + (row * a.Hq + h) * 2 * DH : static_cast<float*>(a.dv) + row * a.dv_stride + (size_t)kvh * DH;
+        float* to_k = part || a.G > 1 ? to_v + DH : static_cast<float*>(a.dk) + row * a.dk_stride + (size_t)kvh * DH;
+        set_cols<DH>(to_v, tx, dv[r], 1.f);
+        set_cols<DH>(to_k, tx, dk[r], a.scale);
     }
 }
 
@@ -384,12 +416,24 @@ __global__ void __launch_bounds__(256) window_group_join_fp32_kernel(const __gri
         const long long rest = i / (2 * DH);
         const int kvh = (int)(rest % a.Hkv);
         const long long row = rest / a.Hkv;
-        const float* p = a.sink_part + ((size_t)row * a.Hq + (size_t)kvh * a.G) * 2 * DH + c;
+        const float* p = a.group_part + ((size_t)row * a.Hq + (size_t)kvh * a.G) * 2 * DH + c;
         float x = 0.f;
         for (int g = 0; g < a.G; ++g) x += p[(size_t)g * 2 * DH];
         if (c < DH) static_cast<float*>(a.dv)[(size_t)row * a.dv_stride + (size_t)kvh * DH + c] = x;
         else static_cast<float*>(a.dk)[(size_t)row * a.dk_stride + (size_t)kvh * DH + c - DH] = x;
     }
+}
+
+// dK, dV of the sinks: head after head of the group, the band's part and the segments' of each.  blockIdx = (row, K/V head, sequence).
+__global__ void __launch_bounds__(256) window_sink_join_fp32_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs, int DH) {
+    const int key = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z, c = threadIdx.x;
+    if (key >= seqs.kv_len[b] || c >= 2 * DH) return;
+    const float* p = a.sink_part + (((size_t)b * a.Hq + (size_t)kvh * a.G) * (1 + a.sink_segs) * a.sink_rows + key) * 2 * DH + c;
+    float x = 0.f;
+    for (int i = 0; i < a.G * (1 + a.sink_segs); ++i) x += p[(size_t)i * a.sink_rows * 2 * DH];
+    const size_t row = (size_t)(seqs.k_start[b] + key);
+    if (c < DH) static_cast<float*>(a.dv)[row * a.dv_stride + (size_t)kvh * DH + c] = x;
+    else static_cast<float*>(a.dk)[row * a.dk_stride + (size_t)kvh * DH + c - DH] = x;
 }
 
 int retile(WinSeqs& s, int batch, const int32_t* len, int rows) {
@@ -427,7 +471,10 @@ int bwd_kv_rows(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
     using SM = Fp32Smem<DH, R, 2, 2>;
     static PerDeviceOnce once;
     if (!raise_limit(window_bwd_kv_fp32_kernel<DH, R>, once, SM())) return -1;
-    window_bwd_kv_fp32_kernel<DH, R><<<dim3(retile(s, a.batch, s.kv_len, R), a.Hq), kThreads, SM::kBytes, stream>>>(a, s);
+    retile(s, a.batch, s.kv_len, R);
+    const int parts = (a.sink_rows + R - 1) / R * a.sink_segs;
+    for (int b = 1; b <= a.batch; ++b) s.item[b] += b * parts;
+    window_bwd_kv_fp32_kernel<DH, R><<<dim3(s.item[a.batch], a.Hq), kThreads, SM::kBytes, stream>>>(a, s);
     return 1;
 }
 
@@ -451,6 +498,10 @@ int bwd(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
         if (a.G > 1) {
             const long long rows = (long long)s.k_start[a.batch - 1] + s.kv_len[a.batch - 1], n = rows * a.Hkv * 2 * DH;
             window_group_join_fp32_kernel<<<dim3((unsigned)((n + 255) / 256 < 148 * 8 ? (n + 255) / 256 : 148 * 8)), 256, 0, stream>>>(a, DH, rows);
+            ++launched;
+        }
+        if (a.sink_segs > 0) {           // (over what the join of the groups left in the sinks' rows)
+            window_sink_join_fp32_kernel<<<dim3(a.sink_rows, a.Hkv, a.batch), 256, 0, stream>>>(a, s, DH);
             ++launched;
         }
     }

@@ -286,3 +286,12 @@ def test_one_row_at_any_distance(dtype):
     got, want = run(q, k, v, do, [1], [1], 0, 0, False), run(*dense, [1], [1], 0, 0, False)
     for name in want:
         assert torch.equal(got[name], want[name]), name
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(2, 2, 64), (4, 1, 32), (2, 1, 128), (3, 3, 16)])
+@pytest.mark.parametrize("window,sinks", [(64, 4), (30, 70), (5, 1), (200, 130)])
+def test_sinks_past_the_band_fp32(hq, hkv, dh, window, sinks):
+    """Long ragged fp32 sequences: the sinks' gradients come from several segments of queries, of several heads."""
+    q_len, kv_len = [700, 0, 90, 1], [760, 20, 90, 0]
+    q, k, v, do = inputs(q_len, kv_len, hq, hkv, dh, "fp32", 23)
+    compare(run(q, k, v, do, q_len, kv_len, window, sinks, True), reference(q, k, v, do, q_len, kv_len, window, sinks, True, "fp32"))
