@@ -1,6 +1,7 @@
 // Entry points of the windowed attention over whole sequences: host-side checks, workspace layout and launch choice.
 #include <cstring>
 
+#include "tensor_map.h"
 #include "window_attn.h"
 
 using namespace beagle;
@@ -8,8 +9,8 @@ using namespace beagle;
 namespace {
 
 struct Layout {
-    size_t stats, part, group, total;
-    int stat_rows, sink_rows, sink_tiles, sink_segs;
+    size_t stats, part, group, split, total;
+    int stat_rows, sink_rows, sink_tiles, sink_segs, splits;
 };
 
 constexpr int kMaxSinks = 1024;          // with a window
@@ -69,30 +70,57 @@ Layout layout(const beagle_window_attn* w, const WinArgs& a, const WinSeqs& s, l
         off += ((size_t)k_rows * a.Hq * 2 * d * sizeof(float) + 255) / 256 * 256;
     }
     L.part = off;
-    if (a.sinks > 0) {
-        // Segments of the queries past the band of the sinks' key tiles, about as long as a band CTA's work (at least eight
-        // tiles, fp32 two), as many as the longest sequence needs.
-        const int rows_s = a.sinks < most_kv ? a.sinks : most_kv;
-        int segs = 0;
+    // Jobs (128 queries of one head) past the band of a sequence's first key tile, and of a key tile's band at most.
+    auto past = [&](int b) -> long long {
+        if (a.sinks == 0 || s.kv_len[b] == 0) return 0;
+        const long long shift = s.kv_len[b] - s.q_len[b] - a.strict;
+        long long end = (s.kv_len[b] < kKTile ? s.kv_len[b] : kKTile) - 1 - shift + a.window;
+        end = end < 0 ? 0 : end > s.q_len[b] ? s.q_len[b] : end;
+        return s.q_len[b] == end ? 0 : (s.q_len[b] - end + kQTile) / kQTile * (fp32 ? 1 : a.G);        // (the fp32 kernels: a CTA per head)
+    };
+    long long band = ((long long)a.window + 2 * kKTile) / kQTile * (fp32 ? 1 : a.G);
+    const int rows_s = a.sinks < most_kv ? a.sinks : most_kv, tiles_s = (rows_s + kKTile - 1) / kKTile;
+    L.splits = 1;
+    if (band < (fp32 ? 2 : 8)) band = fp32 ? 2 : 8;
+    if (!fp32) {
+        // Few key tiles with many jobs each: several CTAs share a tile's jobs, with as few jobs each (two at least) as leave every
+        // CTA, those of the sinks' segments among them, an SM of its own.  (Backward, 8 heads of 128 over one K/V head, 1000 queries:
+        // 127 us unshared, 52 so; 8 x 200, 16 heads over 2, window 9: 57 and 45; below eight jobs a tile the join costs what it saves.)
+        long long tiles = 0, jobs = 0, late = 0;
         for (int b = 0; b < a.batch; ++b) {
-            const long long shift = s.kv_len[b] - s.q_len[b] - a.strict;
-            long long end = (s.kv_len[b] < kKTile ? s.kv_len[b] : kKTile) - 1 - shift + a.window;
-            end = end < 0 ? 0 : end > s.q_len[b] ? s.q_len[b] : end;
-            const int heads = fp32 ? 1 : a.G;            // that one CTA serves; the fp32 kernels' tiles are half as long
-            const long long jobs = (s.q_len[b] - end + 1 + kQTile - 1) / kQTile * heads;
-            if (s.q_len[b] == end || s.kv_len[b] == 0) continue;
-            long long band = ((long long)a.window + 2 * kKTile) / kQTile * heads;
-            const int least = fp32 ? 2 : 8;
-            if (band < least) band = least;
-            const int need = (int)((jobs + band - 1) / band);
-            segs = need > segs ? need : segs;
+            const long long span = (long long)a.window + 2 * kKTile < s.q_len[b] ? (long long)a.window + 2 * kKTile : s.q_len[b];
+            const long long n = (span + kQTile - 1) / kQTile * a.G;
+            jobs = n > jobs ? n : jobs;
+            late = past(b) > late ? past(b) : late;
+            tiles += (s.kv_len[b] + kKTile - 1) / kKTile;
         }
-        L.sink_segs = segs > 64 ? 64 : segs;
-        if (L.sink_segs > 0) {
-            L.sink_rows = rows_s;
-            L.sink_tiles = (rows_s + kKTile - 1) / kKTile;
-            off += (size_t)a.batch * (fp32 ? a.Hq : a.Hkv) * (1 + L.sink_segs) * rows_s * 2 * d * sizeof(float);
+        const long long units = tiles * a.Hkv, sms = device_sm_count();
+        if (units * 2 <= sms && jobs >= 8) {
+            long long each = 2;
+            auto ctas = [&]() { return units * ((jobs + each - 1) / each) + (late + each - 1) / each * tiles_s * a.Hkv * a.batch; };
+            while (each < jobs && ctas() > sms) ++each;
+            const long long n = (jobs + each - 1) / each;
+            L.splits = (int)(n < 16 ? n : 16);
+            if (L.splits > 1) band = each;
         }
+        if (L.splits > 1) {
+            L.split = off;
+            off += (size_t)units * L.splits * kKTile * 2 * d * sizeof(float);
+            L.part = off;
+        }
+    }
+    // Segments of the queries past the band of the sinks' key tiles, about as long as a band CTA's work (at least eight jobs where
+    // the tiles are not shared, fp32 two), as many as the longest sequence needs.
+    int segs = 0;
+    for (int b = 0; b < a.batch; ++b) {
+        const int need = (int)((past(b) + band - 1) / band);
+        segs = need > segs ? need : segs;
+    }
+    L.sink_segs = segs > 64 ? 64 : segs;
+    if (L.sink_segs > 0) {
+        L.sink_rows = rows_s;
+        L.sink_tiles = tiles_s;
+        off += (size_t)a.batch * (fp32 ? a.Hq : a.Hkv) * (1 + L.sink_segs) * rows_s * 2 * d * sizeof(float);
     }
     L.total = (off + 255) / 256 * 256;
     return L;
@@ -163,6 +191,8 @@ beagle_status beagle_window_attn_backward(const beagle_window_attn* w, const voi
     a.stats = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.stats);
     a.sink_part = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.part);
     a.group_part = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.group);
+    a.split_part = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.split);
+    a.splits = L.splits;
     a.stat_rows = L.stat_rows; a.sink_rows = L.sink_rows; a.sink_tiles = L.sink_tiles; a.sink_segs = L.sink_segs;
     const cudaStream_t cs = static_cast<cudaStream_t>(stream);
     const int rc = w->dtype == BEAGLE_BF16 ? window_bwd_bf16(a, s, w->head_dim, q_rows, k_rows, cs) : window_bwd_fp32(a, s, w->head_dim, cs);

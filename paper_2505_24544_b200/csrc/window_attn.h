@@ -23,8 +23,10 @@ struct WinArgs {
     float* lse_out;
     float* stats;                                                // [Hq][2][stat_rows]: -log-sum-exp (log2 units), and -delta, of every query
     float* sink_part;                                            // fp32 partials of the sinks' dK, dV
+    float* split_part;                                           // key side in splits: fp32 [tile][K/V head][split][128][2][DH], dV then dK
     float* group_part;                                           // fp32 kernels: dV, dK of every query head, where heads share keys
     int32_t stat_rows;                                           // sum over the sequences of q_len padded to kStatPad
+    int32_t splits;                                              // CTAs that share the jobs of a key tile
     int32_t sink_rows, sink_tiles, sink_segs;                    // layout of sink_part, see window_attn_bwd.cu and window_attn_fp32.cu
 };
 constexpr int kNoWindow = 0x3fffffff;

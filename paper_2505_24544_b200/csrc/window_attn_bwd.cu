@@ -22,7 +22,8 @@
 //
 // The sinks' keys are read by every later query.  What lies past the band of a key tile is therefore cut into segments of
 // similar length, each a CTA of its own that leaves fp32 partials of the (few) sink rows; a last small launch adds them to the
-// band's partial in the order of the queries.
+// band's partial in the order of the queries.  Where the key tiles are too few for the GPU, several CTAs share the jobs of one and
+// leave fp32 partials that a launch adds in order (splits).
 //
 // Rows behind a sequence (the next one's) are zeroed in shared memory where they would be multiplied by a weight of 0.
 // Every wait is bounded; a CTA that gives up leaves NaN in its rows.
@@ -509,10 +510,12 @@ __device__ __forceinline__ int band_end(int k0, int kv_len, int q_len, int shift
 // Per sequence the grid's list has first its key tiles (bands), then, for each of the sink_tiles, sink_segs segments.
 struct KItem {
     int b, kvh, k0, q_len, kv_len, shift, k_row, seg, band, n;      // seg: -1 = band; band: first query past it; n: jobs
-    int j0;
+    int j0, split;                       // first job; which of the tile's splits
     QueryWalk w;
+    template <bool SPLIT>                // the jobs of a tile are shared
     __device__ __forceinline__ void load(int at, const WinArgs& a, const WinSeqs& s) {
         int item;
+        const int splits = SPLIT ? a.splits : 1;
         const int unit = at / a.Hkv;                             // the heads of a tile side by side: the cheap tiles, the last ones, stay for the end
         kvh = at - unit * a.Hkv;
         b = win_find(s.item, a.batch, unit, item);
@@ -522,14 +525,18 @@ struct KItem {
         const int parts = a.sink_tiles * a.sink_segs;            // the sinks' segments first, then the bands of the tiles
         const bool sink_part = item < parts;
         seg = sink_part ? item % a.sink_segs : -1;
-        k0 = (sink_part ? item / a.sink_segs : item - parts) * kKTile;
+        const int tile = sink_part ? item / a.sink_segs : (item - parts) / splits;
+        split = SPLIT && !sink_part ? item - parts - tile * splits : 0;
+        k0 = tile * kKTile;
         k_row = s.k_start[b] + k0;
         band = band_end(k0, kv_len, q_len, shift, a.window);
         j0 = 0;
         n = 0;
         if (!sink_part) {
             w.init(k0 - shift, band);
-            n = w.n * a.G;
+            const int total = w.n * a.G;
+            j0 = total * split / splits;
+            n = total * (split + 1) / splits - j0;
         } else if (k0 < min(a.sinks, kv_len)) {
             w.init(band, q_len);
             const int total = w.n * a.G;
@@ -538,6 +545,12 @@ struct KItem {
         }
     }
 };
+// Place of a key tile and K/V head in WinArgs::split_part.
+__device__ __forceinline__ int key_unit(int b, int tile, int kvh, const WinArgs& a, const WinSeqs& s) {
+    int at = tile;
+    for (int i = 0; i < b; ++i) at += (s.kv_len[i] + kKTile - 1) / kKTile;
+    return at * a.Hkv + kvh;
+}
 // Jobs of an item in order: the tiles of one head after the other.
 struct Job {
     int h, qb, left;                     // query head, first query, tiles left of this head
@@ -553,7 +566,7 @@ struct Job {
     }
 };
 
-template <int DH>
+template <int DH, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmdO,
                                                                   const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                                                                   const __grid_constant__ CUtensorMap tmdK, const __grid_constant__ CUtensorMap tmdV,
@@ -598,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
         int n = 0, issued = 0, loaded = 0;                       // jobs walked, copies of Q and dO, items with jobs
         for (int r = 0, at; ok && (at = item_at(r)) < items; ++r) {
             KItem x;
-            x.load(at, a, seqs);
+            x.load<SPLIT>(at, a, seqs);
             if (x.n == 0) continue;
             ok = warp_wait(kv_empty, (loaded & 1) ^ 1, s_abort);
             if (!ok) break;
@@ -678,7 +691,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
                 const int at = item_at(++r);
                 more = at < items;
                 if (!more) return;
-                x.load(at, a, seqs);
+                x.load<SPLIT>(at, a, seqs);
                 if (x.n > 0) break;
             }
             job.first(x, a.G);
@@ -771,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
         int n = 0;
         for (int r = 0, at; (at = item_at(r)) < items; ++r) {
             KItem x;
-            x.load(at, a, seqs);
+            x.load<SPLIT>(at, a, seqs);
             const bool sink_part = x.seg >= 0;
             if (sink_part && x.n == 0) continue;                 // the join knows
             const int key = x.k0 + q * 32 + lane;
@@ -829,11 +842,13 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
             if (x.n > 0 && ok) ok = warp_wait2(y_free + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, x_free + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, s_abort);
             // The item is read again rather than held over the loop above, whose registers are short.
             asm volatile("" : "+r"(at));
-            x.load(at, a, seqs);
+            x.load<SPLIT>(at, a, seqs);
             fence_after();
             const float sv = ok ? 1.f : nan_f(), sk = ok ? a.scale : nan_f();
             const int my_key = x.k0 + q * 32 + lane;
-            const bool sink_item = x.seg >= 0, to_part = a.sink_segs > 0 && my_key < min(a.sinks, x.kv_len);        // rows that several items share go to the join, in fp32
+            // rows that several items share go to the joins, in fp32
+            const bool sink_item = x.seg >= 0, in_splits = SPLIT && !sink_item;
+            const bool to_part = in_splits ? my_key < x.kv_len : a.sink_segs > 0 && my_key < min(a.sinks, x.kv_len);
             const size_t row = (size_t)(x.k_row + q * 32 + lane);
             const int col = half * (DH / 2);                     // this thread's half of the columns
             const bool write = my_key < x.kv_len && !sink_item && !to_part;
@@ -842,7 +857,9 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
                 const uint32_t acc = tmem + (m == 0 ? kDV : kDK) + col + lanes;
                 const float f = m == 0 ? sv : sk;
                 if (__any_sync(0xffffffffu, to_part)) {
-                    float* part = a.sink_part + ((((size_t)x.b * a.Hkv + x.kvh) * (1 + a.sink_segs) + (1 + x.seg)) * a.sink_rows + my_key) * 2 * DH + m * DH + col;
+                    float* part = in_splits ? a.split_part + (((size_t)key_unit(x.b, x.k0 / kKTile, x.kvh, a, seqs) * a.splits + x.split) * kKTile + (my_key - x.k0)) * 2 * DH
+                                            : a.sink_part + ((((size_t)x.b * a.Hkv + x.kvh) * (1 + a.sink_segs) + (1 + x.seg)) * a.sink_rows + my_key) * 2 * DH;
+                    part += m * DH + col;
 #pragma unroll 1
                     for (int c = 0; c < DH / 2; c += 16) {
                         uint32_t u[16];
@@ -869,6 +886,34 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
     if (warp == 1) {
         fence_after();
         tmem_dealloc<kTmem>(tmem);
+    }
+}
+
+// Adds the splits of a key tile, in order: to dV and dK, or (rows of sinks that segments share) to the band's place of the sinks'
+// partials.  blockIdx = (sixteen rows of a tile, K/V head, tile of all sequences).
+template <int DH>
+__global__ void __launch_bounds__(256) window_split_join_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
+    constexpr int kVecs = 2 * DH / 4;                            // float4 of a row
+    const int kvh = blockIdx.y;
+    int b = 0, tile = blockIdx.z;
+    for (int n; tile >= (n = (seqs.kv_len[b] + kKTile - 1) / kKTile); ++b) tile -= n;
+    const int kv_len = seqs.kv_len[b];
+    const float4* p = reinterpret_cast<const float4*>(a.split_part) + ((size_t)blockIdx.z * a.Hkv + kvh) * a.splits * kKTile * kVecs;
+    for (int i = threadIdx.x; i < 16 * kVecs; i += 256) {
+        const int r = blockIdx.x * 16 + i / kVecs, c = i % kVecs * 4, key = tile * kKTile + r;
+        if (key >= kv_len) break;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < a.splits; ++s) {
+            const float4 y = p[((size_t)s * kKTile + r) * kVecs + c / 4];
+            x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+        }
+        if (a.sink_segs > 0 && key < a.sinks) {
+            *reinterpret_cast<float4*>(a.sink_part + (((size_t)b * a.Hkv + kvh) * (1 + a.sink_segs) * a.sink_rows + key) * 2 * DH + c) = x;
+        } else {
+            const size_t row = (size_t)(seqs.k_start[b] + key);
+            bf16* dst = c < DH ? static_cast<bf16*>(a.dv) + row * a.dv_stride + c : static_cast<bf16*>(a.dk) + row * a.dk_stride + c - DH;
+            *reinterpret_cast<uint2*>(dst + (size_t)kvh * DH) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+        }
     }
 }
 
@@ -914,7 +959,8 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
     static PerDeviceOnce attr;
     if (!attr.ensure([] {
             return cudaFuncSetAttribute(window_bwd_q_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, SQ::kBytes) == cudaSuccess &&
-                   cudaFuncSetAttribute(window_bwd_kv_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, SK::kBytes) == cudaSuccess;
+                   cudaFuncSetAttribute(window_bwd_kv_kernel<DH, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SK::kBytes) == cudaSuccess &&
+                   cudaFuncSetAttribute(window_bwd_kv_kernel<DH, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SK::kBytes) == cudaSuccess;
         }))
         return -1;
     const int sms = device_sm_count();
@@ -928,7 +974,7 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
     if (hk) {
         WinSeqs t = s;                   // items of the key side: band tiles and sink segments
         t.item[0] = 0;
-        for (int b = 0; b < a.batch; ++b) t.item[b + 1] = t.item[b] + (s.kv_len[b] + kKTile - 1) / kKTile + a.sink_tiles * a.sink_segs;
+        for (int b = 0; b < a.batch; ++b) t.item[b + 1] = t.item[b] + (s.kv_len[b] + kKTile - 1) / kKTile * a.splits + a.sink_tiles * a.sink_segs;
         if (t.item[a.batch] > 0) {
             const long long items = (long long)t.item[a.batch] * a.Hkv;
             if (items > 0x3fffffff) return -1;
@@ -937,8 +983,14 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
             // (5 tiles, 8 x 2048: 731 against 783).
             const long long jobs = ((long long)(a.window < 1 << 24 ? a.window : 1 << 24) + 2 * kKTile) / kQTile * a.G;
             const bool share = jobs < 24 && items > sms;
-            window_bwd_kv_kernel<DH><<<(unsigned)(share ? sms : items), kThreads, SK::kBytes, stream>>>(mq, mdo, mk, mv, mdk, mdv, a, t);
+            (a.splits > 1 ? window_bwd_kv_kernel<DH, true> : window_bwd_kv_kernel<DH, false>)
+                <<<(unsigned)(share ? sms : items), kThreads, SK::kBytes, stream>>>(mq, mdo, mk, mv, mdk, mdv, a, t);
             ++launched;
+            if (a.splits > 1) {
+                const int tiles = (t.item[a.batch] - a.batch * a.sink_tiles * a.sink_segs) / a.splits;
+                window_split_join_kernel<DH><<<dim3(kKTile / 16, a.Hkv, tiles), 256, 0, stream>>>(a, t);
+                ++launched;
+            }
             if (a.sink_segs > 0) {
                 window_sink_join_kernel<DH><<<dim3(a.sink_rows, a.Hkv, a.batch), 2 * DH, 0, stream>>>(a, t);
                 ++launched;

@@ -295,3 +295,16 @@ def test_sinks_past_the_band_fp32(hq, hkv, dh, window, sinks):
     q_len, kv_len = [700, 0, 90, 1], [760, 20, 90, 0]
     q, k, v, do = inputs(q_len, kv_len, hq, hkv, dh, "fp32", 23)
     compare(run(q, k, v, do, q_len, kv_len, window, sinks, True), reference(q, k, v, do, q_len, kv_len, window, sinks, True, "fp32"))
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(8, 1, 128), (8, 1, 64), (16, 2, 64), (6, 1, 128)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (9, 0), (200, 4), (30, 140)])
+def test_shared_key_tiles(hq, hkv, dh, window, sinks):
+    """Few key tiles, many heads on each: several CTAs share a tile's jobs, with and without segments of the sinks."""
+    q_len, kv_len = [600, 0, 130, 1], [650, 5, 130, 1]
+    x = inputs(q_len, kv_len, hq, hkv, dh, "bf16", 29)
+    first = run(*x, q_len, kv_len, window, sinks, False)
+    compare(first, reference(*x, q_len, kv_len, window, sinks, False, "bf16"))
+    again = run(*x, q_len, kv_len, window, sinks, False)
+    for name in first:
+        assert torch.equal(first[name], again[name]), name
