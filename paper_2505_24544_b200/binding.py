@@ -535,22 +535,23 @@ def _host_i32(values: Sequence[int]) -> bytes:
 
 def _check(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], dense: bool = True) -> int:
     """The tensor's address, after checking its type, shape, layout and that it lies on the current device."""
+    device = t.get_device()                      # -1: host memory
+    if t.dtype == dtype and t.shape == shape and device >= 0 and device == torch._C._cuda_getDevice() and (not dense or t.is_contiguous()):
+        return t.data_ptr()
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    if device < 0 or device != torch._C._cuda_getDevice():
         raise ValueError(f"{name}: must be on the current CUDA device")
-    if dense and not t.is_contiguous():
-        raise ValueError(f"{name}: tensor must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name}: tensor must be contiguous")
 
 
 def _row_stride(name: str, t: torch.Tensor, lead: int) -> int:
     """Elements between consecutive rows of a tensor whose last two dimensions ([heads, head_dim]) are dense and whose first
     `lead` dimensions count rows at one distance (a dense tensor, or a slice of a fused projection)."""
-    heads, dh = t.shape[lead:]
-    st = t.stride()
+    heads, dh = t.shape[-2:]
     if t.is_contiguous():
         return heads * dh
+    st = t.stride()
     if (dh > 1 and st[-1] != 1) or (heads > 1 and st[-2] != dh):
         raise ValueError(f"{name}: the heads of a row must be dense")
     if lead == 2 and t.shape[1] > 1:
@@ -598,14 +599,15 @@ class PagedCache:
         _pages_ok(self.lib.beagle_pages_workspace_bytes(C.byref(p), C.byref(n)), "beagle_pages_workspace_bytes")
         self.ws = torch.empty(n.value, dtype=torch.uint8, device=k.device)
         p.ws, p.ws_bytes = self.ws.data_ptr(), n.value
-        self.struct, self.ref = p, C.byref(p)
+        self.struct, self.ref, self.device_index = p, C.byref(p), k.get_device()
         self.attn_ws_bytes: Dict[Tuple[int, int, int], int] = {}      # (query heads, window, sinks) -> workspace of beagle_paged_attn
 
     def on_current_device(self) -> int:
         """The current stream, after checking that the cache lies on the current device."""
-        if self.k.get_device() != torch.cuda.current_device():
+        device = self.device_index
+        if device != torch._C._cuda_getDevice():
             raise ValueError("the cache must be on the current CUDA device")
-        return _stream()
+        return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _pages_ok(st: int, what: str) -> None:
