@@ -7,7 +7,7 @@
 // bound by memory bandwidth (16-byte loads and stores, four in flight per thread).
 //
 // Measured: prompts of up to 8192 tokens for 8 sequences (370 MB moved) 64 us, book-keeping before it 6; copy of 16 serving
-// sequences 63 us (6.5 TB/s), its book-keeping 11.
+// sequences 63 us (6.5 TB/s), its book-keeping 9.
 //
 // Every index that comes from device memory (table entries, lengths, counts) is clamped or range-checked before it is used, so
 // a damaged table yields wrong contents but no access outside the caller's buffers.
@@ -167,12 +167,17 @@ __device__ __forceinline__ int find_free(const Book& b, int want, int32_t* list,
     return min(found, want);
 }
 
-// Gives back the pages of `row` from entry `from` on.  One warp.
-__device__ __forceinline__ void release_row(const Book& b, int32_t* row, int from, int lane) {
-    for (int j = from + lane; j < b.max_pages; j += 32) {
-        const int id = row[j];
-        if (b.page_ok(id)) atomicSub(b.refs + id, 1);
-        if (id != -1) row[j] = -1;
+// Gives back the pages of `row`.  One warp, four entries a lane in flight.
+__device__ __forceinline__ void release_row(const Book& b, int32_t* row, int lane) {
+    for (int j = lane; j < b.max_pages; j += 128) {
+        int id[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) id[u] = j + 32 * u < b.max_pages ? __ldcg(row + j + 32 * u) : -1;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (b.page_ok(id[u])) atomicSub(b.refs + id[u], 1);
+            if (id[u] != -1) row[j + 32 * u] = -1;
+        }
     }
 }
 
@@ -323,23 +328,21 @@ __global__ void __launch_bounds__(128) pages_fork_kernel(const Book b, const Pag
 __global__ void __launch_bounds__(kBookThreads) pages_copy_book_kernel(const Book b, const PageSlots src, const PageSlots dst, int n, int32_t* ok_out) {
     __shared__ int s_warp[33];
     __shared__ int s_need[kMaxCallBatch], s_start[kMaxCallBatch];
+    __shared__ int32_t s_list[kNear];
     const int t = threadIdx.x, lane = t & 31;
     pdl_launch_dependents();
     pdl_wait();
     const BookWs ws = book_ws(b.ws, b.n_pages);
-    for (int i = t >> 5; i < n; i += kBookThreads / 32) release_row(b, b.row(dst.slot[i]), 0, lane);
+    const int len = t < n ? b.clamp_len(__ldcg(b.length + src.slot[t])) : 0;
+    for (int i = t >> 5; i < n; i += kBookThreads / 32) release_row(b, b.row(dst.slot[i]), lane);
     __threadfence();
-    __syncthreads();                                     // what the destinations held is free now
+    const int need = (len + b.page_size - 1) / b.page_size;
+    int want = 0;
+    const int start = block_scan(need, s_warp, want);    // (its barriers: what the destinations held is free now)
     int refs[kScanPer];
     load_refs(b.refs, t * kScanPer, b.n_pages, refs);
-    int need = 0, len = 0, want = 0;
-    if (t < n) {
-        len = b.clamp_len(__ldcg(b.length + src.slot[t]));
-        need = (len + b.page_size - 1) / b.page_size;
-    }
-    const int start = block_scan(need, s_warp, want);
-    const int got = find_free(b, want, ws.dst, s_warp, refs);
-    __syncthreads();
+    int32_t* list = want <= kNear ? s_list : ws.dst;
+    const int got = find_free(b, want, list, s_warp, refs);
     if (t < n) {
         const bool ok = need == 0 || start + need <= got;
         s_need[t] = ok ? need : 0;
@@ -357,11 +360,19 @@ __global__ void __launch_bounds__(kBookThreads) pages_copy_book_kernel(const Boo
     for (int row = t >> 5; row < n; row += kBookThreads / 32) {
         const int32_t* from = b.row(src.slot[row]);
         int32_t* to = b.row(dst.slot[row]);
-        for (int i = lane; i < s_need[row]; i += 32) {
-            const int id = ws.dst[s_start[row] + i];
-            to[i] = id;
-            b.refs[id] = 1;
-            ws.src[s_start[row] + i] = __ldcg(from + i);
+        for (int i = lane; i < s_need[row]; i += 128) {
+            int page[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) page[u] = i + 32 * u < s_need[row] ? __ldcg(from + i + 32 * u) : -1;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i + 32 * u < s_need[row]) {
+                    const int at = s_start[row] + i + 32 * u, id = list[at];
+                    to[i + 32 * u] = id;
+                    b.refs[id] = 1;
+                    ws.src[at] = page[u];
+                    ws.dst[at] = id;
+                }
         }
     }
 }
@@ -373,8 +384,11 @@ __global__ void __launch_bounds__(kBookThreads) pages_compact_book_kernel(const 
     pdl_launch_dependents();
     pdl_wait();
     const BookWs ws = book_ws(b.ws, b.n_pages);
-    int live = 0;
-    for (int base = 0; base < b.n_pages; base += kBookThreads * kScanPer) {
+    int live = 0, first[kScanPer];                       // this thread's counts of the first step, read once
+    load_refs(b.refs, t * kScanPer, b.n_pages, first);
+#pragma unroll
+    for (int i = 0; i < kScanPer; ++i) live += first[i] > 0;
+    for (int base = kBookThreads * kScanPer; base < b.n_pages; base += kBookThreads * kScanPer) {
         int r[kScanPer];
         load_refs(b.refs, base + t * kScanPer, b.n_pages, r);
 #pragma unroll
@@ -389,7 +403,10 @@ __global__ void __launch_bounds__(kBookThreads) pages_compact_book_kernel(const 
     for (int base = 0; base < b.n_pages; base += kBookThreads * kScanPer) {
         const int id0 = base + t * kScanPer;
         int r[kScanPer], mine = 0, total;
-        load_refs(b.refs, id0, b.n_pages, r);
+        if (base > 0) load_refs(b.refs, id0, b.n_pages, r);
+        else
+#pragma unroll
+            for (int i = 0; i < kScanPer; ++i) r[i] = first[i];
         // below `live`: holes; from there on: pages that move.  Both counted in one scan (16 bits would not do: two scans)
 #pragma unroll
         for (int i = 0; i < kScanPer; ++i) mine += id0 + i < live && r[i] == 0;
