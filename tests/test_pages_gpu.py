@@ -416,3 +416,13 @@ def test_serving_run(dtype):
     torch.cuda.synchronize()
     m.same(cache)
     check_attn(cache, [1, 2, 3, 4], q, 50, 2, dtype, out, lse)
+
+
+@pytest.mark.parametrize("dtype,dh,group", [("fp32", d, g) for d in (16, 32, 64, 128) for g in (1, 2, 3, 8)] +
+                         [("bf16", 32, g) for g in (1, 2, 4, 8)] + [("bf16", 256, g) for g in (1, 2, 4)])
+@pytest.mark.parametrize("ps,window,sinks", [(8, 0, 0), (64, 0, 0), (256, 700, 90)])
+def test_every_group_size_off_the_tensor_cores(dtype, dh, group, ps, window, sinks):
+    """Every width and number of query heads a K/V head of the CUDA-core kernel, on sequences that are cut and joined."""
+    cache = filled([3000, 1, 0, 257, 64, 1100], ps, 2, dh, dtype, 17)
+    q = (torch.randn(6, 2 * group, dh, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda") * 2).to(DT[dtype])
+    check_attn(cache, [5, 0, 1, 2, 3, 4], q, window, sinks, dtype)
