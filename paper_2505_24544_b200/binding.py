@@ -691,7 +691,10 @@ def beagle_paged_attn(cache: PagedCache, slots: Sequence[int], q: torch.Tensor, 
 
 def beagle_prefill_pages(ctx: Context, cache: PagedCache, seq_slot: Sequence[int], new_len: Sequence[int], hidden: Optional[torch.Tensor],
                          ok: Optional[torch.Tensor] = None) -> None:
-    """Keys and values of the target's states (packed rows, as ``beagle_prefill_kv``) into the slots' pages."""
+    """Keys and values of the target's states (packed rows, as ``beagle_prefill_kv``) into the slots' pages.  new_len: one count per
+    slot; hidden: [sum(new_len), d] in the storage type; ok: int32 [len(seq_slot)], as for ``beagle_pages_append``."""
+    if len(new_len) != len(seq_slot):
+        raise ValueError("new_len: one count per slot")
     rows = sum(new_len)
     hp = None if hidden is None else _check("hidden", hidden, torch_dtype(ctx.cfg.dtype), (rows, ctx.cfg.hidden))
     ok_ptr = None if ok is None else _check("ok", ok, torch.int32, (len(seq_slot),))

@@ -197,3 +197,27 @@ def test_head_over_pages_refusals(lib):
     assert prefill(pages(lib), size=2 * 768 - 1) == CAPACITY
     assert prefill(pages(lib), lens=(0,), hidden=None, ws=None, size=0) == OK and prefill(pages(lib), slots=()) == OK
     lib.beagle_destroy(h)
+
+
+class RefusingHead:
+    """A head and a cache in the binding's eyes, of hidden size 512 and 4096 tokens; a call that reaches the library fails the test."""
+
+    class Library:
+        def __getattr__(self, name):
+            raise AssertionError(f"{name} was reached")
+
+    def __init__(self):
+        from paper_2505_24544_b200.binding import BeagleConfig
+        self.cfg = BeagleConfig(512, 8, 2, 64, 1024, 4096, 1, 1e-5, 1, 1, 6, 64, 8, 0.0)
+        self.lib, self.handle, self.ref = self.Library(), None, None
+
+    def check(self, status):
+        assert status == OK
+
+
+@pytest.mark.parametrize("new_len", [[], [3], [3, 4, 5]])
+def test_prefill_pages_wants_one_length_per_slot(new_len):
+    """The library reads as many lengths as there are slots: a list of another length is refused before it sees them."""
+    from paper_2505_24544_b200 import binding as b
+    with pytest.raises(ValueError, match="new_len"):
+        b.beagle_prefill_pages(RefusingHead(), RefusingHead(), [0, 1], new_len, None)
