@@ -710,15 +710,20 @@ def beagle_prefill_pages(ctx: Context, cache: PagedCache, seq_slot: Sequence[int
 def beagle_draft_step_pages(ctx: Context, cache: PagedCache, seq_slot: Sequence[int], tokens_in: Optional[torch.Tensor], concat: bool,
                             tokens_out: Optional[torch.Tensor], logits_out: Optional[torch.Tensor] = None, hidden_out: Optional[torch.Tensor] = None,
                             window: int = 0, sinks: int = 0, ok: Optional[torch.Tensor] = None) -> None:
-    """``beagle_draft_step`` over the slots' pages, whole or through a window with sinks."""
+    """``beagle_draft_step`` over the slots' pages, whole or through a window with sinks.  tokens_in: int32 [batch]; tokens_out: int32
+    [batch] (a column view is fine); logits_out: fp32 [batch, V]; hidden_out: [batch, d] in the storage type; ok: int32 [batch], 0
+    where no page was free for the slot's state, which the chain then goes on without."""
+    B = len(seq_slot)
+    in_ptr = None if tokens_in is None else _check("tokens_in", tokens_in, torch.int32, (B,))
     stride, out_ptr = 1, None
     if tokens_out is not None:
-        if tokens_out.dim() != 1 or tokens_out.dtype != torch.int32:
-            raise ValueError("tokens_out must be a 1-D int32 tensor (a column view is fine)")
-        stride, out_ptr = int(tokens_out.stride(0)), tokens_out.data_ptr()
-    ok_ptr = None if ok is None else _check("ok", ok, torch.int32, (len(seq_slot),))
-    ctx.check(ctx.lib.beagle_draft_step_pages(ctx.handle, cache.ref, len(seq_slot), _host_i32(seq_slot), _ptr(tokens_in), int(bool(concat)), window, sinks,
-                                              out_ptr, stride, _ptr(logits_out), _ptr(hidden_out), ok_ptr, cache.on_current_device()))
+        out_ptr = _check("tokens_out", tokens_out, torch.int32, (B,), False)
+        stride = int(tokens_out.stride(0))
+    logits_ptr = None if logits_out is None else _check("logits_out", logits_out, torch.float32, (B, ctx.cfg.vocab))
+    hidden_ptr = None if hidden_out is None else _check("hidden_out", hidden_out, torch_dtype(ctx.cfg.dtype), (B, ctx.cfg.hidden))
+    ok_ptr = None if ok is None else _check("ok", ok, torch.int32, (B,))
+    ctx.check(ctx.lib.beagle_draft_step_pages(ctx.handle, cache.ref, B, _host_i32(seq_slot), in_ptr, int(bool(concat)), window, sinks,
+                                              out_ptr, stride, logits_ptr, hidden_ptr, ok_ptr, cache.on_current_device()))
 
 
 # ---- attention over whole sequences with a window and sinks -------------------------------------

@@ -221,3 +221,35 @@ def test_prefill_pages_wants_one_length_per_slot(new_len):
     from paper_2505_24544_b200 import binding as b
     with pytest.raises(ValueError, match="new_len"):
         b.beagle_prefill_pages(RefusingHead(), RefusingHead(), [0, 1], new_len, None)
+
+
+def test_draft_step_pages_checks_its_tensors(monkeypatch):
+    """Type, shape, layout and device of every tensor of the paged step (host tensors stand for device ones where the device is
+    not what is wrong)."""
+    torch = pytest.importorskip("torch")
+    from paper_2505_24544_b200 import binding as b
+    i32, f32, bf16 = torch.int32, torch.float32, torch.bfloat16
+    good = dict(tokens_in=((2,), i32), tokens_out=((2,), i32), logits_out=((2, 4096), f32), hidden_out=((2, 512), bf16), ok=((2,), i32))
+    bad = dict(tokens_in=[((2,), torch.int64), ((3,), i32), ((2, 1), i32)], tokens_out=[((2,), f32), ((1,), i32), ((2, 1), i32)],
+               logits_out=[((2, 4096), bf16), ((2, 4095), f32), ((1, 4096), f32)], hidden_out=[((2, 512), f32), ((2, 511), bf16), ((3, 512), bf16)],
+               ok=[((2,), torch.int64), ((1,), i32)])
+
+    def call(**kw):
+        x = {n: torch.zeros(s, dtype=t) for n, (s, t) in good.items()}
+        x.update(kw)
+        b.beagle_draft_step_pages(RefusingHead(), RefusingHead(), [0, 1], x["tokens_in"], True, x["tokens_out"], x["logits_out"], x["hidden_out"], 0, 0, x["ok"])
+    with pytest.raises(ValueError, match="device"):
+        call()                                                               # host memory
+    check = b._check
+    monkeypatch.setattr(b, "_check", lambda name, t, dtype, shape, dense=True:
+                        check(name, t, dtype, shape, dense) if t.dtype != dtype or t.shape != shape or (dense and not t.is_contiguous()) else t.data_ptr())
+    with pytest.raises(AssertionError, match="beagle_draft_step_pages was reached"):
+        call()                                                               # nothing wrong: on to the library
+    for name, cases in bad.items():
+        for shape, dtype in cases:
+            with pytest.raises(ValueError, match=name):
+                call(**{name: torch.zeros(shape, dtype=dtype)})
+    for name in ("logits_out", "hidden_out"):
+        shape, dtype = good[name]
+        with pytest.raises(ValueError, match=name):
+            call(**{name: torch.zeros(shape[1], shape[0], dtype=dtype).t()})
