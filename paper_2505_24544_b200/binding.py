@@ -545,6 +545,16 @@ def _check(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...
     raise ValueError(f"{name}: tensor must be contiguous")
 
 
+def _scratch(ws: torch.Tensor) -> Tuple[int, int]:
+    """Address and bytes of a caller's workspace, after checking that it is one run of memory on the current device."""
+    device = ws.get_device()
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise ValueError("ws: must be on the current CUDA device")
+    if not ws.is_contiguous():
+        raise ValueError("ws: tensor must be contiguous")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def _row_stride(name: str, t: torch.Tensor, lead: int) -> int:
     """Elements between consecutive rows of a tensor whose last two dimensions ([heads, head_dim]) are dense and whose first
     `lead` dimensions count rows at one distance (a dense tensor, or a slice of a fused projection)."""
@@ -684,7 +694,7 @@ def beagle_paged_attn(cache: PagedCache, slots: Sequence[int], q: torch.Tensor, 
     need = beagle_paged_attn_workspace_bytes(cache, hq, window, sinks)
     if ws is None and need > 0:
         ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-    wp, wn = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+    wp, wn = (None, 0) if ws is None else _scratch(ws)
     _pages_ok(cache.lib.beagle_paged_attn(cache.ref, B, _host_i32(slots), hq, qp, _row_stride("q", q, 1), window, sinks, op, lp, wp, wn, stream),
               "beagle_paged_attn")
 
@@ -776,8 +786,8 @@ def beagle_window_attn_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
         n = C.c_size_t()
         _pages_ok(lib.beagle_window_attn_workspace_bytes(C.byref(w), C.byref(n)), "beagle_window_attn_workspace_bytes")
         ws = torch.empty(n.value, dtype=torch.uint8, device=q.device)
-    _pages_ok(lib.beagle_window_attn_backward(C.byref(w), op, lp, *ptr["dout"], *ptr["dq"], *ptr["dk"], *ptr["dv"], ws.data_ptr(),
-                                              ws.numel() * ws.element_size(), stream), "beagle_window_attn_backward")
+    _pages_ok(lib.beagle_window_attn_backward(C.byref(w), op, lp, *ptr["dout"], *ptr["dq"], *ptr["dk"], *ptr["dv"], *_scratch(ws), stream),
+              "beagle_window_attn_backward")
 
 
 # ---- convenience wrapper -----------------------------------------------------------------------

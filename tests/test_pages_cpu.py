@@ -253,3 +253,20 @@ def test_draft_step_pages_checks_its_tensors(monkeypatch):
         shape, dtype = good[name]
         with pytest.raises(ValueError, match=name):
             call(**{name: torch.zeros(shape[1], shape[0], dtype=dtype).t()})
+
+
+def test_paged_attn_checks_its_workspace(monkeypatch):
+    """A workspace in host memory, or with gaps, is refused like any other tensor."""
+    torch = pytest.importorskip("torch")
+    from paper_2505_24544_b200 import binding as b
+    cache, q = RefusingHead(), torch.zeros(1, 4, 64, dtype=torch.bfloat16)
+    cache.struct, cache.k, cache.attn_ws_bytes, cache.on_current_device = b.BeaglePages(head_dim=64), q, {(4, 0, 0): 64}, lambda: 0
+    monkeypatch.setattr(b, "_check", lambda name, t, *_: t.data_ptr())           # q and out stand for tensors on the device
+    with pytest.raises(ValueError, match="ws.*device"):
+        b.beagle_paged_attn(cache, [0], q, q, ws=torch.zeros(64, dtype=torch.uint8))
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    with pytest.raises(ValueError, match="ws.*contiguous"):
+        b.beagle_paged_attn(cache, [0], q, q, ws=torch.zeros(64, 2, dtype=torch.uint8)[:, 0])
+    with pytest.raises(AssertionError, match="beagle_paged_attn was reached"):
+        b.beagle_paged_attn(cache, [0], q, q, ws=torch.zeros(64, dtype=torch.uint8))

@@ -88,3 +88,28 @@ def test_workspace_bytes(lib):
     assert size(window=2, sinks=3, **short) == stats + 2 * 2 * (1 + 1) * 3 * 2 * 128 * 4
     assert size(window=2, sinks=1000, **short) == stats + 2 * 2 * (1 + 1) * 130 * 2 * 128 * 4
     assert size(dtype=0, head_dim=32, **short) == -(-stats // 256) * 256 + 135 * 4 * 2 * 32 * 4
+
+
+def test_backward_checks_its_workspace(monkeypatch):
+    """A workspace in host memory, or with gaps, is refused like any other tensor."""
+    torch = pytest.importorskip("torch")
+    from paper_2505_24544_b200 import binding as b
+
+    class Library:
+        def beagle_window_attn_backward(self, *_):
+            raise AssertionError("the library was reached")
+    q, lse = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, 2)
+    monkeypatch.setattr(b, "_check", lambda name, t, *_: t.data_ptr())           # the other tensors stand for ones on the device
+    monkeypatch.setattr(b, "_stream", lambda: 0)
+    monkeypatch.setattr(b, "load_library", Library)
+
+    def call(ws):
+        b.beagle_window_attn_backward(q, q, q, q, lse, q, [3], [3], q, q, q, ws=ws)
+    with pytest.raises(ValueError, match="ws.*device"):
+        call(torch.zeros(64, dtype=torch.uint8))
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    with pytest.raises(ValueError, match="ws.*contiguous"):
+        call(torch.zeros(64, 2, dtype=torch.uint8)[:, 0])
+    with pytest.raises(AssertionError, match="the library was reached"):
+        call(torch.zeros(64, dtype=torch.uint8))
