@@ -426,3 +426,15 @@ def test_every_group_size_off_the_tensor_cores(dtype, dh, group, ps, window, sin
     cache = filled([3000, 1, 0, 257, 64, 1100], ps, 2, dh, dtype, 17)
     q = (torch.randn(6, 2 * group, dh, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda") * 2).to(DT[dtype])
     check_attn(cache, [5, 0, 1, 2, 3, 4], q, window, sinks, dtype)
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 256), ("fp32", 64)])
+@pytest.mark.parametrize("width", [2, 200])
+def test_an_empty_slot_gives_zero_and_minus_infinity(dtype, dh, width):
+    """Whether pairs are divided whole or cut into runs."""
+    cache = filled([0, 40, 0], 32, 2, dh, dtype, 6, width=width)
+    q = torch.ones(3, 4, dh, dtype=DT[dtype], device="cuda")
+    out, lse = torch.full_like(q, 9.0), torch.full((3, 4), 9.0, device="cuda")
+    b.beagle_paged_attn(cache, [0, 1, 2], q, out, lse)
+    assert bool(torch.isneginf(lse[[0, 2]]).all()) and bool(torch.isfinite(lse[1]).all())
+    assert bool((out[[0, 2]] == 0).all()) and bool(torch.isfinite(out[1]).all())

@@ -308,3 +308,42 @@ def test_shared_key_tiles(hq, hkv, dh, window, sinks):
     again = run(*x, q_len, kv_len, window, sinks, False)
     for name in first:
         assert torch.equal(first[name], again[name]), name
+
+
+# Ragged, with empty sequences, queries that see nothing and keys that nobody sees between the others.
+MANY_Q = [400, 0, 130, 700, 1, 257, 520, 90, 300, 64, 129, 200]
+MANY_KV = [400, 70, 130, 640, 1, 300, 720, 0, 200, 64, 40, 200]
+
+
+def tiles(lengths, rows):
+    return sum(-(-n // rows) for n in lengths)
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(16, 16, 128), (16, 16, 64), (32, 16, 64), (32, 4, 128)])
+@pytest.mark.parametrize("window,sinks,strict", [(0, 0, False), (64, 4, True), (300, 0, True), (300, 140, False)])
+def test_more_items_than_sms(hq, hkv, dh, window, sinks, strict):
+    """Every CTA of the backward's query side walks three items or more, its pipeline running on across them, and so does the key side
+    where its items are short (a window, at most two query heads a K/V head); elsewhere that is a CTA an item, several waves of them."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert tiles(MANY_Q, 128) * hq >= 3 * sms and (hkv < 16 or tiles(MANY_KV, 128) * hkv >= 3 * sms)
+    x = inputs(MANY_Q, MANY_KV, hq, hkv, dh, "bf16", 31)
+    first = run(*x, MANY_Q, MANY_KV, window, sinks, strict)
+    compare(first, reference(*x, MANY_Q, MANY_KV, window, sinks, strict, "bf16"))
+    again = run(*x, MANY_Q, MANY_KV, window, sinks, strict)
+    for name in first:
+        assert torch.equal(first[name], again[name]), name
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 8), (8, 2)])
+@pytest.mark.parametrize("dh", [16, 32, 64, 128])
+@pytest.mark.parametrize("window,sinks,strict", [(0, 0, False), (100, 70, True)])
+def test_large_calls_fp32(hq, hkv, dh, window, sinks, strict):
+    """Enough rows for the fp32 kernels' tiles of 64 (the calls of the other tests take 32), at every width."""
+    q_len, kv_len = [520, 0, 700, 65], [600, 30, 640, 100]
+    assert min(tiles(q_len, 64), tiles(kv_len, 64)) * hq >= 148
+    x = inputs(q_len, kv_len, hq, hkv, dh, "fp32", 37)
+    first = run(*x, q_len, kv_len, window, sinks, strict)
+    compare(first, reference(*x, q_len, kv_len, window, sinks, strict, "fp32"))
+    again = run(*x, q_len, kv_len, window, sinks, strict)
+    for name in first:
+        assert torch.equal(first[name], again[name]), name
