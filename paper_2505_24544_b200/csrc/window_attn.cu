@@ -10,11 +10,13 @@ namespace {
 
 struct Layout {
     size_t stats, part, group, split, total;
-    int stat_rows, sink_rows, sink_tiles, sink_segs, splits;
+    int stat_rows, sink_rows, splits;
 };
 
 constexpr int kMaxSinks = 1024;          // with a window
 constexpr long long kMaxRows = 1 << 27;
+constexpr int kMaxSegs = 64;             // segments of the queries past the sinks' band
+constexpr size_t kSmallParts = 4 << 20;
 
 // Everything that does not depend on device pointers.  Fills `s` and the shape part of `a`; rows of queries and keys in total.
 beagle_status check(const beagle_window_attn* w, WinArgs& a, WinSeqs& s, long long& q_rows, long long& k_rows) {
@@ -52,7 +54,8 @@ beagle_status check(const beagle_window_attn* w, WinArgs& a, WinSeqs& s, long lo
     return BEAGLE_OK;
 }
 
-Layout layout(const beagle_window_attn* w, const WinArgs& a, const WinSeqs& s, long long k_rows) {
+// Also fills the sequences' segments and their places in the sinks' partials.
+Layout layout(const beagle_window_attn* w, const WinArgs& a, WinSeqs& s, long long k_rows) {
     Layout L;
     memset(&L, 0, sizeof(L));
     long long rows = kStatPad;           // a tile that starts inside the last sequence may read past its padded end
@@ -78,26 +81,30 @@ Layout layout(const beagle_window_attn* w, const WinArgs& a, const WinSeqs& s, l
         end = end < 0 ? 0 : end > s.q_len[b] ? s.q_len[b] : end;
         return s.q_len[b] == end ? 0 : (s.q_len[b] - end + kQTile) / kQTile * (fp32 ? 1 : a.G);        // (the fp32 kernels: a CTA per head)
     };
+    auto rows_of = [&](int b) { return a.sinks < s.kv_len[b] ? a.sinks : s.kv_len[b]; };
     long long band = ((long long)a.window + 2 * kKTile) / kQTile * (fp32 ? 1 : a.G);
-    const int rows_s = a.sinks < most_kv ? a.sinks : most_kv, tiles_s = (rows_s + kKTile - 1) / kKTile;
     L.splits = 1;
     if (band < (fp32 ? 2 : 8)) band = fp32 ? 2 : 8;
     if (!fp32) {
         // Few key tiles with many jobs each: several CTAs share a tile's jobs, with as few jobs each (two at least) as leave every
         // CTA, those of the sinks' segments among them, an SM of its own.  (Backward, 8 heads of 128 over one K/V head, 1000 queries:
         // 127 us unshared, 52 so; 8 x 200, 16 heads over 2, window 9: 57 and 45; below eight jobs a tile the join costs what it saves.)
-        long long tiles = 0, jobs = 0, late = 0;
+        long long tiles = 0, jobs = 0, late[kMaxCallBatch];
         for (int b = 0; b < a.batch; ++b) {
             const long long span = (long long)a.window + 2 * kKTile < s.q_len[b] ? (long long)a.window + 2 * kKTile : s.q_len[b];
             const long long n = (span + kQTile - 1) / kQTile * a.G;
             jobs = n > jobs ? n : jobs;
-            late = past(b) > late ? past(b) : late;
+            late[b] = past(b);
             tiles += (s.kv_len[b] + kKTile - 1) / kKTile;
         }
         const long long units = tiles * a.Hkv, sms = device_sm_count();
         if (units * 2 <= sms && jobs >= 8) {
             long long each = 2;
-            auto ctas = [&]() { return units * ((jobs + each - 1) / each) + (late + each - 1) / each * tiles_s * a.Hkv * a.batch; };
+            auto ctas = [&]() {
+                long long n = units * ((jobs + each - 1) / each);
+                for (int b = 0; b < a.batch; ++b) n += (late[b] + each - 1) / each * ((rows_of(b) + kKTile - 1) / kKTile) * a.Hkv;
+                return n;
+            };
             while (each < jobs && ctas() > sms) ++each;
             const long long n = (jobs + each - 1) / each;
             L.splits = (int)(n < 16 ? n : 16);
@@ -110,17 +117,24 @@ Layout layout(const beagle_window_attn* w, const WinArgs& a, const WinSeqs& s, l
         }
     }
     // Segments of the queries past the band of the sinks' key tiles, about as long as a band CTA's work (at least eight jobs where
-    // the tiles are not shared, fp32 two), as many as the longest sequence needs.
-    int segs = 0;
+    // the tiles are not shared, fp32 two).  A sequence takes as many as it needs itself: one long sequence among short ones, or more sinks
+    // than the others have keys, costs only its own partials.
+    const long long heads = fp32 ? a.Hq : a.Hkv;
+    long long parts = 0;
+    int most_segs = 0, most_rows = a.sinks < most_kv ? a.sinks : most_kv;
     for (int b = 0; b < a.batch; ++b) {
-        const int need = (int)((past(b) + band - 1) / band);
-        segs = need > segs ? need : segs;
+        const long long need = (past(b) + band - 1) / band;
+        s.segs[b] = (int)(need < kMaxSegs ? need : kMaxSegs);
+        s.part[b] = parts;
+        if (s.segs[b] == 0) continue;
+        parts += heads * (1 + s.segs[b]) * rows_of(b);
+        most_segs = s.segs[b] > most_segs ? s.segs[b] : most_segs;
+        L.sink_rows = rows_of(b) > L.sink_rows ? rows_of(b) : L.sink_rows;
     }
-    L.sink_segs = segs > 64 ? 64 : segs;
-    if (L.sink_segs > 0) {
-        L.sink_rows = rows_s;
-        L.sink_tiles = tiles_s;
-        off += (size_t)a.batch * (fp32 ? a.Hq : a.Hkv) * (1 + L.sink_segs) * rows_s * 2 * d * sizeof(float);
+    if (parts > 0) {
+        // (Up to 4 MB the size goes by the longest sequence alone, so that one workspace does for every mix of lengths below it.)
+        const size_t row = 2 * d * sizeof(float), even = (size_t)a.batch * heads * (1 + most_segs) * most_rows * row, own = parts * row;
+        off += own > kSmallParts ? own : even < kSmallParts ? even : kSmallParts;
     }
     L.total = (off + 255) / 256 * 256;
     return L;
@@ -193,7 +207,7 @@ beagle_status beagle_window_attn_backward(const beagle_window_attn* w, const voi
     a.group_part = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.group);
     a.split_part = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + L.split);
     a.splits = L.splits;
-    a.stat_rows = L.stat_rows; a.sink_rows = L.sink_rows; a.sink_tiles = L.sink_tiles; a.sink_segs = L.sink_segs;
+    a.stat_rows = L.stat_rows; a.sink_rows = L.sink_rows;
     const cudaStream_t cs = static_cast<cudaStream_t>(stream);
     const int rc = w->dtype == BEAGLE_BF16 ? window_bwd_bf16(a, s, w->head_dim, q_rows, k_rows, cs) : window_bwd_fp32(a, s, w->head_dim, cs);
     return rc >= 0 && cudaGetLastError() == cudaSuccess ? BEAGLE_OK : BEAGLE_ERR_CUDA;

@@ -507,7 +507,7 @@ __device__ __forceinline__ int band_end(int k0, int kv_len, int q_len, int shift
 }
 
 // One item: 128 keys of one (sequence, K/V head) and the queries of its band, or a segment of the queries past the band.
-// Per sequence the grid's list has first its key tiles (bands), then, for each of the sink_tiles, sink_segs segments.
+// Per sequence the grid's list has first the segments of each of its sinks' key tiles, then its key tiles (bands).
 struct KItem {
     int b, kvh, k0, q_len, kv_len, shift, k_row, seg, band, n;      // seg: -1 = band; band: first query past it; n: jobs
     int j0, split;                       // first job; which of the tile's splits
@@ -522,10 +522,10 @@ struct KItem {
         q_len = s.q_len[b];
         kv_len = s.kv_len[b];
         shift = kv_len - q_len - a.strict;
-        const int parts = a.sink_tiles * a.sink_segs;            // the sinks' segments first, then the bands of the tiles
+        const int segs = s.segs[b], parts = (min(a.sinks, kv_len) + kKTile - 1) / kKTile * segs;
         const bool sink_part = item < parts;
-        seg = sink_part ? item % a.sink_segs : -1;
-        const int tile = sink_part ? item / a.sink_segs : (item - parts) / splits;
+        seg = sink_part ? item % segs : -1;
+        const int tile = sink_part ? item / segs : (item - parts) / splits;
         split = SPLIT && !sink_part ? item - parts - tile * splits : 0;
         k0 = tile * kKTile;
         k_row = s.k_start[b] + k0;
@@ -537,11 +537,11 @@ struct KItem {
             const int total = w.n * a.G;
             j0 = total * split / splits;
             n = total * (split + 1) / splits - j0;
-        } else if (k0 < min(a.sinks, kv_len)) {
+        } else {
             w.init(band, q_len);
             const int total = w.n * a.G;
-            j0 = (int)((long long)total * seg / a.sink_segs);
-            n = (int)((long long)total * (seg + 1) / a.sink_segs) - j0;
+            j0 = (int)((long long)total * seg / segs);
+            n = (int)((long long)total * (seg + 1) / segs) - j0;
         }
     }
 };
@@ -848,7 +848,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
             const int my_key = x.k0 + q * 32 + lane;
             // rows that several items share go to the joins, in fp32
             const bool sink_item = x.seg >= 0, in_splits = SPLIT && !sink_item;
-            const bool to_part = in_splits ? my_key < x.kv_len : a.sink_segs > 0 && my_key < min(a.sinks, x.kv_len);
+            const bool to_part = in_splits ? my_key < x.kv_len : seqs.segs[x.b] > 0 && my_key < min(a.sinks, x.kv_len);
             const size_t row = (size_t)(x.k_row + q * 32 + lane);
             const int col = half * (DH / 2);                     // this thread's half of the columns
             const bool write = my_key < x.kv_len && !sink_item && !to_part;
@@ -858,7 +858,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_bwd_kv_kernel(const __grid
                 const float f = m == 0 ? sv : sk;
                 if (__any_sync(0xffffffffu, to_part)) {
                     float* part = in_splits ? a.split_part + (((size_t)key_unit(x.b, x.k0 / kKTile, x.kvh, a, seqs) * a.splits + x.split) * kKTile + (my_key - x.k0)) * 2 * DH
-                                            : a.sink_part + ((((size_t)x.b * a.Hkv + x.kvh) * (1 + a.sink_segs) + (1 + x.seg)) * a.sink_rows + my_key) * 2 * DH;
+                                            : a.sink_part + sink_row(a, seqs, x.b, x.kvh, 1 + x.seg, my_key) * 2 * DH;
                     part += m * DH + col;
 #pragma unroll 1
                     for (int c = 0; c < DH / 2; c += 16) {
@@ -907,8 +907,8 @@ __global__ void __launch_bounds__(256) window_split_join_kernel(const __grid_con
             const float4 y = p[((size_t)s * kKTile + r) * kVecs + c / 4];
             x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
         }
-        if (a.sink_segs > 0 && key < a.sinks) {
-            *reinterpret_cast<float4*>(a.sink_part + (((size_t)b * a.Hkv + kvh) * (1 + a.sink_segs) * a.sink_rows + key) * 2 * DH + c) = x;
+        if (seqs.segs[b] > 0 && key < a.sinks) {
+            *reinterpret_cast<float4*>(a.sink_part + sink_row(a, seqs, b, kvh, 0, key) * 2 * DH + c) = x;
         } else {
             const size_t row = (size_t)(seqs.k_start[b] + key);
             bf16* dst = c < DH ? static_cast<bf16*>(a.dv) + row * a.dv_stride + c : static_cast<bf16*>(a.dk) + row * a.dk_stride + c - DH;
@@ -922,16 +922,17 @@ template <int DH>
 __global__ void __launch_bounds__(2 * DH) window_sink_join_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
     const int key = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
     const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
-    if (key >= kv_len) return;
+    const int segs = seqs.segs[b], rows = min(a.sinks, kv_len);
+    if (segs == 0 || key >= rows) return;
     const int k0 = key / kKTile * kKTile;
     QueryWalk w;
     w.init(band_end(k0, kv_len, q_len, shift, a.window), q_len);
     const int total = w.n * a.G;
-    const size_t step = (size_t)a.sink_rows * 2 * DH;
-    const float* p = a.sink_part + (((size_t)b * a.Hkv + kvh) * (1 + a.sink_segs) * a.sink_rows + key) * 2 * DH + threadIdx.x;
+    const size_t step = (size_t)rows * 2 * DH;
+    const float* p = a.sink_part + sink_row(a, seqs, b, kvh, 0, key) * 2 * DH + threadIdx.x;
     float x = *p;
-    for (int s = 0; s < a.sink_segs; ++s)
-        if ((int)((long long)total * (s + 1) / a.sink_segs) > (int)((long long)total * s / a.sink_segs)) x += p[(1 + s) * step];
+    for (int s = 0; s < segs; ++s)
+        if ((int)((long long)total * (s + 1) / segs) > (int)((long long)total * s / segs)) x += p[(1 + s) * step];
     const int c = threadIdx.x % DH;
     const size_t row = (size_t)(seqs.k_start[b] + key);
     bf16* dst = threadIdx.x < DH ? static_cast<bf16*>(a.dv) + row * a.dv_stride : static_cast<bf16*>(a.dk) + row * a.dk_stride;
@@ -974,7 +975,12 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
     if (hk) {
         WinSeqs t = s;                   // items of the key side: band tiles and sink segments
         t.item[0] = 0;
-        for (int b = 0; b < a.batch; ++b) t.item[b + 1] = t.item[b] + (s.kv_len[b] + kKTile - 1) / kKTile * a.splits + a.sink_tiles * a.sink_segs;
+        int tiles = 0;
+        for (int b = 0; b < a.batch; ++b) {
+            const int n = (s.kv_len[b] + kKTile - 1) / kKTile, sinks = ((a.sinks < s.kv_len[b] ? a.sinks : s.kv_len[b]) + kKTile - 1) / kKTile;
+            tiles += n;
+            t.item[b + 1] = t.item[b] + n * a.splits + sinks * s.segs[b];
+        }
         if (t.item[a.batch] > 0) {
             const long long items = (long long)t.item[a.batch] * a.Hkv;
             if (items > 0x3fffffff) return -1;
@@ -987,11 +993,10 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
                 <<<(unsigned)(share ? sms : items), kThreads, SK::kBytes, stream>>>(mq, mdo, mk, mv, mdk, mdv, a, t);
             ++launched;
             if (a.splits > 1) {
-                const int tiles = (t.item[a.batch] - a.batch * a.sink_tiles * a.sink_segs) / a.splits;
                 window_split_join_kernel<DH><<<dim3(kKTile / 16, a.Hkv, tiles), 256, 0, stream>>>(a, t);
                 ++launched;
             }
-            if (a.sink_segs > 0) {
+            if (a.sink_rows > 0) {
                 window_sink_join_kernel<DH><<<dim3(a.sink_rows, a.Hkv, a.batch), 2 * DH, 0, stream>>>(a, t);
                 ++launched;
             }

@@ -321,8 +321,8 @@ __global__ void __launch_bounds__(kThreads) window_bwd_q_fp32_kernel(const __gri
 }
 
 // One CTA = R keys of one (sequence, query head).  What lies past the band of a sink tile is cut into segments, CTAs of their own that
-// come first; the rows of sinks then go to a.sink_part, fp32 [sequence][Hq][1 + segments][sink_rows][2][DH] (the band's part, then the
-// segments'), dV then dK.  a.group_part (where heads share keys): [kv rows][Hq][2][DH].  The last launches add both up in order.
+// come first; the rows of that sequence's sinks then go to a.sink_part (the band's part, then the segments').  a.group_part (where heads
+// share keys): [kv rows][Hq][2][DH], dV then dK.  The last launches add both up in order.
 template <int DH, int R>
 __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs) {
     extern __shared__ __align__(16) float sm[];
@@ -332,20 +332,19 @@ __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __gr
     int tile;
     const int b = win_find(seqs.item, a.batch, blockIdx.x, tile);
     const int q_len = seqs.q_len[b], kv_len = seqs.kv_len[b], shift = kv_len - q_len - a.strict;
-    const int parts = (a.sink_rows + R - 1) / R * a.sink_segs;
-    const int seg = tile < parts ? tile % a.sink_segs : -1;
-    const int k0 = (seg >= 0 ? tile / a.sink_segs : tile - parts) * R, h = blockIdx.y, kvh = h / a.G;
-    if (seg >= 0 && k0 >= kv_len) return;
+    const int segs = seqs.segs[b], parts = (min(a.sinks, kv_len) + R - 1) / R * segs;
+    const int seg = tile < parts ? tile % segs : -1;
+    const int k0 = (seg >= 0 ? tile / segs : tile - parts) * R, h = blockIdx.y, kvh = h / a.G;
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     load_tile<DH, R>(K, static_cast<const float*>(a.k) + (size_t)seqs.k_start[b] * a.k_stride, a.k_stride, k0, kv_len, (size_t)kvh * DH);
     load_tile<DH, R>(V, static_cast<const float*>(a.v) + (size_t)seqs.k_start[b] * a.v_stride, a.v_stride, k0, kv_len, (size_t)kvh * DH);
     const int band = max(0, min(q_len, min(k0 + R, kv_len) - 1 - shift + a.window));      // the first query past the band
-    int from = max(0, k0 - shift), to = k0 < a.sinks && a.sink_segs == 0 ? q_len : band;
+    int from = max(0, k0 - shift), to = k0 < a.sinks && segs == 0 ? q_len : band;
     if (seg >= 0) {
         from = max(from, band);
         const int all = from < q_len ? (q_len - from + kT - 1) / kT : 0;
-        to = min(q_len, from + (int)((long long)all * (seg + 1) / a.sink_segs) * kT);
-        from += (int)((long long)all * seg / a.sink_segs) * kT;
+        to = min(q_len, from + (int)((long long)all * (seg + 1) / segs) * kT);
+        from += (int)((long long)all * seg / segs) * kT;
     }
     const float* stats = a.stats + (size_t)h * 2 * a.stat_rows + stat_row0(seqs, b);
     float dk[RT][DH / 16], dv[RT][DH / 16];
@@ -398,9 +397,9 @@ __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __gr
         const int key = k0 + RT * ty + r;
         if (key >= kv_len) continue;
         const size_t row = (size_t)(seqs.k_start[b] + key);
-        const bool part = a.sink_segs > 0 && key < a.sinks;
+        const bool part = segs > 0 && key < a.sinks;
         if (seg >= 0 && !part) continue;
-        float* to_v = part ? a.sink_part + ((((size_t)b * a.Hq + h) * (1 + a.sink_segs) + (1 + seg)) * a.sink_rows + key) * 2 * DH
+        float* to_v = part ? a.sink_part + sink_row(a, seqs, b, h, 1 + seg, key) * 2 * DH
                     : a.G > 1 ? a.group_part + (row * a.Hq + h) * 2 * DH : static_cast<float*>(a.dv) + row * a.dv_stride + (size_t)kvh * DH;
         float* to_k = part || a.G > 1 ? to_v + DH : static_cast<float*>(a.dk) + row * a.dk_stride + (size_t)kvh * DH;
         set_cols<DH>(to_v, tx, dv[r], 1.f);
@@ -427,10 +426,11 @@ __global__ void __launch_bounds__(256) window_group_join_fp32_kernel(const __gri
 // dK, dV of the sinks: head after head of the group, the band's part and the segments' of each.  blockIdx = (row, K/V head, sequence).
 __global__ void __launch_bounds__(256) window_sink_join_fp32_kernel(const __grid_constant__ WinArgs a, const __grid_constant__ WinSeqs seqs, int DH) {
     const int key = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z, c = threadIdx.x;
-    if (key >= seqs.kv_len[b] || c >= 2 * DH) return;
-    const float* p = a.sink_part + (((size_t)b * a.Hq + (size_t)kvh * a.G) * (1 + a.sink_segs) * a.sink_rows + key) * 2 * DH + c;
+    const int segs = seqs.segs[b], rows = min(a.sinks, seqs.kv_len[b]);
+    if (segs == 0 || key >= rows || c >= 2 * DH) return;
+    const float* p = a.sink_part + sink_row(a, seqs, b, kvh * a.G, 0, key) * 2 * DH + c;
     float x = 0.f;
-    for (int i = 0; i < a.G * (1 + a.sink_segs); ++i) x += p[(size_t)i * a.sink_rows * 2 * DH];
+    for (int i = 0; i < a.G * (1 + segs); ++i) x += p[(size_t)i * rows * 2 * DH];
     const size_t row = (size_t)(seqs.k_start[b] + key);
     if (c < DH) static_cast<float*>(a.dv)[row * a.dv_stride + (size_t)kvh * DH + c] = x;
     else static_cast<float*>(a.dk)[row * a.dk_stride + (size_t)kvh * DH + c - DH] = x;
@@ -472,8 +472,10 @@ int bwd_kv_rows(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
     static PerDeviceOnce once;
     if (!raise_limit(window_bwd_kv_fp32_kernel<DH, R>, once, SM())) return -1;
     retile(s, a.batch, s.kv_len, R);
-    const int parts = (a.sink_rows + R - 1) / R * a.sink_segs;
-    for (int b = 1; b <= a.batch; ++b) s.item[b] += b * parts;
+    for (int b = 0, parts = 0; b < a.batch; ++b) {
+        parts += ((a.sinks < s.kv_len[b] ? a.sinks : s.kv_len[b]) + R - 1) / R * s.segs[b];
+        s.item[b + 1] += parts;
+    }
     window_bwd_kv_fp32_kernel<DH, R><<<dim3(s.item[a.batch], a.Hq), kThreads, SM::kBytes, stream>>>(a, s);
     return 1;
 }
@@ -500,7 +502,7 @@ int bwd(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
             window_group_join_fp32_kernel<<<dim3((unsigned)((n + 255) / 256 < 148 * 8 ? (n + 255) / 256 : 148 * 8)), 256, 0, stream>>>(a, DH, rows);
             ++launched;
         }
-        if (a.sink_segs > 0) {           // (over what the join of the groups left in the sinks' rows)
+        if (a.sink_rows > 0) {           // (over what the join of the groups left in the sinks' rows)
             window_sink_join_fp32_kernel<<<dim3(a.sink_rows, a.Hkv, a.batch), 256, 0, stream>>>(a, s, DH);
             ++launched;
         }

@@ -113,3 +113,27 @@ def test_backward_checks_its_workspace(monkeypatch):
         call(torch.zeros(64, 2, dtype=torch.uint8)[:, 0])
     with pytest.raises(AssertionError, match="the library was reached"):
         call(torch.zeros(64, dtype=torch.uint8))
+
+
+def test_workspace_of_a_long_sequence_among_short_ones(lib):
+    """Partials of the sinks are kept for the sequences that have queries past the band, in their own number of segments and rows: one
+    sequence of 32768 among 63 of 200 (window 512, 1024 sinks) takes what it takes alone."""
+    def size(*lengths, **kw):
+        n = C.c_size_t()
+        shape = dict(window=512, sinks=1024, n_q_heads=8, n_kv_heads=8, head_dim=128, q_stride=1024, k_stride=1024, v_stride=1024)
+        shape.update(kw)
+        assert lib.beagle_window_attn_workspace_bytes(C.byref(attn(q_len_host=lengths, kv_len_host=lengths, **shape)), C.byref(n)) == OK
+        return n.value
+
+    def stats(*lengths):
+        return 8 * (sum(-(-n // 128) * 128 for n in lengths) + 128) * 8
+    long, short = (32768,), (200,) * 63
+    parts = 8 * (1 + 32) * 1024 * 2 * 128 * 4                    # 252 jobs past the band, eight a segment
+    assert size(*long) == stats(*long) + parts
+    assert size(*short) == stats(*short)
+    assert size(*long, *short) == size(*short, *long) == stats(*long, *short) + parts
+    # a few rows past the band in every sequence: as many segments as each needs, as many rows as it has
+    mixed = (32768,) + (700,) * 63
+    assert size(*mixed) == stats(*mixed) + parts + 63 * 8 * 2 * 700 * 2 * 128 * 4
+    fp32 = dict(dtype=0, n_q_heads=8)
+    assert size(*long, *short, **fp32) - size(*long, **fp32) == stats(*long, *short) - stats(*long)

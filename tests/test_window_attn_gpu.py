@@ -347,3 +347,17 @@ def test_large_calls_fp32(hq, hkv, dh, window, sinks, strict):
     again = run(*x, q_len, kv_len, window, sinks, strict)
     for name in first:
         assert torch.equal(first[name], again[name]), name
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dh", [("bf16", 4, 4, 128), ("bf16", 16, 16, 64), ("bf16", 8, 1, 64), ("fp32", 4, 2, 64), ("fp32", 12, 12, 32)])
+@pytest.mark.parametrize("window,sinks", [(30, 140), (64, 4), (100, 600)])
+def test_sinks_of_ragged_sequences(dtype, hq, hkv, dh, window, sinks):
+    """Sequences with many segments of queries past the sinks' band, with one and with none side by side, some with fewer keys than
+    there are sinks: each keeps its own partials."""
+    q_len, kv_len = [40, 1400, 0, 131, 500, 1, 90, 300], [40, 1400, 200, 131, 90, 700, 90, 460]
+    x = inputs(q_len, kv_len, hq, hkv, dh, dtype, 41)
+    first = run(*x, q_len, kv_len, window, sinks, False)
+    compare(first, reference(*x, q_len, kv_len, window, sinks, False, dtype))
+    again = run(*x, q_len, kv_len, window, sinks, False)
+    for name in first:
+        assert torch.equal(first[name], again[name]), name
