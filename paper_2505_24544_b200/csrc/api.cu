@@ -1106,7 +1106,7 @@ beagle_status beagle_prefill_pages(beagle_ctx* ctx, const beagle_pages* pages, i
         for (int m = 0; m < 2; ++m) {                       // K = H W_k^T, V = H W_v^T as dense rows; kernels by row count as in prefill_kv
             const void* W = m == 0 ? ctx->w.w_k : ctx->w.w_v;
             char* out = m == 0 ? K : V;
-            if (total <= (ctx->tc != nullptr ? kServeTcMinBatch : 16)) {
+            if (small) {
                 GemvArgs a;
                 memset(&a, 0, sizeof(a));
                 a.W = W; a.N = ctx->kd; a.K = c.hidden; a.X = hidden_dev; a.ldx = c.hidden; a.B = (int)total; a.out = out; a.ldo = ctx->kd;

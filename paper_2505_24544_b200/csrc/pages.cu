@@ -14,6 +14,7 @@
 #include <cstring>
 
 #include "pages.h"
+#include "tensor_map.h"
 
 using namespace beagle;
 
@@ -487,7 +488,8 @@ void launch_move(const beagle_pages* p, int most_pages, int remap, cudaStream_t 
     const int vecs = (int)((size_t)p->n_kv_heads * p->page_size * p->head_dim * elt_bytes(p) / 16);
     const int chunks = (vecs + kMoveThreads * kMoveVecs - 1) / (kMoveThreads * kMoveVecs);
     const long long most = (long long)most_pages * 2 * chunks;
-    const int grid = (int)(most < 148 * 8 ? (most > 0 ? most : 1) : 148 * 8);       // eight 256-thread CTAs fit an SM
+    const int fit = device_sm_count() * 8;               // eight 256-thread CTAs fit an SM
+    const int grid = (int)(most < fit ? (most > 0 ? most : 1) : fit);
     launch_pdl(pages_move_kernel, dim3(grid), dim3(kMoveThreads), 0, stream, book_of(p), static_cast<uint4*>(p->k), static_cast<uint4*>(p->v), vecs,
                remap, p->max_slots * p->max_pages);
 }
@@ -534,7 +536,7 @@ beagle_status beagle_pages_workspace_bytes(const beagle_pages* p, size_t* bytes)
 beagle_status beagle_pages_reset(const beagle_pages* p, void* stream) {
     const beagle_status st = pages_check(p);
     if (st != BEAGLE_OK) return st;
-    launch_pdl(pages_reset_kernel, dim3(148), dim3(256), 0, static_cast<cudaStream_t>(stream), book_of(p), p->max_slots);
+    launch_pdl(pages_reset_kernel, dim3(device_sm_count()), dim3(256), 0, static_cast<cudaStream_t>(stream), book_of(p), p->max_slots);
     return launched();
 }
 

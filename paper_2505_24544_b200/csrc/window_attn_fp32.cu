@@ -11,6 +11,7 @@
 // order of the heads.
 //
 // Measured: three sequences up to 333, 4 heads of 64, window 64: forward 14 us, query side 20, key side 36, all latency (88 CTAs).
+#include "tensor_map.h"
 #include "window_attn.h"
 
 namespace beagle {
@@ -443,7 +444,7 @@ int retile(WinSeqs& s, int batch, const int32_t* len, int rows) {
 }
 // 64 rows a CTA unless that leaves SMs idle (three sequences up to 333, 4 heads of 64: 48 CTAs of 64 rows, 92 of 32: forward and
 // backward 35 + 88 us against 39 + 105).
-bool small_rows(WinSeqs& s, int batch, const int32_t* len, int heads) { return (long long)retile(s, batch, len, 64) * heads < 148; }
+bool small_rows(WinSeqs& s, int batch, const int32_t* len, int heads) { return (long long)retile(s, batch, len, 64) * heads < device_sm_count(); }
 
 template <typename K, typename SM>
 bool raise_limit(K kernel, PerDeviceOnce& once, SM) {
@@ -499,7 +500,8 @@ int bwd(const WinArgs& a, WinSeqs s, cudaStream_t stream) {
         launched += rc;
         if (a.G > 1) {
             const long long rows = (long long)s.k_start[a.batch - 1] + s.kv_len[a.batch - 1], n = rows * a.Hkv * 2 * DH;
-            window_group_join_fp32_kernel<<<dim3((unsigned)((n + 255) / 256 < 148 * 8 ? (n + 255) / 256 : 148 * 8)), 256, 0, stream>>>(a, DH, rows);
+            const long long ctas = (n + 255) / 256, fit = device_sm_count() * 8;
+            window_group_join_fp32_kernel<<<dim3((unsigned)(ctas < fit ? ctas : fit)), 256, 0, stream>>>(a, DH, rows);
             ++launched;
         }
         if (a.sink_rows > 0) {           // (over what the join of the groups left in the sinks' rows)
