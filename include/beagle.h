@@ -298,7 +298,7 @@ beagle_status beagle_pages_append(const beagle_pages* pages, int32_t batch, cons
                                   const void* k_new_dev, int64_t k_stride, const void* v_new_dev, int64_t v_stride, int32_t* ok_dev, void* stream);
 
 /* Cuts n distinct slots to their first keep_dev[i] positions (int32, clamped to [0, length]; NULL = 0: the slot is freed)
- * and gives back the pages behind. */
+ * and gives back the pages behind.  keep_dev is not part of the cache (its length array). */
 beagle_status beagle_pages_truncate(const beagle_pages* pages, int32_t n, const int32_t* slot_host, const int32_t* keep_dev, void* stream);
 
 /* Slot dst[i] becomes a fork of slot src[i]: it shares every page (no rows move; the first append to either copies the
@@ -330,7 +330,8 @@ beagle_status beagle_paged_attn(const beagle_pages* pages, int32_t batch, const 
 /* The draft head over a paged cache.  The slots of these calls are both the context's (previous token and state of a chain)
  * and the cache's (keys and values); the cache has the context's storage type, n_kv_heads and head_dim (SHAPE otherwise); the
  * context's own cache is not touched.  A slot has one chain: drop it (beagle_rollback) before going over from pages to the
- * context's cache or back.  No rotary option (UNSUPPORTED): its positions live on the host, these lengths do not.  max_ctx and
+ * context's cache or back, and when its pages come to hold another sequence (fork, copy, freed and filled anew): those calls know
+ * no context, and the next step would append the old chain's last state.  No rotary option (UNSUPPORTED): its positions live on the host, these lengths do not.  max_ctx and
  * max_draft do not bound a paged slot; max_pages and the free pages do.
  *
  * beagle_prefill_pages: beagle_prefill_kv into pages.  The new_len[b] rows of hidden_dev (packed) are projected with W_k, W_v
@@ -359,8 +360,10 @@ beagle_status beagle_draft_step_pages(beagle_ctx* ctx, const beagle_pages* pages
  * gradient 0.  q_dev [.., n_q_heads, head_dim], k_dev and v_dev [.., n_kv_heads, head_dim] in the storage type, the heads of a
  * row dense, rows *_stride elements apart (slices of a fused projection are fine; rows 16-byte aligned).
  * n_q_heads a multiple of n_kv_heads; head_dim 64 | 128, fp32 also 16 | 32; with a window sinks <= 1024; at most 2^27 rows.
- * Scores, softmax, statistics and sums are fp32; the bf16 kernels round the softmax weights and dS to bf16 for their products.
- * Keys and values of a sequence must be finite; rows of other sequences and rows behind the last one are never mixed in and
+ * Scores, softmax, statistics and sums are fp32; the bf16 kernels round the softmax weights and dS to bf16 for their products, and the
+ * backward pass forms delta = sum(dout * out) of a row in fp32 from out as it is stored (bf16).
+ * Keys and values of a sequence must be finite, in the backward pass also every row of q, out and dout (rows that see nothing
+ * included; a value that is not spreads over the gradients of its sequence); rows of other sequences and rows behind the last one are never mixed in and
  * outputs behind the last row are left as they were.  A query row with a NaN has a NaN lse and NaN outputs.  Outputs must not
  * overlap inputs.  Results do not depend on timing. */
 typedef struct beagle_window_attn {

@@ -22,7 +22,9 @@
 // Measured: 32 sequences of 512 to 8192, 32 heads over 8 of 128: 103 us of stream (5.8 to 6.0 TB/s of cache) and 5 us of join; 16
 // sequences of 65000 to 131072: 1012 us, the rate of a plain copy; the smallest fp32 call: 4 us on the GPU.  fp32, 32 sequences of 2000,
 // 8 K/V heads of 128 (524 MB): 111 us with one query head each, 118 with four, 142 with eight (loading straight into registers, without the
-// ring, took 165, 212 and 490).
+// ring, took 165, 212 and 490).  bf16, 537 MB, on the same CUDA-core kernel: head_dim 256 with 1 / 4 query heads a pair 112 / 138 us, head_dim 32 with
+// 1 / 4 / 8 192 / 210 / 288: at 64 bytes a row there are four times as many scores and weights to form per byte as at 256.  No pipe is saturated there (issue slots
+// 0.49 to 0.54, DRAM 0.35 to 0.50 of nominal); the consumer warps wait for their own shared-memory reads and shuffles half of the time.
 //
 // Masked positions (past the length, outside the window) have their weight and their V row replaced by zero before use, so
 // whatever the pool holds there (NaN included) has no effect.

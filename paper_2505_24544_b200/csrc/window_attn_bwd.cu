@@ -14,11 +14,16 @@
 //               halves take turns: while the threads form P of the next tile, dK and the next dP^T run, while they form dS,
 //               dV and the next S^T run.
 // Both use all 512 columns of tensor memory and about 200 KB of shared memory: one CTA per SM, two threads per tile row.  The
-// grid is one CTA per SM and walks the items, the pipeline running on across them: the copies and the first products of an item
-// start under the last products and the epilogue of the one before it (as CTAs of their own, items of five tiles spent 7 us of 16
-// on starting up and draining).
+// query side's grid is one CTA per SM and walks the items, the pipeline running on across them: the copies and the first products
+// of an item start under the last products and the epilogue of the one before it (as CTAs of their own, items of five tiles spent 7 us
+// of 16 on starting up and draining).  So is the key side's where a band has few jobs; longer items are CTAs of their own (launch_bwd).
 // P and dS are the tensor-memory operands of their products (rows = lanes), so the accumulating products read one operand
 // from shared memory, and Q, dO, K tiles serve both as K-major and as MN-major operands: nothing is copied or transposed.
+// They are rounded to bf16 for that, the operand type that V, dO, K and Q have.  delta is summed in fp32 from the forward's output as it is
+// stored, in bf16: sum_j P dP, which needs no O, is known only when all of a row's keys have been seen, and then dS would take a
+// second pass over them; an fp32 O from the forward would be twice the bytes.  With short windows this rounding costs dQ more than
+// that of dS (relative error of dQ in a model on the CPU, 512 rows, head_dim 128, with nothing but the result rounded, with dS, with O
+// and with both: window 2: 1.7, 2.4, 4.0, 5.3e-3; window 8: 1.7, 2.3, 2.4, 3.3e-3; window 512: 1.7, 2.4, 1.9, 2.7e-3).
 //
 // The sinks' keys are read by every later query.  What lies past the band of a key tile is therefore cut into segments of
 // similar length, each a CTA of its own that leaves fp32 partials of the (few) sink rows; a last small launch adds them to the
@@ -984,9 +989,13 @@ int launch_bwd(const WinArgs& a, const WinSeqs& s, long long q_rows, long long k
         if (t.item[a.batch] > 0) {
             const long long items = (long long)t.item[a.batch] * a.Hkv;
             if (items > 0x3fffffff) return -1;
-            // Items of many jobs run as CTAs of their own (their start-up is small beside them and the hardware balances them: 17 tiles x
-            // 4 heads, backward of sequences up to 8191 1406 us against 1432 as a fixed share per SM), short ones share a pipeline
-            // (5 tiles, 8 x 2048: 731 against 783).
+            // Items of many jobs run as CTAs of their own (their start-up is small beside them and the hardware balances them), short ones
+            // share a pipeline.  Backward, head_dim 128, shared against unshared, us, by jobs of a band (whole tiles of the window + 256):
+            //   one head a K/V head   6: 708 / 738   10: 854 / 899   18: 1420 / 1458   25: 1760 / 1772
+            //   two                   8: 557 / 577   12: 649 / 631   16: 762 / 722     20: 871 / 822    24: 991 / 883
+            //   four                  16: 580 / 561  20: 616 / 591   24: 694 / 622     40: 903 / 803    72: 1200 / 1202
+            // (8 x 2048; 18 and 25: 4 x 4096; 72: two sequences up to 8191).  With grouped heads, whose items are fewer and longer, the
+            // turn comes at ten jobs already: up to 7 % are left there between ten and 24.
             const long long jobs = ((long long)(a.window < 1 << 24 ? a.window : 1 << 24) + 2 * kKTile) / kQTile * a.G;
             const bool share = jobs < 24 && items > sms;
             (a.splits > 1 ? window_bwd_kv_kernel<DH, true> : window_bwd_kv_kernel<DH, false>)
