@@ -438,3 +438,44 @@ def test_an_empty_slot_gives_zero_and_minus_infinity(dtype, dh, width):
     b.beagle_paged_attn(cache, [0, 1, 2], q, out, lse)
     assert bool(torch.isneginf(lse[[0, 2]]).all()) and bool(torch.isfinite(lse[1]).all())
     assert bool((out[[0, 2]] == 0).all()) and bool(torch.isfinite(out[1]).all())
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 256), ("fp32", 128)])
+def test_pools_past_32_bit_offsets(dtype, dh):
+    """Pools of more than 2^31 elements: rows appended to the last pages, read, copied, moved and forked there as anywhere else."""
+    hkv, ps = 8, 64
+    n_pages = 2 ** 31 // (hkv * ps * dh) + 40
+    cache = b.PagedCache(n_pages, ps, hkv, dh, 4, n_pages, dtype)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    k, v = (torch.randn(1, 700, hkv, dh, generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+    q = torch.randn(1, 16, dh, generator=g, device="cuda").to(DT[dtype])
+
+    def attend(slot):
+        out, lse = torch.empty_like(q), torch.empty(1, 16, device="cuda")
+        b.beagle_paged_attn(cache, [slot], q, out, lse, window=500, sinks=70)
+        return out, lse
+
+    def pages(slot):
+        return cache.table[slot, :11].tolist()
+    b.beagle_pages_append(cache, [0], k, v)
+    want = attend(0)
+    assert pages(0) == list(range(11))
+    cache.refs[11:n_pages - 25] = 1                          # pages that another program holds: the free ones are the last
+    b.beagle_pages_append(cache, [1], k, v)
+    b.beagle_pages_copy(cache, [0], [2])
+    top = n_pages - 25
+    assert pages(1) == list(range(top, top + 11)) and pages(2) == list(range(top + 11, top + 22))
+    for slot in (1, 2):
+        at = torch.tensor(pages(slot), device="cuda")
+        for pool, rows in ((cache.k, k), (cache.v, v)):
+            assert torch.equal(pool[at].permute(0, 2, 1, 3).reshape(-1, hkv, dh)[:700], rows[0])
+        assert all(torch.equal(x, y) for x, y in zip(attend(slot), want))
+    b.beagle_pages_fork(cache, [2], [3])
+    b.beagle_pages_append(cache, [3], k[:, :1], v[:, :1])    # the last page's rows are copied from one end of the pool to the other
+    assert pages(3) == pages(2)[:10] + [top + 22]
+    assert all(torch.equal(x, y) for x, y in zip(attend(2), want))
+    cache.refs[11:top] = 0
+    b.beagle_pages_compact(cache)
+    assert pages(1) == list(range(11, 22)) and int(cache.table.max()) == 33
+    for slot in (1, 2):
+        assert all(torch.equal(x, y) for x, y in zip(attend(slot), want))

@@ -361,3 +361,29 @@ def test_sinks_of_ragged_sequences(dtype, hq, hkv, dh, window, sinks):
     again = run(*x, q_len, kv_len, window, sinks, False)
     for name in first:
         assert torch.equal(first[name], again[name]), name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_past_32_bit_offsets(dtype):
+    """Queries, outputs and gradients of more than 2^31 elements: a sequence behind them has the results that it has alone."""
+    long, n, hq, hkv, dh, window = 530000, 900, 32, 16, 128, 100
+    assert long * hq * dh > 2 ** 31
+    q_len, kv_len = [long, n], [700, 1000]                   # (the long sequence's queries see its few keys at its end)
+    x = inputs([n], [1000], hq, hkv, dh, dtype, 43)
+    alone = run(*x, [n], [1000], window, 0, False)
+    q, do, out = (torch.zeros(long + n, hq, dh, dtype=DT[dtype], device="cuda") for _ in range(3))
+    k, v = (torch.ones(1700, hkv, dh, dtype=DT[dtype], device="cuda") for _ in range(2))
+    q[long:], do[long:], k[700:], v[700:] = x[0], x[3], x[1], x[2]
+    lse = torch.zeros(long + n, hq, device="cuda")
+    b.beagle_window_attn_forward(q, k, v, q_len, kv_len, out, lse, window, 0)
+    assert torch.equal(out[long:], alone["out"]) and torch.equal(lse[long:], alone["lse"])
+    # scores 0: the mean of ones (a sum that is exact, times the sum's inverse: two roundings of half a step, 2 * 2^-24), and ln of how
+    # many keys a query sees
+    assert bool(((out[long - 700:long].double() - 1).abs() <= 2.0 ** -23 * (1 + 2.0 ** -20)).all()) and bool((out[:long - 700] == 0).all()) and bool(torch.isneginf(lse[:long - 700]).all())
+    seen = torch.arange(1, 701, device="cuda").clamp(max=window).double().log()[:, None]
+    assert bool(((lse[long - 700:long].double() - seen).abs() <= 2.0 ** -21 * (1 + seen)).all())
+    dq, dk, dv = torch.full_like(q, 7.0), torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    b.beagle_window_attn_backward(q, k, v, out, lse, do, q_len, kv_len, dq, dk, dv, window, 0)
+    for got, name in ((dq[long:], "dq"), (dk[700:], "dk"), (dv[700:], "dv")):
+        assert torch.equal(got, alone[name]), name
+    assert not bool(dq[:long].any()) and not bool(dk[:700].any()) and not bool(dv[:700].any())
