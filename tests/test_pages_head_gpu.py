@@ -180,3 +180,26 @@ def test_chain_from_a_captured_graph():
     chain(eager)
     torch.cuda.synchronize()
     assert torch.equal(eager, longer) and cache.length.tolist() == [n + 3 for n in lengths]
+
+
+@pytest.mark.parametrize("w", [GQA, FP32], ids=lambda x: x.name)
+def test_a_reused_slot_starts_a_chain_of_its_own(w):
+    """A slot whose old sequence is freed and that becomes a fork: with its old chain dropped it drafts what the slot it was forked
+    from drafts, and the old chain's last state is not appended to it."""
+    w = w.scaled(batch=2, ctx_max=40)
+    head, _, cache = build(w, ps=8)
+    rng = WL.data_rng(w, 9)
+    hidden = to_dev(WL.make_hidden(w, rng, 70), w.dtype)
+    first = to_dev(WL.make_tokens(w, rng, (2,)), w.dtype)
+    head.prefill_pages(cache, [0, 1], [37, 33], hidden)
+    head.draft_step_pages(cache, [1], first[1:])                       # slot 1 has a chain, its last state pending
+    b.beagle_pages_truncate(cache, [1])
+    b.beagle_pages_fork(cache, [0], [1])
+    head.rollback([1])
+    both = first[:1].expand(2).contiguous()
+    tok, logits, _ = head.draft_step_pages(cache, [0, 1], both, want_logits=True)
+    assert cache.length.tolist() == [37, 37] and torch.equal(logits[0], logits[1]) and int(tok[0]) == int(tok[1])
+    tok, logits, _ = head.draft_step_pages(cache, [0, 1], want_logits=True)      # both append their first state, to pages of their own
+    assert cache.length.tolist() == [38, 38] and torch.equal(logits[0], logits[1]) and int(tok[0]) == int(tok[1])
+    assert cache.table[0, :4].tolist() == cache.table[1, :4].tolist() and int(cache.table[0, 4]) != int(cache.table[1, 4])
+    b.beagle_check_device(head.ctx)
