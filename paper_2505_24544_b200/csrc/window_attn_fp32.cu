@@ -217,6 +217,7 @@ __global__ void __launch_bounds__(kThreads) window_fwd_fp32_kernel(const __grid_
         weigh<DH, RT>(P, V, ty, tx, o);
         __syncwarp();
     }
+    cp_wait<0>();                                        // (a CTA without tiles: its queries have landed before it ends)
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
 #pragma unroll
@@ -393,6 +394,7 @@ __global__ void __launch_bounds__(kThreads) window_bwd_kv_fp32_kernel(const __gr
         weigh<DH, RT>(dS, Q, ty, tx, dk);
         __syncwarp();
     }
+    cp_wait<0>();                                        // (a CTA without tiles: its keys and values have landed before it ends)
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int key = k0 + RT * ty + r;
