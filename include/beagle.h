@@ -331,8 +331,8 @@ beagle_status beagle_paged_attn(const beagle_pages* pages, int32_t batch, const 
  * and the cache's (keys and values); the cache has the context's storage type, n_kv_heads and head_dim (SHAPE otherwise); the
  * context's own cache is not touched.  A slot has one chain: drop it (beagle_rollback) before going over from pages to the
  * context's cache or back, and when its pages come to hold another sequence (fork, copy, freed and filled anew): those calls know
- * no context, and the next step would append the old chain's last state.  No rotary option (UNSUPPORTED): its positions live on the host, these lengths do not.  max_ctx and
- * max_draft do not bound a paged slot; max_pages and the free pages do.
+ * no context, and the next step would append the old chain's last state.  No rotary option (UNSUPPORTED): its positions live on
+ * the host, these lengths do not.  max_ctx and max_draft do not bound a paged slot; max_pages and the free pages do.
  *
  * beagle_prefill_pages: beagle_prefill_kv into pages.  The new_len[b] rows of hidden_dev (packed) are projected with W_k, W_v
  *   and appended to slot seq_slot[b] as beagle_pages_append does (ok_dev as there); the chain of the slot starts anew.  The
@@ -363,9 +363,9 @@ beagle_status beagle_draft_step_pages(beagle_ctx* ctx, const beagle_pages* pages
  * Scores, softmax, statistics and sums are fp32; the bf16 kernels round the softmax weights and dS to bf16 for their products, and the
  * backward pass forms delta = sum(dout * out) of a row in fp32 from out as it is stored (bf16).
  * Keys and values of a sequence must be finite, in the backward pass also every row of q, out and dout (rows that see nothing
- * included; a value that is not spreads over the gradients of its sequence); rows of other sequences and rows behind the last one are never mixed in and
- * outputs behind the last row are left as they were.  A query row with a NaN has a NaN lse and NaN outputs.  Outputs must not
- * overlap inputs.  Results do not depend on timing. */
+ * included; a value that is not spreads over the gradients of its sequence); rows of other sequences and rows behind the last one
+ * are never mixed in and outputs behind the last row are left as they were.  A query row with a NaN has a NaN lse and NaN outputs.
+ * Outputs must not overlap inputs.  Results do not depend on timing. */
 typedef struct beagle_window_attn {
     const void* q_dev;
     const void* k_dev;

@@ -132,7 +132,7 @@ Layout layout(const beagle_window_attn* w, const WinArgs& a, WinSeqs& s, long lo
         L.sink_rows = rows_of(b) > L.sink_rows ? rows_of(b) : L.sink_rows;
     }
     if (parts > 0) {
-        // (Up to 4 MB the size goes by the longest sequence alone, so that one workspace does for every mix of lengths below it.)
+        // (Up to 4 MB every sequence is given what the largest takes: the size of small calls does not follow each length.)
         const size_t row = 2 * d * sizeof(float), even = (size_t)a.batch * heads * (1 + most_segs) * most_rows * row, own = parts * row;
         off += own > kSmallParts ? own : even < kSmallParts ? even : kSmallParts;
     }
