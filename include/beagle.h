@@ -250,6 +250,45 @@ beagle_status beagle_block_grad(beagle_ctx* ctx, int32_t batch, int32_t S, const
                                 int32_t logits_dtype, const int32_t* target_ids_dev, float vloss_coef, const beagle_grads* grads,
                                 float* loss_out_dev, void* ws_dev, size_t ws_bytes, void* stream);
 
+/* ---- Rotary positions ------------------------------------------------------------------------------------------------
+ * The rotation of beagle_config.rope_theta as an operator of its own, for positions that lie on the device, both layouts, a part
+ * of the head and contexts longer than the trained one.  Of every head the first rot_dim components are rotated in pairs,
+ *     (x_a, x_b) at position p  ->  mscale * (cos(p f) x_a - sin(p f) x_b,  sin(p f) x_a + cos(p f) x_b),
+ * pair i < rot_dim / 2 being components (i, i + rot_dim / 2) or, interleaved, (2i, 2i + 1); the others pass.  Angles are formed in
+ * double precision, so positions may be any int32.  The structure lives on the host and is passed by value: its values may be
+ * changed, or come from elsewhere (any frequencies).
+ *
+ * beagle_rotary_make fills it: f_i = theta^(-2i / rot_dim), stretched for contexts `factor` times the `original` one:
+ *   NONE    as it is                                   LINEAR  f / factor
+ *   BASE    theta * factor^(r / (r - 2)) for theta, r = rot_dim (the lowest frequency divided by factor, the highest kept)
+ *   BANDS   by the turns n = original * f / 2 pi that a pair makes: f from n = high on, f / factor up to n = low, in between
+ *           linear in n
+ *   RAMP    the same by the pair's number, linear from pair floor(c(high)) to ceil(c(low)) (not below 0, not above rot_dim - 1),
+ *           c(n) = rot_dim ln(original / (2 pi n)) / (2 ln theta)
+ * theta > 1, factor >= 1, 0 < low < high (read by BANDS and RAMP only, like original).  mscale 0: 1, for RAMP 0.1 ln(factor) + 1. */
+#define BEAGLE_ROTARY_MAX_PAIRS 128
+enum { BEAGLE_ROTARY_NONE = 0, BEAGLE_ROTARY_LINEAR = 1, BEAGLE_ROTARY_BASE = 2, BEAGLE_ROTARY_BANDS = 3, BEAGLE_ROTARY_RAMP = 4 };
+typedef struct beagle_rotary {
+    int32_t head_dim;     /* at most 256; rows of heads in 16-byte pieces: a multiple of 8 (bf16) or 4 (fp32)  */
+    int32_t rot_dim;      /* even, 2..head_dim                                                     */
+    int32_t interleaved;
+    int32_t reserved;
+    double  mscale;
+    double  freq[BEAGLE_ROTARY_MAX_PAIRS];      /* radians per position */
+} beagle_rotary;
+
+beagle_status beagle_rotary_make(int32_t head_dim, int32_t rot_dim, int32_t interleaved, double theta, int32_t scaling, double factor,
+                                 double original, double low, double high, double mscale, beagle_rotary* out_host);
+
+/* Rotates `rows` rows of n_q_heads query heads and n_k_heads key heads (either may be 0) in one launch.  Row r is at position
+ * pos_dev[r] (int32), or without pos_dev at pos0 + r modulo period (period 0: pos0 + r).  Heads of a row are dense, rows *_stride
+ * elements apart, 16-byte aligned.  Output rows may be the input's (same pointer and stride) and else must not overlap them.
+ * inverse != 0: the transpose (the gradient of the input from that of the output).  Computed in fp32, rounded once. */
+beagle_status beagle_rotary_apply(const beagle_rotary* rot, int32_t dtype, int64_t rows, const int32_t* pos_dev, int32_t pos0, int64_t period,
+                                  int32_t n_q_heads, const void* q_dev, int64_t q_stride, void* q_out_dev, int64_t q_out_stride,
+                                  int32_t n_k_heads, const void* k_dev, int64_t k_stride, void* k_out_dev, int64_t k_out_stride,
+                                  int32_t inverse, void* stream);
+
 /* ---- Key/value states in pages, and the attention that reads them ----------------------------------------------------
  * A cache whose sequences take fixed-size pages from one pool instead of a reserved run each, so that ragged sequences,
  * forks that share a prefix and sequences longer than any reserved length fit one buffer.  These calls need no context: all
@@ -297,6 +336,17 @@ beagle_status beagle_pages_reset(const beagle_pages* pages, void* stream);
 beagle_status beagle_pages_append(const beagle_pages* pages, int32_t batch, const int32_t* slot_host, int32_t T, const int32_t* n_new_dev,
                                   const void* k_new_dev, int64_t k_stride, const void* v_new_dev, int64_t v_stride, int32_t* ok_dev, void* stream);
 
+/* beagle_pages_append with the position rotation on the way: the key of every new row is rotated (beagle_rotary) at the position
+ * that it takes in its slot, the value goes in as it is.  Queries that belong to the new rows may come along (n_q_heads 0: none):
+ * q_dev [batch, T, n_q_heads, head_dim], rows q_stride elements apart, is rotated at the key's position + q_offset into q_out_dev, the
+ * same, dense (q_dev itself is fine where it is dense).  q_offset 0: a query at its own key's position; 1: at the position behind it, as
+ * the draft head's queries are.  Query rows t < n_new are rotated whether or not the row found room; the others are left as they
+ * were.  The rotation's head_dim is the cache's.  T up to 2^29, q_offset below 2^29.  All else as beagle_pages_append. */
+beagle_status beagle_pages_append_rotary(const beagle_pages* pages, const beagle_rotary* rot, int32_t batch, const int32_t* slot_host, int32_t T,
+                                         const int32_t* n_new_dev, const void* k_new_dev, int64_t k_stride, const void* v_new_dev, int64_t v_stride,
+                                         int32_t n_q_heads, const void* q_dev, int64_t q_stride, void* q_out_dev, int32_t q_offset, int32_t* ok_dev,
+                                         void* stream);
+
 /* Cuts n distinct slots to their first keep_dev[i] positions (int32, clamped to [0, length]; NULL = 0: the slot is freed)
  * and gives back the pages behind.  keep_dev is not part of the cache (its length array). */
 beagle_status beagle_pages_truncate(const beagle_pages* pages, int32_t n, const int32_t* slot_host, const int32_t* keep_dev, void* stream);
@@ -326,6 +376,23 @@ beagle_status beagle_paged_attn_workspace_bytes(const beagle_pages* pages, int32
 beagle_status beagle_paged_attn(const beagle_pages* pages, int32_t batch, const int32_t* slot_host, int32_t n_q_heads, const void* q_dev,
                                 int64_t q_stride, int32_t window, int32_t sinks, void* out_dev, float* lse_dev, void* ws_dev,
                                 size_t ws_bytes, void* stream);
+
+/* beagle_paged_attn for rows whose slots begin with the same positions (forks of one prompt): the common part is read once for all
+ * rows of a group.  The rows of the call come in n_groups groups, group i being the next group_rows_host[i] >= 1 of them.
+ * shared_dev int32 [n_groups]: the first so many positions hold the same keys and values in every slot of the group; they are read
+ * through the group's first slot.  Clamped to 0 and the shortest length of the group.  What lies behind them is read row by row, so
+ * any smaller number gives the same attention.  Everything visible (no window).  Other arguments and results as beagle_paged_attn (results
+ * are its up to rounding, and do not depend on timing).  ws_dev: beagle_paged_attn_shared_workspace_bytes, 16-byte aligned.
+ *
+ * beagle_pages_shared: writes such a shared_dev from the cache itself: per group the positions of the leading whole pages that all of
+ * its slots name alike (0 for a group of one row, for which nothing is gained). */
+beagle_status beagle_pages_shared(const beagle_pages* pages, int32_t batch, const int32_t* slot_host, int32_t n_groups, const int32_t* group_rows_host,
+                                  int32_t* shared_dev, void* stream);
+beagle_status beagle_paged_attn_shared_workspace_bytes(const beagle_pages* pages, int32_t batch, int32_t n_q_heads, int32_t n_groups,
+                                                       const int32_t* group_rows_host, size_t* bytes);
+beagle_status beagle_paged_attn_shared(const beagle_pages* pages, int32_t batch, const int32_t* slot_host, int32_t n_groups,
+                                       const int32_t* group_rows_host, const int32_t* shared_dev, int32_t n_q_heads, const void* q_dev,
+                                       int64_t q_stride, void* out_dev, float* lse_dev, void* ws_dev, size_t ws_bytes, void* stream);
 
 /* The draft head over a paged cache.  The slots of these calls are both the context's (previous token and state of a chain)
  * and the cache's (keys and values); the cache has the context's storage type, n_kv_heads and head_dim (SHAPE otherwise); the
@@ -422,6 +489,21 @@ beagle_status beagle_verify_sample(beagle_ctx* ctx, int32_t batch, int32_t gamma
                                    const float* draft_logits_dev, const void* target_logits_dev, int32_t logits_dtype,
                                    float temperature, const float* u_accept_dev, const float* u_resample_dev,
                                    int32_t* accept_len_dev, int32_t* out_tokens_dev, void* stream);
+
+/* One token per row of logits, drawn with the caller's random numbers: what drafts for beagle_verify_sample are drawn with (with
+ * temperature alone), and what a sampled target emits.  logits_dev [rows, vocab] (logits_dtype BEAGLE_FP32 | BEAGLE_BF16), rows
+ * row_stride elements apart; vocab up to 2^18.  Every parameter is an array of one value per row, or NULL:
+ *   temperature_dev fp32 (NULL: 1; a value not above 0, or NaN: the row's largest logit, no draw), top_k_dev int32 (NULL or <= 0: all),
+ *   top_p_dev fp32 (NULL, >= 1 or NaN: all), min_p_dev fp32 (NULL, <= 0 or NaN: all), u_dev fp32 in [0, 1), required.
+ * With d(v) = (logit(v) - largest) / temperature and the tokens in order of falling logit, the lower id first among equals, a row keeps
+ * the first top_k; of those the shortest leading run whose weight (sum of exp d) is at least top_p times the weight of them all;
+ * of those the ones with exp(d) >= min_p; the first always.  tokens_out_dev int32 [rows]: the smallest id whose cumulative kept weight, in
+ * order of id, exceeds u times the kept weight; logp_out_dev fp32 [rows] (nullable): ln of its share of the kept weight (0 without a
+ * draw).  Weights are 2^-45 of the largest exact and sums are integers: results depend on neither timing nor the rest of the batch.  A NaN logit
+ * counts as -infinity; +infinity takes all the weight (shared among several); a row of -infinity alone gives token -1 and logp NaN. */
+beagle_status beagle_sample(const void* logits_dev, int32_t logits_dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                            const float* temperature_dev, const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev,
+                            const float* u_dev, int32_t* tokens_out_dev, float* logp_out_dev, void* stream);
 
 /* Dynamic draft tree for one sequence (the draft tree of the experimental setup, Section 5.1, i.e. the
  * method of EAGLE-2 with depth = 1 + `depth`, `topk` children per node and `n_candidates` nodes kept; the paper's

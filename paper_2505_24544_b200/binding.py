@@ -35,6 +35,8 @@ EXPORTED_SYMBOLS = (
     "beagle_pages_workspace_bytes", "beagle_pages_reset", "beagle_pages_append", "beagle_pages_truncate", "beagle_pages_fork",
     "beagle_pages_copy", "beagle_pages_compact", "beagle_paged_attn_workspace_bytes", "beagle_paged_attn",
     "beagle_prefill_pages_workspace_bytes", "beagle_prefill_pages", "beagle_draft_step_pages",
+    "beagle_rotary_make", "beagle_rotary_apply", "beagle_pages_append_rotary", "beagle_pages_shared",
+    "beagle_paged_attn_shared_workspace_bytes", "beagle_paged_attn_shared", "beagle_sample",
     "beagle_window_attn_forward", "beagle_window_attn_workspace_bytes", "beagle_window_attn_backward",
 )
 
@@ -61,6 +63,15 @@ class BeagleGrads(C.Structure):
 class BeaglePages(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "table", "length", "refs", "ws")] + [("ws_bytes", C.c_size_t)] + \
                [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype", "max_slots", "max_pages")]
+
+
+BEAGLE_ROTARY_MAX_PAIRS = 128
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
+class BeagleRotary(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("head_dim", "rot_dim", "interleaved", "reserved")] + \
+               [("mscale", C.c_double), ("freq", C.c_double * BEAGLE_ROTARY_MAX_PAIRS)]
 
 
 class BeagleWindowAttn(C.Structure):
@@ -154,6 +165,17 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.beagle_prefill_pages.argtypes = [vp, pg, i32, vp, vp, vp, vp, vp, C.c_size_t, vp]
     lib.beagle_draft_step_pages.argtypes = [vp, pg, i32, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp, vp]
     for name in ("beagle_prefill_pages_workspace_bytes", "beagle_prefill_pages", "beagle_draft_step_pages"):
+        getattr(lib, name).restype = C.c_int
+    ro, f64 = C.POINTER(BeagleRotary), C.c_double
+    lib.beagle_rotary_make.argtypes = [i32, i32, i32, f64, i32, f64, f64, f64, f64, f64, ro]
+    lib.beagle_rotary_apply.argtypes = [ro, i32, i64, vp, i32, i64, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp]
+    lib.beagle_pages_append_rotary.argtypes = [pg, ro, i32, vp, i32, vp, vp, i64, vp, i64, i32, vp, i64, vp, i32, vp, vp]
+    lib.beagle_pages_shared.argtypes = [pg, i32, vp, i32, vp, vp, vp]
+    lib.beagle_paged_attn_shared_workspace_bytes.argtypes = [pg, i32, i32, i32, vp, szp]
+    lib.beagle_paged_attn_shared.argtypes = [pg, i32, vp, i32, vp, vp, i32, vp, i64, vp, vp, vp, C.c_size_t, vp]
+    lib.beagle_sample.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    for name in ("beagle_rotary_make", "beagle_rotary_apply", "beagle_pages_append_rotary", "beagle_pages_shared",
+                 "beagle_paged_attn_shared_workspace_bytes", "beagle_paged_attn_shared", "beagle_sample"):
         getattr(lib, name).restype = C.c_int
     wa = C.POINTER(BeagleWindowAttn)
     lib.beagle_window_attn_forward.argtypes = [wa, vp, vp, vp]
@@ -699,6 +721,138 @@ def beagle_paged_attn(cache: PagedCache, slots: Sequence[int], q: torch.Tensor, 
               "beagle_paged_attn")
 
 
+class Rotary:
+    """Rotary positions (``beagle_rotary``): the layout and the frequencies, on the host.
+
+    ``rot_dim`` first components of a head of ``head_dim`` are rotated (None: all), in pairs (i, i + rot_dim / 2), or (2i, 2i + 1) if
+    ``interleaved``.  ``scaling`` of the frequencies theta^(-2i / rot_dim) for contexts ``factor`` times the ``original`` one: "none",
+    "linear" (all by the factor), "base" (a larger theta), "bands" and "ramp" (the slow pairs by the factor; between ``low`` and ``high`` turns
+    inside the original context a blend, None: 1 and 4 for bands, 1 and 32 for ramp).  ``mscale`` multiplies cosine and sine (None: 1,
+    for "ramp" 0.1 ln(factor) + 1).  ``struct.freq`` may be set to any other frequencies."""
+
+    def __init__(self, head_dim: int, rot_dim: Optional[int] = None, theta: float = 10000.0, interleaved: bool = False, scaling: str = "none",
+                 factor: float = 1.0, original: float = 0.0, low: Optional[float] = None, high: Optional[float] = None, mscale: Optional[float] = None):
+        if scaling not in ROTARY_SCALINGS:
+            raise ValueError(f"scaling: one of {', '.join(ROTARY_SCALINGS)}")
+        if mscale is not None and not mscale > 0:
+            raise ValueError("mscale: above 0")
+        self.lib, self.struct = load_library(), BeagleRotary()
+        self.ref = C.byref(self.struct)
+        _pages_ok(self.lib.beagle_rotary_make(head_dim, head_dim if rot_dim is None else rot_dim, int(bool(interleaved)), theta, ROTARY_SCALINGS[scaling],
+                                              factor, original, 1.0 if low is None else low, (32.0 if scaling == "ramp" else 4.0) if high is None else high,
+                                              0.0 if mscale is None else mscale, self.ref), "beagle_rotary_make")
+
+    @property
+    def frequencies(self) -> list:
+        return list(self.struct.freq[:self.struct.rot_dim // 2])
+
+
+def beagle_rotary_apply(rot: Rotary, q: torch.Tensor, q_out: torch.Tensor, k: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                        pos: Optional[torch.Tensor] = None, pos0: int = 0, period: int = 0, inverse: bool = False) -> None:
+    """Rotates q ([rows, heads, head_dim], float32 / bfloat16, rows may be strided) and, in the same launch, k into q_out and k_out (strided
+    rows too; the inputs themselves are fine).  Row r is at ``pos[r]`` (int32), without pos at pos0 + r modulo ``period`` (0: pos0 + r).
+    inverse: the transpose, which takes the gradients of the outputs to those of the inputs."""
+    if q.dim() != 3 or q.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("q: [rows, heads, head_dim] float32 / bfloat16")
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out: both or neither")
+    rows, hq, dh = q.shape
+    if dh != rot.struct.head_dim:
+        raise ValueError(f"q: heads of {rot.struct.head_dim} components")
+    args, hk = [_check("q", q, q.dtype, (rows, hq, dh), False), _row_stride("q", q, 1), _check("q_out", q_out, q.dtype, (rows, hq, dh), False), _row_stride("q_out", q_out, 1)], 0
+    kargs = [None, 0, None, 0]
+    if k is not None:
+        if k.dim() != 3:
+            raise ValueError("k: [rows, heads, head_dim]")
+        hk = k.shape[1]
+        kargs = [_check("k", k, q.dtype, (rows, hk, dh), False), _row_stride("k", k, 1), _check("k_out", k_out, q.dtype, (rows, hk, dh), False), _row_stride("k_out", k_out, 1)]
+    pp = None if pos is None else _check("pos", pos, torch.int32, (rows,))
+    _pages_ok(rot.lib.beagle_rotary_apply(rot.ref, BEAGLE_BF16 if q.dtype == torch.bfloat16 else BEAGLE_FP32, rows, pp, pos0, period, hq, *args, hk, *kargs,
+                                          int(bool(inverse)), _stream()), "beagle_rotary_apply")
+
+
+def beagle_pages_append_rotary(cache: PagedCache, slots: Sequence[int], rot: Rotary, k_new: torch.Tensor, v_new: torch.Tensor,
+                               n_new: Optional[torch.Tensor] = None, ok: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                               q_out: Optional[torch.Tensor] = None, q_offset: int = 0) -> None:
+    """``beagle_pages_append`` with every new key rotated at the position that it takes.  q: [len(slots), T, n_q_heads, head_dim], the queries of
+    the new rows (rows may be strided), rotated at the key's position + q_offset into q_out (dense; q itself if that is dense); rows from
+    n_new on are left as they were."""
+    c, B = cache.struct, len(slots)
+    shape = (B, k_new.shape[1] if k_new.dim() == 4 else -1, c.n_kv_heads, c.head_dim)
+    kp, vp = _check("k_new", k_new, cache.k.dtype, shape, False), _check("v_new", v_new, cache.k.dtype, shape, False)
+    n_ptr = None if n_new is None else _check("n_new", n_new, torch.int32, (B,))
+    ok_ptr = None if ok is None else _check("ok", ok, torch.int32, (B,))
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out: both or neither")
+    hq, qp, qs, qo = 0, None, 0, None
+    if q is not None:
+        if q.dim() != 4:
+            raise ValueError("q: [batch, T, n_q_heads, head_dim]")
+        hq = q.shape[2]
+        want = (B, shape[1], hq, c.head_dim)
+        qp, qs, qo = _check("q", q, cache.k.dtype, want, False), _row_stride("q", q, 2), _check("q_out", q_out, cache.k.dtype, want)
+    _pages_ok(cache.lib.beagle_pages_append_rotary(cache.ref, rot.ref, B, _host_i32(slots), shape[1], n_ptr, kp, _row_stride("k_new", k_new, 2), vp,
+                                                   _row_stride("v_new", v_new, 2), hq, qp, qs, qo, q_offset, ok_ptr, cache.on_current_device()),
+              "beagle_pages_append_rotary")
+
+
+def beagle_pages_shared(cache: PagedCache, slots: Sequence[int], groups: Sequence[int], shared: torch.Tensor) -> None:
+    """Positions that the slots of every group have in common (whole leading pages), for ``beagle_paged_attn_shared``.  groups: rows of each
+    group, the call's rows in their order; shared: int32 [len(groups)], written."""
+    sp = _check("shared", shared, torch.int32, (len(groups),))
+    _pages_ok(cache.lib.beagle_pages_shared(cache.ref, len(slots), _host_i32(slots), len(groups), _host_i32(groups), sp, cache.on_current_device()),
+              "beagle_pages_shared")
+
+
+def beagle_paged_attn_shared_workspace_bytes(cache: PagedCache, batch: int, n_q_heads: int, groups: Sequence[int]) -> int:
+    v = C.c_size_t()
+    _pages_ok(cache.lib.beagle_paged_attn_shared_workspace_bytes(cache.ref, batch, n_q_heads, len(groups), _host_i32(groups), C.byref(v)),
+              "beagle_paged_attn_shared_workspace_bytes")
+    return v.value
+
+
+def beagle_paged_attn_shared(cache: PagedCache, slots: Sequence[int], groups: Sequence[int], shared: torch.Tensor, q: torch.Tensor, out: torch.Tensor,
+                             lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> None:
+    """``beagle_paged_attn`` (every position visible) for groups of rows whose slots begin with the same keys and values, which are read once.
+    groups: rows of each group, the call's rows in their order; shared: int32 [len(groups)], how many positions they have in common
+    (``beagle_pages_shared``; any smaller number gives the same attention).  q, out, lse as there; ws: scratch of
+    ``beagle_paged_attn_shared_workspace_bytes`` (None: taken from torch's allocator for this call)."""
+    c, B = cache.struct, len(slots)
+    if q.dim() != 3:
+        raise ValueError("q: [batch, n_q_heads, head_dim]")
+    hq = q.shape[1]
+    qp = _check("q", q, cache.k.dtype, (B, hq, c.head_dim), False)
+    op = _check("out", out, cache.k.dtype, (B, hq, c.head_dim))
+    lp = None if lse is None else _check("lse", lse, torch.float32, (B, hq))
+    sp = _check("shared", shared, torch.int32, (len(groups),))
+    stream = cache.on_current_device()
+    if ws is None:
+        ws = torch.empty(beagle_paged_attn_shared_workspace_bytes(cache, B, hq, groups), dtype=torch.uint8, device=q.device)
+    _pages_ok(cache.lib.beagle_paged_attn_shared(cache.ref, B, _host_i32(slots), len(groups), _host_i32(groups), sp, hq, qp, _row_stride("q", q, 1), op, lp,
+                                                 *_scratch(ws), stream), "beagle_paged_attn_shared")
+
+
+def beagle_sample(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                  top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+                  logp: Optional[torch.Tensor] = None) -> None:
+    """One token per row of logits ([rows, vocab] float32 / bfloat16, rows may be strided) from the uniform numbers u (fp32 [rows], in [0, 1)),
+    into tokens (int32 [rows]).  Per row, each optional: temperature (fp32, not above 0: the largest logit), top_k (int32, not above 0: all),
+    top_p (fp32), min_p (fp32); logp (fp32 [rows], written): ln of the token's probability among those kept."""
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("logits: [rows, vocab] float32 / bfloat16")
+    rows, v = logits.shape
+    lp = _check("logits", logits, logits.dtype, (rows, v), False)
+    if v > 1 and logits.stride(1) != 1:
+        raise ValueError("logits: the values of a row must be dense")
+    stride = logits.stride(0) if rows > 1 else v
+    ptr = [None if t is None else _check(n, t, dt, (rows,)) for n, t, dt in
+           (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32))]
+    up, tp = _check("u", u, torch.float32, (rows,)), _check("tokens", tokens, torch.int32, (rows,))
+    op = None if logp is None else _check("logp", logp, torch.float32, (rows,))
+    _pages_ok(load_library().beagle_sample(lp, BEAGLE_BF16 if logits.dtype == torch.bfloat16 else BEAGLE_FP32, rows, v, stride, *ptr, up, tp, op, _stream()),
+              "beagle_sample")
+
+
 def beagle_prefill_pages(ctx: Context, cache: PagedCache, seq_slot: Sequence[int], new_len: Sequence[int], hidden: Optional[torch.Tensor],
                          ok: Optional[torch.Tensor] = None) -> None:
     """Keys and values of the target's states (packed rows, as ``beagle_prefill_kv``) into the slots' pages.  new_len: one count per
@@ -892,6 +1046,13 @@ class BeagleHead:
         out = torch.empty(B, gamma + 1, dtype=torch.int32, device=self.device)
         beagle_verify_sample(self.ctx, draft_tokens, draft_logits, target_logits, u_accept, u_resample, accept, out, temperature)
         return accept, out
+
+    def sample(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
+        """One token per row of logits, as the tensors of parameters say (``beagle_sample``): (tokens int32, their ln probabilities fp32)."""
+        tokens = torch.empty(logits.shape[0], dtype=torch.int32, device=logits.device)
+        logp = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+        beagle_sample(logits, u, tokens, temperature, top_k, top_p, min_p, logp)
+        return tokens, logp
 
     def draft_tree(self, slot, root_token, depth, topk, n_candidates):
         tok = torch.empty(n_candidates, dtype=torch.int32, device=self.device)

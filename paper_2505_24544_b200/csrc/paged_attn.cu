@@ -54,6 +54,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 struct JoinItem;
 struct PagedArgs {
+    static constexpr bool kShared = false;
+    static constexpr int kEntries = kMaxCallBatch;
     const int32_t *table, *length;
     const void *k, *v;                  // pools (the SIMT kernel; the other one has tensor maps)
     const void* q;
@@ -68,16 +70,42 @@ struct PagedArgs {
     PageSlots slots;
 };
 
-// How the visible tiles are divided; computed by every CTA from the lengths (64 values at most).
-struct Schedule {
-    int len[kMaxCallBatch];             // positions of the sequence
-    int lo[kMaxCallBatch];              // first position of the window (0: everything is visible)
-    int sink_tiles[kMaxCallBatch];      // tiles in front of the window's first one
-    int first[kMaxCallBatch];           // first tile of the window
-    int start[kMaxCallBatch + 1];       // prefix sum of (tiles * Hkv)
+// beagle_paged_attn_shared: what is walked are entries instead of the call's rows.  An entry is up to eight query rows (of the grouped
+// heads and of several rows of the call) that read the same positions of the same slot: the common part of a group for eight of its rows
+// times grouped heads, or what a row has behind it.
+struct SharedEntry {
+    uint8_t row0;                       // row of the call whose slot is read; the query rows count from its first grouped head
+    uint8_t group;                      // 255: a group of one row, all of it is read as the row's own
+    uint8_t prefix;                     // 1: the common part, 0: what lies behind it
+    uint8_t n;                          // query rows
+    uint16_t j0;                        // first one: query row j is row row0 + j / G, grouped head j % G
+};
+struct SharedArgs : PagedArgs {         // `batch` counts the entries
+    static constexpr bool kShared = true;
+    static constexpr int kEntries = 2 * kMaxCallBatch;
+    const int32_t* shared;
+    int* start;                         // [kEntries + 1] the schedule's, in the workspace
+    int rows, n_groups, n_pairs;        // rows of the call; entries * Hkv
+    SharedEntry entry[kEntries];
+    uint8_t group_of[kMaxCallBatch];    // of a row; 255 as above
+    uint8_t prefix_entry[kMaxCallBatch];        // first entry of a group's common part (the rows' own entries have the rows' numbers)
+    uint8_t group_row0[kMaxCallBatch];
+    int block;                          // query rows of a common part's entry
 };
 
-__device__ __forceinline__ int tiles_of(const Schedule& s, int b, int Hkv) { return (s.start[b + 1] - s.start[b]) / Hkv; }
+// How the visible tiles are divided; computed by every CTA from the lengths (64 values at most).
+template <int N>
+struct ScheduleOf {
+    int len[N];             // positions of the sequence
+    int lo[N];              // first position of the window (0: everything is visible)
+    int sink_tiles[N];      // tiles in front of the window's first one
+    int first[N];           // first tile of the window
+    int start[N + 1];       // prefix sum of (tiles * Hkv)
+};
+typedef ScheduleOf<kMaxCallBatch> Schedule;
+
+template <int N>
+__device__ __forceinline__ int tiles_of(const ScheduleOf<N>& s, int b, int Hkv) { return (s.start[b + 1] - s.start[b]) / Hkv; }
 // First unit of run r: floor(total * r / runs), in 32 bits (runs <= 2048).
 struct Runs {
     int total, runs, each, rest;
@@ -120,18 +148,78 @@ __device__ __forceinline__ void finish_schedule(Schedule& s) {          // secon
     if (t >= 32 && t < kMaxCallBatch) s.start[t + 1] += s.start[32];
 }
 
+// The same for the entries; whole CTA of at least 128 threads, barriers inside.  The common part of a group: shared_dev, not above its
+// shortest length, in whole tiles.
+__device__ __forceinline__ void build_schedule(const SharedArgs& a, ScheduleOf<SharedArgs::kEntries>& s) {
+    __shared__ int s_len[kMaxCallBatch], s_common[kMaxCallBatch], s_warp[4];
+    const int t = threadIdx.x, lane = t & 31;
+    if (t < a.n_groups) s_common[t] = max(__ldcg(a.shared + t), 0);
+    __syncthreads();
+    if (t < a.rows) {
+        const int n = min(max(__ldcg(a.length + a.slots.slot[t]), 0), a.max_pages << a.page_shift);
+        s_len[t] = n;
+        if (a.group_of[t] != 255) atomicMin(&s_common[a.group_of[t]], n);
+    }
+    __syncthreads();
+    int tiles = 0, incl = 0;
+    if (t < SharedArgs::kEntries) {
+        if (t < a.batch) {
+            const SharedEntry e = a.entry[t];
+            const int common = e.group == 255 ? 0 : s_common[e.group] / kTile * kTile;
+            const int n = e.prefix ? common : s_len[e.row0], lo = e.prefix ? 0 : common;
+            s.len[t] = n; s.lo[t] = lo; s.first[t] = lo / kTile; s.sink_tiles[t] = 0;
+            tiles = ((n + kTile - 1) / kTile - lo / kTile) * a.Hkv;
+        }
+        incl = tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 31) s_warp[t >> 5] = incl;
+    }
+    __syncthreads();
+    if (t < SharedArgs::kEntries) {
+        for (int i = 0; i < t >> 5; ++i) incl += s_warp[i];
+        s.start[t + 1] = incl;
+        if (t == 0) s.start[0] = 0;
+    }
+    __syncthreads();
+}
+__device__ __forceinline__ void build_schedule(const PagedArgs& a, Schedule& s) {
+    make_schedule(a, s);
+    __syncthreads();
+    finish_schedule(s);
+    __syncthreads();
+}
+
+// Where query row g of pair (b, kvh) lies, in heads: row of the call * stride, head.
+__device__ __forceinline__ int rows_of(const PagedArgs& a, int) { return a.G; }
+__device__ __forceinline__ int rows_of(const SharedArgs& a, int b) { return a.entry[b].n; }
+__device__ __forceinline__ int slot_of(const PagedArgs& a, int b) { return a.slots.slot[b]; }
+__device__ __forceinline__ int slot_of(const SharedArgs& a, int b) { return a.slots.slot[a.entry[b].row0]; }
+__device__ __forceinline__ size_t query_at(const PagedArgs& a, int b, int kvh, int g, int dh) { return (size_t)b * a.q_stride + (size_t)(kvh * a.G + g) * dh; }
+__device__ __forceinline__ size_t query_at(const SharedArgs& a, int b, int kvh, int g, int dh) {
+    const int j = a.entry[b].j0 + g, r = j / a.G;
+    return (size_t)(a.entry[b].row0 + r) * a.q_stride + (size_t)(kvh * a.G + j - r * a.G) * dh;
+}
+
 // Walks the units [u, end) of one run: for every tile the pair (b, kvh), the tile's first position and whether the pair ends.
 struct Walk {
     int b, kvh, i, n;                   // sequence, K/V head, tile index inside the pair, tiles of the pair
-    __device__ __forceinline__ void seek(const Schedule& s, int unit, int Hkv) {          // whole warps
+    template <int N>
+    __device__ __forceinline__ void seek(const ScheduleOf<N>& s, int unit, int Hkv) {          // whole warps
         const int lane = threadIdx.x & 31;
-        b = __popc(__ballot_sync(0xffffffffu, s.start[lane + 1] <= unit)) + __popc(__ballot_sync(0xffffffffu, s.start[lane + 33] <= unit));
+        b = 0;
+#pragma unroll
+        for (int x = 1; x <= N; x += 32) b += __popc(__ballot_sync(0xffffffffu, s.start[lane + x] <= unit));
         n = tiles_of(s, b, Hkv);
         const int in = unit - s.start[b];
         kvh = in / n;
         i = in - kvh * n;
     }
-    __device__ __forceinline__ void next(const Schedule& s, int batch, int Hkv) {
+    template <int N>
+    __device__ __forceinline__ void next(const ScheduleOf<N>& s, int batch, int Hkv) {
         if (++i < n) return;
         i = 0;
         if (++kvh < Hkv) return;
@@ -139,7 +227,8 @@ struct Walk {
         do { ++b; } while (b < batch && s.start[b + 1] == s.start[b]);
         if (b < batch) n = tiles_of(s, b, Hkv);
     }
-    __device__ __forceinline__ int tile(const Schedule& s) const { return i < s.sink_tiles[b] ? i : s.first[b] + i - s.sink_tiles[b]; }
+    template <int N>
+    __device__ __forceinline__ int tile(const ScheduleOf<N>& s) const { return i < s.sink_tiles[b] ? i : s.first[b] + i - s.sink_tiles[b]; }
 };
 
 // The G heads of a pair without a visible position: o = 0, lse = -inf.  Whole CTA.
@@ -181,6 +270,19 @@ __device__ __forceinline__ void begin_run(const PagedArgs& a, const Schedule& s,
     }
 }
 
+// The entries' pairs always leave partials, at a place of their own: the part of a pair that begins it at its number, a later one behind
+// them at the run's.
+template <typename T>
+__device__ __forceinline__ void begin_run(const SharedArgs& a, const ScheduleOf<SharedArgs::kEntries>& s, int, int& u0, int& u1) {
+    const Runs runs(s.start[SharedArgs::kEntries], gridDim.x);
+    u0 = runs.begin(blockIdx.x);
+    u1 = runs.begin(blockIdx.x + 1);
+    if (blockIdx.x == 0)                 // for the join
+        for (int i = threadIdx.x; i <= SharedArgs::kEntries; i += blockDim.x) a.start[i] = s.start[i];
+}
+__device__ __forceinline__ int part_at(const PagedArgs&, int, bool, int seg) { return 2 * blockIdx.x + seg; }
+__device__ __forceinline__ int part_at(const SharedArgs& a, int pair, bool begins, int) { return begins ? pair : a.n_pairs + (int)blockIdx.x; }
+
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
 }
@@ -211,15 +313,15 @@ struct PagedSmem {
 
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-template <int DH>
+template <int DH, typename Args>
 __global__ void __launch_bounds__((kConsumers + 1) * 32, kCtasPerSm)
-paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PagedArgs a) {
+paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Args a) {
     using SM = PagedSmem<DH>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
     float* join = reinterpret_cast<float*>(gen + kStages * 2 * SM::kTileBytes);
-    __shared__ Schedule s;
+    __shared__ ScheduleOf<Args::kEntries> s;
     __shared__ __align__(8) uint64_t bars[2 * kStages];
     __shared__ float s_m[kConsumers][8], s_l[kConsumers][8];
     __shared__ int s_abort;
@@ -233,10 +335,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
     pdl_launch_dependents();
     pdl_wait();                          // lengths, table, cache and queries may come from the previous launches
-    make_schedule(a, s);
-    __syncthreads();
-    finish_schedule(s);
-    __syncthreads();
+    build_schedule(a, s);
     int u0, u1;
     begin_run<bf16>(a, s, DH, u0, u1);
     if (u0 >= u1) return;
@@ -256,7 +355,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             const int pos = x.tile(s) * kTile + lane * rows;
             int id = -1;
             // (a part without a visible position stays what it was: its weights and its V rows count as 0)
-            if (lane < parts && pos < s.len[x.b] && (pos + rows > s.lo[x.b] || pos < a.sinks)) id = __ldcg(a.table + (size_t)a.slots.slot[x.b] * a.max_pages + (pos >> a.page_shift));
+            if (lane < parts && pos < s.len[x.b] && (pos + rows > s.lo[x.b] || pos < a.sinks)) id = __ldcg(a.table + (size_t)slot_of(a, x.b) * a.max_pages + (pos >> a.page_shift));
             return (id >= 0 && id < a.n_pages) ? id : -1;
         };
         next_page = page_of(w);
@@ -312,11 +411,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         const int pair = w.b * a.Hkv + w.kvh;
         if (pair != have_q) {
             have_q = pair;
-            const uint32_t* qrow = reinterpret_cast<const uint32_t*>(static_cast<const bf16*>(a.q) + (size_t)w.b * a.q_stride + (size_t)(w.kvh * a.G + (g < a.G ? g : 0)) * DH);
+            const bool some = g < rows_of(a, w.b);
+            const uint32_t* qrow = reinterpret_cast<const uint32_t*>(static_cast<const bf16*>(a.q) + query_at(a, w.b, w.kvh, some ? g : 0, DH));
 #pragma unroll
             for (int ks = 0; ks < DH / 16; ++ks) {
-                qa[ks][0] = g < a.G ? __ldcg(qrow + ks * 8 + c) : 0u;
-                qa[ks][1] = g < a.G ? __ldcg(qrow + ks * 8 + 4 + c) : 0u;
+                qa[ks][0] = some ? __ldcg(qrow + ks * 8 + c) : 0u;
+                qa[ks][1] = some ? __ldcg(qrow + ks * 8 + 4 + c) : 0u;
             }
         }
         const int st = step % kStages;
@@ -423,16 +523,16 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             }
             consumers_sync();
         }
-        if (warp == 0 && g < a.G) {
+        if (warp == 0 && g < rows_of(a, b)) {
             const int head = kvh * a.G + g;
-            if (last && !first_pair_open) {                      // all of the pair's tiles were in this run
+            if (!Args::kShared && last && !first_pair_open) {    // all of the pair's tiles were in this run
                 const float inv = L != 0.f ? 1.f / L : 0.f;
                 uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<bf16*>(a.o) + ((size_t)b * a.Hq + head) * DH) + c;
 #pragma unroll
                 for (int i = 0; i < DH / 8; ++i) dst[4 * i] = pack2(o[i][0] * inv, o[i][1] * inv);
                 if (c == 0 && a.lse != nullptr) a.lse[(size_t)b * a.Hq + head] = L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
             } else {
-                float* dst = a.part + ((size_t)(2 * blockIdx.x + seg) * 8 + g) * (DH + 2);
+                float* dst = a.part + ((size_t)part_at(a, b * a.Hkv + kvh, !first_pair_open, seg) * 8 + g) * (DH + 2);
 #pragma unroll
                 for (int i = 0; i < DH / 8; ++i) *reinterpret_cast<float2*>(dst + 8 * i + 2 * c) = make_float2(o[i][0], o[i][1]);
                 if (c == 0) { dst[DH] = M; dst[DH + 1] = L; }
@@ -466,14 +566,14 @@ struct SimtCfg {
     static_assert(kPer % KPW == 0 && kRing >= 2, "shape");
     static __device__ __forceinline__ int owner(int h) { return GM > LPK ? h / HV : h * kSpan; }      // the lane of a group that keeps head h
 };
-template <typename T, int DH, int GM>
-__global__ void __launch_bounds__((SimtCfg<T, DH, GM>::kWarps + 1) * 32, 2) paged_attn_simt_kernel(const __grid_constant__ PagedArgs a) {
+template <typename T, int DH, int GM, typename Args>
+__global__ void __launch_bounds__((SimtCfg<T, DH, GM>::kWarps + 1) * 32, 2) paged_attn_simt_kernel(const __grid_constant__ Args a) {
     using S = SimtCfg<T, DH, GM>;
     constexpr int VN = S::VN, LPK = S::LPK, KPW = S::KPW, HV = S::HV, kSteps = S::kSteps;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
     float* s_o = reinterpret_cast<float*>(ring + S::kRing * S::kStage);                  // [kWarps / 2][GM][DH]
-    __shared__ Schedule s;
+    __shared__ ScheduleOf<Args::kEntries> s;
     __shared__ __align__(8) uint64_t bars[2 * S::kRing];
     __shared__ float s_m[S::kWarps][GM], s_l[S::kWarps][GM];
     __shared__ int s_abort;
@@ -486,10 +586,7 @@ __global__ void __launch_bounds__((SimtCfg<T, DH, GM>::kWarps + 1) * 32, 2) page
     }
     pdl_launch_dependents();
     pdl_wait();
-    make_schedule(a, s);
-    __syncthreads();
-    finish_schedule(s);
-    __syncthreads();
+    build_schedule(a, s);
     int u0, u1;
     begin_run<T>(a, s, DH, u0, u1);
     if (u0 >= u1) return;
@@ -509,7 +606,7 @@ __global__ void __launch_bounds__((SimtCfg<T, DH, GM>::kWarps + 1) * 32, 2) page
                 int page = -1;
                 // (a part without a visible position stays what it was: its weights and its V rows count as 0)
                 if (lane < parts && pos < s.len[w.b] && (pos + rows > s.lo[w.b] || pos < a.sinks))
-                    page = __ldcg(a.table + (size_t)a.slots.slot[w.b] * a.max_pages + (pos >> a.page_shift));
+                    page = __ldcg(a.table + (size_t)slot_of(a, w.b) * a.max_pages + (pos >> a.page_shift));
                 if (page >= a.n_pages) page = -1;
                 const int copies = __popc(__ballot_sync(0xffffffffu, page >= 0));
                 ok = mbar_wait(empty + 8 * st, ph ^ 1, &s_abort);
@@ -565,8 +662,8 @@ __global__ void __launch_bounds__((SimtCfg<T, DH, GM>::kWarps + 1) * 32, 2) page
             have_q = pair;
 #pragma unroll
             for (int h = 0; h < GM; ++h)
-                if (h < a.G) {
-                    const uint4 x = __ldcg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (size_t)w.b * a.q_stride + (size_t)(w.kvh * a.G + h) * DH + sub * VN));
+                if (h < rows_of(a, w.b)) {
+                    const uint4 x = __ldcg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + query_at(a, w.b, w.kvh, h, DH) + sub * VN));
                     unpack16<T>(x, q[h]);
                 }
         }
@@ -717,8 +814,8 @@ __global__ void __launch_bounds__((SimtCfg<T, DH, GM>::kWarps + 1) * 32, 2) page
 #pragma unroll
                 for (int i = 0; i < VN; ++i) s_o[(warp * GM + h) * DH + sub * VN + i] += o[h][i];
         meet();
-        const bool whole = last && !first_pair_open;
-        for (int i = threadIdx.x; i < a.G * DH; i += S::kWarps * 32) {
+        const bool whole = !Args::kShared && last && !first_pair_open;
+        for (int i = threadIdx.x; i < rows_of(a, b) * DH; i += S::kWarps * 32) {
             const int h = i / DH, d = i % DH;
             float M = -INFINITY, L = 0.f, acc = 0.f;
 #pragma unroll
@@ -732,7 +829,7 @@ __global__ void __launch_bounds__((SimtCfg<T, DH, GM>::kWarps + 1) * 32, 2) page
                 static_cast<T*>(a.o)[((size_t)b * a.Hq + head) * DH + d] = from_float<T>(L != 0.f ? acc / L : 0.f);
                 if (d == 0 && a.lse != nullptr) a.lse[(size_t)b * a.Hq + head] = L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
             } else {
-                float* dst = a.part + ((size_t)(2 * blockIdx.x + seg) * 8 + h) * (DH + 2);
+                float* dst = a.part + ((size_t)part_at(a, b * a.Hkv + kvh, !first_pair_open, seg) * 8 + h) * (DH + 2);
                 dst[d] = acc;
                 if (d == 0) { dst[DH] = M; dst[DH + 1] = L; }
             }
@@ -800,6 +897,103 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
     }
 }
 
+// The same for rows of groups: blockIdx.x = row of the call, blockIdx.y = query head; the partials of the common part and of the row's own.
+template <typename T, int DH>
+__global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(const __grid_constant__ SharedArgs a, int n_runs) {
+    constexpr int kPer = (DH + 31) / 32;
+    __shared__ float s_o[kJoinWarps][DH], s_m[kJoinWarps], s_l[kJoinWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int b = blockIdx.x, head = blockIdx.y, kvh = head / a.G, h = head - kvh * a.G, group = a.group_of[b];
+    const Runs runs(__ldcg(a.start + SharedArgs::kEntries), n_runs);
+    // the two pairs, their runs, and this head's row in their partials
+    int pair[2], r0[2], r1[2], at[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        int e = b;
+        at[x] = h;
+        if (x == 1 && group != 255) {
+            const int j = (b - a.group_row0[group]) * a.G + h;
+            e = a.prefix_entry[group] + j / a.block;
+            at[x] = j % a.block;
+        }
+        const int s0 = __ldcg(a.start + e), n = (__ldcg(a.start + e + 1) - s0) / a.Hkv, u0 = s0 + kvh * n;
+        pair[x] = e * a.Hkv + kvh;
+        r0[x] = 0;
+        r1[x] = -1;
+        if (n > 0 && (x == 0 || group != 255)) { r0[x] = runs.of(u0); r1[x] = runs.of(u0 + n - 1); }
+    }
+    const bool gaps = runs.total < runs.runs;                    // fewer tiles than runs: some runs between are empty and left no partial
+    const int n0 = r1[0] - r0[0] + 1, all = n0 + r1[1] - r0[1] + 1;
+    auto part = [&](int i) -> const float* {                     // NULL: no partial
+        const int x = i < n0 ? 0 : 1, r = x == 0 ? r0[0] + i : r0[1] + i - n0;
+        if (gaps && runs.begin(r) >= runs.begin(r + 1)) return nullptr;
+        return a.part + ((size_t)(r == r0[x] ? pair[x] : a.n_pairs + r) * 8 + at[x]) * (DH + 2);
+    };
+    float M = -INFINITY, L = 0.f, acc[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
+    for (int i = warp * 32 + lane; i < all; i += kJoinWarps * 32) {
+        const float* p = part(i);
+        if (p != nullptr) M = fmaxf(M, __ldcg(p + DH));
+    }
+    M = warp_max(M);
+    if (lane == 0) s_m[warp] = M;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kJoinWarps; ++i) M = fmaxf(M, s_m[i]);
+#pragma unroll 4
+    for (int i = warp; i < all; i += kJoinWarps) {
+        const float* p = part(i);
+        if (p == nullptr) continue;
+        const float m = __ldcg(p + DH);
+        const float f = m == -INFINITY ? 0.f : exp2f(m - M);
+        L += m == -INFINITY ? __ldcg(p + DH + 1) : f * __ldcg(p + DH + 1);
+#pragma unroll
+        for (int x = 0; x < kPer; ++x)
+            if (lane + 32 * x < DH) acc[x] = fmaf(f, __ldcg(p + lane + 32 * x), acc[x]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (lane + 32 * i < DH) s_o[warp][lane + 32 * i] = acc[i];
+    if (lane == 0) s_l[warp] = L;
+    __syncthreads();
+    T* out = static_cast<T*>(a.o) + ((size_t)b * a.Hq + head) * DH;
+    for (int d = threadIdx.x; d < DH; d += kJoinWarps * 32) {
+        float x = 0.f, y = 0.f;
+#pragma unroll
+        for (int i = 0; i < kJoinWarps; ++i) { x += s_o[i][d]; y += s_l[i]; }
+        out[d] = from_float<T>(y != 0.f ? x / y : 0.f);
+        if (d == 0 && a.lse != nullptr) a.lse[(size_t)b * a.Hq + head] = y != 0.f ? (M + log2f(y)) * kLn2 : -INFINITY;
+    }
+}
+
+// beagle_pages_shared: blockIdx.x = group.  The first page at which the table rows of its slots differ or the shortest of them ends.
+__global__ void __launch_bounds__(256) pages_shared_kernel(const int32_t* table, const int32_t* length, const __grid_constant__ PageSlots slots,
+                                                         const __grid_constant__ PageSlots first_row, const __grid_constant__ PageSlots n_rows, int page_size,
+                                                         int max_pages, int32_t* shared) {
+    __shared__ int s_pages;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int g = blockIdx.x, r0 = first_row.slot[g], n = n_rows.slot[g], t = threadIdx.x;
+    if (t == 0) s_pages = n > 1 ? max_pages : 0;
+    __syncthreads();
+    if (t < n) atomicMin(&s_pages, max(__ldcg(length + slots.slot[r0 + t]), 0) / page_size);
+    __syncthreads();
+    const int32_t* lead = table + (size_t)slots.slot[r0] * max_pages;
+    const int pages = s_pages;
+    __syncthreads();
+    for (int r = 1; r < n; ++r) {
+        const int32_t* row = table + (size_t)slots.slot[r0 + r] * max_pages;
+        for (int i = t; i < pages; i += 256)
+            if (__ldcg(row + i) != __ldcg(lead + i)) { atomicMin(&s_pages, i); break; }
+    }
+    __syncthreads();
+    if (t == 0) shared[g] = s_pages * page_size;
+}
+
+constexpr size_t kStartBytes = 1024;     // the schedule's offsets, in front of the shared form's partials
 constexpr int kMaxRuns = 2048;           // bound of the workspace; the grid is min(this, CTAs that fit the GPU)
 constexpr int kSimtCtasPerSm = 2;
 // Pairs of at most this many tiles are not cut: the join launch takes some 3 us, a tile on its own 0.4 (tensor cores), 0.9 (up to four
@@ -819,8 +1013,17 @@ bool whole_pairs(const beagle_pages* p, int Hq, int window, int sinks) {
     return most_tiles(p, window, sinks) <= (uses_mma(p) ? kWholeTiles : Hq / p->n_kv_heads <= 4 ? kWholeTilesSimt : kWholeTilesMany);
 }
 
-template <int DH>
-beagle_status launch_mma(const beagle_pages* p, const PagedArgs& a, int runs, cudaStream_t stream) {
+template <typename T, int DH>
+void launch_join(const PagedArgs& a, int runs, cudaStream_t stream) {
+    if (!a.whole) launch_pdl(paged_attn_join_kernel<T, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a);
+}
+template <typename T, int DH>
+void launch_join(const SharedArgs& a, int runs, cudaStream_t stream) {
+    launch_pdl(paged_shared_join_kernel<T, DH>, dim3(a.rows, a.Hq), dim3(kJoinWarps * 32), 0, stream, a, runs);
+}
+
+template <int DH, typename Args>
+beagle_status launch_mma(const beagle_pages* p, const Args& a, int runs, cudaStream_t stream) {
     using SM = PagedSmem<DH>;
     const EncodeTiled encode = tensor_map_encoder();
     if (encode == nullptr) return BEAGLE_ERR_CUDA;
@@ -834,34 +1037,103 @@ beagle_status launch_mma(const beagle_pages* p, const PagedArgs& a, int runs, cu
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return BEAGLE_ERR_CUDA;
     static PerDeviceOnce smem_attr;
-    if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes) == cudaSuccess; }))
+    if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_kernel<DH, Args>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes) == cudaSuccess; }))
         return BEAGLE_ERR_CUDA;
-    launch_pdl(paged_attn_kernel<DH>, dim3(runs), dim3((kConsumers + 1) * 32), (size_t)SM::kBytes, stream, mk, mv, a);
-    if (!a.whole) launch_pdl(paged_attn_join_kernel<bf16, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a);
+    launch_pdl(paged_attn_kernel<DH, Args>, dim3(runs), dim3((kConsumers + 1) * 32), (size_t)SM::kBytes, stream, mk, mv, a);
+    launch_join<bf16, DH>(a, runs, stream);
     return BEAGLE_OK;
 }
 
-template <typename T, int DH, int GM>
-beagle_status launch_simt_heads(const PagedArgs& a, int runs, cudaStream_t stream) {
+template <typename T, int DH, int GM, typename Args>
+beagle_status launch_simt_heads(const Args& a, int runs, cudaStream_t stream) {
     using S = SimtCfg<T, DH, GM>;
     static PerDeviceOnce smem_attr;
-    if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_simt_kernel<T, DH, GM>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) == cudaSuccess; }))
+    if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_simt_kernel<T, DH, GM, Args>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) == cudaSuccess; }))
         return BEAGLE_ERR_CUDA;
-    launch_pdl(paged_attn_simt_kernel<T, DH, GM>, dim3(runs), dim3((S::kWarps + 1) * 32), (size_t)S::kBytes, stream, a);
+    launch_pdl(paged_attn_simt_kernel<T, DH, GM, Args>, dim3(runs), dim3((S::kWarps + 1) * 32), (size_t)S::kBytes, stream, a);
     return BEAGLE_OK;
 }
 
-template <typename T, int DH>
-beagle_status launch_simt(const PagedArgs& a, int runs, cudaStream_t stream) {
+template <typename T, int DH, typename Args>
+beagle_status launch_simt(const Args& a, int runs, cudaStream_t stream) {
     beagle_status st;
-    if (a.G == 1) st = launch_simt_heads<T, DH, 1>(a, runs, stream);
-    else if (a.G <= 2) st = launch_simt_heads<T, DH, 2>(a, runs, stream);
-    else if (a.G <= 4) st = launch_simt_heads<T, DH, 4>(a, runs, stream);
-    else if constexpr (DH < 256) st = launch_simt_heads<T, DH, 8>(a, runs, stream);
-    else return BEAGLE_ERR_SHAPE;
+    if constexpr (Args::kShared) {                       // entries of the common part have as many rows as a kernel takes
+        st = launch_simt_heads<T, DH, DH < 256 ? 8 : 4>(a, runs, stream);
+    } else {
+        if (a.G == 1) st = launch_simt_heads<T, DH, 1>(a, runs, stream);
+        else if (a.G <= 2) st = launch_simt_heads<T, DH, 2>(a, runs, stream);
+        else if (a.G <= 4) st = launch_simt_heads<T, DH, 4>(a, runs, stream);
+        else if constexpr (DH < 256) st = launch_simt_heads<T, DH, 8>(a, runs, stream);
+        else return BEAGLE_ERR_SHAPE;
+    }
     if (st != BEAGLE_OK) return st;
-    if (!a.whole) launch_pdl(paged_attn_join_kernel<T, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a);
+    launch_join<T, DH>(a, runs, stream);
     return BEAGLE_OK;
+}
+
+template <typename Args>
+beagle_status launch_attn(const beagle_pages* p, const Args& a, int runs, cudaStream_t stream) {
+    beagle_status st;
+    if (uses_mma(p)) st = p->head_dim == 128 ? launch_mma<128>(p, a, runs, stream) : launch_mma<64>(p, a, runs, stream);
+    else if (p->dtype == BEAGLE_BF16) st = p->head_dim == 256 ? launch_simt<bf16, 256>(a, runs, stream) : launch_simt<bf16, 32>(a, runs, stream);
+    else if (p->head_dim == 128) st = launch_simt<float, 128>(a, runs, stream);
+    else if (p->head_dim == 64) st = launch_simt<float, 64>(a, runs, stream);
+    else if (p->head_dim == 32) st = launch_simt<float, 32>(a, runs, stream);
+    else st = launch_simt<float, 16>(a, runs, stream);
+    if (st != BEAGLE_OK) return st;
+    return cudaGetLastError() == cudaSuccess ? BEAGLE_OK : BEAGLE_ERR_CUDA;
+}
+
+// The call's arguments that both forms share, from checked values.
+void fill_args(const beagle_pages* p, int Hq, const void* q, int64_t q_stride, void* out, float* lse, PagedArgs* a) {
+    a->table = p->table; a->length = p->length; a->k = p->k; a->v = p->v; a->q = q; a->o = out; a->lse = lse;
+    a->q_stride = q_stride;
+    a->n_pages = p->n_pages; a->max_pages = p->max_pages;
+    a->page_shift = 0;
+    while ((1 << a->page_shift) < p->page_size) ++a->page_shift;
+    a->Hq = Hq; a->Hkv = p->n_kv_heads; a->G = Hq / p->n_kv_heads;
+    a->scale_log2 = 1.4426950408889634f / sqrtf((float)p->head_dim);
+}
+// Checks of the queries, outputs and workspace.
+beagle_status check_call(const beagle_pages* p, int Hq, const void* q, int64_t q_stride, const void* out, const float* lse, const void* ws, size_t ws_bytes, size_t need) {
+    const int e = p->dtype == BEAGLE_BF16 ? 2 : 4;
+    if (q == nullptr || out == nullptr || (need > 0 && ws == nullptr) || q_stride < (int64_t)Hq * p->head_dim) return BEAGLE_ERR_INVALID_ARG;
+    if ((((uintptr_t)q | (uintptr_t)out | (uintptr_t)ws) & 15) || (q_stride * e) % 16 || ((uintptr_t)lse & 3)) return BEAGLE_ERR_INVALID_ARG;
+    return ws_bytes < need ? BEAGLE_ERR_CAPACITY : BEAGLE_OK;
+}
+// Slots of a call, in range; a slot may be read by several rows.
+beagle_status check_rows(const beagle_pages* p, int batch, const int32_t* slot_host, PageSlots* out) {
+    if (batch < 0 || (batch > 0 && slot_host == nullptr)) return BEAGLE_ERR_INVALID_ARG;
+    if (batch > kMaxCallBatch) return BEAGLE_ERR_CAPACITY;
+    for (int i = 0; i < batch; ++i) {
+        if (slot_host[i] < 0 || slot_host[i] >= p->max_slots) return BEAGLE_ERR_INVALID_ARG;
+        out->slot[i] = slot_host[i];
+    }
+    return BEAGLE_OK;
+}
+beagle_status check_groups(int batch, int n_groups, const int32_t* group_rows) {
+    if (batch < 0 || n_groups < 0 || (n_groups > 0 && group_rows == nullptr)) return BEAGLE_ERR_INVALID_ARG;
+    if (batch > kMaxCallBatch) return BEAGLE_ERR_CAPACITY;
+    int64_t sum = 0;
+    for (int i = 0; i < n_groups && i <= kMaxCallBatch; ++i) {
+        if (group_rows[i] < 1) return BEAGLE_ERR_INVALID_ARG;
+        sum += group_rows[i];
+    }
+    return sum == batch && n_groups <= batch ? BEAGLE_OK : BEAGLE_ERR_INVALID_ARG;
+}
+
+// Query rows of a common part's entry: what the kernel takes as grouped heads.
+int entry_rows(const beagle_pages* p) { return p->dtype == BEAGLE_BF16 && p->head_dim == 256 ? 4 : 8; }
+int count_entries(const beagle_pages* p, int Hq, int batch, int n_groups, const int32_t* group_rows) {
+    const int G = Hq / p->n_kv_heads, block = entry_rows(p);
+    int n = batch;
+    for (int i = 0; i < n_groups; ++i)
+        if (group_rows[i] > 1) n += (group_rows[i] * G + block - 1) / block;
+    return n;
+}
+int shared_runs(const beagle_pages* p) {
+    const int runs = device_sm_count() * (uses_mma(p) ? kCtasPerSm : kSimtCtasPerSm);
+    return runs < kMaxRuns ? runs : kMaxRuns;
 }
 
 beagle_status check_heads(const beagle_pages* p, int Hq) {
@@ -933,50 +1205,99 @@ beagle_status beagle_paged_attn(const beagle_pages* p, int32_t batch, const int3
     if (st != BEAGLE_OK) return st;
     PagedArgs a;
     memset(&a, 0, sizeof(a));
-    if (batch < 0 || (batch > 0 && slot_host == nullptr)) return BEAGLE_ERR_INVALID_ARG;
-    if (batch > kMaxCallBatch) return BEAGLE_ERR_CAPACITY;
-    for (int i = 0; i < batch; ++i) {                   // a slot may be read by several rows of the call
-        if (slot_host[i] < 0 || slot_host[i] >= p->max_slots) return BEAGLE_ERR_INVALID_ARG;
-        a.slots.slot[i] = slot_host[i];
-    }
+    st = check_rows(p, batch, slot_host, &a.slots);
+    if (st != BEAGLE_OK) return st;
     st = check_heads(p, n_q_heads);
     if (st != BEAGLE_OK) return st;
     if (window < 0 || sinks < 0) return BEAGLE_ERR_INVALID_ARG;
     if (batch == 0) return BEAGLE_OK;
-    const int e = p->dtype == BEAGLE_BF16 ? 2 : 4;
     size_t need = 0;
     beagle_paged_attn_workspace_bytes(p, n_q_heads, window, sinks, &need);
-    if (q_dev == nullptr || out_dev == nullptr || (need > 0 && ws_dev == nullptr) || q_stride < (int64_t)n_q_heads * p->head_dim) return BEAGLE_ERR_INVALID_ARG;
-    if ((((uintptr_t)q_dev | (uintptr_t)out_dev | (uintptr_t)ws_dev) & 15) || (q_stride * e) % 16 || ((uintptr_t)lse_dev & 3)) return BEAGLE_ERR_INVALID_ARG;
-    if (ws_bytes < need) return BEAGLE_ERR_CAPACITY;
+    st = check_call(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, ws_dev, ws_bytes, need);
+    if (st != BEAGLE_OK) return st;
     if (!paged_attn_fits(p, batch)) return BEAGLE_ERR_CAPACITY;
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    a.table = p->table; a.length = p->length; a.k = p->k; a.v = p->v; a.q = q_dev; a.o = out_dev; a.lse = lse_dev;
-    a.q_stride = q_stride;
-    a.batch = batch; a.n_pages = p->n_pages; a.max_pages = p->max_pages;
-    a.page_shift = 0;
-    while ((1 << a.page_shift) < p->page_size) ++a.page_shift;
-    a.Hq = n_q_heads; a.Hkv = p->n_kv_heads; a.G = n_q_heads / p->n_kv_heads;
+    fill_args(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, &a);
+    a.batch = batch;
     a.window = window; a.sinks = sinks;
-    a.scale_log2 = 1.4426950408889634f / sqrtf((float)p->head_dim);
     // no more runs than the cache's capacity has tiles
     const long long most = (long long)batch * p->n_kv_heads * most_tiles(p, window, sinks);
-    const bool mma = uses_mma(p);
     a.whole = whole_pairs(p, n_q_heads, window, sinks) ? 1 : 0;
-    long long runs = (long long)device_sm_count() * (mma ? kCtasPerSm : kSimtCtasPerSm);
+    long long runs = (long long)device_sm_count() * (uses_mma(p) ? kCtasPerSm : kSimtCtasPerSm);
     if (runs > kMaxRuns) runs = kMaxRuns;
     if (runs > most) runs = most;
     if (a.whole) runs = (long long)batch * p->n_kv_heads;
     a.join = static_cast<JoinItem*>(ws_dev);
     a.part = a.whole ? nullptr : reinterpret_cast<float*>(a.join + runs);
-    if (mma) st = p->head_dim == 128 ? launch_mma<128>(p, a, (int)runs, stream) : launch_mma<64>(p, a, (int)runs, stream);
-    else if (p->dtype == BEAGLE_BF16) st = p->head_dim == 256 ? launch_simt<bf16, 256>(a, (int)runs, stream) : launch_simt<bf16, 32>(a, (int)runs, stream);
-    else if (p->head_dim == 128) st = launch_simt<float, 128>(a, (int)runs, stream);
-    else if (p->head_dim == 64) st = launch_simt<float, 64>(a, (int)runs, stream);
-    else if (p->head_dim == 32) st = launch_simt<float, 32>(a, (int)runs, stream);
-    else st = launch_simt<float, 16>(a, (int)runs, stream);
+    return launch_attn(p, a, (int)runs, static_cast<cudaStream_t>(stream_));
+}
+
+beagle_status beagle_pages_shared(const beagle_pages* p, int32_t batch, const int32_t* slot_host, int32_t n_groups, const int32_t* group_rows_host,
+                                  int32_t* shared_dev, void* stream) {
+    beagle_status st = pages_check(p);
     if (st != BEAGLE_OK) return st;
+    PageSlots slots, first, count;
+    st = check_rows(p, batch, slot_host, &slots);
+    if (st != BEAGLE_OK) return st;
+    st = check_groups(batch, n_groups, group_rows_host);
+    if (st != BEAGLE_OK || n_groups == 0) return st;
+    if (shared_dev == nullptr || ((uintptr_t)shared_dev & 3)) return BEAGLE_ERR_INVALID_ARG;
+    for (int i = 0, r = 0; i < n_groups; r += group_rows_host[i++]) { first.slot[i] = r; count.slot[i] = group_rows_host[i]; }
+    launch_pdl(pages_shared_kernel, dim3(n_groups), dim3(256), 0, static_cast<cudaStream_t>(stream), p->table, p->length, slots, first, count, p->page_size,
+               p->max_pages, shared_dev);
     return cudaGetLastError() == cudaSuccess ? BEAGLE_OK : BEAGLE_ERR_CUDA;
+}
+
+beagle_status beagle_paged_attn_shared_workspace_bytes(const beagle_pages* p, int32_t batch, int32_t n_q_heads, int32_t n_groups,
+                                                       const int32_t* group_rows_host, size_t* bytes) {
+    if (p == nullptr || bytes == nullptr || p->n_kv_heads <= 0 || p->max_pages <= 0) return BEAGLE_ERR_INVALID_ARG;
+    if (!pages_valid_shape(p)) return BEAGLE_ERR_SHAPE;
+    beagle_status st = check_heads(p, n_q_heads);
+    if (st != BEAGLE_OK) return st;
+    st = check_groups(batch, n_groups, group_rows_host);
+    if (st != BEAGLE_OK) return st;
+    const size_t parts = (size_t)count_entries(p, n_q_heads, batch, n_groups, group_rows_host) * p->n_kv_heads + shared_runs(p);
+    *bytes = (kStartBytes + parts * 8 * (p->head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+    return BEAGLE_OK;
+}
+
+beagle_status beagle_paged_attn_shared(const beagle_pages* p, int32_t batch, const int32_t* slot_host, int32_t n_groups, const int32_t* group_rows_host,
+                                       const int32_t* shared_dev, int32_t n_q_heads, const void* q_dev, int64_t q_stride, void* out_dev, float* lse_dev,
+                                       void* ws_dev, size_t ws_bytes, void* stream_) {
+    beagle_status st = pages_check(p);
+    if (st != BEAGLE_OK) return st;
+    SharedArgs a;
+    memset(static_cast<void*>(&a), 0, sizeof(a));
+    st = check_rows(p, batch, slot_host, &a.slots);
+    if (st != BEAGLE_OK) return st;
+    size_t need = 0;
+    st = beagle_paged_attn_shared_workspace_bytes(p, batch, n_q_heads, n_groups, group_rows_host, &need);
+    if (st != BEAGLE_OK) return st;
+    if (batch == 0) return BEAGLE_OK;
+    if (shared_dev == nullptr || ((uintptr_t)shared_dev & 3)) return BEAGLE_ERR_INVALID_ARG;
+    st = check_call(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, ws_dev, ws_bytes, need);
+    if (st != BEAGLE_OK) return st;
+    fill_args(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, &a);
+    a.block = entry_rows(p);
+    int e = batch;                                       // the rows' own entries first
+    for (int i = 0, r = 0; i < n_groups; r += group_rows_host[i++]) {
+        const int R = group_rows_host[i];
+        a.group_row0[i] = (uint8_t)r;
+        a.prefix_entry[i] = (uint8_t)e;
+        for (int x = 0; x < R; ++x) {
+            a.group_of[r + x] = R > 1 ? (uint8_t)i : (uint8_t)255;
+            a.entry[r + x] = {(uint8_t)(r + x), a.group_of[r + x], 0, (uint8_t)a.G, 0};
+        }
+        for (int j = 0; R > 1 && j < R * a.G; j += a.block)
+            a.entry[e++] = {(uint8_t)r, (uint8_t)i, 1, (uint8_t)(R * a.G - j < a.block ? R * a.G - j : a.block), (uint16_t)j};
+    }
+    if (!paged_attn_fits(p, e)) return BEAGLE_ERR_CAPACITY;
+    a.batch = e; a.rows = batch; a.n_groups = n_groups; a.n_pairs = e * p->n_kv_heads;
+    a.shared = shared_dev;
+    a.start = static_cast<int*>(ws_dev);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + kStartBytes);
+    const long long most = (long long)a.n_pairs * most_tiles(p, 0, 0);
+    const int runs = shared_runs(p);
+    return launch_attn(p, a, (int)(runs < most ? runs : most), static_cast<cudaStream_t>(stream_));
 }
 
 }  // extern "C"

@@ -14,6 +14,7 @@
 #include <cstring>
 
 #include "pages.h"
+#include "rotary.cuh"
 #include "tensor_map.h"
 
 using namespace beagle;
@@ -241,6 +242,18 @@ __global__ void __launch_bounds__(kBookThreads) pages_append_book_kernel(const B
     }
 }
 
+// The filled positions of one head of the page that is copied before it is written.  dv: 16-byte pieces of a head's row.
+__device__ __forceinline__ void copy_tail(const Book& b, const AppendRow& r, uint4* K, uint4* V, int heads, int h, int dv) {
+    const int used = r.len % b.page_size;
+    if (!b.page_ok(r.cow_src) || !b.page_ok(r.cow_dst)) return;
+    const size_t from = ((size_t)r.cow_src * heads + h) * b.page_size * dv, to = ((size_t)r.cow_dst * heads + h) * b.page_size * dv;
+    for (int i = threadIdx.x; i < used * dv; i += kMoveThreads) {
+        const uint4 x = K[from + i], y = V[from + i];
+        K[to + i] = x;
+        V[to + i] = y;
+    }
+}
+
 // Rows of the append, and the valid part of every page that is copied before it is written.  blockIdx.y = row of the call;
 // blockIdx.x < chunks: that many 16-byte pieces of its new rows (keys, then values); past them: one CTA per K/V head for the copy.
 __global__ void __launch_bounds__(kMoveThreads) pages_append_write_kernel(const Book b, const __grid_constant__ PageSlots slots,
@@ -254,15 +267,7 @@ __global__ void __launch_bounds__(kMoveThreads) pages_append_write_kernel(const 
     const AppendRow r = ws.rows[row];
     const int dv = 1 << piece_shift;                     // 16-byte pieces of one head's row
     if ((int)blockIdx.x >= chunks) {
-        const int used = r.len % b.page_size;
-        if (!b.page_ok(r.cow_src) || !b.page_ok(r.cow_dst)) return;
-        const int h = blockIdx.x - chunks;
-        const size_t from = ((size_t)r.cow_src * heads + h) * b.page_size * dv, to = ((size_t)r.cow_dst * heads + h) * b.page_size * dv;
-        for (int i = threadIdx.x; i < used * dv; i += kMoveThreads) {
-            const uint4 x = K[from + i], y = V[from + i];
-            K[to + i] = x;
-            V[to + i] = y;
-        }
+        copy_tail(b, r, K, V, heads, blockIdx.x - chunks, dv);
         return;
     }
     const int per_pos = heads << piece_shift;
@@ -293,6 +298,97 @@ __global__ void __launch_bounds__(kMoveThreads) pages_append_write_kernel(const 
             K[at[u]] = x[u];
             V[at[u]] = y[u];
         }
+}
+
+// The same with the keys, and the queries that come along, rotated at the positions that the rows take (rotary.cuh).  blockIdx.x < chunks:
+// g.rows tokens of the row; a thread keeps the cosines and sines of its unit and walks over the token's heads, its key and value of
+// a head in flight together.
+struct RotaryRowsArgs {
+    const void *k_new, *v_new, *q;
+    void *K, *V, *q_out;
+    long long k_stride, v_stride, q_stride;              // elements
+    const int32_t* n_new;
+    int heads, Hq, dh, T, q_offset, chunks;
+    RotaryGrid g;
+};
+constexpr int kRotFlight = 4;                            // heads a thread has in flight
+
+template <typename T, int E, bool INTER>
+__global__ void __launch_bounds__(kRotThreads) pages_append_rotary_kernel(const Book b, const __grid_constant__ PageSlots slots,
+                                                                         const __grid_constant__ RotaryArgs rot, const __grid_constant__ RotaryRowsArgs a) {
+    static_assert(kRotThreads == kMoveThreads, "copy_tail walks with kMoveThreads");
+    __shared__ __align__(16) float2 s_cs[kRotEntries];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int row = blockIdx.y, t = threadIdx.x;
+    const BookWs ws = book_ws(b.ws, b.n_pages);
+    const AppendRow r = ws.rows[row];
+    if ((int)blockIdx.x >= a.chunks) {
+        copy_tail(b, r, static_cast<uint4*>(a.K), static_cast<uint4*>(a.V), a.heads, blockIdx.x - a.chunks, a.dh * (int)sizeof(T) / 16);
+        return;
+    }
+    const int n_q = a.Hq == 0 ? 0 : a.n_new != nullptr ? min(max(__ldcg(a.n_new + row), 0), a.T) : a.T;
+    const int tok0 = blockIdx.x * a.g.rows, n = max(r.n, n_q);
+    if (tok0 >= n) return;
+    const int n_here = min(a.g.rows, n - tok0);
+    const int u = t % a.g.units, slot = t / a.g.units, rl = slot / a.g.lanes, lane = slot - rl * a.g.lanes, tok = tok0 + rl;
+    const long long srow = (long long)row * a.T + tok;
+    const bool mine = rl < n_here;
+    typedef RotUnit<T, E, INTER> Unit;
+    typedef typename Unit::V V;
+    // keys (queries where q_offset is 0 too)
+    for (int i = t; i < n_here * rot.pairs; i += kRotThreads) s_cs[i] = rot_angle(rot.turns[i % rot.pairs], r.len + tok0 + i / rot.pairs, rot.m, rot.sign);
+    __syncthreads();
+    Unit unit;
+    unit.init(u, rot.pairs, s_cs + min(rl, n_here - 1) * rot.pairs);
+    if (mine && tok < r.n) {
+        const int shift = __ffs(b.page_size) - 1, pos = r.len + tok;
+        const int page = __ldcg(b.row(slots.slot[row]) + (pos >> shift));
+        const T *k = static_cast<const T*>(a.k_new) + srow * a.k_stride, *v = static_cast<const T*>(a.v_new) + srow * a.v_stride;
+        const size_t at = ((((size_t)max(page, 0) * a.heads) << shift) + (pos & (b.page_size - 1))) * a.dh;
+        const size_t step = ((size_t)1 << shift) * a.dh;
+        if (b.page_ok(page))
+            for (int h0 = lane; h0 < a.heads; h0 += a.g.lanes * kRotFlight) {
+                V x[kRotFlight], y[kRotFlight], z[kRotFlight], w[kRotFlight];
+#pragma unroll
+                for (int i = 0; i < kRotFlight; ++i) {
+                    const int h = h0 + i * a.g.lanes;
+                    if (h < a.heads) { unit.load(k + h * a.dh, x[i], y[i]); unit.load(v + h * a.dh, z[i], w[i]); }
+                }
+#pragma unroll
+                for (int i = 0; i < kRotFlight; ++i) {
+                    const int h = h0 + i * a.g.lanes;
+                    if (h < a.heads) {
+                        unit.turn(x[i], y[i]);
+                        unit.store(static_cast<T*>(a.K) + at + h * step, x[i], y[i]);
+                        unit.store(static_cast<T*>(a.V) + at + h * step, z[i], w[i]);
+                    }
+                }
+            }
+    }
+    if (n_q == 0) return;                                // (the whole CTA)
+    if (a.q_offset != 0) {
+        __syncthreads();                                 // every thread has its keys' entries
+        for (int i = t; i < n_here * rot.pairs; i += kRotThreads)
+            s_cs[i] = rot_angle(rot.turns[i % rot.pairs], r.len + a.q_offset + tok0 + i / rot.pairs, rot.m, rot.sign);
+        __syncthreads();
+        unit.init(u, rot.pairs, s_cs + min(rl, n_here - 1) * rot.pairs);
+    }
+    if (!mine || tok >= n_q) return;
+    const T* q = static_cast<const T*>(a.q) + srow * a.q_stride;
+    T* qo = static_cast<T*>(a.q_out) + srow * a.Hq * a.dh;
+    for (int h0 = lane; h0 < a.Hq; h0 += a.g.lanes * kRotFlight) {
+        V x[kRotFlight], y[kRotFlight];
+#pragma unroll
+        for (int i = 0; i < kRotFlight; ++i)
+            if (h0 + i * a.g.lanes < a.Hq) unit.load(q + (h0 + i * a.g.lanes) * a.dh, x[i], y[i]);
+#pragma unroll
+        for (int i = 0; i < kRotFlight; ++i)
+            if (h0 + i * a.g.lanes < a.Hq) {
+                unit.turn(x[i], y[i]);
+                unit.store(qo + (h0 + i * a.g.lanes) * a.dh, x[i], y[i]);
+            }
+    }
 }
 
 __global__ void __launch_bounds__(128) pages_truncate_kernel(const Book b, const PageSlots slots, const int32_t* keep) {
@@ -552,6 +648,58 @@ beagle_status beagle_pages_append(const beagle_pages* p, int32_t batch, const in
         rows.count[b] = T;
     }
     return pages_append_rows(p, batch, slot_host, rows, n_new_dev, k_new_dev, k_stride, v_new_dev, v_stride, ok_dev, static_cast<cudaStream_t>(stream));
+}
+
+beagle_status beagle_pages_append_rotary(const beagle_pages* p, const beagle_rotary* rot, int32_t batch, const int32_t* slot_host, int32_t T,
+                                         const int32_t* n_new_dev, const void* k_new_dev, int64_t k_stride, const void* v_new_dev, int64_t v_stride,
+                                         int32_t n_q_heads, const void* q_dev, int64_t q_stride, void* q_out_dev, int32_t q_offset, int32_t* ok_dev, void* stream_) {
+    beagle_status st = pages_check(p);
+    if (st != BEAGLE_OK) return st;
+    st = rotary_check(rot, p->dtype);
+    if (st != BEAGLE_OK) return st;
+    if (rot->head_dim != p->head_dim) return BEAGLE_ERR_SHAPE;
+    PageSlots slots;
+    st = pages_check_slots(p, batch, slot_host, &slots);
+    if (st != BEAGLE_OK) return st;
+    if (T < 0 || n_q_heads < 0 || q_offset < 0) return BEAGLE_ERR_INVALID_ARG;
+    if (n_q_heads > 65535) return BEAGLE_ERR_SHAPE;
+    if (T > 0x20000000 || q_offset > 0x1fffffff) return BEAGLE_ERR_CAPACITY;             // a slot has less than 2^30 positions: all in 31 bits
+    if (batch == 0) return BEAGLE_OK;
+    const int e = elt_bytes(p), width = p->n_kv_heads * p->head_dim;
+    if (T > 0) {
+        if (k_new_dev == nullptr || v_new_dev == nullptr || k_stride < width || v_stride < width) return BEAGLE_ERR_INVALID_ARG;
+        if ((((uintptr_t)k_new_dev | (uintptr_t)v_new_dev) & 15) || (k_stride * e) % 16 || (v_stride * e) % 16) return BEAGLE_ERR_INVALID_ARG;
+        if (n_q_heads > 0) {
+            if (q_dev == nullptr || q_out_dev == nullptr || q_stride < (int64_t)n_q_heads * p->head_dim) return BEAGLE_ERR_INVALID_ARG;
+            if ((((uintptr_t)q_dev | (uintptr_t)q_out_dev) & 15) || (q_stride * e) % 16) return BEAGLE_ERR_INVALID_ARG;
+            if (q_dev == q_out_dev && q_stride != (int64_t)n_q_heads * p->head_dim) return BEAGLE_ERR_INVALID_ARG;
+        }
+    }
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    AppendRows rows;
+    for (int b = 0; b < kMaxCallBatch; ++b) {
+        rows.start[b] = (long long)b * T;
+        rows.count[b] = T;
+    }
+    RotaryArgs r;
+    rotary_args(rot, 0, &r);
+    RotaryRowsArgs a;
+    memset(&a, 0, sizeof(a));
+    a.k_new = k_new_dev; a.v_new = v_new_dev; a.q = q_dev; a.K = p->k; a.V = p->v; a.q_out = q_out_dev;
+    a.k_stride = k_stride; a.v_stride = v_stride; a.q_stride = q_stride;
+    a.n_new = n_new_dev;
+    a.heads = p->n_kv_heads; a.Hq = T > 0 ? n_q_heads : 0; a.dh = p->head_dim; a.T = T; a.q_offset = q_offset;
+    a.g = rotary_grid(rot, p->dtype, (long long)batch * T, p->n_kv_heads > a.Hq ? p->n_kv_heads : a.Hq);
+    a.chunks = (T + a.g.rows - 1) / a.g.rows;
+    launch_pdl(pages_append_book_kernel, dim3(1), dim3(kBookThreads), 0, stream, book_of(p), slots, rows, batch, n_new_dev, ok_dev);
+    if (T > 0) {
+        const dim3 grid((unsigned)(a.chunks + p->n_kv_heads), batch);
+#define BEAGLE_ROTARY_LAUNCH(TY, E, INTER) launch_pdl(pages_append_rotary_kernel<TY, E, INTER>, grid, dim3(kRotThreads), 0, stream, book_of(p), slots, r, a)
+        if (p->dtype == BEAGLE_BF16) BEAGLE_ROTARY_DISPATCH(bf16, rotary_unit(rot, p->dtype), rot->interleaved, BEAGLE_ROTARY_LAUNCH);
+        else BEAGLE_ROTARY_DISPATCH(float, rotary_unit(rot, p->dtype), rot->interleaved, BEAGLE_ROTARY_LAUNCH);
+#undef BEAGLE_ROTARY_LAUNCH
+    }
+    return launched();
 }
 
 beagle_status beagle_pages_truncate(const beagle_pages* p, int32_t n, const int32_t* slot_host, const int32_t* keep_dev, void* stream) {

@@ -1,0 +1,198 @@
+"""Sampling from given uniform numbers, against the definition in 64 bits."""
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_24544_b200 import binding as b
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def draw(row, t, k, p, mp, u):
+    """Token and ln probability; row: float64 array without NaN."""
+    order = np.argsort(-row, kind="stable")
+    top = row[order[0]]
+    if top == -math.inf:
+        return -1, math.nan
+    if not t > 0:
+        return int(order[0]), 0.0
+    if 0 < k < len(order):
+        order = order[:k]
+    if p <= 0 or mp > 1:
+        order = order[:1]
+    with np.errstate(invalid="ignore"):
+        d = np.where(row[order] == top, 0.0, (row[order] - top) / t)
+    d = np.where(np.isnan(d) | (row[order] == -math.inf), -math.inf, d)          # infinite temperature below an infinite logit; masked
+    if p < 1:
+        run = np.cumsum(np.exp(d))
+        n = min(int(np.searchsorted(run, p * run[-1], side="left")) + 1, len(order))
+        order, d = order[:n], d[:n]
+    if mp > 0:
+        keep = d >= math.log(mp)
+        keep[0] = True
+        order, d = order[keep], d[keep]
+    at = np.argsort(order, kind="stable")
+    ids, w = order[at], np.exp(d[at])
+    run = np.cumsum(w)
+    i = min(int(np.searchsorted(run, u * run[-1], side="right")), len(ids) - 1)
+    return int(ids[i]), float(d[at][i] - math.log(run[-1]))
+
+
+def check(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
+    """Weights are off by 2^-46 of the largest and 2^-45 of themselves at most: a sum of V of them, relative to the total, by less than
+    (V + 2) 2^-45.  A border that a sum comes nearer to may fall to either side: tokens of either are right."""
+    rows, v = logits.shape
+    dev = lambda x, dt: None if x is None else torch.tensor(x, dtype=dt, device="cuda")
+    tokens, logp = torch.full((rows,), -7, dtype=torch.int32, device="cuda"), torch.full((rows,), 7.0, device="cuda")
+    b.beagle_sample(logits, dev(u, torch.float32), tokens, dev(temperature, torch.float32), dev(top_k, torch.int32), dev(top_p, torch.float32),
+                    dev(min_p, torch.float32), logp)
+    z = logits.detach().cpu().double().numpy()
+    z = np.where(np.isnan(z), -math.inf, z)
+    f32 = lambda x: float(np.float32(x))
+    eps = (v + 2) * 2.0 ** -45
+    for i in range(rows):
+        t = 1.0 if temperature is None else f32(temperature[i])
+        k = 0 if top_k is None else top_k[i]
+        p = 1.0 if top_p is None or not f32(top_p[i]) < 1 else f32(top_p[i])
+        mp = 0.0 if min_p is None or not f32(min_p[i]) > 0 else f32(min_p[i])
+        ui = min(max(f32(u[i]), 0.0), 1.0)
+        want = {}
+        for dp in ([0.0] if p >= 1 or p <= 0 else [0.0, -eps, eps]):
+            for du in (0.0, -eps, eps):
+                tok, lp = draw(z[i], t, k, min(p + dp, 1.0), mp, min(max(ui + du, 0.0), 1.0 - 2.0 ** -53))
+                want.setdefault(tok, []).append(lp)
+        got, lp = int(tokens[i]), float(logp[i])
+        assert got in want, (i, got, want, t, k, p, mp, ui)
+        if got == -1:
+            assert math.isnan(lp)
+        else:
+            # the total's relative error, double arithmetic, one rounding to fp32
+            assert min(abs(lp - x) for x in want[got]) <= 2 * eps + 2.0 ** -24 * abs(lp) + 2.0 ** -40, (lp, want[got])
+    again = torch.empty_like(tokens)
+    b.beagle_sample(logits, dev(u, torch.float32), again, dev(temperature, torch.float32), dev(top_k, torch.int32), dev(top_p, torch.float32),
+                    dev(min_p, torch.float32))
+    assert torch.equal(tokens, again)
+    return tokens.tolist()
+
+
+def noise(rows, v, std, dtype, seed=0):
+    return (torch.randn(rows, v, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda") * std).to(DT[dtype])
+
+
+def params(rows, seed, v):
+    r = random.Random(seed)
+    return dict(u=[r.random() for _ in range(rows)], temperature=[r.choice([0.0, 0.3, 0.8, 1.0, 1.7]) for _ in range(rows)],
+                top_k=[r.choice([0, -1, 1, 2, 40, 700, v, v + 5]) for _ in range(rows)], top_p=[r.choice([1.0, 0.1, 0.5, 0.9, 0.999, 2.0]) for _ in range(rows)],
+                min_p=[r.choice([0.0, 0.01, 0.3, 1.0]) for _ in range(rows)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,v", [(1, 1), (3, 2), (40, 33), (20, 1000), (5, 4099), (9, 32000), (40, 8193), (1, 128256), (3, 262144), (150, 20001)])
+@pytest.mark.parametrize("std", [0.05, 3.0, 20.0])
+def test_mixed_requests(dtype, rows, v, std):
+    """bf16 logits have many equal values, std 0.05 a nearly flat distribution (whole vocabularies inside a filter)."""
+    check(noise(rows, v, std, dtype, rows + v), **params(rows, v, v))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("only", ["temperature", "top_k", "top_p", "min_p"])
+def test_one_filter(dtype, only):
+    rows, v = 33, 50257
+    p = params(rows, 5, v)
+    check(noise(rows, v, 2.0, dtype, 8), u=p["u"], **{only: p[only]})
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_many_equal_logits(dtype):
+    """Borders inside long runs of equal logits: the lower ids are kept.  (More of them than are compared pairwise.)"""
+    v = 30011
+    z = torch.zeros(8, v, dtype=DT[dtype], device="cuda")
+    z[:, ::3] = 1.0
+    z[:, 1::3] = -2.0
+    z[:, 7] = 2.0
+    us = [0.0, 0.3, 0.999, 0.5, 0.25, 0.75, 0.9999, 0.1]
+    check(z, us, top_k=[1, 2, 5000, 10001, 10005, 25000, 29999, 600])
+    check(z, us, top_p=[0.001, 0.1, 0.5, 0.9, 0.95, 0.99, 0.9999, 0.6])
+    check(z, us, top_k=[20000] * 8, top_p=[0.001, 0.1, 0.5, 0.9, 0.95, 0.99, 0.9999, 0.6], temperature=[0.5, 1, 2, 4, 1, 1, 9, 1])
+
+
+def test_borders_that_are_exact():
+    """Equal weights: sums are exact on both sides, so are the borders."""
+    v = 4096
+    z = torch.full((6, v), 3.5, device="cuda")
+    tokens = check(z, [0.0, 0.25, 0.5, 0.75, 0.25, 0.5], top_p=[1.0, 1.0, 1.0, 1.0, 0.5, 0.25])
+    assert tokens[:3] == [0, 1024, 2048] and tokens[4:] == [512, 512]
+    tokens = check(z, [0.0, 0.25, 0.5, 0.75, 0.25, 0.5], top_k=[4, 4, 4, 4, 1000, 0])
+    assert tokens == [0, 1, 2, 3, 250, 2048]
+
+
+@pytest.mark.parametrize("low", [-1e4, -3.0e38, -math.inf, math.nan])
+def test_masked_tokens(low):
+    """Masks of every kind, NaN among them, in rows that keep a few tokens, one, and none."""
+    v = 20000
+    z = torch.full((6, v), low, device="cuda")
+    z[0, [5, 700, 19999]] = torch.tensor([1.0, 2.0, 1.5], device="cuda")
+    z[1, 12345] = -7.0
+    z[3, :9000] = noise(1, 9000, 2.0, "fp32", 4)[0]
+    z[4, 100] = -3.0e38
+    p = dict(u=[0.5, 0.9, 0.9, 0.3, 0.7, 0.0])
+    check(z, **p)
+    check(z, **p, temperature=[1.0, 0.5, 0.0, 2.0, 0.1, 1.0], top_k=[2, 0, 0, 50, 3, 0], top_p=[0.9, 0.5, 1.0, 0.8, 0.9, 0.9])
+    tokens = check(z, **p, top_k=[2, 2, 2, 2, 2, 2], min_p=[0.5] * 6)
+    if low != low or low == -math.inf:
+        assert tokens[2] == -1 and tokens[5] == -1
+    check(torch.nan_to_num(z, nan=low, neginf=low).to(torch.bfloat16), **p, top_p=[0.9] * 6)
+
+
+def test_infinite_logits_and_parameters_at_their_ends():
+    z = noise(12, 5000, 2.0, "fp32", 3)
+    z[0, [17, 40]] = math.inf
+    z[1, 3] = math.inf
+    z[2, 3] = math.inf
+    inf, nan = math.inf, math.nan
+    check(z, u=[0.9, 0.2, 0.5, 0.0, 1.0, 0.99999994, 0.5, 0.5, 0.5, 0.5, 0.5, 0.5], temperature=[1.0, 0.0, inf, inf, 1e-30, 1e-3, 1e30, nan, -1.0, 1.0, 1.0, 1.0],
+          top_p=[0.9, 0.9, 1.0, 1.0, 0.9, 1e-30, 0.5, 0.5, 0.5, 0.0, -1.0, nan], min_p=[0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 2.0])
+    check(z, u=[0.5] * 12, min_p=[nan, 1.0, 1.5, 0.5, -1.0, 0.0, 1e-30, 1e-8, 0.1, 0.2, 0.3, 0.9])
+
+
+def test_unaligned_and_strided_rows_another_stream():
+    big = noise(7, 4099 + 13, 3.0, "bf16", 5)
+    side = torch.cuda.Stream()
+    for off in (0, 1, 3, 8, 13):
+        part = big[:, off:off + 4099]
+        check(part, **params(7, off, 4099))
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            check(part.float()[:, 1:], **params(7, off, 4098))
+    torch.cuda.synchronize()
+
+
+def test_captured_and_replayed_with_new_numbers():
+    z, u = noise(4, 32000, 3.0, "fp32", 6), torch.rand(4, device="cuda")
+    tokens, temp = torch.empty(4, dtype=torch.int32, device="cuda"), torch.full((4,), 0.7, device="cuda")
+    b.beagle_sample(z, u, tokens, temperature=temp)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        b.beagle_sample(z, u, tokens, temperature=temp)
+    for i in range(5):
+        u.copy_(torch.rand(4, generator=torch.Generator(device="cuda").manual_seed(i), device="cuda"))
+        z.copy_(noise(4, 32000, 3.0, "fp32", 100 + i))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert tokens.tolist() == check(z, u.tolist(), temperature=[0.7] * 4)
+
+
+def test_frequencies_follow_the_weights():
+    """Evenly spaced numbers through the inverse distribution: every token as often as its share, to within one."""
+    n = 5000
+    z = torch.tensor([[0.0, 1.0, -1.0, 2.0, 0.5]], device="cuda").repeat(n, 1)
+    u = (torch.arange(n, device="cuda") + 0.5) / n
+    tokens = torch.empty(n, dtype=torch.int32, device="cuda")
+    b.beagle_sample(z, u, tokens)
+    share = torch.softmax(z[0].double(), 0) * n
+    assert bool(((torch.bincount(tokens.long(), minlength=5).double() - share).abs() <= 1.0).all())
