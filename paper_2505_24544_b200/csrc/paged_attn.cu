@@ -34,6 +34,7 @@
 #include <cstring>
 
 #include "pages.h"
+#include "paged_attn.cuh"
 #include "tc_ptx.cuh"
 #include "tensor_map.h"
 
@@ -44,192 +45,10 @@ namespace {
 
 using namespace tc;
 
-constexpr int kTile = 64;               // cached positions per tile
 constexpr int kConsumers = 4;           // warps; each owns 16 positions of a tile
 constexpr int kPerWarp = kTile / kConsumers;
 constexpr int kStages = 3;
 constexpr int kCtasPerSm = 2;
-constexpr float kSlack = 8.f;           // how far (log2) a score may exceed the row's reference point before it moves
-constexpr float kLn2 = 0.6931471805599453f;
-
-struct JoinItem;
-struct PagedArgs {
-    static constexpr bool kShared = false;
-    static constexpr int kEntries = kMaxCallBatch;
-    const int32_t *table, *length;
-    const void *k, *v;                  // pools (the SIMT kernel; the other one has tensor maps)
-    const void* q;
-    void* o;
-    float* lse;                         // [batch, Hq] or NULL
-    JoinItem* join;                     // [runs]
-    float* part;                        // [2 * runs][8][dh + 2]: unnormalised O, then maximum (log2 units) and sum
-    long long q_stride;
-    int batch, n_pages, page_shift, max_pages, Hq, Hkv, G, window, sinks;
-    int whole;                          // every (sequence, K/V head) pair is one run
-    float scale_log2;
-    PageSlots slots;
-};
-
-// beagle_paged_attn_shared: what is walked are entries instead of the call's rows.  An entry is up to eight query rows (of the grouped
-// heads and of several rows of the call) that read the same positions of the same slot: the common part of a group for eight of its rows
-// times grouped heads, or what a row has behind it.
-struct SharedEntry {
-    uint8_t row0;                       // row of the call whose slot is read; the query rows count from its first grouped head
-    uint8_t group;                      // 255: a group of one row, all of it is read as the row's own
-    uint8_t prefix;                     // 1: the common part, 0: what lies behind it
-    uint8_t n;                          // query rows
-    uint16_t j0;                        // first one: query row j is row row0 + j / G, grouped head j % G
-};
-struct SharedArgs : PagedArgs {         // `batch` counts the entries
-    static constexpr bool kShared = true;
-    static constexpr int kEntries = 2 * kMaxCallBatch;
-    const int32_t* shared;
-    int* start;                         // [kEntries + 1] the schedule's, in the workspace
-    int rows, n_groups, n_pairs;        // rows of the call; entries * Hkv
-    SharedEntry entry[kEntries];
-    uint8_t group_of[kMaxCallBatch];    // of a row; 255 as above
-    uint8_t prefix_entry[kMaxCallBatch];        // first entry of a group's common part (the rows' own entries have the rows' numbers)
-    uint8_t group_row0[kMaxCallBatch];
-    int block;                          // query rows of a common part's entry
-};
-
-// How the visible tiles are divided; computed by every CTA from the lengths (64 values at most).
-template <int N>
-struct ScheduleOf {
-    int len[N];             // positions of the sequence
-    int lo[N];              // first position of the window (0: everything is visible)
-    int sink_tiles[N];      // tiles in front of the window's first one
-    int first[N];           // first tile of the window
-    int start[N + 1];       // prefix sum of (tiles * Hkv)
-};
-typedef ScheduleOf<kMaxCallBatch> Schedule;
-
-template <int N>
-__device__ __forceinline__ int tiles_of(const ScheduleOf<N>& s, int b, int Hkv) { return (s.start[b + 1] - s.start[b]) / Hkv; }
-// First unit of run r: floor(total * r / runs), in 32 bits (runs <= 2048).
-struct Runs {
-    int total, runs, each, rest;
-    __device__ __forceinline__ Runs(int t, int n) : total(t), runs(n), each(t / n), rest(t - t / n * n) {}
-    __device__ __forceinline__ int begin(int r) const { return each * r + rest * r / runs; }
-    __device__ __forceinline__ int of(int unit) const {                         // the run that holds `unit`
-        int r = min(runs - 1, (int)((float)unit * (float)runs / (float)total));
-        while (r + 1 < runs && begin(r + 1) <= unit) ++r;
-        while (r > 0 && begin(r) > unit) --r;
-        return r;
-    }
-};
-
-// Threads 0..63 of the CTA fill `s`; the caller synchronises afterwards.
-__device__ __forceinline__ void make_schedule(const PagedArgs& a, Schedule& s) {
-    const int t = threadIdx.x;
-    if (t >= kMaxCallBatch) return;
-    int tiles = 0;
-    if (t < a.batch) {
-        const int cap = a.max_pages << a.page_shift;
-        const int n = min(max(__ldcg(a.length + a.slots.slot[t]), 0), cap);
-        const int lo = (a.window > 0 && n > a.window) ? n - a.window : 0;
-        const int first = lo / kTile;
-        const int front = min((min(a.sinks, lo) + kTile - 1) / kTile, first);
-        s.len[t] = n; s.lo[t] = lo; s.first[t] = first; s.sink_tiles[t] = front;
-        tiles = (front + (n + kTile - 1) / kTile - first) * a.Hkv;
-    }
-    // inclusive sum over the 64 threads: two warps
-    int incl = tiles;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, incl, o);
-        if ((t & 31) >= o) incl += v;
-    }
-    s.start[t + 1] = incl;
-    if (t == 0) s.start[0] = 0;
-}
-__device__ __forceinline__ void finish_schedule(Schedule& s) {          // second half: the upper warp's offset; between two barriers
-    const int t = threadIdx.x;
-    if (t >= 32 && t < kMaxCallBatch) s.start[t + 1] += s.start[32];
-}
-
-// The same for the entries; whole CTA of at least 128 threads, barriers inside.  The common part of a group: shared_dev, not above its
-// shortest length, in whole tiles.
-__device__ __forceinline__ void build_schedule(const SharedArgs& a, ScheduleOf<SharedArgs::kEntries>& s) {
-    __shared__ int s_len[kMaxCallBatch], s_common[kMaxCallBatch], s_warp[4];
-    const int t = threadIdx.x, lane = t & 31;
-    if (t < a.n_groups) s_common[t] = max(__ldcg(a.shared + t), 0);
-    __syncthreads();
-    if (t < a.rows) {
-        const int n = min(max(__ldcg(a.length + a.slots.slot[t]), 0), a.max_pages << a.page_shift);
-        s_len[t] = n;
-        if (a.group_of[t] != 255) atomicMin(&s_common[a.group_of[t]], n);
-    }
-    __syncthreads();
-    int tiles = 0, incl = 0;
-    if (t < SharedArgs::kEntries) {
-        if (t < a.batch) {
-            const SharedEntry e = a.entry[t];
-            const int common = e.group == 255 ? 0 : s_common[e.group] / kTile * kTile;
-            const int n = e.prefix ? common : s_len[e.row0], lo = e.prefix ? 0 : common;
-            s.len[t] = n; s.lo[t] = lo; s.first[t] = lo / kTile; s.sink_tiles[t] = 0;
-            tiles = ((n + kTile - 1) / kTile - lo / kTile) * a.Hkv;
-        }
-        incl = tiles;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
-        }
-        if (lane == 31) s_warp[t >> 5] = incl;
-    }
-    __syncthreads();
-    if (t < SharedArgs::kEntries) {
-        for (int i = 0; i < t >> 5; ++i) incl += s_warp[i];
-        s.start[t + 1] = incl;
-        if (t == 0) s.start[0] = 0;
-    }
-    __syncthreads();
-}
-__device__ __forceinline__ void build_schedule(const PagedArgs& a, Schedule& s) {
-    make_schedule(a, s);
-    __syncthreads();
-    finish_schedule(s);
-    __syncthreads();
-}
-
-// Where query row g of pair (b, kvh) lies, in heads: row of the call * stride, head.
-__device__ __forceinline__ int rows_of(const PagedArgs& a, int) { return a.G; }
-__device__ __forceinline__ int rows_of(const SharedArgs& a, int b) { return a.entry[b].n; }
-__device__ __forceinline__ int slot_of(const PagedArgs& a, int b) { return a.slots.slot[b]; }
-__device__ __forceinline__ int slot_of(const SharedArgs& a, int b) { return a.slots.slot[a.entry[b].row0]; }
-__device__ __forceinline__ size_t query_at(const PagedArgs& a, int b, int kvh, int g, int dh) { return (size_t)b * a.q_stride + (size_t)(kvh * a.G + g) * dh; }
-__device__ __forceinline__ size_t query_at(const SharedArgs& a, int b, int kvh, int g, int dh) {
-    const int j = a.entry[b].j0 + g, r = j / a.G;
-    return (size_t)(a.entry[b].row0 + r) * a.q_stride + (size_t)(kvh * a.G + j - r * a.G) * dh;
-}
-
-// Walks the units [u, end) of one run: for every tile the pair (b, kvh), the tile's first position and whether the pair ends.
-struct Walk {
-    int b, kvh, i, n;                   // sequence, K/V head, tile index inside the pair, tiles of the pair
-    template <int N>
-    __device__ __forceinline__ void seek(const ScheduleOf<N>& s, int unit, int Hkv) {          // whole warps
-        const int lane = threadIdx.x & 31;
-        b = 0;
-#pragma unroll
-        for (int x = 1; x <= N; x += 32) b += __popc(__ballot_sync(0xffffffffu, s.start[lane + x] <= unit));
-        n = tiles_of(s, b, Hkv);
-        const int in = unit - s.start[b];
-        kvh = in / n;
-        i = in - kvh * n;
-    }
-    template <int N>
-    __device__ __forceinline__ void next(const ScheduleOf<N>& s, int batch, int Hkv) {
-        if (++i < n) return;
-        i = 0;
-        if (++kvh < Hkv) return;
-        kvh = 0;
-        do { ++b; } while (b < batch && s.start[b + 1] == s.start[b]);
-        if (b < batch) n = tiles_of(s, b, Hkv);
-    }
-    template <int N>
-    __device__ __forceinline__ int tile(const ScheduleOf<N>& s) const { return i < s.sink_tiles[b] ? i : s.first[b] + i - s.sink_tiles[b]; }
-};
 
 // The G heads of a pair without a visible position: o = 0, lse = -inf.  Whole CTA.
 template <typename T>
@@ -239,8 +58,6 @@ __device__ __forceinline__ void empty_pair(const PagedArgs& a, int b, int kvh, i
     if (a.lse != nullptr && threadIdx.x < a.G) a.lse[(size_t)b * a.Hq + kvh * a.G + threadIdx.x] = -INFINITY;
 }
 
-// What the join does for a run: the pair that begins in it and ends in a later one, if there is one.
-struct JoinItem { int pair, last_run, second, total; };          // pair: b * Hkv + kvh or -1; second: it is the run's second partial; all tiles
 
 // The units of this CTA's run; in whole mode, of its pair.  Also zeroes the pairs without a visible position (shared out over the
 // CTAs) and leaves the run's join item.  Whole CTA.
@@ -304,6 +121,13 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&t);
 }
+// A launch behind the one that does the common parts starts as soon as that one's blocks have, which they say after their own wait: all
+// that it reads is there.  It waits at its end, so that its completion still says that everything before it has completed.
+__device__ __forceinline__ void wait_inputs(const PagedArgs&) { pdl_wait(); }
+__device__ __forceinline__ void wait_prefix(const PagedArgs&) {}
+__device__ __forceinline__ void wait_inputs(const SharedArgs& a) { if (!a.after_prefix) pdl_wait(); }
+__device__ __forceinline__ void wait_prefix(const SharedArgs& a) { if (a.after_prefix) pdl_wait(); }
+
 template <int DH>
 struct PagedSmem {
     static constexpr int kTileBytes = kTile * DH * 2;                       // one of K / V
@@ -334,11 +158,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         fence_barrier_init();
     }
     pdl_launch_dependents();
-    pdl_wait();                          // lengths, table, cache and queries may come from the previous launches
+    wait_inputs(a);                      // lengths, table, cache and queries may come from the previous launches
     build_schedule(a, s);
     int u0, u1;
     begin_run<bf16>(a, s, DH, u0, u1);
-    if (u0 >= u1) return;
+    if (u0 >= u1) { wait_prefix(a); return; }
     Walk w;
     w.seek(s, u0, a.Hkv);
 
@@ -387,6 +211,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         if (!ok)                         // copies already requested still land: wait (bounded) for the last of each stage
             for (int n = max(0, issued - kStages); n < issued; ++n)
                 for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(full + 8 * (n % kStages), (n / kStages) & 1); ++i) {}
+        wait_prefix(a);
         return;
     }
 
@@ -544,6 +369,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
         for (int i = 0; i < DH / 8; ++i) o[i][0] = o[i][1] = 0.f;
     }
+    wait_prefix(a);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -897,47 +723,67 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
     }
 }
 
-// The same for rows of groups: blockIdx.x = row of the call, blockIdx.y = query head; the partials of the common part and of the row's own.
+// The same for rows of groups: blockIdx.x = row of the call, blockIdx.y = query head; the partials of the row's own positions and those of the
+// common part, which lie with the row's launch or (`prefix.on`) with the tensor cores'.
+struct PrefixParts {
+    const int* start;
+    const float* part;
+    int n_pairs, runs, part_rows, block;
+    uint8_t on[kMaxCallBatch], entry[kMaxCallBatch];
+};
 template <typename T, int DH>
-__global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(const __grid_constant__ SharedArgs a, int n_runs) {
+__global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(const __grid_constant__ SharedArgs a, const __grid_constant__ PrefixParts prefix, int n_runs) {
     constexpr int kPer = (DH + 31) / 32;
     __shared__ float s_o[kJoinWarps][DH], s_m[kJoinWarps], s_l[kJoinWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     pdl_wait();
     const int b = blockIdx.x, head = blockIdx.y, kvh = head / a.G, h = head - kvh * a.G, group = a.group_of[b];
-    const Runs runs(__ldcg(a.start + SharedArgs::kEntries), n_runs);
-    // the two pairs, their runs, and this head's row in their partials
-    int pair[2], r0[2], r1[2], at[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        int e = b;
-        at[x] = h;
-        if (x == 1 && group != 255) {
-            const int j = (b - a.group_row0[group]) * a.G + h;
-            e = a.prefix_entry[group] + j / a.block;
-            at[x] = j % a.block;
+    const bool common = group != 255, cores = common && prefix.on[group];
+    // source 0: the row's own positions, 1: the common part.  Of each the pair, the runs that worked on it, this head's row in a partial
+    struct Source {
+        const float* part;
+        size_t size;                     // floats of a partial
+        int o, ml;                       // offsets of the row's O and of its (maximum, sum)
+        int pair, n_pairs, r0, r1;
+        Runs runs;
+    };
+    auto source = [&](bool first) {
+        const bool tc = !first && cores;
+        const int* start = tc ? prefix.start : a.start;
+        Source x = {tc ? prefix.part : a.part, 0, 0, 0, 0, tc ? prefix.n_pairs : a.n_pairs, 0, -1, Runs(__ldcg(start + SharedArgs::kEntries), tc ? prefix.runs : n_runs)};
+        int e = b, at = h;
+        if (!first) {
+            const int j = common ? (b - a.group_row0[group]) * a.G + h : 0, block = tc ? prefix.block : a.block;
+            e = common ? (tc ? prefix.entry[group] : a.prefix_entry[group]) + j / block : 0;
+            at = j % block;
         }
-        const int s0 = __ldcg(a.start + e), n = (__ldcg(a.start + e + 1) - s0) / a.Hkv, u0 = s0 + kvh * n;
-        pair[x] = e * a.Hkv + kvh;
-        r0[x] = 0;
-        r1[x] = -1;
-        if (n > 0 && (x == 0 || group != 255)) { r0[x] = runs.of(u0); r1[x] = runs.of(u0 + n - 1); }
-    }
-    const bool gaps = runs.total < runs.runs;                    // fewer tiles than runs: some runs between are empty and left no partial
-    const int n0 = r1[0] - r0[0] + 1, all = n0 + r1[1] - r0[1] + 1;
-    auto part = [&](int i) -> const float* {                     // NULL: no partial
-        const int x = i < n0 ? 0 : 1, r = x == 0 ? r0[0] + i : r0[1] + i - n0;
-        if (gaps && runs.begin(r) >= runs.begin(r + 1)) return nullptr;
-        return a.part + ((size_t)(r == r0[x] ? pair[x] : a.n_pairs + r) * 8 + at[x]) * (DH + 2);
+        const int rows = tc ? prefix.part_rows : 8, s0 = __ldcg(start + e), n = (__ldcg(start + e + 1) - s0) / a.Hkv, u0 = s0 + kvh * n;
+        x.size = (size_t)rows * (DH + 2);
+        x.o = tc ? at * DH : at * (DH + 2);
+        x.ml = tc ? rows * DH + 2 * at : at * (DH + 2) + DH;
+        x.pair = e * a.Hkv + kvh;
+        if (n > 0 && (first || common)) { x.r0 = x.runs.of(u0); x.r1 = x.runs.of(u0 + n - 1); }
+        return x;
+    };
+    const Source own = source(true), shared = source(false);
+    const int n0 = own.r1 - own.r0 + 1, all = n0 + shared.r1 - shared.r0 + 1;
+    // partial i; false: none (fewer tiles than runs: some runs between are empty)
+    auto part = [&](int i, const float*& o, const float*& ml) {
+        const Source& x = i < n0 ? own : shared;
+        const int r = x.r0 + (i < n0 ? i : i - n0);
+        if (x.runs.total < x.runs.runs && x.runs.begin(r) >= x.runs.begin(r + 1)) return false;
+        const float* p = x.part + (size_t)(r == x.r0 ? x.pair : x.n_pairs + r) * x.size;
+        o = p + x.o;
+        ml = p + x.ml;
+        return true;
     };
     float M = -INFINITY, L = 0.f, acc[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
-    for (int i = warp * 32 + lane; i < all; i += kJoinWarps * 32) {
-        const float* p = part(i);
-        if (p != nullptr) M = fmaxf(M, __ldcg(p + DH));
-    }
+    const float *o, *ml;
+    for (int i = warp * 32 + lane; i < all; i += kJoinWarps * 32)
+        if (part(i, o, ml)) M = fmaxf(M, __ldcg(ml));
     M = warp_max(M);
     if (lane == 0) s_m[warp] = M;
     __syncthreads();
@@ -945,14 +791,13 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(cons
     for (int i = 0; i < kJoinWarps; ++i) M = fmaxf(M, s_m[i]);
 #pragma unroll 4
     for (int i = warp; i < all; i += kJoinWarps) {
-        const float* p = part(i);
-        if (p == nullptr) continue;
-        const float m = __ldcg(p + DH);
+        if (!part(i, o, ml)) continue;
+        const float m = __ldcg(ml);
         const float f = m == -INFINITY ? 0.f : exp2f(m - M);
-        L += m == -INFINITY ? __ldcg(p + DH + 1) : f * __ldcg(p + DH + 1);
+        L += m == -INFINITY ? __ldcg(ml + 1) : f * __ldcg(ml + 1);
 #pragma unroll
         for (int x = 0; x < kPer; ++x)
-            if (lane + 32 * x < DH) acc[x] = fmaf(f, __ldcg(p + lane + 32 * x), acc[x]);
+            if (lane + 32 * x < DH) acc[x] = fmaf(f, __ldcg(o + lane + 32 * x), acc[x]);
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
@@ -1017,14 +862,20 @@ template <typename T, int DH>
 void launch_join(const PagedArgs& a, int runs, cudaStream_t stream) {
     if (!a.whole) launch_pdl(paged_attn_join_kernel<T, DH>, dim3(runs, a.G), dim3(kJoinWarps * 32), 0, stream, a);
 }
+struct SharedCall : SharedArgs {         // the rows' launch, and where the tensor cores' partials are
+    PrefixParts prefix;
+};
 template <typename T, int DH>
-void launch_join(const SharedArgs& a, int runs, cudaStream_t stream) {
-    launch_pdl(paged_shared_join_kernel<T, DH>, dim3(a.rows, a.Hq), dim3(kJoinWarps * 32), 0, stream, a, runs);
+void launch_join(const SharedCall& a, int runs, cudaStream_t stream) {
+    launch_pdl(paged_shared_join_kernel<T, DH>, dim3(a.rows, a.Hq), dim3(kJoinWarps * 32), 0, stream, static_cast<const SharedArgs&>(a), a.prefix, runs);
 }
+template <typename Args> struct KernelArgs { typedef PagedArgs type; };
+template <> struct KernelArgs<SharedCall> { typedef SharedArgs type; };
 
 template <int DH, typename Args>
 beagle_status launch_mma(const beagle_pages* p, const Args& a, int runs, cudaStream_t stream) {
     using SM = PagedSmem<DH>;
+    typedef typename KernelArgs<Args>::type KArgs;
     const EncodeTiled encode = tensor_map_encoder();
     if (encode == nullptr) return BEAGLE_ERR_CUDA;
     CUtensorMap mk, mv;
@@ -1037,9 +888,9 @@ beagle_status launch_mma(const beagle_pages* p, const Args& a, int runs, cudaStr
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return BEAGLE_ERR_CUDA;
     static PerDeviceOnce smem_attr;
-    if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_kernel<DH, Args>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes) == cudaSuccess; }))
+    if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_kernel<DH, KArgs>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes) == cudaSuccess; }))
         return BEAGLE_ERR_CUDA;
-    launch_pdl(paged_attn_kernel<DH, Args>, dim3(runs), dim3((kConsumers + 1) * 32), (size_t)SM::kBytes, stream, mk, mv, a);
+    launch_pdl(paged_attn_kernel<DH, KArgs>, dim3(runs), dim3((kConsumers + 1) * 32), (size_t)SM::kBytes, stream, mk, mv, static_cast<const KArgs&>(a));
     launch_join<bf16, DH>(a, runs, stream);
     return BEAGLE_OK;
 }
@@ -1047,10 +898,11 @@ beagle_status launch_mma(const beagle_pages* p, const Args& a, int runs, cudaStr
 template <typename T, int DH, int GM, typename Args>
 beagle_status launch_simt_heads(const Args& a, int runs, cudaStream_t stream) {
     using S = SimtCfg<T, DH, GM>;
+    typedef typename KernelArgs<Args>::type KArgs;
     static PerDeviceOnce smem_attr;
-    if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_simt_kernel<T, DH, GM, Args>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) == cudaSuccess; }))
+    if (!smem_attr.ensure([] { return cudaFuncSetAttribute(paged_attn_simt_kernel<T, DH, GM, KArgs>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) == cudaSuccess; }))
         return BEAGLE_ERR_CUDA;
-    launch_pdl(paged_attn_simt_kernel<T, DH, GM, Args>, dim3(runs), dim3((S::kWarps + 1) * 32), (size_t)S::kBytes, stream, a);
+    launch_pdl(paged_attn_simt_kernel<T, DH, GM, KArgs>, dim3(runs), dim3((S::kWarps + 1) * 32), (size_t)S::kBytes, stream, static_cast<const KArgs&>(a));
     return BEAGLE_OK;
 }
 
@@ -1122,18 +974,59 @@ beagle_status check_groups(int batch, int n_groups, const int32_t* group_rows) {
     return sum == batch && n_groups <= batch ? BEAGLE_OK : BEAGLE_ERR_INVALID_ARG;
 }
 
+// Groups with more query rows than this (rows times grouped heads) have their common part on the tensor cores' 128-row tiles, the others in
+// entries of eight rows.
+constexpr int kFewRows = 16;
+
 // Query rows of a common part's entry: what the kernel takes as grouped heads.
 int entry_rows(const beagle_pages* p) { return p->dtype == BEAGLE_BF16 && p->head_dim == 256 ? 4 : 8; }
-int count_entries(const beagle_pages* p, int Hq, int batch, int n_groups, const int32_t* group_rows) {
-    const int G = Hq / p->n_kv_heads, block = entry_rows(p);
-    int n = batch;
-    for (int i = 0; i < n_groups; ++i)
-        if (group_rows[i] > 1) n += (group_rows[i] * G + block - 1) / block;
-    return n;
+
+// The entries of a call, from checked groups.
+void plan_shared(const beagle_pages* p, int Hq, int batch, int n_groups, const int32_t* group_rows, SharedCall* a, PrefixArgs* f) {
+    const int G = Hq / p->n_kv_heads;
+    a->block = entry_rows(p);
+    f->block = prefix_block(G);
+    int e = batch, fe = 0, most = 0;                     // the rows' own entries first
+    for (int i = 0, r = 0; i < n_groups; r += group_rows[i++]) {
+        const int R = group_rows[i], rows = R * G;
+        f->on[i] = a->prefix.on[i] = R > 1 && uses_mma(p) && rows > kFewRows;
+        a->group_row0[i] = (uint8_t)r;
+        a->prefix_entry[i] = (uint8_t)e;
+        a->prefix.entry[i] = (uint8_t)fe;
+        for (int x = 0; x < R; ++x) {
+            a->group_of[r + x] = R > 1 ? (uint8_t)i : (uint8_t)255;
+            a->entry[r + x] = {(uint8_t)(r + x), a->group_of[r + x], 0, (uint8_t)G, 0};
+        }
+        if (R == 1) continue;
+        const int block = f->on[i] ? f->block : a->block;
+        for (int j = 0; j < rows; j += block) {
+            const int n = rows - j < block ? rows - j : block;
+            const SharedEntry x = {(uint8_t)r, (uint8_t)i, 1, (uint8_t)n, (uint16_t)j};
+            if (f->on[i]) { f->entry[fe++] = x; most = n > most ? n : most; }
+            else a->entry[e++] = x;
+        }
+    }
+    memcpy(f->group_of, a->group_of, sizeof(f->group_of));
+    a->batch = e;
+    a->rows = f->rows = batch;
+    a->n_groups = f->n_groups = n_groups;
+    a->n_pairs = e * p->n_kv_heads;
+    f->batch = fe;
+    f->n_pairs = fe * p->n_kv_heads;
+    f->part_rows = (most + 3) / 4 * 4;
+    a->after_prefix = fe > 0;
 }
 int shared_runs(const beagle_pages* p) {
     const int runs = device_sm_count() * (uses_mma(p) ? kCtasPerSm : kSimtCtasPerSm);
     return runs < kMaxRuns ? runs : kMaxRuns;
+}
+// Bytes of the call's workspace and where the two launches' partials begin.
+size_t shared_ws(const beagle_pages* p, const SharedArgs& a, const PrefixArgs& f, size_t* own, size_t* common) {
+    const size_t row = (size_t)(p->head_dim + 2) * sizeof(float), mine = 2 * kStartBytes,
+                 theirs = mine + ((size_t)(a.n_pairs + shared_runs(p)) * 8 * row + 255) / 256 * 256;
+    if (own != nullptr) *own = mine;
+    if (common != nullptr) *common = theirs;
+    return theirs + (f.batch > 0 ? ((size_t)(f.n_pairs + shared_runs(p)) * f.part_rows * row + 255) / 256 * 256 : 0);
 }
 
 beagle_status check_heads(const beagle_pages* p, int Hq) {
@@ -1255,8 +1148,12 @@ beagle_status beagle_paged_attn_shared_workspace_bytes(const beagle_pages* p, in
     if (st != BEAGLE_OK) return st;
     st = check_groups(batch, n_groups, group_rows_host);
     if (st != BEAGLE_OK) return st;
-    const size_t parts = (size_t)count_entries(p, n_q_heads, batch, n_groups, group_rows_host) * p->n_kv_heads + shared_runs(p);
-    *bytes = (kStartBytes + parts * 8 * (p->head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+    SharedCall a;
+    PrefixArgs f;
+    memset(static_cast<void*>(&a), 0, sizeof(a));
+    memset(static_cast<void*>(&f), 0, sizeof(f));
+    plan_shared(p, n_q_heads, batch, n_groups, group_rows_host, &a, &f);
+    *bytes = shared_ws(p, a, f, nullptr, nullptr);
     return BEAGLE_OK;
 }
 
@@ -1265,39 +1162,45 @@ beagle_status beagle_paged_attn_shared(const beagle_pages* p, int32_t batch, con
                                        void* ws_dev, size_t ws_bytes, void* stream_) {
     beagle_status st = pages_check(p);
     if (st != BEAGLE_OK) return st;
-    SharedArgs a;
+    SharedCall a;
+    PrefixArgs f;
     memset(static_cast<void*>(&a), 0, sizeof(a));
+    memset(static_cast<void*>(&f), 0, sizeof(f));
     st = check_rows(p, batch, slot_host, &a.slots);
     if (st != BEAGLE_OK) return st;
-    size_t need = 0;
-    st = beagle_paged_attn_shared_workspace_bytes(p, batch, n_q_heads, n_groups, group_rows_host, &need);
+    st = check_heads(p, n_q_heads);
+    if (st != BEAGLE_OK) return st;
+    st = check_groups(batch, n_groups, group_rows_host);
     if (st != BEAGLE_OK) return st;
     if (batch == 0) return BEAGLE_OK;
     if (shared_dev == nullptr || ((uintptr_t)shared_dev & 3)) return BEAGLE_ERR_INVALID_ARG;
-    st = check_call(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, ws_dev, ws_bytes, need);
+    plan_shared(p, n_q_heads, batch, n_groups, group_rows_host, &a, &f);
+    st = check_call(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, ws_dev, ws_bytes, shared_ws(p, a, f, nullptr, nullptr));
     if (st != BEAGLE_OK) return st;
+    if (!paged_attn_fits(p, a.batch) || !paged_attn_fits(p, f.batch)) return BEAGLE_ERR_CAPACITY;
     fill_args(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, &a);
-    a.block = entry_rows(p);
-    int e = batch;                                       // the rows' own entries first
-    for (int i = 0, r = 0; i < n_groups; r += group_rows_host[i++]) {
-        const int R = group_rows_host[i];
-        a.group_row0[i] = (uint8_t)r;
-        a.prefix_entry[i] = (uint8_t)e;
-        for (int x = 0; x < R; ++x) {
-            a.group_of[r + x] = R > 1 ? (uint8_t)i : (uint8_t)255;
-            a.entry[r + x] = {(uint8_t)(r + x), a.group_of[r + x], 0, (uint8_t)a.G, 0};
-        }
-        for (int j = 0; R > 1 && j < R * a.G; j += a.block)
-            a.entry[e++] = {(uint8_t)r, (uint8_t)i, 1, (uint8_t)(R * a.G - j < a.block ? R * a.G - j : a.block), (uint16_t)j};
+    f.slots = a.slots;
+    fill_args(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, &f);
+    a.shared = f.shared = shared_dev;
+    char* base = static_cast<char*>(ws_dev);
+    a.start = reinterpret_cast<int*>(base);
+    f.start = reinterpret_cast<int*>(base + kStartBytes);
+    size_t own = 0, common = 0;
+    shared_ws(p, a, f, &own, &common);
+    a.part = reinterpret_cast<float*>(base + own);
+    f.part = reinterpret_cast<float*>(base + common);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const int runs = shared_runs(p);                     // (not more than the cache's capacity has tiles)
+    if (f.batch > 0) {
+        const long long most = (long long)f.n_pairs * most_tiles(p, 0, 0);
+        f.runs = (int)(runs < most ? runs : most);
+        a.prefix.start = f.start; a.prefix.part = f.part;
+        a.prefix.n_pairs = f.n_pairs; a.prefix.runs = f.runs; a.prefix.part_rows = f.part_rows; a.prefix.block = f.block;
+        st = launch_prefix(p, f, f.runs, stream);
+        if (st != BEAGLE_OK) return st;
     }
-    if (!paged_attn_fits(p, e)) return BEAGLE_ERR_CAPACITY;
-    a.batch = e; a.rows = batch; a.n_groups = n_groups; a.n_pairs = e * p->n_kv_heads;
-    a.shared = shared_dev;
-    a.start = static_cast<int*>(ws_dev);
-    a.part = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + kStartBytes);
     const long long most = (long long)a.n_pairs * most_tiles(p, 0, 0);
-    const int runs = shared_runs(p);
-    return launch_attn(p, a, (int)(runs < most ? runs : most), static_cast<cudaStream_t>(stream_));
+    return launch_attn(p, a, (int)(runs < most ? runs : most), stream);
 }
 
 }  // extern "C"

@@ -111,6 +111,36 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.ftz.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+// Scores of 32 columns -> their maximum (masked: only where `vis` has a bit; the others become -inf).
+template <bool MASK>
+__device__ __forceinline__ float chunk_max(uint32_t* r, uint32_t vis, float mx) {
+    if (MASK) {
+#pragma unroll
+        for (int x = 0; x < 32; ++x) r[x] = (vis >> x & 1u) ? r[x] : 0xff800000u;
+    }
+    float y = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 32; x += 4) {                            // two chains
+        mx = max3(mx, __uint_as_float(r[x]), __uint_as_float(r[x + 1]));
+        y = max3(y, __uint_as_float(r[x + 2]), __uint_as_float(r[x + 3]));
+    }
+    return fmaxf(mx, y);
+}
+// exp2(S * scale + neg) of 32 columns as bf16 pairs; their sum (of the unrounded weights) is added to `sum`.
+__device__ __forceinline__ void chunk_exp(const uint32_t* r, uint64_t scale2, uint64_t neg2, uint32_t* p, uint64_t& sum0, uint64_t& sum1) {
+#pragma unroll
+    for (int x = 0; x < 32; x += 4) {
+        float e[4];
+        un2(fma2(pk2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), scale2, neg2), e[0], e[1]);
+        un2(fma2(pk2(__uint_as_float(r[x + 2]), __uint_as_float(r[x + 3])), scale2, neg2), e[2], e[3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = exp2f(e[i]);
+        sum0 = add2(sum0, pk2(e[0], e[1]));
+        sum1 = add2(sum1, pk2(e[2], e[3]));
+        p[x >> 1] = pack_bf16(e[0], e[1]);
+        p[(x >> 1) + 1] = pack_bf16(e[2], e[3]);
+    }
+}
 // Zeroes rows [from, to) of an operand tile of `rows` rows x DH bf16 (64-column blocks of rows * 128 bytes; whole rows, so the
 // swizzle inside a row does not matter).  One warp.
 template <int DH>

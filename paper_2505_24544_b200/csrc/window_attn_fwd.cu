@@ -57,37 +57,6 @@ struct KeyWalk {
     }
 };
 
-// Scores of 32 columns -> their maximum (masked: only where `vis` has a bit; the others become -inf).
-template <bool MASK>
-__device__ __forceinline__ float chunk_max(uint32_t* r, uint32_t vis, float mx) {
-    if (MASK) {
-#pragma unroll
-        for (int x = 0; x < 32; ++x) r[x] = (vis >> x & 1u) ? r[x] : 0xff800000u;
-    }
-    float y = -INFINITY;
-#pragma unroll
-    for (int x = 0; x < 32; x += 4) {                            // two chains
-        mx = max3(mx, __uint_as_float(r[x]), __uint_as_float(r[x + 1]));
-        y = max3(y, __uint_as_float(r[x + 2]), __uint_as_float(r[x + 3]));
-    }
-    return fmaxf(mx, y);
-}
-// exp2(S * scale + neg) of 32 columns as bf16 pairs; their sum (of the unrounded weights) is added to `sum`.
-__device__ __forceinline__ void chunk_exp(const uint32_t* r, uint64_t scale2, uint64_t neg2, uint32_t* p, uint64_t& sum0, uint64_t& sum1) {
-#pragma unroll
-    for (int x = 0; x < 32; x += 4) {
-        float e[4];
-        un2(fma2(pk2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), scale2, neg2), e[0], e[1]);
-        un2(fma2(pk2(__uint_as_float(r[x + 2]), __uint_as_float(r[x + 3])), scale2, neg2), e[2], e[3]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e[i] = exp2f(e[i]);
-        sum0 = add2(sum0, pk2(e[0], e[1]));
-        sum1 = add2(sum1, pk2(e[2], e[3]));
-        p[x >> 1] = pack_bf16(e[0], e[1]);
-        p[(x >> 1) + 1] = pack_bf16(e[2], e[3]);
-    }
-}
-
 template <int DH>
 __global__ void __launch_bounds__(kThreads, 2) window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                                                                const __grid_constant__ CUtensorMap tmV, const __grid_constant__ WinArgs a,
