@@ -725,6 +725,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
 
 // The same for rows of groups: blockIdx.x = row of the call, blockIdx.y = query head; the partials of the row's own positions and those of the
 // common part, which lie with the row's launch or (`prefix.on`) with the tensor cores'.
+constexpr int kJoinFlight = 4;
 struct PrefixParts {
     const int* start;
     const float* part;
@@ -733,7 +734,6 @@ struct PrefixParts {
 };
 template <typename T, int DH>
 __global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(const __grid_constant__ SharedArgs a, const __grid_constant__ PrefixParts prefix, int n_runs) {
-    constexpr int kPer = (DH + 31) / 32;
     __shared__ float s_o[kJoinWarps][DH], s_m[kJoinWarps], s_l[kJoinWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
@@ -768,49 +768,80 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(cons
     };
     const Source own = source(true), shared = source(false);
     const int n0 = own.r1 - own.r0 + 1, all = n0 + shared.r1 - shared.r0 + 1;
-    // partial i; false: none (fewer tiles than runs: some runs between are empty)
-    auto part = [&](int i, const float*& o, const float*& ml) {
-        const Source& x = i < n0 ? own : shared;
-        const int r = x.r0 + (i < n0 ? i : i - n0);
-        if (x.runs.total < x.runs.runs && x.runs.begin(r) >= x.runs.begin(r + 1)) return false;
-        const float* p = x.part + (size_t)(r == x.r0 ? x.pair : x.n_pairs + r) * x.size;
-        o = p + x.o;
-        ml = p + x.ml;
-        return true;
-    };
-    float M = -INFINITY, L = 0.f, acc[kPer];
+    // Every warp takes each eighth partial, kJoinFlight of them in flight, with a maximum of its own; then the warps meet.  A lane holds
+    // kPer neighbouring components.
+    constexpr int kPer = DH >= 128 ? 4 : DH >= 64 ? 2 : 1, kSteps = (DH + 32 * kPer - 1) / (32 * kPer);
+    float M = -INFINITY, L = 0.f, acc[kSteps][kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
-    const float *o, *ml;
-    for (int i = warp * 32 + lane; i < all; i += kJoinWarps * 32)
-        if (part(i, o, ml)) M = fmaxf(M, __ldcg(ml));
-    M = warp_max(M);
-    if (lane == 0) s_m[warp] = M;
-    __syncthreads();
+    for (int x = 0; x < kSteps; ++x)
 #pragma unroll
-    for (int i = 0; i < kJoinWarps; ++i) M = fmaxf(M, s_m[i]);
-#pragma unroll 4
-    for (int i = warp; i < all; i += kJoinWarps) {
-        if (!part(i, o, ml)) continue;
-        const float m = __ldcg(ml);
-        const float f = m == -INFINITY ? 0.f : exp2f(m - M);
-        L += m == -INFINITY ? __ldcg(ml + 1) : f * __ldcg(ml + 1);
+        for (int y = 0; y < kPer; ++y) acc[x][y] = 0.f;
+    for (int i0 = warp; i0 < all; i0 += kJoinWarps * kJoinFlight) {
+        float m[kJoinFlight], l[kJoinFlight], o[kJoinFlight][kSteps][kPer];
 #pragma unroll
-        for (int x = 0; x < kPer; ++x)
-            if (lane + 32 * x < DH) acc[x] = fmaf(f, __ldcg(o + lane + 32 * x), acc[x]);
+        for (int z = 0; z < kJoinFlight; ++z) {
+            const int i = i0 + z * kJoinWarps;
+            const Source& x = i < n0 ? own : shared;
+            const int r = x.r0 + (i < n0 ? i : i - n0);
+            // (fewer tiles than runs: some runs between are empty and left no partial)
+            const bool some = i < all && !(x.runs.total < x.runs.runs && x.runs.begin(r) >= x.runs.begin(r + 1));
+            const float* p = x.part + (some ? (size_t)(r == x.r0 ? x.pair : x.n_pairs + r) * x.size : 0);
+            m[z] = some ? __ldcg(p + x.ml) : -INFINITY;
+            l[z] = some ? __ldcg(p + x.ml + 1) : 0.f;
+#pragma unroll
+            for (int d = 0; d < kSteps; ++d)
+#pragma unroll
+                for (int y = 0; y < kPer; y += kPer > 1 ? 2 : 1) {       // (rows of partials begin on 8 bytes)
+                    const int at = (d * 32 + lane) * kPer + y;
+                    if (kPer > 1) {
+                        const float2 v = some && at < DH ? __ldcg(reinterpret_cast<const float2*>(p + x.o + at)) : make_float2(0.f, 0.f);
+                        o[z][d][y] = v.x;
+                        o[z][d][y + (kPer > 1 ? 1 : 0)] = v.y;
+                    } else {
+                        o[z][d][y] = some && at < DH ? __ldcg(p + x.o + at) : 0.f;
+                    }
+                }
+        }
+        float top = M;
+#pragma unroll
+        for (int z = 0; z < kJoinFlight; ++z) top = fmaxf(top, m[z]);
+        const float f0 = M == -INFINITY ? 0.f : exp2f(M - top);
+        L = M == -INFINITY ? L : L * f0;                         // (no position seen: the sum is 0, or NaN after a wait that ran out)
+#pragma unroll
+        for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+            for (int y = 0; y < kPer; ++y) acc[x][y] *= f0;
+#pragma unroll
+        for (int z = 0; z < kJoinFlight; ++z) {
+            const float f = m[z] == -INFINITY ? 0.f : exp2f(m[z] - top);
+            L += m[z] == -INFINITY ? l[z] : f * l[z];
+#pragma unroll
+            for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+                for (int y = 0; y < kPer; ++y) acc[x][y] = fmaf(f, m[z] == -INFINITY ? 0.f : o[z][x][y], acc[x][y]);
+        }
+        M = top;
     }
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-        if (lane + 32 * i < DH) s_o[warp][lane + 32 * i] = acc[i];
-    if (lane == 0) s_l[warp] = L;
+    for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+        for (int y = 0; y < kPer; ++y)
+            if ((x * 32 + lane) * kPer + y < DH) s_o[warp][(x * 32 + lane) * kPer + y] = acc[x][y];
+    if (lane == 0) { s_m[warp] = M; s_l[warp] = L; }
     __syncthreads();
     T* out = static_cast<T*>(a.o) + ((size_t)b * a.Hq + head) * DH;
     for (int d = threadIdx.x; d < DH; d += kJoinWarps * 32) {
-        float x = 0.f, y = 0.f;
+        float top = -INFINITY, x = 0.f, y = 0.f;
 #pragma unroll
-        for (int i = 0; i < kJoinWarps; ++i) { x += s_o[i][d]; y += s_l[i]; }
+        for (int i = 0; i < kJoinWarps; ++i) top = fmaxf(top, s_m[i]);
+#pragma unroll
+        for (int i = 0; i < kJoinWarps; ++i) {
+            const float f = s_m[i] == -INFINITY ? 0.f : exp2f(s_m[i] - top);
+            x = fmaf(f, s_o[i][d], x);
+            y += s_m[i] == -INFINITY ? s_l[i] : f * s_l[i];
+        }
         out[d] = from_float<T>(y != 0.f ? x / y : 0.f);
-        if (d == 0 && a.lse != nullptr) a.lse[(size_t)b * a.Hq + head] = y != 0.f ? (M + log2f(y)) * kLn2 : -INFINITY;
+        if (d == 0 && a.lse != nullptr) a.lse[(size_t)b * a.Hq + head] = y != 0.f ? (top + log2f(y)) * kLn2 : -INFINITY;
     }
 }
 
@@ -976,7 +1007,7 @@ beagle_status check_groups(int batch, int n_groups, const int32_t* group_rows) {
 
 // Groups with more query rows than this (rows times grouped heads) have their common part on the tensor cores' 128-row tiles, the others in
 // entries of eight rows.
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 8;
 
 // Query rows of a common part's entry: what the kernel takes as grouped heads.
 int entry_rows(const beagle_pages* p) { return p->dtype == BEAGLE_BF16 && p->head_dim == 256 ? 4 : 8; }

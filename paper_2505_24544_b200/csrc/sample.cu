@@ -1,18 +1,23 @@
 // One token per row of logits from a given uniform number, after temperature, top-k, top-p and min-p (beagle_sample).
 //
 // All three filters keep a leading run of the tokens in order of (logit falling, id rising), so the kept set is one threshold on the
-// 64-bit entry (order-preserving logit bits, inverted id), found without sorting; the draw is an inverse CDF in order of id.
+// 64-bit entry (order-preserving logit bits, inverted id).  The draw is an inverse CDF in order of id.
 //
 // Weights exp((l - largest) / T) are formed in double precision and rounded to integers, 2^45 for the largest: sums of up to 2^18 of
 // them fit 64 bits and do not depend on their order, so neither the number of thread blocks of a row nor timing has an influence on
 // the result, and a token differs from exact arithmetic's only if a sum comes within some 2^-45 of a border.
 //
 // A row belongs to a cluster of up to 8 thread blocks, each of which keeps its slice of the logits in shared memory: they are read
-// from memory once (the floor of the call), all passes after that stay on chip.  Per filter: a histogram of the tokens' distance from
-// the largest (2048 bins, 32-bit counts); for top-p the bins' counts bracket their weights, which leaves a few bins in which the
-// border can lie; one pass forms the exact weights before, inside and behind them; the tokens inside (usually a few dozen) are gathered
-// by the first block, which finds the border by comparing all pairs.  More than kList of them: their range of logit bits is
-// divided further, by 2048 a level with exact weights, until few are left, or only equal logits, which are taken in order of id.
+// from memory once (the floor of the call), all passes after that stay on chip and take two fp32 operations a token where nothing more is
+// known of it.  What costs is the double-precision weight (some 25 instructions), so it is formed
+//   - of all tokens only if top-k does not limit them: the total is needed then;
+//   - otherwise of candidates alone, those a bound in fp32 does not exclude.  top-k: at least k groups of a few neighbours (the ones read as
+//     one 16-byte piece) have their largest in the leading bins of a histogram, so the k-th token is in those too.  top-p: the tokens
+//     beyond a distance x weigh at most V 2^-x together.  min-p: its distance.
+// Up to kGather candidates, nearly always, go to the first block, which sorts them and finishes the row alone; the others leave.  More of
+// them: the cluster finds each border with a histogram whose counts bracket the weights, one exact pass, and a list of the tokens
+// in the few bins left, compared pairwise; more than kList of those: their range of logit bits is divided further, by 2048 a level
+// with exact weights, until few are left, or only equal logits, which are taken in order of id.
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
@@ -30,11 +35,14 @@ typedef unsigned long long u64;
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBins = 2048, kPerThread = kBins / kThreads;
+constexpr int kGather = 4096;            // candidates that the first block finishes alone
 constexpr int kList = kThreads;          // tokens that the first block compares pairwise
 constexpr int kMaxCluster = 8;
 constexpr int kMaxVocab = 1 << 18;
+constexpr int kMaxGroups = kMaxVocab / kMaxCluster / 128 + 8;      // of 32 16-byte pieces (128 fp32 logits, 256 bf16) in a block's slice
 constexpr double kOne = 35184372088832.0;        // 2^45
 constexpr float kFar = 47.f;             // log2 distance from which on the weight is 0 (2^45 * 2^-47 rounds to 0)
+constexpr float kMost = 3.402823466e38f;
 
 struct SampleArgs {
     const void* logits;
@@ -47,25 +55,33 @@ struct SampleArgs {
 };
 
 struct Shared {
-    u64 mass[kBins];
-    uint32_t count[kBins];
-    u64 list[kList], list_w[kList];
+    union {
+        u64 entry[kGather];              // the candidates of the row (first block)
+        struct { u64 mass[kBins], list[kList], list_w[kList]; } wide;
+    };
+    union {
+        uint32_t count[kBins];
+        uint16_t cand[kGather];          // this block's candidates: positions in its slice
+    };
+    u64 group[kMaxGroups];               // weight of every group of 32 pieces
+    u64 scan[kWarps];
     double root[32];                     // 2^(-j / 32)
-    u64 scan[kWarps + 1];
-    u64 best, sum[3], total, thr, found;
-    uint32_t least, lo, hi, n_list, bin[2];
+    u64 sum[2], total, thr, found;
+    uint32_t top, least, id, lo, hi, n_cand, n_list, bin[2], cut;
 };
 
-__device__ __forceinline__ float value_of(float v) { return v != v ? -CUDART_INF_F : v; }
-__device__ __forceinline__ float value_of(bf16 v) { return value_of(__bfloat162float(v)); }
-// Order-preserving bits; -0 and +0 are equal.
+__device__ __forceinline__ float value_of(float v) { return v; }
+__device__ __forceinline__ float value_of(bf16 v) { return __bfloat162float(v); }
+// Order-preserving bits; -0, +0 and subnormal values are equal (the fp32 operations here flush those).
 __device__ __forceinline__ uint32_t bits_of(float v) {
     uint32_t u = __float_as_uint(v);
-    u = u == 0x80000000u ? 0u : u;
+    u = (u & 0x7f800000u) == 0u ? 0u : u;
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 __device__ __forceinline__ float of_bits(uint32_t u) { return __uint_as_float((u & 0x80000000u) ? (u & 0x7fffffffu) : ~u); }
 __device__ __forceinline__ u64 entry_of(uint32_t bits, int id) { return ((u64)bits << 32) | (0xffffffffu - (uint32_t)id); }
+__device__ __forceinline__ float value_of_entry(u64 e) { return of_bits((uint32_t)(e >> 32)); }
+__device__ __forceinline__ int id_of_entry(u64 e) { return (int)(0xffffffffu - (uint32_t)e); }
 
 // Exclusive sum over the block's threads; the block's total for every thread.
 template <typename N>
@@ -91,34 +107,57 @@ __device__ __forceinline__ N block_exclusive(N v, u64* scratch, N& total) {
     return before + incl - v;
 }
 
+// Sorts x[0 .. n), n a power of two, falling or rising.  Whole block, a barrier at both ends.
+template <bool FALLING, typename N>
+__device__ __forceinline__ void block_sort(N* x, int n) {
+    __syncthreads();
+    for (int k = 2; k <= n; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            for (int p = threadIdx.x; p < n / 2; p += kThreads) {
+                const int i = 2 * p - (p & (j - 1)), o = i + j;
+                const N a = x[i], b = x[o];
+                const bool swap = (a < b) == (((i & k) == 0) == FALLING);
+                if (swap) { x[i] = b; x[o] = a; }
+            }
+            __syncthreads();
+        }
+}
+
 template <typename T>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant__ SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     Shared& s = *reinterpret_cast<Shared*>(smem);
     constexpr int VN = 16 / (int)sizeof(T);
     T* slice = reinterpret_cast<T*>(smem + (sizeof(Shared) + 15) / 16 * 16);
     cg::cluster_group cluster = cg::this_cluster();
-    const int C = cluster.num_blocks(), rank = cluster.block_rank(), row = blockIdx.x / C, t = threadIdx.x, lane = t & 31;
+    const int C = cluster.num_blocks(), rank = cluster.block_rank(), row = blockIdx.x / C, t = threadIdx.x, lane = t & 31, warp = t >> 5;
     pdl_launch_dependents();
     pdl_wait();
 
-    // ---- the slice into shared memory, at the same distance from a 16-byte border as in memory; the largest and the least finite logit
+    // ---- the slice into shared memory, at the same distance from a 16-byte border as in memory; -infinity around it.  Token i is
+    // slice[pad + i]; pieces of VN tokens are read whole from here on.
     const int first = min(rank * a.slice, a.vocab), n = min(a.slice, a.vocab - first);
     const T* src = static_cast<const T*>(a.logits) + (size_t)row * a.stride + first;
-    const int pad = (int)(((uintptr_t)src & 15) / sizeof(T));
-    slice += pad;
-    u64 best = 0;
-    float least = CUDART_INF_F;
-    auto look = [&](T raw, int i) {
-        const float v = value_of(raw);
-        const u64 k = argmax_key(v, first + i);
-        best = k > best ? k : best;
-        if (v > -CUDART_INF_F) least = fminf(least, v);
+    const int pad = (int)(((uintptr_t)src & 15) / sizeof(T)), pieces = (pad + n + VN - 1) / VN, id0 = first - pad;
+    // the piece's tokens in fp32, and their largest (NaN never is)
+    auto piece = [&](int p, float* v) {
+        const uint4 x = *reinterpret_cast<const uint4*>(slice + p * VN);
+        unpack16<T>(x, v);
+    };
+    auto largest = [&](const float* v) {
+        float m = v[0];
+#pragma unroll
+        for (int i = 1; i < VN; ++i) m = fmaxf(m, v[i]);
+        return m == m ? m : -CUDART_INF_F;
+    };
+    float top = -CUDART_INF_F, least = CUDART_INF_F;             // least: of the pieces' largest
+    auto look = [&](float m) {
+        top = fmaxf(top, m);
+        if (m > -CUDART_INF_F) least = fminf(least, m);
     };
     {
         const int head = min(n, (VN - pad) % VN), vecs = (n - head) / VN, tail = head + vecs * VN;
-        if (t < head) { slice[t] = src[t]; look(src[t], t); }
-        if (t < n - tail) { slice[tail + t] = src[tail + t]; look(src[tail + t], tail + t); }
+        const int p0 = (pad + head) / VN;                        // first whole piece
         for (int i0 = t; i0 < vecs; i0 += 4 * kThreads) {
             uint4 v[4];
 #pragma unroll
@@ -127,52 +166,87 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
 #pragma unroll
             for (int x = 0; x < 4; ++x)
                 if (i0 + x * kThreads < vecs) {
-                    const int at = head + (i0 + x * kThreads) * VN;
-                    *reinterpret_cast<uint4*>(slice + at) = v[x];
-                    const T* e = reinterpret_cast<const T*>(&v[x]);
-#pragma unroll
-                    for (int y = 0; y < VN; ++y) look(e[y], at + y);
+                    *reinterpret_cast<uint4*>(slice + (size_t)(p0 + i0 + x * kThreads) * VN) = v[x];
+                    float f[VN];
+                    unpack16<T>(v[x], f);
+                    look(largest(f));
                 }
         }
+        if (t < 2 * VN) {                                        // the two ragged ends, in order
+            const int at = t < VN ? t : (pad + tail) / VN * VN + t - VN;         // place in the slice
+            const bool edge = t < VN ? at < pad + head : at >= pad + tail && at < pieces * VN;
+            if (edge) {
+                const int i = at - pad;
+                const bool in = i >= 0 && i < n;
+                slice[at] = in ? src[i] : from_float<T>(-CUDART_INF_F);
+                if (in) { const float v = value_of(src[i]); look(v == v ? v : -CUDART_INF_F); }
+            }
+        }
     }
-    if (t == 0) { s.best = 0; s.least = 0xffffffffu; }
+    if (t == 0) { s.top = 0; s.least = 0xffffffffu; s.id = 0xffffffffu; s.n_cand = 0; }
     if (t < 32) s.root[t] = exp2(-(double)t / 32.0);
+    for (int i = t; i < kBins; i += kThreads) s.count[i] = 0;
     __syncthreads();
-    best = warp_max_u64(best);
-    for (int o = 16; o > 0; o >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
-    if (lane == 0) { atomicMax(&s.best, best); atomicMin(&s.least, bits_of(least)); }
-    cluster.sync();
-    uint32_t least_bits = 0xffffffffu;
-    for (int i = 0; i < C; ++i) {
-        const u64 b = *cluster.map_shared_rank(&s.best, i);
-        best = b > best ? b : best;
-        least_bits = min(least_bits, *cluster.map_shared_rank(&s.least, i));
+    {
+        const uint32_t hi = __reduce_max_sync(0xffffffffu, bits_of(top)), lo = __reduce_min_sync(0xffffffffu, bits_of(least));
+        if (lane == 0) { atomicMax(&s.top, hi); atomicMin(&s.least, lo); }
     }
-    const float top = of_bits((uint32_t)(best >> 32));           // (argmax_key's bits are bits_of's)
-    const int top_id = argmax_key_index(best);
+    cluster.sync();
+    {
+        uint32_t hi = 0, lo = 0xffffffffu;
+        for (int i = 0; i < C; ++i) {
+            hi = max(hi, *cluster.map_shared_rank(&s.top, i));
+            lo = min(lo, *cluster.map_shared_rank(&s.least, i));
+        }
+        top = of_bits(hi);
+        least = of_bits(lo);
+    }
 
     // ---- the row's parameters
     const uint32_t temp_bits = a.temperature != nullptr ? __float_as_uint(__ldcg(a.temperature + row)) : __float_as_uint(1.f);
     const bool drawn = temp_bits - 1u < 0x7f800000u;             // above 0, infinity included
     int k = a.top_k != nullptr ? __ldcg(a.top_k + row) : 0;
-    const float top_p = a.top_p != nullptr ? __ldcg(a.top_p + row) : 1.f;
+    float top_p = a.top_p != nullptr ? __ldcg(a.top_p + row) : 1.f;
     const float min_p = a.min_p != nullptr ? __ldcg(a.min_p + row) : 0.f;
     if (top_p <= 0.f || min_p > 1.f) k = 1;                      // only the first
-    if (!drawn || k == 1 || top == -CUDART_INF_F) {
+    if (!drawn || k == 1 || top == -CUDART_INF_F) {              // its lowest id
+        const bool none = top == -CUDART_INF_F;
+        uint32_t id = 0xffffffffu;
+        if (!none)
+            for (int p = t; p < pieces; p += kThreads) {
+                float v[VN];
+                piece(p, v);
+#pragma unroll
+                for (int i = VN - 1; i >= 0; --i)
+                    if (v[i] == top) id = min(id, (uint32_t)(id0 + p * VN + i));
+            }
+        id = __reduce_min_sync(0xffffffffu, id);
+        if (lane == 0 && id != 0xffffffffu) atomicMin(cluster.map_shared_rank(&s.id, 0), id);
+        cluster.sync();
         if (rank == 0 && t == 0) {
-            a.tokens[row] = top == -CUDART_INF_F ? -1 : top_id;
-            if (a.logp != nullptr) a.logp[row] = top == -CUDART_INF_F ? CUDART_NAN_F : 0.f;
+            a.tokens[row] = none ? -1 : (int)s.id;
+            if (a.logp != nullptr) a.logp[row] = none ? CUDART_NAN_F : 0.f;
         }
-        cluster.sync();                                          // the others have read this block's words
         return;
     }
-    const double c2 = 1.4426950408889634074 / (double)__uint_as_float(temp_bits), dtop = (double)top;
+    if (k >= a.vocab || k < 0) k = 0;
+    if (!(top_p < 1.f)) top_p = 1.f;
+    if (top == CUDART_INF_F) {                                   // the infinite ones share the weight: 0 and -infinity do the same
+        __syncthreads();
+        for (int i = t; i < pieces * VN; i += kThreads) slice[i] = from_float<T>(value_of(slice[i]) == top ? 0.f : -CUDART_INF_F);
+        top = least = 0.f;
+        __syncthreads();
+    }
+    const double c2 = fmin(1.4426950408889634074 / (double)__uint_as_float(temp_bits), 1e300), dtop = (double)top;
     const double most = min_p > 0.f ? -log2((double)min_p) : CUDART_INF;         // distance that min_p allows
-
-    // log2 distance from the largest; infinity for a token without weight (the comparison first: inf - inf, 0 * inf)
-    auto distance = [&](float v) { return v == top ? 0.0 : v == -CUDART_INF_F ? CUDART_INF : (dtop - (double)v) * c2; };
-    auto near = [&](double x) { return x <= (double)kFar; };     // (false for NaN: infinite temperature below an infinite logit)
-    // round(2^45 * 2^-x), 0 <= x <= 47: x = k / 32 + r, 2^-r from its Taylor series, |r ln 2| <= 0.011: error 2e-15
+    // Half the distance of a logit from the largest in fp32, which does not overflow; `far`: those with a weight
+    const float half_top = 0.5f * top;
+    auto half = [&](float v) { return fmaf(v, -0.5f, half_top); };
+    const float unit = (float)(2.0 * c2);                        // log2 distance of a half of 1
+    const float far = fminf((float)fmin((double)kFar / (2.0 * c2) * 1.000001, (double)kMost), kMost);
+    auto near = [&](float v) { return half(v) <= far; };         // (false for NaN and -infinity)
+    auto distance = [&](float v) { return (dtop - (double)v) * c2; };            // log2, of a near token
+    // round(2^45 * 2^-x), 0 <= x <= 47.1: x = j / 32 + r, 2^-r from its Taylor series, |r ln 2| <= 0.011: error 2e-15
     auto weight = [&](double x) {
         constexpr double kMagic = 6755399441055744.0;            // 1.5 * 2^52
         const double m = fma(x, 32.0, kMagic);
@@ -183,178 +257,340 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
         p = fma(r, p, 2.4022650695910071e-1);
         p = fma(r, p, -6.9314718055994531e-1);
         p = fma(r, p, 1.0);
-        const double scale = __longlong_as_double((long long)(1023 + 45 - (j >> 5)) << 52);
+        const double scale = __hiloint2double((1023 + 45 - (j >> 5)) << 20, 0);
         return (u64)(__double_as_longlong(fma(p * s.root[j & 31], scale, 4503599627370496.0)) - 0x4330000000000000ll);
     };
-    // Each thread walks over a run of neighbouring tokens, of odd length: no bank conflicts between the threads.
-    const int run = ((n + kThreads - 1) / kThreads) | 1;
-    const int begin = min(t * run, n), end = min(begin + run, n);
     u64 thr = 0;                                                 // kept so far: entries from thr on
 
-    // Smallest id whose cumulative measure exceeds floor(u * total) + skip, and the measure's total.  Every thread of the cluster.
-    auto locate = [&](auto measure, double u, u64 skip, u64& total) {
-        u64 mine = 0, sum;
-        for (int i = begin; i < end; ++i) mine += measure(value_of(slice[i]), first + i);
-        u64 before = block_exclusive<u64>(mine, s.scan, sum);
-        if (t == 0) s.total = sum;
+    // Weight of every group of 32 pieces, of the tokens that are near, not below thr and within min_p if `last`; the row's total for every thread.
+    auto weigh = [&](bool last) {
+        const float thr_v = thr != 0 ? value_of_entry(thr) : -kMost;
+        const double limit = last ? most : CUDART_INF;
+        const int groups = (pieces + 31) / 32;
+        u64 all = 0;
+        for (int g = warp; g < groups; g += kWarps) {
+            const int p = 32 * g + lane;
+            u64 w = 0;
+            if (p < pieces) {
+                float v[VN];
+                piece(p, v);
+#pragma unroll
+                for (int i = 0; i < VN; ++i) {
+                    const bool in = near(v[i]) && v[i] >= thr_v && (v[i] > thr_v || thr == 0 || entry_of(bits_of(v[i]), id0 + p * VN + i) >= thr);
+                    if (in) {
+                        const double x = distance(v[i]);
+                        if (x <= limit || v[i] == top) w += weight(x);
+                    }
+                }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+            if (lane == 0) s.group[g] = w;
+            all += w;
+        }
+        __syncthreads();
+        u64 total;
+        block_exclusive<u64>(lane == 0 ? all : 0, s.scan, total);
+        if (t == 0) s.total = total;
         cluster.sync();
         total = 0;
-        for (int i = 0; i < C; ++i) {
-            const u64 x = *cluster.map_shared_rank(&s.total, i);
-            before += i < rank ? x : 0;
-            total += x;
-        }
-        u64 target = (u64)(u * (double)total) + skip;
-        target = target < total ? target : total - 1;
+        for (int i = 0; i < C; ++i) total += *cluster.map_shared_rank(&s.total, i);
+        return total;
+    };
+    // Smallest id whose cumulative measure exceeds the target (below the total).  s.group holds the groups' sums and s.total the block's;
+    // measure(value, id) as they were formed.  The entry for every thread of the cluster.
+    auto locate = [&](auto measure, u64 target) {
+        u64 before = 0, sum;
+        for (int i = 0; i < rank; ++i) before += *cluster.map_shared_rank(&s.total, i);
+        const int groups = (pieces + 31) / 32;
+        const u64 mine = t < groups ? s.group[t] : 0;
+        before += block_exclusive<u64>(mine, s.scan, sum);
         const uint32_t owner = __ballot_sync(0xffffffffu, before <= target && target < before + mine);
-        if (owner != 0) {                                        // one warp of the cluster: its lanes share the run
-            const int l = __ffs(owner) - 1, b = __shfl_sync(0xffffffffu, begin, l), e = __shfl_sync(0xffffffffu, end, l);
-            u64 acc = __shfl_sync(0xffffffffu, before, l);
-            for (int i0 = b; i0 < e; i0 += 32) {
-                const u64 m = i0 + lane < e ? measure(value_of(slice[i0 + lane]), first + i0 + lane) : 0;
-                u64 incl = m;
+        if (owner != 0) {                                        // one warp of the cluster: a lane takes a piece
+            const int l = __ffs(owner) - 1, p = 32 * (warp * 32 + l) + lane;
+            const u64 start = __shfl_sync(0xffffffffu, before, l);
+            float v[VN];
+            u64 w[VN], all = 0;
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const u64 x = __shfl_up_sync(0xffffffffu, incl, o);
-                    if (lane >= o) incl += x;
+            for (int i = 0; i < VN; ++i) v[i] = -CUDART_INF_F;
+            if (p < pieces) piece(p, v);
+#pragma unroll
+            for (int i = 0; i < VN; ++i) all += w[i] = measure(v[i], id0 + p * VN + i);
+            u64 incl = all;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 x = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += x;
+            }
+            u64 cum = start + incl - all;
+            if (cum <= target && target < cum + all) {
+                bool found = false;
+#pragma unroll
+                for (int i = 0; i < VN; ++i) {
+                    cum += w[i];
+                    if (!found && cum > target) {
+                        found = true;
+                        *cluster.map_shared_rank(&s.found, 0) = entry_of(bits_of(v[i]), id0 + p * VN + i);
+                    }
                 }
-                const uint32_t hit = __ballot_sync(0xffffffffu, acc + incl > target);
-                if (hit != 0) {
-                    if (lane == __ffs(hit) - 1) *cluster.map_shared_rank(&s.found, 0) = entry_of(bits_of(value_of(slice[i0 + lane])), first + i0 + lane);
-                    break;
-                }
-                acc += __shfl_sync(0xffffffffu, incl, 31);
             }
         }
         cluster.sync();
         return *cluster.map_shared_rank(&s.found, 0);
     };
+    auto emit = [&](u64 e, u64 total) {
+        a.tokens[row] = id_of_entry(e);
+        if (a.logp != nullptr) a.logp[row] = (float)(-(distance(value_of_entry(e)) * 0.69314718055994530942 + log((double)total / kOne)));
+    };
+    const float uf = __ldcg(a.u + row);
+    const double u = uf > 0.f ? (double)uf : 0.0;
+    auto target_of = [&](u64 total) {
+        const u64 x = (u64)(u * (double)total);
+        return x < total ? x : total - 1;
+    };
+    auto kept = [&](float v, int id) {                           // the last step's measure
+        if (!near(v) || entry_of(bits_of(v), id) < thr) return (u64)0;
+        const double x = distance(v);
+        return x <= most || v == top ? weight(x) : (u64)0;
+    };
 
-    // Moves thr to the end of the shortest leading run whose measure is at least the goal: by_mass the share p of all kept weight, else k
-    // tokens.  Every thread of the cluster.
-    auto select = [&](bool by_mass, double p) {
-        const float span = fminf(kFar, (float)distance(of_bits(least_bits)));
-        const float inv = span > 0.f ? (float)kBins / span : 0.f;
-        auto bin_of = [&](double x) { return min(kBins - 1, (int)((float)x * inv)); };       // rises with x
-        for (int i = t; i < kBins; i += kThreads) s.count[i] = 0;
-        __syncthreads();
-        for (int i = begin; i < end; ++i) {
-            const float v = value_of(slice[i]);
-            const double x = distance(v);
-            if (near(x) && entry_of(bits_of(v), first + i) >= thr) atomicAdd(&s.count[bin_of(x)], 1u);
-        }
-        if (t < 2) s.bin[t] = kBins - 1;
-        if (t == 0) { s.hi = 0; s.lo = 0xffffffffu; s.n_list = 0; s.sum[0] = s.sum[1] = s.sum[2] = 0; }
-        cluster.sync();
-        uint32_t c[kPerThread] = {}, mine = 0, all;
+    // ---- all tokens' weight, where top-k does not limit them
+    const bool filtered = k > 0 || top_p < 1.f || min_p > 0.f;
+    u64 total = 0;
+    if (k == 0 && (top_p < 1.f || !filtered)) total = weigh(false);
+    if (!filtered) {
+        const u64 e = locate(kept, target_of(total));
+        if (rank == 0 && t == 0) emit(e, total);
+        cluster.sync();                                          // (the others have read this block's words)
+        return;
+    }
+
+    // ---- candidates: half(v) * scale < bound holds for every token that can be kept
+    const float span = fminf(far, half(least));
+    const float inv = span > 1e-30f ? (float)kBins / span : 0.f;         // bins of distance
+    auto bin_of = [&](float v) { return min(kBins - 1, (int)(half(v) * inv)); };         // falls with v
+    float scale = 1.f, bound = far < kMost ? far * 1.000001f + 1e-37f : kMost;
+    if (min_p > 0.f) bound = fminf(bound, (float)fmin((most + 1e-9) / (2.0 * c2) * 1.00001, (double)kMost) + 1e-37f);
+    if (k == 0 && top_p < 1.f) {
+        // V 2^-x <= (1 - p) total: what lies beyond x is not needed to reach p total
+        const double x = log2((double)a.vocab * kOne / ((1.0 - (double)top_p) * (double)total)) + 1e-6;
+        bound = fminf(bound, (float)fmin(fmax(x, 0.0) / (2.0 * c2) * 1.00001, (double)kMost) + 1e-37f);
+    }
+    uint32_t c[kPerThread];
+    auto gather_counts = [&]() {                                 // the cluster's counts of this thread's bins
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) c[i] = 0;
         for (int i = 0; i < C; ++i) {
             const uint4 x = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(s.count, i) + t * kPerThread);
             c[0] += x.x; c[1] += x.y; c[2] += x.z; c[3] += x.w;
         }
         static_assert(kPerThread == 4, "one 16-byte read of the counts");
+    };
+    if (k > 0) {
+        for (int p = t; p < pieces; p += kThreads) {
+            float v[VN];
+            piece(p, v);
+            const float m = largest(v);
+            if (near(m)) atomicAdd(&s.count[bin_of(m)], 1u);
+        }
+        if (t == 0) s.bin[0] = kBins;
+        cluster.sync();
+        gather_counts();
+        uint32_t mine = c[0] + c[1] + c[2] + c[3], all;
+        uint32_t cum = block_exclusive<uint32_t>(mine, s.scan, all);
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i) mine += c[i];
+        for (int i = 0; i < kPerThread; ++i) {
+            if (cum < (uint32_t)k && cum + c[i] >= (uint32_t)k) s.bin[0] = t * kPerThread + i;
+            cum += c[i];
+        }
+        cluster.sync();                                          // (the counts have been read, s.cand may be written over them)
+        if (inv > 0.f && s.bin[0] < kBins - 1) { scale = inv; bound = (float)(s.bin[0] + 1); }        // (the last bin also holds what lies beyond the span)
+    }
+    for (int p = t; p < pieces; p += kThreads) {
+        float v[VN];
+        piece(p, v);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = 0; i < VN; ++i) mask |= half(v[i]) * scale < bound ? 1u << i : 0u;
+        if (mask != 0) {
+            uint32_t at = atomicAdd(&s.n_cand, (uint32_t)__popc(mask));
+            for (; mask != 0; mask &= mask - 1, ++at)
+                if (at < kGather) s.cand[at] = (uint16_t)(p * VN + __ffs(mask) - 1);
+        }
+    }
+    cluster.sync();
+    uint32_t n_all = 0, base = 0;
+    for (int i = 0; i < C; ++i) {
+        const uint32_t x = *cluster.map_shared_rank(&s.n_cand, i);
+        base += i < rank ? x : 0;
+        n_all += x;
+    }
+    if (n_all <= kGather) {
+        u64* to = cluster.map_shared_rank(s.entry, 0) + base;
+        for (int i = t; i < (int)s.n_cand; i += kThreads) to[i] = entry_of(bits_of(value_of(slice[s.cand[i]])), id0 + s.cand[i]);
+        cluster.sync();
+        if (rank != 0) return;
+        // ---- the first block alone
+        const int m = (int)n_all;
+        int size = 2;
+        while (size < m) size *= 2;
+        for (int i = m + t; i < size; i += kThreads) s.entry[i] = 0;
+        block_sort<true>(s.entry, size);
+        u64* cum = reinterpret_cast<u64*>(slice);                // cumulative weight of the sorted entries
+        const int per = (m + kThreads - 1) / kThreads;
+        const int b = min(t * per, m), e = min(b + per, m);
+        u64 mine = 0, all;
+        for (int i = b; i < e; ++i) { mine += weight(distance(value_of_entry(s.entry[i]))); cum[i] = mine; }
+        const u64 before = block_exclusive<u64>(mine, s.scan, all);
+        for (int i = b; i < e; ++i) cum[i] += before;
+        if (t == 0) s.cut = k > 0 ? min(m, k) : m;
+        __syncthreads();
+        int keep = s.cut;
+        if (top_p < 1.f) {
+            const double goal = (double)top_p * (double)(k > 0 ? cum[keep - 1] : total);
+            __syncthreads();
+            for (int i = b; i < min(e, keep); ++i)
+                if ((double)cum[i] >= goal) { atomicMin(&s.cut, (uint32_t)i + 1u); break; }
+            __syncthreads();
+            keep = s.cut;
+        }
+        if (min_p > 0.f) {
+            __syncthreads();
+            for (int i = b; i < min(e, keep); ++i) {
+                const float v = value_of_entry(s.entry[i]);
+                if (distance(v) > most && v != top) { atomicMin(&s.cut, (uint32_t)max(i, 1)); break; }
+            }
+            __syncthreads();
+            keep = s.cut;
+        }
+        // in order of id: (id, place) in one word
+        uint32_t* order = reinterpret_cast<uint32_t*>(cum + m);
+        size = 2;
+        while (size < keep) size *= 2;
+        for (int i = t; i < size; i += kThreads) order[i] = i < keep ? ((uint32_t)id_of_entry(s.entry[i]) << 12 | (uint32_t)i) : 0xffffffffu;
+        block_sort<false>(order, size);
+        const u64 kept_total = cum[keep - 1], target = target_of(kept_total);
+        const int per2 = (keep + kThreads - 1) / kThreads, b2 = min(t * per2, keep), e2 = min(b2 + per2, keep);
+        auto w_of = [&](int i) { const uint32_t x = order[i] & 4095u; return cum[x] - (x > 0 ? cum[x - 1] : 0); };
+        u64 sum = 0;
+        for (int i = b2; i < e2; ++i) sum += w_of(i);
+        u64 run = block_exclusive<u64>(sum, s.scan, all);
+        if (run <= target && target < run + sum)
+            for (int i = b2; i < e2; ++i) {
+                run += w_of(i);
+                if (run > target) { emit(s.entry[order[i] & 4095u], kept_total); break; }
+            }
+        return;
+    }
+
+    // ---- more candidates: the whole cluster.  Moves thr to the end of the shortest leading run whose measure is at least the goal:
+    // weight (by_mass) or tokens.
+    auto select = [&](bool by_mass, double goal) {
+        for (int i = t; i < kBins; i += kThreads) s.count[i] = 0;
+        if (t < 2) s.bin[t] = kBins - 1;
+        if (t == 0) { s.hi = 0; s.lo = 0xffffffffu; s.n_list = 0; s.sum[0] = 0; }
+        __syncthreads();
+        const float thr_v = thr != 0 ? value_of_entry(thr) : -kMost;
+        // f(value, id, bin) of the tokens that can be kept
+        auto for_tokens = [&](auto f) {
+            for (int p = t; p < pieces; p += kThreads) {
+                float v[VN];
+                piece(p, v);
+#pragma unroll
+                for (int i = 0; i < VN; ++i)
+                    if (half(v[i]) * scale < bound && near(v[i]) && v[i] >= thr_v) {
+                        const int id = id0 + p * VN + i;
+                        if (thr == 0 || entry_of(bits_of(v[i]), id) >= thr) f(v[i], id, bin_of(v[i]));
+                    }
+            }
+        };
+        for_tokens([&](float, int, int b) { atomicAdd(&s.count[b], 1u); });
+        cluster.sync();
+        gather_counts();
+        const uint32_t mine = c[0] + c[1] + c[2] + c[3];
+        uint32_t all;
         const uint32_t count_before = block_exclusive<uint32_t>(mine, s.scan, all);
-        if (!by_mass && all <= (uint32_t)k) { cluster.sync(); return; }          // everything that has weight is kept
+        if (!by_mass && (double)all <= goal) { cluster.sync(); return; }         // everything that has weight is kept
         if (by_mass) {
             // a bin's weights lie between those of its two ends: bounds of the cumulative weight, with a margin for their rounding
-            const float w = inv > 0.f ? 1.f / inv : 0.f;
-            float up[kPerThread], down[kPerThread], up_mine = 0.f, down_mine = 0.f, up_all, down_all;
+            const float w = inv > 0.f ? unit / inv : 0.f, want = (float)(goal / kOne);
+            float up[kPerThread], down[kPerThread], up_mine = 0.f, down_mine = 0.f, unused;
 #pragma unroll
             for (int i = 0; i < kPerThread; ++i) {
                 const int b = t * kPerThread + i;
                 up[i] = (float)c[i] * exp2f(-(float)b * w);
-                down[i] = b == kBins - 1 && span >= kFar ? 0.f : (float)c[i] * exp2f(-(float)(b + 1) * w);
+                down[i] = b == kBins - 1 ? 0.f : (float)c[i] * exp2f(-(float)(b + 1) * w);
                 up_mine += up[i]; down_mine += down[i];
             }
-            float cu = block_exclusive<float>(up_mine, s.scan, up_all), cd = block_exclusive<float>(down_mine, s.scan, down_all);
-            const float from = (float)p * down_all * 0.999f, to = (float)p * up_all * 1.001f;
+            float cu = block_exclusive<float>(up_mine, s.scan, unused), cd = block_exclusive<float>(down_mine, s.scan, unused);
 #pragma unroll
             for (int i = 0; i < kPerThread; ++i) {
                 cu += up[i]; cd += down[i];
-                if (c[i] > 0 && cu >= from) atomicMin(&s.bin[0], t * kPerThread + i);
-                if (c[i] > 0 && cd >= to) atomicMin(&s.bin[1], t * kPerThread + i);
+                if (c[i] > 0 && cu * 1.001f >= want) atomicMin(&s.bin[0], t * kPerThread + i);
+                if (c[i] > 0 && cd * 0.999f >= want) atomicMin(&s.bin[1], t * kPerThread + i);
             }
         } else {
             uint32_t cum = count_before;
 #pragma unroll
             for (int i = 0; i < kPerThread; ++i) {
-                if (cum < (uint32_t)k && cum + c[i] >= (uint32_t)k) s.bin[0] = s.bin[1] = t * kPerThread + i;
+                if ((double)cum < goal && (double)(cum + c[i]) >= goal) s.bin[0] = s.bin[1] = t * kPerThread + i;
                 cum += c[i];
             }
         }
         __syncthreads();
         const int b0 = s.bin[0], b1 = s.bin[1];
         // tokens inside: few enough for the list?  (the same number in every block)
-        uint32_t cand = 0, n_cand;
+        uint32_t in = 0, n_in;
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i) cand += t * kPerThread + i >= b0 && t * kPerThread + i <= b1 ? c[i] : 0;
-        block_exclusive<uint32_t>(cand, s.scan, n_cand);
-        auto measure = [&](double x) { return by_mass ? weight(x) : (u64)1; };
+        for (int i = 0; i < kPerThread; ++i) in += t * kPerThread + i >= b0 && t * kPerThread + i <= b1 ? c[i] : 0;
+        block_exclusive<uint32_t>(in, s.scan, n_in);
+        auto measure = [&](float v) { return by_mass ? weight(distance(v)) : (u64)1; };
         auto put = [&](u64 e) {
             const uint32_t at = atomicAdd(cluster.map_shared_rank(&s.n_list, 0), 1u);
-            if (at < kList) cluster.map_shared_rank(s.list, 0)[at] = e;
+            if (at < kList) cluster.map_shared_rank(s.wide.list, 0)[at] = e;
         };
-        u64 part[3] = {0, 0, 0};                                 // measure before, inside, behind
+        u64 part = 0;                                            // measure before
         uint32_t lo = 0xffffffffu, hi = 0;
-        for (int i = begin; i < end; ++i) {
-            const float v = value_of(slice[i]);
-            const double x = distance(v);
-            const u64 e = entry_of(bits_of(v), first + i);
-            if (!near(x) || e < thr) continue;
-            const int b = bin_of(x);
-            const bool inside = b >= b0 && b <= b1;
-            if (by_mass || b < b0) part[b < b0 ? 0 : inside ? 1 : 2] += measure(x);
-            if (inside) {
-                lo = min(lo, bits_of(v));
-                hi = max(hi, bits_of(v));
-                if (n_cand <= kList) put(e);
+        for_tokens([&](float v, int id, int b) {
+            if (b < b0) part += measure(v);
+            else if (b <= b1) {
+                const uint32_t x = bits_of(v);
+                lo = min(lo, x);
+                hi = max(hi, x);
+                if (n_in <= kList) put(entry_of(x, id));
             }
-        }
-#pragma unroll
-        for (int x = 0; x < 3; ++x) {
-            for (int o = 16; o > 0; o >>= 1) part[x] += __shfl_xor_sync(0xffffffffu, part[x], o);
-            if (lane == 0 && part[x] != 0) atomicAdd(&s.sum[x], part[x]);
-        }
+        });
+        for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
         lo = __reduce_min_sync(0xffffffffu, lo);
         hi = __reduce_max_sync(0xffffffffu, hi);
-        if (lane == 0) { atomicMin(&s.lo, lo); atomicMax(&s.hi, hi); }
+        if (lane == 0) { atomicAdd(&s.sum[0], part); atomicMin(&s.lo, lo); atomicMax(&s.hi, hi); }
         cluster.sync();
-        u64 before = 0, total = 0;
+        u64 before = 0;
         for (int i = 0; i < C; ++i) {
-            const u64* x = cluster.map_shared_rank(s.sum, i);
-            before += x[0];
-            total += x[0] + x[1] + x[2];
+            before += *cluster.map_shared_rank(&s.sum[0], i);
             lo = min(lo, *cluster.map_shared_rank(&s.lo, i));
             hi = max(hi, *cluster.map_shared_rank(&s.hi, i));
         }
-        const double goal = by_mass ? p * (double)total : (double)k;
         // divide the range of logit bits until the list holds what is left, or one value is
-        while (n_cand > kList && lo < hi) {
+        while (n_in > kList && lo < hi) {
             const int shift = max(0, 21 - __clz(hi - lo));       // (hi - lo) >> shift < 2048
-            for (int i = t; i < kBins; i += kThreads) { s.count[i] = 0; s.mass[i] = 0; }
-            cluster.sync();                                      // everyone has read the counts and sums of the step before
-            for (int i = begin; i < end; ++i) {
-                const float v = value_of(slice[i]);
-                const uint32_t key = bits_of(v);
-                if (key < lo || key > hi || entry_of(key, first + i) < thr) continue;
-                const double x = distance(v);
-                if (!near(x)) continue;
-                const int b = (int)((hi - key) >> shift);
-                atomicAdd(&s.count[b], 1u);
-                if (by_mass) atomicAdd(&s.mass[b], weight(x));
-            }
+            for (int i = t; i < kBins; i += kThreads) { s.count[i] = 0; s.wide.mass[i] = 0; }
             if (t == 0) s.bin[0] = 0xffffffffu;
+            cluster.sync();                                      // (everyone has read the counts and sums of the step before)
+            for_tokens([&](float v, int, int) {
+                const uint32_t x = bits_of(v);
+                if (x < lo || x > hi) return;
+                const int b = (int)((hi - x) >> shift);
+                atomicAdd(&s.count[b], 1u);
+                if (by_mass) atomicAdd(&s.wide.mass[b], measure(v));
+            });
             cluster.sync();
-            u64 m[kPerThread] = {}, m_mine = 0, m_all;
+            gather_counts();
+            u64 m[kPerThread], m_mine = 0, m_all;
 #pragma unroll
             for (int i = 0; i < kPerThread; ++i) {
-                c[i] = 0;
-                for (int r = 0; r < C; ++r) {
-                    c[i] += cluster.map_shared_rank(s.count, r)[t * kPerThread + i];
-                    if (by_mass) m[i] += cluster.map_shared_rank(s.mass, r)[t * kPerThread + i];
-                }
-                if (!by_mass) m[i] = c[i];
+                m[i] = by_mass ? 0 : c[i];
+                for (int r = 0; r < C && by_mass; ++r) m[i] += cluster.map_shared_rank(s.wide.mass, r)[t * kPerThread + i];
                 m_mine += m[i];
             }
             u64 cum = before + block_exclusive<u64>(m_mine, s.scan, m_all);
@@ -371,75 +607,83 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
             const uint32_t b = s.bin[0];
             if (b == 0xffffffffu) break;                         // (rounding of the goal at the very end of the range: all of it is kept)
             before = s.sum[0];
-            n_cand = (uint32_t)s.sum[1];
+            n_in = (uint32_t)s.sum[1];
             const uint32_t top_key = hi - (b << shift);
             lo = max(lo, top_key - min(top_key, (1u << shift) - 1u));
             hi = top_key;
-            if (n_cand <= kList) {
+            if (n_in <= kList) {
                 if (t == 0) s.n_list = 0;
                 cluster.sync();
-                for (int i = begin; i < end; ++i) {
-                    const uint32_t key = bits_of(value_of(slice[i]));
-                    const u64 e = entry_of(key, first + i);
-                    if (key >= lo && key <= hi && e >= thr) put(e);
-                }
+                for_tokens([&](float v, int id, int) {
+                    const uint32_t x = bits_of(v);
+                    if (x >= lo && x <= hi) put(entry_of(x, id));
+                });
             }
             cluster.sync();
         }
-        if (n_cand <= kList) {
+        if (n_in <= kList) {
             if (rank == 0) {
                 // entry i is the border if the measure up to it reaches the goal and the measure before it does not
-                const int m = min((int)n_cand, (int)s.n_list);
+                const int m = min((int)n_in, (int)s.n_list);
                 if (t == 0) s.thr = thr;
-                if (t < m) s.list_w[t] = measure(distance(of_bits((uint32_t)(s.list[t] >> 32))));
+                if (t < m) s.wide.list_w[t] = measure(value_of_entry(s.wide.list[t]));
                 __syncthreads();
                 if (t < m) {
-                    const u64 e = s.list[t];
+                    const u64 e = s.wide.list[t];
                     u64 cum = before;
-                    for (int i = 0; i < m; ++i) cum += s.list[i] > e ? s.list_w[i] : 0;
-                    if ((double)cum < goal && (double)(cum + s.list_w[t]) >= goal) s.thr = e;
+                    for (int i = 0; i < m; ++i) cum += s.wide.list[i] > e ? s.wide.list_w[i] : 0;
+                    if ((double)cum < goal && (double)(cum + s.wide.list_w[t]) >= goal) s.thr = e;
                 }
             }
             cluster.sync();
             thr = *cluster.map_shared_rank(&s.thr, 0);
         } else if (lo == hi) {
             // equal logits: the first so many of them in order of id
-            const u64 w = measure(distance(of_bits(lo)));
-            u64 want = 1;
+            const u64 w = measure(of_bits(lo)), keep_thr = thr;
             const double miss = goal - (double)before;
-            if (miss > (double)w) want = (u64)ceil(miss / (double)w);
-            u64 ties;
-            const u64 keep_thr = thr;
-            const u64 e = locate([&](float v, int id) { return (u64)(bits_of(v) == lo && entry_of(lo, id) >= keep_thr); }, 0.0, want - 1, ties);
-            thr = e;
+            const u64 want = miss > (double)w ? (u64)ceil(miss / (double)w) : 1;
+            auto tie = [&](float v, int id) { return (u64)(bits_of(v) == lo && entry_of(lo, id) >= keep_thr); };
+            const int groups = (pieces + 31) / 32;
+            u64 mine_all = 0, sum;
+            for (int g = warp; g < groups; g += kWarps) {
+                const int p = 32 * g + lane;
+                uint32_t x = 0;
+                if (p < pieces) {
+                    float v[VN];
+                    piece(p, v);
+#pragma unroll
+                    for (int i = 0; i < VN; ++i) x += (uint32_t)tie(v[i], id0 + p * VN + i);
+                }
+                x = __reduce_add_sync(0xffffffffu, x);
+                if (lane == 0) { s.group[g] = x; mine_all += x; }
+            }
+            __syncthreads();
+            block_exclusive<u64>(mine_all, s.scan, sum);
+            if (t == 0) s.total = sum;
+            cluster.sync();
+            u64 ties = 0;
+            for (int i = 0; i < C; ++i) ties += *cluster.map_shared_rank(&s.total, i);
+            thr = locate(tie, min(want, ties) - 1);
         }
         cluster.sync();
     };
 
-    if (k > 0 && k < a.vocab) select(false, 0.0);
-    if (top_p < 1.f) select(true, (double)top_p);
-    u64 total;
-    const float uf = __ldcg(a.u + row);
-    const u64 e = locate(
-        [&](float v, int id) {
-            if (entry_of(bits_of(v), id) < thr) return (u64)0;
-            const double x = distance(v);
-            return near(x) && (x <= most || x == 0.0) ? weight(x) : (u64)0;
-        },
-        uf > 0.f ? (double)uf : 0.0, 0, total);
-    if (rank == 0 && t == 0) {
-        a.tokens[row] = (int)(0xffffffffu - (uint32_t)e);
-        if (a.logp != nullptr)
-            a.logp[row] = (float)(-(distance(of_bits((uint32_t)(e >> 32))) * 0.69314718055994530942 + log((double)total / kOne)));
+    cluster.sync();                                              // (everyone has read the numbers of candidates; the counts start anew)
+    if (k > 0) {
+        select(false, (double)k);
+        if (top_p < 1.f) total = weigh(false);
     }
+    if (top_p < 1.f) select(true, (double)top_p * (double)total);
+    total = weigh(true);
+    const u64 e = locate(kept, target_of(total));
+    if (rank == 0 && t == 0) emit(e, total);
     cluster.sync();
 }
 
-// Blocks of a row: as many as the slice needs, more while the GPU has room for them.
+// Blocks of a row: slices of up to 64 KB, so that two blocks share an SM; more blocks while the GPU has room for them.
 int blocks_of_row(int rows, int vocab, int elt) {
-    const int most_bytes = 128 * 1024;
     int c = 1;
-    while (c < kMaxCluster && (((long long)vocab * elt > (long long)c * most_bytes) || (vocab > c * 4096 && (long long)rows * c < device_sm_count()))) c *= 2;
+    while (c < kMaxCluster && ((long long)vocab * elt > (long long)c * 64 * 1024 || (vocab > c * 4096 && (long long)rows * c < device_sm_count()))) c *= 2;
     return c;
 }
 
@@ -447,7 +691,11 @@ template <typename T>
 beagle_status launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
     const int c = blocks_of_row(rows, a.vocab, (int)sizeof(T));
     a.slice = ((a.vocab + c - 1) / c + 7) / 8 * 8;
-    const size_t bytes = (sizeof(Shared) + 15) / 16 * 16 + (size_t)(a.slice + 16) * sizeof(T);
+    // the slice; the first block's sums and order of its candidates take its place
+    size_t area = (size_t)(a.slice + 32) * sizeof(T);
+    const size_t finish = (size_t)(a.vocab < kGather ? a.vocab : kGather) * 8 + (size_t)kGather * 4;
+    if (area < finish) area = finish;
+    const size_t bytes = (sizeof(Shared) + 15) / 16 * 16 + area;
     static PerDeviceOnce attr;
     if (!attr.ensure([] { return cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) == cudaSuccess; }))
         return BEAGLE_ERR_CUDA;
