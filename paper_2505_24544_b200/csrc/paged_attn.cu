@@ -34,21 +34,13 @@
 #include <cstring>
 
 #include "pages.h"
-#include "paged_attn.cuh"
-#include "tc_ptx.cuh"
+#include "paged_rows.cuh"
 #include "tensor_map.h"
 
 using namespace beagle;
 
 namespace beagle {
 namespace {
-
-using namespace tc;
-
-constexpr int kConsumers = 4;           // warps; each owns 16 positions of a tile
-constexpr int kPerWarp = kTile / kConsumers;
-constexpr int kStages = 3;
-constexpr int kCtasPerSm = 2;
 
 // The G heads of a pair without a visible position: o = 0, lse = -inf.  Whole CTA.
 template <typename T>
@@ -87,55 +79,10 @@ __device__ __forceinline__ void begin_run(const PagedArgs& a, const Schedule& s,
     }
 }
 
-// The entries' pairs always leave partials, at a place of their own: the part of a pair that begins it at its number, a later one behind
-// them at the run's.
 template <typename T>
 __device__ __forceinline__ void begin_run(const SharedArgs& a, const ScheduleOf<SharedArgs::kEntries>& s, int, int& u0, int& u1) {
-    const Runs runs(s.start[SharedArgs::kEntries], gridDim.x);
-    u0 = runs.begin(blockIdx.x);
-    u1 = runs.begin(blockIdx.x + 1);
-    if (blockIdx.x == 0)                 // for the join
-        for (int i = threadIdx.x; i <= SharedArgs::kEntries; i += blockDim.x) a.start[i] = s.start[i];
+    begin_shared(a, s, threadIdx.x, blockDim.x, u0, u1);
 }
-__device__ __forceinline__ int part_at(const PagedArgs&, int, bool, int seg) { return 2 * blockIdx.x + seg; }
-__device__ __forceinline__ int part_at(const SharedArgs& a, int pair, bool begins, int) { return begins ? pair : a.n_pairs + (int)blockIdx.x; }
-
-__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
-}
-// D (16 x 8, fp32) += A (16 x 16) B (16 x 8); rows 8..15 of A are zero (at most eight query heads share a K/V head)
-__device__ __forceinline__ void mma_rows8(float* d, uint32_t a0, uint32_t a2, uint32_t b0, uint32_t b1) {
-    float z0 = 0.f, z1 = 0.f;
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%5}, {%7,%8}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(z0), "+f"(z1)
-                 : "r"(a0), "r"(0u), "r"(a2), "r"(b0), "r"(b1));
-}
-// Untiled copy: both addresses 16-byte aligned, `bytes` a multiple of 16.
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&t);
-}
-// A launch behind the one that does the common parts starts as soon as that one's blocks have, which they say after their own wait: all
-// that it reads is there.  It waits at its end, so that its completion still says that everything before it has completed.
-__device__ __forceinline__ void wait_inputs(const PagedArgs&) { pdl_wait(); }
-__device__ __forceinline__ void wait_prefix(const PagedArgs&) {}
-__device__ __forceinline__ void wait_inputs(const SharedArgs& a) { if (!a.after_prefix) pdl_wait(); }
-__device__ __forceinline__ void wait_prefix(const SharedArgs& a) { if (a.after_prefix) pdl_wait(); }
-
-template <int DH>
-struct PagedSmem {
-    static constexpr int kTileBytes = kTile * DH * 2;                       // one of K / V
-    static constexpr int kJoin = 2 * 8 * DH * 4;                            // two warps' O rows on their way to the other two
-    static constexpr int kBytes = kStages * 2 * kTileBytes + kJoin + 1024;  // + alignment slack
-};
-
-__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 template <int DH, typename Args>
 __global__ void __launch_bounds__((kConsumers + 1) * 32, kCtasPerSm)
@@ -150,7 +97,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     __shared__ float s_m[kConsumers][8], s_l[kConsumers][8];
     __shared__ int s_abort;
     const uint32_t full = smem_u32(bars), empty = full + 8 * kStages;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, kConsumers); }
@@ -158,218 +104,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         fence_barrier_init();
     }
     pdl_launch_dependents();
-    wait_inputs(a);                      // lengths, table, cache and queries may come from the previous launches
+    pdl_wait();                          // lengths, table, cache and queries may come from the previous launches
     build_schedule(a, s);
     int u0, u1;
     begin_run<bf16>(a, s, DH, u0, u1);
-    if (u0 >= u1) { wait_prefix(a); return; }
-    Walk w;
-    w.seek(s, u0, a.Hkv);
-
-    if (warp == kConsumers) {
-        // ---------------- producer: lane p copies page p of the tile (a tile spans 1, 2, 4 or 8 pages)
-        const int rows = min(1 << a.page_shift, kTile);          // rows of one copy
-        const int parts = kTile / rows;
-        const uint32_t part_bytes = (uint32_t)rows * DH * 2;
-        const uint64_t once = policy_evict_first();
-        bool ok = true;
-        int issued = 0;
-        int next_page = -1;
-        auto page_of = [&](const Walk& x) {                      // this lane's page of the walk's tile, -1 if it holds no position
-            const int pos = x.tile(s) * kTile + lane * rows;
-            int id = -1;
-            // (a part without a visible position stays what it was: its weights and its V rows count as 0)
-            if (lane < parts && pos < s.len[x.b] && (pos + rows > s.lo[x.b] || pos < a.sinks)) id = __ldcg(a.table + (size_t)slot_of(a, x.b) * a.max_pages + (pos >> a.page_shift));
-            return (id >= 0 && id < a.n_pages) ? id : -1;
-        };
-        next_page = page_of(w);
-        for (int u = u0; u < u1; ++u) {
-            const int st = issued % kStages;
-            const int page = next_page;
-            const int pos = w.tile(s) * kTile + lane * rows;
-            const int row = page >= 0 ? ((page * a.Hkv + w.kvh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : 0;
-            w.next(s, a.batch, a.Hkv);
-            if (u + 1 < u1) next_page = page_of(w);              // the next tile's entry is on its way while this one waits for its slot
-            const int copies = __popc(__ballot_sync(0xffffffffu, page >= 0));
-            ok = mbar_wait(empty + 8 * st, ((issued / kStages) & 1) ^ 1, &s_abort);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            if (lane == 0) {
-                if (copies > 0) mbar_expect_tx(full + 8 * st, 2 * copies * part_bytes);
-                else mbar_arrive(full + 8 * st);
-            }
-            __syncwarp();
-            if (page >= 0) {
-                const uint32_t dst = base + st * 2 * SM::kTileBytes + lane * part_bytes;
-#pragma unroll
-                for (int h = 0; h < DH / 64; ++h) tma_load_2d_hint(dst + h * rows * 128, &tmK, full + 8 * st, 64 * h, row, once);
-#pragma unroll
-                for (int h = 0; h < DH / 64; ++h) tma_load_2d_hint(dst + SM::kTileBytes + h * rows * 128, &tmV, full + 8 * st, 64 * h, row, once);
-            }
-            ++issued;
-        }
-        if (!ok)                         // copies already requested still land: wait (bounded) for the last of each stage
-            for (int n = max(0, issued - kStages); n < issued; ++n)
-                for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(full + 8 * (n % kStages), (n / kStages) & 1); ++i) {}
-        wait_prefix(a);
-        return;
-    }
-
-    // ---------------- consumers
-    const int g = lane >> 2, c = lane & 3;
-    const int r_log = min(a.page_shift, 6);                      // log2 rows of a copy
-    const int half_step = 128 << r_log, part_step = DH * 2 << r_log, r_mask = (1 << r_log) - 1;
-    // byte offset of 16-byte piece `chunk` of row r: [copy][64-column half][row][128 bytes], swizzled inside 8 rows
-    auto off = [&](int r, int chunk) {
-        return (uint32_t)((r >> r_log) * part_step + (chunk >> 3) * half_step + (r & r_mask) * 128 + (((chunk & 7) ^ (r & 7)) << 4));
-    };
-    const int row0 = warp * kPerWarp;
-    float o[DH / 8][2], m = -INFINITY, l = 0.f;
-    uint32_t qa[DH / 16][2];
-    int have_q = -1;                                             // the pair whose queries are in registers
-    int seg = 0;                                                 // partial slot: the run's first pair that continues, else the second
-    bool ok = true, first_pair_open = w.i > 0;                   // the first pair began in an earlier run
-#pragma unroll
-    for (int i = 0; i < DH / 8; ++i) o[i][0] = o[i][1] = 0.f;
-    int step = 0;
-    for (int u = u0; u < u1; ++u, ++step) {
-        const int pair = w.b * a.Hkv + w.kvh;
-        if (pair != have_q) {
-            have_q = pair;
-            const bool some = g < rows_of(a, w.b);
-            const uint32_t* qrow = reinterpret_cast<const uint32_t*>(static_cast<const bf16*>(a.q) + query_at(a, w.b, w.kvh, some ? g : 0, DH));
-#pragma unroll
-            for (int ks = 0; ks < DH / 16; ++ks) {
-                qa[ks][0] = some ? __ldcg(qrow + ks * 8 + c) : 0u;
-                qa[ks][1] = some ? __ldcg(qrow + ks * 8 + 4 + c) : 0u;
-            }
-        }
-        const int st = step % kStages;
-        const int pos0 = w.tile(s) * kTile + row0;               // first position of this warp
-        const int len = s.len[w.b], lo = s.lo[w.b];
-        const bool plain = pos0 + kPerWarp <= len && (pos0 >= lo || pos0 + kPerWarp <= a.sinks);
-        // A wait that runs out leaves NaN in what depends on it; the warp still meets the others where pairs end.
-        if (ok) ok = mbar_wait(full + 8 * st, (step / kStages) & 1, &s_abort);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) l = __int_as_float(0x7fffffff);
-        const uint32_t sK = base + st * 2 * SM::kTileBytes, sV = sK + SM::kTileBytes;
-        if (ok && pos0 < len && (pos0 + kPerWarp > lo || pos0 < a.sinks)) {
-            float sc[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
-#pragma unroll
-            for (int dg = 0; dg < DH / 32; ++dg)
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    uint32_t b0, b1, b2, b3;
-                    ldsm4(sK + off(row0 + nt * 8 + (lane & 7), 4 * dg + (lane >> 3)), b0, b1, b2, b3);
-                    mma_rows8(sc[nt], qa[2 * dg][0], qa[2 * dg][1], b0, b1);
-                    mma_rows8(sc[nt], qa[2 * dg + 1][0], qa[2 * dg + 1][1], b2, b3);
-                }
-            uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;   // V rows (2c, 2c+1) and (2c+8, 2c+9) as 16-bit lanes
-            float mx = -INFINITY;
-#pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float x = sc[nt][e] * a.scale_log2;
-                    if (!plain) {
-                        const int pos = pos0 + nt * 8 + 2 * c + e;
-                        const bool vis = pos < len && (pos >= lo || pos < a.sinks);
-                        x = vis ? x : -INFINITY;
-                        if (!vis) (nt == 0 ? keep0 : keep1) &= e == 0 ? 0xffff0000u : 0x0000ffffu;
-                    }
-                    sc[nt][e] = x;
-                    mx = fmaxf(mx, x);
-                }
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            // the reference point moves only when a score exceeds it by more than kSlack: weights stay below 2^8
-            const bool grow = mx > m + kSlack;
-            if (__any_sync(0xffffffffu, grow)) {
-                const float f = (grow && m != -INFINITY) ? exp2f(m - mx) : 1.f;
-                if (grow) m = mx;
-                l *= f;
-#pragma unroll
-                for (int i = 0; i < DH / 8; ++i) { o[i][0] *= f; o[i][1] *= f; }
-            }
-            const float neg = m == -INFINITY ? 0.f : -m;         // no visible position so far: every score is -inf, every weight 0
-            uint32_t pa[2];
-#pragma unroll
-            for (int nt = 0; nt < 2; ++nt) {
-                const float p0 = exp2f(sc[nt][0] + neg), p1 = exp2f(sc[nt][1] + neg);
-                l += p0 + p1;                                    // fp32, unrounded; the product below takes the weights in bf16
-                pa[nt] = pack2(p0, p1);
-            }
-            const int mi = lane >> 3;
-#pragma unroll
-            for (int jp = 0; jp < DH / 16; ++jp) {
-                uint32_t b0, b1, b2, b3;
-                ldsm4_t(sV + off(row0 + 8 * (mi & 1) + (lane & 7), 2 * jp + (mi >> 1)), b0, b1, b2, b3);
-                if (!plain) { b0 &= keep0; b1 &= keep1; b2 &= keep0; b3 &= keep1; }
-                mma_rows8(o[2 * jp], pa[0], pa[1], b0, b1);
-                mma_rows8(o[2 * jp + 1], pa[0], pa[1], b2, b3);
-            }
-        }
-        __syncwarp();
-        if (ok && lane == 0) mbar_arrive(empty + 8 * st);
-        const int b = w.b, kvh = w.kvh;
-        const bool last = w.i + 1 == w.n;
-        w.next(s, a.batch, a.Hkv);
-        if (!last && u + 1 < u1) continue;
-
-        // ---- the pair (or this run's part of it) is done: join the four warps, rows = heads
-        l += __shfl_xor_sync(0xffffffffu, l, 1);
-        l += __shfl_xor_sync(0xffffffffu, l, 2);
-        if (c == 0) { s_m[warp][g] = m; s_l[warp][g] = l; }
-        consumers_sync();
-        float M = -INFINITY, L = 0.f;
-#pragma unroll
-        for (int i = 0; i < kConsumers; ++i) M = fmaxf(M, s_m[i][g]);
-#pragma unroll
-        for (int i = 0; i < kConsumers; ++i) L += s_m[i][g] == -INFINITY ? s_l[i][g] : s_l[i][g] * exp2f(s_m[i][g] - M);      // (no position seen: the sum is 0)
-        const float f = m == -INFINITY ? 0.f : exp2f(m - M);
-#pragma unroll
-        for (int i = 0; i < DH / 8; ++i) { o[i][0] *= f; o[i][1] *= f; }
-        // warps 2, 3 hand theirs to 0, 1; then 1 to 0
-#pragma unroll
-        for (int from = 2; from >= 1; --from) {
-            if (warp >= from && warp < 2 * from) {
-                float* dst = join + (size_t)(warp - from) * 8 * DH + g * DH + 2 * c;
-#pragma unroll
-                for (int i = 0; i < DH / 8; ++i) *reinterpret_cast<float2*>(dst + 8 * i) = make_float2(o[i][0], o[i][1]);
-            }
-            consumers_sync();
-            if (warp < from) {
-                const float* src = join + (size_t)warp * 8 * DH + g * DH + 2 * c;
-#pragma unroll
-                for (int i = 0; i < DH / 8; ++i) {
-                    const float2 x = *reinterpret_cast<const float2*>(src + 8 * i);
-                    o[i][0] += x.x; o[i][1] += x.y;
-                }
-            }
-            consumers_sync();
-        }
-        if (warp == 0 && g < rows_of(a, b)) {
-            const int head = kvh * a.G + g;
-            if (!Args::kShared && last && !first_pair_open) {    // all of the pair's tiles were in this run
-                const float inv = L != 0.f ? 1.f / L : 0.f;
-                uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<bf16*>(a.o) + ((size_t)b * a.Hq + head) * DH) + c;
-#pragma unroll
-                for (int i = 0; i < DH / 8; ++i) dst[4 * i] = pack2(o[i][0] * inv, o[i][1] * inv);
-                if (c == 0 && a.lse != nullptr) a.lse[(size_t)b * a.Hq + head] = L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
-            } else {
-                float* dst = a.part + ((size_t)part_at(a, b * a.Hkv + kvh, !first_pair_open, seg) * 8 + g) * (DH + 2);
-#pragma unroll
-                for (int i = 0; i < DH / 8; ++i) *reinterpret_cast<float2*>(dst + 8 * i + 2 * c) = make_float2(o[i][0], o[i][1]);
-                if (c == 0) { dst[DH] = M; dst[DH + 1] = L; }
-            }
-        }
-        first_pair_open = false;
-        seg = 1;
-        m = -INFINITY; l = 0.f;
-#pragma unroll
-        for (int i = 0; i < DH / 8; ++i) o[i][0] = o[i][1] = 0.f;
-    }
-    wait_prefix(a);
+    if (u0 >= u1) return;
+    attn_rows<DH>(tmK, tmV, a, s, base, join, full, empty, s_m, s_l, &s_abort, threadIdx.x >> 5, u0, u1);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -727,44 +467,38 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
 // common part, which lie with the row's launch or (`prefix.on`) with the tensor cores'.
 constexpr int kJoinFlight = 4;
 struct PrefixParts {
-    const int* start;
+    const int2* span;
     const float* part;
-    int n_pairs, runs, part_rows, block;
+    int n_pairs, part_rows, block;
     uint8_t on[kMaxCallBatch], entry[kMaxCallBatch];
 };
 template <typename T, int DH>
-__global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(const __grid_constant__ SharedArgs a, const __grid_constant__ PrefixParts prefix, int n_runs) {
+__global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(const __grid_constant__ SharedArgs a, const __grid_constant__ PrefixParts prefix) {
     __shared__ float s_o[kJoinWarps][DH], s_m[kJoinWarps], s_l[kJoinWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     pdl_wait();
     const int b = blockIdx.x, head = blockIdx.y, kvh = head / a.G, h = head - kvh * a.G, group = a.group_of[b];
     const bool common = group != 255, cores = common && prefix.on[group];
-    // source 0: the row's own positions, 1: the common part.  Of each the pair, the runs that worked on it, this head's row in a partial
+    // the row's own positions and the common part: of each the pair, the runs that worked on it, this head's row in a partial
     struct Source {
         const float* part;
         size_t size;                     // floats of a partial
         int o, ml;                       // offsets of the row's O and of its (maximum, sum)
         int pair, n_pairs, r0, r1;
-        Runs runs;
     };
     auto source = [&](bool first) {
         const bool tc = !first && cores;
-        const int* start = tc ? prefix.start : a.start;
-        Source x = {tc ? prefix.part : a.part, 0, 0, 0, 0, tc ? prefix.n_pairs : a.n_pairs, 0, -1, Runs(__ldcg(start + SharedArgs::kEntries), tc ? prefix.runs : n_runs)};
         int e = b, at = h;
         if (!first) {
             const int j = common ? (b - a.group_row0[group]) * a.G + h : 0, block = tc ? prefix.block : a.block;
             e = common ? (tc ? prefix.entry[group] : a.prefix_entry[group]) + j / block : 0;
             at = j % block;
         }
-        const int rows = tc ? prefix.part_rows : 8, s0 = __ldcg(start + e), n = (__ldcg(start + e + 1) - s0) / a.Hkv, u0 = s0 + kvh * n;
-        x.size = (size_t)rows * (DH + 2);
-        x.o = tc ? at * DH : at * (DH + 2);
-        x.ml = tc ? rows * DH + 2 * at : at * (DH + 2) + DH;
-        x.pair = e * a.Hkv + kvh;
-        if (n > 0 && (first || common)) { x.r0 = x.runs.of(u0); x.r1 = x.runs.of(u0 + n - 1); }
-        return x;
+        const int rows = tc ? prefix.part_rows : 8, pair = e * a.Hkv + kvh;
+        const int2 runs = first || common ? __ldcg((tc ? prefix.span : a.span) + pair) : make_int2(0, -1);
+        return Source{tc ? prefix.part : a.part, (size_t)rows * (DH + 2), tc ? at * DH : at * (DH + 2), tc ? rows * DH + 2 * at : at * (DH + 2) + DH,
+                      pair, tc ? prefix.n_pairs : a.n_pairs, runs.x, runs.y};
     };
     const Source own = source(true), shared = source(false);
     const int n0 = own.r1 - own.r0 + 1, all = n0 + shared.r1 - shared.r0 + 1;
@@ -783,8 +517,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(cons
             const int i = i0 + z * kJoinWarps;
             const Source& x = i < n0 ? own : shared;
             const int r = x.r0 + (i < n0 ? i : i - n0);
-            // (fewer tiles than runs: some runs between are empty and left no partial)
-            const bool some = i < all && !(x.runs.total < x.runs.runs && x.runs.begin(r) >= x.runs.begin(r + 1));
+            const bool some = i < all;
             const float* p = x.part + (some ? (size_t)(r == x.r0 ? x.pair : x.n_pairs + r) * x.size : 0);
             m[z] = some ? __ldcg(p + x.ml) : -INFINITY;
             l[z] = some ? __ldcg(p + x.ml + 1) : 0.f;
@@ -869,7 +602,6 @@ __global__ void __launch_bounds__(256) pages_shared_kernel(const int32_t* table,
     if (t == 0) shared[g] = s_pages * page_size;
 }
 
-constexpr size_t kStartBytes = 1024;     // the schedule's offsets, in front of the shared form's partials
 constexpr int kMaxRuns = 2048;           // bound of the workspace; the grid is min(this, CTAs that fit the GPU)
 constexpr int kSimtCtasPerSm = 2;
 // Pairs of at most this many tiles are not cut: the join launch takes some 3 us, a tile on its own 0.4 (tensor cores), 0.9 (up to four
@@ -897,8 +629,8 @@ struct SharedCall : SharedArgs {         // the rows' launch, and where the tens
     PrefixParts prefix;
 };
 template <typename T, int DH>
-void launch_join(const SharedCall& a, int runs, cudaStream_t stream) {
-    launch_pdl(paged_shared_join_kernel<T, DH>, dim3(a.rows, a.Hq), dim3(kJoinWarps * 32), 0, stream, static_cast<const SharedArgs&>(a), a.prefix, runs);
+void launch_join(const SharedCall& a, int, cudaStream_t stream) {
+    launch_pdl(paged_shared_join_kernel<T, DH>, dim3(a.rows, a.Hq), dim3(kJoinWarps * 32), 0, stream, static_cast<const SharedArgs&>(a), a.prefix);
 }
 template <typename Args> struct KernelArgs { typedef PagedArgs type; };
 template <> struct KernelArgs<SharedCall> { typedef SharedArgs type; };
@@ -965,6 +697,14 @@ beagle_status launch_attn(const beagle_pages* p, const Args& a, int runs, cudaSt
     else st = launch_simt<float, 16>(a, runs, stream);
     if (st != BEAGLE_OK) return st;
     return cudaGetLastError() == cudaSuccess ? BEAGLE_OK : BEAGLE_ERR_CUDA;
+}
+
+beagle_status check_heads(const beagle_pages* p, int Hq) {
+    if (Hq <= 0) return BEAGLE_ERR_INVALID_ARG;
+    if (Hq % p->n_kv_heads || Hq / p->n_kv_heads > 8) return BEAGLE_ERR_SHAPE;
+    // the widest rows with more than four grouped heads: as for the decode step of the draft head, no kernel has that shape
+    if (p->dtype == BEAGLE_BF16 && p->head_dim == 256 && Hq / p->n_kv_heads > 4) return BEAGLE_ERR_SHAPE;
+    return BEAGLE_OK;
 }
 
 // The call's arguments that both forms share, from checked values.
@@ -1045,27 +785,23 @@ void plan_shared(const beagle_pages* p, int Hq, int batch, int n_groups, const i
     f->batch = fe;
     f->n_pairs = fe * p->n_kv_heads;
     f->part_rows = (most + 3) / 4 * 4;
-    a->after_prefix = fe > 0;
 }
 int shared_runs(const beagle_pages* p) {
     const int runs = device_sm_count() * (uses_mma(p) ? kCtasPerSm : kSimtCtasPerSm);
     return runs < kMaxRuns ? runs : kMaxRuns;
 }
-// Bytes of the call's workspace and where the two launches' partials begin.
-size_t shared_ws(const beagle_pages* p, const SharedArgs& a, const PrefixArgs& f, size_t* own, size_t* common) {
-    const size_t row = (size_t)(p->head_dim + 2) * sizeof(float), mine = 2 * kStartBytes,
-                 theirs = mine + ((size_t)(a.n_pairs + shared_runs(p)) * 8 * row + 255) / 256 * 256;
-    if (own != nullptr) *own = mine;
-    if (common != nullptr) *common = theirs;
-    return theirs + (f.batch > 0 ? ((size_t)(f.n_pairs + shared_runs(p)) * f.part_rows * row + 255) / 256 * 256 : 0);
-}
-
-beagle_status check_heads(const beagle_pages* p, int Hq) {
-    if (Hq <= 0) return BEAGLE_ERR_INVALID_ARG;
-    if (Hq % p->n_kv_heads || Hq / p->n_kv_heads > 8) return BEAGLE_ERR_SHAPE;
-    // the widest rows with more than four grouped heads: as for the decode step of the draft head, no kernel has that shape
-    if (p->dtype == BEAGLE_BF16 && p->head_dim == 256 && Hq / p->n_kv_heads > 4) return BEAGLE_ERR_SHAPE;
-    return BEAGLE_OK;
+// The call's workspace: where each form's runs of the pairs and partials lie; bytes.
+struct SharedLayout { size_t span, prefix_span, part, prefix_part, bytes; };
+SharedLayout shared_ws(const beagle_pages* p, const SharedArgs& a, const PrefixArgs& f) {
+    const size_t row = (size_t)(p->head_dim + 2) * sizeof(float);
+    auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    SharedLayout l;
+    l.span = 0;
+    l.prefix_span = l.span + up(a.n_pairs * sizeof(int2));
+    l.part = l.prefix_span + up(f.n_pairs * sizeof(int2));
+    l.prefix_part = l.part + up((size_t)(a.n_pairs + shared_runs(p)) * 8 * row);
+    l.bytes = l.prefix_part + (f.batch > 0 ? up((size_t)(f.n_pairs + shared_runs(p)) * f.part_rows * row) : 0);
+    return l;
 }
 
 }  // namespace
@@ -1184,7 +920,7 @@ beagle_status beagle_paged_attn_shared_workspace_bytes(const beagle_pages* p, in
     memset(static_cast<void*>(&a), 0, sizeof(a));
     memset(static_cast<void*>(&f), 0, sizeof(f));
     plan_shared(p, n_q_heads, batch, n_groups, group_rows_host, &a, &f);
-    *bytes = shared_ws(p, a, f, nullptr, nullptr);
+    *bytes = shared_ws(p, a, f).bytes;
     return BEAGLE_OK;
 }
 
@@ -1206,7 +942,8 @@ beagle_status beagle_paged_attn_shared(const beagle_pages* p, int32_t batch, con
     if (batch == 0) return BEAGLE_OK;
     if (shared_dev == nullptr || ((uintptr_t)shared_dev & 3)) return BEAGLE_ERR_INVALID_ARG;
     plan_shared(p, n_q_heads, batch, n_groups, group_rows_host, &a, &f);
-    st = check_call(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, ws_dev, ws_bytes, shared_ws(p, a, f, nullptr, nullptr));
+    const SharedLayout l = shared_ws(p, a, f);
+    st = check_call(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, ws_dev, ws_bytes, l.bytes);
     if (st != BEAGLE_OK) return st;
     if (!paged_attn_fits(p, a.batch) || !paged_attn_fits(p, f.batch)) return BEAGLE_ERR_CAPACITY;
     fill_args(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, &a);
@@ -1214,23 +951,22 @@ beagle_status beagle_paged_attn_shared(const beagle_pages* p, int32_t batch, con
     fill_args(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, &f);
     a.shared = f.shared = shared_dev;
     char* base = static_cast<char*>(ws_dev);
-    a.start = reinterpret_cast<int*>(base);
-    f.start = reinterpret_cast<int*>(base + kStartBytes);
-    size_t own = 0, common = 0;
-    shared_ws(p, a, f, &own, &common);
-    a.part = reinterpret_cast<float*>(base + own);
-    f.part = reinterpret_cast<float*>(base + common);
+    a.span = reinterpret_cast<int2*>(base + l.span);
+    f.span = reinterpret_cast<int2*>(base + l.prefix_span);
+    a.part = reinterpret_cast<float*>(base + l.part);
+    f.part = reinterpret_cast<float*>(base + l.prefix_part);
+    a.prefix.span = f.span; a.prefix.part = f.part;
+    a.prefix.n_pairs = f.n_pairs; a.prefix.part_rows = f.part_rows; a.prefix.block = f.block;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    const int runs = shared_runs(p);                     // (not more than the cache's capacity has tiles)
+    const int runs = shared_runs(p);
     if (f.batch > 0) {
-        const long long most = (long long)f.n_pairs * most_tiles(p, 0, 0);
-        f.runs = (int)(runs < most ? runs : most);
-        a.prefix.start = f.start; a.prefix.part = f.part;
-        a.prefix.n_pairs = f.n_pairs; a.prefix.runs = f.runs; a.prefix.part_rows = f.part_rows; a.prefix.block = f.block;
-        st = launch_prefix(p, f, f.runs, stream);
+        st = launch_grouped(p, a, f, runs, stream);
         if (st != BEAGLE_OK) return st;
+        if (p->head_dim == 128) launch_join<bf16, 128>(a, runs, stream);
+        else launch_join<bf16, 64>(a, runs, stream);
+        return cudaGetLastError() == cudaSuccess ? BEAGLE_OK : BEAGLE_ERR_CUDA;
     }
-    const long long most = (long long)a.n_pairs * most_tiles(p, 0, 0);
+    const long long most = (long long)a.n_pairs * most_tiles(p, 0, 0);           // (no more runs than the cache's capacity has tiles)
     return launch_attn(p, a, (int)(runs < most ? runs : most), stream);
 }
 

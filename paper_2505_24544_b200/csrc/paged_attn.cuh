@@ -1,5 +1,5 @@
 // Attention over a paged key/value cache: arguments, and how the visible tiles are divided among thread blocks on the device, where the
-// lengths are.  Shared by the one-token kernels (paged_attn.cu) and the common part of groups of rows (paged_prefix.cu).
+// lengths are.  Shared by the one-token kernels (paged_attn.cu) and the common part of groups of rows (paged_grouped.cu).
 #pragma once
 #include "pages.h"
 
@@ -42,14 +42,13 @@ struct SharedArgs : PagedArgs {         // `batch` counts the entries
     static constexpr bool kShared = true;
     static constexpr int kEntries = 2 * kMaxCallBatch;
     const int32_t* shared;
-    int* start;                         // [kEntries + 1] the schedule's, in the workspace
+    int2* span;                         // [n_pairs] first and last run that worked on a pair (first > last: none), in the workspace
     int rows, n_groups, n_pairs;        // rows of the call; entries * Hkv
     SharedEntry entry[kEntries];
     uint8_t group_of[kMaxCallBatch];    // of a row; 255 as above
     uint8_t prefix_entry[kMaxCallBatch];        // first entry of a group's common part (the rows' own entries have the rows' numbers)
     uint8_t group_row0[kMaxCallBatch];
     int block;                          // query rows of a common part's entry
-    int after_prefix;                   // the launch before it is paged_prefix.cu's, whose results only the join needs
 };
 
 // How the visible tiles are divided; computed by every CTA from the lengths (64 values at most).
@@ -190,13 +189,27 @@ struct Walk {
     __device__ __forceinline__ int tile(const ScheduleOf<N>& s) const { return i < s.sink_tiles[b] ? i : s.first[b] + i - s.sink_tiles[b]; }
 };
 
+// The shared form's runs: never more than there are tiles, so that every run between two others has some.
+__device__ __forceinline__ Runs shared_runs_of(int total) { return Runs(total, max(1, min(total, (int)gridDim.x))); }
+// The units of this CTA's run; threads 0 <= t < n leave word of which runs work on which pair (shared out over the CTAs).
+__device__ __forceinline__ void begin_shared(const SharedArgs& a, const ScheduleOf<SharedArgs::kEntries>& s, int t, int n_threads, int& u0, int& u1) {
+    const Runs runs = shared_runs_of(s.start[SharedArgs::kEntries]);
+    u0 = (int)blockIdx.x < runs.runs ? runs.begin(blockIdx.x) : runs.total;
+    u1 = (int)blockIdx.x < runs.runs ? runs.begin(blockIdx.x + 1) : runs.total;
+    if (t < 0) return;
+    for (int p = blockIdx.x + gridDim.x * t; p < a.n_pairs; p += gridDim.x * n_threads) {
+        const int e = p / a.Hkv, n = tiles_of(s, e, a.Hkv), first = s.start[e] + (p - e * a.Hkv) * n;
+        a.span[p] = n > 0 ? make_int2(runs.of(first), runs.of(first + n - 1)) : make_int2(0, -1);
+    }
+}
+
 // What beagle_paged_attn_shared leaves to the tensor cores: the common parts of groups with many query rows.  `entry` holds blocks of up
 // to 128 query rows; part_rows is the largest of them, rounded up to 4: a partial is part_rows rows of O, then their (maximum, sum).
 struct PrefixArgs : SharedArgs {
-    int part_rows, runs;
+    int part_rows;
     uint8_t on[kMaxCallBatch];           // of a group: its common part is done there
 };
-beagle_status launch_prefix(const beagle_pages* p, const PrefixArgs& a, int runs, cudaStream_t stream);
+beagle_status launch_grouped(const beagle_pages* p, const SharedArgs& rows, const PrefixArgs& prefix, int runs, cudaStream_t stream);
 int prefix_block(int G);                 // query rows of a block: whole rows of the call
 
 }  // namespace beagle

@@ -12,15 +12,12 @@
 // exceeds it by more than 2^8.  S is double-buffered.  All positions of the common part are visible: nothing is masked.
 #include <cuda.h>
 
-#include "paged_attn.cuh"
-#include "tc_ptx.cuh"
+#include "paged_rows.cuh"
 #include "tensor_map.h"
 #include "win_ptx.cuh"
 
 namespace beagle {
 namespace {
-
-using namespace tc;
 
 constexpr int kThreads = 192;            // warp 0: TMA producer, warp 1: issues the products, warps 2-5: softmax
 constexpr int kRows = 128;               // query rows of a tile
@@ -28,7 +25,9 @@ constexpr int kRows = 128;               // query rows of a tile
 template <int DH>
 struct PrefixSmem {
     static constexpr int kQ = kRows * DH * 2, kT = kTile * DH * 2;           // Q; a K or V tile, two stages of each
-    static constexpr int kBytes = kQ + 4 * kT + 256 + 1024;                  // + barriers, alignment slack
+    static constexpr int kRing = kQ + 4 * kT;                                // as much as the rows' ring
+    static_assert(kRing == kStages * 2 * PagedSmem<DH>::kTileBytes, "both kinds of work use the same memory in turn");
+    static constexpr int kBytes = kRing + PagedSmem<DH>::kJoin + 1024;       // + alignment slack
 };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2) {
@@ -37,48 +36,20 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
                  : "memory");
 }
 
+// The common parts' run [u, u1) of this CTA: warp 0 producer, 1 issues the products, 2..5 softmax.  Ends with all of shared and tensor memory free.
 template <int DH>
-__global__ void __launch_bounds__(kThreads, 2) paged_prefix_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                                                                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PrefixArgs a) {
+__device__ __forceinline__ void attn_prefix(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PrefixArgs& a,
+                                            const ScheduleOf<SharedArgs::kEntries>& s, uint8_t* smem, uint64_t* bars, uint32_t tmem, volatile int* s_abort, int warp,
+                                            int u, int u1) {
     using SM = PrefixSmem<DH>;
     constexpr int kHalves = DH / 64;
-    constexpr uint32_t kTmem = 256, kO = 128;            // S / P at columns 0 and 64, O at 128
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    constexpr uint32_t kO = 128;                                 // S / P at columns 0 and 64, O at 128
     const uint32_t sQ = smem_u32(smem), sK = sQ + SM::kQ, sV = sK + 2 * SM::kT;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + SM::kQ + 4 * SM::kT);
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t q_full = bar0, k_full = bar0 + 16, k_empty = bar0 + 32, v_full = bar0 + 48, s_full = bar0 + 64, p_full = bar0 + 80,
                    pv_done = bar0 + 96;                          // all but the first: one per stage
-    uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(bars + 14);
-    volatile int* s_abort = reinterpret_cast<int*>(bars + 15);
-    __shared__ ScheduleOf<SharedArgs::kEntries> s;
-
-    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    if (threadIdx.x == 0) {
-        mbar_init(q_full, 1);
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(k_full + 8 * i, 1); mbar_init(k_empty + 8 * i, 1); mbar_init(v_full + 8 * i, 1);
-            mbar_init(s_full + 8 * i, 1); mbar_init(p_full + 8 * i, 4); mbar_init(pv_done + 8 * i, 1);
-        }
-        *s_abort = 0;
-        fence_barrier_init();
-    }
-    if (warp == 1) tmem_alloc<kTmem>(smem_u32(&s_tmem));
-    fence_before();
-    pdl_wait();
-    // (after the wait: what comes next may rely on everything before this kernel)
-    pdl_launch_dependents();
-    build_schedule(a, s);
-    fence_after();
-    const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-    const Runs runs(s.start[SharedArgs::kEntries], gridDim.x);
-    const int u1 = runs.begin(blockIdx.x + 1);
-    int u = runs.begin(blockIdx.x);
-    if (blockIdx.x == 0)                                         // for the join
-        for (int i = threadIdx.x; i <= SharedArgs::kEntries; i += kThreads) a.start[i] = s.start[i];
-
-    bool ok = true;
+    const int lane = threadIdx.x & 31;
+    bool ok = *s_abort == 0;
     int done = 0;                                                // tiles of this CTA's earlier pairs: stages and phases run on
     for (int seg = 0; u < u1; ++seg) {
         Walk w;
@@ -251,6 +222,58 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prefix_kernel(const __grid_
         fence_after();
         ok = *s_abort == 0;
     }
+}
+
+template <int DH>
+__global__ void __launch_bounds__(kThreads, 2) paged_grouped_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                                                                   const __grid_constant__ CUtensorMap tmV, const __grid_constant__ SharedArgs rows,
+                                                                   const __grid_constant__ PrefixArgs prefix) {
+    using SM = PrefixSmem<DH>;
+    constexpr uint32_t kTmem = 256;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    __shared__ __align__(8) uint64_t bars[14 + 2 * kStages];
+    __shared__ ScheduleOf<SharedArgs::kEntries> s_rows, s_prefix;
+    __shared__ float s_m[kConsumers][8], s_l[kConsumers][8];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
+    const uint32_t full = smem_u32(bars + 14), empty = full + 8 * kStages;
+    if (threadIdx.x == 0) {
+        const uint32_t bar0 = smem_u32(bars);
+        mbar_init(bar0, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar0 + 16 + 8 * i, 1); mbar_init(bar0 + 32 + 8 * i, 1); mbar_init(bar0 + 48 + 8 * i, 1);
+            mbar_init(bar0 + 64 + 8 * i, 1); mbar_init(bar0 + 80 + 8 * i, 4); mbar_init(bar0 + 96 + 8 * i, 1);
+        }
+        for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, kConsumers); }
+        s_abort = 0;
+        fence_barrier_init();
+    }
+    if (warp == 1) tmem_alloc<kTmem>(smem_u32(&s_tmem));
+    fence_before();
+    pdl_launch_dependents();
+    pdl_wait();
+    build_schedule(rows, s_rows);
+    build_schedule(prefix, s_prefix);
+    fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+    int u0, u1, p0, p1;
+    const int helper = (int)threadIdx.x - 32;                    // the second warp, which has the least to do
+    begin_shared(rows, s_rows, helper, kThreads - 32, u0, u1);
+    begin_shared(prefix, s_prefix, helper, kThreads - 32, p0, p1);
+    // the upper half of the CTAs, the second ones on their SMs, begin with the rows: one kind of work waits for memory, the other for the products
+    const bool rows_first = blockIdx.x >= gridDim.x / 2;
+    for (int phase = 0; phase < 2; ++phase) {
+        if ((phase == 0) == rows_first) {
+            const int role = warp == 0 ? kConsumers : warp - 2;  // (the second warp: none)
+            if (u0 < u1 && role >= 0)
+                attn_rows<DH>(tmK, tmV, rows, s_rows, smem_u32(smem), reinterpret_cast<float*>(smem + SM::kRing), full, empty, s_m, s_l, &s_abort, role, u0, u1);
+            __syncthreads();
+        } else {
+            attn_prefix<DH>(tmQ, tmK, tmV, prefix, s_prefix, smem, bars, tmem, &s_abort, warp, p0, p1);
+        }
+    }
     fence_before();
     __syncthreads();
     if (warp == 1) {
@@ -260,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_prefix_kernel(const __grid_
 }
 
 template <int DH>
-beagle_status launch(const beagle_pages* p, const PrefixArgs& a, int runs, cudaStream_t stream) {
+beagle_status launch(const beagle_pages* p, const SharedArgs& rows, const PrefixArgs& a, int runs, cudaStream_t stream) {
     using SM = PrefixSmem<DH>;
     const EncodeTiled encode = tensor_map_encoder();
     if (encode == nullptr) return BEAGLE_ERR_CUDA;
@@ -279,9 +302,9 @@ beagle_status launch(const beagle_pages* p, const PrefixArgs& a, int runs, cudaS
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return BEAGLE_ERR_CUDA;
     static PerDeviceOnce attr;
-    if (!attr.ensure([] { return cudaFuncSetAttribute(paged_prefix_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes) == cudaSuccess; }))
+    if (!attr.ensure([] { return cudaFuncSetAttribute(paged_grouped_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes) == cudaSuccess; }))
         return BEAGLE_ERR_CUDA;
-    launch_pdl(paged_prefix_kernel<DH>, dim3(runs), dim3(kThreads), (size_t)SM::kBytes, stream, mq, mk, mv, a);
+    launch_pdl(paged_grouped_kernel<DH>, dim3(runs), dim3(kThreads), (size_t)SM::kBytes, stream, mq, mk, mv, rows, a);
     return cudaGetLastError() == cudaSuccess ? BEAGLE_OK : BEAGLE_ERR_CUDA;
 }
 
@@ -289,8 +312,8 @@ beagle_status launch(const beagle_pages* p, const PrefixArgs& a, int runs, cudaS
 
 int prefix_block(int G) { return kRows / G * G; }
 
-beagle_status launch_prefix(const beagle_pages* p, const PrefixArgs& a, int runs, cudaStream_t stream) {
-    return p->head_dim == 128 ? launch<128>(p, a, runs, stream) : launch<64>(p, a, runs, stream);
+beagle_status launch_grouped(const beagle_pages* p, const SharedArgs& rows, const PrefixArgs& prefix, int runs, cudaStream_t stream) {
+    return p->head_dim == 128 ? launch<128>(p, rows, prefix, runs, stream) : launch<64>(p, rows, prefix, runs, stream);
 }
 
 }  // namespace beagle
