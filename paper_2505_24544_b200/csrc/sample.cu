@@ -10,16 +10,19 @@
 // A row belongs to a cluster of up to 8 thread blocks, each of which keeps its slice of the logits in shared memory: they are read
 // from memory once (the floor of the call), all passes after that stay on chip and take two fp32 operations a token where nothing more is
 // known of it.  What costs is the double-precision weight (some 25 instructions), so it is formed
-//   - of all tokens only if top-k does not limit them: the total is needed then;
+//   - of all tokens, once, only if top-k does not limit them: the total is needed then.  top-p: a histogram of fp32 weights says beforehand
+//     in which few bins of distance the border lies, so that the same pass finds the exact weight before them and lists their tokens;
 //   - otherwise of candidates alone, those a bound in fp32 does not exclude.  top-k: at least k groups of a few neighbours (the ones read as
-//     one 16-byte piece) have their largest in the leading bins of a histogram, so the k-th token is in those too.  top-p: the tokens
-//     beyond a distance x weigh at most V 2^-x together.  min-p: its distance.
-// Up to kGather candidates, nearly always, go to the first block, which sorts them and finishes the row alone; the others leave.  More of
-// them: the cluster finds each border with a histogram whose counts bracket the weights, one exact pass, and a list of the tokens
+//     one 16-byte piece) have their largest in the leading bins of a histogram, so the k-th token is in those too.  min-p: its distance.
+// Up to kGather candidates or tokens of the border's bins, nearly always, go to the first block, which sorts them.  More of them:
+// the cluster finds each border with a histogram whose counts bracket the weights, one exact pass, and a list of the tokens
 // in the few bins left, compared pairwise; more than kList of those: their range of logit bits is divided further, by 2048 a level
 // with exact weights, until few are left, or only equal logits, which are taken in order of id.
 #include <cooperative_groups.h>
 #include <math_constants.h>
+
+#include <atomic>
+#include <type_traits>
 
 #include "../../include/beagle.h"
 #include "common.cuh"
@@ -41,13 +44,14 @@ constexpr int kMaxCluster = 8;
 constexpr int kMaxVocab = 1 << 18;
 constexpr int kMaxGroups = kMaxVocab / kMaxCluster / 128 + 8;      // of 32 16-byte pieces (128 fp32 logits, 256 bf16) in a block's slice
 constexpr double kOne = 35184372088832.0;        // 2^45
+constexpr u64 kMagicBits = 0x4330000000000000ull;        // of 2^52: a double from there on holds an integer in its low bits
 constexpr float kFar = 47.f;             // log2 distance from which on the weight is 0 (2^45 * 2^-47 rounds to 0)
 constexpr float kMost = 3.402823466e38f;
 
 struct SampleArgs {
     const void* logits;
     long long stride;
-    int vocab, slice;                    // slice: tokens of a block (a multiple of 8)
+    int rows, vocab, slice;                    // slice: tokens of a block (a multiple of 8)
     const float *temperature, *top_p, *min_p, *u;
     const int32_t* top_k;
     int32_t* tokens;
@@ -65,8 +69,8 @@ struct Shared {
     };
     u64 group[kMaxGroups];               // weight of every group of 32 pieces
     u64 scan[kWarps];
-    double root[32];                     // 2^(-j / 32)
-    u64 sum[2], total, thr, found;
+    double root[32];                     // 2^(45 - j / 32)
+    u64 sum[2], all, total, thr, found;
     uint32_t top, least, id, lo, hi, n_cand, n_list, bin[2], cut;
 };
 
@@ -123,16 +127,12 @@ __device__ __forceinline__ void block_sort(N* x, int n) {
         }
 }
 
+// One row.  A block that returns is done with the others' shared memory, and they with its own, but for the first block's when it finishes alone.
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
-    extern __shared__ __align__(16) uint8_t smem[];
-    Shared& s = *reinterpret_cast<Shared*>(smem);
+__device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluster_group& cluster, Shared& s, uint8_t* area, int row) {
     constexpr int VN = 16 / (int)sizeof(T);
-    T* slice = reinterpret_cast<T*>(smem + (sizeof(Shared) + 15) / 16 * 16);
-    cg::cluster_group cluster = cg::this_cluster();
-    const int C = cluster.num_blocks(), rank = cluster.block_rank(), row = blockIdx.x / C, t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    pdl_launch_dependents();
-    pdl_wait();
+    T* slice = reinterpret_cast<T*>(area);
+    const int C = cluster.num_blocks(), rank = cluster.block_rank(), t = threadIdx.x, lane = t & 31, warp = t >> 5;
 
     // ---- the slice into shared memory, at the same distance from a 16-byte border as in memory; -infinity around it.  Token i is
     // slice[pad + i]; pieces of VN tokens are read whole from here on.
@@ -150,11 +150,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         for (int i = 1; i < VN; ++i) m = fmaxf(m, v[i]);
         return m == m ? m : -CUDART_INF_F;
     };
-    float top = -CUDART_INF_F, least = CUDART_INF_F;             // least: of the pieces' largest
-    auto look = [&](float m) {
-        top = fmaxf(top, m);
-        if (m > -CUDART_INF_F) least = fminf(least, m);
-    };
+    float top = -CUDART_INF_F, least = CUDART_INF_F;
     {
         const int head = min(n, (VN - pad) % VN), vecs = (n - head) / VN, tail = head + vecs * VN;
         const int p0 = (pad + head) / VN;                        // first whole piece
@@ -169,7 +165,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
                     *reinterpret_cast<uint4*>(slice + (size_t)(p0 + i0 + x * kThreads) * VN) = v[x];
                     float f[VN];
                     unpack16<T>(v[x], f);
-                    look(largest(f));
+#pragma unroll
+                    for (int y = 0; y < VN; ++y) { top = fmaxf(top, f[y]); least = fminf(least, f[y]); }     // (not NaN)
                 }
         }
         if (t < 2 * VN) {                                        // the two ragged ends, in order
@@ -179,12 +176,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
                 const int i = at - pad;
                 const bool in = i >= 0 && i < n;
                 slice[at] = in ? src[i] : from_float<T>(-CUDART_INF_F);
-                if (in) { const float v = value_of(src[i]); look(v == v ? v : -CUDART_INF_F); }
+                if (in) { top = fmaxf(top, value_of(src[i])); least = fminf(least, value_of(src[i])); }
             }
         }
     }
     if (t == 0) { s.top = 0; s.least = 0xffffffffu; s.id = 0xffffffffu; s.n_cand = 0; }
-    if (t < 32) s.root[t] = exp2(-(double)t / 32.0);
     for (int i = t; i < kBins; i += kThreads) s.count[i] = 0;
     __syncthreads();
     {
@@ -246,27 +242,30 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const float far = fminf((float)fmin((double)kFar / (2.0 * c2) * 1.000001, (double)kMost), kMost);
     auto near = [&](float v) { return half(v) <= far; };         // (false for NaN and -infinity)
     auto distance = [&](float v) { return (dtop - (double)v) * c2; };            // log2, of a near token
-    // round(2^45 * 2^-x), 0 <= x <= 47.1: x = j / 32 + r, 2^-r from its Taylor series, |r ln 2| <= 0.011: error 2e-15
-    auto weight = [&](double x) {
-        constexpr double kMagic = 6755399441055744.0;            // 1.5 * 2^52
-        const double m = fma(x, 32.0, kMagic);
+    // 2^52 + round(2^45 * 2^-x) as the bits of a double, 0 <= x <= 47.1: x = j / 32 + r, 2^-r by Chebyshev interpolation of degree 5 on
+    // [-1/64, 1/64] (error 2^-49)
+    auto weight_bits = [&](double x) {
+        constexpr double kRound = 6755399441055744.0;            // 1.5 * 2^52
+        const double m = fma(x, 32.0, kRound);
         const int j = __double2loint(m);
-        const double r = fma(m - kMagic, -0.03125, x);
-        double p = fma(r, -1.3333558146428443e-3, 9.6181291076284772e-3);
-        p = fma(r, p, -5.5504108664821580e-2);
-        p = fma(r, p, 2.4022650695910071e-1);
-        p = fma(r, p, -6.9314718055994531e-1);
+        const double r = fma(m - kRound, -0.03125, x);
+        double p = fma(r, -1.3338724772135417e-3, 9.618110954761505e-3);
+        p = fma(r, p, -5.550410848400134e-2);
+        p = fma(r, p, 2.4022650696921724e-1);
+        p = fma(r, p, -6.931471805599585e-1);
         p = fma(r, p, 1.0);
-        const double scale = __hiloint2double((1023 + 45 - (j >> 5)) << 20, 0);
-        return (u64)(__double_as_longlong(fma(p * s.root[j & 31], scale, 4503599627370496.0)) - 0x4330000000000000ll);
+        const double w = s.root[j & 31];                         // times 2^-(j / 32) in whole powers: its exponent less
+        return (u64)__double_as_longlong(fma(p, __hiloint2double(__double2hiint(w) - ((j << 15) & 0xfff00000), __double2loint(w)), 4503599627370496.0));
     };
+    auto weight = [&](double x) { return weight_bits(x) - kMagicBits; };
     u64 thr = 0;                                                 // kept so far: entries from thr on
 
-    // Weight of every group of 32 pieces, of the tokens that are near, not below thr and within min_p if `last`; the row's total for every thread.
-    auto weigh = [&](bool last) {
-        const float thr_v = thr != 0 ? value_of_entry(thr) : -kMost;
-        const double limit = last ? most : CUDART_INF;
-        const int groups = (pieces + 31) / 32;
+    // Weight of every group of 32 pieces, of the tokens that are near or, if `limited`, kept (not below thr and within the limit); the row's total
+    // for every thread.  (Excluded tokens run through the arithmetic as the largest, without a branch; the integers' common offset is taken off once.)
+    auto weigh = [&](auto limited, double limit) {
+        constexpr bool kLimited = decltype(limited)::value;
+        const float thr_v = kLimited && thr != 0 ? value_of_entry(thr) : -CUDART_INF_F;
+        const int thr_id = kLimited && thr != 0 ? id_of_entry(thr) : 0x7fffffff, groups = (pieces + 31) / 32;
         u64 all = 0;
         for (int g = warp; g < groups; g += kWarps) {
             const int p = 32 * g + lane;
@@ -274,14 +273,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             if (p < pieces) {
                 float v[VN];
                 piece(p, v);
+                uint32_t n_in = 0;
 #pragma unroll
                 for (int i = 0; i < VN; ++i) {
-                    const bool in = near(v[i]) && v[i] >= thr_v && (v[i] > thr_v || thr == 0 || entry_of(bits_of(v[i]), id0 + p * VN + i) >= thr);
-                    if (in) {
-                        const double x = distance(v[i]);
-                        if (x <= limit || v[i] == top) w += weight(x);
-                    }
+                    bool in = near(v[i]);
+                    if (kLimited) in = in && (v[i] > thr_v || (v[i] == thr_v && id0 + p * VN + i <= thr_id));
+                    const double x = distance(in ? v[i] : top);
+                    if (kLimited) in = in && (x <= limit || v[i] == top);
+                    const u64 b = weight_bits(x);
+                    w += in ? b : 0;
+                    n_in += in ? 1 : 0;
                 }
+                w -= n_in * kMagicBits;
             }
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
@@ -354,11 +357,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         return x <= most || v == top ? weight(x) : (u64)0;
     };
 
-    // ---- all tokens' weight, where top-k does not limit them
-    const bool filtered = k > 0 || top_p < 1.f || min_p > 0.f;
+    // ---- no filter
     u64 total = 0;
-    if (k == 0 && (top_p < 1.f || !filtered)) total = weigh(false);
-    if (!filtered) {
+    if (k == 0 && top_p == 1.f && !(min_p > 0.f)) {
+        total = weigh(std::false_type(), CUDART_INF);
         const u64 e = locate(kept, target_of(total));
         if (rank == 0 && t == 0) emit(e, total);
         cluster.sync();                                          // (the others have read this block's words)
@@ -366,16 +368,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     }
 
     // ---- candidates: half(v) * scale < bound holds for every token that can be kept
-    const float span = fminf(far, half(least));
+    const float span = fminf(far, half(least));                  // (a masked token makes it `far`)
     const float inv = span > 1e-30f ? (float)kBins / span : 0.f;         // bins of distance
     auto bin_of = [&](float v) { return min(kBins - 1, (int)(half(v) * inv)); };         // falls with v
     float scale = 1.f, bound = far < kMost ? far * 1.000001f + 1e-37f : kMost;
     if (min_p > 0.f) bound = fminf(bound, (float)fmin((most + 1e-9) / (2.0 * c2) * 1.00001, (double)kMost) + 1e-37f);
-    if (k == 0 && top_p < 1.f) {
-        // V 2^-x <= (1 - p) total: what lies beyond x is not needed to reach p total
-        const double x = log2((double)a.vocab * kOne / ((1.0 - (double)top_p) * (double)total)) + 1e-6;
-        bound = fminf(bound, (float)fmin(fmax(x, 0.0) / (2.0 * c2) * 1.00001, (double)kMost) + 1e-37f);
-    }
     uint32_t c[kPerThread];
     auto gather_counts = [&]() {                                 // the cluster's counts of this thread's bins
 #pragma unroll
@@ -386,6 +383,172 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         }
         static_assert(kPerThread == 4, "one 16-byte read of the counts");
     };
+    // The first block: its m entries sorted, and their cumulative weight (before + ..) in the slice's place.
+    u64* cum = reinterpret_cast<u64*>(area);
+    auto sort_entries = [&](int m, u64 before) {
+        int size = 2;
+        while (size < m) size *= 2;
+        for (int i = m + t; i < size; i += kThreads) s.entry[i] = 0;
+        block_sort<true>(s.entry, size);
+        const int per = (m + kThreads - 1) / kThreads, b = min(t * per, m), e = min(b + per, m);
+        u64 mine = 0, all;
+        for (int i = b; i < e; ++i) { mine += weight(distance(value_of_entry(s.entry[i]))); cum[i] = mine; }
+        before += block_exclusive<u64>(mine, s.scan, all);
+        for (int i = b; i < e; ++i) cum[i] += before;
+    };
+    // The candidates of the cluster's lists, `base` of them in lower blocks, into the first block's memory.
+    auto send = [&](uint32_t base) {
+        u64* to = cluster.map_shared_rank(s.entry, 0) + base;
+        for (int i = t; i < (int)s.n_cand; i += kThreads) to[i] = entry_of(bits_of(value_of(slice[s.cand[i]])), id0 + s.cand[i]);
+    };
+
+    // ---- top-p alone (or with min-p): the border's bins, then one pass over the weights
+    if (k == 0 && top_p < 1.f) {
+        for (int p = t; p < pieces; p += kThreads) {
+            float v[VN];
+            piece(p, v);
+#pragma unroll
+            for (int i = 0; i < VN; ++i)
+                if (near(v[i])) atomicAdd(&s.count[bin_of(v[i])], 1u);
+        }
+        if (t < 2) s.bin[t] = kBins - 1;
+        if (t == 0) { s.all = 0; s.total = 0; s.lo = s.hi = kBins - 1; }
+        cluster.sync();
+        gather_counts();
+        {
+            // A bin's weights lie between those of its two ends (1.6 % apart at most), which bounds the cumulative weight; their middle is closer
+            // where many tokens count.
+            const float w = inv > 0.f ? unit / inv : 0.f;
+            float up[kPerThread], down[kPerThread], mid[kPerThread], all_up, all_down, all_mid;
+#pragma unroll
+            for (int i = 0; i < kPerThread; ++i) {
+                const int b = t * kPerThread + i;
+                const float x = exp2f(-(float)b * w), y = exp2f(-(float)(b + 1) * w);
+                up[i] = (float)c[i] * x;
+                down[i] = b == kBins - 1 ? 0.f : (float)c[i] * y;
+                mid[i] = 0.5f * (up[i] + down[i]);
+            }
+            float cu = block_exclusive<float>((up[0] + up[1]) + (up[2] + up[3]), s.scan, all_up);
+            float cd = block_exclusive<float>((down[0] + down[1]) + (down[2] + down[3]), s.scan, all_down);
+            float cm = block_exclusive<float>((mid[0] + mid[1]) + (mid[2] + mid[3]), s.scan, all_mid);
+#pragma unroll
+            for (int i = 0; i < kPerThread; ++i) {
+                cu += up[i]; cd += down[i]; cm += mid[i];
+                const int b = t * kPerThread + i;
+                if (c[i] > 0) {
+                    if (cu * 1.0001f >= top_p * all_down) atomicMin(&s.bin[0], (uint32_t)b);
+                    if (cd >= top_p * all_up * 1.0001f) atomicMin(&s.bin[1], (uint32_t)b);
+                    if (cm >= top_p * all_mid - 1e-3f * all_mid) atomicMin(&s.lo, (uint32_t)b);
+                    if (cm >= top_p * all_mid + 1e-3f * all_mid) atomicMin(&s.hi, (uint32_t)b);
+                }
+            }
+        }
+        __syncthreads();
+        int b0 = s.bin[0], b1 = s.bin[1];
+        uint32_t in = 0, n_in;
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) in += t * kPerThread + i >= b0 && t * kPerThread + i <= b1 ? c[i] : 0;
+        block_exclusive<uint32_t>(in, s.scan, n_in);
+        if (n_in > kGather) { b0 = s.lo; b1 = s.hi; }            // (a border outside of them is noticed below)
+        cluster.sync();                                          // (the histogram has been read, s.cand may be written over it)
+        const float from = (float)b0, to = b1 == kBins - 1 ? CUDART_INF_F : (float)(b1 + 1);
+        u64 sum_all = 0, sum_before = 0;
+        const int groups = (pieces + 31) / 32;
+        for (int g = warp; g < groups; g += kWarps) {
+            const int p = 32 * g + lane;
+            u64 before = 0;
+            if (p < pieces) {
+                float v[VN];
+                piece(p, v);
+                uint32_t mask = 0, n_near = 0, n_before = 0;
+#pragma unroll
+                for (int i = 0; i < VN; ++i) {
+                    const float d = half(v[i]), y = d * inv;
+                    const bool in = d <= far, first = in && y < from;
+                    const u64 b = weight_bits(distance(in ? v[i] : top));
+                    sum_all += in ? b : 0;
+                    n_near += in ? 1 : 0;
+                    before += first ? b : 0;
+                    n_before += first ? 1 : 0;
+                    mask |= in && !first && y < to ? 1u << i : 0u;
+                }
+                sum_all -= n_near * kMagicBits;
+                before -= n_before * kMagicBits;
+                if (mask != 0) {
+                    uint32_t at = atomicAdd(&s.n_cand, (uint32_t)__popc(mask));
+                    for (; mask != 0; mask &= mask - 1, ++at)
+                        if (at < kGather) s.cand[at] = (uint16_t)(p * VN + __ffs(mask) - 1);
+                }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+            if (lane == 0) { s.group[g] = before; sum_before += before; }
+        }
+        for (int o = 16; o > 0; o >>= 1) sum_all += __shfl_xor_sync(0xffffffffu, sum_all, o);
+        if (lane == 0) { atomicAdd(&s.all, sum_all); atomicAdd(&s.total, sum_before); }
+        cluster.sync();
+        u64 before = 0;
+        uint32_t n_all = 0, base = 0;
+        for (int i = 0; i < C; ++i) {
+            total += *cluster.map_shared_rank(&s.all, i);
+            before += *cluster.map_shared_rank(&s.total, i);
+            const uint32_t x = *cluster.map_shared_rank(&s.n_cand, i);
+            base += i < rank ? x : 0;
+            n_all += x;
+        }
+        const double goal = (double)top_p * (double)total;
+        if (n_all <= kGather && (double)before < goal) {
+            send(base);
+            cluster.sync();
+            // (its slice is needed again: weights are formed twice, not kept)
+            if (rank == 0) {
+                if (t == 0) s.thr = 0;
+                const int m = (int)n_all;
+                int size = 2;
+                while (size < m) size *= 2;
+                for (int i = m + t; i < size; i += kThreads) s.entry[i] = 0;
+                block_sort<true>(s.entry, size);
+                const int per = (m + kThreads - 1) / kThreads, b = min(t * per, m), e = min(b + per, m);
+                u64 mine = 0, unused;
+                for (int i = b; i < e; ++i) mine += weight(distance(value_of_entry(s.entry[i])));
+                u64 run = before + block_exclusive<u64>(mine, s.scan, unused);
+                for (int i = b; i < e; ++i) {
+                    const u64 x = weight(distance(value_of_entry(s.entry[i])));
+                    if ((double)run < goal && (double)(run + x) >= goal) s.thr = s.entry[i];
+                    run += x;
+                }
+            }
+            cluster.sync();
+            thr = *cluster.map_shared_rank(&s.thr, 0);
+            if (thr != 0) {
+                if (distance(value_of_entry(thr)) <= most) {
+                    // what is kept of the bins joins its groups' sums
+                    u64 mine = 0, sum;
+                    for (int i = t; i < (int)s.n_cand; i += kThreads) {
+                        const float v = value_of(slice[s.cand[i]]);
+                        if (entry_of(bits_of(v), id0 + s.cand[i]) >= thr) {
+                            const u64 x = weight(distance(v));
+                            atomicAdd(&s.group[s.cand[i] / (32 * VN)], x);
+                            mine += x;
+                        }
+                    }
+                    block_exclusive<u64>(mine, s.scan, sum);
+                    if (t == 0) s.total += sum;
+                    cluster.sync();
+                    total = 0;
+                    for (int i = 0; i < C; ++i) total += *cluster.map_shared_rank(&s.total, i);
+                } else {                                         // min-p cuts deeper
+                    total = weigh(std::true_type(), most);
+                }
+                const u64 e = locate(kept, target_of(total));
+                if (rank == 0 && t == 0) emit(e, total);
+                cluster.sync();
+                return;
+            }
+        }
+        cluster.sync();
+    }
+
     if (k > 0) {
         for (int p = t; p < pieces; p += kThreads) {
             float v[VN];
@@ -406,7 +569,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         cluster.sync();                                          // (the counts have been read, s.cand may be written over them)
         if (inv > 0.f && s.bin[0] < kBins - 1) { scale = inv; bound = (float)(s.bin[0] + 1); }        // (the last bin also holds what lies beyond the span)
     }
-    for (int p = t; p < pieces; p += kThreads) {
+    // (top-p alone comes here only if the cluster has to search for its border)
+    const bool search = k == 0 && top_p < 1.f;
+    for (int p = t; p < pieces && !search; p += kThreads) {
         float v[VN];
         piece(p, v);
         uint32_t mask = 0;
@@ -425,29 +590,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         base += i < rank ? x : 0;
         n_all += x;
     }
-    if (n_all <= kGather) {
-        u64* to = cluster.map_shared_rank(s.entry, 0) + base;
-        for (int i = t; i < (int)s.n_cand; i += kThreads) to[i] = entry_of(bits_of(value_of(slice[s.cand[i]])), id0 + s.cand[i]);
+    if (!search && n_all <= kGather) {
+        send(base);
         cluster.sync();
         if (rank != 0) return;
         // ---- the first block alone
         const int m = (int)n_all;
-        int size = 2;
-        while (size < m) size *= 2;
-        for (int i = m + t; i < size; i += kThreads) s.entry[i] = 0;
-        block_sort<true>(s.entry, size);
-        u64* cum = reinterpret_cast<u64*>(slice);                // cumulative weight of the sorted entries
-        const int per = (m + kThreads - 1) / kThreads;
-        const int b = min(t * per, m), e = min(b + per, m);
-        u64 mine = 0, all;
-        for (int i = b; i < e; ++i) { mine += weight(distance(value_of_entry(s.entry[i]))); cum[i] = mine; }
-        const u64 before = block_exclusive<u64>(mine, s.scan, all);
-        for (int i = b; i < e; ++i) cum[i] += before;
+        sort_entries(m, 0);
+        const int per = (m + kThreads - 1) / kThreads, b = min(t * per, m), e = min(b + per, m);
         if (t == 0) s.cut = k > 0 ? min(m, k) : m;
         __syncthreads();
         int keep = s.cut;
-        if (top_p < 1.f) {
-            const double goal = (double)top_p * (double)(k > 0 ? cum[keep - 1] : total);
+        if (top_p < 1.f) {                                       // (k > 0)
+            const double goal = (double)top_p * (double)cum[keep - 1];
             __syncthreads();
             for (int i = b; i < min(e, keep); ++i)
                 if ((double)cum[i] >= goal) { atomicMin(&s.cut, (uint32_t)i + 1u); break; }
@@ -465,14 +620,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         }
         // in order of id: (id, place) in one word
         uint32_t* order = reinterpret_cast<uint32_t*>(cum + m);
-        size = 2;
+        int size = 2;
         while (size < keep) size *= 2;
         for (int i = t; i < size; i += kThreads) order[i] = i < keep ? ((uint32_t)id_of_entry(s.entry[i]) << 12 | (uint32_t)i) : 0xffffffffu;
         block_sort<false>(order, size);
         const u64 kept_total = cum[keep - 1], target = target_of(kept_total);
         const int per2 = (keep + kThreads - 1) / kThreads, b2 = min(t * per2, keep), e2 = min(b2 + per2, keep);
         auto w_of = [&](int i) { const uint32_t x = order[i] & 4095u; return cum[x] - (x > 0 ? cum[x - 1] : 0); };
-        u64 sum = 0;
+        u64 sum = 0, all;
         for (int i = b2; i < e2; ++i) sum += w_of(i);
         u64 run = block_exclusive<u64>(sum, s.scan, all);
         if (run <= target && target < run + sum)
@@ -671,14 +826,32 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     cluster.sync();                                              // (everyone has read the numbers of candidates; the counts start anew)
     if (k > 0) {
         select(false, (double)k);
-        if (top_p < 1.f) total = weigh(false);
+        if (top_p < 1.f) total = weigh(std::true_type(), CUDART_INF);
     }
     if (top_p < 1.f) select(true, (double)top_p * (double)total);
-    total = weigh(true);
+    total = weigh(std::true_type(), most);
     const u64 e = locate(kept, target_of(total));
     if (rank == 0 && t == 0) emit(e, total);
     cluster.sync();
 }
+
+// The clusters that fit the GPU at once walk over the rows: starting one takes some 0.3 us of the whole GPU.
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    Shared& s = *reinterpret_cast<Shared*>(smem);
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int C = cluster.num_blocks();
+    if (threadIdx.x < 32) s.root[threadIdx.x] = exp2(45.0 - (double)threadIdx.x / 32.0);
+    pdl_launch_dependents();
+    pdl_wait();
+    for (int row = blockIdx.x / C; row < a.rows; row += gridDim.x / C) {
+        __syncthreads();                                         // (the row before is done with the block's memory)
+        sample_row<T>(a, cluster, s, smem + (sizeof(Shared) + 15) / 16 * 16, row);
+    }
+}
+
+constexpr size_t kHalfSm = 112 * 1024;   // dynamic shared memory of a block that shares its SM with another
 
 // Blocks of a row: slices of up to 64 KB, so that two blocks share an SM; more blocks while the GPU has room for them.
 int blocks_of_row(int rows, int vocab, int elt) {
@@ -687,22 +860,40 @@ int blocks_of_row(int rows, int vocab, int elt) {
     return c;
 }
 
+// Clusters of c = 1, 2, 4, 8 blocks that the current device holds at once, with blocks of kHalfSm bytes or (large) more.
 template <typename T>
-beagle_status launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
-    const int c = blocks_of_row(rows, a.vocab, (int)sizeof(T));
+int resident_clusters(const cudaLaunchConfig_t& cfg, int c, bool large) {
+    static std::atomic<int> known[PerDeviceOnce::kMaxDevices][2][4];
+    int dev = 0, n = 0, slot = c == 1 ? 0 : c == 2 ? 1 : c == 4 ? 2 : 3;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= PerDeviceOnce::kMaxDevices) return 1;
+    std::atomic<int>& k = known[dev][large ? 1 : 0][slot];
+    n = k.load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaOccupancyMaxActiveClusters(&n, sample_kernel<T>, &cfg) != cudaSuccess || n <= 0) { cudaGetLastError(); n = device_sm_count() / c; }
+        k.store(n > 0 ? n : 1, std::memory_order_relaxed);
+    }
+    return n > 0 ? n : 1;
+}
+
+template <typename T>
+beagle_status launch_sample(SampleArgs a, cudaStream_t stream) {
+    const int c = blocks_of_row(a.rows, a.vocab, (int)sizeof(T));
     a.slice = ((a.vocab + c - 1) / c + 7) / 8 * 8;
     // the slice; the first block's sums and order of its candidates take its place
     size_t area = (size_t)(a.slice + 32) * sizeof(T);
     const size_t finish = (size_t)(a.vocab < kGather ? a.vocab : kGather) * 8 + (size_t)kGather * 4;
     if (area < finish) area = finish;
-    const size_t bytes = (sizeof(Shared) + 15) / 16 * 16 + area;
+    size_t bytes = (sizeof(Shared) + 15) / 16 * 16 + area;
+    const bool large = bytes > kHalfSm;
     static PerDeviceOnce attr;
-    if (!attr.ensure([] { return cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) == cudaSuccess; }))
+    constexpr size_t kLarge = 200 * 1024;
+    static_assert((sizeof(Shared) + 15) / 16 * 16 + (kMaxVocab / kMaxCluster + 40) * sizeof(T) <= kLarge, "the largest slice");
+    if (!attr.ensure([] { return cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLarge) == cudaSuccess; }))
         return BEAGLE_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)rows * c);
+    cfg.gridDim = dim3((unsigned)c);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = bytes;
+    cfg.dynamicSmemBytes = large ? kLarge : kHalfSm;     // (what the number below is known for)
     cfg.stream = stream;
     cudaLaunchAttribute attrs[2];
     attrs[0].id = cudaLaunchAttributeClusterDimension;
@@ -711,6 +902,10 @@ beagle_status launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
     attrs[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attrs[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attrs;
+    cfg.numAttrs = 1;
+    const int fit = resident_clusters<T>(cfg, c, large);
+    cfg.gridDim = dim3((unsigned)((a.rows < fit ? a.rows : fit) * c));
+    cfg.dynamicSmemBytes = bytes;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a) == cudaSuccess && cudaGetLastError() == cudaSuccess ? BEAGLE_OK : BEAGLE_ERR_CUDA;
 }
@@ -727,13 +922,13 @@ extern "C" beagle_status beagle_sample(const void* logits_dev, int32_t logits_dt
     if (logits_dtype != BEAGLE_FP32 && logits_dtype != BEAGLE_BF16) return BEAGLE_ERR_INVALID_ARG;
     if (rows < 0 || vocab <= 0 || row_stride < vocab) return BEAGLE_ERR_INVALID_ARG;
     if (vocab > kMaxVocab) return BEAGLE_ERR_SHAPE;
-    if (rows > 0x7fffffff / kMaxCluster) return BEAGLE_ERR_CAPACITY;
+    if (rows > 0x7fffffff / kMaxCluster) return BEAGLE_ERR_CAPACITY;     // (rows and blocks are counted in 32 bits)
     if (rows == 0) return BEAGLE_OK;
     if (logits_dev == nullptr || u_dev == nullptr || tokens_out_dev == nullptr) return BEAGLE_ERR_INVALID_ARG;
     if (((uintptr_t)logits_dev & (logits_dtype == BEAGLE_BF16 ? 1 : 3)) ||
         (((uintptr_t)temperature_dev | (uintptr_t)top_k_dev | (uintptr_t)top_p_dev | (uintptr_t)min_p_dev | (uintptr_t)u_dev | (uintptr_t)tokens_out_dev |
           (uintptr_t)logp_out_dev) & 3))
         return BEAGLE_ERR_INVALID_ARG;
-    SampleArgs a{logits_dev, row_stride, vocab, 0, temperature_dev, top_p_dev, min_p_dev, u_dev, top_k_dev, tokens_out_dev, logp_out_dev};
-    return logits_dtype == BEAGLE_BF16 ? launch_sample<bf16>(a, rows, static_cast<cudaStream_t>(stream)) : launch_sample<float>(a, rows, static_cast<cudaStream_t>(stream));
+    SampleArgs a{logits_dev, row_stride, rows, vocab, 0, temperature_dev, top_p_dev, min_p_dev, u_dev, top_k_dev, tokens_out_dev, logp_out_dev};
+    return logits_dtype == BEAGLE_BF16 ? launch_sample<bf16>(a, static_cast<cudaStream_t>(stream)) : launch_sample<float>(a, static_cast<cudaStream_t>(stream));
 }
