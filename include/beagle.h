@@ -493,13 +493,13 @@ beagle_status beagle_verify_sample(beagle_ctx* ctx, int32_t batch, int32_t gamma
 /* One token per row of logits, drawn with the caller's random numbers: what drafts for beagle_verify_sample are drawn with (with
  * temperature alone), and what a sampled target emits.  logits_dev [rows, vocab] (logits_dtype BEAGLE_FP32 | BEAGLE_BF16), rows
  * row_stride elements apart; vocab up to 2^18.  Every parameter is an array of one value per row, or NULL:
- *   temperature_dev fp32 (NULL: 1; a value not above 0, or NaN: the row's largest logit, no draw), top_k_dev int32 (NULL or <= 0: all),
+ *   temperature_dev fp32 (NULL: 1; a value not above 0, or NaN: the row's largest logit, no draw; above 1e30: 1e30), top_k_dev int32 (NULL or <= 0: all),
  *   top_p_dev fp32 (NULL, >= 1 or NaN: all), min_p_dev fp32 (NULL, <= 0 or NaN: all), u_dev fp32 in [0, 1), required.
  * With d(v) = (logit(v) - largest) / temperature and the tokens in order of falling logit, the lower id first among equals, a row keeps
  * the first top_k; of those the shortest leading run whose weight (sum of exp d) is at least top_p times the weight of them all;
  * of those the ones with exp(d) >= min_p; the first always.  tokens_out_dev int32 [rows]: the smallest id whose cumulative kept weight, in
  * order of id, exceeds u times the kept weight; logp_out_dev fp32 [rows] (nullable): ln of its share of the kept weight (0 without a
- * draw).  Weights are 2^-45 of the largest exact and sums are integers: results depend on neither timing nor the rest of the batch.  A NaN logit
+ * draw).  Weights are exact to 2^-45 of the largest and sums are integers: results depend on neither timing nor the rest of the batch.  A NaN logit
  * counts as -infinity, a subnormal one as 0; +infinity takes all the weight (shared among several); a row of -infinity alone gives token -1 and logp NaN. */
 beagle_status beagle_sample(const void* logits_dev, int32_t logits_dtype, int32_t rows, int32_t vocab, int64_t row_stride,
                             const float* temperature_dev, const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev,

@@ -38,20 +38,26 @@ typedef unsigned long long u64;
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBins = 2048, kPerThread = kBins / kThreads;
-constexpr int kGather = 4096;            // candidates that the first block finishes alone
-constexpr int kList = kThreads;          // tokens that the first block compares pairwise
+constexpr int kMassBins = 1024;          // of the first block's selections
+constexpr int kGather = 3500;            // candidates that the first block finishes alone
+constexpr int kList = kThreads;          // tokens that a block compares pairwise (the cluster's search)
+constexpr int kFew = 64;                 // the same of the first block's own selections
 constexpr int kMaxCluster = 8;
 constexpr int kMaxVocab = 1 << 18;
 constexpr int kMaxGroups = kMaxVocab / kMaxCluster / 128 + 8;      // of 32 16-byte pieces (128 fp32 logits, 256 bf16) in a block's slice
 constexpr double kOne = 35184372088832.0;        // 2^45
-constexpr u64 kMagicBits = 0x4330000000000000ull;        // of 2^52: a double from there on holds an integer in its low bits
-constexpr float kFar = 47.f;             // log2 distance from which on the weight is 0 (2^45 * 2^-47 rounds to 0)
+constexpr double kFar = 47.0;            // log2 distance from which on the weight is 0 (2^45 * 2^-47 rounds to 0)
 constexpr float kMost = 3.402823466e38f;
+
+// 2^-r on [-1/64, 1/64] by Chebyshev interpolation of degree 5 (error 2^-49), and the numbers around it; in constant memory, where an instruction
+// takes them as they are (immediate doubles cost two moves each time).
+__constant__ double c_exp[9] = {-1.3338724772135417e-3, 9.618110954761505e-3, -5.550410848400134e-2, 2.4022650696921724e-1, -6.931471805599585e-1, 1.0,
+                               6755399441055744.0 /* 1.5 * 2^52 */, 4503599627370496.0 /* 2^52 */, -0.03125};
 
 struct SampleArgs {
     const void* logits;
     long long stride;
-    int rows, vocab, slice;                    // slice: tokens of a block (a multiple of 8)
+    int rows, vocab, slice;              // slice: tokens of a block (a multiple of 8)
     const float *temperature, *top_p, *min_p, *u;
     const int32_t* top_k;
     int32_t* tokens;
@@ -65,13 +71,16 @@ struct Shared {
     };
     union {
         uint32_t count[kBins];
-        uint16_t cand[kGather];          // this block's candidates: positions in its slice
+        u64 mass[kMassBins];
+        struct { u64 key[kFew], w[kFew]; } few;
     };
+    uint16_t cand[kGather];              // this block's candidates: positions in its slice
     u64 group[kMaxGroups];               // weight of every group of 32 pieces
-    u64 scan[kWarps];
+    u64 scan[2 * kWarps];
     double root[32];                     // 2^(45 - j / 32)
     u64 sum[2], all, total, thr, found;
-    uint32_t top, least, id, lo, hi, n_cand, n_list, bin[2], cut;
+    uint32_t n_gather[2];                // candidates of the cluster (first block), of this row and of the one before
+    uint32_t top, least, id, lo, hi, n_cand, n_list, n_in, bin[2], mid[2];
 };
 
 __device__ __forceinline__ float value_of(float v) { return v; }
@@ -111,25 +120,162 @@ __device__ __forceinline__ N block_exclusive(N v, u64* scratch, N& total) {
     return before + incl - v;
 }
 
-// Sorts x[0 .. n), n a power of two, falling or rising.  Whole block, a barrier at both ends.
-template <bool FALLING, typename N>
-__device__ __forceinline__ void block_sort(N* x, int n) {
-    __syncthreads();
-    for (int k = 2; k <= n; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int p = threadIdx.x; p < n / 2; p += kThreads) {
-                const int i = 2 * p - (p & (j - 1)), o = i + j;
-                const N a = x[i], b = x[o];
-                const bool swap = (a < b) == (((i & k) == 0) == FALLING);
-                if (swap) { x[i] = b; x[o] = a; }
-            }
-            __syncthreads();
+// The same for three fp32 values, side by side.  s: 3 * kWarps words.
+__device__ __forceinline__ void block_exclusive3(float* v, float* total, float* s) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float incl[3];
+#pragma unroll
+    for (int y = 0; y < 3; ++y) incl[y] = v[y];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+        for (int y = 0; y < 3; ++y) {
+            const float x = __shfl_up_sync(0xffffffffu, incl[y], o);
+            if (lane >= o) incl[y] += x;
         }
+    __syncthreads();
+#pragma unroll
+    for (int y = 0; y < 3; ++y)
+        if (lane == 31) s[y * kWarps + warp] = incl[y];
+    __syncthreads();
+#pragma unroll
+    for (int y = 0; y < 3; ++y) {
+        float before = 0.f;
+        total[y] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) {
+            before += i < warp ? s[y * kWarps + i] : 0.f;
+            total[y] += s[y * kWarps + i];
+        }
+        v[y] = before + incl[y] - v[y];
+    }
 }
 
-// One row.  A block that returns is done with the others' shared memory, and they with its own, but for the first block's when it finishes alone.
+// The block's sum for every thread.
+__device__ __forceinline__ u64 block_sum(u64 v, u64* scratch) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    u64 all = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) all += scratch[i];
+    return all;
+}
+
+// Of n items, each with a key of its own and a measure (0: not there), in order of falling key: the key at which the shortest leading run with at
+// least `goal` ends, 0 if all of them have less.  Whole block.  Ranges of more than kFew items are divided by kMassBins a level.
+template <typename Key, typename Measure>
+__device__ __forceinline__ u64 block_select(Shared& s, int n, Key key, Measure measure, u64 goal) {
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    u64 lo = ~0ull, hi = 0, before = 0;
+    if (n > kFew) {
+        for (int i = t; i < n; i += kThreads)
+            if (measure(i) != 0) { const u64 k = key(i); lo = k < lo ? k : lo; hi = k > hi ? k : hi; }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const u64 a = __shfl_xor_sync(0xffffffffu, lo, o), b = __shfl_xor_sync(0xffffffffu, hi, o);
+            lo = a < lo ? a : lo;
+            hi = b > hi ? b : hi;
+        }
+        __syncthreads();
+        if (lane == 0) { s.scan[warp] = lo; s.scan[kWarps + warp] = hi; }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) { lo = s.scan[i] < lo ? s.scan[i] : lo; hi = s.scan[kWarps + i] > hi ? s.scan[kWarps + i] : hi; }
+    } else {
+        lo = 0;
+        hi = ~0ull;
+    }
+    for (;;) {
+        __syncthreads();
+        if (t == 0) { s.n_list = 0; s.found = 0; s.bin[0] = 0xffffffffu; }
+        __syncthreads();
+        // (those that fit are listed at once)
+        for (int i = t; i < n; i += kThreads) {
+            const u64 k = key(i);
+            if (k < lo || k > hi) continue;
+            const u64 w = measure(i);
+            if (w == 0) continue;
+            const uint32_t at = atomicAdd(&s.n_list, 1u);
+            if (at < kFew) { s.few.key[at] = k; s.few.w[at] = w; }
+        }
+        __syncthreads();
+        const int m = (int)s.n_list;
+        if (m <= kFew) {
+            if (t < m) {
+                const u64 k = s.few.key[t];
+                u64 cum = before;
+#pragma unroll 4
+                for (int i = 0; i < m; ++i) cum += s.few.key[i] > k ? s.few.w[i] : 0;
+                if (cum < goal && cum + s.few.w[t] >= goal) s.found = k;
+            }
+            __syncthreads();
+            return s.found;
+        }
+        const int shift = max(0, 54 - __clzll((long long)(hi - lo)));            // (hi - lo) >> shift < 1024
+        for (int i = t; i < kMassBins; i += kThreads) s.mass[i] = 0;
+        __syncthreads();
+        for (int i = t; i < n; i += kThreads) {
+            const u64 k = key(i);
+            if (k < lo || k > hi) continue;
+            const u64 w = measure(i);
+            if (w != 0) atomicAdd(&s.mass[(hi - k) >> shift], w);
+        }
+        __syncthreads();
+        const u64 a = s.mass[2 * t], b = s.mass[2 * t + 1];
+        u64 unused;
+        const u64 at = before + block_exclusive<u64>(a + b, s.scan, unused);
+        if (at < goal && at + a + b >= goal) {
+            const bool second = at + a < goal;
+            s.bin[0] = 2 * t + (second ? 1 : 0);
+            s.sum[0] = second ? at + a : at;
+        }
+        __syncthreads();
+        const uint32_t bin = s.bin[0];
+        if (bin == 0xffffffffu) return 0;
+        before = s.sum[0];
+        const u64 top = hi - ((u64)bin << shift), width = (1ull << shift) - 1;
+        lo = top - lo > width ? top - width : lo;
+        hi = top;
+    }
+}
+
+// What the passes over all tokens do with a 16-byte piece without looking at each: its largest and least (not NaN), and which tokens are not below a bound.
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+    static __device__ __forceinline__ float largest(const uint4& x) { return fmaxf(fmaxf(__uint_as_float(x.x), __uint_as_float(x.y)), fmaxf(__uint_as_float(x.z), __uint_as_float(x.w))); }
+    static __device__ __forceinline__ float least(const uint4& x) { return fminf(fminf(__uint_as_float(x.x), __uint_as_float(x.y)), fminf(__uint_as_float(x.z), __uint_as_float(x.w))); }
+    float bound;
+    __device__ __forceinline__ explicit Piece(float b) : bound(b) {}
+    __device__ __forceinline__ uint32_t mask(const uint4& x) const {
+        return (__uint_as_float(x.x) >= bound ? 1u : 0u) | (__uint_as_float(x.y) >= bound ? 2u : 0u) | (__uint_as_float(x.z) >= bound ? 4u : 0u) | (__uint_as_float(x.w) >= bound ? 8u : 0u);
+    }
+};
+template <> struct Piece<bf16> {
+    static __device__ __forceinline__ __nv_bfloat162 two(uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); }
+    static __device__ __forceinline__ float largest(const uint4& x) {
+        const __nv_bfloat162 m = __hmax2(__hmax2(two(x.x), two(x.y)), __hmax2(two(x.z), two(x.w)));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    static __device__ __forceinline__ float least(const uint4& x) {
+        const __nv_bfloat162 m = __hmin2(__hmin2(two(x.x), two(x.y)), __hmin2(two(x.z), two(x.w)));
+        return fminf(__low2float(m), __high2float(m));
+    }
+    __nv_bfloat162 bound;
+    __device__ __forceinline__ explicit Piece(float b) : bound(__bfloat162bfloat162(__float2bfloat16_rd(b))) {}       // (not above the bound)
+    __device__ __forceinline__ uint32_t mask(const uint4& x) const {
+        const uint32_t a = __hge2_mask(two(x.x), bound), b = __hge2_mask(two(x.y), bound), c = __hge2_mask(two(x.z), bound), d = __hge2_mask(two(x.w), bound);
+        if ((a | b | c | d) == 0) return 0;
+        return (a & 1u) | (a >> 30 & 2u) | (b & 1u) << 2 | (b >> 30 & 2u) << 2 | (c & 1u) << 4 | (c >> 30 & 2u) << 4 | (d & 1u) << 6 | (d >> 30 & 2u) << 6;
+    }
+};
+
+// One row.  What the blocks read of one another's shared memory stays until the cluster has met in the next row (or at the kernel's end): words that
+// are set before that meeting have had a meeting after their last reading.
 template <typename T>
-__device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluster_group& cluster, Shared& s, uint8_t* area, int row) {
+__device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluster_group& cluster, Shared& s, uint8_t* area, int row, int next, int parity) {
     constexpr int VN = 16 / (int)sizeof(T);
     T* slice = reinterpret_cast<T*>(area);
     const int C = cluster.num_blocks(), rank = cluster.block_rank(), t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -139,17 +285,13 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
     const int first = min(rank * a.slice, a.vocab), n = min(a.slice, a.vocab - first);
     const T* src = static_cast<const T*>(a.logits) + (size_t)row * a.stride + first;
     const int pad = (int)(((uintptr_t)src & 15) / sizeof(T)), pieces = (pad + n + VN - 1) / VN, id0 = first - pad;
-    // the piece's tokens in fp32, and their largest (NaN never is)
-    auto piece = [&](int p, float* v) {
-        const uint4 x = *reinterpret_cast<const uint4*>(slice + p * VN);
-        unpack16<T>(x, v);
-    };
-    auto largest = [&](const float* v) {
-        float m = v[0];
-#pragma unroll
-        for (int i = 1; i < VN; ++i) m = fmaxf(m, v[i]);
-        return m == m ? m : -CUDART_INF_F;
-    };
+    auto raw_piece = [&](int p) { return *reinterpret_cast<const uint4*>(slice + p * VN); };
+    auto piece = [&](int p, float* v) { unpack16<T>(raw_piece(p), v); };         // in fp32
+    // the row's parameters are on their way meanwhile
+    const uint32_t temp_bits = a.temperature != nullptr ? __float_as_uint(__ldcg(a.temperature + row)) : __float_as_uint(1.f);
+    int k = a.top_k != nullptr ? __ldcg(a.top_k + row) : 0;
+    float top_p = a.top_p != nullptr ? __ldcg(a.top_p + row) : 1.f;
+    const float min_p = a.min_p != nullptr ? __ldcg(a.min_p + row) : 0.f, uf = __ldcg(a.u + row);
     float top = -CUDART_INF_F, least = CUDART_INF_F;
     {
         const int head = min(n, (VN - pad) % VN), vecs = (n - head) / VN, tail = head + vecs * VN;
@@ -163,10 +305,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
             for (int x = 0; x < 4; ++x)
                 if (i0 + x * kThreads < vecs) {
                     *reinterpret_cast<uint4*>(slice + (size_t)(p0 + i0 + x * kThreads) * VN) = v[x];
-                    float f[VN];
-                    unpack16<T>(v[x], f);
-#pragma unroll
-                    for (int y = 0; y < VN; ++y) { top = fmaxf(top, f[y]); least = fminf(least, f[y]); }     // (not NaN)
+                    top = fmaxf(top, Piece<T>::largest(v[x]));
+                    least = fminf(least, Piece<T>::least(v[x]));
                 }
         }
         if (t < 2 * VN) {                                        // the two ragged ends, in order
@@ -179,6 +319,10 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                 if (in) { top = fmaxf(top, value_of(src[i])); least = fminf(least, value_of(src[i])); }
             }
         }
+        // the cluster's next row comes from L2
+        if (next < a.rows && t * 128 < n * (int)sizeof(T))
+            for (int i = t * 128; i < n * (int)sizeof(T); i += kThreads * 128)
+                prefetch_l2(reinterpret_cast<const char*>(static_cast<const T*>(a.logits) + (size_t)next * a.stride + first) + i);
     }
     if (t == 0) { s.top = 0; s.least = 0xffffffffu; s.id = 0xffffffffu; s.n_cand = 0; }
     for (int i = t; i < kBins; i += kThreads) s.count[i] = 0;
@@ -196,14 +340,10 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         }
         top = of_bits(hi);
         least = of_bits(lo);
+        if (t == 0) s.n_gather[parity ^ 1] = 0;                  // everyone has read the last row's
     }
 
-    // ---- the row's parameters
-    const uint32_t temp_bits = a.temperature != nullptr ? __float_as_uint(__ldcg(a.temperature + row)) : __float_as_uint(1.f);
-    const bool drawn = temp_bits - 1u < 0x7f800000u;             // above 0, infinity included
-    int k = a.top_k != nullptr ? __ldcg(a.top_k + row) : 0;
-    float top_p = a.top_p != nullptr ? __ldcg(a.top_p + row) : 1.f;
-    const float min_p = a.min_p != nullptr ? __ldcg(a.min_p + row) : 0.f;
+    const bool drawn = temp_bits - 1u < 0x7f800000u;             // temperature above 0, infinity included
     if (top_p <= 0.f || min_p > 1.f) k = 1;                      // only the first
     if (!drawn || k == 1 || top == -CUDART_INF_F) {              // its lowest id
         const bool none = top == -CUDART_INF_F;
@@ -233,35 +373,32 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         top = least = 0.f;
         __syncthreads();
     }
-    const double c2 = fmin(1.4426950408889634074 / (double)__uint_as_float(temp_bits), 1e300), dtop = (double)top;
+    // (temperatures above 1e30 do what 1e30 does to logits that are not of that size themselves)
+    const double temp = fmin((double)__uint_as_float(temp_bits), 1e30), c2 = fmin(1.4426950408889634074 / temp, 1e300), dtop = (double)top;
     const double most = min_p > 0.f ? -log2((double)min_p) : CUDART_INF;         // distance that min_p allows
-    // Half the distance of a logit from the largest in fp32, which does not overflow; `far`: those with a weight
-    const float half_top = 0.5f * top;
-    auto half = [&](float v) { return fmaf(v, -0.5f, half_top); };
-    const float unit = (float)(2.0 * c2);                        // log2 distance of a half of 1
-    const float far = fminf((float)fmin((double)kFar / (2.0 * c2) * 1.000001, (double)kMost), kMost);
-    auto near = [&](float v) { return half(v) <= far; };         // (false for NaN and -infinity)
+    // A value not above any logit that is at most x away (log2); at least the least finite fp32
+    auto value_at = [&](double x) { return fmaxf(__double2float_rd(fmax(dtop - x / c2, -(double)kMost)), -kMost); };
+    const float far = fmaxf(__double2float_ru(fmax(dtop - kFar / c2, -(double)kMost)), -kMost);          // logits from here on have a weight, if any
+    auto near = [&](float v) { return v >= far; };               // (false for NaN and -infinity)
     auto distance = [&](float v) { return (dtop - (double)v) * c2; };            // log2, of a near token
-    // 2^52 + round(2^45 * 2^-x) as the bits of a double, 0 <= x <= 47.1: x = j / 32 + r, 2^-r by Chebyshev interpolation of degree 5 on
-    // [-1/64, 1/64] (error 2^-49)
-    auto weight_bits = [&](double x) {
-        constexpr double kRound = 6755399441055744.0;            // 1.5 * 2^52
-        const double m = fma(x, 32.0, kRound);
+    // round(2^45 * 2^-x), 0 <= x <= 47.1, as a double: x = j / 32 + r
+    auto weight_d = [&](double x) {
+        const double m = fma(x, 32.0, c_exp[6]);
         const int j = __double2loint(m);
-        const double r = fma(m - kRound, -0.03125, x);
-        double p = fma(r, -1.3338724772135417e-3, 9.618110954761505e-3);
-        p = fma(r, p, -5.550410848400134e-2);
-        p = fma(r, p, 2.4022650696921724e-1);
-        p = fma(r, p, -6.931471805599585e-1);
-        p = fma(r, p, 1.0);
+        const double r = fma(m - c_exp[6], c_exp[8], x);
+        double p = fma(r, c_exp[0], c_exp[1]);
+        p = fma(r, p, c_exp[2]);
+        p = fma(r, p, c_exp[3]);
+        p = fma(r, p, c_exp[4]);
+        p = fma(r, p, c_exp[5]);
         const double w = s.root[j & 31];                         // times 2^-(j / 32) in whole powers: its exponent less
-        return (u64)__double_as_longlong(fma(p, __hiloint2double(__double2hiint(w) - ((j << 15) & 0xfff00000), __double2loint(w)), 4503599627370496.0));
+        return fma(p, __hiloint2double(__double2hiint(w) - ((j << 15) & 0xfff00000), __double2loint(w)), c_exp[7]) - c_exp[7];
     };
-    auto weight = [&](double x) { return weight_bits(x) - kMagicBits; };
+    auto weight = [&](double x) { return (u64)weight_d(x); };
     u64 thr = 0;                                                 // kept so far: entries from thr on
 
     // Weight of every group of 32 pieces, of the tokens that are near or, if `limited`, kept (not below thr and within the limit); the row's total
-    // for every thread.  (Excluded tokens run through the arithmetic as the largest, without a branch; the integers' common offset is taken off once.)
+    // for every thread.  (Excluded tokens run through the arithmetic as the largest, without a branch.  A lane's sum stays below 2^53: exact.)
     auto weigh = [&](auto limited, double limit) {
         constexpr bool kLimited = decltype(limited)::value;
         const float thr_v = kLimited && thr != 0 ? value_of_entry(thr) : -CUDART_INF_F;
@@ -269,23 +406,21 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         u64 all = 0;
         for (int g = warp; g < groups; g += kWarps) {
             const int p = 32 * g + lane;
-            u64 w = 0;
+            double sum = 0.0;
             if (p < pieces) {
                 float v[VN];
                 piece(p, v);
-                uint32_t n_in = 0;
 #pragma unroll
                 for (int i = 0; i < VN; ++i) {
                     bool in = near(v[i]);
                     if (kLimited) in = in && (v[i] > thr_v || (v[i] == thr_v && id0 + p * VN + i <= thr_id));
                     const double x = distance(in ? v[i] : top);
                     if (kLimited) in = in && (x <= limit || v[i] == top);
-                    const u64 b = weight_bits(x);
-                    w += in ? b : 0;
-                    n_in += in ? 1 : 0;
+                    const double y = weight_d(x);
+                    if (in) sum += y;
                 }
-                w -= n_in * kMagicBits;
             }
+            u64 w = (u64)sum;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
             if (lane == 0) s.group[g] = w;
@@ -301,78 +436,75 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         return total;
     };
     // Smallest id whose cumulative measure exceeds the target (below the total).  s.group holds the groups' sums and s.total the block's;
-    // measure(value, id) as they were formed.  The entry for every thread of the cluster.
-    auto locate = [&](auto measure, u64 target) {
+    // measure(value, id) as they were formed.  The thread that has the token calls hit(its entry).
+    auto locate = [&](auto measure, u64 target, auto hit) {
         u64 before = 0, sum;
         for (int i = 0; i < rank; ++i) before += *cluster.map_shared_rank(&s.total, i);
+        if (target < before || target >= before + s.total) return;               // (the same for the whole block)
         const int groups = (pieces + 31) / 32;
         const u64 mine = t < groups ? s.group[t] : 0;
         before += block_exclusive<u64>(mine, s.scan, sum);
         const uint32_t owner = __ballot_sync(0xffffffffu, before <= target && target < before + mine);
-        if (owner != 0) {                                        // one warp of the cluster: a lane takes a piece
-            const int l = __ffs(owner) - 1, p = 32 * (warp * 32 + l) + lane;
-            const u64 start = __shfl_sync(0xffffffffu, before, l);
-            float v[VN];
-            u64 w[VN], all = 0;
+        if (owner == 0) return;
+        const int l = __ffs(owner) - 1, p = 32 * (warp * 32 + l) + lane;         // one warp: a lane takes a piece
+        const u64 start = __shfl_sync(0xffffffffu, before, l);
+        float v[VN];
+        u64 w[VN], all = 0;
 #pragma unroll
-            for (int i = 0; i < VN; ++i) v[i] = -CUDART_INF_F;
-            if (p < pieces) piece(p, v);
+        for (int i = 0; i < VN; ++i) v[i] = -CUDART_INF_F;
+        if (p < pieces) piece(p, v);
 #pragma unroll
-            for (int i = 0; i < VN; ++i) all += w[i] = measure(v[i], id0 + p * VN + i);
-            u64 incl = all;
+        for (int i = 0; i < VN; ++i) all += w[i] = measure(v[i], id0 + p * VN + i);
+        u64 incl = all;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const u64 x = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += x;
-            }
-            u64 cum = start + incl - all;
-            if (cum <= target && target < cum + all) {
-                bool found = false;
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        u64 cum = start + incl - all;
+        if (cum <= target && target < cum + all) {
+            bool found = false;
 #pragma unroll
-                for (int i = 0; i < VN; ++i) {
-                    cum += w[i];
-                    if (!found && cum > target) {
-                        found = true;
-                        *cluster.map_shared_rank(&s.found, 0) = entry_of(bits_of(v[i]), id0 + p * VN + i);
-                    }
-                }
+            for (int i = 0; i < VN; ++i) {
+                cum += w[i];
+                if (!found && cum > target) { found = true; hit(entry_of(bits_of(v[i]), id0 + p * VN + i)); }
             }
         }
-        cluster.sync();
-        return *cluster.map_shared_rank(&s.found, 0);
     };
     auto emit = [&](u64 e, u64 total) {
         a.tokens[row] = id_of_entry(e);
         if (a.logp != nullptr) a.logp[row] = (float)(-(distance(value_of_entry(e)) * 0.69314718055994530942 + log((double)total / kOne)));
     };
-    const float uf = __ldcg(a.u + row);
     const double u = uf > 0.f ? (double)uf : 0.0;
     auto target_of = [&](u64 total) {
         const u64 x = (u64)(u * (double)total);
         return x < total ? x : total - 1;
+    };
+    auto share_of = [&](u64 total) {                             // the weight that top-p asks for
+        const u64 x = (u64)ceil((double)top_p * (double)total);
+        return x > 1 ? x : 1;
     };
     auto kept = [&](float v, int id) {                           // the last step's measure
         if (!near(v) || entry_of(bits_of(v), id) < thr) return (u64)0;
         const double x = distance(v);
         return x <= most || v == top ? weight(x) : (u64)0;
     };
+    // (s.total is not written again before the next row's first meeting of the cluster)
+    auto draw = [&](u64 total) { locate(kept, target_of(total), [&](u64 e) { emit(e, total); }); };
 
     // ---- no filter
     u64 total = 0;
     if (k == 0 && top_p == 1.f && !(min_p > 0.f)) {
-        total = weigh(std::false_type(), CUDART_INF);
-        const u64 e = locate(kept, target_of(total));
-        if (rank == 0 && t == 0) emit(e, total);
-        cluster.sync();                                          // (the others have read this block's words)
+        draw(weigh(std::false_type(), CUDART_INF));
         return;
     }
 
-    // ---- candidates: half(v) * scale < bound holds for every token that can be kept
-    const float span = fminf(far, half(least));                  // (a masked token makes it `far`)
-    const float inv = span > 1e-30f ? (float)kBins / span : 0.f;         // bins of distance
-    auto bin_of = [&](float v) { return min(kBins - 1, (int)(half(v) * inv)); };         // falls with v
-    float scale = 1.f, bound = far < kMost ? far * 1.000001f + 1e-37f : kMost;
-    if (min_p > 0.f) bound = fminf(bound, (float)fmin((most + 1e-9) / (2.0 * c2) * 1.00001, (double)kMost) + 1e-37f);
+    // bins of distance, by a product that rises with it
+    const float bottom = fmaxf(far, least), span = top - bottom;                 // (a masked token makes it `far`)
+    const float inv = span > 1e-30f && span < 1e36f ? (float)kBins / span : 0.f;
+    auto place = [&](float v) { return (top - v) * inv; };
+    auto bin_of = [&](float v) { return min(kBins - 1, (int)place(v)); };
+    const float unit = (float)c2;                                // log2 distance of 1
     uint32_t c[kPerThread];
     auto gather_counts = [&]() {                                 // the cluster's counts of this thread's bins
 #pragma unroll
@@ -383,24 +515,26 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         }
         static_assert(kPerThread == 4, "one 16-byte read of the counts");
     };
-    // The first block: its m entries sorted, and their cumulative weight (before + ..) in the slice's place.
-    u64* cum = reinterpret_cast<u64*>(area);
-    auto sort_entries = [&](int m, u64 before) {
-        int size = 2;
-        while (size < m) size *= 2;
-        for (int i = m + t; i < size; i += kThreads) s.entry[i] = 0;
-        block_sort<true>(s.entry, size);
-        const int per = (m + kThreads - 1) / kThreads, b = min(t * per, m), e = min(b + per, m);
-        u64 mine = 0, all;
-        for (int i = b; i < e; ++i) { mine += weight(distance(value_of_entry(s.entry[i]))); cum[i] = mine; }
-        before += block_exclusive<u64>(mine, s.scan, all);
-        for (int i = b; i < e; ++i) cum[i] += before;
+    auto list = [&](int p, uint32_t mask) {                      // tokens of a piece among the block's candidates
+        uint32_t at = atomicAdd(&s.n_cand, (uint32_t)__popc(mask));
+        for (; mask != 0; mask &= mask - 1, ++at)
+            if (at < kGather) s.cand[at] = (uint16_t)(p * VN + __ffs(mask) - 1);
     };
-    // The candidates of the cluster's lists, `base` of them in lower blocks, into the first block's memory.
-    auto send = [&](uint32_t base) {
-        u64* to = cluster.map_shared_rank(s.entry, 0) + base;
-        for (int i = t; i < (int)s.n_cand; i += kThreads) to[i] = entry_of(bits_of(value_of(slice[s.cand[i]])), id0 + s.cand[i]);
+    // The blocks' candidates into the first one's memory, if they fit; their number.  (Their order there has no influence.)
+    auto send = [&]() {
+        __syncthreads();
+        const uint32_t mine = s.n_cand;
+        if (t == 0) s.n_in = atomicAdd(cluster.map_shared_rank(&s.n_gather[parity], 0), mine);
+        __syncthreads();
+        const uint32_t base = s.n_in;
+        if (base + mine <= kGather) {
+            u64* to = cluster.map_shared_rank(s.entry, 0) + base;
+            for (int i = t; i < (int)mine; i += kThreads) to[i] = entry_of(bits_of(value_of(slice[s.cand[i]])), id0 + s.cand[i]);
+        }
+        cluster.sync();
+        return (int)*cluster.map_shared_rank(&s.n_gather[parity], 0);
     };
+    auto key_at = [&](int i) { return s.entry[i]; };
 
     // ---- top-p alone (or with min-p): the border's bins, then one pass over the weights
     if (k == 0 && top_p < 1.f) {
@@ -411,119 +545,97 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
             for (int i = 0; i < VN; ++i)
                 if (near(v[i])) atomicAdd(&s.count[bin_of(v[i])], 1u);
         }
-        if (t < 2) s.bin[t] = kBins - 1;
-        if (t == 0) { s.all = 0; s.total = 0; s.lo = s.hi = kBins - 1; }
+        if (t < 2) s.bin[t] = s.mid[t] = kBins - 1;
+        if (t == 0) { s.all = 0; s.total = 0; s.n_in = 0; }
         cluster.sync();
         gather_counts();
         {
             // A bin's weights lie between those of its two ends (1.6 % apart at most), which bounds the cumulative weight; their middle is closer
             // where many tokens count.
             const float w = inv > 0.f ? unit / inv : 0.f;
-            float up[kPerThread], down[kPerThread], mid[kPerThread], all_up, all_down, all_mid;
+            float x[3][kPerThread], cum[3] = {0.f, 0.f, 0.f}, all[3];
 #pragma unroll
             for (int i = 0; i < kPerThread; ++i) {
                 const int b = t * kPerThread + i;
-                const float x = exp2f(-(float)b * w), y = exp2f(-(float)(b + 1) * w);
-                up[i] = (float)c[i] * x;
-                down[i] = b == kBins - 1 ? 0.f : (float)c[i] * y;
-                mid[i] = 0.5f * (up[i] + down[i]);
+                x[0][i] = (float)c[i] * exp2f(-(float)b * w);
+                x[1][i] = b == kBins - 1 ? 0.f : (float)c[i] * exp2f(-(float)(b + 1) * w);
+                x[2][i] = 0.5f * (x[0][i] + x[1][i]);
+#pragma unroll
+                for (int y = 0; y < 3; ++y) cum[y] += x[y][i];
             }
-            float cu = block_exclusive<float>((up[0] + up[1]) + (up[2] + up[3]), s.scan, all_up);
-            float cd = block_exclusive<float>((down[0] + down[1]) + (down[2] + down[3]), s.scan, all_down);
-            float cm = block_exclusive<float>((mid[0] + mid[1]) + (mid[2] + mid[3]), s.scan, all_mid);
+            block_exclusive3(cum, all, reinterpret_cast<float*>(s.scan));
 #pragma unroll
             for (int i = 0; i < kPerThread; ++i) {
-                cu += up[i]; cd += down[i]; cm += mid[i];
-                const int b = t * kPerThread + i;
+#pragma unroll
+                for (int y = 0; y < 3; ++y) cum[y] += x[y][i];
+                const uint32_t b = (uint32_t)(t * kPerThread + i);
                 if (c[i] > 0) {
-                    if (cu * 1.0001f >= top_p * all_down) atomicMin(&s.bin[0], (uint32_t)b);
-                    if (cd >= top_p * all_up * 1.0001f) atomicMin(&s.bin[1], (uint32_t)b);
-                    if (cm >= top_p * all_mid - 1e-3f * all_mid) atomicMin(&s.lo, (uint32_t)b);
-                    if (cm >= top_p * all_mid + 1e-3f * all_mid) atomicMin(&s.hi, (uint32_t)b);
+                    if (cum[0] * 1.0001f >= top_p * all[1]) atomicMin(&s.bin[0], b);
+                    if (cum[1] >= top_p * all[0] * 1.0001f) atomicMin(&s.bin[1], b);
+                    if (cum[2] >= (top_p - 1e-3f) * all[2]) atomicMin(&s.mid[0], b);
+                    if (cum[2] >= (top_p + 1e-3f) * all[2]) atomicMin(&s.mid[1], b);
                 }
             }
         }
         __syncthreads();
         int b0 = s.bin[0], b1 = s.bin[1];
-        uint32_t in = 0, n_in;
+        {
+            uint32_t in = 0;
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i) in += t * kPerThread + i >= b0 && t * kPerThread + i <= b1 ? c[i] : 0;
-        block_exclusive<uint32_t>(in, s.scan, n_in);
-        if (n_in > kGather) { b0 = s.lo; b1 = s.hi; }            // (a border outside of them is noticed below)
-        cluster.sync();                                          // (the histogram has been read, s.cand may be written over it)
-        const float from = (float)b0, to = b1 == kBins - 1 ? CUDART_INF_F : (float)(b1 + 1);
-        u64 sum_all = 0, sum_before = 0;
+            for (int i = 0; i < kPerThread; ++i) in += t * kPerThread + i >= b0 && t * kPerThread + i <= b1 ? c[i] : 0;
+            in = __reduce_add_sync(0xffffffffu, in);
+            if (lane == 0 && in != 0) atomicAdd(&s.n_in, in);
+        }
+        __syncthreads();
+        if (s.n_in > kGather) { b0 = s.mid[0]; b1 = s.mid[1]; }  // (a border outside of them is noticed below)
+        const float from = b0 > 0 ? (float)b0 : -CUDART_INF_F, to = b1 == kBins - 1 ? CUDART_INF_F : (float)(b1 + 1);
+        double all_d = 0.0;                                      // (of some hundred tokens: exact)
+        u64 sum_before = 0;
         const int groups = (pieces + 31) / 32;
         for (int g = warp; g < groups; g += kWarps) {
             const int p = 32 * g + lane;
-            u64 before = 0;
+            double first_d = 0.0;
             if (p < pieces) {
                 float v[VN];
                 piece(p, v);
-                uint32_t mask = 0, n_near = 0, n_before = 0;
+                uint32_t mask = 0;
 #pragma unroll
                 for (int i = 0; i < VN; ++i) {
-                    const float d = half(v[i]), y = d * inv;
-                    const bool in = d <= far, first = in && y < from;
-                    const u64 b = weight_bits(distance(in ? v[i] : top));
-                    sum_all += in ? b : 0;
-                    n_near += in ? 1 : 0;
-                    before += first ? b : 0;
-                    n_before += first ? 1 : 0;
+                    const float y = place(v[i]);
+                    const bool in = near(v[i]), first = in && y < from;
+                    const double w = weight_d(distance(in ? v[i] : top));
+                    if (in) all_d += w;
+                    if (first) first_d += w;
                     mask |= in && !first && y < to ? 1u << i : 0u;
                 }
-                sum_all -= n_near * kMagicBits;
-                before -= n_before * kMagicBits;
-                if (mask != 0) {
-                    uint32_t at = atomicAdd(&s.n_cand, (uint32_t)__popc(mask));
-                    for (; mask != 0; mask &= mask - 1, ++at)
-                        if (at < kGather) s.cand[at] = (uint16_t)(p * VN + __ffs(mask) - 1);
-                }
+                if (mask != 0) list(p, mask);
             }
+            u64 before = (u64)first_d;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
             if (lane == 0) { s.group[g] = before; sum_before += before; }
         }
+        u64 sum_all = (u64)all_d;
         for (int o = 16; o > 0; o >>= 1) sum_all += __shfl_xor_sync(0xffffffffu, sum_all, o);
         if (lane == 0) { atomicAdd(&s.all, sum_all); atomicAdd(&s.total, sum_before); }
-        cluster.sync();
+        const int m = send();
         u64 before = 0;
-        uint32_t n_all = 0, base = 0;
         for (int i = 0; i < C; ++i) {
             total += *cluster.map_shared_rank(&s.all, i);
             before += *cluster.map_shared_rank(&s.total, i);
-            const uint32_t x = *cluster.map_shared_rank(&s.n_cand, i);
-            base += i < rank ? x : 0;
-            n_all += x;
         }
-        const double goal = (double)top_p * (double)total;
-        if (n_all <= kGather && (double)before < goal) {
-            send(base);
-            cluster.sync();
-            // (its slice is needed again: weights are formed twice, not kept)
+        const u64 goal = share_of(total);
+        if (m <= kGather && before < goal) {
             if (rank == 0) {
-                if (t == 0) s.thr = 0;
-                const int m = (int)n_all;
-                int size = 2;
-                while (size < m) size *= 2;
-                for (int i = m + t; i < size; i += kThreads) s.entry[i] = 0;
-                block_sort<true>(s.entry, size);
-                const int per = (m + kThreads - 1) / kThreads, b = min(t * per, m), e = min(b + per, m);
-                u64 mine = 0, unused;
-                for (int i = b; i < e; ++i) mine += weight(distance(value_of_entry(s.entry[i])));
-                u64 run = before + block_exclusive<u64>(mine, s.scan, unused);
-                for (int i = b; i < e; ++i) {
-                    const u64 x = weight(distance(value_of_entry(s.entry[i])));
-                    if ((double)run < goal && (double)(run + x) >= goal) s.thr = s.entry[i];
-                    run += x;
-                }
+                const u64 e = block_select(s, m, key_at, [&](int i) { return weight(distance(value_of_entry(s.entry[i]))); }, goal - before);
+                if (t == 0) s.thr = e;
             }
             cluster.sync();
             thr = *cluster.map_shared_rank(&s.thr, 0);
             if (thr != 0) {
                 if (distance(value_of_entry(thr)) <= most) {
                     // what is kept of the bins joins its groups' sums
-                    u64 mine = 0, sum;
+                    u64 mine = 0;
                     for (int i = t; i < (int)s.n_cand; i += kThreads) {
                         const float v = value_of(slice[s.cand[i]]);
                         if (entry_of(bits_of(v), id0 + s.cand[i]) >= thr) {
@@ -532,115 +644,76 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                             mine += x;
                         }
                     }
-                    block_exclusive<u64>(mine, s.scan, sum);
-                    if (t == 0) s.total += sum;
+                    mine = block_sum(mine, s.scan);
+                    if (t == 0) s.total += mine;
                     cluster.sync();
                     total = 0;
                     for (int i = 0; i < C; ++i) total += *cluster.map_shared_rank(&s.total, i);
                 } else {                                         // min-p cuts deeper
                     total = weigh(std::true_type(), most);
                 }
-                const u64 e = locate(kept, target_of(total));
-                if (rank == 0 && t == 0) emit(e, total);
-                cluster.sync();
+                draw(total);
                 return;
             }
         }
         cluster.sync();
     }
 
+    // ---- top-k, min-p: candidates, tokens that may be kept
+    float bound = far;
+    if (min_p > 0.f && top_p == 1.f) bound = fmaxf(bound, value_at(most + 1e-6));        // (top-p counts the weight of what min-p drops)
     if (k > 0) {
         for (int p = t; p < pieces; p += kThreads) {
-            float v[VN];
-            piece(p, v);
-            const float m = largest(v);
+            const float m = Piece<T>::largest(raw_piece(p));
             if (near(m)) atomicAdd(&s.count[bin_of(m)], 1u);
         }
         if (t == 0) s.bin[0] = kBins;
         cluster.sync();
         gather_counts();
-        uint32_t mine = c[0] + c[1] + c[2] + c[3], all;
-        uint32_t cum = block_exclusive<uint32_t>(mine, s.scan, all);
+        uint32_t all, cum = block_exclusive<uint32_t>(c[0] + c[1] + c[2] + c[3], s.scan, all);
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
             if (cum < (uint32_t)k && cum + c[i] >= (uint32_t)k) s.bin[0] = t * kPerThread + i;
             cum += c[i];
         }
-        cluster.sync();                                          // (the counts have been read, s.cand may be written over them)
-        if (inv > 0.f && s.bin[0] < kBins - 1) { scale = inv; bound = (float)(s.bin[0] + 1); }        // (the last bin also holds what lies beyond the span)
-    }
-    // (top-p alone comes here only if the cluster has to search for its border)
-    const bool search = k == 0 && top_p < 1.f;
-    for (int p = t; p < pieces && !search; p += kThreads) {
-        float v[VN];
-        piece(p, v);
-        uint32_t mask = 0;
-#pragma unroll
-        for (int i = 0; i < VN; ++i) mask |= half(v[i]) * scale < bound ? 1u << i : 0u;
-        if (mask != 0) {
-            uint32_t at = atomicAdd(&s.n_cand, (uint32_t)__popc(mask));
-            for (; mask != 0; mask &= mask - 1, ++at)
-                if (at < kGather) s.cand[at] = (uint16_t)(p * VN + __ffs(mask) - 1);
-        }
-    }
-    cluster.sync();
-    uint32_t n_all = 0, base = 0;
-    for (int i = 0; i < C; ++i) {
-        const uint32_t x = *cluster.map_shared_rank(&s.n_cand, i);
-        base += i < rank ? x : 0;
-        n_all += x;
-    }
-    if (!search && n_all <= kGather) {
-        send(base);
-        cluster.sync();
-        if (rank != 0) return;
-        // ---- the first block alone
-        const int m = (int)n_all;
-        sort_entries(m, 0);
-        const int per = (m + kThreads - 1) / kThreads, b = min(t * per, m), e = min(b + per, m);
-        if (t == 0) s.cut = k > 0 ? min(m, k) : m;
         __syncthreads();
-        int keep = s.cut;
-        if (top_p < 1.f) {                                       // (k > 0)
-            const double goal = (double)top_p * (double)cum[keep - 1];
-            __syncthreads();
-            for (int i = b; i < min(e, keep); ++i)
-                if ((double)cum[i] >= goal) { atomicMin(&s.cut, (uint32_t)i + 1u); break; }
-            __syncthreads();
-            keep = s.cut;
+        // the logits of the bins up to that one: not below this (rounded down; one bin more for the product's rounding)
+        if (inv > 0.f && s.bin[0] < kBins - 2) bound = fmaxf(bound, top - (float)(s.bin[0] + 2) / inv * 1.000001f);
+    }
+    if (!(k == 0 && top_p < 1.f)) {                              // (top-p alone comes here only if the cluster has to search for its border)
+        const Piece<T> test(bound);
+        for (int p = t; p < pieces; p += kThreads) {
+            const uint32_t mask = test.mask(raw_piece(p));
+            if (mask != 0) list(p, mask);
         }
-        if (min_p > 0.f) {
-            __syncthreads();
-            for (int i = b; i < min(e, keep); ++i) {
-                const float v = value_of_entry(s.entry[i]);
-                if (distance(v) > most && v != top) { atomicMin(&s.cut, (uint32_t)max(i, 1)); break; }
+        const int m = send();
+        if (m <= kGather) {
+            if (rank != 0) return;
+            // ---- the first block alone
+            auto w_at = [&](int i) { const float v = value_of_entry(s.entry[i]); return near(v) ? weight(distance(v)) : (u64)0; };
+            if (k > 0 && m > k) thr = block_select(s, m, key_at, [&](int) { return (u64)1; }, (u64)k);
+            if (top_p < 1.f) {                                   // (k > 0)
+                u64 mine = 0;
+                for (int i = t; i < m; i += kThreads) mine += s.entry[i] >= thr ? w_at(i) : 0;
+                const u64 goal = share_of(block_sum(mine, s.scan)), was = thr;
+                thr = block_select(s, m, key_at, [&](int i) { return s.entry[i] >= was ? w_at(i) : (u64)0; }, goal);
             }
-            __syncthreads();
-            keep = s.cut;
+            auto kept_at = [&](int i) { return kept(value_of_entry(s.entry[i]), id_of_entry(s.entry[i])); };
+            u64 mine = 0;
+            for (int i = t; i < m; i += kThreads) mine += kept_at(i);
+            const u64 all = block_sum(mine, s.scan);
+            // in order of id: the inverted id as the key
+            const u64 id = block_select(s, m, [&](int i) { return s.entry[i] & 0xffffffffull; }, kept_at, target_of(all) + 1);
+            for (int i = t; i < m; i += kThreads)
+                if ((s.entry[i] & 0xffffffffull) == id) emit(s.entry[i], all);
+            return;
         }
-        // in order of id: (id, place) in one word
-        uint32_t* order = reinterpret_cast<uint32_t*>(cum + m);
-        int size = 2;
-        while (size < keep) size *= 2;
-        for (int i = t; i < size; i += kThreads) order[i] = i < keep ? ((uint32_t)id_of_entry(s.entry[i]) << 12 | (uint32_t)i) : 0xffffffffu;
-        block_sort<false>(order, size);
-        const u64 kept_total = cum[keep - 1], target = target_of(kept_total);
-        const int per2 = (keep + kThreads - 1) / kThreads, b2 = min(t * per2, keep), e2 = min(b2 + per2, keep);
-        auto w_of = [&](int i) { const uint32_t x = order[i] & 4095u; return cum[x] - (x > 0 ? cum[x - 1] : 0); };
-        u64 sum = 0, all;
-        for (int i = b2; i < e2; ++i) sum += w_of(i);
-        u64 run = block_exclusive<u64>(sum, s.scan, all);
-        if (run <= target && target < run + sum)
-            for (int i = b2; i < e2; ++i) {
-                run += w_of(i);
-                if (run > target) { emit(s.entry[order[i] & 4095u], kept_total); break; }
-            }
-        return;
+        cluster.sync();
     }
 
     // ---- more candidates: the whole cluster.  Moves thr to the end of the shortest leading run whose measure is at least the goal:
     // weight (by_mass) or tokens.
-    auto select = [&](bool by_mass, double goal) {
+    auto select = [&](bool by_mass, u64 goal) {
         for (int i = t; i < kBins; i += kThreads) s.count[i] = 0;
         if (t < 2) s.bin[t] = kBins - 1;
         if (t == 0) { s.hi = 0; s.lo = 0xffffffffu; s.n_list = 0; s.sum[0] = 0; }
@@ -653,7 +726,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                 piece(p, v);
 #pragma unroll
                 for (int i = 0; i < VN; ++i)
-                    if (half(v[i]) * scale < bound && near(v[i]) && v[i] >= thr_v) {
+                    if (v[i] >= bound && near(v[i]) && v[i] >= thr_v) {
                         const int id = id0 + p * VN + i;
                         if (thr == 0 || entry_of(bits_of(v[i]), id) >= thr) f(v[i], id, bin_of(v[i]));
                     }
@@ -665,10 +738,10 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         const uint32_t mine = c[0] + c[1] + c[2] + c[3];
         uint32_t all;
         const uint32_t count_before = block_exclusive<uint32_t>(mine, s.scan, all);
-        if (!by_mass && (double)all <= goal) { cluster.sync(); return; }         // everything that has weight is kept
+        if (!by_mass && all <= goal) { cluster.sync(); return; }         // everything that has weight is kept
         if (by_mass) {
             // a bin's weights lie between those of its two ends: bounds of the cumulative weight, with a margin for their rounding
-            const float w = inv > 0.f ? unit / inv : 0.f, want = (float)(goal / kOne);
+            const float w = inv > 0.f ? unit / inv : 0.f, want = (float)((double)goal / kOne);
             float up[kPerThread], down[kPerThread], up_mine = 0.f, down_mine = 0.f, unused;
 #pragma unroll
             for (int i = 0; i < kPerThread; ++i) {
@@ -688,7 +761,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
             uint32_t cum = count_before;
 #pragma unroll
             for (int i = 0; i < kPerThread; ++i) {
-                if ((double)cum < goal && (double)(cum + c[i]) >= goal) s.bin[0] = s.bin[1] = t * kPerThread + i;
+                if (cum < goal && cum + c[i] >= goal) s.bin[0] = s.bin[1] = t * kPerThread + i;
                 cum += c[i];
             }
         }
@@ -751,7 +824,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
             u64 cum = before + block_exclusive<u64>(m_mine, s.scan, m_all);
 #pragma unroll
             for (int i = 0; i < kPerThread; ++i) {
-                if ((double)cum < goal && (double)(cum + m[i]) >= goal) {
+                if (cum < goal && cum + m[i] >= goal) {
                     s.bin[0] = t * kPerThread + i;
                     s.sum[0] = cum;
                     s.sum[1] = c[i];
@@ -760,7 +833,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
             }
             __syncthreads();
             const uint32_t b = s.bin[0];
-            if (b == 0xffffffffu) break;                         // (rounding of the goal at the very end of the range: all of it is kept)
+            if (b == 0xffffffffu) break;                         // (the border lies behind: all of it is kept)
             before = s.sum[0];
             n_in = (uint32_t)s.sum[1];
             const uint32_t top_key = hi - (b << shift);
@@ -787,7 +860,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                     const u64 e = s.wide.list[t];
                     u64 cum = before;
                     for (int i = 0; i < m; ++i) cum += s.wide.list[i] > e ? s.wide.list_w[i] : 0;
-                    if ((double)cum < goal && (double)(cum + s.wide.list_w[t]) >= goal) s.thr = e;
+                    if (cum < goal && cum + s.wide.list_w[t] >= goal) s.thr = e;
                 }
             }
             cluster.sync();
@@ -795,8 +868,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         } else if (lo == hi) {
             // equal logits: the first so many of them in order of id
             const u64 w = measure(of_bits(lo)), keep_thr = thr;
-            const double miss = goal - (double)before;
-            const u64 want = miss > (double)w ? (u64)ceil(miss / (double)w) : 1;
+            const u64 want = goal > before + w ? (goal - before + w - 1) / w : 1;
             auto tie = [&](float v, int id) { return (u64)(bits_of(v) == lo && entry_of(lo, id) >= keep_thr); };
             const int groups = (pieces + 31) / 32;
             u64 mine_all = 0, sum;
@@ -818,21 +890,19 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
             cluster.sync();
             u64 ties = 0;
             for (int i = 0; i < C; ++i) ties += *cluster.map_shared_rank(&s.total, i);
-            thr = locate(tie, min(want, ties) - 1);
+            locate(tie, min(want, ties) - 1, [&](u64 e) { *cluster.map_shared_rank(&s.thr, 0) = e; });
+            cluster.sync();
+            thr = *cluster.map_shared_rank(&s.thr, 0);
         }
         cluster.sync();
     };
 
-    cluster.sync();                                              // (everyone has read the numbers of candidates; the counts start anew)
     if (k > 0) {
-        select(false, (double)k);
+        select(false, (u64)k);
         if (top_p < 1.f) total = weigh(std::true_type(), CUDART_INF);
     }
-    if (top_p < 1.f) select(true, (double)top_p * (double)total);
-    total = weigh(std::true_type(), most);
-    const u64 e = locate(kept, target_of(total));
-    if (rank == 0 && t == 0) emit(e, total);
-    cluster.sync();
+    if (top_p < 1.f) select(true, share_of(total));
+    draw(weigh(std::true_type(), most));
 }
 
 // The clusters that fit the GPU at once walk over the rows: starting one takes some 0.3 us of the whole GPU.
@@ -843,15 +913,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const cg::cluster_group cluster = cg::this_cluster();
     const int C = cluster.num_blocks();
     if (threadIdx.x < 32) s.root[threadIdx.x] = exp2(45.0 - (double)threadIdx.x / 32.0);
+    if (threadIdx.x < 2) s.n_gather[threadIdx.x] = 0;
     pdl_launch_dependents();
     pdl_wait();
-    for (int row = blockIdx.x / C; row < a.rows; row += gridDim.x / C) {
+    int parity = 0;
+    for (int row = blockIdx.x / C; row < a.rows; row += gridDim.x / C, parity ^= 1) {
         __syncthreads();                                         // (the row before is done with the block's memory)
-        sample_row<T>(a, cluster, s, smem + (sizeof(Shared) + 15) / 16 * 16, row);
+        sample_row<T>(a, cluster, s, smem + (sizeof(Shared) + 15) / 16 * 16, row, row + gridDim.x / C, parity);
     }
+    cluster.sync();                                              // nobody reads a block's memory after it has ended
 }
 
-constexpr size_t kHalfSm = 112 * 1024;   // dynamic shared memory of a block that shares its SM with another
+constexpr size_t kHalfSm = 113 * 1024 - 128;     // dynamic shared memory of a block that shares its SM with another
 
 // Blocks of a row: slices of up to 64 KB, so that two blocks share an SM; more blocks while the GPU has room for them.
 int blocks_of_row(int rows, int vocab, int elt) {
@@ -879,11 +952,7 @@ template <typename T>
 beagle_status launch_sample(SampleArgs a, cudaStream_t stream) {
     const int c = blocks_of_row(a.rows, a.vocab, (int)sizeof(T));
     a.slice = ((a.vocab + c - 1) / c + 7) / 8 * 8;
-    // the slice; the first block's sums and order of its candidates take its place
-    size_t area = (size_t)(a.slice + 32) * sizeof(T);
-    const size_t finish = (size_t)(a.vocab < kGather ? a.vocab : kGather) * 8 + (size_t)kGather * 4;
-    if (area < finish) area = finish;
-    size_t bytes = (sizeof(Shared) + 15) / 16 * 16 + area;
+    const size_t bytes = (sizeof(Shared) + 15) / 16 * 16 + (size_t)(a.slice + 32) * sizeof(T);
     const bool large = bytes > kHalfSm;
     static PerDeviceOnce attr;
     constexpr size_t kLarge = 200 * 1024;
