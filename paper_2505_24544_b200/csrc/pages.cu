@@ -301,8 +301,8 @@ __global__ void __launch_bounds__(kMoveThreads) pages_append_write_kernel(const 
 }
 
 // The same with the keys, and the queries that come along, rotated at the positions that the rows take (rotary.cuh).  blockIdx.x < chunks:
-// g.rows tokens of the row; a thread keeps the cosines and sines of its unit and walks over the token's heads, its key and value of
-// a head in flight together.
+// g.rows tokens of the row; a thread keeps the cosines and sines of its unit and walks over the token's heads, a head's key and value
+// together (the first of them on their way while the cosines and sines are formed).
 struct RotaryRowsArgs {
     const void *k_new, *v_new, *q;
     void *K, *V, *q_out;
@@ -311,10 +311,8 @@ struct RotaryRowsArgs {
     int heads, Hq, dh, T, q_offset, chunks;
     RotaryGrid g;
 };
-constexpr int kRotFlight = 4;                            // heads a thread has in flight
-
 template <typename T, int E, bool INTER>
-__global__ void __launch_bounds__(kRotThreads) pages_append_rotary_kernel(const Book b, const __grid_constant__ PageSlots slots,
+__global__ void __launch_bounds__(kRotThreads, 4) pages_append_rotary_kernel(const Book b, const __grid_constant__ PageSlots slots,
                                                                          const __grid_constant__ RotaryArgs rot, const __grid_constant__ RotaryRowsArgs a) {
     static_assert(kRotThreads == kMoveThreads, "copy_tail walks with kMoveThreads");
     __shared__ __align__(16) float2 s_cs[kRotEntries];
@@ -334,36 +332,30 @@ __global__ void __launch_bounds__(kRotThreads) pages_append_rotary_kernel(const 
     const int u = t % a.g.units, slot = t / a.g.units, rl = slot / a.g.lanes, lane = slot - rl * a.g.lanes, tok = tok0 + rl;
     const long long srow = (long long)row * a.T + tok;
     const bool mine = rl < n_here;
-    typedef RotUnit<T, E, INTER> Unit;
-    typedef typename Unit::V V;
-    // keys (queries where q_offset is 0 too)
+    RotUnit<T, E, INTER> unit;
+    typename RotUnit<T, E, INTER>::V x, y, z, w;
+    unit.place(u, rot.pairs);
+    const T *k = static_cast<const T*>(a.k_new) + srow * a.k_stride, *v = static_cast<const T*>(a.v_new) + srow * a.v_stride;
+    const bool writes = mine && tok < r.n;
+    auto load = [&](int h) {
+        unit.load(k + h * a.dh, x, y);
+        unit.load(v + h * a.dh, z, w);
+    };
+    if (writes && lane < a.heads) load(lane);
+    // (the queries' too where q_offset is 0)
     for (int i = t; i < n_here * rot.pairs; i += kRotThreads) s_cs[i] = rot_angle(rot.turns[i % rot.pairs], r.len + tok0 + i / rot.pairs, rot.m, rot.sign);
     __syncthreads();
-    Unit unit;
-    unit.init(u, rot.pairs, s_cs + min(rl, n_here - 1) * rot.pairs);
-    if (mine && tok < r.n) {
+    unit.entries(s_cs + min(rl, n_here - 1) * rot.pairs);
+    if (writes) {
         const int shift = __ffs(b.page_size) - 1, pos = r.len + tok;
         const int page = __ldcg(b.row(slots.slot[row]) + (pos >> shift));
-        const T *k = static_cast<const T*>(a.k_new) + srow * a.k_stride, *v = static_cast<const T*>(a.v_new) + srow * a.v_stride;
-        const size_t at = ((((size_t)max(page, 0) * a.heads) << shift) + (pos & (b.page_size - 1))) * a.dh;
-        const size_t step = ((size_t)1 << shift) * a.dh;
+        const size_t step = ((size_t)1 << shift) * a.dh, at = (size_t)max(page, 0) * a.heads * step + (size_t)(pos & (b.page_size - 1)) * a.dh;
         if (b.page_ok(page))
-            for (int h0 = lane; h0 < a.heads; h0 += a.g.lanes * kRotFlight) {
-                V x[kRotFlight], y[kRotFlight], z[kRotFlight], w[kRotFlight];
-#pragma unroll
-                for (int i = 0; i < kRotFlight; ++i) {
-                    const int h = h0 + i * a.g.lanes;
-                    if (h < a.heads) { unit.load(k + h * a.dh, x[i], y[i]); unit.load(v + h * a.dh, z[i], w[i]); }
-                }
-#pragma unroll
-                for (int i = 0; i < kRotFlight; ++i) {
-                    const int h = h0 + i * a.g.lanes;
-                    if (h < a.heads) {
-                        unit.turn(x[i], y[i]);
-                        unit.store(static_cast<T*>(a.K) + at + h * step, x[i], y[i]);
-                        unit.store(static_cast<T*>(a.V) + at + h * step, z[i], w[i]);
-                    }
-                }
+            for (int h = lane; h < a.heads; h += a.g.lanes) {
+                if (h != lane) load(h);
+                unit.turn(x, y);
+                unit.store(static_cast<T*>(a.K) + at + h * step, x, y);
+                unit.store(static_cast<T*>(a.V) + at + h * step, z, w);
             }
     }
     if (n_q == 0) return;                                // (the whole CTA)
@@ -372,22 +364,15 @@ __global__ void __launch_bounds__(kRotThreads) pages_append_rotary_kernel(const 
         for (int i = t; i < n_here * rot.pairs; i += kRotThreads)
             s_cs[i] = rot_angle(rot.turns[i % rot.pairs], r.len + a.q_offset + tok0 + i / rot.pairs, rot.m, rot.sign);
         __syncthreads();
-        unit.init(u, rot.pairs, s_cs + min(rl, n_here - 1) * rot.pairs);
+        unit.entries(s_cs + min(rl, n_here - 1) * rot.pairs);
     }
     if (!mine || tok >= n_q) return;
     const T* q = static_cast<const T*>(a.q) + srow * a.q_stride;
     T* qo = static_cast<T*>(a.q_out) + srow * a.Hq * a.dh;
-    for (int h0 = lane; h0 < a.Hq; h0 += a.g.lanes * kRotFlight) {
-        V x[kRotFlight], y[kRotFlight];
-#pragma unroll
-        for (int i = 0; i < kRotFlight; ++i)
-            if (h0 + i * a.g.lanes < a.Hq) unit.load(q + (h0 + i * a.g.lanes) * a.dh, x[i], y[i]);
-#pragma unroll
-        for (int i = 0; i < kRotFlight; ++i)
-            if (h0 + i * a.g.lanes < a.Hq) {
-                unit.turn(x[i], y[i]);
-                unit.store(qo + (h0 + i * a.g.lanes) * a.dh, x[i], y[i]);
-            }
+    for (int h = lane; h < a.Hq; h += a.g.lanes) {
+        unit.load(q + h * a.dh, x, y);
+        unit.turn(x, y);
+        unit.store(qo + h * a.dh, x, y);
     }
 }
 

@@ -1,9 +1,13 @@
 // Rotation of the queries and keys of whole rows by their positions, and its transpose (beagle_rotary_apply).
 //
-// Bound by memory: every element is read and written once, 3 flop each.  A CTA takes a few rows: its threads first form the
-// (cosine, sine) entries of those rows in shared memory, one double-precision product and one fp32 sine and cosine per entry, then
-// each thread keeps the entries of its unit (16 bytes of a head and, in the half layout, their partners) in registers and walks
-// over the heads, four loads in flight.  Queries and keys go in one launch, so that the entries are formed once for both.
+// Bound by memory: every element is read and written once, 3 flop each.  A CTA takes a few rows: its threads form the (cosine, sine)
+// entries of those rows in shared memory, one double-precision product and one fp32 sine and cosine per entry, while their first
+// loads are on their way; then each thread keeps the entries of its unit (16 bytes of a head and, in the half layout, their partners)
+// in registers and walks over the heads.  Queries and keys go in one launch, so that the entries are formed once for both.
+//
+// Measured: 8 x 2048 positions, 32 + 32 heads of 128, bf16, forward and backward (1.07 GB): 177 us, 6.1 TB/s; 8191 positions, 32 + 8 heads,
+// interleaved, a quarter rotated (168 MB): 43 us.  One head at a time in a thread and six CTAs per SM; four heads in flight in two
+// CTAs per SM took 240 and 53, entries formed by every thread for itself, without shared memory, 179 and 47.
 #include <cmath>
 #include <cstring>
 
@@ -13,8 +17,6 @@
 namespace beagle {
 
 namespace {
-
-constexpr int kFlight = 4;               // heads a thread has in flight
 
 struct RotaryRows {
     const void *q, *k;
@@ -27,44 +29,36 @@ struct RotaryRows {
 };
 
 template <typename T, int E, bool INTER>
-__global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_constant__ RotaryArgs r, const __grid_constant__ RotaryRows a) {
+__global__ void __launch_bounds__(kRotThreads, kRotCtas) rotary_kernel(const __grid_constant__ RotaryArgs r, const __grid_constant__ RotaryRows a) {
     __shared__ __align__(16) float2 s_cs[kRotEntries];
     pdl_launch_dependents();
     pdl_wait();
     const int t = threadIdx.x;
     const long long row0 = (long long)blockIdx.x * a.g.rows;
+    const int u = t % a.g.units, slot = t / a.g.units, rl = slot / a.g.lanes, lane = slot - rl * a.g.lanes, H = a.Hq + a.Hk;
+    const long long row = row0 + rl;
+    const bool mine = rl < a.g.rows && row < a.rows;
+    RotUnit<T, E, INTER> unit;
+    typename RotUnit<T, E, INTER>::V x, y;
+    unit.place(u, r.pairs);
+    const T *q = static_cast<const T*>(a.q) + row * a.q_stride, *k = static_cast<const T*>(a.k) + row * a.k_stride;
+    T *qo = static_cast<T*>(a.q_out) + row * a.q_out_stride, *ko = static_cast<T*>(a.k_out) + row * a.k_out_stride;
+    auto load = [&](int h) { unit.load(h < a.Hq ? q + h * a.dh : k + (h - a.Hq) * a.dh, x, y); };
+    if (mine && lane < H) load(lane);
     for (int i = t; i < a.g.rows * r.pairs; i += kRotThreads) {
-        const long long row = row0 + i / r.pairs;
-        if (row < a.rows) {
-            const int pos = a.pos != nullptr ? __ldcg(a.pos + row) : (int)(a.pos0 + row % a.period);
+        const long long at = row0 + i / r.pairs;
+        if (at < a.rows) {
+            const int pos = a.pos != nullptr ? __ldcg(a.pos + at) : (int)(a.pos0 + at % a.period);
             s_cs[i] = rot_angle(r.turns[i % r.pairs], pos, r.m, r.sign);
         }
     }
     __syncthreads();
-    const int u = t % a.g.units, slot = t / a.g.units, rl = slot / a.g.lanes, lane = slot - rl * a.g.lanes;
-    const long long row = row0 + rl;
-    if (rl >= a.g.rows || row >= a.rows) return;
-    RotUnit<T, E, INTER> unit;
-    typedef typename RotUnit<T, E, INTER>::V V;
-    unit.init(u, r.pairs, s_cs + rl * r.pairs);
-    const T *q = static_cast<const T*>(a.q) + row * a.q_stride, *k = static_cast<const T*>(a.k) + row * a.k_stride;
-    T *qo = static_cast<T*>(a.q_out) + row * a.q_out_stride, *ko = static_cast<T*>(a.k_out) + row * a.k_out_stride;
-    const int H = a.Hq + a.Hk;
-    for (int h0 = lane; h0 < H; h0 += a.g.lanes * kFlight) {
-        V x[kFlight], y[kFlight];
-#pragma unroll
-        for (int i = 0; i < kFlight; ++i) {
-            const int h = h0 + i * a.g.lanes;
-            if (h < H) unit.load(h < a.Hq ? q + h * a.dh : k + (h - a.Hq) * a.dh, x[i], y[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < kFlight; ++i) {
-            const int h = h0 + i * a.g.lanes;
-            if (h < H) {
-                unit.turn(x[i], y[i]);
-                unit.store(h < a.Hq ? qo + h * a.dh : ko + (h - a.Hq) * a.dh, x[i], y[i]);
-            }
-        }
+    if (!mine) return;
+    unit.entries(s_cs + rl * r.pairs);
+    for (int h = lane; h < H; h += a.g.lanes) {
+        if (h != lane) load(h);
+        unit.turn(x, y);
+        unit.store(h < a.Hq ? qo + h * a.dh : ko + (h - a.Hq) * a.dh, x, y);
     }
 }
 
@@ -102,9 +96,9 @@ RotaryGrid rotary_grid(const beagle_rotary* r, int dtype, long long rows, int he
     RotaryGrid g;
     g.units = r->interleaved ? r->head_dim / e : pairs / e + (r->head_dim - r->rot_dim) / e;
     const int slots = kRotThreads / g.units;         // a head has at most 256 elements
-    // many rows: few heads side by side, so that a CTA takes several rows and a thread several heads per set of entries;
-    // few rows: the heads of a row over as many threads as there are
-    g.lanes = rows >= (long long)device_sm_count() * 8 ? 4 : heads;
+    // many rows: a CTA takes several, so that it has entries to form for all of its threads, and a thread several heads with the same
+    // ones; few rows: the heads of a row over as many threads as there are
+    g.lanes = rows >= (long long)device_sm_count() * 8 ? 8 : heads;
     if (g.lanes > slots) g.lanes = slots;
     g.rows = slots / g.lanes;
     if (g.rows > kRotEntries / pairs) g.rows = kRotEntries / pairs;

@@ -24,6 +24,7 @@ int rotary_unit(const beagle_rotary* r, int dtype);
 
 constexpr int kRotThreads = 256;
 constexpr int kRotEntries = 2048;        // (cosine, sine) entries of a CTA in shared memory
+constexpr int kRotCtas = 6;              // per SM: a thread has one or two 16-byte pieces in flight, the rest is up to the number of threads
 
 // How a CTA of kRotThreads divides `rows` rows of `heads` heads: `units` threads share a head, `lanes` heads of a row are worked on
 // side by side, `rows` rows.
@@ -75,24 +76,25 @@ struct RotUnit {
     int at, partner;                     // element offsets; partner < 0: none
     bool rotates;
     int count;                           // interleaved: pairs of the unit that are rotated
-    // cs_row: the row's (cosine, sine) entries
-    __device__ __forceinline__ void init(int u, int pairs, const float2* cs_row) {
+    __device__ __forceinline__ void place(int u, int pairs) {
         partner = -1;
         count = 0;
         if (INTER) {
             at = u * E;
             rotates = at < 2 * pairs;
             count = min(kCs, pairs - at / 2);
-#pragma unroll
-            for (int i = 0; i < kCs; ++i) cs[i] = i < count ? cs_row[at / 2 + i] : make_float2(1.f, 0.f);
         } else {
             const int n = pairs / E;
             rotates = u < n;
             at = rotates ? u * E : 2 * pairs + (u - n) * E;
             partner = rotates ? at + pairs : -1;
-#pragma unroll
-            for (int i = 0; i < kCs; ++i) cs[i] = rotates ? cs_row[at + i] : make_float2(1.f, 0.f);
         }
+    }
+    // cs_row: the row's (cosine, sine) entries
+    __device__ __forceinline__ void entries(const float2* cs_row) {
+        const int first = INTER ? at / 2 : at, n = INTER ? count : kCs;
+#pragma unroll
+        for (int i = 0; i < kCs; ++i) cs[i] = rotates && i < n ? cs_row[first + i] : make_float2(1.f, 0.f);
     }
     __device__ __forceinline__ void load(const T* head, V& x, V& y) const {
         x = *reinterpret_cast<const V*>(head + at);
