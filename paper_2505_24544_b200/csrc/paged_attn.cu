@@ -463,8 +463,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
     }
 }
 
-// The same for rows of groups: blockIdx.x = row of the call, blockIdx.y = query head; the partials of the row's own positions and those of the
+// The same for rows of groups, two (row of the call, query head) items a CTA; the partials of the row's own positions and those of the
 // common part, which lie with the row's launch or (`prefix.on`) with the tensor cores'.
+constexpr int kSharedJoinWarps = 4;      // of a head
 constexpr int kJoinFlight = 4;
 struct PrefixParts {
     const int2* span;
@@ -473,19 +474,24 @@ struct PrefixParts {
     uint8_t on[kMaxCallBatch], entry[kMaxCallBatch];
 };
 template <typename T, int DH>
-__global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(const __grid_constant__ SharedArgs a, const __grid_constant__ PrefixParts prefix) {
-    __shared__ float s_o[kJoinWarps][DH], s_m[kJoinWarps], s_l[kJoinWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(2 * kSharedJoinWarps * 32) paged_shared_join_kernel(const __grid_constant__ SharedArgs a, const __grid_constant__ PrefixParts prefix) {
+    // a lane holds kPer neighbouring components, four warps share a head's partials
+    constexpr int kPer = DH >= 128 ? 4 : DH >= 64 ? 2 : 1, kSteps = (DH + 32 * kPer - 1) / (32 * kPer), W = kSharedJoinWarps;
+    __shared__ float s_o[2][W][DH], s_m[2][W], s_l[2][W];
+    const int half = threadIdx.x / (W * 32), warp = threadIdx.x / 32 % W, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     pdl_wait();
-    const int b = blockIdx.x, head = blockIdx.y, kvh = head / a.G, h = head - kvh * a.G, group = a.group_of[b];
+    const int item = 2 * blockIdx.x + half, b = item / a.Hq, head = item - b * a.Hq, kvh = head / a.G, h = head - kvh * a.G;
+    const bool there = b < a.rows;
+    const int group = there ? a.group_of[b] : 255;
     const bool common = group != 255, cores = common && prefix.on[group];
-    // the row's own positions and the common part: of each the pair, the runs that worked on it, this head's row in a partial
+    // the row's own positions and the common part: of each the partials' base and distance, and how many there are.  Partial i of a source is the
+    // (i % split)th of run r0 + i / split.
     struct Source {
         const float* part;
         size_t size;                     // floats of a partial
         int o, ml;                       // offsets of the row's O and of its (maximum, sum)
-        int pair, n_pairs, r0, r1;
+        int pair, n_pairs, r0, n, split;
     };
     auto source = [&](bool first) {
         const bool tc = !first && cores;
@@ -495,49 +501,46 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(cons
             e = common ? (tc ? prefix.entry[group] : a.prefix_entry[group]) + j / block : 0;
             at = j % block;
         }
-        const int rows = tc ? prefix.part_rows : 8, pair = e * a.Hkv + kvh;
-        const int2 runs = first || common ? __ldcg((tc ? prefix.span : a.span) + pair) : make_int2(0, -1);
+        const int rows = tc ? prefix.part_rows : 8, pair = e * a.Hkv + kvh, split = tc ? 1 : a.split;
+        const int2 runs = there && (first || common) ? __ldcg((tc ? prefix.span : a.span) + pair) : make_int2(0, -1);
         return Source{tc ? prefix.part : a.part, (size_t)rows * (DH + 2), tc ? at * DH : at * (DH + 2), tc ? rows * DH + 2 * at : at * (DH + 2) + DH,
-                      pair, tc ? prefix.n_pairs : a.n_pairs, runs.x, runs.y};
+                      pair, tc ? prefix.n_pairs : a.n_pairs, runs.x, (runs.y - runs.x + 1) * split, split};
     };
     const Source own = source(true), shared = source(false);
-    const int n0 = own.r1 - own.r0 + 1, all = n0 + shared.r1 - shared.r0 + 1;
-    // Every warp takes each eighth partial, kJoinFlight of them in flight, with a maximum of its own; then the warps meet.  A lane holds
-    // kPer neighbouring components.
-    constexpr int kPer = DH >= 128 ? 4 : DH >= 64 ? 2 : 1, kSteps = (DH + 32 * kPer - 1) / (32 * kPer);
+    const int all = own.n + shared.n;
     float M = -INFINITY, L = 0.f, acc[kSteps][kPer];
 #pragma unroll
     for (int x = 0; x < kSteps; ++x)
 #pragma unroll
         for (int y = 0; y < kPer; ++y) acc[x][y] = 0.f;
-    for (int i0 = warp; i0 < all; i0 += kJoinWarps * kJoinFlight) {
-        float m[kJoinFlight], l[kJoinFlight], o[kJoinFlight][kSteps][kPer];
+    for (int i0 = warp; i0 < all; i0 += W * kJoinFlight) {
+        float2 ml[kJoinFlight];
+        float o[kJoinFlight][kSteps][kPer];
 #pragma unroll
         for (int z = 0; z < kJoinFlight; ++z) {
-            const int i = i0 + z * kJoinWarps;
-            const Source& x = i < n0 ? own : shared;
-            const int r = x.r0 + (i < n0 ? i : i - n0);
-            const bool some = i < all;
-            const float* p = x.part + (some ? (size_t)(r == x.r0 ? x.pair : x.n_pairs + r) * x.size : 0);
-            m[z] = some ? __ldcg(p + x.ml) : -INFINITY;
-            l[z] = some ? __ldcg(p + x.ml + 1) : 0.f;
+            const int i = i0 + z * W;
+            const bool some = i < all, mine = i < own.n;
+            const Source& x = mine ? own : shared;
+            const int at = some ? (mine ? i : i - own.n) : 0, run = at / x.split;
+            const float* p = x.part + (some ? ((size_t)(run == 0 ? x.pair : x.n_pairs + x.r0 + run) * x.split + (at - run * x.split)) * x.size : 0);
+            ml[z] = some ? __ldcg(reinterpret_cast<const float2*>(p + x.ml)) : make_float2(-INFINITY, 0.f);
 #pragma unroll
             for (int d = 0; d < kSteps; ++d)
 #pragma unroll
                 for (int y = 0; y < kPer; y += kPer > 1 ? 2 : 1) {       // (rows of partials begin on 8 bytes)
-                    const int at = (d * 32 + lane) * kPer + y;
+                    const int c = (d * 32 + lane) * kPer + y;
                     if (kPer > 1) {
-                        const float2 v = some && at < DH ? __ldcg(reinterpret_cast<const float2*>(p + x.o + at)) : make_float2(0.f, 0.f);
+                        const float2 v = some && c < DH ? __ldcg(reinterpret_cast<const float2*>(p + x.o + c)) : make_float2(0.f, 0.f);
                         o[z][d][y] = v.x;
                         o[z][d][y + (kPer > 1 ? 1 : 0)] = v.y;
                     } else {
-                        o[z][d][y] = some && at < DH ? __ldcg(p + x.o + at) : 0.f;
+                        o[z][d][y] = some && c < DH ? __ldcg(p + x.o + c) : 0.f;
                     }
                 }
         }
         float top = M;
 #pragma unroll
-        for (int z = 0; z < kJoinFlight; ++z) top = fmaxf(top, m[z]);
+        for (int z = 0; z < kJoinFlight; ++z) top = fmaxf(top, ml[z].x);
         const float f0 = M == -INFINITY ? 0.f : exp2f(M - top);
         L = M == -INFINITY ? L : L * f0;                         // (no position seen: the sum is 0, or NaN after a wait that ran out)
 #pragma unroll
@@ -546,12 +549,12 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(cons
             for (int y = 0; y < kPer; ++y) acc[x][y] *= f0;
 #pragma unroll
         for (int z = 0; z < kJoinFlight; ++z) {
-            const float f = m[z] == -INFINITY ? 0.f : exp2f(m[z] - top);
-            L += m[z] == -INFINITY ? l[z] : f * l[z];
+            const float f = ml[z].x == -INFINITY ? 0.f : exp2f(ml[z].x - top);
+            L += ml[z].x == -INFINITY ? ml[z].y : f * ml[z].y;
 #pragma unroll
             for (int x = 0; x < kSteps; ++x)
 #pragma unroll
-                for (int y = 0; y < kPer; ++y) acc[x][y] = fmaf(f, m[z] == -INFINITY ? 0.f : o[z][x][y], acc[x][y]);
+                for (int y = 0; y < kPer; ++y) acc[x][y] = fmaf(f, ml[z].x == -INFINITY ? 0.f : o[z][x][y], acc[x][y]);
         }
         M = top;
     }
@@ -559,19 +562,20 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_shared_join_kernel(cons
     for (int x = 0; x < kSteps; ++x)
 #pragma unroll
         for (int y = 0; y < kPer; ++y)
-            if ((x * 32 + lane) * kPer + y < DH) s_o[warp][(x * 32 + lane) * kPer + y] = acc[x][y];
-    if (lane == 0) { s_m[warp] = M; s_l[warp] = L; }
+            if ((x * 32 + lane) * kPer + y < DH) s_o[half][warp][(x * 32 + lane) * kPer + y] = acc[x][y];
+    if (lane == 0) { s_m[half][warp] = M; s_l[half][warp] = L; }
     __syncthreads();
+    if (!there) return;
     T* out = static_cast<T*>(a.o) + ((size_t)b * a.Hq + head) * DH;
-    for (int d = threadIdx.x; d < DH; d += kJoinWarps * 32) {
+    for (int d = threadIdx.x % (W * 32); d < DH; d += W * 32) {
         float top = -INFINITY, x = 0.f, y = 0.f;
 #pragma unroll
-        for (int i = 0; i < kJoinWarps; ++i) top = fmaxf(top, s_m[i]);
+        for (int i = 0; i < W; ++i) top = fmaxf(top, s_m[half][i]);
 #pragma unroll
-        for (int i = 0; i < kJoinWarps; ++i) {
-            const float f = s_m[i] == -INFINITY ? 0.f : exp2f(s_m[i] - top);
-            x = fmaf(f, s_o[i][d], x);
-            y += s_m[i] == -INFINITY ? s_l[i] : f * s_l[i];
+        for (int i = 0; i < W; ++i) {
+            const float f = s_m[half][i] == -INFINITY ? 0.f : exp2f(s_m[half][i] - top);
+            x = fmaf(f, s_o[half][i][d], x);
+            y += s_m[half][i] == -INFINITY ? s_l[half][i] : f * s_l[half][i];
         }
         out[d] = from_float<T>(y != 0.f ? x / y : 0.f);
         if (d == 0 && a.lse != nullptr) a.lse[(size_t)b * a.Hq + head] = y != 0.f ? (top + log2f(y)) * kLn2 : -INFINITY;
@@ -630,7 +634,7 @@ struct SharedCall : SharedArgs {         // the rows' launch, and where the tens
 };
 template <typename T, int DH>
 void launch_join(const SharedCall& a, int, cudaStream_t stream) {
-    launch_pdl(paged_shared_join_kernel<T, DH>, dim3(a.rows, a.Hq), dim3(kJoinWarps * 32), 0, stream, static_cast<const SharedArgs&>(a), a.prefix);
+    launch_pdl(paged_shared_join_kernel<T, DH>, dim3((a.rows * a.Hq + 1) / 2), dim3(2 * kSharedJoinWarps * 32), 0, stream, static_cast<const SharedArgs&>(a), a.prefix);
 }
 template <typename Args> struct KernelArgs { typedef PagedArgs type; };
 template <> struct KernelArgs<SharedCall> { typedef SharedArgs type; };
@@ -756,6 +760,7 @@ int entry_rows(const beagle_pages* p) { return p->dtype == BEAGLE_BF16 && p->hea
 void plan_shared(const beagle_pages* p, int Hq, int batch, int n_groups, const int32_t* group_rows, SharedCall* a, PrefixArgs* f) {
     const int G = Hq / p->n_kv_heads;
     a->block = entry_rows(p);
+    a->split = uses_mma(p) ? kConsumers : 1;
     f->block = prefix_block(G);
     int e = batch, fe = 0, most = 0;                     // the rows' own entries first
     for (int i = 0, r = 0; i < n_groups; r += group_rows[i++]) {
@@ -799,7 +804,7 @@ SharedLayout shared_ws(const beagle_pages* p, const SharedArgs& a, const PrefixA
     l.span = 0;
     l.prefix_span = l.span + up(a.n_pairs * sizeof(int2));
     l.part = l.prefix_span + up(f.n_pairs * sizeof(int2));
-    l.prefix_part = l.part + up((size_t)(a.n_pairs + shared_runs(p)) * 8 * row);
+    l.prefix_part = l.part + up((size_t)(a.n_pairs + shared_runs(p)) * a.split * 8 * row);
     l.bytes = l.prefix_part + (f.batch > 0 ? up((size_t)(f.n_pairs + shared_runs(p)) * f.part_rows * row) : 0);
     return l;
 }

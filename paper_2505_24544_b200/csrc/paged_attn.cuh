@@ -49,6 +49,7 @@ struct SharedArgs : PagedArgs {         // `batch` counts the entries
     uint8_t prefix_entry[kMaxCallBatch];        // first entry of a group's common part (the rows' own entries have the rows' numbers)
     uint8_t group_row0[kMaxCallBatch];
     int block;                          // query rows of a common part's entry
+    int split;                          // partials that a run leaves of a pair: one of each consumer warp on mma.sync, else 1
 };
 
 // How the visible tiles are divided; computed by every CTA from the lengths (64 values at most).
@@ -106,44 +107,57 @@ __device__ __forceinline__ void finish_schedule(Schedule& s) {          // secon
     if (t >= 32 && t < kMaxCallBatch) s.start[t + 1] += s.start[32];
 }
 
-// The same for the entries; whole CTA of at least 128 threads, barriers inside.  The common part of a group: shared_dev, not above its
-// shortest length, in whole tiles.
-__device__ __forceinline__ void build_schedule(const SharedArgs& a, ScheduleOf<SharedArgs::kEntries>& s) {
-    __shared__ int s_len[kMaxCallBatch], s_common[kMaxCallBatch], s_warp[4];
+// The same for the entries, of up to two sets over the same rows (`b` may be `a`: one set); whole CTA of at least 128 threads, barriers
+// inside.  The common part of a group: shared_dev, not above its shortest length, in whole tiles.
+__device__ __forceinline__ void build_schedules(const SharedArgs& a, ScheduleOf<SharedArgs::kEntries>& sa, const SharedArgs& b, ScheduleOf<SharedArgs::kEntries>& sb) {
+    __shared__ int s_len[kMaxCallBatch], s_common[kMaxCallBatch], s_warp[2][4];
     const int t = threadIdx.x, lane = t & 31;
+    int n = 0;
+    if (t < a.rows) n = min(max(__ldcg(a.length + a.slots.slot[t]), 0), a.max_pages << a.page_shift);
     if (t < a.n_groups) s_common[t] = max(__ldcg(a.shared + t), 0);
     __syncthreads();
     if (t < a.rows) {
-        const int n = min(max(__ldcg(a.length + a.slots.slot[t]), 0), a.max_pages << a.page_shift);
         s_len[t] = n;
         if (a.group_of[t] != 255) atomicMin(&s_common[a.group_of[t]], n);
     }
     __syncthreads();
-    int tiles = 0, incl = 0;
+    const bool two = &a != &b;
+    int incl[2] = {0, 0};
     if (t < SharedArgs::kEntries) {
-        if (t < a.batch) {
-            const SharedEntry e = a.entry[t];
-            const int common = e.group == 255 ? 0 : s_common[e.group] / kTile * kTile;
-            const int n = e.prefix ? common : s_len[e.row0], lo = e.prefix ? 0 : common;
-            s.len[t] = n; s.lo[t] = lo; s.first[t] = lo / kTile; s.sink_tiles[t] = 0;
-            tiles = ((n + kTile - 1) / kTile - lo / kTile) * a.Hkv;
-        }
-        incl = tiles;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
+        for (int x = 0; x < 2; ++x) {
+            const SharedArgs& y = x ? b : a;
+            ScheduleOf<SharedArgs::kEntries>& s = x ? sb : sa;
+            if (t < y.batch && (x == 0 || two)) {
+                const SharedEntry e = y.entry[t];
+                const int common = e.group == 255 ? 0 : s_common[e.group] / kTile * kTile;
+                const int len = e.prefix ? common : s_len[e.row0], lo = e.prefix ? 0 : common;
+                s.len[t] = len; s.lo[t] = lo; s.first[t] = lo / kTile; s.sink_tiles[t] = 0;
+                incl[x] = ((len + kTile - 1) / kTile - lo / kTile) * y.Hkv;
+            }
         }
-        if (lane == 31) s_warp[t >> 5] = incl;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int v = __shfl_up_sync(0xffffffffu, incl[x], o);
+                if (lane >= o) incl[x] += v;
+            }
+        if (lane == 31) { s_warp[0][t >> 5] = incl[0]; s_warp[1][t >> 5] = incl[1]; }
     }
     __syncthreads();
     if (t < SharedArgs::kEntries) {
-        for (int i = 0; i < t >> 5; ++i) incl += s_warp[i];
-        s.start[t + 1] = incl;
-        if (t == 0) s.start[0] = 0;
+        for (int i = 0; i < t >> 5; ++i) { incl[0] += s_warp[0][i]; incl[1] += s_warp[1][i]; }
+        sa.start[t + 1] = incl[0];
+        if (t == 0) sa.start[0] = 0;
+        if (two) {
+            sb.start[t + 1] = incl[1];
+            if (t == 0) sb.start[0] = 0;
+        }
     }
     __syncthreads();
 }
+__device__ __forceinline__ void build_schedule(const SharedArgs& a, ScheduleOf<SharedArgs::kEntries>& s) { build_schedules(a, s, a, s); }
 __device__ __forceinline__ void build_schedule(const PagedArgs& a, Schedule& s) {
     make_schedule(a, s);
     __syncthreads();

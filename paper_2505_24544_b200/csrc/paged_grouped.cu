@@ -27,7 +27,7 @@ struct PrefixSmem {
     static constexpr int kQ = kRows * DH * 2, kT = kTile * DH * 2;           // Q; a K or V tile, two stages of each
     static constexpr int kRing = kQ + 4 * kT;                                // as much as the rows' ring
     static_assert(kRing == kStages * 2 * PagedSmem<DH>::kTileBytes, "both kinds of work use the same memory in turn");
-    static constexpr int kBytes = kRing + PagedSmem<DH>::kJoin + 1024;       // + alignment slack
+    static constexpr int kBytes = kRing + 1024;                              // + alignment slack
 };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2) {
@@ -234,7 +234,6 @@ __global__ void __launch_bounds__(kThreads, 2) paged_grouped_kernel(const __grid
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     __shared__ __align__(8) uint64_t bars[14 + 2 * kStages];
     __shared__ ScheduleOf<SharedArgs::kEntries> s_rows, s_prefix;
-    __shared__ float s_m[kConsumers][8], s_l[kConsumers][8];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
@@ -254,8 +253,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_grouped_kernel(const __grid
     fence_before();
     pdl_launch_dependents();
     pdl_wait();
-    build_schedule(rows, s_rows);
-    build_schedule(prefix, s_prefix);
+    build_schedules(rows, s_rows, prefix, s_prefix);
     fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
     int u0, u1, p0, p1;
@@ -268,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_grouped_kernel(const __grid
         if ((phase == 0) == rows_first) {
             const int role = warp == 0 ? kConsumers : warp - 2;  // (the second warp: none)
             if (u0 < u1 && role >= 0)
-                attn_rows<DH>(tmK, tmV, rows, s_rows, smem_u32(smem), reinterpret_cast<float*>(smem + SM::kRing), full, empty, s_m, s_l, &s_abort, role, u0, u1);
+                attn_rows<DH>(tmK, tmV, rows, s_rows, smem_u32(smem), nullptr, full, empty, nullptr, nullptr, &s_abort, role, u0, u1);
             __syncthreads();
         } else {
             attn_prefix<DH>(tmQ, tmK, tmV, prefix, s_prefix, smem, bars, tmem, &s_abort, warp, p0, p1);

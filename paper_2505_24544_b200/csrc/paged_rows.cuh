@@ -51,7 +51,7 @@ struct PagedSmem {
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 // The units [u0, u1).  Warp `warp`: 0..3 consumers, 4 producer, which fills the ring at `base` (1024-byte aligned, kStages * 2 tiles); join: kJoin
-// bytes; full, empty: kStages barriers each, of 1 and kConsumers arrivals.  Barriers have not been used before.
+// bytes, and s_m, s_l, where the warps meet (the shared form does not use them); full, empty: kStages barriers each, of 1 and kConsumers arrivals.  Barriers have not been used before.
 template <int DH, typename Args>
 __device__ __forceinline__ void attn_rows(const CUtensorMap& tmK, const CUtensorMap& tmV, const Args& a, const ScheduleOf<Args::kEntries>& s, uint32_t base,
                                           float* join, uint32_t full, uint32_t empty, float (*s_m)[8], float (*s_l)[8], volatile int* s_abort, int warp, int u0,
@@ -213,6 +213,20 @@ __device__ __forceinline__ void attn_rows(const CUtensorMap& tmK, const CUtensor
         // ---- the pair (or this run's part of it) is done: join the four warps, rows = heads
         l += __shfl_xor_sync(0xffffffffu, l, 1);
         l += __shfl_xor_sync(0xffffffffu, l, 2);
+        if constexpr (Args::kShared) {
+            // many short pairs: every warp leaves its part for the join, the warps need not meet
+            if (g < rows_of(a, b)) {
+                float* dst = a.part + (((size_t)part_at(a, b * a.Hkv + kvh, !first_pair_open, seg) * kConsumers + warp) * 8 + g) * (DH + 2);
+#pragma unroll
+                for (int i = 0; i < DH / 8; ++i) *reinterpret_cast<float2*>(dst + 8 * i + 2 * c) = make_float2(o[i][0], o[i][1]);
+                if (c == 0) *reinterpret_cast<float2*>(dst + DH) = make_float2(m, l);
+            }
+            first_pair_open = false;
+            m = -INFINITY; l = 0.f;
+#pragma unroll
+            for (int i = 0; i < DH / 8; ++i) o[i][0] = o[i][1] = 0.f;
+            continue;
+        }
         if (c == 0) { s_m[warp][g] = m; s_l[warp][g] = l; }
         consumers_sync();
         float M = -INFINITY, L = 0.f;
@@ -244,7 +258,7 @@ __device__ __forceinline__ void attn_rows(const CUtensorMap& tmK, const CUtensor
         }
         if (warp == 0 && g < rows_of(a, b)) {
             const int head = kvh * a.G + g;
-            if (!Args::kShared && last && !first_pair_open) {    // all of the pair's tiles were in this run
+            if (last && !first_pair_open) {    // all of the pair's tiles were in this run
                 const float inv = L != 0.f ? 1.f / L : 0.f;
                 uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<bf16*>(a.o) + ((size_t)b * a.Hq + head) * DH) + c;
 #pragma unroll
