@@ -81,7 +81,7 @@ __device__ __forceinline__ void begin_run(const PagedArgs& a, const Schedule& s,
 
 template <typename T>
 __device__ __forceinline__ void begin_run(const SharedArgs& a, const ScheduleOf<SharedArgs::kEntries>& s, int, int& u0, int& u1) {
-    begin_shared(a, s, threadIdx.x, blockDim.x, u0, u1);
+    begin_shared(a, s, blockIdx.x, gridDim.x, threadIdx.x, blockDim.x, u0, u1);
 }
 
 template <int DH, typename Args>
@@ -109,7 +109,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     int u0, u1;
     begin_run<bf16>(a, s, DH, u0, u1);
     if (u0 >= u1) return;
-    attn_rows<DH>(tmK, tmV, a, s, base, join, full, empty, s_m, s_l, &s_abort, threadIdx.x >> 5, u0, u1);
+    attn_rows<DH>(tmK, tmV, a, s, base, join, full, empty, s_m, s_l, &s_abort, threadIdx.x >> 5, blockIdx.x, u0, u1);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__((SimtCfg<T, DH, GM>::kWarps + 1) * 32, 2) page
                 static_cast<T*>(a.o)[((size_t)b * a.Hq + head) * DH + d] = from_float<T>(L != 0.f ? acc / L : 0.f);
                 if (d == 0 && a.lse != nullptr) a.lse[(size_t)b * a.Hq + head] = L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
             } else {
-                float* dst = a.part + ((size_t)part_at(a, b * a.Hkv + kvh, !first_pair_open, seg) * 8 + h) * (DH + 2);
+                float* dst = a.part + ((size_t)part_at(a, b * a.Hkv + kvh, !first_pair_open, seg, blockIdx.x) * 8 + h) * (DH + 2);
                 dst[d] = acc;
                 if (d == 0) { dst[DH] = M; dst[DH + 1] = L; }
             }

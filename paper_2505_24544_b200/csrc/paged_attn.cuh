@@ -203,13 +203,13 @@ struct Walk {
     __device__ __forceinline__ int tile(const ScheduleOf<N>& s) const { return i < s.sink_tiles[b] ? i : s.first[b] + i - s.sink_tiles[b]; }
 };
 
-// The shared form's runs: never more than there are tiles, so that every run between two others has some.
-__device__ __forceinline__ Runs shared_runs_of(int total) { return Runs(total, max(1, min(total, (int)gridDim.x))); }
-// The units of this CTA's run; threads 0 <= t < n leave word of which runs work on which pair (shared out over the CTAs).
-__device__ __forceinline__ void begin_shared(const SharedArgs& a, const ScheduleOf<SharedArgs::kEntries>& s, int t, int n_threads, int& u0, int& u1) {
-    const Runs runs = shared_runs_of(s.start[SharedArgs::kEntries]);
-    u0 = (int)blockIdx.x < runs.runs ? runs.begin(blockIdx.x) : runs.total;
-    u1 = (int)blockIdx.x < runs.runs ? runs.begin(blockIdx.x + 1) : runs.total;
+// The units of run `run` of `count`, never more runs than there are tiles, so that every run between two others has some.  Threads 0 <= t < n
+// leave word of which runs work on which pair (shared out over the CTAs of the grid).
+__device__ __forceinline__ void begin_shared(const SharedArgs& a, const ScheduleOf<SharedArgs::kEntries>& s, int run, int count, int t, int n_threads, int& u0, int& u1) {
+    const int total = s.start[SharedArgs::kEntries];
+    const Runs runs(total, max(1, min(total, count)));
+    u0 = run >= 0 && run < runs.runs ? runs.begin(run) : 0;
+    u1 = run >= 0 && run < runs.runs ? runs.begin(run + 1) : 0;
     if (t < 0) return;
     for (int p = blockIdx.x + gridDim.x * t; p < a.n_pairs; p += gridDim.x * n_threads) {
         const int e = p / a.Hkv, n = tiles_of(s, e, a.Hkv), first = s.start[e] + (p - e * a.Hkv) * n;

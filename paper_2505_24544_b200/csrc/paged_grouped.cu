@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kThreads = 192;            // warp 0: TMA producer, warp 1: issues the products, warps 2-5: softmax
 constexpr int kRows = 128;               // query rows of a tile
+constexpr float kPrefixCost = 6.f, kRowsCost = 5.f;      // of a tile
 
 template <int DH>
 struct PrefixSmem {
@@ -40,7 +41,7 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
 template <int DH>
 __device__ __forceinline__ void attn_prefix(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PrefixArgs& a,
                                             const ScheduleOf<SharedArgs::kEntries>& s, uint8_t* smem, uint64_t* bars, uint32_t tmem, volatile int* s_abort, int warp,
-                                            int u, int u1) {
+                                            int run, int u, int u1) {
     using SM = PrefixSmem<DH>;
     constexpr int kHalves = DH / 64;
     constexpr uint32_t kO = 128;                                 // S / P at columns 0 and 64, O at 128
@@ -200,7 +201,7 @@ __device__ __forceinline__ void attn_prefix(const CUtensorMap& tmQ, const CUtens
                 if (lane == 0) mbar_arrive(p_full + 8 * st);
             }
             if (ok) ok = warp_wait(pv_done + 8 * ((done + J - 1) & 1), ((done + J - 1) >> 1) & 1, s_abort);
-            const int part = w.i == 0 ? w.b * a.Hkv + w.kvh : a.n_pairs + blockIdx.x;
+            const int part = w.i == 0 ? w.b * a.Hkv + w.kvh : a.n_pairs + run;
             float* dst = a.part + (size_t)part * a.part_rows * (DH + 2);
             fence_after();
 #pragma unroll
@@ -256,21 +257,26 @@ __global__ void __launch_bounds__(kThreads, 2) paged_grouped_kernel(const __grid
     build_schedules(rows, s_rows, prefix, s_prefix);
     fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-    int u0, u1, p0, p1;
+    // The CTAs do one kind of work each, shared out by what a tile of it takes (kPrefixCost : kRowsCost; an SM does 1.4 and 1.2 tiles a microsecond), the two
+    // kinds side by side on an SM as far as possible: one waits for memory, the other for the products.
+    const int total_p = s_prefix.start[SharedArgs::kEntries], total_r = s_rows.start[SharedArgs::kEntries], n = (int)gridDim.x;
+    const float cost_p = (float)total_p * kPrefixCost, cost_r = (float)total_r * kRowsCost;
+    int n_prefix = total_p + total_r > 0 ? (int)((float)n * cost_p / (cost_p + cost_r) + 0.5f) : 0;
+    if (total_p > 0) n_prefix = max(n_prefix, 1);
+    if (total_r > 0) n_prefix = min(n_prefix, n - 1);
+    const int half = (n + 1) / 2, at = (int)blockIdx.x < half ? 2 * (int)blockIdx.x : 2 * ((int)blockIdx.x - half) + 1;       // neighbours share an SM
+    const int before = (int)((long long)at * n_prefix / n);      // CTAs of the first kind in front of this one
+    const bool does_prefix = (int)((long long)(at + 1) * n_prefix / n) > before;
     const int helper = (int)threadIdx.x - 32;                    // the second warp, which has the least to do
-    begin_shared(rows, s_rows, helper, kThreads - 32, u0, u1);
-    begin_shared(prefix, s_prefix, helper, kThreads - 32, p0, p1);
-    // the upper half of the CTAs, the second ones on their SMs, begin with the rows: one kind of work waits for memory, the other for the products
-    const bool rows_first = blockIdx.x >= gridDim.x / 2;
-    for (int phase = 0; phase < 2; ++phase) {
-        if ((phase == 0) == rows_first) {
-            const int role = warp == 0 ? kConsumers : warp - 2;  // (the second warp: none)
-            if (u0 < u1 && role >= 0)
-                attn_rows<DH>(tmK, tmV, rows, s_rows, smem_u32(smem), nullptr, full, empty, nullptr, nullptr, &s_abort, role, u0, u1);
-            __syncthreads();
-        } else {
-            attn_prefix<DH>(tmQ, tmK, tmV, prefix, s_prefix, smem, bars, tmem, &s_abort, warp, p0, p1);
-        }
+    int u0, u1, p0, p1;
+    begin_shared(rows, s_rows, does_prefix ? -1 : at - before, n - n_prefix, helper, kThreads - 32, u0, u1);
+    begin_shared(prefix, s_prefix, does_prefix ? before : -1, n_prefix, helper, kThreads - 32, p0, p1);
+    if (does_prefix) {
+        attn_prefix<DH>(tmQ, tmK, tmV, prefix, s_prefix, smem, bars, tmem, &s_abort, warp, before, p0, p1);
+    } else {
+        const int role = warp == 0 ? kConsumers : warp - 2;      // (the second warp: none)
+        if (u0 < u1 && role >= 0)
+            attn_rows<DH>(tmK, tmV, rows, s_rows, smem_u32(smem), nullptr, full, empty, nullptr, nullptr, &s_abort, role, at - before, u0, u1);
     }
     fence_before();
     __syncthreads();

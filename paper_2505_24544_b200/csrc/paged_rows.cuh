@@ -17,8 +17,8 @@ constexpr int kCtasPerSm = 2;
 
 // The entries' pairs always leave partials, at a place of their own: the part of a pair that begins it at its number, a later one behind
 // them at the run's.
-__device__ __forceinline__ int part_at(const PagedArgs&, int, bool, int seg) { return 2 * blockIdx.x + seg; }
-__device__ __forceinline__ int part_at(const SharedArgs& a, int pair, bool begins, int) { return begins ? pair : a.n_pairs + (int)blockIdx.x; }
+__device__ __forceinline__ int part_at(const PagedArgs&, int, bool, int seg, int run) { return 2 * run + seg; }
+__device__ __forceinline__ int part_at(const SharedArgs& a, int pair, bool begins, int, int run) { return begins ? pair : a.n_pairs + run; }
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
@@ -50,12 +50,12 @@ struct PagedSmem {
 
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-// The units [u0, u1).  Warp `warp`: 0..3 consumers, 4 producer, which fills the ring at `base` (1024-byte aligned, kStages * 2 tiles); join: kJoin
+// The units [u0, u1) of run `run`.  Warp `warp`: 0..3 consumers, 4 producer, which fills the ring at `base` (1024-byte aligned, kStages * 2 tiles); join: kJoin
 // bytes, and s_m, s_l, where the warps meet (the shared form does not use them); full, empty: kStages barriers each, of 1 and kConsumers arrivals.  Barriers have not been used before.
 template <int DH, typename Args>
 __device__ __forceinline__ void attn_rows(const CUtensorMap& tmK, const CUtensorMap& tmV, const Args& a, const ScheduleOf<Args::kEntries>& s, uint32_t base,
-                                          float* join, uint32_t full, uint32_t empty, float (*s_m)[8], float (*s_l)[8], volatile int* s_abort, int warp, int u0,
-                                          int u1) {
+                                          float* join, uint32_t full, uint32_t empty, float (*s_m)[8], float (*s_l)[8], volatile int* s_abort, int warp, int run,
+                                          int u0, int u1) {
     using SM = PagedSmem<DH>;
     const int lane = threadIdx.x & 31;
     Walk w;
@@ -216,7 +216,7 @@ __device__ __forceinline__ void attn_rows(const CUtensorMap& tmK, const CUtensor
         if constexpr (Args::kShared) {
             // many short pairs: every warp leaves its part for the join, the warps need not meet
             if (g < rows_of(a, b)) {
-                float* dst = a.part + (((size_t)part_at(a, b * a.Hkv + kvh, !first_pair_open, seg) * kConsumers + warp) * 8 + g) * (DH + 2);
+                float* dst = a.part + (((size_t)part_at(a, b * a.Hkv + kvh, !first_pair_open, seg, run) * kConsumers + warp) * 8 + g) * (DH + 2);
 #pragma unroll
                 for (int i = 0; i < DH / 8; ++i) *reinterpret_cast<float2*>(dst + 8 * i + 2 * c) = make_float2(o[i][0], o[i][1]);
                 if (c == 0) *reinterpret_cast<float2*>(dst + DH) = make_float2(m, l);
@@ -265,7 +265,7 @@ __device__ __forceinline__ void attn_rows(const CUtensorMap& tmK, const CUtensor
                 for (int i = 0; i < DH / 8; ++i) dst[4 * i] = pack2(o[i][0] * inv, o[i][1] * inv);
                 if (c == 0 && a.lse != nullptr) a.lse[(size_t)b * a.Hq + head] = L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
             } else {
-                float* dst = a.part + ((size_t)part_at(a, b * a.Hkv + kvh, !first_pair_open, seg) * 8 + g) * (DH + 2);
+                float* dst = a.part + ((size_t)part_at(a, b * a.Hkv + kvh, !first_pair_open, seg, run) * 8 + g) * (DH + 2);
 #pragma unroll
                 for (int i = 0; i < DH / 8; ++i) *reinterpret_cast<float2*>(dst + 8 * i + 2 * c) = make_float2(o[i][0], o[i][1]);
                 if (c == 0) { dst[DH] = M; dst[DH + 1] = L; }
