@@ -37,6 +37,11 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
                  : "memory");
 }
 
+// 32 bytes, a whole sector, at once: each thread writes a row of its own.
+__device__ __forceinline__ void store32(float* p, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+
 // The common parts' run [u, u1) of this CTA: warp 0 producer, 1 issues the products, 2..5 softmax.  Ends with all of shared and tensor memory free.
 template <int DH>
 __device__ __forceinline__ void attn_prefix(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const PrefixArgs& a,
@@ -67,44 +72,47 @@ __device__ __forceinline__ void attn_prefix(const CUtensorMap& tmQ, const CUtens
                 const int id = lane < parts ? __ldcg(table + (pos >> a.page_shift)) : -1;
                 return id >= 0 && id < a.n_pages ? id : -1;
             };
-            int page = page_of(0);
-            bool waiting = false;                                // a request for the queries is out
+            int page = page_of(0);                               // this lane's of the tile whose values come next
             if (ok && lane == 0) {
                 mbar_expect_tx(q_full, kHalves * (kRows / a.G) * a.G * 128);
 #pragma unroll
                 for (int hf = 0; hf < kHalves; ++hf) tma_load_3d(sQ + hf * (kRows * 128), &tmQ, q_full, hf * 64, w.kvh * a.G, e.row0 + e.j0 / a.G);
             }
-            waiting = ok;
+            const bool waiting = ok;                             // a request for the queries is out
             int k_issued = done, v_issued = done;
-            for (int j = 0; j < J && ok; ++j) {
-                const int jg = done + j, st = jg & 1, ph = (jg >> 1) & 1;
+            auto copy = [&](int j, int id, const CUtensorMap* tm, uint32_t dst, uint32_t full) {
                 const int pos = (w.i + j) * kTile + lane * rows;
-                const int row = page >= 0 ? ((page * a.Hkv + w.kvh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : 0;
-                const bool copy = page >= 0;
-                const int copies = __popc(__ballot_sync(0xffffffffu, copy));
-                if (j + 1 < J) page = page_of(j + 1);
-                ok = warp_wait(k_empty + 8 * st, ph ^ 1, s_abort);
-                if (!ok) break;
+                const int row = id >= 0 ? ((id * a.Hkv + w.kvh) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : 0;
+                const int copies = __popc(__ballot_sync(0xffffffffu, id >= 0));
                 if (lane == 0) {
-                    if (copies > 0) mbar_expect_tx(k_full + 8 * st, kHalves * copies * bytes);
-                    else mbar_arrive(k_full + 8 * st);
+                    if (copies > 0) mbar_expect_tx(full, kHalves * copies * bytes);
+                    else mbar_arrive(full);
                 }
                 __syncwarp();
-                if (copy)
+                if (id >= 0)
 #pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf) tma_load_2d(sK + st * SM::kT + hf * (kTile * 128) + lane * bytes, &tmK, k_full + 8 * st, 64 * hf, row);
+                    for (int hf = 0; hf < kHalves; ++hf) tma_load_2d(dst + hf * (kTile * 128) + lane * bytes, tm, full, 64 * hf, row);
+                __syncwarp();
+            };
+            auto keys = [&](int j, int id) {
+                const int jg = done + j, st = jg & 1;
+                ok = warp_wait(k_empty + 8 * st, ((jg >> 1) & 1) ^ 1, s_abort);
+                if (!ok) return;
+                copy(j, id, &tmK, sK + st * SM::kT, k_full + 8 * st);
                 ++k_issued;
-                ok = warp_wait(pv_done + 8 * st, ph ^ 1, s_abort);
+            };
+            if (ok) keys(0, page);
+            for (int j = 0; j < J && ok; ++j) {
+                // the next tile's keys before this one's values, whose place is free later
+                const int next = j + 1 < J ? page_of(j + 1) : -1;
+                if (j + 1 < J) keys(j + 1, next);
                 if (!ok) break;
-                if (lane == 0) {
-                    if (copies > 0) mbar_expect_tx(v_full + 8 * st, kHalves * copies * bytes);
-                    else mbar_arrive(v_full + 8 * st);
-                }
-                __syncwarp();
-                if (copy)
-#pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf) tma_load_2d(sV + st * SM::kT + hf * (kTile * 128) + lane * bytes, &tmV, v_full + 8 * st, 64 * hf, row);
+                const int jg = done + j, st = jg & 1;
+                ok = warp_wait(pv_done + 8 * st, ((jg >> 1) & 1) ^ 1, s_abort);
+                if (!ok) break;
+                copy(j, page, &tmV, sV + st * SM::kT, v_full + 8 * st);
                 ++v_issued;
+                page = next;
             }
             if (!ok) {                                           // copies already requested still land (bounded)
                 if (waiting)
@@ -211,7 +219,7 @@ __device__ __forceinline__ void attn_prefix(const CUtensorMap& tmQ, const CUtens
                 tmem_ld_wait();
                 if (jr < e.n)
 #pragma unroll
-                    for (int x = 0; x < 32; x += 4) *reinterpret_cast<uint4*>(dst + jr * DH + c0 + x) = make_uint4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+                    for (int x = 0; x < 32; x += 8) store32(dst + jr * DH + c0 + x, o + x);
             }
             // a wait that ran out leaves NaN in what depends on it
             if (jr < e.n) *reinterpret_cast<float2*>(dst + a.part_rows * DH + 2 * jr) = make_float2(m, ok ? l : __int_as_float(0x7fffffff));
@@ -250,6 +258,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_grouped_kernel(const __grid
         s_abort = 0;
         fence_barrier_init();
     }
+    if (threadIdx.x == 32 * 3) { prefetch_tensormap(&tmQ); prefetch_tensormap(&tmK); prefetch_tensormap(&tmV); }
     if (warp == 1) tmem_alloc<kTmem>(smem_u32(&s_tmem));
     fence_before();
     pdl_launch_dependents();
