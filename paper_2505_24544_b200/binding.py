@@ -593,6 +593,22 @@ def _row_stride(name: str, t: torch.Tensor, lead: int) -> int:
     return st[0] if t.shape[0] > 1 else heads * dh           # one row: any distance
 
 
+def _rows(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], lead: int, device: int) -> Tuple[int, int]:
+    """Address and row distance (``_row_stride``) of a tensor whose rows may be strided, checked as ``_check`` does; device: the current one."""
+    if t.dtype == dtype and t.shape == shape and t.get_device() == device:
+        return t.data_ptr(), shape[-2] * shape[-1] if t.is_contiguous() else _row_stride(name, t, lead)
+    return _check(name, t, dtype, shape, False), 0                   # (raises)
+
+
+def _dense(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...], device: int) -> Optional[int]:
+    """Address of a dense tensor, checked as ``_check`` does, or None for None."""
+    if t is None:
+        return None
+    if t.dtype == dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    return _check(name, t, dtype, shape)
+
+
 class PagedCache:
     """A key/value cache in pages (``beagle_pages``): the device tensors, owned here, and the structure that names them.
 
@@ -633,6 +649,7 @@ class PagedCache:
         p.ws, p.ws_bytes = self.ws.data_ptr(), n.value
         self.struct, self.ref, self.device_index = p, C.byref(p), k.get_device()
         self.attn_ws_bytes: Dict[Tuple[int, int, int], int] = {}      # (query heads, window, sinks) -> workspace of beagle_paged_attn
+        self.shared_ws_bytes: Dict[Tuple[int, ...], int] = {}         # (batch, query heads, groups) -> of beagle_paged_attn_shared
 
     def on_current_device(self) -> int:
         """The current stream, after checking that the cache lies on the current device."""
@@ -756,19 +773,23 @@ def beagle_rotary_apply(rot: Rotary, q: torch.Tensor, q_out: torch.Tensor, k: Op
         raise ValueError("q: [rows, heads, head_dim] float32 / bfloat16")
     if (k is None) != (k_out is None):
         raise ValueError("k and k_out: both or neither")
-    rows, hq, dh = q.shape
+    rows, hq, dh = shape = tuple(q.shape)
     if dh != rot.struct.head_dim:
         raise ValueError(f"q: heads of {rot.struct.head_dim} components")
-    args, hk = [_check("q", q, q.dtype, (rows, hq, dh), False), _row_stride("q", q, 1), _check("q_out", q_out, q.dtype, (rows, hq, dh), False), _row_stride("q_out", q_out, 1)], 0
-    kargs = [None, 0, None, 0]
+    dt, device = q.dtype, torch._C._cuda_getDevice()
+    qp, qs = _rows("q", q, dt, shape, 1, device)
+    qo, qos = (qp, qs) if q_out is q else _rows("q_out", q_out, dt, shape, 1, device)
+    hk, kp, ks, ko, kos = 0, None, 0, None, 0
     if k is not None:
         if k.dim() != 3:
             raise ValueError("k: [rows, heads, head_dim]")
         hk = k.shape[1]
-        kargs = [_check("k", k, q.dtype, (rows, hk, dh), False), _row_stride("k", k, 1), _check("k_out", k_out, q.dtype, (rows, hk, dh), False), _row_stride("k_out", k_out, 1)]
-    pp = None if pos is None else _check("pos", pos, torch.int32, (rows,))
-    _pages_ok(rot.lib.beagle_rotary_apply(rot.ref, BEAGLE_BF16 if q.dtype == torch.bfloat16 else BEAGLE_FP32, rows, pp, pos0, period, hq, *args, hk, *kargs,
-                                          int(bool(inverse)), _stream()), "beagle_rotary_apply")
+        shape = (rows, hk, dh)
+        kp, ks = _rows("k", k, dt, shape, 1, device)
+        ko, kos = (kp, ks) if k_out is k else _rows("k_out", k_out, dt, shape, 1, device)
+    pp = _dense("pos", pos, torch.int32, (rows,), device)
+    _pages_ok(rot.lib.beagle_rotary_apply(rot.ref, BEAGLE_BF16 if dt == torch.bfloat16 else BEAGLE_FP32, rows, pp, pos0, period, hq, qp, qs, qo, qos, hk, kp, ks,
+                                          ko, kos, int(bool(inverse)), torch._C._cuda_getCurrentRawStream(device)), "beagle_rotary_apply")
 
 
 def beagle_pages_append_rotary(cache: PagedCache, slots: Sequence[int], rot: Rotary, k_new: torch.Tensor, v_new: torch.Tensor,
@@ -777,11 +798,13 @@ def beagle_pages_append_rotary(cache: PagedCache, slots: Sequence[int], rot: Rot
     """``beagle_pages_append`` with every new key rotated at the position that it takes.  q: [len(slots), T, n_q_heads, head_dim], the queries of
     the new rows (rows may be strided), rotated at the key's position + q_offset into q_out (dense; q itself if that is dense); rows from
     n_new on are left as they were."""
-    c, B = cache.struct, len(slots)
-    shape = (B, k_new.shape[1] if k_new.dim() == 4 else -1, c.n_kv_heads, c.head_dim)
-    kp, vp = _check("k_new", k_new, cache.k.dtype, shape, False), _check("v_new", v_new, cache.k.dtype, shape, False)
-    n_ptr = None if n_new is None else _check("n_new", n_new, torch.int32, (B,))
-    ok_ptr = None if ok is None else _check("ok", ok, torch.int32, (B,))
+    c, B, dt, stream = cache.struct, len(slots), cache.k.dtype, cache.on_current_device()
+    device = cache.device_index
+    T = k_new.shape[1] if k_new.dim() == 4 else -1
+    shape = (B, T, c.n_kv_heads, c.head_dim)
+    kp, ks = _rows("k_new", k_new, dt, shape, 2, device)
+    vp, vs = _rows("v_new", v_new, dt, shape, 2, device)
+    n_ptr, ok_ptr = _dense("n_new", n_new, torch.int32, (B,), device), _dense("ok", ok, torch.int32, (B,), device)
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out: both or neither")
     hq, qp, qs, qo = 0, None, 0, None
@@ -789,10 +812,10 @@ def beagle_pages_append_rotary(cache: PagedCache, slots: Sequence[int], rot: Rot
         if q.dim() != 4:
             raise ValueError("q: [batch, T, n_q_heads, head_dim]")
         hq = q.shape[2]
-        want = (B, shape[1], hq, c.head_dim)
-        qp, qs, qo = _check("q", q, cache.k.dtype, want, False), _row_stride("q", q, 2), _check("q_out", q_out, cache.k.dtype, want)
-    _pages_ok(cache.lib.beagle_pages_append_rotary(cache.ref, rot.ref, B, _host_i32(slots), shape[1], n_ptr, kp, _row_stride("k_new", k_new, 2), vp,
-                                                   _row_stride("v_new", v_new, 2), hq, qp, qs, qo, q_offset, ok_ptr, cache.on_current_device()),
+        shape = (B, T, hq, c.head_dim)
+        qp, qs = _rows("q", q, dt, shape, 2, device)
+        qo = _dense("q_out", q_out, dt, shape, device)
+    _pages_ok(cache.lib.beagle_pages_append_rotary(cache.ref, rot.ref, B, _host_i32(slots), T, n_ptr, kp, ks, vp, vs, hq, qp, qs, qo, q_offset, ok_ptr, stream),
               "beagle_pages_append_rotary")
 
 
@@ -805,10 +828,16 @@ def beagle_pages_shared(cache: PagedCache, slots: Sequence[int], groups: Sequenc
 
 
 def beagle_paged_attn_shared_workspace_bytes(cache: PagedCache, batch: int, n_q_heads: int, groups: Sequence[int]) -> int:
-    v = C.c_size_t()
-    _pages_ok(cache.lib.beagle_paged_attn_shared_workspace_bytes(cache.ref, batch, n_q_heads, len(groups), _host_i32(groups), C.byref(v)),
-              "beagle_paged_attn_shared_workspace_bytes")
-    return v.value
+    key = (batch, n_q_heads, *groups)
+    n = cache.shared_ws_bytes.get(key)
+    if n is None:
+        v = C.c_size_t()
+        _pages_ok(cache.lib.beagle_paged_attn_shared_workspace_bytes(cache.ref, batch, n_q_heads, len(groups), _host_i32(groups), C.byref(v)),
+                  "beagle_paged_attn_shared_workspace_bytes")
+        if len(cache.shared_ws_bytes) >= 1000:                       # (every grouping has a size of its own)
+            cache.shared_ws_bytes.clear()
+        n = cache.shared_ws_bytes[key] = v.value
+    return n
 
 
 def beagle_paged_attn_shared(cache: PagedCache, slots: Sequence[int], groups: Sequence[int], shared: torch.Tensor, q: torch.Tensor, out: torch.Tensor,
@@ -817,19 +846,19 @@ def beagle_paged_attn_shared(cache: PagedCache, slots: Sequence[int], groups: Se
     groups: rows of each group, the call's rows in their order; shared: int32 [len(groups)], how many positions they have in common
     (``beagle_pages_shared``; any smaller number gives the same attention).  q, out, lse as there; ws: scratch of
     ``beagle_paged_attn_shared_workspace_bytes`` (None: taken from torch's allocator for this call)."""
-    c, B = cache.struct, len(slots)
+    c, B, dt, stream = cache.struct, len(slots), cache.k.dtype, cache.on_current_device()
+    device = cache.device_index
     if q.dim() != 3:
         raise ValueError("q: [batch, n_q_heads, head_dim]")
     hq = q.shape[1]
-    qp = _check("q", q, cache.k.dtype, (B, hq, c.head_dim), False)
-    op = _check("out", out, cache.k.dtype, (B, hq, c.head_dim))
-    lp = None if lse is None else _check("lse", lse, torch.float32, (B, hq))
-    sp = _check("shared", shared, torch.int32, (len(groups),))
-    stream = cache.on_current_device()
+    shape = (B, hq, c.head_dim)
+    qp, qs = _rows("q", q, dt, shape, 1, device)
+    op = _dense("out", out, dt, shape, device)
+    lp, sp = _dense("lse", lse, torch.float32, (B, hq), device), _dense("shared", shared, torch.int32, (len(groups),), device)
     if ws is None:
         ws = torch.empty(beagle_paged_attn_shared_workspace_bytes(cache, B, hq, groups), dtype=torch.uint8, device=q.device)
-    _pages_ok(cache.lib.beagle_paged_attn_shared(cache.ref, B, _host_i32(slots), len(groups), _host_i32(groups), sp, hq, qp, _row_stride("q", q, 1), op, lp,
-                                                 *_scratch(ws), stream), "beagle_paged_attn_shared")
+    _pages_ok(cache.lib.beagle_paged_attn_shared(cache.ref, B, _host_i32(slots), len(groups), _host_i32(groups), sp, hq, qp, qs, op, lp, *_scratch(ws), stream),
+              "beagle_paged_attn_shared")
 
 
 def beagle_sample(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor, temperature: Optional[torch.Tensor] = None,
@@ -840,17 +869,18 @@ def beagle_sample(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor, t
     top_p (fp32), min_p (fp32); logp (fp32 [rows], written): ln of the token's probability among those kept."""
     if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("logits: [rows, vocab] float32 / bfloat16")
-    rows, v = logits.shape
-    lp = _check("logits", logits, logits.dtype, (rows, v), False)
+    rows, v = shape = tuple(logits.shape)
+    device = torch._C._cuda_getDevice()
+    if logits.get_device() != device:
+        _check("logits", logits, logits.dtype, shape, False)
     if v > 1 and logits.stride(1) != 1:
         raise ValueError("logits: the values of a row must be dense")
-    stride = logits.stride(0) if rows > 1 else v
-    ptr = [None if t is None else _check(n, t, dt, (rows,)) for n, t, dt in
-           (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32))]
-    up, tp = _check("u", u, torch.float32, (rows,)), _check("tokens", tokens, torch.int32, (rows,))
-    op = None if logp is None else _check("logp", logp, torch.float32, (rows,))
-    _pages_ok(load_library().beagle_sample(lp, BEAGLE_BF16 if logits.dtype == torch.bfloat16 else BEAGLE_FP32, rows, v, stride, *ptr, up, tp, op, _stream()),
-              "beagle_sample")
+    f32, i32, n = torch.float32, torch.int32, (rows,)
+    _pages_ok(load_library().beagle_sample(
+        logits.data_ptr(), BEAGLE_BF16 if logits.dtype == torch.bfloat16 else BEAGLE_FP32, rows, v, logits.stride(0) if rows > 1 else v,
+        _dense("temperature", temperature, f32, n, device), _dense("top_k", top_k, i32, n, device), _dense("top_p", top_p, f32, n, device),
+        _dense("min_p", min_p, f32, n, device), _dense("u", u, f32, n, device), _dense("tokens", tokens, i32, n, device), _dense("logp", logp, f32, n, device),
+        torch._C._cuda_getCurrentRawStream(device)), "beagle_sample")
 
 
 def beagle_prefill_pages(ctx: Context, cache: PagedCache, seq_slot: Sequence[int], new_len: Sequence[int], hidden: Optional[torch.Tensor],

@@ -75,12 +75,11 @@ beagle_status rotary_check(const beagle_rotary* r, int dtype) {
 }
 
 void rotary_args(const beagle_rotary* r, int inverse, RotaryArgs* out) {
-    memset(out, 0, sizeof(*out));
     out->pairs = r->rot_dim / 2;
     out->interleaved = r->interleaved;
     out->m = (float)r->mscale;
     out->sign = inverse ? -1.f : 1.f;
-    for (int i = 0; i < out->pairs; ++i) out->turns[i] = r->freq[i] / 6.283185307179586476925;
+    for (int i = 0; i < out->pairs; ++i) out->turns[i] = r->freq[i] * 0.15915494309189533577;        // 1 / 2 pi
 }
 
 int rotary_unit(const beagle_rotary* r, int dtype) {
