@@ -12,6 +12,8 @@
 // known of it.  What costs is the double-precision weight (some 25 instructions), so it is formed
 //   - of all tokens, once, only if top-k does not limit them: the total is needed then.  top-p: a histogram of fp32 weights says beforehand
 //     in which few bins of distance the border lies, so that the same pass finds the exact weight before them and lists their tokens;
+//     bf16 logits have few values: there the tokens of every code are counted and the border falls on one code, exactly, and the
+//     tokens' weights come from a table by code (1408 codes of either sign; the few logits nearer to 0 are computed);
 //   - otherwise of candidates alone, those a bound in fp32 does not exclude.  top-k: at least k groups of a few neighbours (the ones read as
 //     one 16-byte piece) have their largest in the leading bins of a histogram, so the k-th token is in those too.  min-p: its distance.
 // Up to kGather candidates or tokens of the border's bins, nearly always, go to the first block, which sorts them.  More of them:
@@ -41,6 +43,7 @@ constexpr int kBins = 2048, kPerThread = kBins / kThreads;
 constexpr int kMassBins = 1024;          // of the first block's selections
 constexpr int kGather = 3500;            // candidates that the first block finishes alone
 constexpr int kList = kThreads;          // tokens that a block compares pairwise (the cluster's search)
+constexpr int kSide = 1408;              // bf16 codes of one sign with a place of their own: eleven binades below the largest magnitude
 constexpr int kFew = 64;                 // the same of the first block's own selections
 constexpr int kMaxCluster = 8;
 constexpr int kMaxVocab = 1 << 18;
@@ -67,6 +70,8 @@ struct SampleArgs {
 struct Shared {
     union {
         u64 entry[kGather];              // the candidates of the row (first block)
+        uint32_t codes[2 * kSide];       // bf16: tokens of every code
+        double code_w[2 * kSide];        // and the weight of one
         struct { u64 mass[kBins], list[kList], list_w[kList]; } wide;
     };
     union {
@@ -78,9 +83,9 @@ struct Shared {
     u64 group[kMaxGroups];               // weight of every group of 32 pieces
     u64 scan[2 * kWarps];
     double root[32];                     // 2^(45 - j / 32)
-    u64 sum[2], all, total, thr, found;
+    u64 sum[2], all, total, thr, found, middle;
     uint32_t n_gather[2];                // candidates of the cluster (first block), of this row and of the one before
-    uint32_t top, least, id, lo, hi, n_cand, n_list, n_in, bin[2], mid[2];
+    uint32_t top, least, id, lo, hi, n_cand, n_list, n_in, bin[2], mid[2], want, ties;
 };
 
 __device__ __forceinline__ float value_of(float v) { return v; }
@@ -489,18 +494,196 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         const double x = distance(v);
         return x <= most || v == top ? weight(x) : (u64)0;
     };
+    // The entry of the `want`th token, in order of id, among those with these bits that are kept (the last one's if there are not so many).
+    auto tie_border = [&](uint32_t bits, u64 want) {
+        const u64 keep_thr = thr;
+        auto tie = [&](float v, int id) { return (u64)(bits_of(v) == bits && entry_of(bits, id) >= keep_thr); };
+        const int groups = (pieces + 31) / 32;
+        u64 mine_all = 0;
+        for (int g = warp; g < groups; g += kWarps) {
+            const int p = 32 * g + lane;
+            uint32_t x = 0;
+            if (p < pieces) {
+                float v[VN];
+                piece(p, v);
+#pragma unroll
+                for (int i = 0; i < VN; ++i) x += (uint32_t)tie(v[i], id0 + p * VN + i);
+            }
+            x = __reduce_add_sync(0xffffffffu, x);
+            if (lane == 0) { s.group[g] = x; mine_all += x; }
+        }
+        mine_all = block_sum(lane == 0 ? mine_all : 0, s.scan);
+        if (t == 0) s.total = mine_all;
+        cluster.sync();
+        u64 ties = 0;
+        for (int i = 0; i < C; ++i) ties += *cluster.map_shared_rank(&s.total, i);
+        locate(tie, min(want, ties) - 1, [&](u64 e) { *cluster.map_shared_rank(&s.thr, 0) = e; });
+        cluster.sync();
+        const u64 e = *cluster.map_shared_rank(&s.thr, 0);
+        cluster.sync();                                          // (s.total and s.thr may be written again)
+        return e;
+    };
     // (s.total is not written again before the next row's first meeting of the cluster)
     auto draw = [&](u64 total) { locate(kept, target_of(total), [&](u64 e) { emit(e, total); }); };
 
-    // ---- no filter
     u64 total = 0;
+    const float bottom = fmaxf(far, least);                      // (a masked token makes it `far`)
+    if constexpr (sizeof(T) == 2) {
+        // ---- bf16, not limited by top-k: codes.  Positive ones from the largest downwards, then negative ones up to the largest magnitude that is
+        // near; `code` numbers them in order of falling logit.
+        const int top_code = top > 0.f ? (int)(__float_as_uint(top) >> 16) : -1, low_mag = bottom < 0.f ? (int)(__float_as_uint(-bottom) >> 16) : -1;
+        constexpr int kLeast = kSide + 128;                      // (no subnormal values among them)
+        if (k == 0 && (top_p < 1.f || !(min_p > 0.f)) && (top_code < 0 || top_code >= kLeast) && (low_mag < 0 || low_mag >= kLeast) && top_code + low_mag >= 0) {
+            const int neg0 = 32768 - low_mag + 2 * kSide - 1;
+            // the place of a code (sign-extended), or -1: none of its own
+            auto code = [&](int x) {
+                const int b = x >= 0 ? top_code - x : x + neg0;
+                return (uint32_t)(b - (x < 0 ? kSide : 0)) < (uint32_t)kSide ? b : -1;
+            };
+            auto value_of_code = [&](int b) {
+                const uint32_t m = b < kSide ? (uint32_t)(top_code - b) : 0x8000u | (uint32_t)(low_mag - (2 * kSide - 1 - b));
+                return __uint_as_float(m << 16);
+            };
+            auto code_exists = [&](int b) { return b < kSide ? top_code >= 0 : low_mag >= 0; };
+            auto code_at = [&](const uint4& x, int i) {
+                const uint32_t w = i < 2 ? x.x : i < 4 ? x.y : i < 6 ? x.z : x.w;
+                return (i & 1) ? (int)w >> 16 : (int)(w << 16) >> 16;
+            };
+            const int groups = (pieces + 31) / 32;
+            bool search = false;                                 // the border is not on a code of its own
+            if (top_p < 1.f) {
+                for (int i = t; i < 2 * kSide; i += kThreads) s.codes[i] = 0;
+                if (t == 0) { s.all = s.middle = 0; s.bin[0] = 0xffffffffu; }
+                __syncthreads();
+                u64 middle = 0;                                  // weight of the logits without a place: nearer to 0 than all the others
+                for (int p = t; p < pieces; p += kThreads) {
+                    const uint4 x = raw_piece(p);
+                    uint32_t none = 0;
+#pragma unroll
+                    for (int i = 0; i < VN; ++i) {
+                        const int b = code(code_at(x, i));
+                        if (b >= 0) atomicAdd(&s.codes[b], 1u);
+                        else none |= 1u << i;
+                    }
+                    for (; none != 0; none &= none - 1) {
+                        const float v = value_of(slice[p * VN + __ffs(none) - 1]);
+                        if (near(v)) middle += weight(distance(v));
+                    }
+                }
+                if (middle != 0) atomicAdd(&s.middle, middle);
+                cluster.sync();
+                // exact cumulative weight over the codes
+                constexpr int kPer = (2 * kSide + kThreads - 1) / kThreads;
+                uint32_t n_of[kPer];
+                u64 w_of[kPer], sum = 0, all;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const int b = t * kPer + i;
+                    n_of[i] = 0;
+                    w_of[i] = 0;
+                    if (b < 2 * kSide && code_exists(b)) {
+                        for (int r = 0; r < C; ++r) n_of[i] += cluster.map_shared_rank(s.codes, r)[b];
+                        const float v = value_of_code(b);
+                        if (n_of[i] != 0 && near(v)) w_of[i] = weight(distance(v));
+                    }
+                    sum += n_of[i] * w_of[i];
+                }
+                u64 mid = 0;
+                for (int r = 0; r < C; ++r) mid += *cluster.map_shared_rank(&s.middle, r);
+                u64 cum = block_exclusive<u64>(sum, s.scan, all);
+                total = all + mid;
+                const u64 goal = share_of(total);
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const int b = t * kPer + i;
+                    const u64 before = cum + (b >= kSide ? mid : 0), here = n_of[i] * w_of[i];
+                    if (before < goal && before + here >= goal) {
+                        s.bin[0] = b;
+                        s.want = (uint32_t)((goal - before + w_of[i] - 1) / w_of[i]);
+                        s.ties = n_of[i];
+                    }
+                    cum += here;
+                }
+                __syncthreads();
+                search = s.bin[0] == 0xffffffffu;                // among the logits without a place
+                if (!search) {
+                    const uint32_t bits = bits_of(value_of_code((int)s.bin[0]));
+                    const uint32_t want = s.want, ties = s.ties;
+                    cluster.sync();                              // (the codes' counts have been read)
+                    thr = want < ties ? tie_border(bits, want) : entry_of(bits, kMaxVocab);
+                } else {
+                    cluster.sync();
+                }
+            }
+            if (!search) {
+                // weights by code; what is not kept weighs nothing
+                for (int b = t; b < 2 * kSide; b += kThreads) {
+                    double w = 0.0;
+                    if (code_exists(b)) {
+                        const float v = value_of_code(b);
+                        if (near(v) && (thr == 0 || bits_of(v) >= (uint32_t)(thr >> 32))) {
+                            const double x = distance(v);
+                            if (x <= most || v == top) w = weight_d(x);
+                        }
+                    }
+                    s.code_w[b] = w;
+                }
+                __syncthreads();
+                const float thr_v = thr != 0 ? value_of_entry(thr) : -kMost;
+                const int thr_id = thr != 0 ? id_of_entry(thr) : 0x7fffffff;
+                const Piece<T> test(thr_v);
+                u64 sums = 0;
+                for (int g = warp; g < groups; g += kWarps) {
+                    const int p = 32 * g + lane;
+                    double sum = 0.0;
+                    if (p < pieces) {
+                        const uint4 x = raw_piece(p);
+                        uint32_t rest = 0;                       // looked at one by one
+                        if (thr == 0) {
+#pragma unroll
+                            for (int i = 0; i < VN; ++i) {
+                                const int b = code(code_at(x, i));
+                                sum += s.code_w[max(b, 0)] * (b >= 0 ? 1.0 : 0.0);
+                                rest |= b < 0 ? 1u << i : 0u;
+                            }
+                        } else {
+                            rest = test.mask(x);
+                        }
+                        for (; rest != 0; rest &= rest - 1) {
+                            const int at = p * VN + __ffs(rest) - 1, b = code((int)reinterpret_cast<const int16_t*>(slice)[at]);
+                            const float v = value_of(slice[at]);
+                            if (v == thr_v && id0 + at > thr_id) continue;
+                            if (b >= 0) sum += s.code_w[b];
+                            else sum += (double)kept(v, id0 + at);
+                        }
+                    }
+                    u64 w = (u64)sum;
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+                    if (lane == 0) s.group[g] = w;
+                    sums += w;
+                }
+                sums = block_sum(lane == 0 ? sums : 0, s.scan);
+                if (t == 0) s.total = sums;
+                cluster.sync();
+                total = 0;
+                for (int i = 0; i < C; ++i) total += *cluster.map_shared_rank(&s.total, i);
+                draw(total);
+                return;
+            }
+            for (int i = t; i < kBins; i += kThreads) s.count[i] = 0;
+            __syncthreads();
+        }
+    }
+
+    // ---- no filter
     if (k == 0 && top_p == 1.f && !(min_p > 0.f)) {
         draw(weigh(std::false_type(), CUDART_INF));
         return;
     }
 
     // bins of distance, by a product that rises with it
-    const float bottom = fmaxf(far, least), span = top - bottom;                 // (a masked token makes it `far`)
+    const float span = top - bottom;
     const float inv = span > 1e-30f && span < 1e36f ? (float)kBins / span : 0.f;
     auto place = [&](float v) { return (top - v) * inv; };
     auto bin_of = [&](float v) { return min(kBins - 1, (int)place(v)); };
@@ -620,6 +803,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         if (lane == 0) { atomicAdd(&s.all, sum_all); atomicAdd(&s.total, sum_before); }
         const int m = send();
         u64 before = 0;
+        total = 0;
         for (int i = 0; i < C; ++i) {
             total += *cluster.map_shared_rank(&s.all, i);
             before += *cluster.map_shared_rank(&s.total, i);
@@ -867,32 +1051,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
             thr = *cluster.map_shared_rank(&s.thr, 0);
         } else if (lo == hi) {
             // equal logits: the first so many of them in order of id
-            const u64 w = measure(of_bits(lo)), keep_thr = thr;
-            const u64 want = goal > before + w ? (goal - before + w - 1) / w : 1;
-            auto tie = [&](float v, int id) { return (u64)(bits_of(v) == lo && entry_of(lo, id) >= keep_thr); };
-            const int groups = (pieces + 31) / 32;
-            u64 mine_all = 0, sum;
-            for (int g = warp; g < groups; g += kWarps) {
-                const int p = 32 * g + lane;
-                uint32_t x = 0;
-                if (p < pieces) {
-                    float v[VN];
-                    piece(p, v);
-#pragma unroll
-                    for (int i = 0; i < VN; ++i) x += (uint32_t)tie(v[i], id0 + p * VN + i);
-                }
-                x = __reduce_add_sync(0xffffffffu, x);
-                if (lane == 0) { s.group[g] = x; mine_all += x; }
-            }
-            __syncthreads();
-            block_exclusive<u64>(mine_all, s.scan, sum);
-            if (t == 0) s.total = sum;
-            cluster.sync();
-            u64 ties = 0;
-            for (int i = 0; i < C; ++i) ties += *cluster.map_shared_rank(&s.total, i);
-            locate(tie, min(want, ties) - 1, [&](u64 e) { *cluster.map_shared_rank(&s.thr, 0) = e; });
-            cluster.sync();
-            thr = *cluster.map_shared_rank(&s.thr, 0);
+            const u64 w = measure(of_bits(lo));
+            thr = tie_border(lo, goal > before + w ? (goal - before + w - 1) / w : 1);
         }
         cluster.sync();
     };

@@ -196,3 +196,37 @@ def test_frequencies_follow_the_weights():
     b.beagle_sample(z, u, tokens)
     share = torch.softmax(z[0].double(), 0) * n
     assert bool(((torch.bincount(tokens.long(), minlength=5).double() - share).abs() <= 1.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kind", ["negative", "positive", "zero top", "tiny", "mostly zero", "wide", "one value", "subnormal", "few codes"])
+def test_where_the_logits_lie(dtype, kind):
+    """All of one sign, around 0, of any size: codes of either sign, the logits nearest to 0, and rows whose border lies among those."""
+    v, g = 30000, torch.Generator(device="cuda").manual_seed(9)
+    z = torch.randn(10, v, generator=g, device="cuda")
+    small = torch.rand(10, v, generator=g, device="cuda")
+    z = {"negative": z.abs() * -3 - 0.5, "positive": z.abs() * 3, "zero top": torch.where(small < 0.01, 0.0, z.abs() * -2), "tiny": z * 1e-25, "mostly zero": torch.where(small < 0.02, z * 4, z * 1e-6),
+         "wide": z * torch.exp(small * 40 - 35), "one value": z * 0 - 1.5, "subnormal": z * 1e-39, "few codes": torch.randint(0, 5, (10, v), generator=g, device="cuda") * 1.0 - 2}[kind]
+    z = z.to(DT[dtype])
+    us = [0.0, 0.1, 0.2, 0.3, 0.4, 0.5, 0.6, 0.7, 0.9, 0.999]
+    if kind == "subnormal":                              # they count as 0: all equal
+        z = torch.where(z.float().abs() < 1.1754944e-38, torch.zeros_like(z), z)
+    check(z, us)
+    check(z, us, top_p=[0.001, 0.2, 0.4, 0.5, 0.6, 0.7, 0.8, 0.9, 0.99, 0.9999])
+    check(z, us, temperature=[0.2, 0.5, 1, 2, 5, 0.2, 0.5, 1, 2, 5], top_p=[0.5] * 10, min_p=[0.0, 0.5, 0.01, 0.9, 0.99, 0.001, 0.2, 0.7, 1e-6, 0.3])
+    check(z, us, temperature=[0.3] * 10, top_k=[1, 3, 10, 100, 1000, 5000, 20000, 29999, 0, 2], top_p=[0.7] * 10)
+    masked = torch.where(small < 0.7, torch.full_like(z, -math.inf), z)
+    check(masked, us, top_p=[0.9] * 5 + [1.0] * 5)
+
+
+def test_subnormal_logits_count_as_zero():
+    z = torch.zeros(1, 8, device="cuda")
+    z[0, 3], z[0, 5] = 1e-39, -1e-40
+    tokens = torch.empty(1, dtype=torch.int32, device="cuda")
+    for u, want in ((0.0, 0), (0.3, 2), (0.99, 7)):
+        b.beagle_sample(z, torch.tensor([u], device="cuda"), tokens)
+        assert tokens.item() == want
+    b.beagle_sample(z, torch.tensor([0.9], device="cuda"), tokens, top_k=torch.tensor([2], dtype=torch.int32, device="cuda"))
+    assert tokens.item() == 1
+    b.beagle_sample(z, torch.tensor([0.9], device="cuda"), tokens, temperature=torch.zeros(1, device="cuda"))
+    assert tokens.item() == 0
