@@ -573,19 +573,24 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                 if (middle != 0) atomicAdd(&s.middle, middle);
                 cluster.sync();
                 // exact cumulative weight over the codes
-                constexpr int kPer = (2 * kSide + kThreads - 1) / kThreads;
-                uint32_t n_of[kPer];
+                constexpr int kPer = 6;                          // of a thread
+                static_assert(kPer * kThreads >= 2 * kSide && 2 * kSide % 2 == 0, "all codes, in pairs");
+                uint32_t n_of[kPer] = {0, 0, 0, 0, 0, 0};
                 u64 w_of[kPer], sum = 0, all;
+                for (int r = 0; r < C; ++r) {
+                    const uint32_t* counts = cluster.map_shared_rank(s.codes, r);
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const int b = t * kPer + i;
-                    n_of[i] = 0;
-                    w_of[i] = 0;
-                    if (b < 2 * kSide && code_exists(b)) {
-                        for (int r = 0; r < C; ++r) n_of[i] += cluster.map_shared_rank(s.codes, r)[b];
-                        const float v = value_of_code(b);
-                        if (n_of[i] != 0 && near(v)) w_of[i] = weight(distance(v));
-                    }
+                    for (int i = 0; i < kPer; i += 2)
+                        if (t * kPer + i < 2 * kSide) {
+                            const uint2 x = *reinterpret_cast<const uint2*>(counts + t * kPer + i);
+                            n_of[i] += x.x;
+                            n_of[i + 1] += x.y;
+                        }
+                }
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {                 // (the arithmetic runs for codes that no token has, too)
+                    const float v = value_of_code(min(t * kPer + i, 2 * kSide - 1));
+                    w_of[i] = n_of[i] != 0 && near(v) ? weight(distance(n_of[i] != 0 && near(v) ? v : top)) : 0;
                     sum += n_of[i] * w_of[i];
                 }
                 u64 mid = 0;
