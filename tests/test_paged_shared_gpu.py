@@ -227,3 +227,58 @@ def test_sampling_from_a_forked_prompt(dtype):
         assert tokens.tolist() == check(logits, u.tolist(), temperature=[0.9] * B, top_k=[40] * B)
     assert cache.length.tolist() == [n0 + 25] * B and shared.tolist() == [n0 // ps * ps]
     assert len({tuple(r[n0 // ps:]) for r in cache.table.tolist()}) == B       # every sample has its own tail
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 64), ("fp32", 128)])
+def test_pools_past_32_bit_offsets(dtype, dh):
+    """Common and own pages at the end of pools of more than 2^31 elements."""
+    ps, hkv = 256, 2
+    n_pages = 2 ** 31 // (ps * hkv * dh) + 16
+    cache = b.PagedCache(n_pages, ps, hkv, dh, 5, 4, dtype)
+    lens = [600, 512, 700, 1000, 513]
+    g = torch.Generator(device="cuda").manual_seed(3)
+    free, table = list(range(n_pages - 1, n_pages - 14, -1)), [[-1] * 4 for _ in lens]
+    common = [free.pop(0), free.pop(0)]
+    for s, n in enumerate(lens):
+        for i in range(-(-n // ps)):
+            table[s][i] = common[i] if i < 2 else free.pop(0)
+    for p in {x for row in table for x in row if x >= 0}:
+        for pool in (cache.k, cache.v):
+            pool[p] = torch.randn(hkv, ps, dh, generator=g, device="cuda").to(DT[dtype])
+    cache.table.copy_(i32(table))
+    cache.length.copy_(i32(lens))
+    q = randn(5, 8, dh, dtype=dtype, seed=4)
+    attend(cache, [0, 1, 2, 3, 4], [5], i32([512]).cuda(), q, dtype)
+    shared = torch.empty(1, dtype=torch.int32, device="cuda")
+    b.beagle_pages_shared(cache, [0, 1, 2, 3, 4], [5], shared)
+    assert shared.tolist() == [512]
+
+
+def test_two_streams_and_two_graphs_at_once():
+    """Calls with workspaces of their own, on two streams and in two captured graphs, give what one alone gives."""
+    cache, shared = forked([20, 5], [900, 300], list(range(25)), 16, 2, 128, "bf16", 10)
+    groups, slots, sh = [20, 5], list(range(25)), i32(shared).cuda()
+    qs = [randn(25, 8, 128, dtype="bf16", seed=s) for s in (1, 2)]
+    want = [attend(cache, slots, groups, sh, q, "bf16") for q in qs]
+    n = b.beagle_paged_attn_shared_workspace_bytes(cache, 25, 8, groups)
+    ws, outs, graphs = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in qs], [torch.empty_like(q) for q in qs], []
+    torch.cuda.synchronize()
+    for q, w, o in zip(qs, ws, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            b.beagle_paged_attn_shared(cache, slots, groups, sh, q, o, ws=w)
+    streams = [torch.cuda.Stream() for _ in qs]
+    for _ in range(20):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, x) for o, x in zip(outs, want))
+
+
+def test_rows_behind_the_batch_stay():
+    cache, shared = forked([3, 2], [128, 64], [5, 6, 7, 8, 9], 16, 2, 64, "bf16", 11)
+    q = randn(9, 4, 64, dtype="bf16", seed=6)
+    out, lse = torch.full_like(q, 7.0), torch.full((9, 4), 7.0, device="cuda")
+    b.beagle_paged_attn_shared(cache, list(range(5)), [3, 2], i32(shared).cuda(), q[:5], out[:5], lse[:5])
+    assert bool((out[5:] == 7.0).all()) and bool((lse[5:] == 7.0).all()) and not bool((out[:5] == 7.0).all())

@@ -234,3 +234,64 @@ def test_queries_rotated_in_place_and_from_a_fused_projection():
     b.beagle_pages_append_rotary(cache, [1, 0], rot, k, v, None, None, dense, dense)
     assert torch.equal(out, dense)
     close(out.flatten(0, 1), *reference(rot, q.reshape(10, 4, 64), torch.arange(5).repeat(2)), "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_past_32_bit_offsets(dtype):
+    """Rows whose offsets pass 2^31 elements, in the input, the output, and both."""
+    far = 2 ** 30 + 64
+    big = torch.zeros(2 * far + 4096, dtype=DT[dtype], device="cuda")
+    rot = b.Rotary(64)
+    rows = torch.as_strided(big, (3, 2, 64), (far, 64, 1))
+    x = randn(3, 2, 64, dtype=dtype, seed=1)
+    rows.copy_(x)
+    out = torch.empty_like(x)
+    b.beagle_rotary_apply(rot, rows, out, pos0=5)
+    close(out, *reference(rot, x, torch.arange(5, 8)), dtype)
+    b.beagle_rotary_apply(rot, rows, rows, pos0=5)
+    assert torch.equal(rows, out) and int((big != 0).sum()) <= 3 * 128
+    del big
+
+
+def test_append_past_32_bit_offsets():
+    """Pools of more than 2^31 elements: keys and values land in the last pages, copies of shared pages come from there."""
+    rot = b.Rotary(128)
+    ps, hkv = 256, 8
+    n_pages = 2 ** 31 // (ps * hkv * 128) + 40
+    cache = new_cache(n_pages, ps, hkv, 128, 3, 6, "bf16")
+    cache.refs[: n_pages - 12] = 1                       # only the last pages are free
+    k, v = randn(1, 300, hkv, 128, dtype="bf16", seed=1), randn(1, 300, hkv, 128, dtype="bf16", seed=2)
+    ok = torch.zeros(1, dtype=torch.int32, device="cuda")
+    b.beagle_pages_append_rotary(cache, [0], rot, k, v, None, ok)
+    b.beagle_pages_fork(cache, [0], [1])
+    b.beagle_pages_append_rotary(cache, [1], rot, k[:, :5], v[:, :5], None, ok)
+    assert ok.item() == 1 and cache.length.tolist()[:2] == [300, 305]
+    for slot, n in ((0, 300), (1, 305)):
+        pages = [int(x) for x in cache.table[slot, :2]]
+        assert min(pages) >= n_pages - 12
+        got = torch.cat([cache.k[p] for p in pages], 1)[:, :n].transpose(0, 1)
+        src = torch.cat([k[0], k[0, :5]])[:n]
+        close(got, *reference(rot, src, torch.arange(n)), "bf16")
+        assert torch.equal(torch.cat([cache.v[p] for p in pages], 1)[:, :n].transpose(0, 1), torch.cat([v[0], v[0, :5]])[:n])
+    assert int(cache.table[0, 1]) != int(cache.table[1, 1])
+
+
+def test_a_damaged_table_stays_inside_the_pools():
+    """Page ids and lengths out of range: nothing outside the cache is touched, the other slot gets its rows."""
+    rot = b.Rotary(64)
+    cache = new_cache(12, 16, 2, 64, 3, 4, "bf16")
+    k, v = randn(2, 20, 2, 64, dtype="bf16", seed=1), randn(2, 20, 2, 64, dtype="bf16", seed=2)
+    b.beagle_pages_append_rotary(cache, [0, 1], rot, k, v)
+    cache.table[0, 1] = 2 ** 31 - 1
+    cache.length[2] = 2 ** 31 - 1
+    cache.table[2, 3] = -9
+    ok = torch.zeros(3, dtype=torch.int32, device="cuda")
+    q = randn(3, 4, 4, 64, dtype="bf16", seed=3)
+    out = torch.zeros_like(q)
+    k, v = randn(3, 4, 2, 64, dtype="bf16", seed=4), randn(3, 4, 2, 64, dtype="bf16", seed=5)
+    b.beagle_pages_append_rotary(cache, [0, 2, 1], rot, k, v, None, ok, q, out)
+    torch.cuda.synchronize()
+    assert ok.tolist()[1:] == [0, 1]
+    page = int(cache.table[1, 1])
+    close(cache.k[page, :, 4:8].transpose(0, 1), *reference(rot, k[2], torch.arange(20, 24)), "bf16")
+    close(out[2], *reference(rot, q[2], torch.arange(20, 24)), "bf16")

@@ -230,3 +230,69 @@ def test_subnormal_logits_count_as_zero():
     assert tokens.item() == 1
     b.beagle_sample(z, torch.tensor([0.9], device="cuda"), tokens, temperature=torch.zeros(1, device="cuda"))
     assert tokens.item() == 0
+
+
+def test_many_rows_past_32_bit_offsets():
+    """17000 rows of 128256 (2.2e9 logits): the blocks walk over the rows; each row's token is its own peak, its neighbours' NaN do not reach it."""
+    rows, v = 17000, 128256
+    z = torch.zeros(rows, v, dtype=torch.bfloat16, device="cuda")
+    peak = torch.randint(0, v, (rows,), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    z.scatter_(1, peak[:, None], 40.0)
+    z[::7] = float("nan")
+    tokens, u = torch.empty(rows, dtype=torch.int32, device="cuda"), torch.rand(rows, device="cuda")
+    b.beagle_sample(z, u, tokens)
+    want = peak.to(torch.int32)
+    want[::7] = -1
+    assert torch.equal(tokens, want)
+    b.beagle_sample(z, u, tokens, top_k=torch.full((rows,), 5, dtype=torch.int32, device="cuda"), top_p=torch.full((rows,), 0.5, device="cuda"))
+    assert torch.equal(tokens, want)
+
+
+def test_two_streams_at_once():
+    z = noise(100, 50000, 3.0, "fp32", 12)
+    p = params(100, 3, 50000)
+    want = check(z, **p)
+    dev = lambda x, dt: torch.tensor(x, dtype=dt, device="cuda")
+    args = dict(temperature=dev(p["temperature"], torch.float32), top_k=dev(p["top_k"], torch.int32), top_p=dev(p["top_p"], torch.float32), min_p=dev(p["min_p"], torch.float32))
+    u = dev(p["u"], torch.float32)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in range(3)], []
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                t = torch.empty(100, dtype=torch.int32, device="cuda")
+                b.beagle_sample(z, u, t, **args)
+                outs.append(t)
+    torch.cuda.synchronize()
+    assert all(t.tolist() == want for t in outs)
+
+
+def test_refusals_of_the_binding():
+    z, u, t = torch.zeros(3, 10, device="cuda"), torch.zeros(3, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    for bad in (dict(logits=z.double()), dict(logits=z[0]), dict(logits=z.t()), dict(logits=z.cpu()), dict(u=u[:2]), dict(u=u.double()), dict(tokens=t.long()), dict(tokens=t.cpu()),
+                dict(temperature=u.cpu()), dict(top_k=u), dict(top_p=t), dict(logp=t)):
+        a = dict(logits=z, u=u, tokens=t)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            b.beagle_sample(**a)
+    with pytest.raises(b.BeagleError):
+        b.beagle_sample(torch.zeros(1, 2 ** 18 + 1, device="cuda"), u[:1], t[:1])
+    b.beagle_sample(z[:0], u[:0], t[:0])                 # no rows: nothing to do
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_drafts_for_acceptance_under_sampling(dtype):
+    """Tokens drawn with beagle_sample from the draft's own distribution, then beagle_verify_sample: with equal draft and target logits every
+    draft is accepted, and the extra token is the one that beagle_sample draws from the same numbers."""
+    from paper_2505_24544_b200 import workloads as WL
+    from paper_2505_24544_b200.binding import BeagleHead
+    w = WL.WORKLOADS["c1_tiny_fp32"]
+    head = BeagleHead.from_workload(w, WL.make_weights(w), device="cuda:0")
+    gamma, B, v = 3, 4, w.vocab
+    z = noise(B * (gamma + 1), v, 2.0, dtype, 5).view(B, gamma + 1, v)
+    u = torch.rand(B, gamma + 1, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    temp = torch.full((B * (gamma + 1),), 0.8, device="cuda")
+    tokens, _ = head.sample(z.view(-1, v), u.view(-1), temperature=temp)
+    drafts = tokens.view(B, gamma + 1)
+    accept, out = head.verify_sample(drafts[:, :gamma].contiguous(), z[:, :gamma].float().transpose(0, 1).contiguous(), z, torch.rand(B, gamma, device="cuda"), u[:, gamma].contiguous(), 0.8)
+    assert accept.tolist() == [gamma] * B and torch.equal(out, drafts)
