@@ -19,6 +19,10 @@
 // G * 4 flop per 4 bytes next to unpacking at memory speed.
 // Other types and widths: paged_attn_simt_kernel, the same ring in front of the CUDA cores.
 //
+// beagle_paged_attn_shared, rows in groups with a common part, walks entries (paged_attn.cuh) in place of rows: here with the same two kernels if all
+// groups are small or the type is not the tensor cores', else in paged_grouped.cu; paged_shared_join_kernel adds up what the runs leave of a
+// row's own positions and of its group's common part, one (row, head) to four warps, the runs in order.
+//
 // Measured: 32 sequences of 512 to 8192, 32 heads over 8 of 128: 103 us of stream (5.8 to 6.0 TB/s of cache) and 5 us of join; 16
 // sequences of 65000 to 131072: 1012 us, the rate of a plain copy; the smallest fp32 call: 4 us on the GPU.  fp32, 32 sequences of 2000,
 // 8 K/V heads of 128 (524 MB): 111 us with one query head each, 118 with four, 142 with eight (loading straight into registers, without the
@@ -750,7 +754,8 @@ beagle_status check_groups(int batch, int n_groups, const int32_t* group_rows) {
 }
 
 // Groups with more query rows than this (rows times grouped heads) have their common part on the tensor cores' 128-row tiles, the others in
-// entries of eight rows.
+// entries of eight rows, the rows of an mma.sync product.  Measured as entries / on the tensor cores, us, heads of 128, 8 K/V heads: 8 groups
+// of 2 query rows over 4096 positions 43 / 49, of 8 47 / 53, 7 groups of 9 66 / 49, one group of 8 over 16384 40 / 38, of 9 49 / 38.
 constexpr int kFewRows = 8;
 
 // Query rows of a common part's entry: what the kernel takes as grouped heads.

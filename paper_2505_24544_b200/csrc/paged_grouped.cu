@@ -1,15 +1,23 @@
-// The common part of groups of rows whose slots begin with the same positions (beagle_paged_attn_shared), on the tensor cores.
+// Attention of groups of rows whose slots begin with the same positions (beagle_paged_attn_shared) where the groups are large enough for the
+// tensor cores: one launch for the common parts, on tcgen05, and for what each row has behind them (paged_rows.cuh, mma.sync).
 //
-// The query rows of a group (rows times grouped heads) that read one K/V head are the 128 rows of a tcgen05 tile, so each cached tile is
-// read once for all of them: R G flop per byte, memory-bound up to some 200 query rows, bound by the softmax between the products after that.
-// The tiles of 64 positions of all (block of query rows, K/V head) pairs, one after the other, are cut into equal runs on the device, one
-// per CTA, two CTAs per SM (paged_attn.cuh); a run leaves one partial per pair that it touches (O in fp32, not normalised, with the
-// maximum and sum of each row), which the join launch adds to what the rows see behind the common part, in a fixed order.
+// Common part: the query rows of a group (rows times grouped heads) that read one K/V head are the 128 rows of a tcgen05 tile, so each
+// cached tile is read once for all of them: R G flop per byte, memory-bound up to some 200 query rows, then bound by the softmax between the products.
+// The tiles of 64 positions of all (block of query rows, K/V head) pairs, one after the other, are cut into equal runs on the device
+// (paged_attn.cuh); a run leaves one partial per pair that it touches (O in fp32, not normalised, with the maximum and sum of each row),
+// which the join launch adds to what the rows see behind the common part, in a fixed order.
 //
-// One CTA: a producer warp (pages by TMA, 128-byte swizzle, two stages of K and V; the queries of the block as one box of a
+// Two CTAs per SM, each with one kind of work, shared out by the tiles, the kinds side by side as far as possible: common parts wait
+// for the hand-over between softmax and products, rows for memory.  Measured: 32 rows over 8192 common positions, 32/8 heads of 128, some hundred
+// positions behind: 30 us with the join (the two kinds in launches of their own 38); four groups of 16 rows, 32/32 heads: 81 us; 64 rows over
+// 65536, up to 8192 behind: 146 us (all CTAs first one kind, then the other: 167); alone the common parts run at 207 tiles a microsecond
+// (868 TFLOP/s with 128 query rows, half of the tensor cores' rate) and the rows at 5.8 TB/s.
+//
+// A common part's CTA: a producer warp (pages by TMA, 128-byte swizzle, two stages of K and V; the queries of the block as one box of a
 // [row, head, component] map), a warp that issues the products, and four warps with one thread per query row: S = Q K^T into tensor memory ->
 // P = exp2(S - m) in bf16 over S -> O += P V with P as the tensor-memory operand.  m is the row's reference point, moved only when a tile
-// exceeds it by more than 2^8.  S is double-buffered.  All positions of the common part are visible: nothing is masked.
+// exceeds it by more than 2^8.  S is double-buffered.  All positions of the common part are visible: nothing is masked.  P is rounded to
+// bf16 because the product takes both operands in one type; its row sum is of the unrounded weights, in fp32.
 #include <cuda.h>
 
 #include "paged_rows.cuh"
@@ -21,7 +29,6 @@ namespace {
 
 constexpr int kThreads = 192;            // warp 0: TMA producer, warp 1: issues the products, warps 2-5: softmax
 constexpr int kRows = 128;               // query rows of a tile
-constexpr float kPrefixCost = 6.f, kRowsCost = 5.f;      // of a tile
 
 template <int DH>
 struct PrefixSmem {
@@ -266,11 +273,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_grouped_kernel(const __grid
     build_schedules(rows, s_rows, prefix, s_prefix);
     fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-    // The CTAs do one kind of work each, shared out by what a tile of it takes (kPrefixCost : kRowsCost; an SM does 1.4 and 1.2 tiles a microsecond), the two
-    // kinds side by side on an SM as far as possible: one waits for memory, the other for the products.
+    // The CTAs do one kind of work each, shared out by its tiles, the two kinds side by side on an SM as far as possible: one waits for
+    // memory, the other for the products.  64 rows over 65536: 146 us; with a common part's tile counted as 0.8, 1.2 and 1.4 of a row's 159, 151, 172.
     const int total_p = s_prefix.start[SharedArgs::kEntries], total_r = s_rows.start[SharedArgs::kEntries], n = (int)gridDim.x;
-    const float cost_p = (float)total_p * kPrefixCost, cost_r = (float)total_r * kRowsCost;
-    int n_prefix = total_p + total_r > 0 ? (int)((float)n * cost_p / (cost_p + cost_r) + 0.5f) : 0;
+    int n_prefix = total_p > 0 || total_r > 0 ? (int)((float)n * (float)total_p / ((float)total_p + (float)total_r) + 0.5f) : 0;
     if (total_p > 0) n_prefix = max(n_prefix, 1);
     if (total_r > 0) n_prefix = min(n_prefix, n - 1);
     const int half = (n + 1) / 2, at = (int)blockIdx.x < half ? 2 * (int)blockIdx.x : 2 * ((int)blockIdx.x - half) + 1;       // neighbours share an SM

@@ -7,7 +7,8 @@
 // bound by memory bandwidth (16-byte loads and stores, four in flight per thread).
 //
 // Measured: prompts of up to 8192 tokens for 8 sequences (370 MB moved) 64 us, book-keeping before it 6; copy of 16 serving
-// sequences 63 us (6.5 TB/s), its book-keeping 9.
+// sequences 63 us (6.5 TB/s), its book-keeping 9.  The append that rotates (beagle_pages_append_rotary): eight prompts of up to 8192 tokens (367 MB
+// read and written) 77 us with the book-keeping; with the first loads behind the cosines and sines, and 2 CTAs per SM, 90.
 //
 // Every index that comes from device memory (table entries, lengths, counts) is clamped or range-checked before it is used, so
 // a damaged table yields wrong contents but no access outside the caller's buffers.
