@@ -42,6 +42,7 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kBins = 2048, kPerThread = kBins / kThreads;
 constexpr int kMassBins = 1024;          // of the first block's selections
 constexpr int kGather = 3500;            // candidates that the first block finishes alone
+constexpr int kPairs = 256;              // candidates that it compares pairwise, a thread each
 constexpr int kList = kThreads;          // tokens that a block compares pairwise (the cluster's search)
 constexpr int kSide = 1408;              // bf16 codes of one sign with a place of their own: eleven binades below the largest magnitude
 constexpr int kFew = 64;                 // the same of the first block's own selections
@@ -83,7 +84,7 @@ struct Shared {
     u64 group[kMaxGroups];               // weight of every group of 32 pieces
     u64 scan[2 * kWarps];
     double root[32];                     // 2^(45 - j / 32)
-    u64 sum[2], all, total, thr, found, middle;
+    u64 sum[2], all, all_n, total, thr, found, middle, middle_n;
     uint32_t n_gather[2];                // candidates of the cluster (first block), of this row and of the one before
     uint32_t top, least, id, lo, hi, n_cand, n_list, n_in, bin[2], mid[2], want, ties;
 };
@@ -338,15 +339,19 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
     }
     cluster.sync();
     {
-        uint32_t hi = 0, lo = 0xffffffffu;
-        for (int i = 0; i < C; ++i) {
-            hi = max(hi, *cluster.map_shared_rank(&s.top, i));
-            lo = min(lo, *cluster.map_shared_rank(&s.least, i));
-        }
-        top = of_bits(hi);
-        least = of_bits(lo);
+        const uint32_t hi = lane < C ? *cluster.map_shared_rank(&s.top, lane) : 0, lo = lane < C ? *cluster.map_shared_rank(&s.least, lane) : 0xffffffffu;
+        top = of_bits(__reduce_max_sync(0xffffffffu, hi));
+        least = of_bits(__reduce_min_sync(0xffffffffu, lo));
         if (t == 0) s.n_gather[parity ^ 1] = 0;                  // everyone has read the last row's
     }
+
+    // Sum of a word of the blocks' shared memory over the cluster, or over the blocks in front of `end`; whole warps, a lane reads a block's.
+    auto sum_lanes = [&](u64 x) {
+#pragma unroll
+        for (int o = kMaxCluster / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        return __shfl_sync(0xffffffffu, x, 0);
+    };
+    auto cluster_sum = [&](u64* x, int end) { return sum_lanes(lane < end ? *cluster.map_shared_rank(x, lane) : 0); };
 
     const bool drawn = temp_bits - 1u < 0x7f800000u;             // temperature above 0, infinity included
     if (top_p <= 0.f || min_p > 1.f) k = 1;                      // only the first
@@ -436,30 +441,18 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         block_exclusive<u64>(lane == 0 ? all : 0, s.scan, total);
         if (t == 0) s.total = total;
         cluster.sync();
-        total = 0;
-        for (int i = 0; i < C; ++i) total += *cluster.map_shared_rank(&s.total, i);
-        return total;
+        return cluster_sum(&s.total, C);
     };
-    // Smallest id whose cumulative measure exceeds the target (below the total).  s.group holds the groups' sums and s.total the block's;
-    // measure(value, id) as they were formed.  The thread that has the token calls hit(its entry).
-    auto locate = [&](auto measure, u64 target, auto hit) {
-        u64 before = 0, sum;
-        for (int i = 0; i < rank; ++i) before += *cluster.map_shared_rank(&s.total, i);
-        if (target < before || target >= before + s.total) return;               // (the same for the whole block)
-        const int groups = (pieces + 31) / 32;
-        const u64 mine = t < groups ? s.group[t] : 0;
-        before += block_exclusive<u64>(mine, s.scan, sum);
-        const uint32_t owner = __ballot_sync(0xffffffffu, before <= target && target < before + mine);
-        if (owner == 0) return;
-        const int l = __ffs(owner) - 1, p = 32 * (warp * 32 + l) + lane;         // one warp: a lane takes a piece
-        const u64 start = __shfl_sync(0xffffffffu, before, l);
-        float v[VN];
-        u64 w[VN], all = 0;
+    auto values = [&](int p, float* v) {                         // of a piece, or of none
 #pragma unroll
         for (int i = 0; i < VN; ++i) v[i] = -CUDART_INF_F;
         if (p < pieces) piece(p, v);
+    };
+    // A warp with a group's pieces, one a lane, their measures and what lies before them: the first token at which the target is exceeded.
+    auto within = [&](int p, const float* v, const u64* w, u64 start, u64 target, auto hit) {
+        u64 all = 0;
 #pragma unroll
-        for (int i = 0; i < VN; ++i) all += w[i] = measure(v[i], id0 + p * VN + i);
+        for (int i = 0; i < VN; ++i) all += w[i];
         u64 incl = all;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -475,6 +468,24 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                 if (!found && cum > target) { found = true; hit(entry_of(bits_of(v[i]), id0 + p * VN + i)); }
             }
         }
+    };
+    // Smallest id whose cumulative measure exceeds the target (below the total).  s.group holds the groups' sums and s.total the block's;
+    // measure(value, id) as they were formed.  The thread that has the token calls hit(its entry).
+    auto locate = [&](auto measure, u64 target, auto hit) {
+        u64 before = cluster_sum(&s.total, rank), sum;
+        if (target < before || target >= before + s.total) return;               // (the same for the whole block)
+        const int groups = (pieces + 31) / 32;
+        const u64 mine = t < groups ? s.group[t] : 0;
+        before += block_exclusive<u64>(mine, s.scan, sum);
+        const uint32_t owner = __ballot_sync(0xffffffffu, before <= target && target < before + mine);
+        if (owner == 0) return;
+        const int l = __ffs(owner) - 1, p = 32 * (warp * 32 + l) + lane;         // one warp: a lane takes a piece
+        float v[VN];
+        u64 w[VN];
+        values(p, v);
+#pragma unroll
+        for (int i = 0; i < VN; ++i) w[i] = measure(v[i], id0 + p * VN + i);
+        within(p, v, w, __shfl_sync(0xffffffffu, before, l), target, hit);
     };
     auto emit = [&](u64 e, u64 total) {
         a.tokens[row] = id_of_entry(e);
@@ -515,8 +526,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         mine_all = block_sum(lane == 0 ? mine_all : 0, s.scan);
         if (t == 0) s.total = mine_all;
         cluster.sync();
-        u64 ties = 0;
-        for (int i = 0; i < C; ++i) ties += *cluster.map_shared_rank(&s.total, i);
+        const u64 ties = cluster_sum(&s.total, C);
         locate(tie, min(want, ties) - 1, [&](u64 e) { *cluster.map_shared_rank(&s.thr, 0) = e; });
         cluster.sync();
         const u64 e = *cluster.map_shared_rank(&s.thr, 0);
@@ -533,7 +543,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         // near; `code` numbers them in order of falling logit.
         const int top_code = top > 0.f ? (int)(__float_as_uint(top) >> 16) : -1, low_mag = bottom < 0.f ? (int)(__float_as_uint(-bottom) >> 16) : -1;
         constexpr int kLeast = kSide + 128;                      // (no subnormal values among them)
-        if (k == 0 && (top_p < 1.f || !(min_p > 0.f)) && (top_code < 0 || top_code >= kLeast) && (low_mag < 0 || low_mag >= kLeast) && top_code + low_mag >= 0) {
+        if ((k == 0 || k > kPairs) && (top_p < 1.f || !(min_p > 0.f)) && (top_code < 0 || top_code >= kLeast) && (low_mag < 0 || low_mag >= kLeast) && top_code + low_mag >= 0) {
             const int neg0 = 32768 - low_mag + 2 * kSide - 1;
             // the place of a code (sign-extended), or -1: none of its own
             auto code = [&](int x) {
@@ -549,13 +559,14 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                 const uint32_t w = i < 2 ? x.x : i < 4 ? x.y : i < 6 ? x.z : x.w;
                 return (i & 1) ? (int)w >> 16 : (int)(w << 16) >> 16;
             };
+            static_assert(kSide % kMaxCluster == 0, "shares of the codes");
             const int groups = (pieces + 31) / 32;
-            bool search = false;                                 // the border is not on a code of its own
-            if (top_p < 1.f) {
+            bool cuts = false, search = false;                                 // the border is not on a code of its own
+            if (top_p < 1.f || k > 0) {
                 for (int i = t; i < 2 * kSide; i += kThreads) s.codes[i] = 0;
-                if (t == 0) { s.all = s.middle = 0; s.bin[0] = 0xffffffffu; }
+                if (t == 0) { s.middle = s.middle_n = s.found = 0; s.bin[0] = 0xffffffffu; }
                 __syncthreads();
-                u64 middle = 0;                                  // weight of the logits without a place: nearer to 0 than all the others
+                u64 middle = 0, middle_n = 0;                    // weight and number of the logits without a place: nearer to 0 than all the others
                 for (int p = t; p < pieces; p += kThreads) {
                     const uint4 x = raw_piece(p);
                     uint32_t none = 0;
@@ -567,58 +578,88 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                     }
                     for (; none != 0; none &= none - 1) {
                         const float v = value_of(slice[p * VN + __ffs(none) - 1]);
-                        if (near(v)) middle += weight(distance(v));
+                        if (near(v)) { middle += weight(distance(v)); ++middle_n; }
                     }
                 }
-                if (middle != 0) atomicAdd(&s.middle, middle);
+                if (middle_n != 0) { atomicAdd(&s.middle, middle); atomicAdd(&s.middle_n, middle_n); }
                 cluster.sync();
-                // exact cumulative weight over the codes
-                constexpr int kPer = 6;                          // of a thread
-                static_assert(kPer * kThreads >= 2 * kSide && 2 * kSide % 2 == 0, "all codes, in pairs");
-                uint32_t n_of[kPer] = {0, 0, 0, 0, 0, 0};
-                u64 w_of[kPer], sum = 0, all;
-                for (int r = 0; r < C; ++r) {
-                    const uint32_t* counts = cluster.map_shared_rank(s.codes, r);
+                // exact cumulative weight over the codes: a block takes as many of them as the others, a thread q
+                const int share = 2 * kSide / C, q = (share + kThreads - 1) / kThreads;          // (kSide is a multiple of the cluster's size)
+                const int b0 = rank * share + min(t * q, share), b1 = rank * share + min(t * q + q, share);
+                // near tokens of a code, and the weight of one
+                auto of_code = [&](int b, uint32_t& n) {
+                    n = 0;
+                    for (int r = 0; r < C; r += 4) {             // (four on their way at once)
+                        uint32_t x[4];
 #pragma unroll
-                    for (int i = 0; i < kPer; i += 2)
-                        if (t * kPer + i < 2 * kSide) {
-                            const uint2 x = *reinterpret_cast<const uint2*>(counts + t * kPer + i);
-                            n_of[i] += x.x;
-                            n_of[i + 1] += x.y;
-                        }
-                }
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) {                 // (the arithmetic runs for codes that no token has, too)
-                    const float v = value_of_code(min(t * kPer + i, 2 * kSide - 1));
-                    w_of[i] = n_of[i] != 0 && near(v) ? weight(distance(n_of[i] != 0 && near(v) ? v : top)) : 0;
-                    sum += n_of[i] * w_of[i];
-                }
-                u64 mid = 0;
-                for (int r = 0; r < C; ++r) mid += *cluster.map_shared_rank(&s.middle, r);
-                u64 cum = block_exclusive<u64>(sum, s.scan, all);
-                total = all + mid;
-                const u64 goal = share_of(total);
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const int b = t * kPer + i;
-                    const u64 before = cum + (b >= kSide ? mid : 0), here = n_of[i] * w_of[i];
-                    if (before < goal && before + here >= goal) {
-                        s.bin[0] = b;
-                        s.want = (uint32_t)((goal - before + w_of[i] - 1) / w_of[i]);
-                        s.ties = n_of[i];
+                        for (int y = 0; y < 4; ++y) x[y] = r + y < C ? cluster.map_shared_rank(s.codes, r + y)[b] : 0;
+                        n += x[0] + x[1] + x[2] + x[3];
                     }
-                    cum += here;
+                    const float v = value_of_code(b);
+                    if (!near(v)) n = 0;
+                    return n != 0 ? weight(distance(v)) : 0;
+                };
+                u64 sum = 0, all;
+                uint32_t sum_n = 0, all_n;
+#pragma unroll 1
+                for (int b = b0; b < b1; ++b) {
+                    uint32_t n;
+                    const u64 w = of_code(b, n);
+                    sum += n * w;
+                    sum_n += n;
                 }
-                __syncthreads();
-                search = s.bin[0] == 0xffffffffu;                // among the logits without a place
-                if (!search) {
-                    const uint32_t bits = bits_of(value_of_code((int)s.bin[0]));
-                    const uint32_t want = s.want, ties = s.ties;
-                    cluster.sync();                              // (the codes' counts have been read)
-                    thr = want < ties ? tie_border(bits, want) : entry_of(bits, kMaxVocab);
-                } else {
+                const u64 mid = cluster_sum(&s.middle, C);
+                const uint32_t mid_n = (uint32_t)cluster_sum(&s.middle_n, C);
+                u64 cum = block_exclusive<u64>(sum, s.scan, all);
+                uint32_t cum_n = block_exclusive<uint32_t>(sum_n, s.scan, all_n);
+                if (t == 0) { s.all = all; s.all_n = all_n; }
+                cluster.sync();
+                cum += cluster_sum(&s.all, rank);
+                cum_n += (uint32_t)cluster_sum(&s.all_n, rank);
+                total = cluster_sum(&s.all, C) + mid;
+                all_n = (uint32_t)cluster_sum(&s.all_n, C) + mid_n;
+                // f(code, its tokens, the weight of one, weight and tokens before), of this thread's codes
+                auto for_codes = [&](auto f) {
+                    u64 c = cum;
+                    uint32_t c_n = cum_n;
+#pragma unroll 1
+                    for (int b = b0; b < b1; ++b) {
+                        uint32_t n;
+                        const u64 w = of_code(b, n);
+                        f(b, n, w, c + (b >= kSide ? mid : 0), c_n + (b >= kSide ? mid_n : 0));
+                        c += n * w;
+                        c_n += n;
+                    }
+                };
+                auto border = [&](int b, uint32_t want) {
+                    for (int r = 0; r < C; ++r) {
+                        *cluster.map_shared_rank(&s.bin[0], r) = b;
+                        *cluster.map_shared_rank(&s.want, r) = want;
+                    }
+                };
+                const uint32_t most_n = k > 0 && (uint32_t)k < all_n ? (uint32_t)k : 0xffffffffu;
+                cuts = top_p < 1.f || most_n != 0xffffffffu;
+                if (most_n != 0xffffffffu) {                     // top-k's border; top-p is a share of what is in front of it
+                    if (cum_n < most_n && cum_n + sum_n + mid_n >= most_n)
+                        for_codes([&](int b, uint32_t n, u64 w, u64 before, uint32_t before_n) {
+                            if (before_n >= most_n || before_n + n < most_n) return;
+                            if (top_p == 1.f) border(b, most_n - before_n);
+                            for (int r = 0; r < C; ++r) *cluster.map_shared_rank(&s.found, r) = before + (most_n - before_n) * w;
+                        });
                     cluster.sync();
+                    total = s.found;                             // (0: it lies among the logits without a place)
                 }
+                if (top_p < 1.f && total != 0) {
+                    const u64 goal = share_of(total);
+                    if (cum < goal && cum + sum + mid >= goal)
+                        for_codes([&](int b, uint32_t n, u64 w, u64 before, uint32_t before_n) {
+                            const uint32_t there = min(n, most_n - min(most_n, before_n));
+                            if (before < goal && before + there * w >= goal) border(b, (uint32_t)((goal - before + w - 1) / w));
+                        });
+                }
+                cluster.sync();                                  // (and the codes' counts have been read)
+                search = cuts && s.bin[0] == 0xffffffffu;        // among the logits without a place
+                if (cuts && !search) thr = entry_of(bits_of(value_of_code((int)s.bin[0])), kMaxVocab);
             }
             if (!search) {
                 // weights by code; what is not kept weighs nothing
@@ -634,13 +675,16 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                     s.code_w[b] = w;
                 }
                 __syncthreads();
+                // the border's tokens, of which the first s.want in order of id are kept, are counted apart
                 const float thr_v = thr != 0 ? value_of_entry(thr) : -kMost;
-                const int thr_id = thr != 0 ? id_of_entry(thr) : 0x7fffffff;
                 const Piece<T> test(thr_v);
+                uint16_t* ties = s.cand;                         // of every group
                 u64 sums = 0;
+                uint32_t tie_sums = 0;
                 for (int g = warp; g < groups; g += kWarps) {
                     const int p = 32 * g + lane;
                     double sum = 0.0;
+                    uint32_t n_ties = 0;
                     if (p < pieces) {
                         const uint4 x = raw_piece(p);
                         uint32_t rest = 0;                       // looked at one by one
@@ -657,23 +701,83 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                         for (; rest != 0; rest &= rest - 1) {
                             const int at = p * VN + __ffs(rest) - 1, b = code((int)reinterpret_cast<const int16_t*>(slice)[at]);
                             const float v = value_of(slice[at]);
-                            if (v == thr_v && id0 + at > thr_id) continue;
-                            if (b >= 0) sum += s.code_w[b];
+                            if (v == thr_v) ++n_ties;
+                            else if (b >= 0) sum += s.code_w[b];
                             else sum += (double)kept(v, id0 + at);
                         }
                     }
                     u64 w = (u64)sum;
 #pragma unroll
                     for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-                    if (lane == 0) s.group[g] = w;
+                    if (thr != 0) n_ties = __reduce_add_sync(0xffffffffu, n_ties);
+                    if (lane == 0) { s.group[g] = w; ties[g] = (uint16_t)n_ties; }
                     sums += w;
+                    tie_sums += n_ties;
                 }
                 sums = block_sum(lane == 0 ? sums : 0, s.scan);
                 if (t == 0) s.total = sums;
+                auto by_code = [&](float v, int id) {
+                    const int b = code((int)__float_as_uint(v) >> 16);
+                    return b >= 0 ? (u64)s.code_w[b] : kept(v, id);
+                };
+                if (thr == 0) {
+                    cluster.sync();
+                    total = cluster_sum(&s.total, C);
+                    locate(by_code, target_of(total), [&](u64 e) { emit(e, total); });
+                    return;
+                }
+                const uint32_t here = (uint32_t)block_sum(lane == 0 ? tie_sums : 0, s.scan), want = s.want;
+                const u64 w_tie = (u64)s.code_w[s.bin[0]];       // (0 where min-p excludes it)
+                if (t == 0) s.ties = here;
                 cluster.sync();
-                total = 0;
-                for (int i = 0; i < C; ++i) total += *cluster.map_shared_rank(&s.total, i);
-                draw(total);
+                auto kept_ties = [&](uint32_t before, uint32_t n) { return min(n, want - min(want, before)); };
+                u64 start, mine;
+                uint32_t ties_start;
+                {                                                // a lane does a block's
+                    const uint32_t y = lane < C ? *cluster.map_shared_rank(&s.ties, lane) : 0;
+                    u64 x = lane < C ? *cluster.map_shared_rank(&s.total, lane) : 0;
+                    uint32_t before = y;
+#pragma unroll
+                    for (int o = 1; o < kMaxCluster; o <<= 1) {
+                        const uint32_t z = __shfl_up_sync(0xffffffffu, before, o);
+                        if (lane >= o) before += z;
+                    }
+                    before -= y;
+                    x += kept_ties(before, y) * w_tie;
+                    total = sum_lanes(x);
+                    start = sum_lanes(lane < rank ? x : 0);
+                    mine = __shfl_sync(0xffffffffu, x, rank);
+                    ties_start = __shfl_sync(0xffffffffu, before, rank);
+                }
+                const u64 target = target_of(total);
+                if (target < start || target >= start + mine) return;            // (the same for the whole block)
+                const uint32_t y = t < groups ? ties[t] : 0;
+                uint32_t unused;
+                ties_start += block_exclusive<uint32_t>(y, s.scan, unused);
+                const u64 x = t < groups ? s.group[t] + kept_ties(ties_start, y) * w_tie : 0;
+                start += block_exclusive<u64>(x, s.scan, mine);
+                const uint32_t owner = __ballot_sync(0xffffffffu, start <= target && target < start + x);
+                if (owner == 0) return;
+                const int l = __ffs(owner) - 1, p = 32 * (warp * 32 + l) + lane;
+                float v[VN];
+                u64 w[VN];
+                values(p, v);
+                uint32_t n_ties = 0;
+#pragma unroll
+                for (int i = 0; i < VN; ++i) n_ties += v[i] == thr_v ? 1 : 0;
+                uint32_t at = n_ties;                            // ties before this lane's
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const uint32_t z = __shfl_up_sync(0xffffffffu, at, o);
+                    if (lane >= o) at += z;
+                }
+                at += __shfl_sync(0xffffffffu, ties_start, l) - n_ties;
+#pragma unroll
+                for (int i = 0; i < VN; ++i) {
+                    w[i] = by_code(v[i], 0);
+                    if (v[i] == thr_v) w[i] = at++ < want ? w_tie : 0;
+                }
+                within(p, v, w, __shfl_sync(0xffffffffu, start, l), target, [&](u64 e) { emit(e, total); });
                 return;
             }
             for (int i = t; i < kBins; i += kThreads) s.count[i] = 0;
@@ -697,9 +801,13 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
     auto gather_counts = [&]() {                                 // the cluster's counts of this thread's bins
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) c[i] = 0;
-        for (int i = 0; i < C; ++i) {
-            const uint4 x = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(s.count, i) + t * kPerThread);
-            c[0] += x.x; c[1] += x.y; c[2] += x.z; c[3] += x.w;
+        for (int r = 0; r < C; r += 4) {                         // (four on their way at once)
+            uint4 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                x[i] = r + i < C ? *reinterpret_cast<const uint4*>(cluster.map_shared_rank(s.count, r + i) + t * kPerThread) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { c[0] += x[i].x; c[1] += x[i].y; c[2] += x[i].z; c[3] += x[i].w; }
         }
         static_assert(kPerThread == 4, "one 16-byte read of the counts");
     };
@@ -807,12 +915,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         for (int o = 16; o > 0; o >>= 1) sum_all += __shfl_xor_sync(0xffffffffu, sum_all, o);
         if (lane == 0) { atomicAdd(&s.all, sum_all); atomicAdd(&s.total, sum_before); }
         const int m = send();
-        u64 before = 0;
-        total = 0;
-        for (int i = 0; i < C; ++i) {
-            total += *cluster.map_shared_rank(&s.all, i);
-            before += *cluster.map_shared_rank(&s.total, i);
-        }
+        const u64 before = cluster_sum(&s.total, C);
+        total = cluster_sum(&s.all, C);
         const u64 goal = share_of(total);
         if (m <= kGather && before < goal) {
             if (rank == 0) {
@@ -836,8 +940,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                     mine = block_sum(mine, s.scan);
                     if (t == 0) s.total += mine;
                     cluster.sync();
-                    total = 0;
-                    for (int i = 0; i < C; ++i) total += *cluster.map_shared_rank(&s.total, i);
+                    total = cluster_sum(&s.total, C);
                 } else {                                         // min-p cuts deeper
                     total = weigh(std::true_type(), most);
                 }
@@ -870,16 +973,61 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         if (inv > 0.f && s.bin[0] < kBins - 2) bound = fmaxf(bound, top - (float)(s.bin[0] + 2) / inv * 1.000001f);
     }
     if (!(k == 0 && top_p < 1.f)) {                              // (top-p alone comes here only if the cluster has to search for its border)
+        // a warp takes pieces that lie side by side, so that the candidates arrive in the first block in order of id
         const Piece<T> test(bound);
-        for (int p = t; p < pieces; p += kThreads) {
-            const uint32_t mask = test.mask(raw_piece(p));
-            if (mask != 0) list(p, mask);
+        const int per = (pieces + kThreads - 1) / kThreads * 32, p0 = warp * per, p1 = min(pieces, p0 + per);
+        uint32_t mine = 0;
+        for (int p = p0 + lane; p < p1; p += 32) mine += __popc(test.mask(raw_piece(p)));
+        mine = __reduce_add_sync(0xffffffffu, mine);
+        uint32_t all, at = block_exclusive<uint32_t>(lane == 0 ? mine : 0, s.scan, all);
+        at = __shfl_sync(0xffffffffu, at, 0);
+        if (t == 0) s.all = all;
+        cluster.sync();
+        at += (uint32_t)cluster_sum(&s.all, rank);
+        const int m = (int)cluster_sum(&s.all, C);
+        if (m <= kGather && mine != 0) {
+            u64* to = cluster.map_shared_rank(s.entry, 0);
+            for (int p = p0 + lane; p - lane < p1; p += 32) {
+                uint32_t mask = p < p1 ? test.mask(raw_piece(p)) : 0;
+                if (__ballot_sync(0xffffffffu, mask != 0) == 0) continue;
+                const uint32_t n_here = __popc(mask);
+                uint32_t incl = n_here;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
+                    if (lane >= o) incl += x;
+                }
+                for (uint32_t y = at + incl - n_here; mask != 0; mask &= mask - 1, ++y) {
+                    const int i = p * VN + __ffs(mask) - 1;
+                    to[y] = entry_of(bits_of(value_of(slice[i])), id0 + i);
+                }
+                at += __shfl_sync(0xffffffffu, incl, 31);
+            }
         }
-        const int m = send();
+        cluster.sync();
         if (m <= kGather) {
             if (rank != 0) return;
             // ---- the first block alone
             auto w_at = [&](int i) { const float v = value_of_entry(s.entry[i]); return near(v) ? weight(distance(v)) : (u64)0; };
+            if (m <= kPairs) {                                   // a thread a candidate: how many, and how much weight, lie in front of it
+                const u64 e = t < m ? s.entry[t] : 0;
+                u64 w = t < m ? w_at(t) : 0, before = 0, whole;
+                if (t < m) s.mass[t] = w;
+                __syncthreads();
+                int front = 0;
+                if (t < m) {
+#pragma unroll 4
+                    for (int i = 0; i < m; ++i)
+                        if (s.entry[i] > e) { ++front; before += s.mass[i]; }
+                }
+                if (k > 0 && front >= k) w = 0;
+                if (top_p < 1.f && before >= share_of(block_sum(w, s.scan))) w = 0;      // (k > 0)
+                const float v = value_of_entry(e);
+                if (w != 0 && !(distance(v) <= most || v == top)) w = 0;
+                const u64 cum = block_exclusive<u64>(w, s.scan, whole), target = target_of(whole);
+                if (cum <= target && target < cum + w) emit(e, whole);
+                return;
+            }
             if (k > 0 && m > k) thr = block_select(s, m, key_at, [&](int) { return (u64)1; }, (u64)k);
             if (top_p < 1.f) {                                   // (k > 0)
                 u64 mine = 0;
@@ -887,14 +1035,19 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                 const u64 goal = share_of(block_sum(mine, s.scan)), was = thr;
                 thr = block_select(s, m, key_at, [&](int i) { return s.entry[i] >= was ? w_at(i) : (u64)0; }, goal);
             }
+            // in order of id
             auto kept_at = [&](int i) { return kept(value_of_entry(s.entry[i]), id_of_entry(s.entry[i])); };
-            u64 mine = 0;
-            for (int i = t; i < m; i += kThreads) mine += kept_at(i);
-            const u64 all = block_sum(mine, s.scan);
-            // in order of id: the inverted id as the key
-            const u64 id = block_select(s, m, [&](int i) { return s.entry[i] & 0xffffffffull; }, kept_at, target_of(all) + 1);
-            for (int i = t; i < m; i += kThreads)
-                if ((s.entry[i] & 0xffffffffull) == id) emit(s.entry[i], all);
+            const int q = (m + kThreads - 1) / kThreads, i0 = min(m, t * q), i1 = min(m, i0 + q);
+            u64 w = 0, whole;
+            for (int i = i0; i < i1; ++i) w += kept_at(i);
+            u64 cum = block_exclusive<u64>(w, s.scan, whole);
+            const u64 target = target_of(whole);
+            if (cum <= target && target < cum + w)
+                for (int i = i0; i < i1; ++i) {
+                    const u64 x = kept_at(i);
+                    if (cum <= target && target < cum + x) emit(s.entry[i], whole);
+                    cum += x;
+                }
             return;
         }
         cluster.sync();
@@ -982,12 +1135,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         hi = __reduce_max_sync(0xffffffffu, hi);
         if (lane == 0) { atomicAdd(&s.sum[0], part); atomicMin(&s.lo, lo); atomicMax(&s.hi, hi); }
         cluster.sync();
-        u64 before = 0;
-        for (int i = 0; i < C; ++i) {
-            before += *cluster.map_shared_rank(&s.sum[0], i);
-            lo = min(lo, *cluster.map_shared_rank(&s.lo, i));
-            hi = max(hi, *cluster.map_shared_rank(&s.hi, i));
-        }
+        u64 before = cluster_sum(&s.sum[0], C);
+        lo = __reduce_min_sync(0xffffffffu, lane < C ? *cluster.map_shared_rank(&s.lo, lane) : 0xffffffffu);
+        hi = __reduce_max_sync(0xffffffffu, lane < C ? *cluster.map_shared_rank(&s.hi, lane) : 0);
         // divide the range of logit bits until the list holds what is left, or one value is
         while (n_in > kList && lo < hi) {
             const int shift = max(0, 21 - __clz(hi - lo));       // (hi - lo) >> shift < 2048
