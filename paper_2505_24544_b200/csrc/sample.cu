@@ -28,6 +28,7 @@
 
 #include "../../include/beagle.h"
 #include "common.cuh"
+#include "tc_ptx.cuh"
 #include "tensor_map.h"
 
 namespace beagle {
@@ -35,6 +36,7 @@ namespace beagle {
 namespace {
 
 namespace cg = cooperative_groups;
+using namespace tc;
 typedef unsigned long long u64;
 
 constexpr int kThreads = 512;
@@ -62,6 +64,7 @@ struct SampleArgs {
     const void* logits;
     long long stride;
     int rows, vocab, slice;              // slice: tokens of a block (a multiple of 8)
+    int more;                            // more rows than clusters fit the GPU
     const float *temperature, *top_p, *min_p, *u;
     const int32_t* top_k;
     int32_t* tokens;
@@ -69,6 +72,9 @@ struct SampleArgs {
 };
 
 struct Shared {
+    uint4 answer;                        // to the request for another row (first block)
+    u64 answer_bar;
+    int next;                            // that row, or -1
     union {
         u64 entry[kGather];              // the candidates of the row (first block)
         uint32_t codes[2 * kSide];       // bf16: tokens of every code
@@ -84,6 +90,7 @@ struct Shared {
     u64 group[kMaxGroups];               // weight of every group of 32 pieces
     u64 scan[2 * kWarps];
     double root[32];                     // 2^(45 - j / 32)
+    double c2, most;                     // 1 / (temperature ln 2); the distance that min_p allows, log2
     u64 sum[2], all, all_n, total, thr, found, middle, middle_n;
     uint32_t n_gather[2];                // candidates of the cluster (first block), of this row and of the one before
     uint32_t top, least, id, lo, hi, n_cand, n_list, n_in, bin[2], mid[2], want, ties;
@@ -278,10 +285,35 @@ template <> struct Piece<bf16> {
     }
 };
 
-// One row.  What the blocks read of one another's shared memory stays until the cluster has met in the next row (or at the kernel's end): words that
+// A row is a cluster of the launch.  A cluster that works on one asks for another that has not begun, to do it too; one thread of its first
+// block.  (Starting a cluster takes some 0.3 us of the whole GPU, and rows take between 12 and 35 us, so that a fixed share of them
+// leaves clusters idle: 448 mixed rows OLD against NEW us.)
+__device__ __forceinline__ void ask_for_row(Shared& s) {
+    const uint32_t bar = smem_u32(&s.answer_bar);
+    mbar_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(&s.answer)), "r"(bar) : "memory");
+}
+// The first block's index of the cluster that was given, or -1 for none.
+__device__ __forceinline__ int row_given(Shared& s, int parity) {
+    const uint32_t bar = smem_u32(&s.answer_bar);
+    bool ok = false;
+    for (uint32_t i = 0; i < kSpinLimit && !ok; ++i) ok = mbar_try_wait(bar, parity);
+    uint32_t given = 0, block = 0;
+    if (ok)
+        asm volatile("{\n.reg .pred p;\n.reg .b128 r;\nld.shared.b128 r, [%2];\n"
+                     "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\nselp.u32 %0, 1, 0, p;\nmov.u32 %1, 0;\n"
+                     "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}"
+                     : "=r"(given), "=r"(block)
+                     : "r"(smem_u32(&s.answer))
+                     : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // (the next answer is written there)
+    return given ? (int)block : -1;
+}
+
+// One row; next: the row that the cluster does after it, or -1.  What the blocks read of one another's shared memory stays until the cluster has met in the next row (or at the kernel's end): words that
 // are set before that meeting have had a meeting after their last reading.
 template <typename T>
-__device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluster_group& cluster, Shared& s, uint8_t* area, int row, int next, int parity) {
+__device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluster_group& cluster, Shared& s, uint8_t* area, int row, int& next, int parity) {
     constexpr int VN = 16 / (int)sizeof(T);
     T* slice = reinterpret_cast<T*>(area);
     const int C = cluster.num_blocks(), rank = cluster.block_rank(), t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -299,6 +331,11 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
     float top_p = a.top_p != nullptr ? __ldcg(a.top_p + row) : 1.f;
     const float min_p = a.min_p != nullptr ? __ldcg(a.min_p + row) : 0.f, uf = __ldcg(a.u + row);
     float top = -CUDART_INF_F, least = CUDART_INF_F;
+    if (t == kThreads - 1) {
+        // (temperatures above 1e30 do what 1e30 does to logits that are not of that size themselves)
+        s.c2 = fmin(1.4426950408889634074 / fmin((double)__uint_as_float(temp_bits), 1e30), 1e300);
+        s.most = min_p > 0.f ? -log2((double)min_p) : CUDART_INF;
+    }
     {
         const int head = min(n, (VN - pad) % VN), vecs = (n - head) / VN, tail = head + vecs * VN;
         const int p0 = (pad + head) / VN;                        // first whole piece
@@ -325,10 +362,6 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                 if (in) { top = fmaxf(top, value_of(src[i])); least = fminf(least, value_of(src[i])); }
             }
         }
-        // the cluster's next row comes from L2
-        if (next < a.rows && t * 128 < n * (int)sizeof(T))
-            for (int i = t * 128; i < n * (int)sizeof(T); i += kThreads * 128)
-                prefetch_l2(reinterpret_cast<const char*>(static_cast<const T*>(a.logits) + (size_t)next * a.stride + first) + i);
     }
     if (t == 0) { s.top = 0; s.least = 0xffffffffu; s.id = 0xffffffffu; s.n_cand = 0; }
     for (int i = t; i < kBins; i += kThreads) s.count[i] = 0;
@@ -337,13 +370,23 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         const uint32_t hi = __reduce_max_sync(0xffffffffu, bits_of(top)), lo = __reduce_min_sync(0xffffffffu, bits_of(least));
         if (lane == 0) { atomicMax(&s.top, hi); atomicMin(&s.least, lo); }
     }
-    cluster.sync();
-    {
-        const uint32_t hi = lane < C ? *cluster.map_shared_rank(&s.top, lane) : 0, lo = lane < C ? *cluster.map_shared_rank(&s.least, lane) : 0xffffffffu;
-        top = of_bits(__reduce_max_sync(0xffffffffu, hi));
-        least = of_bits(__reduce_min_sync(0xffffffffu, lo));
-        if (t == 0) s.n_gather[parity ^ 1] = 0;                  // everyone has read the last row's
+    if (a.more && rank == 0 && t == 0) {
+        const int block = row_given(s, parity);
+        s.next = block >= 0 ? block / C : -1;
     }
+    cluster.sync();
+    {                                                            // a lane reads a block's word, all in one trip
+        const uint32_t* from = lane < C ? cluster.map_shared_rank(&s.top, lane) : lane >= kMaxCluster && lane < kMaxCluster + C ? cluster.map_shared_rank(&s.least, lane - kMaxCluster)
+                             : cluster.map_shared_rank(reinterpret_cast<uint32_t*>(&s.next), 0);
+        const uint32_t x = *from;
+        top = of_bits(__reduce_max_sync(0xffffffffu, lane < C ? x : 0));
+        least = of_bits(__reduce_min_sync(0xffffffffu, lane >= kMaxCluster && lane < kMaxCluster + C ? x : 0xffffffffu));
+        next = a.more ? (int)__shfl_sync(0xffffffffu, x, 31) : -1;
+    }
+    if (next >= 0)                                               // it comes from L2
+        for (int i = t * 128; i < n * (int)sizeof(T); i += kThreads * 128)
+            prefetch_l2(reinterpret_cast<const char*>(static_cast<const T*>(a.logits) + (size_t)next * a.stride + first) + i);
+    if (t == 0) s.n_gather[parity ^ 1] = 0;                      // everyone has read the last row's
 
     // Sum of a word of the blocks' shared memory over the cluster, or over the blocks in front of `end`; whole warps, a lane reads a block's.
     auto sum_lanes = [&](u64 x) {
@@ -383,9 +426,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         top = least = 0.f;
         __syncthreads();
     }
-    // (temperatures above 1e30 do what 1e30 does to logits that are not of that size themselves)
-    const double temp = fmin((double)__uint_as_float(temp_bits), 1e30), c2 = fmin(1.4426950408889634074 / temp, 1e300), dtop = (double)top;
-    const double most = min_p > 0.f ? -log2((double)min_p) : CUDART_INF;         // distance that min_p allows
+    const double c2 = s.c2, most = s.most, dtop = (double)top;
     // A value not above any logit that is at most x away (log2); at least the least finite fp32
     auto value_at = [&](double x) { return fmaxf(__double2float_rd(fmax(dtop - x / c2, -(double)kMost)), -kMost); };
     const float far = fmaxf(__double2float_ru(fmax(dtop - kFar / c2, -(double)kMost)), -kMost);          // logits from here on have a weight, if any
@@ -564,7 +605,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
             bool cuts = false, search = false;                                 // the border is not on a code of its own
             if (top_p < 1.f || k > 0) {
                 for (int i = t; i < 2 * kSide; i += kThreads) s.codes[i] = 0;
-                if (t == 0) { s.middle = s.middle_n = s.found = 0; s.bin[0] = 0xffffffffu; }
+                if (t == 0) { s.found = 0; s.bin[0] = 0xffffffffu; }
                 __syncthreads();
                 u64 middle = 0, middle_n = 0;                    // weight and number of the logits without a place: nearer to 0 than all the others
                 for (int p = t; p < pieces; p += kThreads) {
@@ -581,7 +622,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                         if (near(v)) { middle += weight(distance(v)); ++middle_n; }
                     }
                 }
-                if (middle_n != 0) { atomicAdd(&s.middle, middle); atomicAdd(&s.middle_n, middle_n); }
+                middle = block_sum(middle, s.scan);
+                middle_n = block_sum(middle_n, s.scan);
+                if (t == 0) { s.middle = middle; s.middle_n = middle_n; }
                 cluster.sync();
                 // exact cumulative weight over the codes: a block takes as many of them as the others, a thread q
                 const int share = 2 * kSide / C, q = (share + kThreads - 1) / kThreads;          // (kSide is a multiple of the cluster's size)
@@ -973,59 +1016,46 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         if (inv > 0.f && s.bin[0] < kBins - 2) bound = fmaxf(bound, top - (float)(s.bin[0] + 2) / inv * 1.000001f);
     }
     if (!(k == 0 && top_p < 1.f)) {                              // (top-p alone comes here only if the cluster has to search for its border)
-        // a warp takes pieces that lie side by side, so that the candidates arrive in the first block in order of id
         const Piece<T> test(bound);
-        const int per = (pieces + kThreads - 1) / kThreads * 32, p0 = warp * per, p1 = min(pieces, p0 + per);
-        uint32_t mine = 0;
-        for (int p = p0 + lane; p < p1; p += 32) mine += __popc(test.mask(raw_piece(p)));
-        mine = __reduce_add_sync(0xffffffffu, mine);
-        uint32_t all, at = block_exclusive<uint32_t>(lane == 0 ? mine : 0, s.scan, all);
-        at = __shfl_sync(0xffffffffu, at, 0);
-        if (t == 0) s.all = all;
-        cluster.sync();
-        at += (uint32_t)cluster_sum(&s.all, rank);
-        const int m = (int)cluster_sum(&s.all, C);
-        if (m <= kGather && mine != 0) {
-            u64* to = cluster.map_shared_rank(s.entry, 0);
-            for (int p = p0 + lane; p - lane < p1; p += 32) {
-                uint32_t mask = p < p1 ? test.mask(raw_piece(p)) : 0;
-                if (__ballot_sync(0xffffffffu, mask != 0) == 0) continue;
-                const uint32_t n_here = __popc(mask);
-                uint32_t incl = n_here;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
-                    if (lane >= o) incl += x;
-                }
-                for (uint32_t y = at + incl - n_here; mask != 0; mask &= mask - 1, ++y) {
-                    const int i = p * VN + __ffs(mask) - 1;
-                    to[y] = entry_of(bits_of(value_of(slice[i])), id0 + i);
-                }
-                at += __shfl_sync(0xffffffffu, incl, 31);
-            }
+        for (int p = t; p < pieces; p += kThreads) {
+            const uint32_t mask = test.mask(raw_piece(p));
+            if (mask != 0) list(p, mask);
         }
-        cluster.sync();
+        const int m = send();
         if (m <= kGather) {
             if (rank != 0) return;
             // ---- the first block alone
             auto w_at = [&](int i) { const float v = value_of_entry(s.entry[i]); return near(v) ? weight(distance(v)) : (u64)0; };
-            if (m <= kPairs) {                                   // a thread a candidate: how many, and how much weight, lie in front of it
-                const u64 e = t < m ? s.entry[t] : 0;
-                u64 w = t < m ? w_at(t) : 0, before = 0, whole;
-                if (t < m) s.mass[t] = w;
+            if (m <= kPairs) {                                   // compared pairwise, `per` threads a candidate
+                int shift = 1;
+                while (shift < 5 && (m << shift) <= kThreads / 2) ++shift;
+                const int per = 1 << shift, i = t >> shift;
+                const bool there = i < m, speaks = there && (t & (per - 1)) == 0;        // (one of them speaks for the candidate)
+                const u64 e = there ? s.entry[i] : 0;
+                u64 w = there ? w_at(i) : 0, before = 0;
+                if (speaks) s.mass[i] = w;
                 __syncthreads();
-                int front = 0;
-                if (t < m) {
-#pragma unroll 4
-                    for (int i = 0; i < m; ++i)
-                        if (s.entry[i] > e) { ++front; before += s.mass[i]; }
+                int front = 0;                                   // how many, and how much weight, lie in front of it
+                if (there)
+                    for (int y = t & (per - 1); y < m; y += per)
+                        if (s.entry[y] > e) { ++front; before += s.mass[y]; }
+                for (int o = per / 2; o > 0; o >>= 1) {
+                    front += __shfl_xor_sync(0xffffffffu, front, o);
+                    before += __shfl_xor_sync(0xffffffffu, before, o);
                 }
                 if (k > 0 && front >= k) w = 0;
-                if (top_p < 1.f && before >= share_of(block_sum(w, s.scan))) w = 0;      // (k > 0)
+                if (top_p < 1.f && before >= share_of(block_sum(speaks ? w : 0, s.scan))) w = 0;         // (k > 0)
                 const float v = value_of_entry(e);
                 if (w != 0 && !(distance(v) <= most || v == top)) w = 0;
-                const u64 cum = block_exclusive<u64>(w, s.scan, whole), target = target_of(whole);
-                if (cum <= target && target < cum + w) emit(e, whole);
+                const u64 whole = block_sum(speaks ? w : 0, s.scan), target = target_of(whole);
+                if (speaks) s.mass[i] = w;
+                __syncthreads();
+                before = 0;                                      // weight of the lower ids that are kept
+                if (there)
+                    for (int y = t & (per - 1); y < m; y += per)
+                        if ((uint32_t)s.entry[y] > (uint32_t)e) before += s.mass[y];
+                for (int o = per / 2; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+                if (speaks && before <= target && target < before + w) emit(e, whole);
                 return;
             }
             if (k > 0 && m > k) thr = block_select(s, m, key_at, [&](int) { return (u64)1; }, (u64)k);
@@ -1035,19 +1065,14 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                 const u64 goal = share_of(block_sum(mine, s.scan)), was = thr;
                 thr = block_select(s, m, key_at, [&](int i) { return s.entry[i] >= was ? w_at(i) : (u64)0; }, goal);
             }
-            // in order of id
             auto kept_at = [&](int i) { return kept(value_of_entry(s.entry[i]), id_of_entry(s.entry[i])); };
-            const int q = (m + kThreads - 1) / kThreads, i0 = min(m, t * q), i1 = min(m, i0 + q);
-            u64 w = 0, whole;
-            for (int i = i0; i < i1; ++i) w += kept_at(i);
-            u64 cum = block_exclusive<u64>(w, s.scan, whole);
-            const u64 target = target_of(whole);
-            if (cum <= target && target < cum + w)
-                for (int i = i0; i < i1; ++i) {
-                    const u64 x = kept_at(i);
-                    if (cum <= target && target < cum + x) emit(s.entry[i], whole);
-                    cum += x;
-                }
+            u64 mine = 0;
+            for (int i = t; i < m; i += kThreads) mine += kept_at(i);
+            const u64 all = block_sum(mine, s.scan);
+            // in order of id: the inverted id as the key
+            const u64 id = block_select(s, m, [&](int i) { return s.entry[i] & 0xffffffffull; }, kept_at, target_of(all) + 1);
+            for (int i = t; i < m; i += kThreads)
+                if ((s.entry[i] & 0xffffffffull) == id) emit(s.entry[i], all);
             return;
         }
         cluster.sync();
@@ -1220,7 +1245,6 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
     draw(weigh(std::true_type(), most));
 }
 
-// The clusters that fit the GPU at once walk over the rows: starting one takes some 0.3 us of the whole GPU.
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
@@ -1229,12 +1253,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const int C = cluster.num_blocks();
     if (threadIdx.x < 32) s.root[threadIdx.x] = exp2(45.0 - (double)threadIdx.x / 32.0);
     if (threadIdx.x < 2) s.n_gather[threadIdx.x] = 0;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&s.answer_bar), 1);
+        fence_barrier_init();
+    }
     pdl_launch_dependents();
     pdl_wait();
-    int parity = 0;
-    for (int row = blockIdx.x / C; row < a.rows; row += gridDim.x / C, parity ^= 1) {
+    for (int row = blockIdx.x / C, parity = 0, next; row >= 0; row = next, parity ^= 1) {
         __syncthreads();                                         // (the row before is done with the block's memory)
-        sample_row<T>(a, cluster, s, smem + (sizeof(Shared) + 15) / 16 * 16, row, row + gridDim.x / C, parity);
+        if (a.more && threadIdx.x == 0 && cluster.block_rank() == 0) ask_for_row(s);
+        sample_row<T>(a, cluster, s, smem + (sizeof(Shared) + 15) / 16 * 16, row, next, parity);
     }
     cluster.sync();                                              // nobody reads a block's memory after it has ended
 }
@@ -1288,7 +1316,8 @@ beagle_status launch_sample(SampleArgs a, cudaStream_t stream) {
     cfg.attrs = attrs;
     cfg.numAttrs = 1;
     const int fit = resident_clusters<T>(cfg, c, large);
-    cfg.gridDim = dim3((unsigned)((a.rows < fit ? a.rows : fit) * c));
+    cfg.gridDim = dim3((unsigned)(a.rows * c));
+    a.more = a.rows > fit;
     cfg.dynamicSmemBytes = bytes;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a) == cudaSuccess && cudaGetLastError() == cudaSuccess ? BEAGLE_OK : BEAGLE_ERR_CUDA;
@@ -1313,6 +1342,6 @@ extern "C" beagle_status beagle_sample(const void* logits_dev, int32_t logits_dt
         (((uintptr_t)temperature_dev | (uintptr_t)top_k_dev | (uintptr_t)top_p_dev | (uintptr_t)min_p_dev | (uintptr_t)u_dev | (uintptr_t)tokens_out_dev |
           (uintptr_t)logp_out_dev) & 3))
         return BEAGLE_ERR_INVALID_ARG;
-    SampleArgs a{logits_dev, row_stride, rows, vocab, 0, temperature_dev, top_p_dev, min_p_dev, u_dev, top_k_dev, tokens_out_dev, logp_out_dev};
+    SampleArgs a{logits_dev, row_stride, rows, vocab, 0, 0, temperature_dev, top_p_dev, min_p_dev, u_dev, top_k_dev, tokens_out_dev, logp_out_dev};
     return logits_dtype == BEAGLE_BF16 ? launch_sample<bf16>(a, static_cast<cudaStream_t>(stream)) : launch_sample<float>(a, static_cast<cudaStream_t>(stream));
 }
