@@ -382,7 +382,8 @@ beagle_status beagle_paged_attn(const beagle_pages* pages, int32_t batch, const 
  * shared_dev int32 [n_groups]: the first so many positions hold the same keys and values in every slot of the group; they are read
  * through the group's first slot.  Clamped to 0 and the shortest length of the group.  What lies behind them is read row by row, so
  * any smaller number gives the same attention.  Everything visible (no window).  Other arguments and results as beagle_paged_attn (results
- * are its up to rounding, and do not depend on timing).  ws_dev: beagle_paged_attn_shared_workspace_bytes, 16-byte aligned.
+ * are its up to rounding, and do not depend on timing).  ws_dev: beagle_paged_attn_shared_workspace_bytes, 16-byte aligned, contents irrelevant
+ * between calls; two calls that may run at the same time need two.
  *
  * beagle_pages_shared: writes such a shared_dev from the cache itself: per group the positions of the leading whole pages that all of
  * its slots name alike (0 for a group of one row, for which nothing is gained). */

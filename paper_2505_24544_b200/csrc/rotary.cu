@@ -5,8 +5,8 @@
 // loads are on their way; then each thread keeps the entries of its unit (16 bytes of a head and, in the half layout, their partners)
 // in registers and walks over the heads.  Queries and keys go in one launch, so that the entries are formed once for both.
 //
-// Measured: 8 x 2048 positions, 32 + 32 heads of 128, bf16, forward and backward (1.07 GB): 177 us, 6.1 TB/s; 8191 positions, 32 + 8 heads,
-// interleaved, a quarter rotated (168 MB): 43 us.  One head at a time in a thread and six CTAs per SM; four heads in flight in two
+// Measured: 8 x 2048 positions, 32 + 32 heads of 128, bf16, forward and backward (1.07 GB): 174 us, 6.1 TB/s; 8191 positions, 32 + 8 heads,
+// interleaved, a quarter rotated (168 MB): 37 us.  One head at a time in a thread and six CTAs per SM; four heads in flight in two
 // CTAs per SM took 240 and 53, entries formed by every thread for itself, without shared memory, 179 and 47.
 #include <cmath>
 #include <cstring>
@@ -96,7 +96,8 @@ RotaryGrid rotary_grid(const beagle_rotary* r, int dtype, long long rows, int he
     g.units = r->interleaved ? r->head_dim / e : pairs / e + (r->head_dim - r->rot_dim) / e;
     const int slots = kRotThreads / g.units;         // a head has at most 256 elements
     // many rows: a CTA takes several, so that it has entries to form for all of its threads, and a thread several heads with the same
-    // ones; few rows: the heads of a row over as many threads as there are
+    // ones; few rows: the heads of a row over as many threads as there are.  Measured, 8 heads side by side / all, us, heads of 128, bf16: 32 rows of
+    // 32 + 8 heads 11 / 9, of 128 + 8 19 / 11; 1184 rows 14 / 14 and 27 / 23; 2368 rows 16 / 18 and 37 / 35; 9472 rows 40 / 48 and 111 / 107.
     g.lanes = rows >= (long long)device_sm_count() * 8 ? 8 : heads;
     if (g.lanes > slots) g.lanes = slots;
     g.rows = slots / g.lanes;

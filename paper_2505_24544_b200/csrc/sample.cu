@@ -12,14 +12,20 @@
 // known of it.  What costs is the double-precision weight (some 25 instructions), so it is formed
 //   - of all tokens, once, only if top-k does not limit them: the total is needed then.  top-p: a histogram of fp32 weights says beforehand
 //     in which few bins of distance the border lies, so that the same pass finds the exact weight before them and lists their tokens;
-//     bf16 logits have few values: there the tokens of every code are counted and the border falls on one code, exactly, and the
-//     tokens' weights come from a table by code (1408 codes of either sign; the few logits nearer to 0 are computed);
+//   - by code where the logits are bf16 and have few values (1408 codes of either sign; the few logits nearer to 0 are computed): a table
+//     holds the weight of every code.  top-p, and top-k beyond kPairs: the tokens of every code are counted, each block adds up its share of the codes,
+//     and the border falls on one code, exactly, of whose tokens the first so many in order of id are kept;
 //   - otherwise of candidates alone, those a bound in fp32 does not exclude.  top-k: at least k groups of a few neighbours (the ones read as
 //     one 16-byte piece) have their largest in the leading bins of a histogram, so the k-th token is in those too.  min-p: its distance.
-// Up to kGather candidates or tokens of the border's bins, nearly always, go to the first block, which sorts them.  More of them:
-// the cluster finds each border with a histogram whose counts bracket the weights, one exact pass, and a list of the tokens
-// in the few bins left, compared pairwise; more than kList of those: their range of logit bits is divided further, by 2048 a level
-// with exact weights, until few are left, or only equal logits, which are taken in order of id.
+// Up to kGather candidates or tokens of the border's bins, nearly always, go to the first block: up to kPairs are compared pairwise, more
+// selected by histograms of their keys.  More than kGather of them: the cluster finds each border with a histogram whose counts bracket the
+// weights, one exact pass, and a list of the tokens in the few bins left, compared pairwise; more than kList of those: their range of logit
+// bits is divided further, by 2048 a level with exact weights, until few are left, or only equal logits, which are taken in order of id.
+//
+// Bound by latency: a row is a chain of some ten short passes with a meeting of the cluster after most (a microsecond each, with the words read
+// from the other blocks), 20 to 30 us from end to end; two blocks share an SM, so 71 rows of 128256 bf16 logits are under way at a time.  Measured,
+// 448 such rows (115 MB): temperature alone 166 us (weights from the table: half of a row's time), top-k of 50 119, top-p 225, min-p 113, mixed
+// filters 172; one row of 32000 fp32 logits with top-k 12 us with the call, of 128256 bf16 ones with top-p 29.
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
@@ -287,7 +293,7 @@ template <> struct Piece<bf16> {
 
 // A row is a cluster of the launch.  A cluster that works on one asks for another that has not begun, to do it too; one thread of its first
 // block.  (Starting a cluster takes some 0.3 us of the whole GPU, and rows take between 12 and 35 us, so that a fixed share of them
-// leaves clusters idle: 448 mixed rows OLD against NEW us.)
+// leaves clusters idle: 448 mixed rows 200 against 182 us.)
 __device__ __forceinline__ void ask_for_row(Shared& s) {
     const uint32_t bar = smem_u32(&s.answer_bar);
     mbar_expect_tx(bar, 16);
@@ -395,6 +401,18 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         return __shfl_sync(0xffffffffu, x, 0);
     };
     auto cluster_sum = [&](u64* x, int end) { return sum_lanes(lane < end ? *cluster.map_shared_rank(x, lane) : 0); };
+    // The same of two words in one trip, over the cluster and over the blocks in front of this one.
+    struct Two { u64 x, y, x_before, y_before; };
+    auto cluster_sums = [&](u64* x, u64* y) {
+        const int i = lane % kMaxCluster;
+        u64 v = lane < 2 * kMaxCluster && i < C ? *cluster.map_shared_rank(lane < kMaxCluster ? x : y, i) : 0, w = i < rank ? v : 0;
+#pragma unroll
+        for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
+            v += __shfl_xor_sync(0xffffffffu, v, o);
+            w += __shfl_xor_sync(0xffffffffu, w, o);
+        }
+        return Two{__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, kMaxCluster), __shfl_sync(0xffffffffu, w, 0), __shfl_sync(0xffffffffu, w, kMaxCluster)};
+    };
 
     const bool drawn = temp_bits - 1u < 0x7f800000u;             // temperature above 0, infinity included
     if (top_p <= 0.f || min_p > 1.f) k = 1;                      // only the first
@@ -580,7 +598,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
     u64 total = 0;
     const float bottom = fmaxf(far, least);                      // (a masked token makes it `far`)
     if constexpr (sizeof(T) == 2) {
-        // ---- bf16, not limited by top-k: codes.  Positive ones from the largest downwards, then negative ones up to the largest magnitude that is
+        // ---- bf16, limited by top-p or by a large top-k: codes.  (k = 400 / 3000 with top-p 0.95, us: one row by candidates 39 / 64, by code 33 / 33,
+        // 142 rows 88 / 168 and 86 / 90; k = 50 by candidates 23 and 53.)  Positive ones from the largest downwards, then negative ones up to the largest magnitude that is
         // near; `code` numbers them in order of falling logit.
         const int top_code = top > 0.f ? (int)(__float_as_uint(top) >> 16) : -1, low_mag = bottom < 0.f ? (int)(__float_as_uint(-bottom) >> 16) : -1;
         constexpr int kLeast = kSide + 128;                      // (no subnormal values among them)
@@ -651,16 +670,20 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
                     sum += n * w;
                     sum_n += n;
                 }
-                const u64 mid = cluster_sum(&s.middle, C);
-                const uint32_t mid_n = (uint32_t)cluster_sum(&s.middle_n, C);
+                const Two middles = cluster_sums(&s.middle, &s.middle_n);
+                const u64 mid = middles.x;
+                const uint32_t mid_n = (uint32_t)middles.y;
                 u64 cum = block_exclusive<u64>(sum, s.scan, all);
                 uint32_t cum_n = block_exclusive<uint32_t>(sum_n, s.scan, all_n);
                 if (t == 0) { s.all = all; s.all_n = all_n; }
                 cluster.sync();
-                cum += cluster_sum(&s.all, rank);
-                cum_n += (uint32_t)cluster_sum(&s.all_n, rank);
-                total = cluster_sum(&s.all, C) + mid;
-                all_n = (uint32_t)cluster_sum(&s.all_n, C) + mid_n;
+                {
+                    const Two sums = cluster_sums(&s.all, &s.all_n);
+                    cum += sums.x_before;
+                    cum_n += (uint32_t)sums.y_before;
+                    total = sums.x + mid;
+                    all_n = (uint32_t)sums.y + mid_n;
+                }
                 // f(code, its tokens, the weight of one, weight and tokens before), of this thread's codes
                 auto for_codes = [&](auto f) {
                     u64 c = cum;
@@ -958,8 +981,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         for (int o = 16; o > 0; o >>= 1) sum_all += __shfl_xor_sync(0xffffffffu, sum_all, o);
         if (lane == 0) { atomicAdd(&s.all, sum_all); atomicAdd(&s.total, sum_before); }
         const int m = send();
-        const u64 before = cluster_sum(&s.total, C);
-        total = cluster_sum(&s.all, C);
+        const Two sums = cluster_sums(&s.total, &s.all);
+        const u64 before = sums.x;
+        total = sums.y;
         const u64 goal = share_of(total);
         if (m <= kGather && before < goal) {
             if (rank == 0) {
@@ -1269,7 +1293,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 
 constexpr size_t kHalfSm = 113 * 1024 - 128;     // dynamic shared memory of a block that shares its SM with another
 
-// Blocks of a row: slices of up to 64 KB, so that two blocks share an SM; more blocks while the GPU has room for them.
+// Blocks of a row: slices of up to 64 KB, so that two blocks share an SM; more blocks while the GPU has room for them.  Slices of 32 KB: 448 rows of
+// 128256 bf16 logits 233 instead of 166 us (temperature) and 354 instead of 225 (top-p), the same where rows are few.  As few blocks as the slices
+// need: one row of 32000 bf16 logits 25 instead of 16 us (temperature) and 34 instead of 25 (top-p), 32 rows of 128256 33 instead of 31
+// and 41 instead of 38 (but 23 instead of 29 with top-k, where one block does most of the work).
 int blocks_of_row(int rows, int vocab, int elt) {
     int c = 1;
     while (c < kMaxCluster && ((long long)vocab * elt > (long long)c * 64 * 1024 || (vocab > c * 4096 && (long long)rows * c < device_sm_count()))) c *= 2;
