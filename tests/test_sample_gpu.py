@@ -296,3 +296,64 @@ def test_drafts_for_acceptance_under_sampling(dtype):
     drafts = tokens.view(B, gamma + 1)
     accept, out = head.verify_sample(drafts[:, :gamma].contiguous(), z[:, :gamma].float().transpose(0, 1).contiguous(), z, torch.rand(B, gamma, device="cuda"), u[:, gamma].contiguous(), 0.8)
     assert accept.tolist() == [gamma] * B and torch.equal(out, drafts)
+
+
+@pytest.mark.parametrize("v", [300, 5000, 32000, 128256])
+@pytest.mark.parametrize("kind", ["noise", "ties", "one high", "two sides", "masked"])
+def test_large_top_k_by_code(v, kind):
+    """bf16 with top-k beyond the candidates that are compared pairwise: the border on a code, on one of many equal logits, among the
+    logits next to 0 that have no code of their own, behind the last logit that weighs anything."""
+    rows = 24
+    z = noise(rows, v, 3.0, "bf16", v)
+    if kind == "ties":
+        z = (z * 2).round() / 2
+    elif kind == "one high":                             # nearly all lie below 2^-11 of the largest
+        z = z * 2.0 ** -10
+        z[:, 17] = 9.0
+    elif kind == "two sides":                            # -0.0, 0, both signs, far below the largest
+        z = torch.where(z > 0, z * 2.0 ** -14, z)
+        z[:, ::5] = 0.0
+        z[:, 1::5] = -0.0
+    elif kind == "masked":
+        z[:, torch.arange(v, device="cuda") % 7 != 3] = float("-inf")
+        z[:, ::11] = float("nan")
+    r = random.Random(v)
+    check(z, u=[r.random() for _ in range(rows)], temperature=[r.choice([0.3, 1.0, 1.7]) for _ in range(rows)],
+          top_k=[r.choice([257, 258, 299, 400, 1000, 3000, v // 2, v - 1]) for _ in range(rows)], top_p=[r.choice([1.0, 0.2, 0.9, 0.9999]) for _ in range(rows)],
+          min_p=[r.choice([0.0, 0.0, 0.05]) for _ in range(rows)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("m", [1, 2, 31, 32, 33, 64, 65, 128, 129, 255, 256, 257, 258, 3499, 3500, 3501])
+def test_numbers_of_candidates(dtype, m):
+    """As many tokens as min-p keeps, around the borders between the ways to finish a row."""
+    rows, v = 4, 20000
+    z = torch.full((rows, v), -5.0, dtype=DT[dtype], device="cuda")
+    at = torch.randperm(v, generator=torch.Generator(device="cuda").manual_seed(m), device="cuda")[:m]
+    z[:, at] = torch.rand(rows, m, generator=torch.Generator(device="cuda").manual_seed(m), device="cuda").to(DT[dtype])
+    check(z, u=[0.0, 0.3, 0.77, 0.99999994], min_p=[0.1] * rows)
+    check(z, u=[0.0, 0.3, 0.77, 0.99999994], top_k=[m] * rows, top_p=[1.0, 0.5, 0.9, 0.99])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_more_rows_than_fit_the_gpu(dtype):
+    """Clusters take over rows of others; captured and replayed too, with other parameters in the same tensors."""
+    rows, v = 700, 33000
+    z = noise(rows, v, 3.0, dtype, 4)
+    p = params(rows, 6, v)
+    want = check(z, **p)
+    dev = lambda x, dt: torch.tensor(x, dtype=dt, device="cuda")
+    args = dict(temperature=dev(p["temperature"], torch.float32), top_k=dev(p["top_k"], torch.int32), top_p=dev(p["top_p"], torch.float32), min_p=dev(p["min_p"], torch.float32))
+    u, tokens = dev(p["u"], torch.float32), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.beagle_sample(z, u, tokens, **args)
+    for turn in range(5):
+        tokens.zero_()
+        graph.replay()
+        assert tokens.tolist() == want
+    for x in (u, *args.values()):
+        x.copy_(x.flip(0))
+    z.copy_(z.flip(0))
+    graph.replay()
+    assert tokens.tolist() == want[::-1]
