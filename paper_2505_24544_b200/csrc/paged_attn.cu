@@ -491,13 +491,12 @@ __global__ void __launch_bounds__(2 * kSharedJoinWarps * 32) paged_shared_join_k
     const bool there = b < a.rows;
     const int group = there ? a.group_of[b] : 255;
     const bool common = group != 255, cores = common && prefix.on[group];
-    // the row's own positions and the common part: of each the partials' base and distance, and how many there are.  Partial i of a source is the
-    // (i % split)th of run r0 + i / split.
+    // the row's own positions and the common part.  Partial i of a source is the (i % split)th of run r0 + i / split; the first run's lie by pair, the
+    // others' by run, one behind the other: head + i * size for i < split, else rest + i * size.
     struct Source {
-        const float* part;
-        size_t size;                     // floats of a partial
-        int o, ml;                       // offsets of the row's O and of its (maximum, sum)
-        int pair, n_pairs, r0, n, split;
+        const float *head, *rest;        // at the row's O
+        int size, ml;                    // floats of a partial; from the row's O to its (maximum, sum)
+        int n, split;
     };
     auto source = [&](bool first) {
         const bool tc = !first && cores;
@@ -507,10 +506,11 @@ __global__ void __launch_bounds__(2 * kSharedJoinWarps * 32) paged_shared_join_k
             e = common ? (tc ? prefix.entry[group] : a.prefix_entry[group]) + j / block : 0;
             at = j % block;
         }
-        const int rows = tc ? prefix.part_rows : 8, pair = e * a.Hkv + kvh, split = tc ? 1 : a.split;
+        const int rows = tc ? prefix.part_rows : 8, pair = e * a.Hkv + kvh, split = tc ? 1 : a.split, size = rows * (DH + 2), o = tc ? at * DH : at * (DH + 2);
         const int2 runs = there && (first || common) ? __ldcg((tc ? prefix.span : a.span) + pair) : make_int2(0, -1);
-        return Source{tc ? prefix.part : a.part, (size_t)rows * (DH + 2), tc ? at * DH : at * (DH + 2), tc ? rows * DH + 2 * at : at * (DH + 2) + DH,
-                      pair, tc ? prefix.n_pairs : a.n_pairs, runs.x, (runs.y - runs.x + 1) * split, split};
+        const float* part = (tc ? prefix.part : a.part) + o;
+        return Source{part + (size_t)pair * split * size, part + (size_t)((tc ? prefix.n_pairs : a.n_pairs) + runs.x) * split * size, size,
+                      (tc ? rows * DH + 2 * at : at * (DH + 2) + DH) - o, (runs.y - runs.x + 1) * split, split};
     };
     const Source own = source(true), shared = source(false);
     const int all = own.n + shared.n;
@@ -526,21 +526,20 @@ __global__ void __launch_bounds__(2 * kSharedJoinWarps * 32) paged_shared_join_k
         for (int z = 0; z < kJoinFlight; ++z) {
             const int i = i0 + z * W;
             const bool some = i < all, mine = i < own.n;
-            const Source& x = mine ? own : shared;
-            const int at = some ? (mine ? i : i - own.n) : 0, run = at / x.split;
-            const float* p = x.part + (some ? ((size_t)(run == 0 ? x.pair : x.n_pairs + x.r0 + run) * x.split + (at - run * x.split)) * x.size : 0);
-            ml[z] = some ? __ldcg(reinterpret_cast<const float2*>(p + x.ml)) : make_float2(-INFINITY, 0.f);
+            const int at = mine ? i : i - own.n;
+            const float* p = (at < (mine ? own.split : shared.split) ? (mine ? own.head : shared.head) : (mine ? own.rest : shared.rest)) + (size_t)(uint32_t)at * (mine ? own.size : shared.size);
+            ml[z] = some ? __ldcg(reinterpret_cast<const float2*>(p + (mine ? own.ml : shared.ml))) : make_float2(-INFINITY, 0.f);
 #pragma unroll
             for (int d = 0; d < kSteps; ++d)
 #pragma unroll
                 for (int y = 0; y < kPer; y += kPer > 1 ? 2 : 1) {       // (rows of partials begin on 8 bytes)
                     const int c = (d * 32 + lane) * kPer + y;
                     if (kPer > 1) {
-                        const float2 v = some && c < DH ? __ldcg(reinterpret_cast<const float2*>(p + x.o + c)) : make_float2(0.f, 0.f);
+                        const float2 v = some && c < DH ? __ldcg(reinterpret_cast<const float2*>(p + c)) : make_float2(0.f, 0.f);
                         o[z][d][y] = v.x;
                         o[z][d][y + (kPer > 1 ? 1 : 0)] = v.y;
                     } else {
-                        o[z][d][y] = some && c < DH ? __ldcg(p + x.o + c) : 0.f;
+                        o[z][d][y] = some && c < DH ? __ldcg(p + c) : 0.f;
                     }
                 }
         }

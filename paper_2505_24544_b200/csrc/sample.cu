@@ -50,10 +50,10 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kBins = 2048, kPerThread = kBins / kThreads;
 constexpr int kMassBins = 1024;          // of the first block's selections
 constexpr int kGather = 3500;            // candidates that the first block finishes alone
-constexpr int kPairs = 256;              // candidates that it compares pairwise, a thread each
+constexpr int kPairs = 256;              // candidates that it compares pairwise
 constexpr int kList = kThreads;          // tokens that a block compares pairwise (the cluster's search)
 constexpr int kSide = 1408;              // bf16 codes of one sign with a place of their own: eleven binades below the largest magnitude
-constexpr int kFew = 64;                 // the same of the first block's own selections
+constexpr int kFew = 64;                 // entries that a selection of the first block compares pairwise
 constexpr int kMaxCluster = 8;
 constexpr int kMaxVocab = 1 << 18;
 constexpr int kMaxGroups = kMaxVocab / kMaxCluster / 128 + 8;      // of 32 16-byte pieces (128 fp32 logits, 256 bf16) in a block's slice
