@@ -467,8 +467,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
     }
 }
 
-// Warps of a head in the join, and partials that each has in flight.  Calls of 32 rows over 8192 / four groups of 16 over 4096, us: 4 and 4 29.6 / 80, 8 and 4,
-// or 4 and 8, 31 / 84, 8 and 8 37 / 93, 4 and 2 31 / 80, 2 and 4 33 / 80.
+// Warps of a head in the join, and partials that each has in flight.  Calls of 32 rows over 8192 / four groups of 16 over 4096, us: 4 and 4 28.9 / 81, 8 and 4
+// 30.4 / 85, 4 and 8 29.2 / 83, 8 and 8 34 / 91, 4 and 2 30.6 / 80, 2 and 4 31.8 / 81.
 constexpr int kSharedJoinWarps = 4;
 constexpr int kJoinFlight = 4;
 // The same for rows of groups, two (row of the call, query head) items a CTA; the partials of the row's own positions and those of the

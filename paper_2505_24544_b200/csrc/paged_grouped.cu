@@ -9,7 +9,7 @@
 //
 // Two CTAs per SM, each with one kind of work, shared out by the tiles, the kinds side by side as far as possible: common parts wait
 // for the hand-over between softmax and products, rows for memory.  Measured: 32 rows over 8192 common positions, 32/8 heads of 128, some hundred
-// positions behind: 30 us with the join (the two kinds in launches of their own 38); four groups of 16 rows, 32/32 heads: 81 us; 64 rows over
+// positions behind: 29 us with the join, of which the join takes 9 (the two kinds in launches of their own: 48, in one 41, at that time); four groups of 16 rows, 32/32 heads: 81 us; 64 rows over
 // 65536, up to 8192 behind: 146 us (all CTAs first one kind, then the other: 167); alone the common parts run at 207 tiles a microsecond
 // (868 TFLOP/s with 128 query rows, half of the tensor cores' rate) and the rows at 5.8 TB/s.
 //
