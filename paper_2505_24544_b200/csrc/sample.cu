@@ -299,7 +299,8 @@ __device__ __forceinline__ void ask_for_row(Shared& s) {
     mbar_expect_tx(bar, 16);
     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(&s.answer)), "r"(bar) : "memory");
 }
-// The first block's index of the cluster that was given, or -1 for none.
+// The first block's index of the cluster that was given, or -1 for none.  (The wait is bounded like every other; the answer comes within a
+// microsecond or two.  If it did not, the cluster would end here, and the rows that it was about to be given keep the tokens they had.)
 __device__ __forceinline__ int row_given(Shared& s, int parity) {
     const uint32_t bar = smem_u32(&s.answer_bar);
     bool ok = false;
