@@ -801,17 +801,21 @@ int shared_runs(const beagle_pages* p) {
     const int runs = device_sm_count() * (uses_mma(p) ? kCtasPerSm : kSimtCtasPerSm);
     return runs < kMaxRuns ? runs : kMaxRuns;
 }
-// The call's workspace: where each form's runs of the pairs and partials lie; bytes.
+// The call's workspace: where each form's runs of the pairs and partials lie, from a border of kWsAlign bytes on; bytes that the caller provides.
+// The caller's memory begins on 16 bytes, but a common part's partials leave as 32 bytes at once, whose address has to be a multiple of
+// that: the parts lie behind the first such border, and a whole one more is asked for.
+constexpr size_t kWsAlign = 256;
+char* shared_ws_base(void* ws) { return reinterpret_cast<char*>(((uintptr_t)ws + kWsAlign - 1) / kWsAlign * kWsAlign); }
 struct SharedLayout { size_t span, prefix_span, part, prefix_part, bytes; };
 SharedLayout shared_ws(const beagle_pages* p, const SharedArgs& a, const PrefixArgs& f) {
     const size_t row = (size_t)(p->head_dim + 2) * sizeof(float);
-    auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    auto up = [](size_t n) { return (n + kWsAlign - 1) / kWsAlign * kWsAlign; };
     SharedLayout l;
     l.span = 0;
     l.prefix_span = l.span + up(a.n_pairs * sizeof(int2));
     l.part = l.prefix_span + up(f.n_pairs * sizeof(int2));
     l.prefix_part = l.part + up((size_t)(a.n_pairs + shared_runs(p)) * a.split * 8 * row);
-    l.bytes = l.prefix_part + (f.batch > 0 ? up((size_t)(f.n_pairs + shared_runs(p)) * f.part_rows * row) : 0);
+    l.bytes = kWsAlign + l.prefix_part + (f.batch > 0 ? up((size_t)(f.n_pairs + shared_runs(p)) * f.part_rows * row) : 0);
     return l;
 }
 
@@ -961,7 +965,7 @@ beagle_status beagle_paged_attn_shared(const beagle_pages* p, int32_t batch, con
     f.slots = a.slots;
     fill_args(p, n_q_heads, q_dev, q_stride, out_dev, lse_dev, &f);
     a.shared = f.shared = shared_dev;
-    char* base = static_cast<char*>(ws_dev);
+    char* base = shared_ws_base(ws_dev);
     a.span = reinterpret_cast<int2*>(base + l.span);
     f.span = reinterpret_cast<int2*>(base + l.prefix_span);
     a.part = reinterpret_cast<float*>(base + l.part);

@@ -32,6 +32,7 @@ constexpr int kRows = 128;               // query rows of a tile
 
 template <int DH>
 struct PrefixSmem {
+    static_assert(4 * (DH + 2) * 4 % 32 == 0 && DH * 4 % 32 == 0, "partials are stored 32 bytes at once");
     static constexpr int kQ = kRows * DH * 2, kT = kTile * DH * 2;           // Q; a K or V tile, two stages of each
     static constexpr int kRing = kQ + 4 * kT;                                // as much as the rows' ring
     static_assert(kRing == kStages * 2 * PagedSmem<DH>::kTileBytes, "both kinds of work use the same memory in turn");
@@ -44,7 +45,8 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
                  : "memory");
 }
 
-// 32 bytes, a whole sector, at once: each thread writes a row of its own.
+// 32 bytes, a whole sector, at once: each thread writes a row of its own.  p on 32 bytes: partials begin on multiples of that (kWsAlign, four rows
+// of DH + 2 floats), and so do their rows.
 __device__ __forceinline__ void store32(float* p, const uint32_t* v) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }

@@ -282,3 +282,19 @@ def test_rows_behind_the_batch_stay():
     out, lse = torch.full_like(q, 7.0), torch.full((9, 4), 7.0, device="cuda")
     b.beagle_paged_attn_shared(cache, list(range(5)), [3, 2], i32(shared).cuda(), q[:5], out[:5], lse[:5])
     assert bool((out[5:] == 7.0).all()) and bool((lse[5:] == 7.0).all()) and not bool((out[:5] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dh", [("bf16", 8, 2, 128), ("bf16", 7, 1, 64), ("bf16", 4, 1, 256), ("fp32", 4, 4, 64)])
+@pytest.mark.parametrize("off", [16, 32, 48, 128, 240, 256])
+def test_workspace_at_any_16_byte_border(dtype, hq, hkv, dh, off):
+    """A piece of a larger buffer as workspace: the same attention, and the bytes around the piece stay."""
+    cache, shared = forked([20, 5, 2], [900, 300, 130], list(range(27)), 16, hkv, dh, dtype, 12)
+    groups, slots, sh = [20, 5, 2], list(range(27)), i32(shared).cuda()
+    q = randn(27, hq, dh, dtype=dtype, seed=8)
+    ref = attend(cache, slots, groups, sh, q, dtype)
+    n = b.beagle_paged_attn_shared_workspace_bytes(cache, 27, hq, groups)
+    buf = torch.full((n + 1024,), 0x5a, dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+    b.beagle_paged_attn_shared(cache, slots, groups, sh, q, out, ws=buf[off:off + n])
+    assert torch.equal(out, ref)
+    assert bool((buf[:off] == 0x5a).all()) and bool((buf[off + n:] == 0x5a).all())

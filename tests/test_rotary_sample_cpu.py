@@ -155,3 +155,26 @@ def test_sample_refusals(lib):
         assert call(**kw) == INVALID, kw
     assert call(vocab=2 ** 18 + 1, stride=2 ** 19) == SHAPE
     assert call(rows=2 ** 31 - 1) == CAPACITY
+
+
+@pytest.mark.parametrize("dtype,dh,hq,hkv", [(1, 128, 32, 8), (1, 64, 8, 8), (1, 64, 7, 1), (1, 256, 4, 1), (0, 64, 4, 4)])
+@pytest.mark.parametrize("groups", [[1, 1], [2], [9, 1], [64], [33, 2, 3]])
+def test_shared_workspace_has_room_at_any_16_byte_border(lib, dtype, dh, hq, hkv, groups):
+    """The partials are stored 32 bytes at once and lie on multiples of 256, the caller's memory on 16: the size has room for all of them
+    behind the border that follows any such address."""
+    G, sms = hq // hkv, 148
+    mma = dtype == 1 and dh in (64, 128)
+    many = [n * G for n in groups if mma and n > 1 and n * G > 8]               # query rows of the groups on 128-row tiles
+    block, few = 128 // G * G, 4 if dh == 256 else 8
+    entries = sum(groups) + sum(-(-n * G // few) for n in groups if n > 1 and not (mma and n * G > 8))
+    tiles = sum(-(-n // block) for n in many)
+    up = lambda x: -(-x // 256) * 256
+    row, rows = (dh + 2) * 4, max([min(n, block) for n in many], default=0)
+    parts = up(entries * hkv * 8) + up(tiles * hkv * 8) + up((entries * hkv + 2 * sms) * (4 if mma else 1) * 8 * row)
+    if tiles:
+        parts += up((tiles * hkv + 2 * sms) * -(-rows // 4) * 4 * row)
+    n = C.c_size_t()
+    p = pages(lib, dtype=dtype, head_dim=dh, n_kv_heads=hkv)
+    assert lib.beagle_paged_attn_shared_workspace_bytes(C.byref(p), sum(groups), hq, len(groups), arr(*groups), C.byref(n)) == OK
+    for at in range(P, P + 256, 16):
+        assert up(at) + parts <= at + n.value
