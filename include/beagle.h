@@ -501,7 +501,8 @@ beagle_status beagle_verify_sample(beagle_ctx* ctx, int32_t batch, int32_t gamma
  * of those the ones with exp(d) >= min_p; the first always.  tokens_out_dev int32 [rows]: the smallest id whose cumulative kept weight, in
  * order of id, exceeds u times the kept weight; logp_out_dev fp32 [rows] (nullable): ln of its share of the kept weight (0 without a
  * draw).  Weights are exact to 2^-45 of the largest and sums are integers: results depend on neither timing nor the rest of the batch.  A NaN logit
- * counts as -infinity, a subnormal one as 0; +infinity takes all the weight (shared among several); a row of -infinity alone gives token -1 and logp NaN. */
+ * counts as -infinity, a subnormal one as 0; +infinity takes all the weight (shared among several); a row of -infinity alone gives token -1 and logp NaN.
+ * Waits on the device are bounded; if one ran out, rows that may be undone would have token -1 and logp NaN too, none what was there before. */
 beagle_status beagle_sample(const void* logits_dev, int32_t logits_dtype, int32_t rows, int32_t vocab, int64_t row_stride,
                             const float* temperature_dev, const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev,
                             const float* u_dev, int32_t* tokens_out_dev, float* logp_out_dev, void* stream);

@@ -30,6 +30,7 @@
 #include <math_constants.h>
 
 #include <atomic>
+#include <cstdlib>
 #include <type_traits>
 
 #include "../../include/beagle.h"
@@ -71,6 +72,7 @@ struct SampleArgs {
     long long stride;
     int rows, vocab, slice;              // slice: tokens of a block (a multiple of 8)
     int more;                            // more rows than clusters fit the GPU
+    uint32_t tries;                      // limit of the wait for another row
     const float *temperature, *top_p, *min_p, *u;
     const int32_t* top_k;
     int32_t* tokens;
@@ -80,7 +82,7 @@ struct SampleArgs {
 struct Shared {
     uint4 answer;                        // to the request for another row (first block)
     u64 answer_bar;
-    int next;                            // that row, or -1
+    int next;                            // that row, -1 for none or kNoAnswer
     union {
         u64 entry[kGather];              // the candidates of the row (first block)
         uint32_t codes[2 * kSide];       // bf16: tokens of every code
@@ -299,12 +301,15 @@ __device__ __forceinline__ void ask_for_row(Shared& s) {
     mbar_expect_tx(bar, 16);
     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(&s.answer)), "r"(bar) : "memory");
 }
-// The first block's index of the cluster that was given, or -1 for none.  (The wait is bounded like every other; the answer comes within a
-// microsecond or two.  If it did not, the cluster would end here, and the rows that it was about to be given keep the tokens they had.)
-__device__ __forceinline__ int row_given(Shared& s, int parity) {
+// The first block's index of the cluster that was given, -1 for none, or kNoAnswer: the wait is bounded like every other (the answer comes within a
+// microsecond or two), and if it runs out some row may be done by nobody, it is not known which.  The cluster then marks all of them (sample_kernel).
+constexpr int kNoAnswer = -2;
+__device__ __forceinline__ int row_given(Shared& s, int parity, uint32_t tries) {
     const uint32_t bar = smem_u32(&s.answer_bar);
     bool ok = false;
-    for (uint32_t i = 0; i < kSpinLimit && !ok; ++i) ok = mbar_try_wait(bar, parity);
+    for (uint32_t i = 0; i < tries && !ok; ++i) ok = mbar_try_wait(bar, parity);
+    if (!ok)                             // an answer on its way still lands (bounded): this memory is the block's until then
+        for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(bar, parity); ++i) {}
     uint32_t given = 0, block = 0;
     if (ok)
         asm volatile("{\n.reg .pred p;\n.reg .b128 r;\nld.shared.b128 r, [%2];\n"
@@ -314,10 +319,10 @@ __device__ __forceinline__ int row_given(Shared& s, int parity) {
                      : "r"(smem_u32(&s.answer))
                      : "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // (the next answer is written there)
-    return given ? (int)block : -1;
+    return !ok ? kNoAnswer : given ? (int)block : -1;
 }
 
-// One row; next: the row that the cluster does after it, or -1.  What the blocks read of one another's shared memory stays until the cluster has met in the next row (or at the kernel's end): words that
+// One row; next: the row that the cluster does after it, -1 or kNoAnswer.  What the blocks read of one another's shared memory stays until the cluster has met in the next row (or at the kernel's end): words that
 // are set before that meeting have had a meeting after their last reading.
 template <typename T>
 __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluster_group& cluster, Shared& s, uint8_t* area, int row, int& next, int parity) {
@@ -378,8 +383,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const cg::cluste
         if (lane == 0) { atomicMax(&s.top, hi); atomicMin(&s.least, lo); }
     }
     if (a.more && rank == 0 && t == 0) {
-        const int block = row_given(s, parity);
-        s.next = block >= 0 ? block / C : -1;
+        const int block = row_given(s, parity, a.tries);
+        s.next = block >= 0 ? block / C : block;
     }
     cluster.sync();
     {                                                            // a lane reads a block's word, all in one trip
@@ -1284,12 +1289,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     }
     pdl_launch_dependents();
     pdl_wait();
-    for (int row = blockIdx.x / C, parity = 0, next; row >= 0; row = next, parity ^= 1) {
+    int row = blockIdx.x / C;
+    for (int parity = 0, next; row >= 0; row = next, parity ^= 1) {
         __syncthreads();                                         // (the row before is done with the block's memory)
         if (a.more && threadIdx.x == 0 && cluster.block_rank() == 0) ask_for_row(s);
         sample_row<T>(a, cluster, s, smem + (sizeof(Shared) + 15) / 16 * 16, row, next, parity);
     }
     cluster.sync();                                              // nobody reads a block's memory after it has ended
+    // No row keeps what its places held before the call: a row that was done, by this cluster or by another up to now, counts as undone too.
+    if (row == kNoAnswer && cluster.block_rank() == 0)
+        for (int i = threadIdx.x; i < a.rows; i += kThreads) {
+            a.tokens[i] = -1;
+            if (a.logp != nullptr) a.logp[i] = CUDART_NAN_F;
+        }
 }
 
 constexpr size_t kHalfSm = 113 * 1024 - 128;     // dynamic shared memory of a block that shares its SM with another
@@ -1370,6 +1382,9 @@ extern "C" beagle_status beagle_sample(const void* logits_dev, int32_t logits_dt
         (((uintptr_t)temperature_dev | (uintptr_t)top_k_dev | (uintptr_t)top_p_dev | (uintptr_t)min_p_dev | (uintptr_t)u_dev | (uintptr_t)tokens_out_dev |
           (uintptr_t)logp_out_dev) & 3))
         return BEAGLE_ERR_INVALID_ARG;
-    SampleArgs a{logits_dev, row_stride, rows, vocab, 0, 0, temperature_dev, top_p_dev, min_p_dev, u_dev, top_k_dev, tokens_out_dev, logp_out_dev};
+    SampleArgs a{logits_dev, row_stride, rows, vocab, 0, 0, kSpinLimit, temperature_dev, top_p_dev, min_p_dev, u_dev, top_k_dev, tokens_out_dev, logp_out_dev};
+#ifdef BEAGLE_BOUNDS_CHECK
+    if (const char* tries = getenv("BEAGLE_SAMPLE_TRIES")) a.tries = (uint32_t)strtoul(tries, nullptr, 10);      // (tests of the wait that runs out)
+#endif
     return logits_dtype == BEAGLE_BF16 ? launch_sample<bf16>(a, static_cast<cudaStream_t>(stream)) : launch_sample<float>(a, static_cast<cudaStream_t>(stream));
 }

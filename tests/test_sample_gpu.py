@@ -1,6 +1,9 @@
 """Sampling from given uniform numbers, against the definition in 64 bits."""
 import math
+import os
 import random
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -357,3 +360,37 @@ def test_more_rows_than_fit_the_gpu(dtype):
     z.copy_(z.flip(0))
     graph.replay()
     assert tokens.tolist() == want[::-1]
+
+
+SHORT_WAIT = """
+import os
+import torch
+from paper_2505_24544_b200 import binding as b
+g = torch.Generator(device="cuda").manual_seed(4)
+for dtype, rows, v in ((torch.bfloat16, 700, 33000), (torch.float32, 1000, 5000), (torch.float32, 600, 33000)):
+    z, u = (torch.randn(rows, v, generator=g, device="cuda") * 3).to(dtype), torch.rand(rows, generator=g, device="cuda")
+    want, right = torch.empty(rows, dtype=torch.int32, device="cuda"), torch.empty(rows, device="cuda")
+    b.beagle_sample(z, u, want, logp=right)
+    tokens, logp = torch.full_like(want, 1 << 20), torch.full_like(right, 7.0)
+    os.environ["BEAGLE_SAMPLE_TRIES"] = "0"
+    b.beagle_sample(z, u, tokens, logp=logp)
+    alone = torch.full_like(want, 1 << 20)
+    b.beagle_sample(z, u, alone)
+    del os.environ["BEAGLE_SAMPLE_TRIES"]
+    torch.cuda.synchronize()
+    for t in (tokens, alone):
+        assert bool(((t == want) | (t == -1)).all()) and bool((t == -1).any()), t.tolist()
+    assert bool(((logp == right) | logp.isnan()).all()) and bool(logp.isnan().any())
+    b.beagle_sample(z, u, tokens, logp=logp)
+    assert torch.equal(tokens, want) and torch.equal(logp, right)
+print("no row kept what it had")
+"""
+
+
+def test_a_wait_that_runs_out_leaves_no_old_tokens():
+    """In the build for tests the wait for another row can be given no tries: clusters then end after their first row, and of the rows that
+    nobody does none keeps what was there; the next call is whole again."""
+    from paper_2505_24544_b200 import build
+    env = dict(os.environ, BEAGLE_LIBRARY=build.build(checked=True))
+    r = subprocess.run([sys.executable, "-c", SHORT_WAIT], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), env=env, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0 and "no row kept what it had" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
