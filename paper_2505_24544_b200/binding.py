@@ -555,6 +555,13 @@ def _host_i32(values: Sequence[int]) -> bytes:
     return array("i", values).tobytes()
 
 
+def _in_bits(bits: int, **values: int) -> None:
+    """Refuses whole numbers that a signed argument of so many bits does not hold (ctypes would hand on their low bits)."""
+    for name, x in values.items():
+        if not -1 << (bits - 1) <= x < 1 << (bits - 1):
+            raise ValueError(f"{name}: {x} is beyond {bits} bits")
+
+
 def _check(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], dense: bool = True) -> int:
     """The tensor's address, after checking its type, shape, layout and that it lies on the current device."""
     device = t.get_device()                      # -1: host memory
@@ -753,9 +760,11 @@ class Rotary:
             raise ValueError(f"scaling: one of {', '.join(ROTARY_SCALINGS)}")
         if mscale is not None and not mscale > 0:
             raise ValueError("mscale: above 0")
+        rot_dim = head_dim if rot_dim is None else rot_dim
+        _in_bits(32, head_dim=head_dim, rot_dim=rot_dim)
         self.lib, self.struct = load_library(), BeagleRotary()
         self.ref = C.byref(self.struct)
-        _pages_ok(self.lib.beagle_rotary_make(head_dim, head_dim if rot_dim is None else rot_dim, int(bool(interleaved)), theta, ROTARY_SCALINGS[scaling],
+        _pages_ok(self.lib.beagle_rotary_make(head_dim, rot_dim, int(bool(interleaved)), theta, ROTARY_SCALINGS[scaling],
                                               factor, original, 1.0 if low is None else low, (32.0 if scaling == "ramp" else 4.0) if high is None else high,
                                               0.0 if mscale is None else mscale, self.ref), "beagle_rotary_make")
 
@@ -769,6 +778,9 @@ def beagle_rotary_apply(rot: Rotary, q: torch.Tensor, q_out: torch.Tensor, k: Op
     """Rotates q ([rows, heads, head_dim], float32 / bfloat16, rows may be strided) and, in the same launch, k into q_out and k_out (strided
     rows too; the inputs themselves are fine).  Row r is at ``pos[r]`` (int32), without pos at pos0 + r modulo ``period`` (0: pos0 + r).
     inverse: the transpose, which takes the gradients of the outputs to those of the inputs."""
+    if pos0 or period:
+        _in_bits(32, pos0=pos0)
+        _in_bits(64, period=period)
     if q.dim() != 3 or q.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("q: [rows, heads, head_dim] float32 / bfloat16")
     if (k is None) != (k_out is None):
@@ -798,6 +810,8 @@ def beagle_pages_append_rotary(cache: PagedCache, slots: Sequence[int], rot: Rot
     """``beagle_pages_append`` with every new key rotated at the position that it takes.  q: [len(slots), T, n_q_heads, head_dim], the queries of
     the new rows (rows may be strided), rotated at the key's position + q_offset into q_out (dense; q itself if that is dense); rows from
     n_new on are left as they were."""
+    if q_offset:
+        _in_bits(32, q_offset=q_offset)
     c, B, dt, stream = cache.struct, len(slots), cache.k.dtype, cache.on_current_device()
     device = cache.device_index
     T = k_new.shape[1] if k_new.dim() == 4 else -1

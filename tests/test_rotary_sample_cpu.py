@@ -178,3 +178,19 @@ def test_shared_workspace_has_room_at_any_16_byte_border(lib, dtype, dh, hq, hkv
     assert lib.beagle_paged_attn_shared_workspace_bytes(C.byref(p), sum(groups), hq, len(groups), arr(*groups), C.byref(n)) == OK
     for at in range(P, P + 256, 16):
         assert up(at) + parts <= at + n.value
+
+
+def test_whole_numbers_that_the_interface_cannot_hold_are_refused():
+    """Their low bits would be a position, an offset or a width of their own."""
+    import torch
+    from paper_2505_24544_b200 import binding as b
+    rot, q = b.Rotary(64), torch.zeros(3, 2, 64)
+    for kw in (dict(pos0=2 ** 31), dict(pos0=2 ** 32 + 5), dict(pos0=-2 ** 31 - 1), dict(period=2 ** 63), dict(period=2 ** 64 + 1)):
+        with pytest.raises(ValueError, match=next(iter(kw))):
+            b.beagle_rotary_apply(rot, q, q, **kw)
+    for off in (2 ** 32, 2 ** 32 + 1, -2 ** 32):
+        with pytest.raises(ValueError, match="q_offset"):
+            b.beagle_pages_append_rotary(None, [0], rot, q[None], q[None], q_offset=off)
+    for kw in (dict(head_dim=2 ** 32 + 64), dict(head_dim=64, rot_dim=2 ** 32 + 32)):
+        with pytest.raises(ValueError):
+            b.Rotary(**kw)
