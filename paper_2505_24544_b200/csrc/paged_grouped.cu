@@ -268,12 +268,14 @@ __global__ void __launch_bounds__(kThreads, 2) paged_grouped_kernel(const __grid
         fence_barrier_init();
     }
     if (threadIdx.x == 32 * 3) { prefetch_tensormap(&tmQ); prefetch_tensormap(&tmK); prefetch_tensormap(&tmV); }
+    // Tensor memory is taken after the kernels before have ended and before those behind may begin: a block that waits for its turn holds none that
+    // a block in front of it could still ask for, and nobody behind it can take what it is about to ask for.
+    pdl_wait();
     if (warp == 1) tmem_alloc<kTmem>(smem_u32(&s_tmem));
     fence_before();
-    pdl_launch_dependents();
-    pdl_wait();
     build_schedules(rows, s_rows, prefix, s_prefix);
     fence_after();
+    pdl_launch_dependents();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
     // The CTAs do one kind of work each, shared out by its tiles, the two kinds side by side on an SM as far as possible: one waits for
     // memory, the other for the products.  64 rows over 65536: 146 us; with a common part's tile counted as 0.8, 1.2 and 1.4 of a row's 159, 151, 172.

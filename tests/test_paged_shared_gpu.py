@@ -298,3 +298,48 @@ def test_workspace_at_any_16_byte_border(dtype, hq, hkv, dh, off):
     b.beagle_paged_attn_shared(cache, slots, groups, sh, q, out, ws=buf[off:off + n])
     assert torch.equal(out, ref)
     assert bool((buf[:off] == 0x5a).all()) and bool((buf[off + n:] == 0x5a).all())
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_between_draft_steps_on_the_tensor_cores(dh):
+    """Draft steps and shared attention one behind the other, each begun while the one before still runs, both with tensor memory: what
+    each gives alone, eager and replayed from a graph."""
+    from test_pages_head_gpu import GQA, WL, build, to_dev
+    w = GQA.scaled(batch=20, gamma=3, ctx_max=100)
+    head, _, own = build(w, ps=16)
+    rng = WL.data_rng(w, 5)
+    lengths, slots = [int(n) for n in WL.make_context_lengths(w, rng)], list(range(20))
+    head.prefill_pages(own, slots, lengths, to_dev(WL.make_hidden(w, rng, sum(lengths)), w.dtype))
+    first = to_dev(WL.make_tokens(w, rng, (20,)), w.dtype)
+    cache, shared = forked([20, 5], [900, 300], list(range(25)), 16, 2, dh, "bf16", 13)
+    groups, rows, sh = [20, 5], list(range(25)), i32(shared).cuda()
+    qs = [randn(25, 8, dh, dtype="bf16", seed=s) for s in (1, 2, 3)]
+    want = [attend(cache, rows, groups, sh, q, "bf16") for q in qs]
+    keep = own.length.clone()
+
+    def chain(draft, outs):
+        keep.copy_(own.length)
+        for s in range(w.gamma):
+            b.beagle_draft_step_pages(head.ctx, own, slots, first if s == 0 else None, True, draft[:, s])
+            if outs is not None:
+                b.beagle_paged_attn_shared(cache, rows, groups, sh, qs[s], outs[s])
+        b.beagle_pages_truncate(own, slots, keep)
+
+    alone, both = (torch.zeros(20, w.gamma, dtype=torch.int32, device="cuda") for _ in range(2))
+    outs = [torch.empty_like(q) for q in qs]
+    chain(alone, None)
+    head.rollback(slots)
+    chain(both, outs)
+    torch.cuda.synchronize()
+    assert torch.equal(alone, both) and all(torch.equal(x, y) for x, y in zip(outs, want))
+    head.rollback(slots)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain(both, outs)
+    for _ in range(20):
+        both.zero_()
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(alone, both) and all(torch.equal(x, y) for x, y in zip(outs, want))
