@@ -343,3 +343,17 @@ def test_between_draft_steps_on_the_tensor_cores(dh):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(alone, both) and all(torch.equal(x, y) for x, y in zip(outs, want))
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dh", KINDS)
+@pytest.mark.parametrize("ps", [8, 64, 256])
+def test_one_row_at_a_time_over_forked_slots(dtype, hq, hkv, dh, ps):
+    """The attention of rows on their own over the same kind of cache, pages in several slots at once and NaN behind every length."""
+    groups, prefix = [1, 5, 2, 20, 9], [70, 0, 64, 700, 1024]
+    r = random.Random(ps + 1)
+    cache, _ = forked(groups, prefix, [r.choice([0, 1, 5, 63, 64, 65, 130]) for _ in range(sum(groups))], ps, hkv, dh, dtype, 14)
+    slots = r.sample(range(sum(groups)), sum(groups))
+    q = (randn(len(slots), hq, dh, dtype=dtype, seed=9) * 2).to(DT[dtype])
+    out, lse = torch.full_like(q, 9.0), torch.full(q.shape[:2], 9.0, device="cuda")
+    b.beagle_paged_attn(cache, slots, q, out, lse=lse)
+    check_attn(cache, slots, q, 0, 0, dtype, out, lse)
