@@ -273,7 +273,7 @@ typedef struct beagle_rotary {
     int32_t rot_dim;      /* even, 2..head_dim                                                     */
     int32_t interleaved;
     int32_t reserved;
-    double  mscale;
+    double  mscale;       /* finite in fp32 too */
     double  freq[BEAGLE_ROTARY_MAX_PAIRS];      /* radians per position */
 } beagle_rotary;
 

@@ -8,6 +8,7 @@
 // Measured: 8 x 2048 positions, 32 + 32 heads of 128, bf16, forward and backward (1.07 GB): 174 us, 6.1 TB/s; 8191 positions, 32 + 8 heads,
 // interleaved, a quarter rotated (168 MB): 37 us.  One head at a time in a thread and six CTAs per SM; four heads in flight in two
 // CTAs per SM took 240 and 53, entries formed by every thread for itself, without shared memory, 179 and 47.
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 
@@ -64,10 +65,13 @@ __global__ void __launch_bounds__(kRotThreads, kRotCtas) rotary_kernel(const __g
 
 }  // namespace
 
+// (the kernels multiply by it in fp32: an infinite factor would make NaN of every 0)
+static bool finite_in_fp32(double x) { return std::fabs(x) <= FLT_MAX; }
+
 beagle_status rotary_check(const beagle_rotary* r, int dtype) {
     if (r == nullptr || (dtype != BEAGLE_FP32 && dtype != BEAGLE_BF16)) return BEAGLE_ERR_INVALID_ARG;
     const int full = dtype == BEAGLE_BF16 ? 8 : 4;
-    if (r->head_dim <= 0 || r->rot_dim <= 0 || (r->interleaved != 0 && r->interleaved != 1) || !std::isfinite(r->mscale)) return BEAGLE_ERR_INVALID_ARG;
+    if (r->head_dim <= 0 || r->rot_dim <= 0 || (r->interleaved != 0 && r->interleaved != 1) || !finite_in_fp32(r->mscale)) return BEAGLE_ERR_INVALID_ARG;
     if (r->head_dim > 2 * BEAGLE_ROTARY_MAX_PAIRS || r->head_dim % full || r->rot_dim % 2 || r->rot_dim > r->head_dim) return BEAGLE_ERR_SHAPE;
     for (int i = 0; i < r->rot_dim / 2; ++i)
         if (!std::isfinite(r->freq[i])) return BEAGLE_ERR_INVALID_ARG;
@@ -115,7 +119,7 @@ beagle_status beagle_rotary_make(int32_t head_dim, int32_t rot_dim, int32_t inte
                                  double low, double high, double mscale, beagle_rotary* out) {
     if (out == nullptr || head_dim <= 0 || rot_dim <= 0 || (interleaved != 0 && interleaved != 1)) return BEAGLE_ERR_INVALID_ARG;
     if (head_dim > 2 * BEAGLE_ROTARY_MAX_PAIRS || rot_dim > head_dim || rot_dim % 2) return BEAGLE_ERR_SHAPE;
-    if (!std::isfinite(theta) || !(theta > 1.0) || !std::isfinite(mscale) || mscale < 0.0) return BEAGLE_ERR_INVALID_ARG;
+    if (!std::isfinite(theta) || !(theta > 1.0) || !finite_in_fp32(mscale) || mscale < 0.0) return BEAGLE_ERR_INVALID_ARG;
     if (scaling < BEAGLE_ROTARY_NONE || scaling > BEAGLE_ROTARY_RAMP) return BEAGLE_ERR_INVALID_ARG;
     if (scaling != BEAGLE_ROTARY_NONE && (!std::isfinite(factor) || !(factor >= 1.0))) return BEAGLE_ERR_INVALID_ARG;
     const bool by_turns = scaling == BEAGLE_ROTARY_BANDS || scaling == BEAGLE_ROTARY_RAMP;

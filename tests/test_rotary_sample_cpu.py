@@ -194,3 +194,16 @@ def test_whole_numbers_that_the_interface_cannot_hold_are_refused():
     for kw in (dict(head_dim=2 ** 32 + 64), dict(head_dim=64, rot_dim=2 ** 32 + 32)):
         with pytest.raises(ValueError):
             b.Rotary(**kw)
+
+
+@pytest.mark.parametrize("mscale", [1e39, -1e39, 1.7e308])
+def test_a_factor_beyond_fp32_is_refused(lib, mscale):
+    """The kernels multiply by it in fp32: it would be infinite, and NaN times 0."""
+    assert mscale < 0 or rotary(lib, mscale=mscale)[0] == INVALID
+    _, r = rotary(lib)
+    r.mscale = mscale
+    assert lib.beagle_rotary_apply(C.byref(r), 1, 0, None, 0, 0, 0, None, 0, None, 0, 1, None, 64, None, 64, 0, None) == INVALID
+    p = pages(lib)
+    assert lib.beagle_pages_append_rotary(C.byref(p), C.byref(r), 0, None, 0, None, None, 0, None, 0, 0, None, 0, None, 0, None, None) == INVALID
+    r.mscale = 3e38
+    assert lib.beagle_pages_append_rotary(C.byref(p), C.byref(r), 0, None, 0, None, None, 0, None, 0, 0, None, 0, None, 0, None, None) == OK
