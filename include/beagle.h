@@ -377,8 +377,9 @@ beagle_status beagle_paged_attn(const beagle_pages* pages, int32_t batch, const 
                                 int64_t q_stride, int32_t window, int32_t sinks, void* out_dev, float* lse_dev, void* ws_dev,
                                 size_t ws_bytes, void* stream);
 
-/* beagle_paged_attn for rows whose slots begin with the same positions (forks of one prompt): the common part is read once for all
- * rows of a group.  The rows of the call come in n_groups groups, group i being the next group_rows_host[i] >= 1 of them.
+/* beagle_paged_attn for rows whose slots begin with the same positions (forks of one prompt): the common part is read once for many rows of
+ * a group instead of once a row: per 128 query rows (rows times grouped heads; bf16, head_dim 64 / 128, groups of more than 8 of them), else per 8 (per 4
+ * at bf16 head_dim 256).  The rows of the call come in n_groups groups, group i being the next group_rows_host[i] >= 1 of them.
  * shared_dev int32 [n_groups]: the first so many positions hold the same keys and values in every slot of the group; they are read
  * through the group's first slot.  Clamped to 0 and the shortest length of the group.  What lies behind them is read row by row, so
  * any smaller number gives the same attention.  Everything visible (no window).  Other arguments and results as beagle_paged_attn (results

@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
     }
 }
 
-// Warps of a head in the join, and partials that each has in flight.  Calls of 32 rows over 8192 / four groups of 16 over 4096, us: 4 and 4 28.9 / 81, 8 and 4
+// Warps of a head in the join, and partials that each has in flight.  Calls of 32 rows over 8192 / four groups of 16 over 2094 to 3511, us: 4 and 4 28.9 / 81, 8 and 4
 // 30.4 / 85, 4 and 8 29.2 / 83, 8 and 8 34 / 91, 4 and 2 30.6 / 80, 2 and 4 31.8 / 81.
 constexpr int kSharedJoinWarps = 4;
 constexpr int kJoinFlight = 4;
@@ -588,6 +588,7 @@ __global__ void __launch_bounds__(2 * kSharedJoinWarps * 32) paged_shared_join_k
 }
 
 // beagle_pages_shared: blockIdx.x = group.  The first page at which the table rows of its slots differ or the shortest of them ends.
+// Bound by latency: row after row, a trip to L2 each (32 rows of 128 pages 9 us, 64 rows of 1024 53, 127 after a flush).
 __global__ void __launch_bounds__(256) pages_shared_kernel(const int32_t* table, const int32_t* length, const __grid_constant__ PageSlots slots,
                                                          const __grid_constant__ PageSlots first_row, const __grid_constant__ PageSlots n_rows, int page_size,
                                                          int max_pages, int32_t* shared) {

@@ -1,17 +1,18 @@
 // Attention of groups of rows whose slots begin with the same positions (beagle_paged_attn_shared) where the groups are large enough for the
 // tensor cores: one launch for the common parts, on tcgen05, and for what each row has behind them (paged_rows.cuh, mma.sync).
 //
-// Common part: the query rows of a group (rows times grouped heads) that read one K/V head are the 128 rows of a tcgen05 tile, so each
-// cached tile is read once for all of them: R G flop per byte, memory-bound up to some 200 query rows, then bound by the softmax between the products.
+// Common part: up to 128 query rows of a group (rows times grouped heads) that read one K/V head are the rows of a tcgen05 tile, so each
+// cached tile is read once for all of them: R G flop per byte.  More than 128 of them are blocks of their own, each of which reads every tile; from
+// DRAM the tiles still come once (64 rows of four grouped heads over 65536 positions: 544 MB read, 534 of cache), the second time from L2.
 // The tiles of 64 positions of all (block of query rows, K/V head) pairs, one after the other, are cut into equal runs on the device
 // (paged_attn.cuh); a run leaves one partial per pair that it touches (O in fp32, not normalised, with the maximum and sum of each row),
 // which the join launch adds to what the rows see behind the common part, in a fixed order.
 //
 // Two CTAs per SM, each with one kind of work, shared out by the tiles, the kinds side by side as far as possible: common parts wait
 // for the hand-over between softmax and products, rows for memory.  Measured: 32 rows over 8192 common positions, 32/8 heads of 128, some hundred
-// positions behind: 29 us with the join, of which the join takes 9 (the two kinds in launches of their own: 48, in one 41, at that time); four groups of 16 rows, 32/32 heads: 81 us; 64 rows over
-// 65536, up to 8192 behind: 146 us (all CTAs first one kind, then the other: 167); alone the common parts run at 207 tiles a microsecond
-// (868 TFLOP/s with 128 query rows, half of the tensor cores' rate) and the rows at 5.8 TB/s.
+// positions behind: 28 us with the join, of which the join takes 9 (the two kinds in launches of their own: 48, in one 41, at that time); four groups of 16 rows over
+// 2094 to 3511, 32/32 heads: 81 us; 64 rows over 65536, 100 to 2048 behind: 146 us, tensor pipe 0.43 busy (all CTAs first one kind, then the other: 167); alone the
+// common parts run at 207 tiles a microsecond (868 TFLOP/s with 128 query rows, half of the tensor cores' rate) and the rows at 5.8 TB/s.
 //
 // A common part's CTA: a producer warp (pages by TMA, 128-byte swizzle, two stages of K and V; the queries of the block as one box of a
 // [row, head, component] map), a warp that issues the products, and four warps with one thread per query row: S = Q K^T into tensor memory ->

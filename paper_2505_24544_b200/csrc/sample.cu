@@ -24,8 +24,9 @@
 //
 // Bound by latency: a row is a chain of some ten short passes with a meeting of the cluster after most (a microsecond each, with the words read
 // from the other blocks), 20 to 30 us from end to end; two blocks share an SM, so 71 rows of 128256 bf16 logits are under way at a time.  Measured,
-// 448 such rows (115 MB): temperature alone 166 us (weights from the table: half of a row's time), top-k of 50 119, top-p 225, min-p 113, mixed
-// filters 172; one row of 32000 fp32 logits with top-k 12 us with the call, of 128256 bf16 ones with top-p 29.
+// 448 such rows (115 MB): temperature alone 164 us (weights from the table: half of a row's time), top-k of 50 121, top-p of 0.9 224, min-p of 0.05 94, mixed
+// filters 169; the same in fp32 (230 MB) 229, 258, 500 and 168; one row of 32000 fp32 logits with top-k 12 us with the call, of 128256 bf16 ones with top-p
+// 31 after a flush, 22 in a row.
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
